@@ -41,8 +41,14 @@ typedef enum gk_status {
     GK_ERR_CUDA = -6,      /* a CUDA runtime call failed (see gk_last_cuda_error) */
     GK_ERR_NOMEM = -7,     /* workspace allocation failed */
     GK_ERR_CAPACITY = -8,  /* gk_set_capacity: cap < 0 */
-    GK_ERR_LIMIT = -9      /* size beyond a fixed built-in limit */
+    GK_ERR_LIMIT = -9,     /* size beyond a fixed built-in limit */
+    GK_ERR_TYPE = -10,     /* gk_vocab_*: not one of the element types the call takes */
+    GK_ERR_STRIDE = -11,   /* gk_vocab_*: a row stride shorter than the row */
+    GK_ERR_TEMPERATURE = -12 /* gk_vocab_*: temperature not positive and finite */
 } gk_status;
+
+/* Element types of the gk_vocab_* calls. */
+typedef enum gk_type { GK_TYPE_F32 = 0, GK_TYPE_BF16 = 1, GK_TYPE_F16 = 2 } gk_type;
 
 /* Values of gk_stats.status (bit flags, written by the device). */
 #define GK_DEV_OK 0
@@ -308,6 +314,96 @@ int gk_sparsify_static(const float* g, float* eps, int64_t d, int64_t k, int32_t
  * the current device.  Returns GK_ERR_SIZE for max_rounds outside 1 .. 4.
  */
 int gk_set_params(int unbiased_std, int max_rounds);
+
+/*
+ * gk_vocab_loss -- softmax cross entropy at the vocabulary head of a language model, and its
+ * gradient: the loss whose gradient the sparsifiers above compress (the paper's LSTM workload
+ * has such a head; the paper does not treat it).  With z = h w^T, without keeping z,
+ *     lse_n = log sum_v exp z_nv;   loss_n = lse_n - z_n,t(n);
+ *     dz_nv = g_n (exp(z_nv - lse_n) - [v = t(n)]);   dh = dz w;   dw = dz^T h.
+ * Products of 16-bit operands are summed in fp32, lse and loss are fp32; dz is rounded to the
+ * operands' type before the products dh and dw, which are rounded once more at the end.
+ *
+ *   h          DEVICE in   n rows of D elements of `dtype`, row stride ldh >= D (in elements)
+ *   w          DEVICE in   V rows of D elements, row stride ldw >= D.  Rows that start on 16-byte
+ *                          boundaries are read in place; otherwise the call copies w first.
+ *   dtype      GK_TYPE_BF16 or GK_TYPE_F16, of h, w, dh and dw
+ *   n, D, V    0 <= n <= 2^22, 1 <= D <= 2^16, 1 <= V <= 2^26
+ *   target     DEVICE in   n int64 classes.  A row whose target is ignore_index, or outside
+ *                          [0, V), is left out: loss 0, lse 0, a zero row in dh, no share in dw,
+ *                          whatever h holds there (its infinities and NaN included), and no work.
+ *   row_grad   DEVICE in   g: n floats, the gradient of each row's loss; NULL: 1 / rows that
+ *                          count, the gradient of their mean
+ *   loss_out, lse_out      DEVICE out  n floats each
+ *   dh_out     DEVICE out  n rows of D, row stride lddh; NULL: not wanted
+ *   dw_out     DEVICE out  V rows of D, row stride lddw; NULL: not wanted
+ * With neither dh nor dw only the forward pass runs (scoring).  dh and dw must not overlap h, w or
+ * each other.  Results do not depend on timing: no atomics on floating-point data.
+ *
+ * The workspace is the call's own, per (device, stream), grown on first use (gk_vocab_reserve
+ * does that ahead; a call that fits allocates nothing and can be captured in a graph).  The
+ * largest part is one piece of the vocabulary as n rows of 16-bit values, bounded by
+ * gk_vocab_set_budget; a vocabulary that does not fit one piece costs the product h w^T twice.
+ */
+int gk_vocab_loss(const void* h, int64_t ldh, const void* w, int64_t ldw, int32_t dtype, int64_t n, int64_t D,
+                  int64_t V, const int64_t* target, int64_t ignore_index, const float* row_grad, float* loss_out,
+                  float* lse_out, void* dh_out, int64_t lddh, void* dw_out, int64_t lddw, gk_stream_t stream);
+
+/*
+ * gk_vocab_distill -- distillation from a teacher's top logits through the same head: each row
+ * has K pairs (index, logit) of the teacher, as gk_vocab_topk writes them.  With temperature T,
+ *     q_nj = exp(t_nj / T - L_n),  L_n = t_lse[n], or log sum_j exp(t_nj / T) where t_lse is NULL;
+ *     lse_n = log sum_v exp(z_nv / T);
+ *     loss_n = sum_j q_nj (log q_nj - z_n,i(n,j) / T + lse_n);
+ *     dz_nv = (g_n / T) (exp(z_nv / T - lse_n) sum_j q_nj - sum_{j: i(n,j) = v} q_nj).
+ *
+ *   t_idx      DEVICE in   n x K int32 (contiguous), in any order; an index given twice counts
+ *                          twice.  Pairs with an index outside [0, V) or a logit of -inf are left
+ *                          out (rows with fewer pairs are filled up with -1); a row without any
+ *                          pair is left out as in gk_vocab_loss.
+ *   t_val      DEVICE in   n x K floats, the teacher's logits (not divided by T)
+ *   K          1 <= K <= 1024
+ *   t_lse      DEVICE in   n floats, the teacher's log-sum-exp at T over its whole vocabulary
+ *                          (gk_vocab_topk's lse_out): q is then the teacher's probability and
+ *                          sums to at most 1.  NULL: q is normalised over the K pairs.
+ *   temperature  T > 0
+ * The other arguments as for gk_vocab_loss.
+ */
+int gk_vocab_distill(const void* h, int64_t ldh, const void* w, int64_t ldw, int32_t dtype, int64_t n, int64_t D,
+                     int64_t V, const int32_t* t_idx, const float* t_val, int32_t K, const float* t_lse,
+                     float temperature, const float* row_grad, float* loss_out, float* lse_out, void* dh_out,
+                     int64_t lddh, void* dw_out, int64_t lddw, gk_stream_t stream);
+
+/*
+ * gk_vocab_topk -- the k largest logits of each row as a message for gk_vocab_distill, in the form
+ * of topk_exact's: exactly k pairs a row in ascending index order, equal values taken in order of
+ * increasing index (+0 and -0 tie, NaN counts as above +inf).  Values here are compared as
+ * they are, not by magnitude.
+ *
+ *   logits     DEVICE in   n rows of V elements of `dtype` (GK_TYPE_F32, _BF16 or _F16), row stride ld >= V
+ *   n, V, k    n >= 0, 1 <= V <= 2^31 - 1, 1 <= k <= min(V, 1024)
+ *   temperature  T > 0, for lse_out only
+ *   idx_out    DEVICE out  n x k int32;   val_out  DEVICE out  n x k floats
+ *   lse_out    DEVICE out  n floats, log sum_v exp(logit / T); -inf for a row of nothing but
+ *                          -inf.  NULL: not wanted
+ */
+int gk_vocab_topk(const void* logits, int64_t ld, int32_t dtype, int64_t n, int64_t V, int32_t k, float temperature,
+                  int32_t* idx_out, float* val_out, float* lse_out, gk_stream_t stream);
+
+/* Bytes that one piece of the vocabulary may take in the workspace of gk_vocab_loss and
+ * gk_vocab_distill (default 2 GiB).  A piece has at least 256 columns.  Process-wide; returns
+ * GK_ERR_CAPACITY if bytes < 0. */
+int gk_vocab_set_budget(int64_t bytes);
+
+/* Create (or grow) the workspace of (current device, stream) for gk_vocab_loss (K = 1) and
+ * gk_vocab_distill calls of these sizes at the present budget, with or without gradients, with
+ * rows of w on 16-byte boundaries if D is a multiple of 8.  Synchronous. */
+int gk_vocab_reserve(int64_t n, int64_t D, int64_t V, int32_t K, int grad, gk_stream_t stream);
+int64_t gk_vocab_workspace_bytes(int64_t n, int64_t D, int64_t V, int32_t K, int grad);
+
+/* Synchronise `stream` and write to HOST host_out[0..1] of the last gk_vocab_loss or
+ * gk_vocab_distill call on it: GK_DEV_* flags, rows that counted. */
+int gk_vocab_last_info(gk_stream_t stream, int64_t* host_out);
 
 /* Output capacity of idx_out / val_out for the sparsify calls, in pairs.
  * 0 (the default) means "d".  Process-wide; returns GK_ERR_CAPACITY if cap < 0. */

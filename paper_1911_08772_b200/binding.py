@@ -27,6 +27,8 @@ EXPORTS = [
     "gk_stage_timing", "gk_last_stage_ms", "gk_last_cta_trace", "gk_launch_count", "gk_strerror", "gk_last_cuda_error", "gk_version",
     "gk_error_ratio", "dgck_select", "dgck_sparsify", "dgck_last_info",
     "gk_apply_sparse", "gk_apply_gathered", "gk_histogram", "gk_debug_set", "gk_last_path_info", "gk_select", "gk_set_params",
+    "gk_vocab_loss", "gk_vocab_distill", "gk_vocab_topk", "gk_vocab_set_budget", "gk_vocab_reserve",
+    "gk_vocab_workspace_bytes", "gk_vocab_last_info",
 ]
 
 
@@ -123,6 +125,22 @@ def load() -> C.CDLL:
     L.gk_set_params.restype = C.c_int
     L.gk_debug_set.argtypes = [C.c_int, i64]
     L.gk_debug_set.restype = C.c_int
+    head = [vp, i64, vp, i64, i32, i64, i64, i64]
+    grads = [vp, vp, vp, vp, i64, vp, i64, vp]
+    L.gk_vocab_loss.argtypes = head + [vp, i64] + grads
+    L.gk_vocab_loss.restype = C.c_int
+    L.gk_vocab_distill.argtypes = head + [vp, vp, i32, vp, C.c_float] + grads
+    L.gk_vocab_distill.restype = C.c_int
+    L.gk_vocab_topk.argtypes = [vp, i64, i32, i64, i64, i32, C.c_float, vp, vp, vp, vp]
+    L.gk_vocab_topk.restype = C.c_int
+    L.gk_vocab_set_budget.argtypes = [i64]
+    L.gk_vocab_set_budget.restype = C.c_int
+    L.gk_vocab_reserve.argtypes = [i64, i64, i64, i32, C.c_int, vp]
+    L.gk_vocab_reserve.restype = C.c_int
+    L.gk_vocab_workspace_bytes.argtypes = [i64, i64, i64, i32, C.c_int]
+    L.gk_vocab_workspace_bytes.restype = i64
+    L.gk_vocab_last_info.argtypes = [vp, C.POINTER(i64)]
+    L.gk_vocab_last_info.restype = C.c_int
     for name in ("gk_sparsify", "gk_sparsify_segmented", "topk_exact", "topk_sparsify", "gk_sparsify_host",
                  "gk_set_capacity", "gk_set_path", "gk_reserve", "gk_last_stats", "gk_last_segment_stats", "gk_version"):
         getattr(L, name).restype = C.c_int
@@ -276,6 +294,119 @@ def gk_sparsify_host(g, eps, k: int, idx_out, val_out):
     _check(load().gk_sparsify_host(ptr(g), ptr(eps), d, k, ptr(idx_out), ptr(val_out),
                                    C.addressof(nnz), C.byref(st)))
     return int(nnz.value), Stats.of(st)
+
+
+def _type(dtype) -> int:
+    import torch
+    code = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}.get(dtype)
+    if code is None:
+        raise GkError(f"element type {dtype} is not one of float32, bfloat16, float16")
+    return code
+
+
+def _rows(t, dtype, rows=None, cols=None, name="tensor"):
+    """(pointer, row stride) of a 2-D CUDA tensor whose rows are contiguous, on the current device."""
+    import torch
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise GkError(f"{name}: expected a CUDA tensor")
+    if t.dim() != 2 or t.dtype != dtype:
+        raise GkError(f"{name}: expected a 2-D {dtype} tensor, got {t.dim()}-D {t.dtype}")
+    if t.device.index != torch.cuda.current_device():
+        raise GkError(f"{name} is not on the current device")
+    if (rows is not None and t.shape[0] != rows) or (cols is not None and t.shape[1] != cols):
+        raise GkError(f"{name}: expected shape ({rows}, {cols}), got {tuple(t.shape)}")
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise GkError(f"{name}: the elements of a row must be contiguous")
+    # the stride of a lone row says nothing
+    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else t.shape[1])
+
+
+def _vec(t, dtype, shape, name):
+    import torch
+    p = _dev(t, dtype)
+    if tuple(t.shape) != tuple(shape):
+        raise GkError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.device.index != torch.cuda.current_device():
+        raise GkError(f"{name} is not on the current device")
+    return p
+
+
+def _head(h, w, loss_out, lse_out, row_grad, dh, dw):
+    """The arguments that the two losses share: (before the targets, after them)."""
+    import torch
+    if not isinstance(h, torch.Tensor) or h.dim() != 2 or not isinstance(w, torch.Tensor) or w.dim() != 2:
+        raise GkError("h and w must be 2-D CUDA tensors")
+    n, D = h.shape
+    V = w.shape[0]
+    hp, ldh = _rows(h, h.dtype, name="h")
+    wp, ldw = _rows(w, h.dtype, cols=D, name="w")
+    dhp, lddh = (None, D) if dh is None else _rows(dh, h.dtype, n, D, "dh")
+    dwp, lddw = (None, D) if dw is None else _rows(dw, h.dtype, V, D, "dw")
+    return ([hp, ldh, wp, ldw, _type(h.dtype), n, D, V],
+            [None if row_grad is None else _vec(row_grad, torch.float32, (n,), "row_grad"),
+             _vec(loss_out, torch.float32, (n,), "loss_out"), _vec(lse_out, torch.float32, (n,), "lse_out"),
+             dhp, lddh, dwp, lddw, _stream()])
+
+
+def gk_vocab_loss(h, w, target, loss_out, lse_out, row_grad=None, dh=None, dw=None, ignore_index: int = -100) -> None:
+    """Softmax cross entropy of z = h w^T without keeping z, per row, and its gradients dh and dw
+    where they are given (see gk.h).  h (n, D), w (V, D), dh, dw: bfloat16 or float16, row strides
+    allowed; target (n,) int64; loss_out, lse_out (n,) float32; row_grad (n,) float32 or None for
+    the gradient of the mean over the rows that count."""
+    import torch
+    before, after = _head(h, w, loss_out, lse_out, row_grad, dh, dw)
+    _check(load().gk_vocab_loss(*before, _vec(target, torch.int64, (h.shape[0],), "target"), ignore_index, *after))
+
+
+def gk_vocab_distill(h, w, t_idx, t_val, loss_out, lse_out, t_lse=None, temperature: float = 1.0, row_grad=None,
+                     dh=None, dw=None) -> None:
+    """Distillation from a teacher's top logits t_idx (n, K) int32, t_val (n, K) float32 through
+    z = h w^T (see gk.h); t_lse (n,): the teacher's log-sum-exp at this temperature, None to
+    normalise over the K pairs.  The other arguments as for gk_vocab_loss."""
+    import torch
+    before, after = _head(h, w, loss_out, lse_out, row_grad, dh, dw)
+    n = h.shape[0]
+    if not isinstance(t_idx, torch.Tensor) or t_idx.dim() != 2:
+        raise GkError("t_idx must be a 2-D CUDA tensor")
+    K = t_idx.shape[1]
+    _check(load().gk_vocab_distill(*before, _vec(t_idx, torch.int32, (n, K), "t_idx"), _vec(t_val, torch.float32, (n, K), "t_val"),
+                                   K, None if t_lse is None else _vec(t_lse, torch.float32, (n,), "t_lse"),
+                                   temperature, *after))
+
+
+def gk_vocab_topk(logits, k: int, idx_out, val_out, lse_out=None, temperature: float = 1.0) -> None:
+    """The k largest logits of each row in ascending index order, and the row's log-sum-exp at this
+    temperature (see gk.h).  logits (n, V): float32, bfloat16 or float16, row stride allowed;
+    idx_out (n, k) int32, val_out (n, k) float32, lse_out (n,) float32 or None."""
+    import torch
+    if not isinstance(logits, torch.Tensor) or logits.dim() != 2:
+        raise GkError("logits must be a 2-D CUDA tensor")
+    n, V = logits.shape
+    p, ld = _rows(logits, logits.dtype, name="logits")
+    _check(load().gk_vocab_topk(p, ld, _type(logits.dtype), n, V, k, temperature, _vec(idx_out, torch.int32, (n, k), "idx_out"),
+                                _vec(val_out, torch.float32, (n, k), "val_out"),
+                                None if lse_out is None else _vec(lse_out, torch.float32, (n,), "lse_out"), _stream()))
+
+
+def gk_vocab_set_budget(nbytes: int) -> None:
+    """Bytes that one piece of the vocabulary may take in the workspace of the two losses."""
+    _check(load().gk_vocab_set_budget(nbytes))
+
+
+def gk_vocab_reserve(n: int, D: int, V: int, K: int = 1, grad: bool = True) -> None:
+    _check(load().gk_vocab_reserve(n, D, V, K, int(grad), _stream()))
+
+
+def gk_vocab_workspace_bytes(n: int, D: int, V: int, K: int = 1, grad: bool = True) -> int:
+    return int(load().gk_vocab_workspace_bytes(n, D, V, K, int(grad)))
+
+
+def gk_vocab_last_info():
+    """(GK_DEV_* flags, rows that counted) of the last gk_vocab_loss or gk_vocab_distill call on the
+    current stream.  Synchronises the stream."""
+    out = (C.c_int64 * 2)()
+    _check(load().gk_vocab_last_info(_stream(), out))
+    return int(out[0]), int(out[1])
 
 
 def gk_set_capacity(cap: int) -> None:

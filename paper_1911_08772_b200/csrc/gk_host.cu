@@ -305,6 +305,9 @@ extern "C" const char* gk_strerror(int code) {
         case GK_ERR_NOMEM: return "could not allocate the scratch workspace";
         case GK_ERR_CAPACITY: return "capacity must be >= 0";
         case GK_ERR_LIMIT: return "size beyond a built-in limit";
+        case GK_ERR_TYPE: return "element type not taken by this call";
+        case GK_ERR_STRIDE: return "row stride shorter than the row";
+        case GK_ERR_TEMPERATURE: return "temperature must be positive and finite";
         default: return "unknown gk_status";
     }
 }

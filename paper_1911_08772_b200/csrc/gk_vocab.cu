@@ -1,0 +1,596 @@
+// The vocabulary head: softmax cross entropy and distillation from a teacher's top logits through
+// z = h w^T, without keeping the logits, with their gradients (include/gk.h: gk_vocab_loss,
+// gk_vocab_distill).  This file: the entry points, the workspace and the passes between the
+// products; the products themselves are in gk_vocab_gemm.cu.
+//
+// With T the temperature, lse_n = log sum_v exp(z_nv / T), p_nv = exp(z_nv / T - lse_n):
+//     loss_n = sum_j q_nj (log q_nj - z_n,i(n,j) / T + lse_n)      (q = 1 at the class: lse_n - z_n,t)
+//     dz_nv  = (g_n / T) (Q_n p_nv - sum_{j: i(n,j) = v} q_nj),     Q_n = sum_j q_nj
+//     dh = dz w,   dw = dz^T h.
+//
+// One call:
+//   1. (distill) the teacher's probabilities; the rows that count, numbered in their order;
+//   2. those rows of h copied together, and the logits at the targets as K dot products a row;
+//   3. logits tile by tile: the tile's maximum and sum, and exp(z / T - maximum) in 16 bits for the
+//      first piece of the vocabulary (all of it where the budget allows);
+//   4. the row's log-sum-exp from the tiles, loss;
+//   5. per piece: logit gradients in 16 bits (from the kept exponentials, or from the product
+//      taken again), then dw and dh as products with them.
+// Kept between the steps is one piece, whose size the budget bounds whatever n and V are.  The
+// exponentials are kept relative to their tile's maximum: 16 bits then hold each with a relative
+// error of 2^-9 (bf16) or 2^-12 (fp16), which a logit rounded to 16 bits would not give.
+#include <atomic>
+#include <map>
+#include <mutex>
+#include <utility>
+
+#include "gk_vocab.cuh"
+
+namespace gk {
+
+constexpr float kLn2 = 0.69314718055994531f;
+constexpr double kLog2e = 1.4426950408889634;
+
+__device__ __forceinline__ float warp_sum_f(float v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+__device__ __forceinline__ float warp_max_f(float v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+    return v;
+}
+
+// ---------------------------------------------------------------------------
+// 1. Teacher probabilities, one warp a row.
+// ---------------------------------------------------------------------------
+__global__ void __launch_bounds__(256) k_vocab_teacher(VocabCall c) {
+    const int64_t r = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    const int lane = threadIdx.x & 31;
+    if (r >= c.n) return;
+    const int32_t* ti = c.t_idx + r * c.K;
+    const float* tv = c.t_val + r * c.K;
+    // the largest logit is taken off before the division by T, so that masks of the type's lowest
+    // value do not overflow; with the teacher's own log-sum-exp there is nothing to take off
+    float top = -INFINITY;
+    bool any = false, ascending = true;
+    for (int j = lane; j < c.K; j += 32) {
+        const int32_t i = ti[j];
+        const float t = tv[j];
+        if (i >= 0 && i < c.V && t != -INFINITY) { any = true; top = fmaxf(top, t); }
+        if (j > 0 && ti[j - 1] >= i) ascending = false;
+    }
+    any = __any_sync(0xffffffffu, any);
+    ascending = __all_sync(0xffffffffu, ascending);
+    float L;
+    if (c.t_lse) {
+        L = c.t_lse[r];
+        top = 0.f;
+    } else {
+        top = warp_max_f(top);
+        float s = 0.f;
+        for (int j = lane; j < c.K; j += 32)
+            if (ti[j] >= 0 && ti[j] < c.V && tv[j] != -INFINITY) s += expf((tv[j] - top) * c.inv_T);
+        L = logf(warp_sum_f(s));
+    }
+    float Q = 0.f;
+    for (int j = lane; j < c.K; j += 32) {
+        const bool on = ti[j] >= 0 && ti[j] < c.V && tv[j] != -INFINITY;
+        const float q = on ? expf((tv[j] - top) * c.inv_T - L) : 0.f;
+        c.q[r * c.K + j] = q;
+        Q += q;
+    }
+    Q = warp_sum_f(Q);
+    if (lane == 0) c.teacher[r] = make_float4(Q, L, top, (ascending ? 1.f : 0.f) + (any ? 2.f : 0.f));
+}
+
+// ---------------------------------------------------------------------------
+// The rows that count, numbered in their order by one CTA; the power of two that brings the
+// gradients' largest row coefficient to [1, 2) (bf16) or [1024, 2048) (fp16, whose smallest
+// step is 2^-24: an entry 2^-34 of the largest is still held).
+// ---------------------------------------------------------------------------
+__global__ void __launch_bounds__(1024) k_vocab_rows(VocabCall c) {
+    __shared__ int warp_n[32];
+    __shared__ float warp_g[32];
+    const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+    int base = 0;
+    float top = 0.f;
+    bool bad = false;
+    for (int64_t r0 = 0; r0 < c.n; r0 += 1024) {
+        const int64_t r = r0 + tid;
+        bool on = false;
+        float Q = 1.f;
+        if (r < c.n) {
+            if (c.target) {
+                const int64_t t = c.target[r];
+                on = t != c.ignore_index && t >= 0 && t < c.V;
+            } else {
+                const float4 te = c.teacher[r];
+                on = te.w >= 2.f;
+                Q = te.x;
+            }
+        }
+        const unsigned ballot = __ballot_sync(0xffffffffu, on);
+        __syncthreads();
+        if (lane == 0) warp_n[wid] = __popc(ballot);
+        __syncthreads();
+        int before = 0, total = 0;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+            const int v = warp_n[i];
+            before += i < wid ? v : 0;
+            total += v;
+        }
+        if (on) {
+            const int at = base + before + __popc(ballot & ((1u << lane) - 1u));
+            c.row_of[at] = (int32_t)r;
+            c.at_of[r] = at;
+            const float g = fabsf(Q * (c.row_grad ? c.row_grad[r] : 1.f));
+            top = fmaxf(top, g);
+            bad |= !(g < INFINITY);
+        } else if (r < c.n) {
+            c.at_of[r] = -1;
+            c.loss[r] = 0.f;
+            c.lse[r] = 0.f;
+        }
+        base += total;
+    }
+    top = warp_max_f(top);
+    bad = __any_sync(0xffffffffu, bad);
+    if (lane == 0) warp_g[wid] = bad ? INFINITY : top;
+    __syncthreads();
+    if (tid == 0) {
+        for (int i = 0; i < 32; ++i) top = fmaxf(top, warp_g[i]);
+        if (!c.row_grad && base > 0) top /= (float)base;
+        top *= c.inv_T;
+        int e = 0;
+        if (top > 0.f && top < INFINITY) frexpf(top, &e);   // top in [2^(e-1), 2^e)
+        e = min(max((c.f16 ? 11 : 1) - e, -100), 100);
+        c.ctl->n_valid = base;
+        c.ctl->status = 0;
+        c.ctl->scale = ldexpf(1.f, e);
+        c.ctl->inv_scale = ldexpf(1.f, -e);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// 2. Compact rows of h (padded with zeros to the pitch, and zero rows to a multiple of 256, which
+// the products read) and the logits at the targets.  One CTA a row, one warp a dot product.
+// ---------------------------------------------------------------------------
+template <bool F16>
+__global__ void __launch_bounds__(128) k_vocab_gather(VocabCall c, bool w_vec) {
+    const int at = blockIdx.x, n_valid = c.ctl->n_valid;
+    const int tid = threadIdx.x, lane = tid & 31;
+    if (at >= (n_valid + kVocabRowPad - 1) / kVocabRowPad * kVocabRowPad) return;
+    uint16_t* to = c.hc + (int64_t)at * c.Dp;
+    if (at >= n_valid) {
+        for (int64_t i = tid; i < c.Dp / 8; i += 128) ((uint4*)to)[i] = make_uint4(0, 0, 0, 0);
+        return;
+    }
+    const int64_t r = c.row_of[at];
+    const uint16_t* from = (const uint16_t*)c.h + r * c.ldh;
+    if (((uintptr_t)from & 15) == 0) {
+        for (int64_t i = tid; i < c.Dp / 8; i += 128) {
+            if (i * 8 + 8 <= c.D) ((uint4*)to)[i] = __ldg((const uint4*)from + i);
+            else
+                for (int64_t j = i * 8; j < i * 8 + 8; ++j) to[j] = j < c.D ? from[j] : (uint16_t)0;
+        }
+    } else {
+        for (int64_t i = tid; i < c.Dp; i += 128) to[i] = i < c.D ? from[i] : (uint16_t)0;
+    }
+    __syncthreads();
+    for (int j = tid >> 5; j < c.K; j += 4) {
+        const int64_t v = c.target ? c.target[r] : (int64_t)c.t_idx[r * c.K + j];
+        float s = 0.f;
+        if (v >= 0 && v < c.V) {
+            const uint16_t* wr = (const uint16_t*)c.w + v * c.ldw;
+            int64_t i = 0;
+            if (w_vec) {
+                const int64_t whole = c.D / 8;
+                for (int64_t b = lane; b < whole; b += 32) {
+                    const uint4 x = ((const uint4*)to)[b];
+                    const uint4 y = __ldg((const uint4*)wr + b);
+                    const unsigned xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        s = fmaf(from16<F16>((uint16_t)xs[q]), from16<F16>((uint16_t)ys[q]), s);
+                        s = fmaf(from16<F16>((uint16_t)(xs[q] >> 16)), from16<F16>((uint16_t)(ys[q] >> 16)), s);
+                    }
+                }
+                i = whole * 8;
+            }
+            for (i += lane; i < c.D; i += 32) s = fmaf(from16<F16>(to[i]), from16<F16>(wr[i]), s);
+        }
+        s = warp_sum_f(s);
+        if (lane == 0) c.zt[(int64_t)at * c.K + j] = s;
+    }
+}
+
+// A copy of w with rows on 16-byte boundaries, where w's own are not.
+__global__ void __launch_bounds__(256) k_vocab_copy_w(VocabCall c) {
+    const uint16_t* from = (const uint16_t*)c.w + (int64_t)blockIdx.x * c.ldw;
+    uint16_t* to = c.wc + (int64_t)blockIdx.x * c.Dp;
+    for (int64_t i = threadIdx.x; i < c.Dp; i += 256) to[i] = i < c.D ? from[i] : (uint16_t)0;
+}
+
+// ---------------------------------------------------------------------------
+// 4. Log-sum-exp and loss.  A CTA takes 32 compact rows; its 8 warps share the tiles, a fixed order
+// joins them.
+// ---------------------------------------------------------------------------
+__global__ void __launch_bounds__(256) k_vocab_rows_done(VocabCall c) {
+    __shared__ float sm[8][32], ss[8][32];
+    const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+    const int64_t at0 = (int64_t)blockIdx.x * 32;
+    const int n_valid = c.ctl->n_valid;
+    if (at0 >= n_valid) return;
+    const int64_t at = at0 + lane;
+    const int64_t tiles = (c.V + kVocabTile - 1) / kVocabTile;
+    float m = -INFINITY, s = 0.f;
+    if (at < n_valid)
+        for (int64_t t = wid; t < tiles; t += 8) {
+            const float2 p = __ldcs(c.part + t * c.n_pad + at);
+            join_max_sum(m, s, p.x, p.y);
+        }
+    sm[wid][lane] = m;
+    ss[wid][lane] = s;
+    __syncthreads();
+    // each warp finishes four rows
+    for (int i = wid * 4; i < wid * 4 + 4; ++i) {
+        const int64_t a = at0 + i;
+        if (a >= n_valid) break;
+        m = sm[0][i];
+        s = ss[0][i];
+#pragma unroll
+        for (int k = 1; k < 8; ++k) join_max_sum(m, s, sm[k][i], ss[k][i]);
+        const float lse2 = m + log2f(s);
+        const int64_t r = c.row_of[a];
+        float Q = 1.f, loss;
+        if (c.target) {
+            loss = (lse2 - c.zt[a] * c.zscale) * kLn2;
+        } else {
+            const float4 te = c.teacher[r];
+            Q = te.x;
+            float sum = 0.f;
+            for (int j = lane; j < c.K; j += 32) {
+                const float q = c.q[r * c.K + j];
+                if (q > 0.f) sum += q * (((c.t_val[r * c.K + j] - te.z) * c.inv_T - te.y) + (lse2 - c.zt[a * c.K + j] * c.zscale) * kLn2);
+                else if (q != q) sum = q;
+            }
+            loss = warp_sum_f(sum);
+        }
+        if (lane == 0) {
+            c.loss[r] = loss;
+            c.lse[r] = lse2 * kLn2;
+            const float unit = c.ctl->scale * ((c.row_grad ? c.row_grad[r] : 1.f / (float)n_valid) * c.inv_T);
+            VocabRow out;
+            out.lse2 = lse2;
+            out.coef = unit * Q;
+            out.unit = unit;
+            out.pad = 0.f;
+            c.row[a] = out;
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// 5. Logit gradients of one piece.  The targets' entries are formed in fp32 from their own logits
+// and written over, so that 1 - p loses nothing where p is near 1.
+// ---------------------------------------------------------------------------
+template <bool F16>
+__device__ __forceinline__ void write_targets(const VocabCall& c, int64_t at, int64_t lo, int64_t hi, int64_t v0,
+                                              int tid, int threads) {
+    const int64_t r = c.row_of[at];
+    const VocabRow vr = c.row[at];
+    const bool distinct = c.target || c.teacher[r].w == 3.f;
+    for (int j = tid; j < c.K; j += threads) {
+        const int64_t v = c.target ? c.target[r] : (int64_t)c.t_idx[r * c.K + j];
+        if (v < lo || v >= hi) continue;
+        float q = c.target ? 1.f : c.q[r * c.K + j];
+        if (!distinct) {      // an index given more than once: each of its pairs writes the same sum
+            q = 0.f;
+            for (int i = 0; i < c.K; ++i)
+                if (c.t_idx[r * c.K + i] == v) q += c.q[r * c.K + i];
+        }
+        const float p = exp2_fast(c.zt[at * c.K + j] * c.zscale - vr.lse2);
+        c.e[at * c.vb + (v - v0)] = to16<F16>(fmaf(vr.coef, p, -(vr.unit * q)));
+    }
+}
+
+constexpr int kGradCols = 4096;   // columns a CTA scales
+
+// From the exponentials kept of the piece [v0, v1): e <- coef exp(m_tile - lse) e, in place.
+template <bool F16>
+__global__ void __launch_bounds__(256) k_vocab_scale(VocabCall c, int64_t v0, int64_t v1) {
+    const int64_t at = blockIdx.x;
+    if (at >= c.ctl->n_valid) return;
+    const int64_t lo = v0 + (int64_t)blockIdx.y * kGradCols;
+    const int64_t hi = lo + kGradCols < v1 ? lo + kGradCols : v1;
+    const VocabRow vr = c.row[at];
+    for (int64_t v = lo + threadIdx.x * 8; v < hi; v += 256 * 8) {
+        const float m = __ldg(&c.part[v / kVocabTile * c.n_pad + at].x);
+        const float f = m == -INFINITY ? 0.f : vr.coef * exp2_fast(m - vr.lse2);
+        uint4* p = (uint4*)(c.e + at * c.vb + (v - v0));
+        uint4 x = *p;
+        unsigned xs[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            xs[q] = pack16<F16>(f * from16<F16>((uint16_t)xs[q]), f * from16<F16>((uint16_t)(xs[q] >> 16)));
+        *p = make_uint4(xs[0], xs[1], xs[2], xs[3]);
+    }
+    __syncthreads();
+    write_targets<F16>(c, at, lo, hi, v0, threadIdx.x, 256);
+}
+
+// The product taken again has written the gradients; only the targets' entries are left.
+template <bool F16>
+__global__ void __launch_bounds__(128) k_vocab_targets(VocabCall c, int64_t v0, int64_t v1) {
+    const int64_t at = blockIdx.x;
+    if (at >= c.ctl->n_valid) return;
+    write_targets<F16>(c, at, v0, v1, v0, threadIdx.x, 128);
+}
+
+// dh in the caller's rows: the splits' partial sums added in their order, zero for rows left out.
+template <bool F16>
+__global__ void __launch_bounds__(256) k_vocab_finish_dh(VocabCall c) {
+    const int64_t r = blockIdx.x;
+    const int at = c.at_of[r];
+    uint16_t* to = (uint16_t*)c.dh + r * c.lddh;
+    const float inv = c.ctl->inv_scale;
+    for (int64_t i = threadIdx.x; i < c.D; i += 256) {
+        float s = 0.f;
+        if (at >= 0)
+            for (int k = 0; k < c.splits; ++k) s += c.dhp[((int64_t)k * c.n_pad + at) * c.Dp + i];
+        to[i] = to16<F16>(s * inv);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Workspace: one block per (device, stream), grown as calls need it.
+// ---------------------------------------------------------------------------
+struct VocabWorkspace {
+    void* base = nullptr;
+    size_t bytes = 0;
+    int sm_count = 0;
+};
+static std::mutex g_vocab_mu;
+static std::map<std::pair<int, cudaStream_t>, VocabWorkspace> g_vocab_ws;
+static std::atomic<int64_t> g_vocab_budget{(int64_t)2 << 30};
+
+static int64_t piece_columns(int64_t n_pad, int64_t V) {
+    const int64_t fit = g_vocab_budget.load() / (2 * n_pad) / 256 * 256;
+    const int64_t all = round_up(V, 256);
+    return fit >= all ? all : fit < 256 ? 256 : fit;
+}
+
+// Lays the workspace out in `c` from `base` (nullptr: only the size is wanted).
+static size_t lay_out(VocabCall& c, bool distill, bool copy_w, char* base) {
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        char* p = base ? base + at : nullptr;
+        at = (at + bytes + 255) / 256 * 256;
+        return p;
+    };
+    const size_t n = (size_t)c.n, np = (size_t)c.n_pad, K = (size_t)c.K;
+    const size_t tiles = (size_t)((c.V + kVocabTile - 1) / kVocabTile);
+    c.ctl = (VocabCtl*)take(sizeof(VocabCtl));
+    c.row_of = (int32_t*)take(4 * n);
+    c.at_of = (int32_t*)take(4 * n);
+    c.q = (float*)(distill ? take(4 * n * K) : nullptr);
+    c.teacher = (float4*)(distill ? take(16 * n) : nullptr);
+    c.hc = (uint16_t*)take(2 * np * c.Dp);
+    c.wc = (uint16_t*)(copy_w ? take(2 * (size_t)c.V * c.Dp) : nullptr);
+    c.zt = (float*)take(4 * np * K);
+    c.part = (float2*)take(8 * tiles * np);
+    c.row = (VocabRow*)take(sizeof(VocabRow) * np);
+    c.e = (uint16_t*)(c.vb > 0 ? take(2 * np * (size_t)c.vb) : nullptr);
+    c.dhp = (float*)(c.splits > 0 ? take(4 * (size_t)c.splits * np * c.Dp) : nullptr);
+    return at;
+}
+
+static int vocab_workspace(size_t bytes, cudaStream_t st, VocabWorkspace** out) {
+    int dev = 0;
+    GK_CUDA_TRY(cudaGetDevice(&dev));
+    std::lock_guard<std::mutex> lock(g_vocab_mu);
+    VocabWorkspace& ws = g_vocab_ws[std::make_pair(dev, st)];
+    if (ws.bytes < bytes) {
+        if (ws.base) {
+            GK_CUDA_TRY(cudaStreamSynchronize(st));   // work already enqueued may still use the old block
+            GK_CUDA_TRY(cudaFree(ws.base));
+            ws.base = nullptr;
+            ws.bytes = 0;
+        }
+        void* p = nullptr;
+        if (cudaMalloc(&p, bytes) != cudaSuccess) { cudaGetLastError(); return GK_ERR_NOMEM; }
+        ws.base = p;
+        ws.bytes = bytes;
+    }
+    if (ws.sm_count == 0) GK_CUDA_TRY(cudaDeviceGetAttribute(&ws.sm_count, cudaDevAttrMultiProcessorCount, dev));
+    *out = &ws;
+    return GK_OK;
+}
+
+static void size_call(VocabCall& c, bool want_dh, bool want_dw, int sm_count) {
+    c.n_pad = round_up(c.n, kVocabRowPad);
+    c.Dp = round_up(c.D, 64);
+    c.vb = want_dh || want_dw ? piece_columns(c.n_pad, c.V) : 0;
+    c.splits = want_dh ? vocab_dh_splits(c.n, c.D, c.vb, sm_count) : 0;
+}
+
+template <bool F16>
+static int enqueue(const VocabCall& c, bool distill, bool w_vec, int sms, cudaStream_t st) {
+    const unsigned n = (unsigned)c.n;
+    const bool grad = c.dh || c.dw;
+    if (distill) k_vocab_teacher<<<(n + 7) / 8, 256, 0, st>>>(c);
+    k_vocab_rows<<<1, 1024, 0, st>>>(c);
+    k_vocab_gather<F16><<<(unsigned)c.n_pad, 128, 0, st>>>(c, w_vec);
+    if (c.wc) k_vocab_copy_w<<<(unsigned)c.V, 256, 0, st>>>(c);
+    GK_CUDA_TRY(cudaGetLastError());
+    note_launch(2 + (distill ? 1 : 0) + (c.wc ? 1 : 0));
+    const int64_t kept = grad ? (c.vb < c.V ? c.vb : c.V) : 0;
+    int rc = GK_OK;
+    if (kept > 0) rc = launch_vocab_logits(c, 0, kept, true, sms, st);
+    if (rc == GK_OK && kept < c.V) rc = launch_vocab_logits(c, kept, c.V, false, sms, st);
+    if (rc != GK_OK) return rc;
+    k_vocab_rows_done<<<(n + 31) / 32, 256, 0, st>>>(c);
+    GK_CUDA_TRY(cudaGetLastError());
+    note_launch();
+    if (!grad) return GK_OK;
+    for (int64_t v0 = 0; v0 < c.V; v0 += c.vb) {
+        const int64_t v1 = v0 + c.vb < c.V ? v0 + c.vb : c.V;
+        if (v0 == 0) {
+            k_vocab_scale<F16><<<dim3(n, (unsigned)((v1 + kGradCols - 1) / kGradCols)), 256, 0, st>>>(c, v0, v1);
+        } else {
+            rc = launch_vocab_again(c, v0, v1, sms, st);
+            if (rc != GK_OK) return rc;
+            k_vocab_targets<F16><<<n, 128, 0, st>>>(c, v0, v1);
+        }
+        GK_CUDA_TRY(cudaGetLastError());
+        note_launch();
+        if (c.dw) rc = launch_vocab_dw(c, v0, v1, sms, st);
+        if (rc == GK_OK && c.dh) rc = launch_vocab_dh(c, v0, v1, v0 == 0, sms, st);
+        if (rc != GK_OK) return rc;
+    }
+    if (c.dh) {
+        k_vocab_finish_dh<F16><<<n, 256, 0, st>>>(c);
+        GK_CUDA_TRY(cudaGetLastError());
+        note_launch();
+    }
+    return GK_OK;
+}
+
+static bool overlap(const void* a, size_t an, const void* b, size_t bn) {
+    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+    return x < y + bn && y < x + an;
+}
+static size_t extent(int64_t rows, int64_t cols, int64_t ld) { return rows < 1 ? 0 : 2 * (size_t)((rows - 1) * ld + cols); }
+
+// What both entry points check, in the order of the arguments.
+static int check_head(const VocabCall& c, int32_t dtype) {
+    if (c.n < 0 || c.D < 1 || c.V < 1) return GK_ERR_SIZE;
+    if (c.n > (1 << 22) || c.D > (1 << 16) || c.V > (1 << 26)) return GK_ERR_LIMIT;
+    if (dtype != GK_TYPE_BF16 && dtype != GK_TYPE_F16) return GK_ERR_TYPE;
+    if (!c.w || (c.n > 0 && (!c.h || !c.loss || !c.lse))) return GK_ERR_NULL;
+    if (c.ldh < c.D || c.ldw < c.D || (c.dh && c.lddh < c.D) || (c.dw && c.lddw < c.D)) return GK_ERR_STRIDE;
+    if ((((uintptr_t)c.h | (uintptr_t)c.w | (uintptr_t)c.dh | (uintptr_t)c.dw) & 1) != 0) return GK_ERR_ALIGN;
+    const size_t hb = extent(c.n, c.D, c.ldh), wb = extent(c.V, c.D, c.ldw);
+    const size_t dhb = c.dh ? extent(c.n, c.D, c.lddh) : 0, dwb = c.dw ? extent(c.V, c.D, c.lddw) : 0;
+    if (dhb && (overlap(c.dh, dhb, c.h, hb) || overlap(c.dh, dhb, c.w, wb))) return GK_ERR_ALIAS;
+    if (dwb && (overlap(c.dw, dwb, c.h, hb) || overlap(c.dw, dwb, c.w, wb))) return GK_ERR_ALIAS;
+    if (dhb && dwb && overlap(c.dh, dhb, c.dw, dwb)) return GK_ERR_ALIAS;
+    return GK_OK;
+}
+
+static int run_head(VocabCall& c, bool distill, cudaStream_t st) {
+    if (c.n == 0) {   // no rows: the weights' gradient is zero
+        if (c.dw) GK_CUDA_TRY(cudaMemset2DAsync(c.dw, 2 * c.lddw, 0, 2 * c.D, (size_t)c.V, st));
+        return GK_OK;
+    }
+    VocabWorkspace* ws = nullptr;
+    int rc = vocab_workspace(0, st, &ws);
+    if (rc != GK_OK) return rc;
+    const bool w_vec = (((uintptr_t)c.w | (uintptr_t)(2 * c.ldw)) & 15) == 0;
+    size_call(c, c.dh != nullptr, c.dw != nullptr, ws->sm_count);
+    rc = vocab_workspace(lay_out(c, distill, !w_vec, nullptr), st, &ws);
+    if (rc != GK_OK) return rc;
+    lay_out(c, distill, !w_vec, (char*)ws->base);
+    return c.f16 ? enqueue<true>(c, distill, w_vec, ws->sm_count, st) : enqueue<false>(c, distill, w_vec, ws->sm_count, st);
+}
+
+}  // namespace gk
+
+using namespace gk;
+
+extern "C" int gk_vocab_loss(const void* h, int64_t ldh, const void* w, int64_t ldw, int32_t dtype, int64_t n, int64_t D,
+                             int64_t V, const int64_t* target, int64_t ignore_index, const float* row_grad,
+                             float* loss_out, float* lse_out, void* dh_out, int64_t lddh, void* dw_out, int64_t lddw,
+                             gk_stream_t stream) {
+    VocabCall c = {};
+    c.n = n; c.D = D; c.V = V;
+    c.h = h; c.ldh = ldh; c.w = w; c.ldw = ldw; c.dh = dh_out; c.lddh = lddh; c.dw = dw_out; c.lddw = lddw;
+    c.target = target; c.ignore_index = ignore_index; c.row_grad = row_grad; c.loss = loss_out; c.lse = lse_out;
+    const int rc = check_head(c, dtype);
+    if (rc != GK_OK) return rc;
+    if (n > 0 && !target) return GK_ERR_NULL;
+    c.K = 1;
+    c.f16 = dtype == GK_TYPE_F16;
+    c.inv_T = 1.f;
+    c.zscale = (float)kLog2e;
+    return run_head(c, false, (cudaStream_t)stream);
+}
+
+extern "C" int gk_vocab_distill(const void* h, int64_t ldh, const void* w, int64_t ldw, int32_t dtype, int64_t n,
+                                int64_t D, int64_t V, const int32_t* t_idx, const float* t_val, int32_t K,
+                                const float* t_lse, float temperature, const float* row_grad, float* loss_out,
+                                float* lse_out, void* dh_out, int64_t lddh, void* dw_out, int64_t lddw,
+                                gk_stream_t stream) {
+    VocabCall c = {};
+    c.n = n; c.D = D; c.V = V;
+    c.h = h; c.ldh = ldh; c.w = w; c.ldw = ldw; c.dh = dh_out; c.lddh = lddh; c.dw = dw_out; c.lddw = lddw;
+    c.t_idx = t_idx; c.t_val = t_val; c.t_lse = t_lse; c.row_grad = row_grad; c.loss = loss_out; c.lse = lse_out;
+    const int rc = check_head(c, dtype);
+    if (rc != GK_OK) return rc;
+    if (n > 0 && (!t_idx || !t_val)) return GK_ERR_NULL;
+    if (K < 1 || K > kVocabMaxPairs) return GK_ERR_K;
+    if (!(temperature > 0.f) || !(temperature < INFINITY)) return GK_ERR_TEMPERATURE;
+    c.K = K;
+    c.f16 = dtype == GK_TYPE_F16;
+    c.inv_T = 1.f / temperature;
+    c.zscale = (float)(kLog2e / (double)temperature);
+    return run_head(c, true, (cudaStream_t)stream);
+}
+
+extern "C" int gk_vocab_set_budget(int64_t bytes) {
+    if (bytes < 0) return GK_ERR_CAPACITY;
+    g_vocab_budget.store(bytes);
+    return GK_OK;
+}
+
+// Sizes of the largest call a workspace is asked for: a distillation with K pairs and both
+// gradients (or no gradient), over rows of w on any boundary.
+static size_t largest(VocabCall& c, int64_t n, int64_t D, int64_t V, int32_t K, int grad, int sms) {
+    c.n = n; c.D = D; c.V = V; c.K = K;
+    size_call(c, grad != 0, grad != 0, sms);
+    return lay_out(c, true, D % 8 != 0, nullptr);
+}
+
+static int head_sizes_ok(int64_t n, int64_t D, int64_t V, int32_t K) {
+    if (n < 1 || D < 1 || V < 1) return GK_ERR_SIZE;
+    if (n > (1 << 22) || D > (1 << 16) || V > (1 << 26)) return GK_ERR_LIMIT;
+    return K < 1 || K > kVocabMaxPairs ? GK_ERR_K : GK_OK;
+}
+
+extern "C" int64_t gk_vocab_workspace_bytes(int64_t n, int64_t D, int64_t V, int32_t K, int grad) {
+    if (head_sizes_ok(n, D, V, K) != GK_OK) return 0;
+    VocabCall c = {};
+    return (int64_t)largest(c, n, D, V, K, grad, 148);
+}
+
+extern "C" int gk_vocab_reserve(int64_t n, int64_t D, int64_t V, int32_t K, int grad, gk_stream_t stream) {
+    const int rc = head_sizes_ok(n, D, V, K);
+    if (rc != GK_OK) return rc;
+    VocabWorkspace* ws = nullptr;
+    const int wrc = vocab_workspace(0, (cudaStream_t)stream, &ws);
+    if (wrc != GK_OK) return wrc;
+    VocabCall c = {};
+    return vocab_workspace(largest(c, n, D, V, K, grad, ws->sm_count), (cudaStream_t)stream, &ws);
+}
+
+extern "C" int gk_vocab_last_info(gk_stream_t stream, int64_t* host_out) {
+    if (!host_out) return GK_ERR_NULL;
+    int dev = 0;
+    GK_CUDA_TRY(cudaGetDevice(&dev));
+    void* base = nullptr;
+    {
+        std::lock_guard<std::mutex> lock(g_vocab_mu);
+        auto it = g_vocab_ws.find(std::make_pair(dev, (cudaStream_t)stream));
+        if (it != g_vocab_ws.end()) base = it->second.base;
+    }
+    if (!base) return GK_ERR_NULL;
+    VocabCtl ctl;
+    GK_CUDA_TRY(cudaStreamSynchronize((cudaStream_t)stream));
+    GK_CUDA_TRY(cudaMemcpy(&ctl, base, sizeof(ctl), cudaMemcpyDeviceToHost));
+    host_out[0] = ctl.status;
+    host_out[1] = ctl.n_valid;
+    return GK_OK;
+}

@@ -109,3 +109,50 @@ def test_the_operator_and_the_setters_validate_on_the_host(lib):
     assert lib.gk_set_path(3) == -2 and lib.gk_set_path(-1) == -2
     assert lib.gk_debug_set(99, 0) == -2 and lib.gk_debug_set(-1, 0) == -2      # unknown keys
     assert lib.gk_debug_set(0, -2) == -2                                         # value out of range
+
+
+def test_the_vocabulary_head_validates_on_the_host(lib):
+    a, st = 0x100000, None
+
+    def loss(h=a, ldh=8, w=a + 0x10000, ldw=8, dtype=1, n=4, D=8, V=5, target=a, loss_out=a, lse=a, dh=None, lddh=8, dw=None, lddw=8):
+        return lib.gk_vocab_loss(h, ldh, w, ldw, dtype, n, D, V, target, -100, None, loss_out, lse, dh, lddh, dw, lddw, st)
+
+    assert loss(n=-1) == -2 and loss(D=0) == -2 and loss(V=0) == -2
+    assert loss(n=2 ** 22 + 1) == -9 and loss(D=2 ** 16 + 1) == -9 and loss(V=2 ** 26 + 1) == -9
+    assert loss(dtype=0) == -10 and loss(dtype=7) == -10
+    assert loss(h=None) == -1 and loss(w=None) == -1 and loss(target=None) == -1 and loss(loss_out=None) == -1 and loss(lse=None) == -1
+    assert loss(ldh=7) == -11 and loss(ldw=7) == -11 and loss(dh=a + 0x20000, lddh=7) == -11 and loss(dw=a + 0x20000, lddw=7) == -11
+    assert loss(h=a + 1) == -4 and loss(dw=a + 0x20001) == -4
+    assert loss(dh=a + 8) == -5 and loss(dw=a + 0x10000 + 32) == -5 and loss(dh=a + 0x20000, dw=a + 0x20008) == -5
+
+    def distill(K=3, T=1.0, idx=a, val=a):
+        return lib.gk_vocab_distill(a, 8, a + 0x10000, 8, 1, 4, 8, 5, idx, val, K, None, T, None, a, a, None, 8, None, 8, st)
+
+    assert distill(K=0) == -3 and distill(K=1025) == -3
+    assert distill(T=0.0) == -12 and distill(T=float("nan")) == -12 and distill(T=float("inf")) == -12
+    assert distill(idx=None) == -1 and distill(val=None) == -1
+
+    def topk(z=a, ld=50, dtype=0, n=2, V=50, k=4, T=1.0, idx=a, val=a):
+        return lib.gk_vocab_topk(z, ld, dtype, n, V, k, T, idx, val, None, st)
+
+    assert topk(n=-1) == -2 and topk(V=0) == -2 and topk(dtype=3) == -10 and topk(z=None) == -1 and topk(idx=None) == -1
+    assert topk(ld=49) == -11 and topk(z=a + 2) == -4 and topk(k=0) == -3 and topk(k=51) == -3 and topk(T=-1.0) == -12
+    assert topk(n=0, z=None) == 0
+    assert lib.gk_vocab_set_budget(-1) == -8
+
+
+def test_error_text_of_the_vocabulary_head(lib):
+    for code in (-10, -11, -12):
+        assert "unknown" not in binding.gk_strerror(code)
+
+
+def test_the_vocabulary_heads_workspace_is_bounded_by_the_budget(lib):
+    base = binding.gk_vocab_workspace_bytes(8192, 4096, 128000)
+    try:
+        binding.gk_vocab_set_budget(64 << 20)
+        small = binding.gk_vocab_workspace_bytes(8192, 4096, 128000)
+        assert base - small > 1 << 30
+        assert binding.gk_vocab_workspace_bytes(8192, 4096, 128000, grad=False) < small
+    finally:
+        binding.gk_vocab_set_budget(2 << 30)
+    assert binding.gk_vocab_workspace_bytes(0, 64, 64) == 0
