@@ -11,14 +11,16 @@
 // One call:
 //   1. (distill) the teacher's probabilities; the rows that count, numbered in their order;
 //   2. those rows of h copied together, and the logits at the targets as K dot products a row;
-//   3. logits tile by tile: the tile's maximum and sum, and exp(z / T - maximum) in 16 bits for the
-//      first piece of the vocabulary (all of it where the budget allows);
+//   3. logits tile by tile: the tile's maximum and sum, and for the first piece of the vocabulary (all
+//      of it where the budget allows) their distances from that maximum in 16 bits;
 //   4. the row's log-sum-exp from the tiles, loss;
-//   5. per piece: logit gradients in 16 bits (from the kept exponentials, or from the product
+//   5. per piece: logit gradients in 16 bits (from the kept distances, or from the product
 //      taken again), then dw and dh as products with them.
-// Kept between the steps is one piece, whose size the budget bounds whatever n and V are.  The
-// exponentials are kept relative to their tile's maximum: 16 bits then hold each with a relative
-// error of 2^-9 (bf16) or 2^-12 (fp16), which a logit rounded to 16 bits would not give.
+// Kept between the steps is one piece, whose size the budget bounds whatever n and V are.  A
+// distance is kept in fixed point, for bf16 in steps of 2^-9 in the exponent of two: the exponential
+// it stands for is then off by at most 2^-10 log 2 = 6.8e-4 of itself, where a bf16 exponential is off by
+// up to 2^-9 = 2.0e-3, and a logit of 16 by 3e-2; the 65536 steps reach 2^-128, as bf16 itself does.  For
+// fp16 the steps are 2^-11 (1.7e-4, against 4.9e-4) and reach 2^-32, where fp16 gradients have ended.
 #include <atomic>
 #include <map>
 #include <mutex>
@@ -299,23 +301,33 @@ __device__ __forceinline__ void write_targets(const VocabCall& c, int64_t at, in
 
 constexpr int kGradCols = 4096;   // columns a CTA scales
 
-// From the exponentials kept of the piece [v0, v1): e <- coef exp(m_tile - lse) e, in place.
+// From the distances kept of the piece [v0, v1): e <- coef 2^(m_tile - lse - x / steps), in place, and zero
+// for the rows up to the padding, which the product for dw sums over.
 template <bool F16>
 __global__ void __launch_bounds__(256) k_vocab_scale(VocabCall c, int64_t v0, int64_t v1) {
     const int64_t at = blockIdx.x;
-    if (at >= c.ctl->n_valid) return;
+    const int n_valid = c.ctl->n_valid;
+    if (at >= round_up(n_valid, 64)) return;
     const int64_t lo = v0 + (int64_t)blockIdx.y * kGradCols;
     const int64_t hi = lo + kGradCols < v1 ? lo + kGradCols : v1;
+    if (at >= n_valid) {
+        for (int64_t v = lo + threadIdx.x * 8; v < hi; v += 256 * 8) *(uint4*)(c.e + at * c.vb + (v - v0)) = make_uint4(0, 0, 0, 0);
+        return;
+    }
     const VocabRow vr = c.row[at];
     for (int64_t v = lo + threadIdx.x * 8; v < hi; v += 256 * 8) {
-        const float m = __ldg(&c.part[v / kVocabTile * c.n_pad + at].x);
-        const float f = m == -INFINITY ? 0.f : vr.coef * exp2_fast(m - vr.lse2);
+        const float base = __ldg(&c.part[v / kVocabTile * c.n_pad + at].x) - vr.lse2;
         uint4* p = (uint4*)(c.e + at * c.vb + (v - v0));
-        uint4 x = *p;
+        const uint4 x = *p;
         unsigned xs[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-            xs[q] = pack16<F16>(f * from16<F16>((uint16_t)xs[q]), f * from16<F16>((uint16_t)(xs[q] >> 16)));
+        for (int q = 0; q < 4; ++q) {
+            // the bits of 2^23 + x, less 2^23
+            const float lo_x = __uint_as_float(0x4b000000u | (xs[q] & 0xffffu)) - 8388608.f;
+            const float hi_x = __uint_as_float(0x4b000000u | (xs[q] >> 16)) - 8388608.f;
+            xs[q] = pack16<F16>(vr.coef * exp2_fast(fmaf(lo_x, -1.f / kept_steps<F16>(), base)),
+                                vr.coef * exp2_fast(fmaf(hi_x, -1.f / kept_steps<F16>(), base)));
+        }
         *p = make_uint4(xs[0], xs[1], xs[2], xs[3]);
     }
     __syncthreads();
@@ -439,7 +451,7 @@ static int enqueue(const VocabCall& c, bool distill, bool w_vec, int sms, cudaSt
     for (int64_t v0 = 0; v0 < c.V; v0 += c.vb) {
         const int64_t v1 = v0 + c.vb < c.V ? v0 + c.vb : c.V;
         if (v0 == 0) {
-            k_vocab_scale<F16><<<dim3(n, (unsigned)((v1 + kGradCols - 1) / kGradCols)), 256, 0, st>>>(c, v0, v1);
+            k_vocab_scale<F16><<<dim3((unsigned)round_up(n, 64), (unsigned)((v1 + kGradCols - 1) / kGradCols)), 256, 0, st>>>(c, v0, v1);
         } else {
             rc = launch_vocab_again(c, v0, v1, sms, st);
             if (rc != GK_OK) return rc;

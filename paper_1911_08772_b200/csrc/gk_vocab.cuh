@@ -10,7 +10,7 @@
 
 namespace gk {
 
-constexpr int kVocabTile = 64;         // columns of the vocabulary whose maximum and sum are kept together
+constexpr int kVocabTile = 256;        // columns of the vocabulary whose maximum and sum are kept together
 constexpr int kVocabRowPad = 256;       // compact rows are padded to a multiple of this
 constexpr int kVocabMaxPairs = 1024;    // largest K of gk_vocab_distill and gk_vocab_topk
 
@@ -64,17 +64,17 @@ struct VocabCall {
     float* zt;                  // n_pad x K raw logits at the targets
     float2* part;               // per (vocabulary tile, compact row): maximum (units of log 2), sum
     VocabRow* row;              // n_pad
-    uint16_t* e;                // n_pad x vb: one piece's exponentials, then its logit gradients
+    uint16_t* e;                // n_pad x vb: one piece's kept logits, then its logit gradients
     int64_t vb;                 // columns of a piece, a multiple of 256 (the pitch of e)
     float* dhp;                 // splits x n_pad x Dp partial sums of dh
     int splits;
 };
 
-inline int64_t round_up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
+__host__ __device__ inline int64_t round_up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
 
 // The products (gk_vocab_gemm.cu).  v0, v1: the columns of the vocabulary [v0, v1).
 // Logits of all compact rows: per tile of the vocabulary the maximum and the sum; keep: the
-// exponentials relative to the tile's maximum go to e.
+// logits go to e, as 16-bit whole numbers of steps (kept_steps) below the tile's maximum.
 int launch_vocab_logits(const VocabCall& c, int64_t v0, int64_t v1, bool keep, int sm_count, cudaStream_t st);
 // The same product again with the rows' log-sum-exp known: e receives the logit gradients.
 int launch_vocab_again(const VocabCall& c, int64_t v0, int64_t v1, int sm_count, cudaStream_t st);
@@ -91,6 +91,11 @@ __device__ __forceinline__ float exp2_fast(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+
+// Steps a unit of log 2 in which a logit's distance from its tile's maximum is kept: 2^-9 over a
+// range of 128 (the exponents bf16 gradients can have), 2^-11 over 32 (fp16's).
+template <bool F16>
+__device__ __forceinline__ constexpr float kept_steps() { return F16 ? 2048.f : 512.f; }
 
 // 16-bit storage <-> fp32, round to nearest even (F16: fp16, else bf16).
 template <bool F16>
