@@ -325,8 +325,8 @@ int gk_set_params(int unbiased_std, int max_rounds);
  * operands' type before the products dh and dw, which are rounded once more at the end.
  *
  *   h          DEVICE in   n rows of D elements of `dtype`, row stride ldh >= D (in elements)
- *   w          DEVICE in   V rows of D elements, row stride ldw >= D.  Rows that start on 16-byte
- *                          boundaries are read in place; otherwise the call copies w first.
+ *   w          DEVICE in   V rows of D elements, row stride ldw >= D.  Rows that start and end on
+ *                          16-byte boundaries are read in place; otherwise the call copies w first.
  *   dtype      GK_TYPE_BF16 or GK_TYPE_F16, of h, w, dh and dw
  *   n, D, V    0 <= n <= 2^22, 1 <= D <= 2^16, 1 <= V <= 2^26
  *   target     DEVICE in   n int64 classes.  A row whose target is ignore_index, or outside
@@ -397,7 +397,7 @@ int gk_vocab_set_budget(int64_t bytes);
 
 /* Create (or grow) the workspace of (current device, stream) for gk_vocab_loss (K = 1) and
  * gk_vocab_distill calls of these sizes at the present budget, with or without gradients, with
- * rows of w on 16-byte boundaries if D is a multiple of 8.  Synchronous. */
+ * rows of w on 16-byte boundaries where D is a multiple of 8.  Synchronous. */
 int gk_vocab_reserve(int64_t n, int64_t D, int64_t V, int32_t K, int grad, gk_stream_t stream);
 int64_t gk_vocab_workspace_bytes(int64_t n, int64_t D, int64_t V, int32_t K, int grad);
 

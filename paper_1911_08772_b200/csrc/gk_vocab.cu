@@ -209,7 +209,7 @@ __global__ void __launch_bounds__(128) k_vocab_gather(VocabCall c, bool w_vec) {
     }
 }
 
-// A copy of w with rows on 16-byte boundaries, where w's own are not.
+// A copy of w with rows that start and end on 16-byte boundaries, where w's own do not.
 __global__ void __launch_bounds__(256) k_vocab_copy_w(VocabCall c) {
     const uint16_t* from = (const uint16_t*)c.w + (int64_t)blockIdx.x * c.ldw;
     uint16_t* to = c.wc + (int64_t)blockIdx.x * c.Dp;
@@ -501,7 +501,8 @@ static int run_head(VocabCall& c, bool distill, cudaStream_t st) {
     VocabWorkspace* ws = nullptr;
     int rc = vocab_workspace(0, st, &ws);
     if (rc != GK_OK) return rc;
-    const bool w_vec = (((uintptr_t)c.w | (uintptr_t)(2 * c.ldw)) & 15) == 0;
+    // rows that start and end on 16-byte boundaries are copied to shared memory as they lie
+    const bool w_vec = (((uintptr_t)c.w | (uintptr_t)(2 * c.ldw) | (uintptr_t)(2 * c.D)) & 15) == 0;
     size_call(c, c.dh != nullptr, c.dw != nullptr, ws->sm_count);
     rc = vocab_workspace(lay_out(c, distill, !w_vec, nullptr), st, &ws);
     if (rc != GK_OK) return rc;

@@ -10,7 +10,7 @@
 
 namespace gk {
 
-constexpr int kVocabTile = 256;        // columns of the vocabulary whose maximum and sum are kept together
+constexpr int kVocabTile = 128;        // columns of the vocabulary whose maximum and sum are kept together
 constexpr int kVocabRowPad = 256;       // compact rows are padded to a multiple of this
 constexpr int kVocabMaxPairs = 1024;    // largest K of gk_vocab_distill and gk_vocab_topk
 

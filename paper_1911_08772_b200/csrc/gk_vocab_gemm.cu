@@ -1,22 +1,30 @@
 // The products of the vocabulary head (gk_vocab.cu) on the fifth-generation tensor cores.
 //
-// One persistent kernel, four uses of it.  A pair of SMs (a cluster of two CTAs) computes a
-// 256 x 256 tile of the result with tcgen05.mma.cta_group::2: each CTA holds 128 rows of A, 128 of
-// the 256 columns of B, and 128 x 256 fp32 sums in its tensor memory.  Operands arrive by TMA in
-// blocks of 64 along the summed axis, six blocks in flight (32 KB each and CTA); the sums are
-// double buffered (2 x 256 of the 512 columns of tensor memory), so that one tile is read out and
-// finished by four warps while the next one is being summed.
+// One persistent kernel, five uses of it.  A pair of SMs (a cluster of two CTAs) computes a
+// 256 x 512 tile of the result with tcgen05.mma.cta_group::2, as two 256 x 256 halves: each CTA holds
+// 128 rows of A, 128 of the 256 columns of each half of B, and 128 x 512 fp32 sums, which is all of its
+// tensor memory.  Operands arrive by TMA in blocks of 64 along the summed axis, four blocks in
+// flight (48 KB each and CTA).  A tile half as wide with double-buffered sums needs 64 bytes a clock
+// and SM from L2 to keep the tensor pipe fed and kept it 81 % busy (ncu, 4096 x 4096 x 32000); this one
+// needs 48.
+//
+// The sums are not double buffered.  Instead the two halves of a tile are summed out of step at its
+// ends: the first half is ahead by up to four blocks at the end of a tile, so that it is read out while
+// the second half catches up, and again at the start of the next tile, while the second half is
+// read out.  Eight warps read out: four for the lanes, two for the columns of a half.
 //
 //   use          A (M x K)            B (N x K)            what the readout does
-//   kLogits      hc  rows x D         w   columns x D      maximum and sum of the tile's columns per row
-//   kLogitsKeep  the same                                  and the logits, as 16-bit steps below the
-//                                                          tile's maximum
+//   kLogits      hc  rows x D         w   columns x D      maximum and sum of 128 columns per row
+//   kLogitsKeep  the same                                  and the logits, as 16-bit steps below that
+//                                                          maximum
 //   kAgain       the same                                  logit gradients, the log-sum-exp being known
 //   kDw          e^T columns x rows   hc^T D x rows        16-bit rows of dw
 //   kDh          e   rows x columns   w^T  D x columns     fp32 partial sums of dh
 //
 // e, hc and w are stored once, by rows; where the summed axis is not the contiguous one the
 // operand is read as it lies (MN-major descriptors) instead of being transposed in memory.
+// Results leave through shared memory, 32 rows x 128 bytes a warp, as TMA stores: a thread has a row of
+// its own, and stores of 16 bytes to 32 rows at once would take the time of 32.
 #include <cuda.h>
 
 #include "gk_vocab.cuh"
@@ -25,13 +33,15 @@ namespace gk {
 
 enum Product { kLogits, kLogitsKeep, kAgain, kDw, kDh };
 
-constexpr int kTileM = 256, kTileN = 256, kBlockK = 64, kStages = 6;
-constexpr int kOperandBytes = 128 * kBlockK * 2;            // one operand's share of a CTA in a block
-constexpr int kStageBytes = 2 * kOperandBytes;
-constexpr int kProductSmem = kStages * kStageBytes + 1024;  // and the alignment of the first block
-constexpr int kProductThreads = 256;
+constexpr int kTileM = 256, kHalfN = 256, kTileN = 2 * kHalfN, kBlockK = 64, kStages = 4;
+constexpr int kOperandBytes = 128 * kBlockK * 2;            // a CTA's share of A, or of a half of B, in a block
+constexpr int kStageBytes = 3 * kOperandBytes;
+constexpr int kReaders = 8;                                 // warps that read the sums out
+constexpr int kStagingBytes = 32 * 128;                     // of each of them
+constexpr int kProductSmem = kStages * kStageBytes + kReaders * kStagingBytes + 1024;   // and the alignment of the first block
+constexpr int kProductThreads = 128 + 32 * kReaders;
 constexpr int kRasterRows = 8;   // row tiles that are walked together: 8 x 9 tiles at once share operands in L2
-static_assert(kVocabTile == kTileN, "a tile of logits has one maximum and one sum a row");
+static_assert(kVocabTile == 128, "a reading warp's columns have one maximum and one sum a row");
 
 // ---------------------------------------------------------------------------
 // PTX
@@ -63,36 +73,56 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
     uint32_t ok;
     asm volatile(
         "{\n.reg .pred p;\n"
-        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n"
+        "selp.u32 %0, 1, 0, p;\n}"
+        : "=r"(ok) : "r"(bar), "r"(parity), "r"(1000000) : "memory");
+    return ok != 0;
+}
+// The same without waiting.
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n.reg .pred p;\n"
+        "mbarrier.test_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"
         "selp.u32 %0, 1, 0, p;\n}"
         : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok != 0;
 }
-// Bounded: gives up after two seconds, or 2^24 polls, whichever is first.
-__device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity) {
-    const unsigned long long t0 = global_timer_ns();
+// Bounded: gives up after 2^32 clocks (about two seconds), or 2^24 polls, whichever is first.
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) {
+    if (mbar_try(bar, parity)) return true;
+    const long long t0 = clock64();
+#pragma unroll 1
     for (int i = 0; i < (1 << 24); ++i) {
         if (mbar_try(bar, parity)) return true;
-        if ((i & 63) == 63 && global_timer_ns() - t0 > 2000000000ull) return false;
+        if ((i & 63) == 63 && clock64() - t0 > (1ll << 32)) return false;
     }
     return false;
 }
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) {
-#pragma unroll 1
-    for (int i = 0; i < 16; ++i)
-        if (mbar_try(bar, parity)) return true;
-    return mbar_wait_slow(bar, parity);
+// The whole warp waits and the outcome is a vote: with loops over values that the compiler knows to
+// be the same in all lanes, and one elected lane only for the instructions themselves, their
+// operands stay in uniform registers.  (A loop run by lane 0 alone moved six operands per product out
+// of ordinary registers and could not keep the tensor pipe fed: 61 % busy, 4096 x 4096 x 32000.)
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity) {
+    return __all_sync(0xffffffffu, mbar_wait(bar, parity));
+}
+__device__ __forceinline__ bool elected() {
+    uint32_t p;
+    asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(p));
+    return p != 0;
 }
 __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar_cluster) {
     asm volatile(
         "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
         ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar_cluster) : "memory");
 }
-__device__ __forceinline__ void mma_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+// Descriptors as their lower words (address, leading distance); the upper words are constants.
+__device__ __forceinline__ void mma_pair(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, bool accumulate) {
     asm volatile(
-        "{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n"
-        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}"
-        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+        "{\n.reg .pred p;\n.reg .b64 a, b;\nsetp.ne.b32 p, %5, 0;\n"
+        "mov.b64 a, {%1, %3};\nmov.b64 b, {%2, %3};\n"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], a, b, %4, p;\n}"
+        ::"r"(d), "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"((uint32_t)accumulate) : "memory");
 }
 // Arrives at the barrier of this offset in both CTAs once the products issued so far are done.
 __device__ __forceinline__ void commit_pair(uint32_t bar) {
@@ -100,22 +130,57 @@ __device__ __forceinline__ void commit_pair(uint32_t bar) {
         "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
         ::"r"(bar), "h"((uint16_t)3) : "memory");
 }
-// 32 columns of this thread's lane.  All lanes of the warp take part, whatever rows they have.
-__device__ __forceinline__ void tmem_ld32(uint32_t addr, float (&v)[32]) {
-    uint32_t r[32];
+// 64 columns of this thread's lane.  All lanes of the warp take part, whatever rows they have.
+__device__ __forceinline__ void tmem_ld64(uint32_t addr, float (&v)[64]) {
+    uint32_t r[64];
     __syncwarp();
     asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n"
+        "tcgen05.ld.sync.aligned.32x32b.x64.b32 {"
+        "%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, "
+        "%32, %33, %34, %35, %36, %37, %38, %39, %40, %41, %42, %43, %44, %45, %46, %47, "
+        "%48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, %62, %63}, [%64];\n"
         "tcgen05.wait::ld.sync.aligned;"
         : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
           "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
           "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
-          "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+          "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]),
+          "=r"(r[32]), "=r"(r[33]), "=r"(r[34]), "=r"(r[35]), "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]),
+          "=r"(r[40]), "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47]),
+          "=r"(r[48]), "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]), "=r"(r[54]), "=r"(r[55]),
+          "=r"(r[56]), "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]), "=r"(r[62]), "=r"(r[63])
         : "r"(addr) : "memory");
 #pragma unroll
-    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+    for (int i = 0; i < 64; ++i) v[i] = __uint_as_float(r[i]);
+}
+// A warp's 32 rows x 128 bytes in shared memory to global memory: 16-byte words are stored at
+// (word ^ row mod 8), the 128-byte swizzle of the tensor map.
+__device__ __forceinline__ void stage_word(uint32_t staging, int row, int word, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};"
+                 ::"r"(staging + row * 128 + ((word ^ (row & 7)) << 4)), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+// the staging memory may be written again
+__device__ __forceinline__ void stage_reuse(int lane) {
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+    __syncwarp();
+}
+__device__ __forceinline__ void stage_store(uint32_t staging, int lane, const CUtensorMap* map, int x, int y) {
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    if (lane == 0) {
+        asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];"
+                     ::"l"(map), "r"(x), "r"(y), "r"(staging) : "memory");
+        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+    }
+}
+__device__ __forceinline__ void stage_add(uint32_t staging, int lane, const CUtensorMap* map, int x, int y) {
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    if (lane == 0) {
+        asm volatile("cp.reduce.async.bulk.tensor.2d.global.shared::cta.add.tile.bulk_group [%0, {%1, %2}], [%3];"
+                     ::"l"(map), "r"(x), "r"(y), "r"(staging) : "memory");
+        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+    }
 }
 
 // Shared-memory descriptors, 128-byte swizzle.  K-major: rows of 128 bytes (64 values of the summed
@@ -124,126 +189,164 @@ __device__ __forceinline__ void tmem_ld32(uint32_t addr, float (&v)[32]) {
 // axis; the next 64 are a box (64 rows, 8192 bytes) away, the next 8 of the summed axis 1024
 // bytes; 16 further along the summed axis are 2048 bytes.
 template <bool MN>
-__device__ __forceinline__ uint64_t operand_desc(uint32_t addr) {
-    const uint64_t lead = MN ? 8192 / 16 : 1, stride = 1024 / 16;
-    return (uint64_t)((addr & 0x3ffff) >> 4) | lead << 16 | stride << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+__device__ __forceinline__ uint32_t operand_lo(uint32_t addr) {
+    return (addr & 0x3ffff) >> 4 | (MN ? 8192u / 16 : 1u) << 16;
 }
+constexpr uint32_t kOperandHi = 1024 / 16 | 1u << 14 | 2u << 29;
 
 struct ProductArgs {
     VocabCall c;
     int64_t v0, v1;
     int first;       // kDh: overwrite the partial sums
     int splits;      // kDh: parts of the summed axis
-    int wide;        // kDw: rows of dw start on 16-byte boundaries
+    int wide;        // kDw: rows of dw start and end on 16-byte boundaries
+};
+
+// What a reading warp finishes: 128 columns of 32 rows.
+struct Patch {
+    uint32_t tmem;       // its lanes and first column
+    uint32_t staging;
+    int lane;
+    int64_t row0;        // of the warp; the thread's row is row0 + lane
+    int64_t col0;        // of the 128
+    int64_t cols;        // columns of the result from col0 on (may be more than 128, or none)
 };
 
 template <int P, bool F16, bool EDGE>
-__device__ __forceinline__ void read_logits(const ProductArgs& p, uint32_t tmem, int64_t row, int n_valid, int64_t col0, int cols) {
+__device__ __forceinline__ void read_logits(const ProductArgs& p, const Patch& w, const CUtensorMap* out, int n_valid) {
     const VocabCall& c = p.c;
-    float v[32];
+    const int64_t row = w.row0 + w.lane;
+    const int cols = (int)(w.cols < 128 ? w.cols : 128);
+    float v[64];
     float m = -INFINITY;
 #pragma unroll 1
-    for (int ch = 0; ch < kTileN / 32; ++ch) {
-        tmem_ld32(tmem + ch * 32, v);
+    for (int ch = 0; ch < 2; ++ch) {
+        tmem_ld64(w.tmem + ch * 64, v);
 #pragma unroll
-        for (int i = 0; i < 32; ++i)
-            if (!EDGE || ch * 32 + i < cols) m = fmaxf(m, v[i]);
+        for (int i = 0; i < 64; ++i)
+            if (!EDGE || ch * 64 + i < cols) m = fmaxf(m, v[i]);
     }
     const float ref = m == -INFINITY ? 0.f : m;   // all -inf: every term is exp(-inf)
     const float step = -c.zscale * kept_steps<F16>();
     float s[4] = {};
-    uint4* to = (uint4*)(c.e + row * c.vb + (col0 - p.v0));
 #pragma unroll 1
-    for (int ch = 0; ch < kTileN / 32; ++ch) {
-        tmem_ld32(tmem + ch * 32, v);
-        unsigned code[16];
+    for (int ch = 0; ch < 2; ++ch) {
+        tmem_ld64(w.tmem + ch * 64, v);
+        if constexpr (P == kLogitsKeep) stage_reuse(w.lane);
 #pragma unroll
-        for (int i = 0; i < 32; ++i) {
-            const float d = v[i] - ref;
-            const float e = exp2_fast(d * c.zscale);
-            if (!EDGE || ch * 32 + i < cols) s[i & 3] += e;
-            if constexpr (P == kLogitsKeep) {
-                // 2^23 + x has x in its low bits; 65535 steps stand for themselves and more
-                const unsigned x = __float_as_uint(fminf(fmaf(d, step, 8388608.f), 8388608.f + 65535.f));
-                if (i & 1) code[i >> 1] = __byte_perm(code[i >> 1], x, 0x5410);
-                else code[i >> 1] = x;
-            }
-        }
-        if constexpr (P == kLogitsKeep) {
-            if (row < n_valid) {
+        for (int g = 0; g < 8; ++g) {
+            unsigned code[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) to[ch * 4 + i] = make_uint4(code[4 * i], code[4 * i + 1], code[4 * i + 2], code[4 * i + 3]);
+            for (int i = 0; i < 8; ++i) {
+                const float d = v[g * 8 + i] - ref;
+                const float e = exp2_fast(d * c.zscale);
+                if (!EDGE || ch * 64 + g * 8 + i < cols) s[i & 3] += e;
+                if constexpr (P == kLogitsKeep) {
+                    // 2^23 + x has x in its low bits; 65535 steps stand for themselves and more
+                    const unsigned x = __float_as_uint(fminf(fmaf(d, step, 8388608.f), 8388608.f + 65535.f));
+                    if (i & 1) code[i >> 1] = __byte_perm(code[i >> 1], x, 0x5410);
+                    else code[i >> 1] = x;
+                }
             }
+            if constexpr (P == kLogitsKeep) stage_word(w.staging, w.lane, g, code[0], code[1], code[2], code[3]);
         }
+        if constexpr (P == kLogitsKeep)
+            if (!EDGE || ch * 64 < cols) stage_store(w.staging, w.lane, out, (int)(w.col0 - p.v0) + ch * 64, (int)w.row0);
     }
-    if (row < n_valid) c.part[col0 / kVocabTile * c.n_pad + row] = make_float2(m * c.zscale, (s[0] + s[1]) + (s[2] + s[3]));
+    if (row < n_valid) c.part[w.col0 / kVocabTile * c.n_pad + row] = make_float2(m * c.zscale, (s[0] + s[1]) + (s[2] + s[3]));
 }
 
 template <bool F16>
-__device__ __forceinline__ void read_gradients(const ProductArgs& p, uint32_t tmem, int64_t row, int n_valid, int64_t col0) {
+__device__ __forceinline__ void read_gradients(const ProductArgs& p, const Patch& w, const CUtensorMap* out, int n_valid) {
     const VocabCall& c = p.c;
+    const int64_t row = w.row0 + w.lane;
     VocabRow vr = {};
     if (row < n_valid) vr = c.row[row];
-    uint4* to = (uint4*)(c.e + row * c.vb + (col0 - p.v0));
 #pragma unroll 1
-    for (int ch = 0; ch < kTileN / 32; ++ch) {
-        float v[32];
-        tmem_ld32(tmem + ch * 32, v);
-        unsigned o[16];
+    for (int ch = 0; ch < 2; ++ch) {
+        if (ch * 64 >= w.cols) break;
+        float v[64];
+        tmem_ld64(w.tmem + ch * 64, v);
+        stage_reuse(w.lane);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const float a = vr.coef * exp2_fast(fmaf(v[2 * i], c.zscale, -vr.lse2));
-            const float b = vr.coef * exp2_fast(fmaf(v[2 * i + 1], c.zscale, -vr.lse2));
-            o[i] = row < n_valid ? pack16<F16>(a, b) : 0u;    // rows up to the padding are summed over by dw
+        for (int g = 0; g < 8; ++g) {
+            unsigned o[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float a = vr.coef * exp2_fast(fmaf(v[g * 8 + 2 * i], c.zscale, -vr.lse2));
+                const float b = vr.coef * exp2_fast(fmaf(v[g * 8 + 2 * i + 1], c.zscale, -vr.lse2));
+                o[i] = row < n_valid ? pack16<F16>(a, b) : 0u;    // rows up to the padding are summed over by dw
+            }
+            stage_word(w.staging, w.lane, g, o[0], o[1], o[2], o[3]);
         }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) to[ch * 4 + i] = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+        stage_store(w.staging, w.lane, out, (int)(w.col0 - p.v0) + ch * 64, (int)w.row0);
     }
 }
 
 template <bool F16>
-__device__ __forceinline__ void read_dw(const ProductArgs& p, uint32_t tmem, int64_t row, int64_t rows, int64_t col0, bool empty) {
+__device__ __forceinline__ void read_dw(const ProductArgs& p, const Patch& w, const CUtensorMap* out, bool empty) {
     const VocabCall& c = p.c;
     const float inv = c.ctl->inv_scale;
-    uint16_t* to = (uint16_t*)c.dw + (p.v0 + row) * c.lddw + col0;
+    const int64_t rows = p.v1 - p.v0 - w.row0;   // rows of the result from the warp's first on
+    if (rows <= 0) return;
 #pragma unroll 1
-    for (int ch = 0; ch < kTileN / 32; ++ch) {
-        if (col0 + ch * 32 >= c.D) break;
-        float v[32];
-        tmem_ld32(tmem + ch * 32, v);
-        if (row >= rows) continue;
+    for (int ch = 0; ch < 2; ++ch) {
+        if (ch * 64 >= w.cols) break;
+        float v[64];
+        tmem_ld64(w.tmem + ch * 64, v);
+        stage_reuse(w.lane);
 #pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] = empty ? 0.f : v[i] * inv;
-        if (p.wide && col0 + ch * 32 + 32 <= c.D) {
+        for (int i = 0; i < 64; ++i) v[i] = empty ? 0.f : v[i] * inv;
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                ((uint4*)to)[ch * 4 + i] = make_uint4(pack16<F16>(v[8 * i], v[8 * i + 1]), pack16<F16>(v[8 * i + 2], v[8 * i + 3]),
-                                                      pack16<F16>(v[8 * i + 4], v[8 * i + 5]), pack16<F16>(v[8 * i + 6], v[8 * i + 7]));
+        for (int g = 0; g < 8; ++g)
+            stage_word(w.staging, w.lane, g, pack16<F16>(v[8 * g], v[8 * g + 1]), pack16<F16>(v[8 * g + 2], v[8 * g + 3]),
+                       pack16<F16>(v[8 * g + 4], v[8 * g + 5]), pack16<F16>(v[8 * g + 6], v[8 * g + 7]));
+        if (p.wide) {
+            stage_store(w.staging, w.lane, out, (int)w.col0 + ch * 64, (int)w.row0);
         } else {
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-                if (col0 + ch * 32 + i < c.D) to[ch * 32 + i] = to16<F16>(v[i]);
+            // rows on any boundary: a row at a time, two columns a lane
+            __syncwarp();
+            const int64_t col = w.col0 + ch * 64 + w.lane * 2;
+            uint16_t* to = (uint16_t*)c.dw + (p.v0 + w.row0) * c.lddw + col;
+#pragma unroll 8
+            for (int r = 0; r < 32; ++r, to += c.lddw) {
+                uint32_t x;
+                asm volatile("ld.shared.b32 %0, [%1];"
+                             : "=r"(x) : "r"(w.staging + r * 128 + (((w.lane >> 2) ^ (r & 7)) << 4) + (w.lane & 3) * 4) : "memory");
+                if (r >= rows) continue;
+                if (col + 1 < c.D && ((uintptr_t)to & 3) == 0) *(uint32_t*)to = x;
+                else {
+                    if (col < c.D) to[0] = (uint16_t)x;
+                    if (col + 1 < c.D) to[1] = (uint16_t)(x >> 16);
+                }
+            }
+            __syncwarp();
         }
     }
 }
 
-__device__ __forceinline__ void read_dh(const ProductArgs& p, uint32_t tmem, int64_t row, int n_valid, int64_t col0, int split, bool empty) {
-    const VocabCall& c = p.c;
-    float4* to = (float4*)(c.dhp + ((int64_t)split * c.n_pad + row) * c.Dp + col0);
+__device__ __forceinline__ void read_dh(const ProductArgs& p, const Patch& w, const CUtensorMap* out, int n_valid, int split, bool empty) {
+    if (w.row0 >= n_valid) return;
+    const int y = (int)(split * p.c.n_pad + w.row0);
 #pragma unroll 1
-    for (int ch = 0; ch < kTileN / 32; ++ch) {
-        if (col0 + ch * 32 >= c.Dp) break;
-        float v[32];
-        tmem_ld32(tmem + ch * 32, v);
-        if (row >= n_valid) continue;
+    for (int ch = 0; ch < 2; ++ch) {
+        if (ch * 64 >= w.cols) break;
+        float v[64];
+        tmem_ld64(w.tmem + ch * 64, v);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            float4 x = empty ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
-            if (!p.first) {
-                const float4 y = to[ch * 8 + i];
-                x = make_float4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w);
+        for (int i = 0; i < 64; ++i) v[i] = empty ? 0.f : v[i];
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            stage_reuse(w.lane);
+#pragma unroll
+            for (int g = 0; g < 8; ++g) {
+                const float* x = v + half * 32 + g * 4;
+                stage_word(w.staging, w.lane, g, __float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
             }
-            to[ch * 8 + i] = x;
+            const int x0 = (int)w.col0 + ch * 64 + half * 32;
+            // one tile adds to an element and launches follow one another: the order is fixed
+            if (p.first) stage_store(w.staging, w.lane, out, x0, y);
+            else stage_add(w.staging, w.lane, out, x0, y);
         }
     }
 }
@@ -271,22 +374,23 @@ struct Tiles {
 template <int P, bool F16>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1)
 k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
-                const __grid_constant__ ProductArgs p) {
+                const __grid_constant__ CUtensorMap map_out, const __grid_constant__ ProductArgs p) {
     constexpr bool kMnA = P == kDw, kMnB = P == kDw || P == kDh;
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t bar_full[kStages], bar_empty[kStages], bar_sum[2], bar_free[2], bar_drain;
     __shared__ uint32_t tmem_slot;
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, lane = tid & 31;
+    const int warp = (int)__reduce_max_sync(0xffffffffu, (unsigned)tid >> 5);
     const uint32_t rank = cluster_rank();
-    const uint32_t stage0 = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const uint32_t stage0 = (smem_u32(smem_raw) + 1023u) & ~1023u, staging0 = stage0 + kStages * kStageBytes;
     const VocabCall& c = p.c;
-    const int n_valid = c.ctl->n_valid;
+    const int n_valid = (int)__reduce_max_sync(0xffffffffu, (unsigned)c.ctl->n_valid);   // one value, known as such
 
     Tiles tiles;
     {
         const int64_t nv = p.v1 - p.v0, rows = ((int64_t)n_valid + kTileM - 1) / kTileM;
         tiles.tm = P == kDw ? (nv + kTileM - 1) / kTileM : rows;
-        tiles.tn = P == kDw || P == kDh ? (c.D + kTileN - 1) / kTileN : (nv + kTileN - 1) / kTileN;
+        tiles.tn = ((P == kDw || P == kDh ? c.D : nv) + kTileN - 1) / kTileN;
         const int64_t K = P == kDw ? n_valid : P == kDh ? nv : c.D;
         tiles.kb = (int)((K + kBlockK - 1) / kBlockK);
         tiles.splits = P == kDh ? p.splits : 1;
@@ -301,7 +405,7 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(smem_u32(&bar_sum[b]), 1);
-            mbar_init(smem_u32(&bar_free[b]), 8);     // four warps of each CTA
+            mbar_init(smem_u32(&bar_free[b]), 2 * kReaders);
         }
         mbar_init(smem_u32(&bar_drain), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -316,22 +420,25 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = tmem_slot;
 
+    const int64_t n_cols = P == kDw || P == kDh ? c.D : p.v1 - p.v0;   // of the result
     bool ok = true;
     if (warp == 0) {
-        // producer: this CTA's 128 rows of A and of B; the leader's barrier counts both CTAs' bytes
-        if (lane == 0) {
-            int stage = 0;
-            uint32_t phase = 0;
-            for (int64_t t = cluster; t < tiles.total && ok; t += clusters) {
-                int64_t m, n;
-                int split, k0, k1;
-                tiles.at(t, m, n, split);
-                tiles.blocks(split, k0, k1);
-                const int ma = (int)(m * kTileM + rank * 128), nb = (int)(n * kTileN + rank * 128);
-                for (int k = k0; k < k1; ++k) {
-                    if (!(ok = mbar_wait(smem_u32(&bar_empty[stage]), phase ^ 1))) break;
+        // producer: this CTA's 128 rows of A and of each half of B; the leader's barrier counts both CTAs' bytes
+        int stage = 0;
+        uint32_t phase = 0;
+        for (int64_t t = cluster; t < tiles.total && ok; t += clusters) {
+            int64_t m, n;
+            int split, k0, k1;
+            tiles.at(t, m, n, split);
+            tiles.blocks(split, k0, k1);
+            const bool two = n * kTileN + kHalfN < n_cols;
+            const int ma = (int)(m * kTileM + rank * 128), nb = (int)(n * kTileN + rank * 128);
+            const uint32_t bytes = 2 * (two ? 3 : 2) * kOperandBytes;
+            for (int k = k0; k < k1; ++k) {
+                if (!(ok = warp_wait(smem_u32(&bar_empty[stage]), phase ^ 1))) break;
+                if (elected()) {
                     const uint32_t full = smem_u32(&bar_full[stage]);
-                    if (rank == 0) mbar_expect(full, 2 * kStageBytes);
+                    if (rank == 0) mbar_expect(full, bytes);
                     const uint32_t bar = in_cta(full, 0);
                     const uint32_t a = stage0 + stage * kStageBytes, b = a + kOperandBytes;
                     if constexpr (kMnA) {
@@ -340,84 +447,147 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                     } else {
                         tma_load(a, &map_a, k * kBlockK, ma, bar);
                     }
-                    const int vrow = (P == kDh ? (int)p.v0 : 0) + k * kBlockK;
                     if constexpr (kMnB) {
-                        tma_load(b, &map_b, nb, vrow, bar);
-                        tma_load(b + 8192, &map_b, nb + 64, vrow, bar);
+                        const int y = (P == kDh ? (int)p.v0 : 0) + k * kBlockK;
+                        tma_load(b, &map_b, nb, y, bar);
+                        tma_load(b + 8192, &map_b, nb + 64, y, bar);
+                        if (two) {
+                            tma_load(b + kOperandBytes, &map_b, nb + kHalfN, y, bar);
+                            tma_load(b + kOperandBytes + 8192, &map_b, nb + kHalfN + 64, y, bar);
+                        }
                     } else {
                         tma_load(b, &map_b, k * kBlockK, (int)p.v0 + nb, bar);
+                        if (two) tma_load(b + kOperandBytes, &map_b, k * kBlockK, (int)p.v0 + nb + kHalfN, bar);
                     }
-                    if (++stage == kStages) { stage = 0; phase ^= 1; }
                 }
+                __syncwarp();
+                if (++stage == kStages) { stage = 0; phase ^= 1; }
             }
-            if (!ok && rank == 0)   // the copies in flight land before the memory is given back
-                for (int s = 0; s < kStages; ++s) mbar_wait(smem_u32(&bar_full[s]), s < stage ? phase : phase ^ 1);
         }
-        __syncwarp();
+        if (!ok && rank == 0)   // the copies in flight land before the memory is given back
+            for (int s = 0; s < kStages; ++s) mbar_wait(smem_u32(&bar_full[s]), s < stage ? phase : phase ^ 1);
     } else if (warp == 1) {
-        if (rank == 0 && lane == 0) {
+        if (rank == 0) {
             constexpr uint32_t idesc = 1u << 4 | (F16 ? 0u : 1u) << 7 | (F16 ? 0u : 1u) << 10 | (kMnA ? 1u : 0u) << 15 |
-                                       (kMnB ? 1u : 0u) << 16 | (uint32_t)(kTileN / 8) << 17 | (uint32_t)(kTileM / 16) << 24;
-            int stage = 0, buf = 0;
-            uint32_t phase = 0, free_phase = 0;
+                                       (kMnB ? 1u : 0u) << 16 | (uint32_t)(kHalfN / 8) << 17 | (uint32_t)(kTileM / 16) << 24;
+            constexpr uint32_t step_a = (kMnA ? 2048 : 32) / 16, step_b = (kMnB ? 2048 : 32) / 16;
+            const uint32_t a0 = operand_lo<kMnA>(stage0), b0 = operand_lo<kMnB>(stage0 + kOperandBytes);
+            // one block of one half, by the elected lane
+            auto issue = [&](int stage, int half, bool fresh) {
+                const uint32_t a = a0 + stage * (kStageBytes / 16), b = b0 + stage * (kStageBytes / 16) + half * (kOperandBytes / 16);
+                const uint32_t d = tmem + half * kHalfN;
+                mma_pair(d, a, b, kOperandHi, idesc, !fresh);
+#pragma unroll
+                for (int j = 1; j < kBlockK / 16; ++j) mma_pair(d, a + j * step_a, b + j * step_b, kOperandHi, idesc, true);
+            };
+            int stage_a = 0, stage_b = 0;     // next block of the first half, of the second half
+            uint32_t phase = 0, free0 = 0, free1 = 0;
             for (int64_t t = cluster; t < tiles.total && ok; t += clusters) {
                 int64_t m, n;
                 int split, k0, k1;
                 tiles.at(t, m, n, split);
                 tiles.blocks(split, k0, k1);
-                if (!(ok = mbar_wait(smem_u32(&bar_free[buf]), free_phase ^ 1))) break;
+                const int blocks = k1 - k0;
+                const bool two = n * kTileN + kHalfN < n_cols;
+                if (!(ok = warp_wait(smem_u32(&bar_free[0]), free0 ^ 1))) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                for (int k = k0; k < k1; ++k) {
-                    if (!(ok = mbar_wait(smem_u32(&bar_full[stage]), phase))) break;
+                free0 ^= 1;
+                int a = 0, b = 0;             // blocks issued for each half
+                auto first_half = [&](bool release) {
+                    ok = warp_wait(smem_u32(&bar_full[stage_a]), phase);
+                    if (!ok) return;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const uint32_t a = stage0 + stage * kStageBytes, b = a + kOperandBytes;
-#pragma unroll
-                    for (int j = 0; j < kBlockK / 16; ++j)
-                        mma_pair(tmem + buf * kTileN, operand_desc<kMnA>(a + j * (kMnA ? 2048 : 32)),
-                                 operand_desc<kMnB>(b + j * (kMnB ? 2048 : 32)), idesc, k > k0 || j > 0);
-                    commit_pair(smem_u32(&bar_empty[stage]));
-                    if (++stage == kStages) { stage = 0; phase ^= 1; }
+                    if (elected()) {
+                        issue(stage_a, 0, a == 0);
+                        if (release) commit_pair(smem_u32(&bar_empty[stage_a]));
+                        if (a + 1 == blocks) commit_pair(smem_u32(&bar_sum[0]));
+                    }
+                    __syncwarp();
+                    ++a;
+                    if (++stage_a == kStages) { stage_a = 0; phase ^= 1; }
+                };
+                auto second_half = [&]() {
+                    if (elected()) {
+                        issue(stage_b, 1, b == 0);
+                        commit_pair(smem_u32(&bar_empty[stage_b]));
+                        if (b + 1 == blocks) commit_pair(smem_u32(&bar_sum[1]));
+                    }
+                    __syncwarp();
+                    ++b;
+                    if (++stage_b == kStages) stage_b = 0;
+                };
+                if (blocks == 0 && elected()) commit_pair(smem_u32(&bar_sum[0]));
+                __syncwarp();
+                if (!two) {
+                    while (a < blocks && ok) first_half(true);
+                    stage_b = stage_a;
+                    continue;
                 }
-                if (!ok) break;
-                commit_pair(smem_u32(&bar_sum[buf]));
-                if (++buf == 2) { buf = 0; free_phase ^= 1; }
+                // ahead, as far as blocks are in flight, while the second half's sums are still being read out
+                while (ok && a < blocks && a < kStages && !__all_sync(0xffffffffu, mbar_test(smem_u32(&bar_free[1]), free1 ^ 1))) first_half(false);
+                if (!ok || !(ok = warp_wait(smem_u32(&bar_free[1]), free1 ^ 1))) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                free1 ^= 1;
+                if (blocks == 0 && elected()) commit_pair(smem_u32(&bar_sum[1]));
+                __syncwarp();
+                while (b < a && a < blocks) second_half();
+                while (ok && a < blocks - kStages) {
+                    first_half(false);
+                    if (ok) second_half();
+                }
+                while (ok && a < blocks) first_half(false);      // ahead over the last blocks
+                if (ok) while (b < blocks) second_half();
             }
             if (!ok) {   // products in flight end before the tensor memory is freed
-                commit_pair(smem_u32(&bar_drain));
+                if (elected()) commit_pair(smem_u32(&bar_drain));
+                __syncwarp();
                 mbar_wait(smem_u32(&bar_drain), 0);
             }
         }
-        __syncwarp();
     } else if (warp >= 4) {
-        const int quarter = warp & 3;    // the tensor memory lanes this warp can read
-        int buf = 0;
-        uint32_t phase = 0;
-        for (int64_t t = cluster; t < tiles.total; t += clusters) {
+        const int quarter = warp & 3, side = (warp - 4) >> 2;    // the tensor memory lanes this warp can read; its columns
+        uint32_t phases = 0;    // a bit for each half
+        Patch w;
+        w.lane = lane;
+        w.staging = staging0 + (warp - 4) * kStagingBytes;
+        for (int64_t t = cluster; t < tiles.total && ok; t += clusters) {
             int64_t m, n;
             int split, k0, k1;
             tiles.at(t, m, n, split);
             tiles.blocks(split, k0, k1);
-            ok = mbar_wait(smem_u32(&bar_sum[buf]), phase);
-            if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const uint32_t from = tmem + buf * kTileN + ((uint32_t)(quarter * 32) << 16);
-            const int64_t row = m * kTileM + rank * 128 + quarter * 32 + lane, col0 = n * kTileN;
-            if constexpr (P == kLogits || P == kLogitsKeep) {
-                const int64_t left = p.v1 - p.v0 - col0;
-                if (left >= kTileN) read_logits<P, F16, false>(p, from, row, n_valid, p.v0 + col0, kTileN);
-                else read_logits<P, F16, true>(p, from, row, n_valid, p.v0 + col0, (int)left);
-            } else if constexpr (P == kAgain) {
-                read_gradients<F16>(p, from, row, n_valid, p.v0 + col0);
-            } else if constexpr (P == kDw) {
-                read_dw<F16>(p, from, row, p.v1 - p.v0, col0, k0 == k1);
-            } else {
-                read_dh(p, from, row, n_valid, col0, split, k0 == k1);
+            const int halves = n * kTileN + kHalfN < n_cols ? 2 : 1;
+            w.row0 = m * kTileM + rank * 128 + quarter * 32;
+#pragma unroll 1
+            for (int h = 0; h < halves; ++h) {
+                ok = mbar_wait(smem_u32(&bar_sum[h]), phases >> h & 1);
+                if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+                phases ^= 1u << h;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const int64_t col = n * kTileN + h * kHalfN + side * 128;
+                w.tmem = tmem + h * kHalfN + side * 128 + ((uint32_t)(quarter * 32) << 16);
+                w.cols = n_cols - col;
+                if (w.cols > 0) {
+                    if constexpr (P == kLogits || P == kLogitsKeep) {
+                        w.col0 = p.v0 + col;
+                        if (w.cols >= 128) read_logits<P, F16, false>(p, w, &map_out, n_valid);
+                        else read_logits<P, F16, true>(p, w, &map_out, n_valid);
+                    } else if constexpr (P == kAgain) {
+                        w.col0 = p.v0 + col;
+                        read_gradients<F16>(p, w, &map_out, n_valid);
+                    } else if constexpr (P == kDw) {
+                        w.col0 = col;
+                        read_dw<F16>(p, w, &map_out, k0 == k1);
+                    } else {
+                        w.col0 = col;
+                        read_dh(p, w, &map_out, n_valid, split, k0 == k1);
+                    }
+                }
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive_remote(in_cta(smem_u32(&bar_free[h]), 0));
             }
-            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-            __syncwarp();
-            if (lane == 0) mbar_arrive_remote(in_cta(smem_u32(&bar_free[buf]), 0));
-            if (++buf == 2) { buf = 0; phase ^= 1; }
         }
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
     if (!ok) atomicOr(&c.ctl->status, (unsigned)GK_DEV_TIMEOUT);
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -450,16 +620,19 @@ static EncodeFn encode_fn() {
     return fn;
 }
 
-// Rows of `cols` 16-bit values, `pitch` values apart, in boxes of 64 values and `box_rows` rows.
-// Every x a kernel starts a box at is a multiple of 64 values, so every copy starts on 16 bytes.
-static int make_map(CUtensorMap* map, bool f16, const void* base, int64_t cols, int64_t rows, int64_t pitch, int box_rows) {
+// Rows of `cols` values, `pitch` values apart, in boxes of 128 bytes and `box_rows` rows.  Every x
+// a kernel starts a box at is a multiple of 64 16-bit or 32 fp32 values, so every copy starts on 16 bytes.
+enum Element { kBf16, kF16, kF32 };
+static int make_map(CUtensorMap* map, Element type, const void* base, int64_t cols, int64_t rows, int64_t pitch, int box_rows) {
     EncodeFn fn = encode_fn();
     if (!fn) return cuda_fail(cudaErrorNotSupported);
-    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)(2 * pitch)};
-    const cuuint32_t box[2] = {64, (cuuint32_t)box_rows}, steps[2] = {1, 1};
-    const CUresult r = fn(map, f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base),
-                          dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                          CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    const int size = type == kF32 ? 4 : 2;
+    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)(size * pitch)};
+    const cuuint32_t box[2] = {(cuuint32_t)(128 / size), (cuuint32_t)box_rows}, steps[2] = {1, 1};
+    const CUtensorMapDataType t = type == kF32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                : type == kF16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+    const CUresult r = fn(map, t, 2, const_cast<void*>(base), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                          CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? GK_OK : cuda_fail(cudaErrorInvalidValue);
 }
 
@@ -468,17 +641,23 @@ static int launch_product(const ProductArgs& p, int sm_count, cudaStream_t st) {
     const VocabCall& c = p.c;
     const void* w = c.wc ? (const void*)c.wc : c.w;
     const int64_t ldw = c.wc ? c.Dp : c.ldw, nv = p.v1 - p.v0;
-    CUtensorMap a, b;
+    const Element type = F16 ? kF16 : kBf16;
+    CUtensorMap a, b, out;
     int rc;
     if (P == kDw) {
-        rc = make_map(&a, c.f16, c.e, nv, c.n_pad, c.vb, 64);
-        if (rc == GK_OK) rc = make_map(&b, c.f16, c.hc, c.Dp, c.n_pad, c.Dp, 64);
+        rc = make_map(&a, type, c.e, nv, c.n_pad, c.vb, 64);
+        if (rc == GK_OK) rc = make_map(&b, type, c.hc, c.Dp, c.n_pad, c.Dp, 64);
+        out = a;    // rows on other boundaries are stored without a map
+        if (rc == GK_OK && p.wide) rc = make_map(&out, type, (const uint16_t*)c.dw + p.v0 * c.lddw, c.D, nv, c.lddw, 32);
     } else if (P == kDh) {
-        rc = make_map(&a, c.f16, c.e, nv, c.n_pad, c.vb, 128);
-        if (rc == GK_OK) rc = make_map(&b, c.f16, w, c.D, c.V, ldw, 64);
+        rc = make_map(&a, type, c.e, nv, c.n_pad, c.vb, 128);
+        if (rc == GK_OK) rc = make_map(&b, type, w, c.D, c.V, ldw, 64);
+        if (rc == GK_OK) rc = make_map(&out, kF32, c.dhp, c.Dp, p.splits * c.n_pad, c.Dp, 32);
     } else {
-        rc = make_map(&a, c.f16, c.hc, c.Dp, c.n_pad, c.Dp, 128);
-        if (rc == GK_OK) rc = make_map(&b, c.f16, w, c.D, c.V, ldw, 128);
+        rc = make_map(&a, type, c.hc, c.Dp, c.n_pad, c.Dp, 128);
+        if (rc == GK_OK) rc = make_map(&b, type, w, c.D, c.V, ldw, 128);
+        out = a;    // kLogits keeps nothing
+        if (rc == GK_OK && P != kLogits) rc = make_map(&out, type, c.e, nv, c.n_pad, c.vb, 32);
     }
     if (rc != GK_OK) return rc;
     const int64_t tm = ((P == kDw ? nv : c.n) + kTileM - 1) / kTileM;
@@ -486,7 +665,7 @@ static int launch_product(const ProductArgs& p, int sm_count, cudaStream_t st) {
     const int64_t pairs = tm * tn * (P == kDh ? p.splits : 1);
     const int64_t most = sm_count / 2 > 0 ? sm_count / 2 : 1;
     GK_CUDA_TRY(cudaFuncSetAttribute(k_vocab_product<P, F16>, cudaFuncAttributeMaxDynamicSharedMemorySize, kProductSmem));
-    k_vocab_product<P, F16><<<(unsigned)(2 * (pairs < most ? pairs : most)), kProductThreads, kProductSmem, st>>>(a, b, p);
+    k_vocab_product<P, F16><<<(unsigned)(2 * (pairs < most ? pairs : most)), kProductThreads, kProductSmem, st>>>(a, b, out, p);
     GK_CUDA_TRY(cudaGetLastError());
     note_launch();
     return GK_OK;
@@ -500,7 +679,8 @@ static int launch(const VocabCall& c, int64_t v0, int64_t v1, bool first, int sm
     p.v1 = v1;
     p.first = first;
     p.splits = c.splits > 0 ? c.splits : 1;
-    p.wide = (((uintptr_t)c.dw | (uintptr_t)(2 * c.lddw)) & 15) == 0;
+    // (the copies' hardware cuts a row's end in steps of 16 bytes, so the rows' length counts too)
+    p.wide = (((uintptr_t)c.dw | (uintptr_t)(2 * c.lddw) | (uintptr_t)(2 * c.D)) & 15) == 0;
     return c.f16 ? launch_product<P, true>(p, sm_count, st) : launch_product<P, false>(p, sm_count, st);
 }
 
@@ -517,9 +697,21 @@ int launch_vocab_dh(const VocabCall& c, int64_t v0, int64_t v1, bool first, int 
     return launch<kDh>(c, v0, v1, first, sm_count, st);
 }
 
+// Into how many parts the summed axis of dh is split.  dh has few tiles (rows / 256 x D / 512) and a
+// long sum, so without parts most pairs of SMs would idle; each part costs a write and a read of
+// fp32 sums.  The estimate: rounds of tiles at 0.55 us a block of 64 and 4 us a tile, and the sums at
+// 5 TB/s.
 int vocab_dh_splits(int64_t n, int64_t D, int64_t vb, int sm_count) {
-    (void)n; (void)D; (void)vb; (void)sm_count;
-    return 1;
+    const int64_t tiles = (n + kTileM - 1) / kTileM * ((D + kTileN - 1) / kTileN), kb = (vb + kBlockK - 1) / kBlockK;
+    const int64_t pairs = sm_count / 2 > 0 ? sm_count / 2 : 1;
+    int best = 1;
+    double least = 0;
+    for (int s = 1; s <= 32 && (s == 1 || s * 4 <= kb); ++s) {
+        const double rounds = (double)((tiles * s + pairs - 1) / pairs), blocks = (double)((kb + s - 1) / s);
+        const double us = rounds * (0.55 * blocks + 4.0) + (double)s * (double)n * (double)D * 8.0 / 5e6;
+        if (s == 1 || us < least) { least = us; best = s; }
+    }
+    return best;
 }
 
 }  // namespace gk

@@ -129,6 +129,25 @@ def test_row_strides_and_unaligned_rows(pad, shift):
     hard_loss(70, 131, 401, torch.float16, seed=7, pad=pad, shift=shift)
 
 
+@pytest.mark.parametrize("D,pad", [(131, 5), (136, 8), (1, 7), (60, 4)])
+def test_what_lies_between_the_rows_does_not_matter(D, pad):
+    n, V = 70, 401
+    gen = torch.Generator().manual_seed(12)
+    h, w = torch.randn(n, D, generator=gen).half().to(DEV), torch.randn(V, D, generator=gen).half().to(DEV)
+    target = torch.randint(0, V, (n,), generator=gen).to(DEV)
+    outs = []
+    for fill in (0.0, math.nan):
+        hp, wp = (torch.full((t.shape[0], D + pad), fill, dtype=torch.float16, device=DEV)[:, :D] for t in (h, w))
+        hp.copy_(h)
+        wp.copy_(w)
+        out = Out(n, D, V, torch.float16)
+        gk.gk_vocab_loss(hp, wp, target, out.loss[:n], out.lse[:n], dh=out.dh, dw=out.dw)
+        outs.append(out)
+    a, b = outs
+    for x, y in ((a.loss, b.loss), (a.lse, b.lse), (a.dh, b.dh), (a.dw, b.dw)):
+        assert torch.equal(x, y) and bool(torch.isfinite(x).all())
+
+
 @pytest.mark.parametrize("dh,dw", [(True, False), (False, True), (False, False)])
 def test_either_gradient_or_none(dh, dw):
     hard_loss(140, 128, 900, torch.bfloat16, seed=8, left_out=0.2, dh=dh, dw=dw)
