@@ -2,9 +2,9 @@
 //
 // One CTA a row, one pass over it.  The floor is the row's bytes: 4096 x 128000 bf16 are 1.05 GB, 160 us.
 // A sample of the row, one 16-byte word in every few, gives a threshold that a little more than k
-// elements are expected to reach; the pass takes the log-sum-exp with a running maximum and
-// appends the elements that reach the threshold to a list in shared memory, without a barrier.  The k
-// largest of the list are exact whenever it holds at least k and did not overflow; otherwise (values
+// elements are expected to reach; the pass takes the log-sum-exp with a running maximum and notes
+// the 16-byte words with an element that reaches the threshold in shared memory, without a barrier; those
+// words are then looked through.  The k largest of the elements found are exact whenever there are at least k and neither list overflowed; otherwise (values
 // tied in thousands, or a row that the sample misses) the row is walked once more in chunks, the list
 // being cut to its k largest whenever it is full, which needs no luck.
 //
@@ -39,6 +39,24 @@ __device__ __forceinline__ float load_logit(const char* row, int64_t i) {
     if constexpr (TYPE == GK_TYPE_F32) return __ldg((const float*)row + i);
     else return from16<TYPE == GK_TYPE_F16>(__ldg((const uint16_t*)row + i));
 }
+// Two fp32 operations in one instruction.
+__device__ __forceinline__ uint64_t pair(float a, float b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void unpair(uint64_t p, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(p)); }
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
 template <int TYPE>
 __device__ __forceinline__ void unpack(const uint4& x, float (&f)[TYPE == GK_TYPE_F32 ? 4 : 8]) {
     const unsigned w[4] = {x.x, x.y, x.z, x.w};
@@ -62,15 +80,17 @@ struct TopkShared {
     static constexpr int kCap = THREADS == 1024 ? 4096 : 3072;     // list entries
     unsigned key[kCap];
     int idx[kCap];
-    float m[THREADS / 32], s[THREADS / 32];
+    int word[2048];   // noted words
+    float m[THREADS / 32], s[THREADS / 32], sampled[THREADS / 32];
     int count;        // entries appended (may exceed the list)
+    int words;        // words noted (may exceed their list)
     int bits[3];      // counts of three successive steps of a bit search
     int above;        // entries kept so far
 };
 
-// The largest t, t & high = prefix & high, such that at least `want` of the threads' keys reach it, bit by
-// bit from `bit` down; `reach` in: how many there are, out: how many reach t.  Stops early at exactly
-// `want`.  Called by all threads, which agree on every argument but their keys.
+// The largest t that at least `want` of the threads' keys reach, bit by bit from `bit` down, the bits
+// above being t's; `reach` in: how many there are, out: how many reach t.  Stops early at
+// exactly `want`.  Called by all threads, which agree on every argument but their keys.
 template <int THREADS, class Count>
 __device__ __forceinline__ unsigned bit_search(TopkShared<THREADS>& sh, unsigned t, int bit, int want, int& reach, const Count& count) {
     const int tid = threadIdx.x, lane = tid & 31;
@@ -90,10 +110,12 @@ __device__ __forceinline__ unsigned bit_search(TopkShared<THREADS>& sh, unsigned
 }
 
 // Keeps the K largest of the list's `cnt` entries (cnt > K), ties to the lower index, in its first K
-// places in no particular order; returns the K-th key.  All keys lie between lo and hi.
-template <int THREADS>
-__device__ unsigned keep_largest(TopkShared<THREADS>& sh, int cnt, int K, unsigned lo, unsigned hi) {
-    constexpr int kOwn = TopkShared<THREADS>::kCap / THREADS;
+// places in no particular order; returns the K-th key without its lowest `drop` bits, which say no
+// more than the others do (a 16-bit type's).  All keys lie between lo and hi; index_bits hold an index.
+// A thread has OWN entries.
+template <int THREADS, int OWN>
+__device__ __noinline__ unsigned keep_largest(TopkShared<THREADS>& sh, int cnt, int K, unsigned lo, unsigned hi, int drop, int index_bits) {
+    constexpr int kOwn = OWN;
     const int tid = threadIdx.x;
     // this thread's entries stay in registers; places past the list hold key 0, which no value has
     unsigned key[kOwn];
@@ -101,11 +123,13 @@ __device__ unsigned keep_largest(TopkShared<THREADS>& sh, int cnt, int K, unsign
 #pragma unroll
     for (int j = 0; j < kOwn; ++j) {
         const int at = tid + j * THREADS;
-        key[j] = at < cnt ? sh.key[at] : 0u;
+        key[j] = at < cnt ? sh.key[at] >> drop : 0u;
         idx[j] = at < cnt ? sh.idx[at] : 0;
     }
     if (tid == 0) sh.above = 0;
     // the bits above those that differ are lo's
+    lo >>= drop;
+    hi >>= drop;
     const unsigned differ = lo ^ hi;
     const int bit = differ ? 31 - __clz(differ) : -1;
     const unsigned prefix = bit < 0 ? lo : bit == 31 ? 0u : lo >> (bit + 1) << (bit + 1);
@@ -119,7 +143,7 @@ __device__ unsigned keep_largest(TopkShared<THREADS>& sh, int cnt, int K, unsign
     });
     auto keep = [&](int j) {
         const int at = atomicAdd(&sh.above, 1);
-        sh.key[at] = key[j];
+        sh.key[at] = key[j] << drop;
         sh.idx[at] = idx[j];
     };
     // all that reach t where they are K; else those above t, and of those at t the lowest indices
@@ -131,7 +155,7 @@ __device__ unsigned keep_largest(TopkShared<THREADS>& sh, int cnt, int K, unsign
     if (all) return t;
     const int need = K - sh.above;
     int equal = reach - sh.above;
-    const unsigned low = bit_search<THREADS>(sh, 0u, 31, need, equal, [&](unsigned cand) {
+    const unsigned low = bit_search<THREADS>(sh, index_bits < 32 ? ~0u << index_bits : 0u, index_bits - 1, need, equal, [&](unsigned cand) {
         int c = 0;
 #pragma unroll
         for (int j = 0; j < kOwn; ++j)
@@ -159,7 +183,11 @@ k_vocab_topk(const void* logits, int64_t ld, int64_t V, int K, float zscale, flo
     const int64_t words = (V - head) / kVec;
     const uint4* body = (const uint4*)(row + head * kSize);
 
-    if (tid == 0) sh.count = 0;
+    constexpr int kWords = 2048;
+    // the low bits of a 16-bit type's keys follow from its sign
+    constexpr int kDrop = TYPE == GK_TYPE_BF16 ? 16 : TYPE == GK_TYPE_F16 ? 13 : 0;
+    const int index_bits = 32 - __clz((int)(V - 1) | 1);
+    if (tid == 0) { sh.count = 0; sh.words = 0; }
     float tau = -INFINITY;
     if (V > kCap) {
         // The sample: up to four words a thread; of each thread the largest.  With x of the row's k
@@ -175,6 +203,11 @@ k_vocab_topk(const void* logits, int64_t ld, int64_t V, int K, float zscale, flo
 #pragma unroll
             for (int i = 0; i < kVec; ++i) top = fmaxf(top, f[i]);
         }
+        // the largest sampled element is where the log-sum-exp starts: few elements raise it
+        float most = top;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+        if (lane == 0) sh.sampled[wid] = most;
         const float x = (float)K * (float)(per * THREADS * kVec) / (float)V;
         const int r = min((int)(x + 4.f * sqrtf(x) + 4.f), THREADS / 2);
         const unsigned key = order_key(top);
@@ -190,7 +223,10 @@ k_vocab_topk(const void* logits, int64_t ld, int64_t V, int K, float zscale, flo
     }
     __syncthreads();
 
-    float m = -INFINITY, ref = 0.f, s = 0.f;
+    float m = -INFINITY, s = 0.f;
+    if (V > kCap)
+        for (int k = 0; k < THREADS / 32; ++k) m = fmaxf(m, sh.sampled[k]);
+    float ref = finite_ref(m);
     auto append = [&](float v, int64_t i) {
         const int at = atomicAdd(&sh.count, 1);
         if (at < kCap) { sh.key[at] = order_key(v); sh.idx[at] = (int)i; }
@@ -209,24 +245,36 @@ k_vocab_topk(const void* logits, int64_t ld, int64_t V, int K, float zscale, flo
         s += exp2_fast((v - ref) * zscale);
         if (!(v < tau)) append(v, i);
     };
+    uint64_t sums = pair(0.f, 0.f);
     auto word = [&](const uint4& x, int64_t at) {
         float f[kVec];
         unpack<TYPE>(x, f);
         float g = f[0];
-        bool nan = f[0] != f[0];
 #pragma unroll
         for (int i = 1; i < kVec; ++i) g = fmaxf(g, f[i]);
-        raise(g);
-        float e[2] = {0.f, 0.f};
+        if (g > m) {
+            const float r = finite_ref(g), by = m > -INFINITY ? exp2_fast((ref - r) * zscale) : 1.f;   // else the sums are 0 or NaN
+            s *= by;
+            sums = mul2(sums, pair(by, by));
+            m = g;
+            ref = r;
+        }
+        const uint64_t less = pair(-ref, -ref), by = pair(zscale, zscale);
+        uint64_t e[kVec / 2];
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) e[i & 1] += exp2_fast((f[i] - ref) * zscale);
-        const float sum = e[0] + e[1];
-        s += sum;
-        nan = sum != sum;
-        if (!(g < tau) || nan) {
+        for (int i = 0; i < kVec / 2; ++i) {
+            float a, b;
+            unpair(mul2(add2(pair(f[2 * i], f[2 * i + 1]), less), by), a, b);
+            e[i] = pair(exp2_fast(a), exp2_fast(b));
+        }
 #pragma unroll
-            for (int i = 0; i < kVec; ++i)
-                if (!(f[i] < tau)) append(f[i], head + at * kVec + i);
+        for (int w = kVec / 4; w > 0; w /= 2)
+#pragma unroll
+            for (int i = 0; i < w; ++i) e[i] = add2(e[i], e[i + w]);
+        sums = add2(sums, e[0]);
+        if (!(g < tau)) {
+            const int to = atomicAdd(&sh.words, 1);
+            if (to < kWords) sh.word[to] = (int)at;
         }
     };
     if (tid < head) single(tid);
@@ -242,6 +290,11 @@ k_vocab_topk(const void* logits, int64_t ld, int64_t V, int K, float zscale, flo
     }
     for (; at < words; at += THREADS) word(__ldcs(body + at), at);
 
+    {
+        float a, b;
+        unpair(sums, a, b);
+        s += a + b;
+    }
     // log-sum-exp and maximum of the row
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
@@ -255,37 +308,53 @@ k_vocab_topk(const void* logits, int64_t ld, int64_t V, int K, float zscale, flo
     for (int k = 1; k < THREADS / 32; ++k) join_raw(m, s, sh.m[k], sh.s[k], zscale);
     if (lse_out && tid == 0) lse_out[blockIdx.x] = m * inv_T + logf(s);
 
+    // The noted words' elements.  The pass compares a word's maximum, which knows nothing of NaN: a
+    // row with one is taken in chunks.
+    const int noted = sh.words;
+    const bool whole = noted <= kWords && s == s;
+    if (whole)
+        for (int j = tid; j < noted; j += THREADS) {
+            const int64_t w = sh.word[j];
+            float f[kVec];
+            unpack<TYPE>(__ldg(body + w), f);
+#pragma unroll
+            for (int i = 0; i < kVec; ++i)
+                if (!(f[i] < tau)) append(f[i], head + w * kVec + i);
+        }
+    __syncthreads();
     int cnt = sh.count;
-    if (cnt >= K && cnt <= kCap) {
-        if (cnt > K) keep_largest<THREADS>(sh, cnt, K, order_key(tau), s != s ? 0xffffffffu : order_key(m));
+    if (whole && cnt >= K && cnt <= kCap) {
+        if (cnt > K) {
+            if (cnt <= 2 * THREADS) keep_largest<THREADS, 2>(sh, cnt, K, order_key(tau), order_key(m), kDrop, index_bits);
+            else keep_largest<THREADS, kCap / THREADS>(sh, cnt, K, order_key(tau), order_key(m), kDrop, index_bits);
+        }
     } else {
         // The list overflowed or is short.  In chunks: after a cut only larger keys are appended,
         // for an equal one comes later in the row than all that are kept.
-        constexpr int kChunk = 2 * THREADS;
-        unsigned floor_key = 0;
-        bool cut = false;
+        constexpr int kEach = 2048 / THREADS, kChunk = kEach * THREADS;
+        unsigned floor_key = 0;      // below every value's key
         __syncthreads();
         if (tid == 0) sh.count = 0;
         __syncthreads();
         for (int64_t i0 = 0; i0 < V; i0 += kChunk) {
+            unsigned key[kEach];
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
+            for (int j = 0; j < kEach; ++j) {
                 const int64_t i = i0 + j * THREADS + tid;
-                if (i < V) {
-                    const unsigned key = order_key(load_logit<TYPE>(row, i));
-                    if (!cut || key > floor_key) {
-                        const int to = atomicAdd(&sh.count, 1);
-                        sh.key[to] = key;
-                        sh.idx[to] = (int)i;
-                    }
-                }
+                key[j] = i < V ? order_key(load_logit<TYPE>(row, i)) : 0u;
             }
+#pragma unroll
+            for (int j = 0; j < kEach; ++j)
+                if (key[j] > floor_key) {
+                    const int to = atomicAdd(&sh.count, 1);
+                    sh.key[to] = key[j];
+                    sh.idx[to] = (int)(i0 + j * THREADS + tid);
+                }
             __syncthreads();
             cnt = sh.count;
             if (cnt + kChunk > kCap || i0 + kChunk >= V) {
                 if (cnt > K) {
-                    floor_key = keep_largest<THREADS>(sh, cnt, K, 0u, 0xffffffffu);
-                    cut = true;
+                    floor_key = keep_largest<THREADS, kCap / THREADS>(sh, cnt, K, 0u, 0xffffffffu, 0, index_bits);
                     cnt = K;
                 }
                 if (tid == 0) sh.count = cnt;
