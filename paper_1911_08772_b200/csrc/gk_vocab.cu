@@ -10,17 +10,28 @@
 //
 // One call:
 //   1. (distill) the teacher's probabilities; the rows that count, numbered in their order;
-//   2. those rows of h copied together, and the logits at the targets as K dot products a row;
-//   3. logits tile by tile: the tile's maximum and sum, and for the first piece of the vocabulary (all
-//      of it where the budget allows) their distances from that maximum in 16 bits;
+//   2. those rows of h copied together, and the logit at the target as a dot product;
+//   3. logits tile by tile, of which each row keeps the sums of the exponentials, and for the first
+//      piece of the vocabulary (all of it where the budget allows) something of each logit in 16 bits;
+//      (distill) the logits at the teacher's pairs as they pass;
 //   4. the row's log-sum-exp from the tiles, loss;
-//   5. per piece: logit gradients in 16 bits (from the kept distances, or from the product
-//      taken again), then dw and dh as products with them.
-// Kept between the steps is one piece, whose size the budget bounds whatever n and V are.  A
-// distance is kept in fixed point, for bf16 in steps of 2^-9 in the exponent of two: the exponential
-// it stands for is then off by at most 2^-10 log 2 = 6.8e-4 of itself, where a bf16 exponential is off by
-// up to 2^-9 = 2.0e-3, and a logit of 16 by 3e-2; the 65536 steps reach 2^-128, as bf16 itself does.  For
-// fp16 the steps are 2^-11 (1.7e-4, against 4.9e-4) and reach 2^-32, where fp16 gradients have ended.
+//   5. per piece: the operand of the gradients in 16 bits (from what was kept, or from the product
+//      taken again), then dw and dh as products with it.
+// Kept between the steps is one piece, whose size the budget bounds whatever n and V are.
+//
+// What is kept of a logit.  Large bf16 calls keep powers: exp(z_nv / T - r_n), where r_n, the row's
+// reference, is its logit at the target.  As dz_nv = c_n (exp(z_nv / T - r_n) - ...) with
+// c_n = (g_n Q_n / T) exp(r_n - lse_n), they are the operand itself: c_n scales the rows of h before
+// dw and those of dh after it, and no pass over n x V values lies between the products (8192 x 128000: 0.8 of
+// 20 ms).  bf16 has fp32's exponents, so a reference may be 2^100 below the sum (a loss of 69) and nothing
+// overflows; where it is further below, the step is done again with the log-sum-exp itself as the
+// reference.
+// fp16 has no such exponents, and small calls would notice the kernels that look for overflow: they
+// keep a logit's distance from the largest of its 128 columns in fixed point, for bf16 in steps of 2^-9 in
+// the exponent of two: the exponential it stands for is then off by at most 2^-10 log 2 = 6.8e-4 of itself, where
+// a bf16 exponential is off by up to 2^-9 = 2.0e-3, and a logit of 16 by 3e-2; the 65536 steps reach 2^-128, as
+// bf16 itself does.  For fp16 the steps are 2^-11 (1.7e-4, against 4.9e-4) and reach 2^-32, where fp16
+// gradients have ended.  A pass over them makes the logit gradients.
 #include <atomic>
 #include <map>
 #include <mutex>
@@ -57,20 +68,28 @@ __global__ void __launch_bounds__(256) k_vocab_teacher(VocabCall c) {
     // value do not overflow; with the teacher's own log-sum-exp there is nothing to take off
     float top = -INFINITY;
     bool any = false, ascending = true;
+    int largest = 0;
     for (int j = lane; j < c.K; j += 32) {
-        const int32_t i = ti[j];
+        const int32_t i = ti[j], before = j > 0 ? ti[j - 1] : -1;
         const float t = tv[j];
-        if (i >= 0 && i < c.V && t != -INFINITY) { any = true; top = fmaxf(top, t); }
-        if (j > 0 && ti[j - 1] >= i) ascending = false;
+        const bool in = i >= 0 && i < c.V;
+        if (in && t != -INFINITY) {
+            any = true;
+            if (t > top) { top = t; largest = j; }
+        }
+        if (in && j > 0 && (before >= i || before < 0)) ascending = false;
     }
     any = __any_sync(0xffffffffu, any);
     ascending = __all_sync(0xffffffffu, ascending);
+    const float most = warp_max_f(top);
+    const unsigned holds = __ballot_sync(0xffffffffu, top == most);
+    largest = __shfl_sync(0xffffffffu, largest, holds ? __ffs(holds) - 1 : 0);
     float L;
     if (c.t_lse) {
         L = c.t_lse[r];
         top = 0.f;
     } else {
-        top = warp_max_f(top);
+        top = most;
         float s = 0.f;
         for (int j = lane; j < c.K; j += 32)
             if (ti[j] >= 0 && ti[j] < c.V && tv[j] != -INFINITY) s += expf((tv[j] - top) * c.inv_T);
@@ -84,7 +103,7 @@ __global__ void __launch_bounds__(256) k_vocab_teacher(VocabCall c) {
         Q += q;
     }
     Q = warp_sum_f(Q);
-    if (lane == 0) c.teacher[r] = make_float4(Q, L, top, (ascending ? 1.f : 0.f) + (any ? 2.f : 0.f));
+    if (lane == 0) c.teacher[r] = make_float4(Q, L, top, (float)((ascending ? 1 : 0) + (any ? 2 : 0) + 4 * largest));
 }
 
 // ---------------------------------------------------------------------------
@@ -109,7 +128,7 @@ __global__ void __launch_bounds__(1024) k_vocab_rows(VocabCall c) {
                 on = t != c.ignore_index && t >= 0 && t < c.V;
             } else {
                 const float4 te = c.teacher[r];
-                on = te.w >= 2.f;
+                on = teacher_counts(te);
                 Q = te.x;
             }
         }
@@ -151,6 +170,7 @@ __global__ void __launch_bounds__(1024) k_vocab_rows(VocabCall c) {
         e = min(max((c.f16 ? 11 : 1) - e, -100), 100);
         c.ctl->n_valid = base;
         c.ctl->status = 0;
+        c.ctl->missed = 0;
         c.ctl->scale = ldexpf(1.f, e);
         c.ctl->inv_scale = ldexpf(1.f, -e);
     }
@@ -158,13 +178,36 @@ __global__ void __launch_bounds__(1024) k_vocab_rows(VocabCall c) {
 
 // ---------------------------------------------------------------------------
 // 2. Compact rows of h (padded with zeros to the pitch, and zero rows to a multiple of 256, which
-// the products read) and the logits at the targets.  One CTA a row, one warp a dot product.
+// the products read) and the logits at the targets that the products do not deliver: the class, or
+// of a teacher's pairs the largest, which is the row's reference, and all of a row in no order.  One
+// CTA a row, one warp a dot product.
 // ---------------------------------------------------------------------------
+
+// Eight values from 2-byte-aligned memory, zero from `left` on.
+__device__ __forceinline__ uint4 load8(const uint16_t* p, int64_t left) {
+    const uintptr_t a = (uintptr_t)p;
+    if (left >= 8) {
+        if ((a & 15) == 0) return __ldg((const uint4*)p);
+        if ((a & 7) == 0) {
+            const uint2 x = __ldg((const uint2*)p), y = __ldg((const uint2*)p + 1);
+            return make_uint4(x.x, x.y, y.x, y.y);
+        }
+        if ((a & 3) == 0) {
+            const unsigned* q = (const unsigned*)p;
+            return make_uint4(__ldg(q), __ldg(q + 1), __ldg(q + 2), __ldg(q + 3));
+        }
+    }
+    unsigned v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = i < left ? __ldg(p + i) : 0u;
+    return make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
+}
+
 template <bool F16>
-__global__ void __launch_bounds__(128) k_vocab_gather(VocabCall c, bool w_vec) {
+__global__ void __launch_bounds__(128) k_vocab_gather(VocabCall c) {
     const int at = blockIdx.x, n_valid = c.ctl->n_valid;
     const int tid = threadIdx.x, lane = tid & 31;
-    if (at >= (n_valid + kVocabRowPad - 1) / kVocabRowPad * kVocabRowPad) return;
+    if (at >= round_up(n_valid, kVocabRowPad)) return;
     uint16_t* to = c.hc + (int64_t)at * c.Dp;
     if (at >= n_valid) {
         for (int64_t i = tid; i < c.Dp / 8; i += 128) ((uint4*)to)[i] = make_uint4(0, 0, 0, 0);
@@ -172,111 +215,125 @@ __global__ void __launch_bounds__(128) k_vocab_gather(VocabCall c, bool w_vec) {
     }
     const int64_t r = c.row_of[at];
     const uint16_t* from = (const uint16_t*)c.h + r * c.ldh;
-    if (((uintptr_t)from & 15) == 0) {
-        for (int64_t i = tid; i < c.Dp / 8; i += 128) {
-            if (i * 8 + 8 <= c.D) ((uint4*)to)[i] = __ldg((const uint4*)from + i);
-            else
-                for (int64_t j = i * 8; j < i * 8 + 8; ++j) to[j] = j < c.D ? from[j] : (uint16_t)0;
-        }
-    } else {
-        for (int64_t i = tid; i < c.Dp; i += 128) to[i] = i < c.D ? from[i] : (uint16_t)0;
+    for (int64_t i = tid; i < c.Dp / 8; i += 128) ((uint4*)to)[i] = load8(from + i * 8, c.D - i * 8);
+    int first = 0, last = 1;
+    if (!c.target) {
+        const float4 te = c.teacher[r];
+        first = teacher_largest(te);
+        last = c.powers ? first + 1 : first;
+        if (!teacher_ascending(te)) { first = 0; last = c.K; }
     }
     __syncthreads();
-    for (int j = tid >> 5; j < c.K; j += 4) {
+    const uint16_t* w = c.wc ? c.wc : (const uint16_t*)c.w;
+    const int64_t ldw = c.wc ? c.Dp : c.ldw, words = c.wc ? c.Dp / 8 : c.D / 8;   // rows of w in words: see run_head
+    for (int j = first + (tid >> 5); j < last; j += 4) {
         const int64_t v = c.target ? c.target[r] : (int64_t)c.t_idx[r * c.K + j];
         float s = 0.f;
         if (v >= 0 && v < c.V) {
-            const uint16_t* wr = (const uint16_t*)c.w + v * c.ldw;
-            int64_t i = 0;
-            if (w_vec) {
-                const int64_t whole = c.D / 8;
-                for (int64_t b = lane; b < whole; b += 32) {
-                    const uint4 x = ((const uint4*)to)[b];
-                    const uint4 y = __ldg((const uint4*)wr + b);
-                    const unsigned xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+            const uint4* wr = (const uint4*)(w + v * ldw);
+            for (int64_t b = lane; b < words; b += 32) {
+                const uint4 x = ((const uint4*)to)[b];
+                const uint4 y = __ldg(wr + b);
+                const unsigned xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        s = fmaf(from16<F16>((uint16_t)xs[q]), from16<F16>((uint16_t)ys[q]), s);
-                        s = fmaf(from16<F16>((uint16_t)(xs[q] >> 16)), from16<F16>((uint16_t)(ys[q] >> 16)), s);
-                    }
+                for (int q = 0; q < 4; ++q) {
+                    s = fmaf(from16<F16>((uint16_t)xs[q]), from16<F16>((uint16_t)ys[q]), s);
+                    s = fmaf(from16<F16>((uint16_t)(xs[q] >> 16)), from16<F16>((uint16_t)(ys[q] >> 16)), s);
                 }
-                i = whole * 8;
             }
-            for (i += lane; i < c.D; i += 32) s = fmaf(from16<F16>(to[i]), from16<F16>(wr[i]), s);
         }
         s = warp_sum_f(s);
-        if (lane == 0) c.zt[(int64_t)at * c.K + j] = s;
+        if (lane == 0) {
+            c.zt[(int64_t)at * c.K + j] = s;
+            if (c.target || j == teacher_largest(c.teacher[r])) c.row[at].ref = s * c.zscale;
+        }
     }
 }
 
 // A copy of w with rows that start and end on 16-byte boundaries, where w's own do not.
 __global__ void __launch_bounds__(256) k_vocab_copy_w(VocabCall c) {
-    const uint16_t* from = (const uint16_t*)c.w + (int64_t)blockIdx.x * c.ldw;
-    uint16_t* to = c.wc + (int64_t)blockIdx.x * c.Dp;
-    for (int64_t i = threadIdx.x; i < c.Dp; i += 256) to[i] = i < c.D ? from[i] : (uint16_t)0;
-}
-
-// ---------------------------------------------------------------------------
-// 4. Log-sum-exp and loss.  A CTA takes 32 compact rows; its 8 warps share the tiles, a fixed order
-// joins them.
-// ---------------------------------------------------------------------------
-__global__ void __launch_bounds__(256) k_vocab_rows_done(VocabCall c) {
-    __shared__ float sm[8][32], ss[8][32];
-    const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
-    const int64_t at0 = (int64_t)blockIdx.x * 32;
-    const int n_valid = c.ctl->n_valid;
-    if (at0 >= n_valid) return;
-    const int64_t at = at0 + lane;
-    const int64_t tiles = (c.V + kVocabTile - 1) / kVocabTile;
-    float m = -INFINITY, s = 0.f;
-    if (at < n_valid)
-        for (int64_t t = wid; t < tiles; t += 8) {
-            const float2 p = __ldcs(c.part + t * c.n_pad + at);
-            join_max_sum(m, s, p.x, p.y);
-        }
-    sm[wid][lane] = m;
-    ss[wid][lane] = s;
-    __syncthreads();
-    // each warp finishes four rows
-    for (int i = wid * 4; i < wid * 4 + 4; ++i) {
-        const int64_t a = at0 + i;
-        if (a >= n_valid) break;
-        m = sm[0][i];
-        s = ss[0][i];
-#pragma unroll
-        for (int k = 1; k < 8; ++k) join_max_sum(m, s, sm[k][i], ss[k][i]);
-        const float lse2 = m + log2f(s);
-        const int64_t r = c.row_of[a];
-        float Q = 1.f, loss;
-        if (c.target) {
-            loss = (lse2 - c.zt[a] * c.zscale) * kLn2;
-        } else {
-            const float4 te = c.teacher[r];
-            Q = te.x;
-            float sum = 0.f;
-            for (int j = lane; j < c.K; j += 32) {
-                const float q = c.q[r * c.K + j];
-                if (q > 0.f) sum += q * (((c.t_val[r * c.K + j] - te.z) * c.inv_T - te.y) + (lse2 - c.zt[a * c.K + j] * c.zscale) * kLn2);
-                else if (q != q) sum = q;
-            }
-            loss = warp_sum_f(sum);
-        }
-        if (lane == 0) {
-            c.loss[r] = loss;
-            c.lse[r] = lse2 * kLn2;
-            const float unit = c.ctl->scale * ((c.row_grad ? c.row_grad[r] : 1.f / (float)n_valid) * c.inv_T);
-            VocabRow out;
-            out.lse2 = lse2;
-            out.coef = unit * Q;
-            out.unit = unit;
-            out.pad = 0.f;
-            c.row[a] = out;
-        }
+    const int64_t words = c.Dp / 8, total = c.V * words;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+        const int64_t v = i / words, k = (i - v * words) * 8;
+        ((uint4*)c.wc)[i] = load8((const uint16_t*)c.w + v * c.ldw + k, c.D - k);
     }
 }
 
 // ---------------------------------------------------------------------------
-// 5. Logit gradients of one piece.  The targets' entries are formed in fp32 from their own logits
+// 4. Log-sum-exp and loss.  A CTA takes 32 compact rows; its 32 warps share the tiles, a fixed order
+// joins them, and each warp finishes a row.
+// SECOND: after the references did not hold and the logits have been taken again; the log-sum-exp
+// becomes the reference.
+// ---------------------------------------------------------------------------
+template <bool SECOND>
+__global__ void __launch_bounds__(1024) k_vocab_rows_done(VocabCall c) {
+    __shared__ float sm[32][33], ss[32][33];
+    const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+    const int64_t at0 = (int64_t)blockIdx.x * 32;
+    const int n_valid = c.ctl->n_valid;
+    if (at0 >= n_valid || (SECOND && c.ctl->missed == 0)) return;
+    const int64_t tiles = (c.V + kVocabTile - 1) / kVocabTile;
+    float m = -INFINITY, s = 0.f;
+    if (at0 + lane < n_valid) {
+        const float2* p = c.part + at0 + lane;
+#pragma unroll 4
+        for (int64_t t = wid; t < tiles; t += 32) {
+            const float2 x = __ldcs(p + t * c.n_pad);
+            join_max_sum(m, s, x.x, x.y);
+        }
+    }
+    sm[wid][lane] = m;
+    ss[wid][lane] = s;
+    __syncthreads();
+    const int64_t at = at0 + wid;
+    if (at >= n_valid) return;
+    m = sm[lane][wid];
+    s = ss[lane][wid];
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) {
+        // both sides join in the order of their lanes
+        const float m2 = __shfl_xor_sync(0xffffffffu, m, o), s2 = __shfl_xor_sync(0xffffffffu, s, o);
+        float ml = lane & o ? m2 : m, sl = lane & o ? s2 : s;
+        join_max_sum(ml, sl, lane & o ? m : m2, lane & o ? s : s2);
+        m = ml;
+        s = sl;
+    }
+    const float lse2 = m + log2f(s);
+    const int64_t r = c.row_of[at];
+    float Q = 1.f, loss;
+    if (c.target) {
+        loss = (lse2 - c.zt[at] * c.zscale) * kLn2;
+    } else {
+        const float4 te = c.teacher[r];
+        Q = te.x;
+        float sum = 0.f;
+        for (int j = lane; j < c.K; j += 32) {
+            const float q = c.q[r * c.K + j];
+            if (q > 0.f) sum += q * (((c.t_val[r * c.K + j] - te.z) * c.inv_T - te.y) + (lse2 - c.zt[at * c.K + j] * c.zscale) * kLn2);
+            else if (q != q) sum = q;
+        }
+        loss = warp_sum_f(sum);
+    }
+    if (lane == 0) {
+        c.loss[r] = loss;
+        c.lse[r] = lse2 * kLn2;
+        const float unit = c.ctl->scale * ((c.row_grad ? c.row_grad[r] : 1.f / (float)n_valid) * c.inv_T);
+        VocabRow out;
+        out.lse2 = lse2;
+        out.coef = unit * Q;
+        out.unit = unit;
+        out.ref = SECOND ? lse2 : c.row[at].ref;
+        // powers up to 2^100, and their products with w and h, are far from the types' ends
+        if (!SECOND && c.powers && lse2 - out.ref >= 100.f) c.ctl->missed = 1;
+        c.row[at] = out;
+    }
+}
+
+// What a row's powers are worth.
+__device__ __forceinline__ float powers_worth(const VocabRow& r) { return r.coef * exp2f(r.ref - r.lse2); }
+
+// ---------------------------------------------------------------------------
+// 5. The gradients' operand for one piece.  The targets' entries are formed in fp32 from their own logits
 // and written over, so that 1 - p loses nothing where p is near 1.
 // ---------------------------------------------------------------------------
 template <bool F16>
@@ -284,18 +341,20 @@ __device__ __forceinline__ void write_targets(const VocabCall& c, int64_t at, in
                                               int tid, int threads) {
     const int64_t r = c.row_of[at];
     const VocabRow vr = c.row[at];
-    const bool distinct = c.target || c.teacher[r].w == 3.f;
+    const float4 te = c.target ? make_float4(1.f, 0.f, 0.f, 1.f) : c.teacher[r];
+    if (c.powers && !(te.x > 0.f)) return;      // the row's powers are worth nothing
     for (int j = tid; j < c.K; j += threads) {
         const int64_t v = c.target ? c.target[r] : (int64_t)c.t_idx[r * c.K + j];
         if (v < lo || v >= hi) continue;
         float q = c.target ? 1.f : c.q[r * c.K + j];
-        if (!distinct) {      // an index given more than once: each of its pairs writes the same sum
+        if (!teacher_ascending(te)) {      // an index given more than once: each of its pairs writes the same sum
             q = 0.f;
             for (int i = 0; i < c.K; ++i)
                 if (c.t_idx[r * c.K + i] == v) q += c.q[r * c.K + i];
         }
         const float p = exp2_fast(c.zt[at * c.K + j] * c.zscale - vr.lse2);
-        c.e[at * c.vb + (v - v0)] = to16<F16>(fmaf(vr.coef, p, -(vr.unit * q)));
+        const float x = c.powers ? (p - q / te.x) * exp2f(vr.lse2 - vr.ref) : fmaf(vr.coef, p, -(vr.unit * q));
+        c.e[at * c.vb + (v - v0)] = to16<F16>(x);
     }
 }
 
@@ -334,7 +393,28 @@ __global__ void __launch_bounds__(256) k_vocab_scale(VocabCall c, int64_t v0, in
     write_targets<F16>(c, at, lo, hi, v0, threadIdx.x, 256);
 }
 
-// The product taken again has written the gradients; only the targets' entries are left.
+// Powers: hs <- hc times what each row's powers are worth, with zero rows to a multiple of 64, and the
+// targets' entries of the first piece.
+template <bool F16>
+__global__ void __launch_bounds__(128) k_vocab_worth(VocabCall c, int64_t v1) {
+    const int64_t at = blockIdx.x;
+    const int n_valid = c.ctl->n_valid;
+    if (at >= round_up(n_valid, 64)) return;
+    const bool on = at < n_valid;
+    if (on) write_targets<F16>(c, at, 0, v1, 0, threadIdx.x, 128);
+    const float f = on ? powers_worth(c.row[at]) : 0.f;
+    const uint4* from = (const uint4*)(c.hc + at * c.Dp);
+    uint4* to = (uint4*)(c.hs + at * c.Dp);
+    for (int64_t i = threadIdx.x; i < c.Dp / 8; i += 128) {
+        const uint4 x = on ? from[i] : make_uint4(0, 0, 0, 0);
+        unsigned xs[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int q = 0; q < 4; ++q) xs[q] = on ? pack16<F16>(f * from16<F16>((uint16_t)xs[q]), f * from16<F16>((uint16_t)(xs[q] >> 16))) : 0u;
+        to[i] = make_uint4(xs[0], xs[1], xs[2], xs[3]);
+    }
+}
+
+// The product taken again has written a piece's operand; only the targets' entries are left.
 template <bool F16>
 __global__ void __launch_bounds__(128) k_vocab_targets(VocabCall c, int64_t v0, int64_t v1) {
     const int64_t at = blockIdx.x;
@@ -348,7 +428,7 @@ __global__ void __launch_bounds__(256) k_vocab_finish_dh(VocabCall c) {
     const int64_t r = blockIdx.x;
     const int at = c.at_of[r];
     uint16_t* to = (uint16_t*)c.dh + r * c.lddh;
-    const float inv = c.ctl->inv_scale;
+    const float inv = c.ctl->inv_scale * (c.powers && at >= 0 ? powers_worth(c.row[at]) : 1.f);
     for (int64_t i = threadIdx.x; i < c.D; i += 256) {
         float s = 0.f;
         if (at >= 0)
@@ -368,6 +448,10 @@ struct VocabWorkspace {
 static std::mutex g_vocab_mu;
 static std::map<std::pair<int, cudaStream_t>, VocabWorkspace> g_vocab_ws;
 static std::atomic<int64_t> g_vocab_budget{(int64_t)2 << 30};
+
+// Logits from which bf16 calls keep powers: below, the pass that powers save costs less than the three
+// launches that stand by for references that do not hold.
+constexpr int64_t kPowersFrom = 1 << 23;
 
 static int64_t piece_columns(int64_t n_pad, int64_t V) {
     const int64_t fit = g_vocab_budget.load() / (2 * n_pad) / 256 * 256;
@@ -391,6 +475,7 @@ static size_t lay_out(VocabCall& c, bool distill, bool copy_w, char* base) {
     c.q = (float*)(distill ? take(4 * n * K) : nullptr);
     c.teacher = (float4*)(distill ? take(16 * n) : nullptr);
     c.hc = (uint16_t*)take(2 * np * c.Dp);
+    c.hs = c.powers ? (uint16_t*)take(2 * np * c.Dp) : c.hc;
     c.wc = (uint16_t*)(copy_w ? take(2 * (size_t)c.V * c.Dp) : nullptr);
     c.zt = (float*)take(4 * np * K);
     c.part = (float2*)take(8 * tiles * np);
@@ -426,39 +511,54 @@ static void size_call(VocabCall& c, bool want_dh, bool want_dw, int sm_count) {
     c.n_pad = round_up(c.n, kVocabRowPad);
     c.Dp = round_up(c.D, 64);
     c.vb = want_dh || want_dw ? piece_columns(c.n_pad, c.V) : 0;
+    c.powers = !c.f16 && c.vb > 0 && c.n * c.V >= kPowersFrom;
     c.splits = want_dh ? vocab_dh_splits(c.n, c.D, c.vb, sm_count) : 0;
 }
 
 template <bool F16>
-static int enqueue(const VocabCall& c, bool distill, bool w_vec, int sms, cudaStream_t st) {
-    const unsigned n = (unsigned)c.n;
+static int enqueue(const VocabCall& c, bool distill, int sms, cudaStream_t st) {
+    const unsigned n = (unsigned)c.n, groups = (n + 31) / 32;
     const bool grad = c.dh || c.dw;
     if (distill) k_vocab_teacher<<<(n + 7) / 8, 256, 0, st>>>(c);
     k_vocab_rows<<<1, 1024, 0, st>>>(c);
-    k_vocab_gather<F16><<<(unsigned)c.n_pad, 128, 0, st>>>(c, w_vec);
-    if (c.wc) k_vocab_copy_w<<<(unsigned)c.V, 256, 0, st>>>(c);
+    if (c.wc) {
+        const int64_t blocks = (c.V * (c.Dp / 8) + 255) / 256;
+        k_vocab_copy_w<<<(unsigned)(blocks < 16 * sms ? blocks : 16 * sms), 256, 0, st>>>(c);
+    }
+    k_vocab_gather<F16><<<(unsigned)c.n_pad, 128, 0, st>>>(c);
     GK_CUDA_TRY(cudaGetLastError());
     note_launch(2 + (distill ? 1 : 0) + (c.wc ? 1 : 0));
     const int64_t kept = grad ? (c.vb < c.V ? c.vb : c.V) : 0;
     int rc = GK_OK;
-    if (kept > 0) rc = launch_vocab_logits(c, 0, kept, true, sms, st);
-    if (rc == GK_OK && kept < c.V) rc = launch_vocab_logits(c, kept, c.V, false, sms, st);
+    if (kept > 0) rc = c.powers ? launch_vocab_powers(c, 0, kept, false, sms, st) : launch_vocab_logits(c, 0, kept, true, false, sms, st);
+    if (rc == GK_OK && kept < c.V) rc = launch_vocab_logits(c, kept, c.V, false, false, sms, st);
     if (rc != GK_OK) return rc;
-    k_vocab_rows_done<<<(n + 31) / 32, 256, 0, st>>>(c);
+    k_vocab_rows_done<false><<<groups, 1024, 0, st>>>(c);
     GK_CUDA_TRY(cudaGetLastError());
     note_launch();
     if (!grad) return GK_OK;
+    if (c.powers) {
+        rc = launch_vocab_logits(c, 0, kept, false, true, sms, st);
+        if (rc != GK_OK) return rc;
+        k_vocab_rows_done<true><<<groups, 1024, 0, st>>>(c);
+        GK_CUDA_TRY(cudaGetLastError());
+        rc = launch_vocab_powers(c, 0, kept, true, sms, st);
+        if (rc != GK_OK) return rc;
+        k_vocab_worth<F16><<<(unsigned)round_up(n, 64), 128, 0, st>>>(c, kept);
+        GK_CUDA_TRY(cudaGetLastError());
+        note_launch(2);
+    }
     for (int64_t v0 = 0; v0 < c.V; v0 += c.vb) {
         const int64_t v1 = v0 + c.vb < c.V ? v0 + c.vb : c.V;
-        if (v0 == 0) {
-            k_vocab_scale<F16><<<dim3((unsigned)round_up(n, 64), (unsigned)((v1 + kGradCols - 1) / kGradCols)), 256, 0, st>>>(c, v0, v1);
-        } else {
-            rc = launch_vocab_again(c, v0, v1, sms, st);
+        if (v0 > 0) {
+            rc = c.powers ? launch_vocab_powers(c, v0, v1, false, sms, st) : launch_vocab_again(c, v0, v1, sms, st);
             if (rc != GK_OK) return rc;
             k_vocab_targets<F16><<<n, 128, 0, st>>>(c, v0, v1);
+        } else if (!c.powers) {
+            k_vocab_scale<F16><<<dim3((unsigned)round_up(n, 64), (unsigned)((v1 + kGradCols - 1) / kGradCols)), 256, 0, st>>>(c, v0, v1);
         }
         GK_CUDA_TRY(cudaGetLastError());
-        note_launch();
+        note_launch(v0 > 0 || !c.powers ? 1 : 0);
         if (c.dw) rc = launch_vocab_dw(c, v0, v1, sms, st);
         if (rc == GK_OK && c.dh) rc = launch_vocab_dh(c, v0, v1, v0 == 0, sms, st);
         if (rc != GK_OK) return rc;
@@ -507,7 +607,7 @@ static int run_head(VocabCall& c, bool distill, cudaStream_t st) {
     rc = vocab_workspace(lay_out(c, distill, !w_vec, nullptr), st, &ws);
     if (rc != GK_OK) return rc;
     lay_out(c, distill, !w_vec, (char*)ws->base);
-    return c.f16 ? enqueue<true>(c, distill, w_vec, ws->sm_count, st) : enqueue<false>(c, distill, w_vec, ws->sm_count, st);
+    return c.f16 ? enqueue<true>(c, distill, ws->sm_count, st) : enqueue<false>(c, distill, ws->sm_count, st);
 }
 
 }  // namespace gk

@@ -18,6 +18,7 @@ constexpr int kVocabMaxPairs = 1024;    // largest K of gk_vocab_distill and gk_
 struct VocabCtl {
     int n_valid;           // rows that count
     unsigned int status;   // GK_DEV_* flags
+    int missed;            // a row's reference was too far below its logits: powers overflowed
     float scale;           // power of two that brings the largest row coefficient to the 16-bit type's range
     float inv_scale;
 };
@@ -27,7 +28,7 @@ struct VocabRow {
     float lse2;     // log-sum-exp of the scaled logits, in units of log 2
     float coef;     // scale * g_n * Q_n / T: what multiplies p_nv
     float unit;     // scale * g_n / T: what multiplies q_nj
-    float pad;
+    float ref;      // reference of the row's powers, in units of log 2
 };
 
 // One call's sizes and device pointers, passed to the kernels by value.
@@ -58,13 +59,17 @@ struct VocabCall {
     int32_t* row_of;            // compact row -> row
     int32_t* at_of;             // row -> compact row, -1 where left out
     float* q;                   // n x K teacher probabilities (distill), 0 for a pair left out
-    float4* teacher;            // per row: Q, log-sum-exp L relative to a reference, the reference, 1 (strictly ascending indices) + 2 (a pair counts)
+    float4* teacher;            // per row: Q, log-sum-exp L relative to a reference, the reference, and a whole
+                                // number: 1 (indices strictly ascending, pairs left out at the end) + 2 (a pair
+                                // counts) + 4 x place of the largest
+    bool powers;                // e holds powers relative to the rows' references, else logits below their tile's maximum
     uint16_t* hc;               // n_pad x Dp compact rows of h
+    uint16_t* hs;               // powers: hc with each row times what its powers are worth, else hc
     uint16_t* wc;               // V x Dp copy of w where w itself cannot be the source of bulk copies, else nullptr
     float* zt;                  // n_pad x K raw logits at the targets
     float2* part;               // per (vocabulary tile, compact row): maximum (units of log 2), sum
     VocabRow* row;              // n_pad
-    uint16_t* e;                // n_pad x vb: one piece's kept logits, then its logit gradients
+    uint16_t* e;                // n_pad x vb: one piece's powers, or kept logits and then logit gradients
     int64_t vb;                 // columns of a piece, a multiple of 256 (the pitch of e)
     float* dhp;                 // splits x n_pad x Dp partial sums of dh
     int splits;
@@ -72,19 +77,26 @@ struct VocabCall {
 
 __host__ __device__ inline int64_t round_up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
 
-// The products (gk_vocab_gemm.cu).  v0, v1: the columns of the vocabulary [v0, v1).
+// The products (gk_vocab_gemm.cu).  v0, v1: the columns of the vocabulary [v0, v1); if_missed: nothing is
+// done unless ctl->missed.
 // Logits of all compact rows: per tile of the vocabulary the maximum and the sum; keep: the
 // logits go to e, as 16-bit whole numbers of steps (kept_steps) below the tile's maximum.
-int launch_vocab_logits(const VocabCall& c, int64_t v0, int64_t v1, bool keep, int sm_count, cudaStream_t st);
+int launch_vocab_logits(const VocabCall& c, int64_t v0, int64_t v1, bool keep, bool if_missed, int sm_count, cudaStream_t st);
+// The same relative to the rows' references: sums, and the powers go to e.
+int launch_vocab_powers(const VocabCall& c, int64_t v0, int64_t v1, bool if_missed, int sm_count, cudaStream_t st);
 // The same product again with the rows' log-sum-exp known: e receives the logit gradients.
 int launch_vocab_again(const VocabCall& c, int64_t v0, int64_t v1, int sm_count, cudaStream_t st);
-// dw rows [v0, v1) = e^T hc / scale.
+// dw rows [v0, v1) = e^T hs / scale.
 int launch_vocab_dw(const VocabCall& c, int64_t v0, int64_t v1, int sm_count, cudaStream_t st);
 // dhp (split s) (+)= e w[v0:v1]; first: overwrite.
 int launch_vocab_dh(const VocabCall& c, int64_t v0, int64_t v1, bool first, int sm_count, cudaStream_t st);
 int vocab_dh_splits(int64_t n, int64_t D, int64_t vb, int sm_count);
 
 #ifdef __CUDACC__
+
+__device__ __forceinline__ bool teacher_ascending(const float4& t) { return ((int)t.w & 1) != 0; }
+__device__ __forceinline__ bool teacher_counts(const float4& t) { return ((int)t.w & 2) != 0; }
+__device__ __forceinline__ int teacher_largest(const float4& t) { return (int)t.w >> 2; }
 
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;

@@ -13,15 +13,20 @@
 // the second half catches up, and again at the start of the next tile, while the second half is
 // read out.  Eight warps read out: four for the lanes, two for the columns of a half.
 //
+// Where 256 x 256 tiles fill the SMs better (few tiles, or a bad last round) they are used instead, six
+// blocks of 32 KB in flight, one half of the tensor memory summing while the other is read out.
+//
 //   use          A (M x K)            B (N x K)            what the readout does
 //   kLogits      hc  rows x D         w   columns x D      maximum and sum of 128 columns per row
 //   kLogitsKeep  the same                                  and the logits, as 16-bit steps below that
 //                                                          maximum
+//   kPowers      the same                                  sum of 128 columns' powers relative to the row's
+//                                                          reference, and the powers in 16 bits
 //   kAgain       the same                                  logit gradients, the log-sum-exp being known
-//   kDw          e^T columns x rows   hc^T D x rows        16-bit rows of dw
+//   kDw          e^T columns x rows   hs^T D x rows        16-bit rows of dw
 //   kDh          e   rows x columns   w^T  D x columns     fp32 partial sums of dh
 //
-// e, hc and w are stored once, by rows; where the summed axis is not the contiguous one the
+// (hs: hc, or with powers hc with its rows scaled.)  e, hc and w are stored once, by rows; where the summed axis is not the contiguous one the
 // operand is read as it lies (MN-major descriptors) instead of being transposed in memory.
 // Results leave through shared memory, 32 rows x 128 bytes a warp, as TMA stores: a thread has a row of
 // its own, and stores of 16 bytes to 32 rows at once would take the time of 32.
@@ -31,14 +36,15 @@
 
 namespace gk {
 
-enum Product { kLogits, kLogitsKeep, kAgain, kDw, kDh };
+enum Product { kLogits, kLogitsKeep, kPowers, kAgain, kDw, kDh };
 
-constexpr int kTileM = 256, kHalfN = 256, kTileN = 2 * kHalfN, kBlockK = 64, kStages = 4;
+constexpr int kTileM = 256, kHalfN = 256, kTileN = 2 * kHalfN, kBlockK = 64;
 constexpr int kOperandBytes = 128 * kBlockK * 2;            // a CTA's share of A, or of a half of B, in a block
-constexpr int kStageBytes = 3 * kOperandBytes;
+constexpr int kBlockBytes = 12 * kOperandBytes;             // four blocks of a wide tile, six of a narrow one
+constexpr int kMaxStages = 6;
 constexpr int kReaders = 8;                                 // warps that read the sums out
 constexpr int kStagingBytes = 32 * 128;                     // of each of them
-constexpr int kProductSmem = kStages * kStageBytes + kReaders * kStagingBytes + 1024;   // and the alignment of the first block
+constexpr int kProductSmem = kBlockBytes + kReaders * kStagingBytes + 1024;   // and the alignment of the first block
 constexpr int kProductThreads = 128 + 32 * kReaders;
 constexpr int kRasterRows = 8;   // row tiles that are walked together: 8 x 9 tiles at once share operands in L2
 static_assert(kVocabTile == 128, "a reading warp's columns have one maximum and one sum a row");
@@ -130,7 +136,12 @@ __device__ __forceinline__ void commit_pair(uint32_t bar) {
         "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
         ::"r"(bar), "h"((uint16_t)3) : "memory");
 }
-// 64 columns of this thread's lane.  All lanes of the warp take part, whatever rows they have.
+// One column, or 64, of this thread's lane.  All lanes of the warp take part, whatever rows they have.
+__device__ __forceinline__ float tmem_ld1(uint32_t addr) {
+    uint32_t r;
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];\ntcgen05.wait::ld.sync.aligned;" : "=r"(r) : "r"(addr) : "memory");
+    return __uint_as_float(r);
+}
 __device__ __forceinline__ void tmem_ld64(uint32_t addr, float (&v)[64]) {
     uint32_t r[64];
     __syncwarp();
@@ -197,6 +208,8 @@ constexpr uint32_t kOperandHi = 1024 / 16 | 1u << 14 | 2u << 29;
 struct ProductArgs {
     VocabCall c;
     int64_t v0, v1;
+    int narrow;      // tiles of 256 columns instead of 512
+    int if_missed;   // only if the rows' references did not hold
     int first;       // kDh: overwrite the partial sums
     int splits;      // kDh: parts of the summed axis
     int wide;        // kDw: rows of dw start and end on 16-byte boundaries
@@ -210,7 +223,47 @@ struct Patch {
     int64_t row0;        // of the warp; the thread's row is row0 + lane
     int64_t col0;        // of the 128
     int64_t cols;        // columns of the result from col0 on (may be more than 128, or none)
+    int cursor;          // kLogits, kLogitsKeep, kPowers with a teacher: the row's first pair at or after col0
 };
+
+// A row's teacher pairs in ascending order are met one patch of columns at a time: the logit at each is
+// taken from tensor memory as it is summed there, instead of by a dot product of its own.
+// first_pair runs while the patch is still being summed.
+__device__ __forceinline__ int pair_index(const VocabCall& c, const int32_t* pairs, int j) {
+    const int32_t i = j < c.K ? __ldg(pairs + j) : -1;
+    return i < 0 || i >= c.V ? 0x7fffffff : i;     // pairs left out are at the end of an ascending row
+}
+__device__ __forceinline__ int first_pair(const VocabCall& c, int64_t row, int n_valid, int64_t col0) {
+    if (row >= n_valid) return c.K;
+    const int64_t r = c.row_of[row];
+    if (!teacher_ascending(c.teacher[r])) return c.K;     // this row's logits are dot products
+    const int32_t* pairs = c.t_idx + r * c.K;
+    int lo = 0, hi = c.K;
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (pair_index(c, pairs, mid) < col0) lo = mid + 1;
+        else hi = mid;
+    }
+    return lo;
+}
+__device__ __forceinline__ void take_pairs(const VocabCall& c, const Patch& w, int n_valid) {
+    const int64_t row = w.row0 + w.lane;
+    const int32_t* pairs = row < n_valid ? c.t_idx + (int64_t)c.row_of[row] * c.K : nullptr;
+    const int end = (int)(w.col0 + (w.cols < 128 ? w.cols : 128));
+    int j = w.cursor;
+    int next = j < c.K ? pair_index(c, pairs, j) : 0x7fffffff;
+    unsigned lanes;
+    while ((lanes = __ballot_sync(0xffffffffu, next < end)) != 0) {
+        const int col = __shfl_sync(0xffffffffu, next, __ffs(lanes) - 1);
+        const float z = tmem_ld1(w.tmem + (uint32_t)(col - (int)w.col0));
+        if (next == col) {
+            c.zt[row * c.K + j] = z;
+            ++j;
+            next = j < c.K ? pair_index(c, pairs, j) : 0x7fffffff;
+        }
+        __syncwarp();
+    }
+}
 
 template <int P, bool F16, bool EDGE>
 __device__ __forceinline__ void read_logits(const ProductArgs& p, const Patch& w, const CUtensorMap* out, int n_valid) {
@@ -254,6 +307,39 @@ __device__ __forceinline__ void read_logits(const ProductArgs& p, const Patch& w
             if (!EDGE || ch * 64 < cols) stage_store(w.staging, w.lane, out, (int)(w.col0 - p.v0) + ch * 64, (int)w.row0);
     }
     if (row < n_valid) c.part[w.col0 / kVocabTile * c.n_pad + row] = make_float2(m * c.zscale, (s[0] + s[1]) + (s[2] + s[3]));
+}
+
+// Powers of two of the scaled logits relative to the row's reference.  One pass; what they are worth
+// comes with the log-sum-exp: e^T (hs) and (e w) take it as a factor of their rows.
+template <bool F16, bool EDGE>
+__device__ __forceinline__ void read_powers(const ProductArgs& p, const Patch& w, const CUtensorMap* out, int n_valid) {
+    const VocabCall& c = p.c;
+    const int64_t row = w.row0 + w.lane;
+    const int cols = (int)(w.cols < 128 ? w.cols : 128);
+    const bool on = row < n_valid;
+    const float ref = on ? c.row[row].ref : 0.f;
+    float s[4] = {};
+#pragma unroll 1
+    for (int ch = 0; ch < 2; ++ch) {
+        if (EDGE && ch * 64 >= cols) break;
+        float v[64];
+        tmem_ld64(w.tmem + ch * 64, v);
+        stage_reuse(w.lane);
+#pragma unroll
+        for (int g = 0; g < 8; ++g) {
+            float e[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                e[i] = exp2_fast(fmaf(v[g * 8 + i], c.zscale, -ref));
+                if (!EDGE || ch * 64 + g * 8 + i < cols) s[i & 3] += e[i];
+            }
+            // rows up to the padding are summed over by dw
+            stage_word(w.staging, w.lane, g, on ? pack16<F16>(e[0], e[1]) : 0u, on ? pack16<F16>(e[2], e[3]) : 0u,
+                       on ? pack16<F16>(e[4], e[5]) : 0u, on ? pack16<F16>(e[6], e[7]) : 0u);
+        }
+        stage_store(w.staging, w.lane, out, (int)(w.col0 - p.v0) + ch * 64, (int)w.row0);
+    }
+    if (on) c.part[w.col0 / kVocabTile * c.n_pad + row] = make_float2(ref, (s[0] + s[1]) + (s[2] + s[3]));
 }
 
 template <bool F16>
@@ -377,20 +463,24 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                 const __grid_constant__ CUtensorMap map_out, const __grid_constant__ ProductArgs p) {
     constexpr bool kMnA = P == kDw, kMnB = P == kDw || P == kDh;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t bar_full[kStages], bar_empty[kStages], bar_sum[2], bar_free[2], bar_drain;
+    __shared__ uint64_t bar_full[kMaxStages], bar_empty[kMaxStages], bar_sum[2], bar_free[2], bar_drain;
     __shared__ uint32_t tmem_slot;
     const int tid = threadIdx.x, lane = tid & 31;
     const int warp = (int)__reduce_max_sync(0xffffffffu, (unsigned)tid >> 5);
     const uint32_t rank = cluster_rank();
-    const uint32_t stage0 = (smem_u32(smem_raw) + 1023u) & ~1023u, staging0 = stage0 + kStages * kStageBytes;
+    const uint32_t stage0 = (smem_u32(smem_raw) + 1023u) & ~1023u, staging0 = stage0 + kBlockBytes;
     const VocabCall& c = p.c;
+    if (p.if_missed && c.ctl->missed == 0) return;
+    const int width = p.narrow ? kHalfN : kTileN;
+    const int stages = p.narrow ? 6 : 4;
+    const uint32_t stage_bytes = (p.narrow ? 2 : 3) * kOperandBytes;
     const int n_valid = (int)__reduce_max_sync(0xffffffffu, (unsigned)c.ctl->n_valid);   // one value, known as such
 
     Tiles tiles;
     {
         const int64_t nv = p.v1 - p.v0, rows = ((int64_t)n_valid + kTileM - 1) / kTileM;
         tiles.tm = P == kDw ? (nv + kTileM - 1) / kTileM : rows;
-        tiles.tn = ((P == kDw || P == kDh ? c.D : nv) + kTileN - 1) / kTileN;
+        tiles.tn = ((P == kDw || P == kDh ? c.D : nv) + width - 1) / width;
         const int64_t K = P == kDw ? n_valid : P == kDh ? nv : c.D;
         tiles.kb = (int)((K + kBlockK - 1) / kBlockK);
         tiles.splits = P == kDh ? p.splits : 1;
@@ -399,7 +489,7 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     const int64_t cluster = blockIdx.x >> 1, clusters = gridDim.x >> 1;
 
     if (tid == 0) {
-        for (int s = 0; s < kStages; ++s) {
+        for (int s = 0; s < kMaxStages; ++s) {
             mbar_init(smem_u32(&bar_full[s]), 1);
             mbar_init(smem_u32(&bar_empty[s]), 1);
         }
@@ -431,8 +521,8 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
             int split, k0, k1;
             tiles.at(t, m, n, split);
             tiles.blocks(split, k0, k1);
-            const bool two = n * kTileN + kHalfN < n_cols;
-            const int ma = (int)(m * kTileM + rank * 128), nb = (int)(n * kTileN + rank * 128);
+            const bool two = !p.narrow && n * kTileN + kHalfN < n_cols;
+            const int ma = (int)(m * kTileM + rank * 128), nb = (int)(n * width + rank * 128);
             const uint32_t bytes = 2 * (two ? 3 : 2) * kOperandBytes;
             for (int k = k0; k < k1; ++k) {
                 if (!(ok = warp_wait(smem_u32(&bar_empty[stage]), phase ^ 1))) break;
@@ -440,7 +530,7 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                     const uint32_t full = smem_u32(&bar_full[stage]);
                     if (rank == 0) mbar_expect(full, bytes);
                     const uint32_t bar = in_cta(full, 0);
-                    const uint32_t a = stage0 + stage * kStageBytes, b = a + kOperandBytes;
+                    const uint32_t a = stage0 + stage * stage_bytes, b = a + kOperandBytes;
                     if constexpr (kMnA) {
                         tma_load(a, &map_a, ma, k * kBlockK, bar);
                         tma_load(a + 8192, &map_a, ma + 64, k * kBlockK, bar);
@@ -461,11 +551,11 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                     }
                 }
                 __syncwarp();
-                if (++stage == kStages) { stage = 0; phase ^= 1; }
+                if (++stage == stages) { stage = 0; phase ^= 1; }
             }
         }
         if (!ok && rank == 0)   // the copies in flight land before the memory is given back
-            for (int s = 0; s < kStages; ++s) mbar_wait(smem_u32(&bar_full[s]), s < stage ? phase : phase ^ 1);
+            for (int s = 0; s < stages; ++s) mbar_wait(smem_u32(&bar_full[s]), s < stage ? phase : phase ^ 1);
     } else if (warp == 1) {
         if (rank == 0) {
             constexpr uint32_t idesc = 1u << 4 | (F16 ? 0u : 1u) << 7 | (F16 ? 0u : 1u) << 10 | (kMnA ? 1u : 0u) << 15 |
@@ -474,37 +564,36 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
             const uint32_t a0 = operand_lo<kMnA>(stage0), b0 = operand_lo<kMnB>(stage0 + kOperandBytes);
             // one block of one half, by the elected lane
             auto issue = [&](int stage, int half, bool fresh) {
-                const uint32_t a = a0 + stage * (kStageBytes / 16), b = b0 + stage * (kStageBytes / 16) + half * (kOperandBytes / 16);
+                const uint32_t at = stage * (stage_bytes / 16);
+                const uint32_t a = a0 + at, b = b0 + at + (p.narrow ? 0 : half * (kOperandBytes / 16));
                 const uint32_t d = tmem + half * kHalfN;
                 mma_pair(d, a, b, kOperandHi, idesc, !fresh);
 #pragma unroll
                 for (int j = 1; j < kBlockK / 16; ++j) mma_pair(d, a + j * step_a, b + j * step_b, kOperandHi, idesc, true);
             };
-            int stage_a = 0, stage_b = 0;     // next block of the first half, of the second half
+            int stage_a = 0, stage_b = 0;     // next block of the first half (of the only one), of the second half
             uint32_t phase = 0, free0 = 0, free1 = 0;
+            int only = 0;                     // the half a narrow tile has
             for (int64_t t = cluster; t < tiles.total && ok; t += clusters) {
                 int64_t m, n;
                 int split, k0, k1;
                 tiles.at(t, m, n, split);
                 tiles.blocks(split, k0, k1);
                 const int blocks = k1 - k0;
-                const bool two = n * kTileN + kHalfN < n_cols;
-                if (!(ok = warp_wait(smem_u32(&bar_free[0]), free0 ^ 1))) break;
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                free0 ^= 1;
+                const bool two = !p.narrow && n * kTileN + kHalfN < n_cols;
                 int a = 0, b = 0;             // blocks issued for each half
-                auto first_half = [&](bool release) {
+                auto first_half = [&](int half, bool release) {
                     ok = warp_wait(smem_u32(&bar_full[stage_a]), phase);
                     if (!ok) return;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     if (elected()) {
-                        issue(stage_a, 0, a == 0);
+                        issue(stage_a, half, a == 0);
                         if (release) commit_pair(smem_u32(&bar_empty[stage_a]));
-                        if (a + 1 == blocks) commit_pair(smem_u32(&bar_sum[0]));
+                        if (a + 1 == blocks) commit_pair(smem_u32(&bar_sum[half]));
                     }
                     __syncwarp();
                     ++a;
-                    if (++stage_a == kStages) { stage_a = 0; phase ^= 1; }
+                    if (++stage_a == stages) { stage_a = 0; phase ^= 1; }
                 };
                 auto second_half = [&]() {
                     if (elected()) {
@@ -514,28 +603,35 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                     }
                     __syncwarp();
                     ++b;
-                    if (++stage_b == kStages) stage_b = 0;
+                    if (++stage_b == stages) stage_b = 0;
                 };
-                if (blocks == 0 && elected()) commit_pair(smem_u32(&bar_sum[0]));
+                // the first half's sums, or a narrow tile's, have been read out
+                if (!(ok = warp_wait(smem_u32(&bar_free[only]), (only ? free1 : free0) ^ 1))) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                if (only) free1 ^= 1;
+                else free0 ^= 1;
+                if (blocks == 0 && elected()) commit_pair(smem_u32(&bar_sum[only]));
                 __syncwarp();
                 if (!two) {
-                    while (a < blocks && ok) first_half(true);
+                    while (a < blocks && ok) first_half(only, true);
                     stage_b = stage_a;
+                    if (p.narrow) only ^= 1;
                     continue;
                 }
                 // ahead, as far as blocks are in flight, while the second half's sums are still being read out
-                while (ok && a < blocks && a < kStages && !__all_sync(0xffffffffu, mbar_test(smem_u32(&bar_free[1]), free1 ^ 1))) first_half(false);
+                while (ok && a < blocks && a < stages && !__all_sync(0xffffffffu, mbar_test(smem_u32(&bar_free[1]), free1 ^ 1)))
+                    first_half(0, false);
                 if (!ok || !(ok = warp_wait(smem_u32(&bar_free[1]), free1 ^ 1))) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 free1 ^= 1;
                 if (blocks == 0 && elected()) commit_pair(smem_u32(&bar_sum[1]));
                 __syncwarp();
                 while (b < a && a < blocks) second_half();
-                while (ok && a < blocks - kStages) {
-                    first_half(false);
+                while (ok && a < blocks - stages) {
+                    first_half(0, false);
                     if (ok) second_half();
                 }
-                while (ok && a < blocks) first_half(false);      // ahead over the last blocks
+                while (ok && a < blocks) first_half(0, false);      // ahead over the last blocks
                 if (ok) while (b < blocks) second_half();
             }
             if (!ok) {   // products in flight end before the tensor memory is freed
@@ -547,6 +643,7 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     } else if (warp >= 4) {
         const int quarter = warp & 3, side = (warp - 4) >> 2;    // the tensor memory lanes this warp can read; its columns
         uint32_t phases = 0;    // a bit for each half
+        int only = 0;           // the half a narrow tile has
         Patch w;
         w.lane = lane;
         w.staging = staging0 + (warp - 4) * kStagingBytes;
@@ -555,30 +652,35 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
             int split, k0, k1;
             tiles.at(t, m, n, split);
             tiles.blocks(split, k0, k1);
-            const int halves = n * kTileN + kHalfN < n_cols ? 2 : 1;
+            const bool two = !p.narrow && n * kTileN + kHalfN < n_cols;
             w.row0 = m * kTileM + rank * 128 + quarter * 32;
 #pragma unroll 1
-            for (int h = 0; h < halves; ++h) {
-                ok = mbar_wait(smem_u32(&bar_sum[h]), phases >> h & 1);
-                if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-                phases ^= 1u << h;
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const int64_t col = n * kTileN + h * kHalfN + side * 128;
+            for (int h = only; h < (two ? 2 : only + 1); ++h) {
+                const int64_t col = n * width + (two ? h * kHalfN : 0) + side * 128;
                 w.tmem = tmem + h * kHalfN + side * 128 + ((uint32_t)(quarter * 32) << 16);
                 w.cols = n_cols - col;
+                w.col0 = (P == kDw || P == kDh ? 0 : p.v0) + col;
+                constexpr bool kLogitUse = P == kLogits || P == kLogitsKeep || P == kPowers;
+                if constexpr (kLogitUse)
+                    if (c.t_idx && w.cols > 0) w.cursor = first_pair(c, w.row0 + lane, n_valid, w.col0);
+                ok = warp_wait(smem_u32(&bar_sum[h]), phases >> h & 1);
+                if (!ok) break;
+                phases ^= 1u << h;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 if (w.cols > 0) {
+                    if constexpr (kLogitUse)
+                        if (c.t_idx) take_pairs(c, w, n_valid);
                     if constexpr (P == kLogits || P == kLogitsKeep) {
-                        w.col0 = p.v0 + col;
                         if (w.cols >= 128) read_logits<P, F16, false>(p, w, &map_out, n_valid);
                         else read_logits<P, F16, true>(p, w, &map_out, n_valid);
+                    } else if constexpr (P == kPowers) {
+                        if (w.cols >= 128) read_powers<F16, false>(p, w, &map_out, n_valid);
+                        else read_powers<F16, true>(p, w, &map_out, n_valid);
                     } else if constexpr (P == kAgain) {
-                        w.col0 = p.v0 + col;
                         read_gradients<F16>(p, w, &map_out, n_valid);
                     } else if constexpr (P == kDw) {
-                        w.col0 = col;
                         read_dw<F16>(p, w, &map_out, k0 == k1);
                     } else {
-                        w.col0 = col;
                         read_dh(p, w, &map_out, n_valid, split, k0 == k1);
                     }
                 }
@@ -586,6 +688,7 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                 __syncwarp();
                 if (lane == 0) mbar_arrive_remote(in_cta(smem_u32(&bar_free[h]), 0));
             }
+            if (p.narrow) only ^= 1;
         }
         if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
@@ -636,8 +739,18 @@ static int make_map(CUtensorMap* map, Element type, const void* base, int64_t co
     return r == CUDA_SUCCESS ? GK_OK : cuda_fail(cudaErrorInvalidValue);
 }
 
+// An estimate of a product's time in us, for choosing between tiles: rounds of tiles at 0.55 us a
+// block of 64 of a wide tile and 0.29 us of a narrow one (5 % more per column: 4096 x 4096 x 32000, logits,
+// 713 against 749 us), and 4 us a round to fill and empty.
+static double tile_time(int64_t rows, int64_t cols, int64_t kb, int splits, bool narrow, int sm_count) {
+    const int64_t width = narrow ? kHalfN : kTileN, most = sm_count / 2 > 0 ? sm_count / 2 : 1;
+    const int64_t tiles = (rows + kTileM - 1) / kTileM * ((cols + width - 1) / width) * splits;
+    const double rounds = (double)((tiles + most - 1) / most), blocks = (double)((kb + splits - 1) / splits);
+    return rounds * blocks * (narrow ? 0.29 : 0.55) + 4.0 + (rounds - 1.0);
+}
+
 template <int P, bool F16>
-static int launch_product(const ProductArgs& p, int sm_count, cudaStream_t st) {
+static int launch_product(ProductArgs p, int sm_count, cudaStream_t st) {
     const VocabCall& c = p.c;
     const void* w = c.wc ? (const void*)c.wc : c.w;
     const int64_t ldw = c.wc ? c.Dp : c.ldw, nv = p.v1 - p.v0;
@@ -646,7 +759,7 @@ static int launch_product(const ProductArgs& p, int sm_count, cudaStream_t st) {
     int rc;
     if (P == kDw) {
         rc = make_map(&a, type, c.e, nv, c.n_pad, c.vb, 64);
-        if (rc == GK_OK) rc = make_map(&b, type, c.hc, c.Dp, c.n_pad, c.Dp, 64);
+        if (rc == GK_OK) rc = make_map(&b, type, c.hs, c.Dp, c.n_pad, c.Dp, 64);
         out = a;    // rows on other boundaries are stored without a map
         if (rc == GK_OK && p.wide) rc = make_map(&out, type, (const uint16_t*)c.dw + p.v0 * c.lddw, c.D, nv, c.lddw, 32);
     } else if (P == kDh) {
@@ -660,9 +773,12 @@ static int launch_product(const ProductArgs& p, int sm_count, cudaStream_t st) {
         if (rc == GK_OK && P != kLogits) rc = make_map(&out, type, c.e, nv, c.n_pad, c.vb, 32);
     }
     if (rc != GK_OK) return rc;
-    const int64_t tm = ((P == kDw ? nv : c.n) + kTileM - 1) / kTileM;
-    const int64_t tn = ((P == kDw || P == kDh ? c.D : nv) + kTileN - 1) / kTileN;
-    const int64_t pairs = tm * tn * (P == kDh ? p.splits : 1);
+    const int64_t rows = P == kDw ? nv : c.n, cols = P == kDw || P == kDh ? c.D : nv;
+    const int splits = P == kDh ? p.splits : 1;
+    const int64_t kb = ((P == kDw ? c.n : P == kDh ? nv : c.D) + kBlockK - 1) / kBlockK;
+    p.narrow = tile_time(rows, cols, kb, splits, true, sm_count) < tile_time(rows, cols, kb, splits, false, sm_count);
+    const int64_t width = p.narrow ? kHalfN : kTileN;
+    const int64_t pairs = (rows + kTileM - 1) / kTileM * ((cols + width - 1) / width) * splits;
     const int64_t most = sm_count / 2 > 0 ? sm_count / 2 : 1;
     GK_CUDA_TRY(cudaFuncSetAttribute(k_vocab_product<P, F16>, cudaFuncAttributeMaxDynamicSharedMemorySize, kProductSmem));
     k_vocab_product<P, F16><<<(unsigned)(2 * (pairs < most ? pairs : most)), kProductThreads, kProductSmem, st>>>(a, b, out, p);
@@ -672,11 +788,13 @@ static int launch_product(const ProductArgs& p, int sm_count, cudaStream_t st) {
 }
 
 template <int P>
-static int launch(const VocabCall& c, int64_t v0, int64_t v1, bool first, int sm_count, cudaStream_t st) {
+static int launch(const VocabCall& c, int64_t v0, int64_t v1, bool first, bool if_missed, int sm_count, cudaStream_t st) {
     ProductArgs p;
     p.c = c;
     p.v0 = v0;
     p.v1 = v1;
+    p.narrow = 0;
+    p.if_missed = if_missed;
     p.first = first;
     p.splits = c.splits > 0 ? c.splits : 1;
     // (the copies' hardware cuts a row's end in steps of 16 bytes, so the rows' length counts too)
@@ -684,31 +802,32 @@ static int launch(const VocabCall& c, int64_t v0, int64_t v1, bool first, int sm
     return c.f16 ? launch_product<P, true>(p, sm_count, st) : launch_product<P, false>(p, sm_count, st);
 }
 
-int launch_vocab_logits(const VocabCall& c, int64_t v0, int64_t v1, bool keep, int sm_count, cudaStream_t st) {
-    return keep ? launch<kLogitsKeep>(c, v0, v1, true, sm_count, st) : launch<kLogits>(c, v0, v1, true, sm_count, st);
+int launch_vocab_logits(const VocabCall& c, int64_t v0, int64_t v1, bool keep, bool if_missed, int sm_count, cudaStream_t st) {
+    return keep ? launch<kLogitsKeep>(c, v0, v1, true, if_missed, sm_count, st) : launch<kLogits>(c, v0, v1, true, if_missed, sm_count, st);
+}
+int launch_vocab_powers(const VocabCall& c, int64_t v0, int64_t v1, bool if_missed, int sm_count, cudaStream_t st) {
+    return launch<kPowers>(c, v0, v1, true, if_missed, sm_count, st);
 }
 int launch_vocab_again(const VocabCall& c, int64_t v0, int64_t v1, int sm_count, cudaStream_t st) {
-    return launch<kAgain>(c, v0, v1, true, sm_count, st);
+    return launch<kAgain>(c, v0, v1, true, false, sm_count, st);
 }
 int launch_vocab_dw(const VocabCall& c, int64_t v0, int64_t v1, int sm_count, cudaStream_t st) {
-    return launch<kDw>(c, v0, v1, true, sm_count, st);
+    return launch<kDw>(c, v0, v1, true, false, sm_count, st);
 }
 int launch_vocab_dh(const VocabCall& c, int64_t v0, int64_t v1, bool first, int sm_count, cudaStream_t st) {
-    return launch<kDh>(c, v0, v1, first, sm_count, st);
+    return launch<kDh>(c, v0, v1, first, false, sm_count, st);
 }
 
 // Into how many parts the summed axis of dh is split.  dh has few tiles (rows / 256 x D / 512) and a
 // long sum, so without parts most pairs of SMs would idle; each part costs a write and a read of
-// fp32 sums.  The estimate: rounds of tiles at 0.55 us a block of 64 and 4 us a tile, and the sums at
-// 5 TB/s.
+// fp32 sums, taken at 5 TB/s.
 int vocab_dh_splits(int64_t n, int64_t D, int64_t vb, int sm_count) {
-    const int64_t tiles = (n + kTileM - 1) / kTileM * ((D + kTileN - 1) / kTileN), kb = (vb + kBlockK - 1) / kBlockK;
-    const int64_t pairs = sm_count / 2 > 0 ? sm_count / 2 : 1;
+    const int64_t kb = (vb + kBlockK - 1) / kBlockK;
     int best = 1;
     double least = 0;
     for (int s = 1; s <= 32 && (s == 1 || s * 4 <= kb); ++s) {
-        const double rounds = (double)((tiles * s + pairs - 1) / pairs), blocks = (double)((kb + s - 1) / s);
-        const double us = rounds * (0.55 * blocks + 4.0) + (double)s * (double)n * (double)D * 8.0 / 5e6;
+        const double wide = tile_time(n, D, kb, s, false, sm_count), narrow = tile_time(n, D, kb, s, true, sm_count);
+        const double us = (wide < narrow ? wide : narrow) + (double)s * (double)n * (double)D * 8.0 / 5e6;
         if (s == 1 || us < least) { least = us; best = s; }
     }
     return best;

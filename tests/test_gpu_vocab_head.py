@@ -215,6 +215,59 @@ def test_distill_pairs_left_out_and_given_twice(mass):
     distill(40, 64, 30, 1024, torch.bfloat16, seed=23, T=3.0, mass=mass, repeats=True, holes=0.1)
 
 
+LARGE = [(1100, 72, 8000), (4500, 40, 2000), (130, 264, 70001)]      # 2^23 logits and more
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,D,V", LARGE)
+def test_large_calls(n, D, V, dtype):
+    hard_loss(n, D, V, dtype, seed=50, left_out=0.15, spoil=True)
+
+
+@pytest.mark.parametrize("mass", [True, False])
+def test_large_distillation(mass):
+    distill(1100, 72, 8000, 40, torch.bfloat16, seed=51, T=1.5, mass=mass)
+    distill(1100, 72, 8000, 12, torch.bfloat16, seed=52, T=0.8, mass=mass, holes=0.5)
+    distill(2200, 64, 4000, 5, torch.bfloat16, seed=53, mass=mass, holes=0.3, repeats=True)
+
+
+@pytest.mark.parametrize("budget", [0, 2 * 1280 * 3000])
+def test_large_calls_in_pieces(budget):
+    gk.gk_vocab_set_budget(budget)
+    try:
+        hard_loss(1100, 72, 8000, torch.bfloat16, seed=54, left_out=0.1)
+        distill(1100, 72, 8000, 9, torch.bfloat16, seed=55)
+    finally:
+        gk.gk_vocab_set_budget(2 << 30)
+
+
+@pytest.mark.parametrize("budget", [2 << 30, 2 * 1280 * 3000])
+@pytest.mark.parametrize("low", [-40.0, -300.0])
+def test_classes_far_below_the_rest(low, budget):
+    """Losses up to some hundreds: a reference at the class is then no use for the row's powers.  The
+    last column has some rows' highest logit, where a piece of its own may find it."""
+    n, D, V = 1100, 72, 8000
+    gen, h, w, hd, wd = make(n, D, V, torch.bfloat16, 56)
+    h[:, 0] = 1.0
+    w[:, 0] = 0.0
+    target = torch.randint(0, V - 1, (n,), generator=gen)
+    target[::3] = 5
+    w[5, 0] = low
+    w[V - 1] = 0.0
+    w[V - 1, 0] = -low / 4
+    hd.copy_(h)
+    wd.copy_(w)
+    g = torch.randn(n, generator=gen)
+    out = Out(n, D, V, torch.bfloat16)
+    gk.gk_vocab_set_budget(budget)
+    try:
+        gk.gk_vocab_loss(hd, wd, target.to(DEV), out.loss[:n], out.lse[:n], row_grad=g.to(DEV), dh=out.dh, dw=out.dw)
+    finally:
+        gk.gk_vocab_set_budget(2 << 30)
+    check(out, h, w, target[:, None], torch.ones(n, 1, dtype=torch.float64), torch.zeros(n, 1, dtype=torch.float64), 1.0,
+          g.double(), torch.ones(n, dtype=torch.bool), torch.bfloat16)
+
+
 @pytest.mark.parametrize("scale", [1e-6, 1e5])
 def test_gradients_of_rows_of_any_size(scale):
     """Row gradients far from 1: the 16-bit logit gradients are scaled by a power of two."""
