@@ -207,6 +207,10 @@ template <bool F16>
 __global__ void __launch_bounds__(128) k_vocab_gather(VocabCall c) {
     const int at = blockIdx.x, n_valid = c.ctl->n_valid;
     const int tid = threadIdx.x, lane = tid & 31;
+    if (c.dh && at < c.n && c.at_of[at] < 0) {
+        uint16_t* out = (uint16_t*)c.dh + at * c.lddh;
+        for (int64_t i = tid; i < c.D; i += 128) out[i] = 0;
+    }
     if (at >= round_up(n_valid, kVocabRowPad)) return;
     uint16_t* to = c.hc + (int64_t)at * c.Dp;
     if (at >= n_valid) {
@@ -329,9 +333,6 @@ __global__ void __launch_bounds__(1024) k_vocab_rows_done(VocabCall c) {
     }
 }
 
-// What a row's powers are worth.
-__device__ __forceinline__ float powers_worth(const VocabRow& r) { return r.coef * exp2f(r.ref - r.lse2); }
-
 // ---------------------------------------------------------------------------
 // 5. The gradients' operand for one piece.  The targets' entries are formed in fp32 from their own logits
 // and written over, so that 1 - p loses nothing where p is near 1.
@@ -422,19 +423,24 @@ __global__ void __launch_bounds__(128) k_vocab_targets(VocabCall c, int64_t v0, 
     write_targets<F16>(c, at, v0, v1, v0, threadIdx.x, 128);
 }
 
-// dh in the caller's rows: the splits' partial sums added in their order, zero for rows left out.
+// dh in the caller's rows from its parts' sums, added in their order.
 template <bool F16>
 __global__ void __launch_bounds__(256) k_vocab_finish_dh(VocabCall c) {
-    const int64_t r = blockIdx.x;
-    const int at = c.at_of[r];
-    uint16_t* to = (uint16_t*)c.dh + r * c.lddh;
-    const float inv = c.ctl->inv_scale * (c.powers && at >= 0 ? powers_worth(c.row[at]) : 1.f);
-    for (int64_t i = threadIdx.x; i < c.D; i += 256) {
-        float s = 0.f;
-        if (at >= 0)
-            for (int k = 0; k < c.splits; ++k) s += c.dhp[((int64_t)k * c.n_pad + at) * c.Dp + i];
-        to[i] = to16<F16>(s * inv);
+    const int64_t at = blockIdx.x, i = ((int64_t)blockIdx.y * 256 + threadIdx.x) * 2;
+    if (at >= c.ctl->n_valid || i >= c.D) return;
+    const float f = c.ctl->inv_scale * (c.powers ? powers_worth(c.row[at]) : 1.f);
+    const float* from = c.dhp + at * c.Dp + i;
+    const int64_t part = c.n_pad * c.Dp;
+    float2 s = *(const float2*)from;
+#pragma unroll 4
+    for (int k = 1; k < c.splits; ++k) {
+        const float2 x = *(const float2*)(from + k * part);
+        s.x += x.x;
+        s.y += x.y;
     }
+    uint16_t* to = (uint16_t*)c.dh + (int64_t)c.row_of[at] * c.lddh + i;
+    to[0] = to16<F16>(s.x * f);
+    if (i + 1 < c.D) to[1] = to16<F16>(s.y * f);
 }
 
 // ---------------------------------------------------------------------------
@@ -481,7 +487,8 @@ static size_t lay_out(VocabCall& c, bool distill, bool copy_w, char* base) {
     c.part = (float2*)take(8 * tiles * np);
     c.row = (VocabRow*)take(sizeof(VocabRow) * np);
     c.e = (uint16_t*)(c.vb > 0 ? take(2 * np * (size_t)c.vb) : nullptr);
-    c.dhp = (float*)(c.splits > 0 ? take(4 * (size_t)c.splits * np * c.Dp) : nullptr);
+    // one part and one piece: dh's sums are final when its product ends
+    c.dhp = (float*)(c.splits > 1 || (c.splits == 1 && c.vb < c.V) ? take(4 * (size_t)c.splits * np * c.Dp) : nullptr);
     return at;
 }
 
@@ -512,7 +519,7 @@ static void size_call(VocabCall& c, bool want_dh, bool want_dw, int sm_count) {
     c.Dp = round_up(c.D, 64);
     c.vb = want_dh || want_dw ? piece_columns(c.n_pad, c.V) : 0;
     c.powers = !c.f16 && c.vb > 0 && c.n * c.V >= kPowersFrom;
-    c.splits = want_dh ? vocab_dh_splits(c.n, c.D, c.vb, sm_count) : 0;
+    c.splits = want_dh ? vocab_dh_splits(c.n, c.D, c.vb < c.V ? c.vb : c.V, want_dw, sm_count) : 0;
 }
 
 template <bool F16>
@@ -559,12 +566,11 @@ static int enqueue(const VocabCall& c, bool distill, int sms, cudaStream_t st) {
         }
         GK_CUDA_TRY(cudaGetLastError());
         note_launch(v0 > 0 || !c.powers ? 1 : 0);
-        if (c.dw) rc = launch_vocab_dw(c, v0, v1, sms, st);
-        if (rc == GK_OK && c.dh) rc = launch_vocab_dh(c, v0, v1, v0 == 0, sms, st);
+        rc = launch_vocab_grads(c, v0, v1, v0 == 0, sms, st);
         if (rc != GK_OK) return rc;
     }
-    if (c.dh) {
-        k_vocab_finish_dh<F16><<<n, 256, 0, st>>>(c);
+    if (c.dhp) {
+        k_vocab_finish_dh<F16><<<dim3(n, (unsigned)((c.D + 511) / 512)), 256, 0, st>>>(c);
         GK_CUDA_TRY(cudaGetLastError());
         note_launch();
     }

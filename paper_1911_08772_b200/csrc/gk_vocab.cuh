@@ -71,7 +71,7 @@ struct VocabCall {
     VocabRow* row;              // n_pad
     uint16_t* e;                // n_pad x vb: one piece's powers, or kept logits and then logit gradients
     int64_t vb;                 // columns of a piece, a multiple of 256 (the pitch of e)
-    float* dhp;                 // splits x n_pad x Dp partial sums of dh
+    float* dhp;                 // splits x n_pad x Dp partial sums of dh; nullptr: dh is stored by its product
     int splits;
 };
 
@@ -86,11 +86,10 @@ int launch_vocab_logits(const VocabCall& c, int64_t v0, int64_t v1, bool keep, b
 int launch_vocab_powers(const VocabCall& c, int64_t v0, int64_t v1, bool if_missed, int sm_count, cudaStream_t st);
 // The same product again with the rows' log-sum-exp known: e receives the logit gradients.
 int launch_vocab_again(const VocabCall& c, int64_t v0, int64_t v1, int sm_count, cudaStream_t st);
-// dw rows [v0, v1) = e^T hs / scale.
-int launch_vocab_dw(const VocabCall& c, int64_t v0, int64_t v1, int sm_count, cudaStream_t st);
-// dhp (split s) (+)= e w[v0:v1]; first: overwrite.
-int launch_vocab_dh(const VocabCall& c, int64_t v0, int64_t v1, bool first, int sm_count, cudaStream_t st);
-int vocab_dh_splits(int64_t n, int64_t D, int64_t vb, int sm_count);
+// dw rows [v0, v1) = e^T hs / scale, and dh = e w[v0:v1] times each row's factor, or its sums in fp32 in
+// `splits` parts added to dhp (first: overwritten).
+int launch_vocab_grads(const VocabCall& c, int64_t v0, int64_t v1, bool first, int sm_count, cudaStream_t st);
+int vocab_dh_splits(int64_t n, int64_t D, int64_t vb, bool dw, int sm_count);
 
 #ifdef __CUDACC__
 
@@ -135,6 +134,9 @@ __device__ __forceinline__ unsigned pack16(float lo, float hi) {
     else asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
+
+// What a row's powers are worth.
+__device__ __forceinline__ float powers_worth(const VocabRow& r) { return r.coef * exp2f(r.ref - r.lse2); }
 
 // Joins (m, s) pairs of a running maximum and sum, in units of log 2.  A part without a term
 // has m = -inf and s = 0.

@@ -1,6 +1,6 @@
 // The products of the vocabulary head (gk_vocab.cu) on the fifth-generation tensor cores.
 //
-// One persistent kernel, five uses of it.  A pair of SMs (a cluster of two CTAs) computes a
+// One persistent kernel and its uses.  A pair of SMs (a cluster of two CTAs) computes a
 // 256 x 512 tile of the result with tcgen05.mma.cta_group::2, as two 256 x 256 halves: each CTA holds
 // 128 rows of A, 128 of the 256 columns of each half of B, and 128 x 512 fp32 sums, which is all of its
 // tensor memory.  Operands arrive by TMA in blocks of 64 along the summed axis, four blocks in
@@ -23,9 +23,10 @@
 //   kPowers      the same                                  sum of 128 columns' powers relative to the row's
 //                                                          reference, and the powers in 16 bits
 //   kAgain       the same                                  logit gradients, the log-sum-exp being known
-//   kDw          e^T columns x rows   hs^T D x rows        16-bit rows of dw
-//   kDh          e   rows x columns   w^T  D x columns     fp32 partial sums of dh
+//   kGrads, dh   e   rows x columns   w^T  D x columns     16-bit rows of dh, or fp32 partial sums of them
+//   kGrads, dw   e^T columns x rows   hs^T D x rows        16-bit rows of dw
 //
+// The two gradients are tiles of one launch, dh's long ones first, so that they fill the SMs together.
 // (hs: hc, or with powers hc with its rows scaled.)  e, hc and w are stored once, by rows; where the summed axis is not the contiguous one the
 // operand is read as it lies (MN-major descriptors) instead of being transposed in memory.
 // Results leave through shared memory, 32 rows x 128 bytes a warp, as TMA stores: a thread has a row of
@@ -36,7 +37,7 @@
 
 namespace gk {
 
-enum Product { kLogits, kLogitsKeep, kPowers, kAgain, kDw, kDh };
+enum Product { kLogits, kLogitsKeep, kPowers, kAgain, kGrads };
 
 constexpr int kTileM = 256, kHalfN = 256, kTileN = 2 * kHalfN, kBlockK = 64;
 constexpr int kOperandBytes = 128 * kBlockK * 2;            // a CTA's share of A, or of a half of B, in a block
@@ -210,9 +211,10 @@ struct ProductArgs {
     int64_t v0, v1;
     int narrow;      // tiles of 256 columns instead of 512
     int if_missed;   // only if the rows' references did not hold
-    int first;       // kDh: overwrite the partial sums
-    int splits;      // kDh: parts of the summed axis
-    int wide;        // kDw: rows of dw start and end on 16-byte boundaries
+    int first;       // dh: overwrite the partial sums
+    int splits;      // dh: parts of the summed axis
+    int direct;      // dh: one part and one piece, 16-bit rows are stored at once
+    int wide;        // dw: rows start and end on 16-byte boundaries
 };
 
 // What a reading warp finishes: 128 columns of 32 rows.
@@ -369,6 +371,38 @@ __device__ __forceinline__ void read_gradients(const ProductArgs& p, const Patch
     }
 }
 
+// A warp's 32 rows x 64 16-bit columns from its staging memory, a row at a time with two columns a lane,
+// to rows on any boundary.  `to`: where the thread's own row has column 0 of the 64, nullptr: nowhere.
+__device__ __forceinline__ void store_rows(uint32_t staging, int lane, uint16_t* to, int64_t cols) {
+    __syncwarp();
+#pragma unroll 4
+    for (int r = 0; r < 32; ++r) {
+        uint16_t* at = (uint16_t*)__shfl_sync(0xffffffffu, (unsigned long long)to, r);
+        if (!at) continue;
+        at += lane * 2;
+        uint32_t x;
+        asm volatile("ld.shared.b32 %0, [%1];"
+                     : "=r"(x) : "r"(staging + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4) : "memory");
+        if (lane * 2 + 1 < cols && ((uintptr_t)at & 3) == 0) *(uint32_t*)at = x;
+        else {
+            if (lane * 2 < cols) at[0] = (uint16_t)x;
+            if (lane * 2 + 1 < cols) at[1] = (uint16_t)(x >> 16);
+        }
+    }
+    __syncwarp();
+}
+
+template <bool F16>
+__device__ __forceinline__ void stage16(const Patch& w, const float (&v)[64], float f, bool empty) {
+#pragma unroll
+    for (int g = 0; g < 8; ++g) {
+        uint32_t x[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = empty ? 0u : pack16<F16>(v[8 * g + 2 * i] * f, v[8 * g + 2 * i + 1] * f);
+        stage_word(w.staging, w.lane, g, x[0], x[1], x[2], x[3]);
+    }
+}
+
 template <bool F16>
 __device__ __forceinline__ void read_dw(const ProductArgs& p, const Patch& w, const CUtensorMap* out, bool empty) {
     const VocabCall& c = p.c;
@@ -381,46 +415,42 @@ __device__ __forceinline__ void read_dw(const ProductArgs& p, const Patch& w, co
         float v[64];
         tmem_ld64(w.tmem + ch * 64, v);
         stage_reuse(w.lane);
-#pragma unroll
-        for (int i = 0; i < 64; ++i) v[i] = empty ? 0.f : v[i] * inv;
-#pragma unroll
-        for (int g = 0; g < 8; ++g)
-            stage_word(w.staging, w.lane, g, pack16<F16>(v[8 * g], v[8 * g + 1]), pack16<F16>(v[8 * g + 2], v[8 * g + 3]),
-                       pack16<F16>(v[8 * g + 4], v[8 * g + 5]), pack16<F16>(v[8 * g + 6], v[8 * g + 7]));
-        if (p.wide) {
-            stage_store(w.staging, w.lane, out, (int)w.col0 + ch * 64, (int)w.row0);
-        } else {
-            // rows on any boundary: a row at a time, two columns a lane
-            __syncwarp();
-            const int64_t col = w.col0 + ch * 64 + w.lane * 2;
-            uint16_t* to = (uint16_t*)c.dw + (p.v0 + w.row0) * c.lddw + col;
-#pragma unroll 8
-            for (int r = 0; r < 32; ++r, to += c.lddw) {
-                uint32_t x;
-                asm volatile("ld.shared.b32 %0, [%1];"
-                             : "=r"(x) : "r"(w.staging + r * 128 + (((w.lane >> 2) ^ (r & 7)) << 4) + (w.lane & 3) * 4) : "memory");
-                if (r >= rows) continue;
-                if (col + 1 < c.D && ((uintptr_t)to & 3) == 0) *(uint32_t*)to = x;
-                else {
-                    if (col < c.D) to[0] = (uint16_t)x;
-                    if (col + 1 < c.D) to[1] = (uint16_t)(x >> 16);
-                }
-            }
-            __syncwarp();
-        }
+        stage16<F16>(w, v, inv, empty);
+        if (p.wide) stage_store(w.staging, w.lane, out, (int)w.col0 + ch * 64, (int)w.row0);
+        else store_rows(w.staging, w.lane, w.lane < rows ? (uint16_t*)c.dw + (p.v0 + w.row0 + w.lane) * c.lddw + w.col0 + ch * 64 : nullptr,
+                        w.cols - ch * 64);
     }
 }
 
-__device__ __forceinline__ void read_dh(const ProductArgs& p, const Patch& w, const CUtensorMap* out, int n_valid, int split, bool empty) {
+template <bool F16>
+__device__ __forceinline__ void read_dh(const ProductArgs& p, const Patch& w, const CUtensorMap* out, int n_valid, int split) {
+    const VocabCall& c = p.c;
     if (w.row0 >= n_valid) return;
-    const int y = (int)(split * p.c.n_pad + w.row0);
+    const int64_t row = w.row0 + w.lane;
+    if (p.direct) {
+        float f = 0.f;
+        uint16_t* to = nullptr;
+        if (row < n_valid) {
+            f = c.ctl->inv_scale * (c.powers ? powers_worth(c.row[row]) : 1.f);
+            to = (uint16_t*)c.dh + (int64_t)c.row_of[row] * c.lddh + w.col0;
+        }
+#pragma unroll 1
+        for (int ch = 0; ch < 2; ++ch) {
+            if (ch * 64 >= w.cols) break;
+            float v[64];
+            tmem_ld64(w.tmem + ch * 64, v);
+            stage_reuse(w.lane);
+            stage16<F16>(w, v, f, false);
+            store_rows(w.staging, w.lane, to ? to + ch * 64 : nullptr, w.cols - ch * 64);
+        }
+        return;
+    }
+    const int y = (int)(split * c.n_pad + w.row0);
 #pragma unroll 1
     for (int ch = 0; ch < 2; ++ch) {
         if (ch * 64 >= w.cols) break;
         float v[64];
         tmem_ld64(w.tmem + ch * 64, v);
-#pragma unroll
-        for (int i = 0; i < 64; ++i) v[i] = empty ? 0.f : v[i];
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
             stage_reuse(w.lane);
@@ -457,11 +487,23 @@ struct Tiles {
     }
 };
 
+__device__ __forceinline__ Tiles make_tiles(int64_t rows, int64_t cols, int64_t K, int width, int splits) {
+    Tiles t;
+    t.tm = (rows + kTileM - 1) / kTileM;
+    t.tn = (cols + width - 1) / width;
+    t.kb = (int)((K + kBlockK - 1) / kBlockK);
+    t.splits = splits;
+    t.total = t.tm * t.tn * splits;
+    return t;
+}
+
+// map_a2, map_b2, map_out2: dw's operands and result in kGrads.
 template <int P, bool F16>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1)
 k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
-                const __grid_constant__ CUtensorMap map_out, const __grid_constant__ ProductArgs p) {
-    constexpr bool kMnA = P == kDw, kMnB = P == kDw || P == kDh;
+                const __grid_constant__ CUtensorMap map_out, const __grid_constant__ CUtensorMap map_a2,
+                const __grid_constant__ CUtensorMap map_b2, const __grid_constant__ CUtensorMap map_out2,
+                const __grid_constant__ ProductArgs p) {
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t bar_full[kMaxStages], bar_empty[kMaxStages], bar_sum[2], bar_free[2], bar_drain;
     __shared__ uint32_t tmem_slot;
@@ -476,16 +518,10 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     const uint32_t stage_bytes = (p.narrow ? 2 : 3) * kOperandBytes;
     const int n_valid = (int)__reduce_max_sync(0xffffffffu, (unsigned)c.ctl->n_valid);   // one value, known as such
 
-    Tiles tiles;
-    {
-        const int64_t nv = p.v1 - p.v0, rows = ((int64_t)n_valid + kTileM - 1) / kTileM;
-        tiles.tm = P == kDw ? (nv + kTileM - 1) / kTileM : rows;
-        tiles.tn = ((P == kDw || P == kDh ? c.D : nv) + width - 1) / width;
-        const int64_t K = P == kDw ? n_valid : P == kDh ? nv : c.D;
-        tiles.kb = (int)((K + kBlockK - 1) / kBlockK);
-        tiles.splits = P == kDh ? p.splits : 1;
-        tiles.total = tiles.tm * tiles.tn * tiles.splits;
-    }
+    const int64_t nv = p.v1 - p.v0, n_cols = P == kGrads ? c.D : nv;      // columns of the result
+    const Tiles tiles = P == kGrads ? make_tiles(c.dh ? n_valid : 0, c.D, nv, width, p.splits) : make_tiles(n_valid, nv, c.D, width, 1);
+    const Tiles tiles2 = make_tiles(P == kGrads && c.dw ? nv : 0, c.D, n_valid, width, 1);
+    const int64_t total = tiles.total + tiles2.total;
     const int64_t cluster = blockIdx.x >> 1, clusters = gridDim.x >> 1;
 
     if (tid == 0) {
@@ -510,17 +546,17 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = tmem_slot;
 
-    const int64_t n_cols = P == kDw || P == kDh ? c.D : p.v1 - p.v0;   // of the result
     bool ok = true;
     if (warp == 0) {
         // producer: this CTA's 128 rows of A and of each half of B; the leader's barrier counts both CTAs' bytes
         int stage = 0;
         uint32_t phase = 0;
-        for (int64_t t = cluster; t < tiles.total && ok; t += clusters) {
+        for (int64_t t = cluster; t < total && ok; t += clusters) {
             int64_t m, n;
             int split, k0, k1;
-            tiles.at(t, m, n, split);
-            tiles.blocks(split, k0, k1);
+            const bool dw = P == kGrads && t >= tiles.total;
+            (dw ? tiles2 : tiles).at(dw ? t - tiles.total : t, m, n, split);
+            (dw ? tiles2 : tiles).blocks(split, k0, k1);
             const bool two = !p.narrow && n * kTileN + kHalfN < n_cols;
             const int ma = (int)(m * kTileM + rank * 128), nb = (int)(n * width + rank * 128);
             const uint32_t bytes = 2 * (two ? 3 : 2) * kOperandBytes;
@@ -531,21 +567,24 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                     if (rank == 0) mbar_expect(full, bytes);
                     const uint32_t bar = in_cta(full, 0);
                     const uint32_t a = stage0 + stage * stage_bytes, b = a + kOperandBytes;
-                    if constexpr (kMnA) {
-                        tma_load(a, &map_a, ma, k * kBlockK, bar);
-                        tma_load(a + 8192, &map_a, ma + 64, k * kBlockK, bar);
-                    } else {
-                        tma_load(a, &map_a, k * kBlockK, ma, bar);
-                    }
-                    if constexpr (kMnB) {
-                        const int y = (P == kDh ? (int)p.v0 : 0) + k * kBlockK;
-                        tma_load(b, &map_b, nb, y, bar);
-                        tma_load(b + 8192, &map_b, nb + 64, y, bar);
+                    if constexpr (P == kGrads) {
+                        // B lies by the summed axis in both; A in dw
+                        const CUtensorMap* mb = dw ? &map_b2 : &map_b;
+                        const int y = (dw ? 0 : (int)p.v0) + k * kBlockK;
+                        if (dw) {
+                            tma_load(a, &map_a2, ma, y, bar);
+                            tma_load(a + 8192, &map_a2, ma + 64, y, bar);
+                        } else {
+                            tma_load(a, &map_a, k * kBlockK, ma, bar);
+                        }
+                        tma_load(b, mb, nb, y, bar);
+                        tma_load(b + 8192, mb, nb + 64, y, bar);
                         if (two) {
-                            tma_load(b + kOperandBytes, &map_b, nb + kHalfN, y, bar);
-                            tma_load(b + kOperandBytes + 8192, &map_b, nb + kHalfN + 64, y, bar);
+                            tma_load(b + kOperandBytes, mb, nb + kHalfN, y, bar);
+                            tma_load(b + kOperandBytes + 8192, mb, nb + kHalfN + 64, y, bar);
                         }
                     } else {
+                        tma_load(a, &map_a, k * kBlockK, ma, bar);
                         tma_load(b, &map_b, k * kBlockK, (int)p.v0 + nb, bar);
                         if (two) tma_load(b + kOperandBytes, &map_b, k * kBlockK, (int)p.v0 + nb + kHalfN, bar);
                     }
@@ -558,10 +597,12 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
             for (int s = 0; s < stages; ++s) mbar_wait(smem_u32(&bar_full[s]), s < stage ? phase : phase ^ 1);
     } else if (warp == 1) {
         if (rank == 0) {
-            constexpr uint32_t idesc = 1u << 4 | (F16 ? 0u : 1u) << 7 | (F16 ? 0u : 1u) << 10 | (kMnA ? 1u : 0u) << 15 |
-                                       (kMnB ? 1u : 0u) << 16 | (uint32_t)(kHalfN / 8) << 17 | (uint32_t)(kTileM / 16) << 24;
-            constexpr uint32_t step_a = (kMnA ? 2048 : 32) / 16, step_b = (kMnB ? 2048 : 32) / 16;
-            const uint32_t a0 = operand_lo<kMnA>(stage0), b0 = operand_lo<kMnB>(stage0 + kOperandBytes);
+            constexpr bool kMnB = P == kGrads;
+            constexpr uint32_t kDesc = 1u << 4 | (F16 ? 0u : 1u) << 7 | (F16 ? 0u : 1u) << 10 | (kMnB ? 1u : 0u) << 16 |
+                                       (uint32_t)(kHalfN / 8) << 17 | (uint32_t)(kTileM / 16) << 24;
+            constexpr uint32_t step_b = (kMnB ? 2048 : 32) / 16;
+            const uint32_t b0 = operand_lo<kMnB>(stage0 + kOperandBytes);
+            uint32_t idesc = kDesc, step_a = 32 / 16, a0 = operand_lo<false>(stage0);
             // one block of one half, by the elected lane
             auto issue = [&](int stage, int half, bool fresh) {
                 const uint32_t at = stage * (stage_bytes / 16);
@@ -574,13 +615,19 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
             int stage_a = 0, stage_b = 0;     // next block of the first half (of the only one), of the second half
             uint32_t phase = 0, free0 = 0, free1 = 0;
             int only = 0;                     // the half a narrow tile has
-            for (int64_t t = cluster; t < tiles.total && ok; t += clusters) {
+            for (int64_t t = cluster; t < total && ok; t += clusters) {
                 int64_t m, n;
                 int split, k0, k1;
-                tiles.at(t, m, n, split);
-                tiles.blocks(split, k0, k1);
+                const bool dw = P == kGrads && t >= tiles.total;
+                (dw ? tiles2 : tiles).at(dw ? t - tiles.total : t, m, n, split);
+                (dw ? tiles2 : tiles).blocks(split, k0, k1);
                 const int blocks = k1 - k0;
                 const bool two = !p.narrow && n * kTileN + kHalfN < n_cols;
+                if (dw) {
+                    idesc = kDesc | 1u << 15;
+                    step_a = 2048 / 16;
+                    a0 = operand_lo<true>(stage0);
+                }
                 int a = 0, b = 0;             // blocks issued for each half
                 auto first_half = [&](int half, bool release) {
                     ok = warp_wait(smem_u32(&bar_full[stage_a]), phase);
@@ -647,11 +694,12 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         Patch w;
         w.lane = lane;
         w.staging = staging0 + (warp - 4) * kStagingBytes;
-        for (int64_t t = cluster; t < tiles.total && ok; t += clusters) {
+        for (int64_t t = cluster; t < total && ok; t += clusters) {
             int64_t m, n;
             int split, k0, k1;
-            tiles.at(t, m, n, split);
-            tiles.blocks(split, k0, k1);
+            const bool dw = P == kGrads && t >= tiles.total;
+            (dw ? tiles2 : tiles).at(dw ? t - tiles.total : t, m, n, split);
+            (dw ? tiles2 : tiles).blocks(split, k0, k1);
             const bool two = !p.narrow && n * kTileN + kHalfN < n_cols;
             w.row0 = m * kTileM + rank * 128 + quarter * 32;
 #pragma unroll 1
@@ -659,7 +707,7 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                 const int64_t col = n * width + (two ? h * kHalfN : 0) + side * 128;
                 w.tmem = tmem + h * kHalfN + side * 128 + ((uint32_t)(quarter * 32) << 16);
                 w.cols = n_cols - col;
-                w.col0 = (P == kDw || P == kDh ? 0 : p.v0) + col;
+                w.col0 = (P == kGrads ? 0 : p.v0) + col;
                 constexpr bool kLogitUse = P == kLogits || P == kLogitsKeep || P == kPowers;
                 if constexpr (kLogitUse)
                     if (c.t_idx && w.cols > 0) w.cursor = first_pair(c, w.row0 + lane, n_valid, w.col0);
@@ -678,10 +726,9 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                         else read_powers<F16, true>(p, w, &map_out, n_valid);
                     } else if constexpr (P == kAgain) {
                         read_gradients<F16>(p, w, &map_out, n_valid);
-                    } else if constexpr (P == kDw) {
-                        read_dw<F16>(p, w, &map_out, k0 == k1);
                     } else {
-                        read_dh(p, w, &map_out, n_valid, split, k0 == k1);
+                        if (dw) read_dw<F16>(p, w, &map_out2, k0 == k1);
+                        else read_dh<F16>(p, w, &map_out, n_valid, split);
                     }
                 }
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -739,14 +786,24 @@ static int make_map(CUtensorMap* map, Element type, const void* base, int64_t co
     return r == CUDA_SUCCESS ? GK_OK : cuda_fail(cudaErrorInvalidValue);
 }
 
-// An estimate of a product's time in us, for choosing between tiles: rounds of tiles at 0.55 us a
-// block of 64 of a wide tile and 0.29 us of a narrow one (5 % more per column: 4096 x 4096 x 32000, logits,
-// 713 against 749 us), and 4 us a round to fill and empty.
-static double tile_time(int64_t rows, int64_t cols, int64_t kb, int splits, bool narrow, int sm_count) {
+// An estimate of a launch's time in us, for choosing between tiles and parts: what the busiest pair of
+// SMs sums, at 0.55 us a block of 64 of a wide tile and 0.29 us of a narrow one (5 % more per column: 4096 x
+// 4096 x 32000, logits, 713 against 749 us), 1 us a tile and 4 us to fill and empty.  The first kind
+// of tile (dh's, in `splits` parts) is dealt out before the second.
+struct Share { int64_t rows, cols, kb; };
+static double launch_time(const Share& first, int splits, const Share& second, bool narrow, int sm_count) {
     const int64_t width = narrow ? kHalfN : kTileN, most = sm_count / 2 > 0 ? sm_count / 2 : 1;
-    const int64_t tiles = (rows + kTileM - 1) / kTileM * ((cols + width - 1) / width) * splits;
-    const double rounds = (double)((tiles + most - 1) / most), blocks = (double)((kb + splits - 1) / splits);
-    return rounds * blocks * (narrow ? 0.29 : 0.55) + 4.0 + (rounds - 1.0);
+    const int64_t n1 = (first.rows + kTileM - 1) / kTileM * ((first.cols + width - 1) / width) * splits;
+    const int64_t n2 = (second.rows + kTileM - 1) / kTileM * ((second.cols + width - 1) / width);
+    const double block = narrow ? 0.29 : 0.55;
+    const double t1 = (double)((first.kb + splits - 1) / splits) * block + 1.0, t2 = (double)second.kb * block + 1.0;
+    double longest = 0;
+    for (int64_t i = 0; i < most; ++i) {
+        const int64_t a = n1 > i ? (n1 - i + most - 1) / most : 0, all = n1 + n2 > i ? (n1 + n2 - i + most - 1) / most : 0;
+        const double us = (double)a * t1 + (double)(all - a) * t2;
+        if (us > longest) longest = us;
+    }
+    return longest + 4.0;
 }
 
 template <int P, bool F16>
@@ -755,33 +812,36 @@ static int launch_product(ProductArgs p, int sm_count, cudaStream_t st) {
     const void* w = c.wc ? (const void*)c.wc : c.w;
     const int64_t ldw = c.wc ? c.Dp : c.ldw, nv = p.v1 - p.v0;
     const Element type = F16 ? kF16 : kBf16;
-    CUtensorMap a, b, out;
+    CUtensorMap a, b, out, a2, b2, out2;
+    Share first, second = {0, 1, 1};
     int rc;
-    if (P == kDw) {
-        rc = make_map(&a, type, c.e, nv, c.n_pad, c.vb, 64);
-        if (rc == GK_OK) rc = make_map(&b, type, c.hs, c.Dp, c.n_pad, c.Dp, 64);
-        out = a;    // rows on other boundaries are stored without a map
-        if (rc == GK_OK && p.wide) rc = make_map(&out, type, (const uint16_t*)c.dw + p.v0 * c.lddw, c.D, nv, c.lddw, 32);
-    } else if (P == kDh) {
+    if (P == kGrads) {
         rc = make_map(&a, type, c.e, nv, c.n_pad, c.vb, 128);
         if (rc == GK_OK) rc = make_map(&b, type, w, c.D, c.V, ldw, 64);
-        if (rc == GK_OK) rc = make_map(&out, kF32, c.dhp, c.Dp, p.splits * c.n_pad, c.Dp, 32);
+        out = a;     // not used by direct stores
+        if (rc == GK_OK && c.dh && !p.direct) rc = make_map(&out, kF32, c.dhp, c.Dp, p.splits * c.n_pad, c.Dp, 32);
+        if (rc == GK_OK) rc = make_map(&a2, type, c.e, nv, c.n_pad, c.vb, 64);
+        if (rc == GK_OK) rc = make_map(&b2, type, c.hs, c.Dp, c.n_pad, c.Dp, 64);
+        out2 = a2;   // rows on other boundaries are stored without a map
+        if (rc == GK_OK && c.dw && p.wide) rc = make_map(&out2, type, (const uint16_t*)c.dw + p.v0 * c.lddw, c.D, nv, c.lddw, 32);
+        first = {c.dh ? c.n : 0, c.D, (nv + kBlockK - 1) / kBlockK};
+        second = {c.dw ? nv : 0, c.D, (c.n + kBlockK - 1) / kBlockK};
     } else {
         rc = make_map(&a, type, c.hc, c.Dp, c.n_pad, c.Dp, 128);
         if (rc == GK_OK) rc = make_map(&b, type, w, c.D, c.V, ldw, 128);
-        out = a;    // kLogits keeps nothing
+        out = a;     // kLogits keeps nothing
         if (rc == GK_OK && P != kLogits) rc = make_map(&out, type, c.e, nv, c.n_pad, c.vb, 32);
+        a2 = b2 = out2 = a;
+        first = {c.n, nv, (c.D + kBlockK - 1) / kBlockK};
     }
     if (rc != GK_OK) return rc;
-    const int64_t rows = P == kDw ? nv : c.n, cols = P == kDw || P == kDh ? c.D : nv;
-    const int splits = P == kDh ? p.splits : 1;
-    const int64_t kb = ((P == kDw ? c.n : P == kDh ? nv : c.D) + kBlockK - 1) / kBlockK;
-    p.narrow = tile_time(rows, cols, kb, splits, true, sm_count) < tile_time(rows, cols, kb, splits, false, sm_count);
+    p.narrow = launch_time(first, p.splits, second, true, sm_count) < launch_time(first, p.splits, second, false, sm_count);
     const int64_t width = p.narrow ? kHalfN : kTileN;
-    const int64_t pairs = (rows + kTileM - 1) / kTileM * ((cols + width - 1) / width) * splits;
+    const int64_t pairs = (first.rows + kTileM - 1) / kTileM * ((first.cols + width - 1) / width) * p.splits +
+                          (second.rows + kTileM - 1) / kTileM * ((second.cols + width - 1) / width);
     const int64_t most = sm_count / 2 > 0 ? sm_count / 2 : 1;
     GK_CUDA_TRY(cudaFuncSetAttribute(k_vocab_product<P, F16>, cudaFuncAttributeMaxDynamicSharedMemorySize, kProductSmem));
-    k_vocab_product<P, F16><<<(unsigned)(2 * (pairs < most ? pairs : most)), kProductThreads, kProductSmem, st>>>(a, b, out, p);
+    k_vocab_product<P, F16><<<(unsigned)(2 * (pairs < most ? pairs : most)), kProductThreads, kProductSmem, st>>>(a, b, out, a2, b2, out2, p);
     GK_CUDA_TRY(cudaGetLastError());
     note_launch();
     return GK_OK;
@@ -796,7 +856,8 @@ static int launch(const VocabCall& c, int64_t v0, int64_t v1, bool first, bool i
     p.narrow = 0;
     p.if_missed = if_missed;
     p.first = first;
-    p.splits = c.splits > 0 ? c.splits : 1;
+    p.splits = P == kGrads && c.splits > 0 ? c.splits : 1;
+    p.direct = c.dhp == nullptr;
     // (the copies' hardware cuts a row's end in steps of 16 bytes, so the rows' length counts too)
     p.wide = (((uintptr_t)c.dw | (uintptr_t)(2 * c.lddw) | (uintptr_t)(2 * c.D)) & 15) == 0;
     return c.f16 ? launch_product<P, true>(p, sm_count, st) : launch_product<P, false>(p, sm_count, st);
@@ -811,23 +872,20 @@ int launch_vocab_powers(const VocabCall& c, int64_t v0, int64_t v1, bool if_miss
 int launch_vocab_again(const VocabCall& c, int64_t v0, int64_t v1, int sm_count, cudaStream_t st) {
     return launch<kAgain>(c, v0, v1, true, false, sm_count, st);
 }
-int launch_vocab_dw(const VocabCall& c, int64_t v0, int64_t v1, int sm_count, cudaStream_t st) {
-    return launch<kDw>(c, v0, v1, true, false, sm_count, st);
-}
-int launch_vocab_dh(const VocabCall& c, int64_t v0, int64_t v1, bool first, int sm_count, cudaStream_t st) {
-    return launch<kDh>(c, v0, v1, first, false, sm_count, st);
+int launch_vocab_grads(const VocabCall& c, int64_t v0, int64_t v1, bool first, int sm_count, cudaStream_t st) {
+    return launch<kGrads>(c, v0, v1, first, false, sm_count, st);
 }
 
 // Into how many parts the summed axis of dh is split.  dh has few tiles (rows / 256 x D / 512) and a
-// long sum, so without parts most pairs of SMs would idle; each part costs a write and a read of
-// fp32 sums, taken at 5 TB/s.
-int vocab_dh_splits(int64_t n, int64_t D, int64_t vb, int sm_count) {
-    const int64_t kb = (vb + kBlockK - 1) / kBlockK;
+// long sum, so without parts most pairs of SMs would idle; parts cost a write and a read of fp32 sums,
+// taken at 5 TB/s, and a launch that adds them.
+int vocab_dh_splits(int64_t n, int64_t D, int64_t vb, bool dw, int sm_count) {
+    const Share first = {n, D, (vb + kBlockK - 1) / kBlockK}, second = {dw ? vb : 0, D, (n + kBlockK - 1) / kBlockK};
     int best = 1;
     double least = 0;
-    for (int s = 1; s <= 32 && (s == 1 || s * 4 <= kb); ++s) {
-        const double wide = tile_time(n, D, kb, s, false, sm_count), narrow = tile_time(n, D, kb, s, true, sm_count);
-        const double us = (wide < narrow ? wide : narrow) + (double)s * (double)n * (double)D * 8.0 / 5e6;
+    for (int s = 1; s <= 32 && (s == 1 || s * 4 <= first.kb); ++s) {
+        const double wide = launch_time(first, s, second, false, sm_count), narrow = launch_time(first, s, second, true, sm_count);
+        const double us = (wide < narrow ? wide : narrow) + (s > 1 ? 4.0 + (double)s * (double)n * (double)D * 8.0 / 5e6 : 0.0);
         if (s == 1 || us < least) { least = us; best = s; }
     }
     return best;
