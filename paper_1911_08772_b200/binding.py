@@ -296,56 +296,70 @@ def gk_sparsify_host(g, eps, k: int, idx_out, val_out):
     return int(nnz.value), Stats.of(st)
 
 
+_TYPES = {"torch.float32": 0, "torch.bfloat16": 1, "torch.float16": 2}
+
+
 def _type(dtype) -> int:
-    import torch
-    code = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}.get(dtype)
+    code = _TYPES.get(str(dtype))
     if code is None:
         raise GkError(f"element type {dtype} is not one of float32, bfloat16, float16")
     return code
 
 
-def _rows(t, dtype, rows=None, cols=None, name="tensor"):
+def _rows(t, dtype, device, rows=None, cols=None, name="tensor"):
     """(pointer, row stride) of a 2-D CUDA tensor whose rows are contiguous, on the current device."""
-    import torch
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
-        raise GkError(f"{name}: expected a CUDA tensor")
-    if t.dim() != 2 or t.dtype != dtype:
-        raise GkError(f"{name}: expected a 2-D {dtype} tensor, got {t.dim()}-D {t.dtype}")
-    if t.device.index != torch.cuda.current_device():
+    if not t.is_cuda or t.dim() != 2 or t.dtype != dtype:
+        raise GkError(f"{name}: expected a 2-D {dtype} CUDA tensor, got {t.dim()}-D {t.dtype} on {t.device}")
+    if t.get_device() != device:
         raise GkError(f"{name} is not on the current device")
-    if (rows is not None and t.shape[0] != rows) or (cols is not None and t.shape[1] != cols):
+    n, m = t.shape
+    if (rows is not None and n != rows) or (cols is not None and m != cols):
         raise GkError(f"{name}: expected shape ({rows}, {cols}), got {tuple(t.shape)}")
-    if t.shape[1] > 1 and t.stride(1) != 1:
+    ld, step = t.stride()
+    if m > 1 and step != 1:
         raise GkError(f"{name}: the elements of a row must be contiguous")
     # the stride of a lone row says nothing
-    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else t.shape[1])
+    return t.data_ptr(), (ld if n > 1 else m)
 
 
-def _vec(t, dtype, shape, name):
+def _vec(t, dtype, device, shape, name):
     import torch
-    p = _dev(t, dtype)
-    if tuple(t.shape) != tuple(shape):
-        raise GkError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
-    if t.device.index != torch.cuda.current_device():
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != dtype or t.shape != shape or not t.is_contiguous():
+        raise GkError(f"{name}: expected a contiguous {dtype} CUDA tensor of shape {tuple(shape)}")
+    if t.get_device() != device:
         raise GkError(f"{name} is not on the current device")
-    return p
+    return t.data_ptr()
 
 
-def _head(h, w, loss_out, lse_out, row_grad, dh, dw):
+def _matrices(*tensors) -> int:
+    """The current device, for tensors that are all 2-D."""
+    import torch
+    for t in tensors:
+        if not isinstance(t, torch.Tensor) or t.dim() != 2:
+            raise GkError("expected 2-D CUDA tensors")
+    return torch.cuda.current_device()
+
+
+def _head(h, w, loss_out, lse_out, row_grad, dh, dw, device):
     """The arguments that the two losses share: (before the targets, after them)."""
     import torch
-    if not isinstance(h, torch.Tensor) or h.dim() != 2 or not isinstance(w, torch.Tensor) or w.dim() != 2:
-        raise GkError("h and w must be 2-D CUDA tensors")
     n, D = h.shape
     V = w.shape[0]
-    hp, ldh = _rows(h, h.dtype, name="h")
-    wp, ldw = _rows(w, h.dtype, cols=D, name="w")
-    dhp, lddh = (None, D) if dh is None else _rows(dh, h.dtype, n, D, "dh")
-    dwp, lddw = (None, D) if dw is None else _rows(dw, h.dtype, V, D, "dw")
-    return ([hp, ldh, wp, ldw, _type(h.dtype), n, D, V],
-            [None if row_grad is None else _vec(row_grad, torch.float32, (n,), "row_grad"),
-             _vec(loss_out, torch.float32, (n,), "loss_out"), _vec(lse_out, torch.float32, (n,), "lse_out"),
-             dhp, lddh, dwp, lddw, _stream()])
+    dtype, f32 = h.dtype, torch.float32
+    hp, ldh = _rows(h, dtype, device, name="h")
+    wp, ldw = _rows(w, dtype, device, cols=D, name="w")
+    dhp, lddh = (None, D) if dh is None else _rows(dh, dtype, device, n, D, "dh")
+    dwp, lddw = (None, D) if dw is None else _rows(dw, dtype, device, V, D, "dw")
+    row = (n,)
+    return ((hp, ldh, wp, ldw, _type(dtype), n, D, V),
+            (None if row_grad is None else _vec(row_grad, f32, device, row, "row_grad"),
+             _vec(loss_out, f32, device, row, "loss_out"), _vec(lse_out, f32, device, row, "lse_out"),
+             dhp, lddh, dwp, lddw, _stream_of(device)))
+
+
+def _stream_of(device: int) -> int:
+    import torch
+    return torch._C._cuda_getCurrentRawStream(device)
 
 
 def gk_vocab_loss(h, w, target, loss_out, lse_out, row_grad=None, dh=None, dw=None, ignore_index: int = -100) -> None:
@@ -354,8 +368,9 @@ def gk_vocab_loss(h, w, target, loss_out, lse_out, row_grad=None, dh=None, dw=No
     allowed; target (n,) int64; loss_out, lse_out (n,) float32; row_grad (n,) float32 or None for
     the gradient of the mean over the rows that count."""
     import torch
-    before, after = _head(h, w, loss_out, lse_out, row_grad, dh, dw)
-    _check(load().gk_vocab_loss(*before, _vec(target, torch.int64, (h.shape[0],), "target"), ignore_index, *after))
+    device = _matrices(h, w)
+    before, after = _head(h, w, loss_out, lse_out, row_grad, dh, dw, device)
+    _check(load().gk_vocab_loss(*before, _vec(target, torch.int64, device, (h.shape[0],), "target"), ignore_index, *after))
 
 
 def gk_vocab_distill(h, w, t_idx, t_val, loss_out, lse_out, t_lse=None, temperature: float = 1.0, row_grad=None,
@@ -364,13 +379,12 @@ def gk_vocab_distill(h, w, t_idx, t_val, loss_out, lse_out, t_lse=None, temperat
     z = h w^T (see gk.h); t_lse (n,): the teacher's log-sum-exp at this temperature, None to
     normalise over the K pairs.  The other arguments as for gk_vocab_loss."""
     import torch
-    before, after = _head(h, w, loss_out, lse_out, row_grad, dh, dw)
-    n = h.shape[0]
-    if not isinstance(t_idx, torch.Tensor) or t_idx.dim() != 2:
-        raise GkError("t_idx must be a 2-D CUDA tensor")
-    K = t_idx.shape[1]
-    _check(load().gk_vocab_distill(*before, _vec(t_idx, torch.int32, (n, K), "t_idx"), _vec(t_val, torch.float32, (n, K), "t_val"),
-                                   K, None if t_lse is None else _vec(t_lse, torch.float32, (n,), "t_lse"),
+    device = _matrices(h, w, t_idx)
+    before, after = _head(h, w, loss_out, lse_out, row_grad, dh, dw, device)
+    n, K = h.shape[0], t_idx.shape[1]
+    _check(load().gk_vocab_distill(*before, _vec(t_idx, torch.int32, device, (n, K), "t_idx"),
+                                   _vec(t_val, torch.float32, device, (n, K), "t_val"), K,
+                                   None if t_lse is None else _vec(t_lse, torch.float32, device, (n,), "t_lse"),
                                    temperature, *after))
 
 
@@ -379,13 +393,14 @@ def gk_vocab_topk(logits, k: int, idx_out, val_out, lse_out=None, temperature: f
     temperature (see gk.h).  logits (n, V): float32, bfloat16 or float16, row stride allowed;
     idx_out (n, k) int32, val_out (n, k) float32, lse_out (n,) float32 or None."""
     import torch
-    if not isinstance(logits, torch.Tensor) or logits.dim() != 2:
-        raise GkError("logits must be a 2-D CUDA tensor")
+    device = _matrices(logits)
     n, V = logits.shape
-    p, ld = _rows(logits, logits.dtype, name="logits")
-    _check(load().gk_vocab_topk(p, ld, _type(logits.dtype), n, V, k, temperature, _vec(idx_out, torch.int32, (n, k), "idx_out"),
-                                _vec(val_out, torch.float32, (n, k), "val_out"),
-                                None if lse_out is None else _vec(lse_out, torch.float32, (n,), "lse_out"), _stream()))
+    p, ld = _rows(logits, logits.dtype, device, name="logits")
+    _check(load().gk_vocab_topk(p, ld, _type(logits.dtype), n, V, k, temperature,
+                                _vec(idx_out, torch.int32, device, (n, k), "idx_out"),
+                                _vec(val_out, torch.float32, device, (n, k), "val_out"),
+                                None if lse_out is None else _vec(lse_out, torch.float32, device, (n,), "lse_out"),
+                                _stream_of(device)))
 
 
 def gk_vocab_set_budget(nbytes: int) -> None:

@@ -33,6 +33,8 @@
 // its own, and stores of 16 bytes to 32 rows at once would take the time of 32.
 #include <cuda.h>
 
+#include <atomic>
+
 #include "gk_vocab.cuh"
 
 namespace gk {
@@ -497,6 +499,49 @@ __device__ __forceinline__ Tiles make_tiles(int64_t rows, int64_t cols, int64_t 
     return t;
 }
 
+// A cluster's share of the tiles, in the order in which it takes them.  The first kind (dh's) is dealt
+// out in turn, so that some clusters have one more than the others; the others then get as much of the
+// second kind (dw's) as makes up for it, and the rest is dealt in turn again, beginning with them.
+struct Deal {
+    int64_t n1, n2, clusters, heavy;      // heavy: clusters with one more of the first kind
+    int64_t extra;                        // tiles of the second kind that make up for it
+    int64_t index, at;                    // the cluster, its next tile of the present kind
+    bool light;
+    int kind;                             // 0: first, 1: extra, 2: rest
+    __device__ __forceinline__ Deal(const Tiles& a, const Tiles& b, int64_t cluster, int64_t clusters_) {
+        n1 = a.total;
+        n2 = b.total;
+        clusters = clusters_;
+        heavy = n1 % clusters;
+        light = cluster >= heavy;
+        // a tile costs its blocks and about two more
+        const int64_t each = heavy ? (a.kb / a.splits + 2) / (b.kb + 2) : 0;
+        extra = each * (clusters - heavy);
+        if (extra > n2) extra = n2;
+        at = cluster;
+        kind = 0;
+        index = cluster;
+    }
+    // The next tile: `dw`: of the second kind; false: none left.
+    __device__ __forceinline__ bool next(int64_t& t, bool& dw) {
+        if (kind == 0) {
+            if (at < n1) { t = at; dw = false; at += clusters; return true; }
+            kind = 1;
+            at = light ? index - heavy : n2;
+        }
+        if (kind == 1) {
+            if (at < extra) { t = at; dw = true; at += clusters - heavy; return true; }
+            kind = 2;
+            at = extra + (light ? index - heavy : index + clusters - heavy);
+        }
+        if (at >= n2) return false;
+        t = at;
+        dw = true;
+        at += clusters;
+        return true;
+    }
+};
+
 // map_a2, map_b2, map_out2: dw's operands and result in kGrads.
 template <int P, bool F16>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1)
@@ -521,7 +566,6 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     const int64_t nv = p.v1 - p.v0, n_cols = P == kGrads ? c.D : nv;      // columns of the result
     const Tiles tiles = P == kGrads ? make_tiles(c.dh ? n_valid : 0, c.D, nv, width, p.splits) : make_tiles(n_valid, nv, c.D, width, 1);
     const Tiles tiles2 = make_tiles(P == kGrads && c.dw ? nv : 0, c.D, n_valid, width, 1);
-    const int64_t total = tiles.total + tiles2.total;
     const int64_t cluster = blockIdx.x >> 1, clusters = gridDim.x >> 1;
 
     if (tid == 0) {
@@ -551,11 +595,13 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         // producer: this CTA's 128 rows of A and of each half of B; the leader's barrier counts both CTAs' bytes
         int stage = 0;
         uint32_t phase = 0;
-        for (int64_t t = cluster; t < total && ok; t += clusters) {
+        int64_t t;
+        bool dw;
+        for (Deal deal(tiles, tiles2, cluster, clusters); ok && deal.next(t, dw);) {
             int64_t m, n;
             int split, k0, k1;
-            const bool dw = P == kGrads && t >= tiles.total;
-            (dw ? tiles2 : tiles).at(dw ? t - tiles.total : t, m, n, split);
+            if (P != kGrads) dw = false;
+            (dw ? tiles2 : tiles).at(t, m, n, split);
             (dw ? tiles2 : tiles).blocks(split, k0, k1);
             const bool two = !p.narrow && n * kTileN + kHalfN < n_cols;
             const int ma = (int)(m * kTileM + rank * 128), nb = (int)(n * width + rank * 128);
@@ -615,11 +661,13 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
             int stage_a = 0, stage_b = 0;     // next block of the first half (of the only one), of the second half
             uint32_t phase = 0, free0 = 0, free1 = 0;
             int only = 0;                     // the half a narrow tile has
-            for (int64_t t = cluster; t < total && ok; t += clusters) {
+            int64_t t;
+            bool dw;
+            for (Deal deal(tiles, tiles2, cluster, clusters); ok && deal.next(t, dw);) {
                 int64_t m, n;
                 int split, k0, k1;
-                const bool dw = P == kGrads && t >= tiles.total;
-                (dw ? tiles2 : tiles).at(dw ? t - tiles.total : t, m, n, split);
+                if (P != kGrads) dw = false;
+                (dw ? tiles2 : tiles).at(t, m, n, split);
                 (dw ? tiles2 : tiles).blocks(split, k0, k1);
                 const int blocks = k1 - k0;
                 const bool two = !p.narrow && n * kTileN + kHalfN < n_cols;
@@ -694,11 +742,13 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         Patch w;
         w.lane = lane;
         w.staging = staging0 + (warp - 4) * kStagingBytes;
-        for (int64_t t = cluster; t < total && ok; t += clusters) {
+        int64_t t;
+        bool dw;
+        for (Deal deal(tiles, tiles2, cluster, clusters); ok && deal.next(t, dw);) {
             int64_t m, n;
             int split, k0, k1;
-            const bool dw = P == kGrads && t >= tiles.total;
-            (dw ? tiles2 : tiles).at(dw ? t - tiles.total : t, m, n, split);
+            if (P != kGrads) dw = false;
+            (dw ? tiles2 : tiles).at(t, m, n, split);
             (dw ? tiles2 : tiles).blocks(split, k0, k1);
             const bool two = !p.narrow && n * kTileN + kHalfN < n_cols;
             w.row0 = m * kTileM + rank * 128 + quarter * 32;
@@ -789,7 +839,7 @@ static int make_map(CUtensorMap* map, Element type, const void* base, int64_t co
 // An estimate of a launch's time in us, for choosing between tiles and parts: what the busiest pair of
 // SMs sums, at 0.55 us a block of 64 of a wide tile and 0.29 us of a narrow one (5 % more per column: 4096 x
 // 4096 x 32000, logits, 713 against 749 us), 1 us a tile and 4 us to fill and empty.  The first kind
-// of tile (dh's, in `splits` parts) is dealt out before the second.
+// of tile (dh's, in `splits` parts) is dealt out before the second, which evens the shares out.
 struct Share { int64_t rows, cols, kb; };
 static double launch_time(const Share& first, int splits, const Share& second, bool narrow, int sm_count) {
     const int64_t width = narrow ? kHalfN : kTileN, most = sm_count / 2 > 0 ? sm_count / 2 : 1;
@@ -797,13 +847,9 @@ static double launch_time(const Share& first, int splits, const Share& second, b
     const int64_t n2 = (second.rows + kTileM - 1) / kTileM * ((second.cols + width - 1) / width);
     const double block = narrow ? 0.29 : 0.55;
     const double t1 = (double)((first.kb + splits - 1) / splits) * block + 1.0, t2 = (double)second.kb * block + 1.0;
-    double longest = 0;
-    for (int64_t i = 0; i < most; ++i) {
-        const int64_t a = n1 > i ? (n1 - i + most - 1) / most : 0, all = n1 + n2 > i ? (n1 + n2 - i + most - 1) / most : 0;
-        const double us = (double)a * t1 + (double)(all - a) * t2;
-        if (us > longest) longest = us;
-    }
-    return longest + 4.0;
+    const double rounds1 = (double)((n1 + most - 1) / most), all = ((double)n1 * t1 + (double)n2 * t2) / (double)most;
+    const double longest = rounds1 * t1, even = n2 ? all + 0.5 * t2 : 0.0;
+    return (longest > even ? longest : even) + 4.0;
 }
 
 template <int P, bool F16>
@@ -840,7 +886,13 @@ static int launch_product(ProductArgs p, int sm_count, cudaStream_t st) {
     const int64_t pairs = (first.rows + kTileM - 1) / kTileM * ((first.cols + width - 1) / width) * p.splits +
                           (second.rows + kTileM - 1) / kTileM * ((second.cols + width - 1) / width);
     const int64_t most = sm_count / 2 > 0 ? sm_count / 2 : 1;
-    GK_CUDA_TRY(cudaFuncSetAttribute(k_vocab_product<P, F16>, cudaFuncAttributeMaxDynamicSharedMemorySize, kProductSmem));
+    static std::atomic<unsigned long long> ready{0};      // devices on which the kernel may have its shared memory
+    int dev = 0;
+    GK_CUDA_TRY(cudaGetDevice(&dev));
+    if (dev > 63 || !(ready.load() >> dev & 1)) {
+        GK_CUDA_TRY(cudaFuncSetAttribute(k_vocab_product<P, F16>, cudaFuncAttributeMaxDynamicSharedMemorySize, kProductSmem));
+        if (dev < 64) ready.fetch_or(1ull << dev);
+    }
     k_vocab_product<P, F16><<<(unsigned)(2 * (pairs < most ? pairs : most)), kProductThreads, kProductSmem, st>>>(a, b, out, a2, b2, out2, p);
     GK_CUDA_TRY(cudaGetLastError());
     note_launch();
