@@ -59,6 +59,7 @@ __device__ __forceinline__ float warp_max_f(float v) {
 // 1. Teacher probabilities, one warp a row.
 // ---------------------------------------------------------------------------
 __global__ void __launch_bounds__(256) k_vocab_teacher(VocabCall c) {
+    after_previous();
     const int64_t r = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
     const int lane = threadIdx.x & 31;
     if (r >= c.n) return;
@@ -107,72 +108,107 @@ __global__ void __launch_bounds__(256) k_vocab_teacher(VocabCall c) {
 }
 
 // ---------------------------------------------------------------------------
-// The rows that count, numbered in their order by one CTA; the power of two that brings the
-// gradients' largest row coefficient to [1, 2) (bf16) or [1024, 2048) (fp16, whose smallest
-// step is 2^-24: an entry 2^-34 of the largest is still held).
+// The rows that count, numbered in their order, and the power of two that brings the gradients' largest
+// row coefficient to [1, 2) (bf16) or [1024, 2048) (fp16, whose smallest step is 2^-24: an entry 2^-34 of the
+// largest is still held).
 // ---------------------------------------------------------------------------
+
+// Whether row r counts, and the magnitude of its gradient's coefficient (times T).
+__device__ __forceinline__ bool row_counts(const VocabCall& c, int64_t r, float& g) {
+    g = 0.f;
+    if (r >= c.n) return false;
+    bool on;
+    float Q = 1.f;
+    const float rg = c.row_grad ? c.row_grad[r] : 1.f;
+    if (c.target) {
+        const int64_t t = c.target[r];
+        on = t != c.ignore_index && t >= 0 && t < c.V;
+    } else {
+        const float4 te = c.teacher[r];
+        on = teacher_counts(te);
+        Q = te.x;
+    }
+    if (on) {
+        g = fabsf(Q * rg);
+        if (!(g < INFINITY)) g = INFINITY;      // a NaN too
+    }
+    return on;
+}
+__device__ __forceinline__ void write_ctl(const VocabCall& c, int n_valid, float top) {
+    if (!c.row_grad && n_valid > 0) top /= (float)n_valid;
+    top *= c.inv_T;
+    int e = 0;
+    if (top > 0.f && top < INFINITY) frexpf(top, &e);   // top in [2^(e-1), 2^e)
+    e = min(max((c.f16 ? 11 : 1) - e, -100), 100);
+    c.ctl->n_valid = n_valid;
+    c.ctl->status = 0;
+    c.ctl->missed = 0;
+    c.ctl->scale = ldexpf(1.f, e);
+    c.ctl->inv_scale = ldexpf(1.f, -e);
+}
+
+// By one CTA, 8192 rows at a time: all loads first, then one scan over the 256 counts of (32 rows).
 __global__ void __launch_bounds__(1024) k_vocab_rows(VocabCall c) {
-    __shared__ int warp_n[32];
+    constexpr int kEach = 8;
+    __shared__ int count[kEach * 32], part[8];
     __shared__ float warp_g[32];
+    after_previous();
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
     int base = 0;
     float top = 0.f;
-    bool bad = false;
-    for (int64_t r0 = 0; r0 < c.n; r0 += 1024) {
-        const int64_t r = r0 + tid;
-        bool on = false;
-        float Q = 1.f;
-        if (r < c.n) {
-            if (c.target) {
-                const int64_t t = c.target[r];
-                on = t != c.ignore_index && t >= 0 && t < c.V;
-            } else {
-                const float4 te = c.teacher[r];
-                on = teacher_counts(te);
-                Q = te.x;
+    for (int64_t r0 = 0; r0 < c.n; r0 += kEach * 1024) {
+        unsigned ballot[kEach];
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            float g;
+            ballot[j] = row_counts(c, r0 + j * 1024 + tid, g);
+            top = fmaxf(top, g);
+        }
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) ballot[j] = __ballot_sync(0xffffffffu, ballot[j]);
+        __syncthreads();
+        if (lane == 0)
+#pragma unroll
+            for (int j = 0; j < kEach; ++j) count[j * 32 + wid] = __popc(ballot[j]);
+        __syncthreads();
+        int own = 0, incl = 0;
+        if (tid < kEach * 32) {
+            own = incl = count[tid];
+#pragma unroll
+            for (int o = 1; o < 32; o *= 2) {
+                const int v = __shfl_up_sync(0xffffffffu, incl, o);
+                if (lane >= o) incl += v;
+            }
+            if (lane == 31) part[wid] = incl;
+        }
+        __syncthreads();
+        if (tid < kEach * 32) {
+            int before = incl - own;
+            for (int i = 0; i < wid; ++i) before += part[i];
+            count[tid] = before;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            const int64_t r = r0 + j * 1024 + tid;
+            if (ballot[j] >> lane & 1) {
+                const int at = base + count[j * 32 + wid] + __popc(ballot[j] & ((1u << lane) - 1u));
+                c.row_of[at] = (int32_t)r;
+                c.at_of[r] = at;
+            } else if (r < c.n) {
+                c.at_of[r] = -1;
+                c.loss[r] = 0.f;
+                c.lse[r] = 0.f;
             }
         }
-        const unsigned ballot = __ballot_sync(0xffffffffu, on);
-        __syncthreads();
-        if (lane == 0) warp_n[wid] = __popc(ballot);
-        __syncthreads();
-        int before = 0, total = 0;
-#pragma unroll
-        for (int i = 0; i < 32; ++i) {
-            const int v = warp_n[i];
-            before += i < wid ? v : 0;
-            total += v;
-        }
-        if (on) {
-            const int at = base + before + __popc(ballot & ((1u << lane) - 1u));
-            c.row_of[at] = (int32_t)r;
-            c.at_of[r] = at;
-            const float g = fabsf(Q * (c.row_grad ? c.row_grad[r] : 1.f));
-            top = fmaxf(top, g);
-            bad |= !(g < INFINITY);
-        } else if (r < c.n) {
-            c.at_of[r] = -1;
-            c.loss[r] = 0.f;
-            c.lse[r] = 0.f;
-        }
-        base += total;
+        for (int i = 0; i < kEach; ++i) base += part[i];
     }
     top = warp_max_f(top);
-    bad = __any_sync(0xffffffffu, bad);
-    if (lane == 0) warp_g[wid] = bad ? INFINITY : top;
+    if (lane == 0) warp_g[wid] = top;
     __syncthreads();
     if (tid == 0) {
         for (int i = 0; i < 32; ++i) top = fmaxf(top, warp_g[i]);
-        if (!c.row_grad && base > 0) top /= (float)base;
-        top *= c.inv_T;
-        int e = 0;
-        if (top > 0.f && top < INFINITY) frexpf(top, &e);   // top in [2^(e-1), 2^e)
-        e = min(max((c.f16 ? 11 : 1) - e, -100), 100);
-        c.ctl->n_valid = base;
-        c.ctl->status = 0;
-        c.ctl->missed = 0;
-        c.ctl->scale = ldexpf(1.f, e);
-        c.ctl->inv_scale = ldexpf(1.f, -e);
+        write_ctl(c, base, top);
     }
 }
 
@@ -203,21 +239,74 @@ __device__ __forceinline__ uint4 load8(const uint16_t* p, int64_t left) {
     return make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
 }
 
-template <bool F16>
+// RANK (few rows): each CTA takes a row of the caller's and finds its number itself, by looking at all rows
+// (2048 rows are 16 loads a thread, where a launch of its own costs 3 to 6 us); one of them writes the
+// control block.
+constexpr int64_t kRankRows = 2048;
+
+template <bool F16, bool RANK>
 __global__ void __launch_bounds__(128) k_vocab_gather(VocabCall c) {
-    const int at = blockIdx.x, n_valid = c.ctl->n_valid;
+    __shared__ int counts[2][4];
+    __shared__ float tops[4];
+    after_previous();
     const int tid = threadIdx.x, lane = tid & 31;
-    if (c.dh && at < c.n && c.at_of[at] < 0) {
-        uint16_t* out = (uint16_t*)c.dh + at * c.lddh;
+    int at = blockIdx.x, n_valid;
+    int64_t r;
+    bool left_out;
+    if constexpr (RANK) {
+        r = blockIdx.x;
+        int before = 0, all = 0;
+        float top = 0.f;
+        bool mine = false;
+#pragma unroll 4
+        for (int64_t i = tid; i < c.n; i += 128) {
+            float g;
+            const bool on = row_counts(c, i, g);
+            all += on;
+            before += on && i < r;
+            mine |= on && i == r;
+            top = fmaxf(top, g);
+        }
+        all = __reduce_add_sync(0xffffffffu, all);
+        before = __reduce_add_sync(0xffffffffu, before);
+        top = warp_max_f(top);
+        if (lane == 0) { counts[0][tid >> 5] = all; counts[1][tid >> 5] = before; tops[tid >> 5] = top; }
+        left_out = !__syncthreads_or(mine) && r < c.n;
+        n_valid = counts[0][0] + counts[0][1] + counts[0][2] + counts[0][3];
+        at = counts[1][0] + counts[1][1] + counts[1][2] + counts[1][3];
+        if (tid == 0) {
+            if (r == 0) write_ctl(c, n_valid, fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])));
+            if (left_out) {
+                c.at_of[r] = -1;
+                c.loss[r] = 0.f;
+                c.lse[r] = 0.f;
+            } else if (r < c.n) {
+                c.row_of[at] = (int32_t)r;
+                c.at_of[r] = at;
+            }
+        }
+        // rows up to the padding are zero
+        if (r >= n_valid && r < round_up(n_valid, kVocabRowPad))
+            for (int64_t i = tid; i < c.Dp / 8; i += 128) ((uint4*)(c.hc + r * c.Dp))[i] = make_uint4(0, 0, 0, 0);
+    } else {
+        n_valid = c.ctl->n_valid;
+        left_out = at < c.n && c.at_of[at] < 0;
+    }
+    if (c.dh && left_out) {
+        uint16_t* out = (uint16_t*)c.dh + (int64_t)blockIdx.x * c.lddh;
         for (int64_t i = tid; i < c.D; i += 128) out[i] = 0;
     }
-    if (at >= round_up(n_valid, kVocabRowPad)) return;
     uint16_t* to = c.hc + (int64_t)at * c.Dp;
-    if (at >= n_valid) {
-        for (int64_t i = tid; i < c.Dp / 8; i += 128) ((uint4*)to)[i] = make_uint4(0, 0, 0, 0);
-        return;
+    if constexpr (RANK) {
+        if (left_out || r >= c.n) return;
+    } else {
+        if (at >= round_up(n_valid, kVocabRowPad)) return;
+        if (at >= n_valid) {
+            for (int64_t i = tid; i < c.Dp / 8; i += 128) ((uint4*)to)[i] = make_uint4(0, 0, 0, 0);
+            return;
+        }
+        r = c.row_of[at];
     }
-    const int64_t r = c.row_of[at];
     const uint16_t* from = (const uint16_t*)c.h + r * c.ldh;
     for (int64_t i = tid; i < c.Dp / 8; i += 128) ((uint4*)to)[i] = load8(from + i * 8, c.D - i * 8);
     int first = 0, last = 1;
@@ -256,6 +345,7 @@ __global__ void __launch_bounds__(128) k_vocab_gather(VocabCall c) {
 
 // A copy of w with rows that start and end on 16-byte boundaries, where w's own do not.
 __global__ void __launch_bounds__(256) k_vocab_copy_w(VocabCall c) {
+    after_previous();
     const int64_t words = c.Dp / 8, total = c.V * words;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
         const int64_t v = i / words, k = (i - v * words) * 8;
@@ -269,22 +359,69 @@ __global__ void __launch_bounds__(256) k_vocab_copy_w(VocabCall c) {
 // SECOND: after the references did not hold and the logits have been taken again; the log-sum-exp
 // becomes the reference.
 // ---------------------------------------------------------------------------
+
+// A row from its log-sum-exp, by one warp: its loss (write) and what the gradients need of it.
+template <bool SECOND>
+__device__ __forceinline__ VocabRow finish_row(const VocabCall& c, int64_t at, int n_valid, float lse2, int lane, bool write) {
+    const int64_t r = c.row_of[at];
+    float Q = 1.f, loss = 0.f;
+    if (c.target) {
+        if (write) loss = (lse2 - c.zt[at] * c.zscale) * kLn2;
+    } else {
+        const float4 te = c.teacher[r];
+        Q = te.x;
+        if (write) {
+            float sum = 0.f;
+            for (int j = lane; j < c.K; j += 32) {
+                const float q = c.q[r * c.K + j];
+                if (q > 0.f) sum += q * (((c.t_val[r * c.K + j] - te.z) * c.inv_T - te.y) + (lse2 - c.zt[at * c.K + j] * c.zscale) * kLn2);
+                else if (q != q) sum = q;
+            }
+            loss = warp_sum_f(sum);
+        }
+    }
+    if (write && lane == 0) {
+        c.loss[r] = loss;
+        c.lse[r] = lse2 * kLn2;
+    }
+    VocabRow out;
+    out.unit = c.ctl->scale * ((c.row_grad ? c.row_grad[r] : 1.f / (float)n_valid) * c.inv_T);
+    out.lse2 = lse2;
+    out.coef = out.unit * Q;
+    out.ref = SECOND ? lse2 : c.powers ? c.row[at].ref : 0.f;
+    // powers up to 2^100, and their products with w and h, are far from the types' ends
+    if (!SECOND && c.powers && lane == 0 && lse2 - out.ref >= 100.f) c.ctl->missed = 1;
+    return out;
+}
+
 template <bool SECOND>
 __global__ void __launch_bounds__(1024) k_vocab_rows_done(VocabCall c) {
     __shared__ float sm[32][33], ss[32][33];
+    after_previous();
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
     const int64_t at0 = (int64_t)blockIdx.x * 32;
     const int n_valid = c.ctl->n_valid;
     if (at0 >= n_valid || (SECOND && c.ctl->missed == 0)) return;
     const int64_t tiles = (c.V + kVocabTile - 1) / kVocabTile;
+    // With 32 rows a lane is a row; with fewer, lanes of a row share its tiles (one row: 1024 loads at once).
+    const int rows = (int)(n_valid - at0 < 32 ? n_valid - at0 : 32);
+    const int pitch = rows > 16 ? 32 : rows > 8 ? 16 : rows > 4 ? 8 : rows > 2 ? 4 : rows;
+    const int mine = lane % pitch, share = lane / pitch, shares = 32 / pitch;
     float m = -INFINITY, s = 0.f;
-    if (at0 + lane < n_valid) {
-        const float2* p = c.part + at0 + lane;
+    if (mine < rows) {
+        const float2* p = c.part + at0 + mine;
 #pragma unroll 4
-        for (int64_t t = wid; t < tiles; t += 32) {
+        for (int64_t t = wid * shares + share; t < tiles; t += 32 * shares) {
             const float2 x = __ldcs(p + t * c.n_pad);
             join_max_sum(m, s, x.x, x.y);
         }
+    }
+    for (int o = pitch; o < 32; o *= 2) {
+        const float m2 = __shfl_xor_sync(0xffffffffu, m, o), s2 = __shfl_xor_sync(0xffffffffu, s, o);
+        float ml = lane & o ? m2 : m, sl = lane & o ? s2 : s;
+        join_max_sum(ml, sl, lane & o ? m : m2, lane & o ? s : s2);
+        m = ml;
+        s = sl;
     }
     sm[wid][lane] = m;
     ss[wid][lane] = s;
@@ -302,35 +439,8 @@ __global__ void __launch_bounds__(1024) k_vocab_rows_done(VocabCall c) {
         m = ml;
         s = sl;
     }
-    const float lse2 = m + log2f(s);
-    const int64_t r = c.row_of[at];
-    float Q = 1.f, loss;
-    if (c.target) {
-        loss = (lse2 - c.zt[at] * c.zscale) * kLn2;
-    } else {
-        const float4 te = c.teacher[r];
-        Q = te.x;
-        float sum = 0.f;
-        for (int j = lane; j < c.K; j += 32) {
-            const float q = c.q[r * c.K + j];
-            if (q > 0.f) sum += q * (((c.t_val[r * c.K + j] - te.z) * c.inv_T - te.y) + (lse2 - c.zt[at * c.K + j] * c.zscale) * kLn2);
-            else if (q != q) sum = q;
-        }
-        loss = warp_sum_f(sum);
-    }
-    if (lane == 0) {
-        c.loss[r] = loss;
-        c.lse[r] = lse2 * kLn2;
-        const float unit = c.ctl->scale * ((c.row_grad ? c.row_grad[r] : 1.f / (float)n_valid) * c.inv_T);
-        VocabRow out;
-        out.lse2 = lse2;
-        out.coef = unit * Q;
-        out.unit = unit;
-        out.ref = SECOND ? lse2 : c.row[at].ref;
-        // powers up to 2^100, and their products with w and h, are far from the types' ends
-        if (!SECOND && c.powers && lse2 - out.ref >= 100.f) c.ctl->missed = 1;
-        c.row[at] = out;
-    }
+    const VocabRow out = finish_row<SECOND>(c, at, n_valid, m + log2f(s), lane, true);
+    if (lane == 0) c.row[at] = out;
 }
 
 // ---------------------------------------------------------------------------
@@ -338,10 +448,9 @@ __global__ void __launch_bounds__(1024) k_vocab_rows_done(VocabCall c) {
 // and written over, so that 1 - p loses nothing where p is near 1.
 // ---------------------------------------------------------------------------
 template <bool F16>
-__device__ __forceinline__ void write_targets(const VocabCall& c, int64_t at, int64_t lo, int64_t hi, int64_t v0,
+__device__ __forceinline__ void write_targets(const VocabCall& c, int64_t at, const VocabRow& vr, int64_t lo, int64_t hi, int64_t v0,
                                               int tid, int threads) {
     const int64_t r = c.row_of[at];
-    const VocabRow vr = c.row[at];
     const float4 te = c.target ? make_float4(1.f, 0.f, 0.f, 1.f) : c.teacher[r];
     if (c.powers && !(te.x > 0.f)) return;      // the row's powers are worth nothing
     for (int j = tid; j < c.K; j += threads) {
@@ -360,11 +469,16 @@ __device__ __forceinline__ void write_targets(const VocabCall& c, int64_t at, in
 }
 
 constexpr int kGradCols = 4096;   // columns a CTA scales
+constexpr int64_t kOwnTiles = 128;   // tiles a CTA joins itself
 
 // From the distances kept of the piece [v0, v1): e <- coef 2^(m_tile - lse - x / steps), in place, and zero
-// for the rows up to the padding, which the product for dw sums over.
-template <bool F16>
+// for the rows up to the padding, which the product for dw sums over.  DONE (vocabularies of up to
+// 128 tiles): each CTA joins the row's tiles itself, and the first of a row writes its loss, instead
+// of a launch of its own before this one.
+template <bool F16, bool DONE>
 __global__ void __launch_bounds__(256) k_vocab_scale(VocabCall c, int64_t v0, int64_t v1) {
+    __shared__ float sm[4], ss[4];
+    after_previous();
     const int64_t at = blockIdx.x;
     const int n_valid = c.ctl->n_valid;
     if (at >= round_up(n_valid, 64)) return;
@@ -374,7 +488,37 @@ __global__ void __launch_bounds__(256) k_vocab_scale(VocabCall c, int64_t v0, in
         for (int64_t v = lo + threadIdx.x * 8; v < hi; v += 256 * 8) *(uint4*)(c.e + at * c.vb + (v - v0)) = make_uint4(0, 0, 0, 0);
         return;
     }
-    const VocabRow vr = c.row[at];
+    VocabRow vr;
+    if constexpr (DONE) {
+        const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+        const int64_t tiles = (c.V + kVocabTile - 1) / kVocabTile;
+        float m = -INFINITY, s = 0.f;
+        if (wid < 4) {
+            if (tid < tiles) {
+                const float2 x = __ldg(c.part + tid * c.n_pad + at);
+                m = x.x;
+                s = x.y;
+            }
+#pragma unroll
+            for (int o = 1; o < 32; o *= 2) {
+                const float m2 = __shfl_xor_sync(0xffffffffu, m, o), s2 = __shfl_xor_sync(0xffffffffu, s, o);
+                float ml = lane & o ? m2 : m, sl = lane & o ? s2 : s;
+                join_max_sum(ml, sl, lane & o ? m : m2, lane & o ? s : s2);
+                m = ml;
+                s = sl;
+            }
+            if (lane == 0) { sm[wid] = m; ss[wid] = s; }
+        }
+        __syncthreads();
+        m = sm[0];
+        s = ss[0];
+#pragma unroll
+        for (int k = 1; k < 4; ++k) join_max_sum(m, s, sm[k], ss[k]);
+        vr = finish_row<false>(c, at, n_valid, m + log2f(s), lane, blockIdx.y == 0 && wid == 0);
+        if (blockIdx.y == 0 && tid == 0) c.row[at] = vr;
+    } else {
+        vr = c.row[at];
+    }
     for (int64_t v = lo + threadIdx.x * 8; v < hi; v += 256 * 8) {
         const float base = __ldg(&c.part[v / kVocabTile * c.n_pad + at].x) - vr.lse2;
         uint4* p = (uint4*)(c.e + at * c.vb + (v - v0));
@@ -391,18 +535,19 @@ __global__ void __launch_bounds__(256) k_vocab_scale(VocabCall c, int64_t v0, in
         *p = make_uint4(xs[0], xs[1], xs[2], xs[3]);
     }
     __syncthreads();
-    write_targets<F16>(c, at, lo, hi, v0, threadIdx.x, 256);
+    write_targets<F16>(c, at, vr, lo, hi, v0, threadIdx.x, 256);
 }
 
 // Powers: hs <- hc times what each row's powers are worth, with zero rows to a multiple of 64, and the
 // targets' entries of the first piece.
 template <bool F16>
 __global__ void __launch_bounds__(128) k_vocab_worth(VocabCall c, int64_t v1) {
+    after_previous();
     const int64_t at = blockIdx.x;
     const int n_valid = c.ctl->n_valid;
     if (at >= round_up(n_valid, 64)) return;
     const bool on = at < n_valid;
-    if (on) write_targets<F16>(c, at, 0, v1, 0, threadIdx.x, 128);
+    if (on) write_targets<F16>(c, at, c.row[at], 0, v1, 0, threadIdx.x, 128);
     const float f = on ? powers_worth(c.row[at]) : 0.f;
     const uint4* from = (const uint4*)(c.hc + at * c.Dp);
     uint4* to = (uint4*)(c.hs + at * c.Dp);
@@ -418,14 +563,16 @@ __global__ void __launch_bounds__(128) k_vocab_worth(VocabCall c, int64_t v1) {
 // The product taken again has written a piece's operand; only the targets' entries are left.
 template <bool F16>
 __global__ void __launch_bounds__(128) k_vocab_targets(VocabCall c, int64_t v0, int64_t v1) {
+    after_previous();
     const int64_t at = blockIdx.x;
     if (at >= c.ctl->n_valid) return;
-    write_targets<F16>(c, at, v0, v1, v0, threadIdx.x, 128);
+    write_targets<F16>(c, at, c.row[at], v0, v1, v0, threadIdx.x, 128);
 }
 
 // dh in the caller's rows from its parts' sums, added in their order.
 template <bool F16>
 __global__ void __launch_bounds__(256) k_vocab_finish_dh(VocabCall c) {
+    after_previous();
     const int64_t at = blockIdx.x, i = ((int64_t)blockIdx.y * 256 + threadIdx.x) * 2;
     if (at >= c.ctl->n_valid || i >= c.D) return;
     const float f = c.ctl->inv_scale * (c.powers ? powers_worth(c.row[at]) : 1.f);
@@ -526,33 +673,35 @@ template <bool F16>
 static int enqueue(const VocabCall& c, bool distill, int sms, cudaStream_t st) {
     const unsigned n = (unsigned)c.n, groups = (n + 31) / 32;
     const bool grad = c.dh || c.dw;
-    if (distill) k_vocab_teacher<<<(n + 7) / 8, 256, 0, st>>>(c);
-    k_vocab_rows<<<1, 1024, 0, st>>>(c);
+    if (distill) {
+        k_vocab_teacher<<<(n + 7) / 8, 256, 0, st>>>(c);
+        GK_CUDA_TRY(cudaGetLastError());
+    }
+    if (c.n > kRankRows) GK_CUDA_TRY(launch_next(k_vocab_rows, dim3(1), 1024, 0, st, c));
     if (c.wc) {
         const int64_t blocks = (c.V * (c.Dp / 8) + 255) / 256;
-        k_vocab_copy_w<<<(unsigned)(blocks < 16 * sms ? blocks : 16 * sms), 256, 0, st>>>(c);
+        GK_CUDA_TRY(launch_next(k_vocab_copy_w, dim3((unsigned)(blocks < 16 * sms ? blocks : 16 * sms)), 256, 0, st, c));
     }
-    k_vocab_gather<F16><<<(unsigned)c.n_pad, 128, 0, st>>>(c);
-    GK_CUDA_TRY(cudaGetLastError());
-    note_launch(2 + (distill ? 1 : 0) + (c.wc ? 1 : 0));
+    GK_CUDA_TRY(launch_next(c.n > kRankRows ? k_vocab_gather<F16, false> : k_vocab_gather<F16, true>, dim3((unsigned)c.n_pad), 128, 0, st, c));
+    note_launch(1 + (distill ? 1 : 0) + (c.n > kRankRows ? 1 : 0) + (c.wc ? 1 : 0));
     const int64_t kept = grad ? (c.vb < c.V ? c.vb : c.V) : 0;
     int rc = GK_OK;
     if (kept > 0) rc = c.powers ? launch_vocab_powers(c, 0, kept, false, sms, st) : launch_vocab_logits(c, 0, kept, true, false, sms, st);
     if (rc == GK_OK && kept < c.V) rc = launch_vocab_logits(c, kept, c.V, false, false, sms, st);
     if (rc != GK_OK) return rc;
-    k_vocab_rows_done<false><<<groups, 1024, 0, st>>>(c);
-    GK_CUDA_TRY(cudaGetLastError());
-    note_launch();
+    const bool own = grad && !c.powers && (c.V + kVocabTile - 1) / kVocabTile <= kOwnTiles;
+    if (!own) {
+        GK_CUDA_TRY(launch_next(k_vocab_rows_done<false>, dim3(groups), 1024, 0, st, c));
+        note_launch();
+    }
     if (!grad) return GK_OK;
     if (c.powers) {
         rc = launch_vocab_logits(c, 0, kept, false, true, sms, st);
         if (rc != GK_OK) return rc;
-        k_vocab_rows_done<true><<<groups, 1024, 0, st>>>(c);
-        GK_CUDA_TRY(cudaGetLastError());
+        GK_CUDA_TRY(launch_next(k_vocab_rows_done<true>, dim3(groups), 1024, 0, st, c));
         rc = launch_vocab_powers(c, 0, kept, true, sms, st);
         if (rc != GK_OK) return rc;
-        k_vocab_worth<F16><<<(unsigned)round_up(n, 64), 128, 0, st>>>(c, kept);
-        GK_CUDA_TRY(cudaGetLastError());
+        GK_CUDA_TRY(launch_next(k_vocab_worth<F16>, dim3((unsigned)round_up(n, 64)), 128, 0, st, c, kept));
         note_launch(2);
     }
     for (int64_t v0 = 0; v0 < c.V; v0 += c.vb) {
@@ -560,18 +709,18 @@ static int enqueue(const VocabCall& c, bool distill, int sms, cudaStream_t st) {
         if (v0 > 0) {
             rc = c.powers ? launch_vocab_powers(c, v0, v1, false, sms, st) : launch_vocab_again(c, v0, v1, sms, st);
             if (rc != GK_OK) return rc;
-            k_vocab_targets<F16><<<n, 128, 0, st>>>(c, v0, v1);
+            GK_CUDA_TRY(launch_next(k_vocab_targets<F16>, dim3(n), 128, 0, st, c, v0, v1));
+            note_launch();
         } else if (!c.powers) {
-            k_vocab_scale<F16><<<dim3((unsigned)round_up(n, 64), (unsigned)((v1 + kGradCols - 1) / kGradCols)), 256, 0, st>>>(c, v0, v1);
+            const dim3 grid((unsigned)round_up(n, 64), (unsigned)((v1 + kGradCols - 1) / kGradCols));
+            GK_CUDA_TRY(launch_next(own ? k_vocab_scale<F16, true> : k_vocab_scale<F16, false>, grid, 256, 0, st, c, v0, v1));
+            note_launch();
         }
-        GK_CUDA_TRY(cudaGetLastError());
-        note_launch(v0 > 0 || !c.powers ? 1 : 0);
         rc = launch_vocab_grads(c, v0, v1, v0 == 0, sms, st);
         if (rc != GK_OK) return rc;
     }
     if (c.dhp) {
-        k_vocab_finish_dh<F16><<<dim3(n, (unsigned)((c.D + 511) / 512)), 256, 0, st>>>(c);
-        GK_CUDA_TRY(cudaGetLastError());
+        GK_CUDA_TRY(launch_next(k_vocab_finish_dh<F16>, dim3(n, (unsigned)((c.D + 511) / 512)), 256, 0, st, c));
         note_launch();
     }
     return GK_OK;

@@ -75,6 +75,23 @@ struct VocabCall {
     int splits;
 };
 
+// Launches after a call's first: the kernel may be set up while the one before it ends, and waits for
+// that with after_previous() before it reads or writes anything of the call.
+template <class... Params, class... Args>
+inline cudaError_t launch_next(void (*kernel)(Params...), dim3 grid, unsigned threads, size_t smem, cudaStream_t st, Args&&... args) {
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, static_cast<Args&&>(args)...);
+}
+
 __host__ __device__ inline int64_t round_up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
 
 // The products (gk_vocab_gemm.cu).  v0, v1: the columns of the vocabulary [v0, v1); if_missed: nothing is
@@ -92,6 +109,11 @@ int launch_vocab_grads(const VocabCall& c, int64_t v0, int64_t v1, bool first, i
 int vocab_dh_splits(int64_t n, int64_t D, int64_t vb, bool dw, int sm_count);
 
 #ifdef __CUDACC__
+
+// Everything before it in the stream is done and seen; the next kernel may be set up.
+__device__ __forceinline__ void after_previous() {
+    asm volatile("griddepcontrol.wait;\ngriddepcontrol.launch_dependents;" ::: "memory");
+}
 
 __device__ __forceinline__ bool teacher_ascending(const float4& t) { return ((int)t.w & 1) != 0; }
 __device__ __forceinline__ bool teacher_counts(const float4& t) { return ((int)t.w & 2) != 0; }

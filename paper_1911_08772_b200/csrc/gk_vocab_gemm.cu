@@ -557,15 +557,9 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     const uint32_t rank = cluster_rank();
     const uint32_t stage0 = (smem_u32(smem_raw) + 1023u) & ~1023u, staging0 = stage0 + kBlockBytes;
     const VocabCall& c = p.c;
-    if (p.if_missed && c.ctl->missed == 0) return;
     const int width = p.narrow ? kHalfN : kTileN;
     const int stages = p.narrow ? 6 : 4;
     const uint32_t stage_bytes = (p.narrow ? 2 : 3) * kOperandBytes;
-    const int n_valid = (int)__reduce_max_sync(0xffffffffu, (unsigned)c.ctl->n_valid);   // one value, known as such
-
-    const int64_t nv = p.v1 - p.v0, n_cols = P == kGrads ? c.D : nv;      // columns of the result
-    const Tiles tiles = P == kGrads ? make_tiles(c.dh ? n_valid : 0, c.D, nv, width, p.splits) : make_tiles(n_valid, nv, c.D, width, 1);
-    const Tiles tiles2 = make_tiles(P == kGrads && c.dw ? nv : 0, c.D, n_valid, width, 1);
     const int64_t cluster = blockIdx.x >> 1, clusters = gridDim.x >> 1;
 
     if (tid == 0) {
@@ -589,9 +583,18 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     cluster_barrier();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = tmem_slot;
+    after_previous();
+
+    const int n_valid = (int)__reduce_max_sync(0xffffffffu, (unsigned)c.ctl->n_valid);   // one value, known as such
+
+    const int64_t nv = p.v1 - p.v0, n_cols = P == kGrads ? c.D : nv;      // columns of the result
+    const Tiles tiles = P == kGrads ? make_tiles(c.dh ? n_valid : 0, c.D, nv, width, p.splits) : make_tiles(n_valid, nv, c.D, width, 1);
+    const Tiles tiles2 = make_tiles(P == kGrads && c.dw ? nv : 0, c.D, n_valid, width, 1);
+    const bool idle = p.if_missed && c.ctl->missed == 0;
 
     bool ok = true;
-    if (warp == 0) {
+    if (idle) {
+    } else if (warp == 0) {
         // producer: this CTA's 128 rows of A and of each half of B; the leader's barrier counts both CTAs' bytes
         int stage = 0;
         uint32_t phase = 0;
@@ -893,8 +896,8 @@ static int launch_product(ProductArgs p, int sm_count, cudaStream_t st) {
         GK_CUDA_TRY(cudaFuncSetAttribute(k_vocab_product<P, F16>, cudaFuncAttributeMaxDynamicSharedMemorySize, kProductSmem));
         if (dev < 64) ready.fetch_or(1ull << dev);
     }
-    k_vocab_product<P, F16><<<(unsigned)(2 * (pairs < most ? pairs : most)), kProductThreads, kProductSmem, st>>>(a, b, out, a2, b2, out2, p);
-    GK_CUDA_TRY(cudaGetLastError());
+    GK_CUDA_TRY(launch_next(k_vocab_product<P, F16>, dim3((unsigned)(2 * (pairs < most ? pairs : most))), kProductThreads, kProductSmem, st,
+                            a, b, out, a2, b2, out2, p));
     note_launch();
     return GK_OK;
 }
