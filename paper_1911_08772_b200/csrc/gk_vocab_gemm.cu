@@ -217,6 +217,7 @@ struct ProductArgs {
     int splits;      // dh: parts of the summed axis
     int direct;      // dh: one part and one piece, 16-bit rows are stored at once
     int wide;        // dw: rows start and end on 16-byte boundaries
+    int dh_unit, dw_unit;   // values in the boundary that rows start on: 1, 2, 4, 8
 };
 
 // What a reading warp finishes: 128 columns of 32 rows.
@@ -373,25 +374,43 @@ __device__ __forceinline__ void read_gradients(const ProductArgs& p, const Patch
     }
 }
 
-// A warp's 32 rows x 64 16-bit columns from its staging memory, a row at a time with two columns a lane,
-// to rows on any boundary.  `to`: where the thread's own row has column 0 of the 64, nullptr: nowhere.
+// A warp's 32 rows x 64 16-bit columns from its staging memory to rows on boundaries of VEC values, VEC a lane:
+// one row at a time by two values, two by four, four by eight (dw of 10000 x 1500, whose rows start on 8
+// bytes: 62 us for both gradients by two, 45 by four).  `to`: where the thread's own row has column 0 of
+// the 64, nullptr: nowhere.
+template <int VEC>
 __device__ __forceinline__ void store_rows(uint32_t staging, int lane, uint16_t* to, int64_t cols) {
+    constexpr int kLanes = 64 / VEC, kRows = 32 / kLanes;
     __syncwarp();
+    const int col = lane % kLanes * VEC;
 #pragma unroll 4
-    for (int r = 0; r < 32; ++r) {
+    for (int r0 = 0; r0 < 32; r0 += kRows) {
+        const int r = r0 + lane / kLanes;
         uint16_t* at = (uint16_t*)__shfl_sync(0xffffffffu, (unsigned long long)to, r);
-        if (!at) continue;
-        at += lane * 2;
-        uint32_t x;
-        asm volatile("ld.shared.b32 %0, [%1];"
-                     : "=r"(x) : "r"(staging + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4) : "memory");
-        if (lane * 2 + 1 < cols && ((uintptr_t)at & 3) == 0) *(uint32_t*)at = x;
-        else {
-            if (lane * 2 < cols) at[0] = (uint16_t)x;
-            if (lane * 2 + 1 < cols) at[1] = (uint16_t)(x >> 16);
+        if (!at || col >= cols) continue;
+        const uint32_t from = staging + r * 128 + (((col >> 3) ^ (r & 7)) << 4) + (col & 7) * 2;
+        uint32_t x[4];
+        if constexpr (VEC == 2) asm volatile("ld.shared.b32 %0, [%1];" : "=r"(x[0]) : "r"(from) : "memory");
+        else if constexpr (VEC == 4) asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(x[0]), "=r"(x[1]) : "r"(from) : "memory");
+        else asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(from) : "memory");
+        at += col;
+        if (col + VEC <= cols && ((uintptr_t)at & (2 * VEC - 1)) == 0) {
+            if constexpr (VEC == 2) *(uint32_t*)at = x[0];
+            else if constexpr (VEC == 4) *(uint2*)at = make_uint2(x[0], x[1]);
+            else *(uint4*)at = make_uint4(x[0], x[1], x[2], x[3]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i)
+                if (col + i < cols) at[i] = (uint16_t)(x[i / 2] >> (i % 2 * 16));
         }
     }
     __syncwarp();
+}
+// `unit`: the boundary in values that all rows start on.
+__device__ __forceinline__ void store_rows(uint32_t staging, int lane, uint16_t* to, int64_t cols, int unit) {
+    if (unit >= 8) store_rows<8>(staging, lane, to, cols);
+    else if (unit >= 4) store_rows<4>(staging, lane, to, cols);
+    else store_rows<2>(staging, lane, to, cols);
 }
 
 template <bool F16>
@@ -420,7 +439,7 @@ __device__ __forceinline__ void read_dw(const ProductArgs& p, const Patch& w, co
         stage16<F16>(w, v, inv, empty);
         if (p.wide) stage_store(w.staging, w.lane, out, (int)w.col0 + ch * 64, (int)w.row0);
         else store_rows(w.staging, w.lane, w.lane < rows ? (uint16_t*)c.dw + (p.v0 + w.row0 + w.lane) * c.lddw + w.col0 + ch * 64 : nullptr,
-                        w.cols - ch * 64);
+                        w.cols - ch * 64, p.dw_unit);
     }
 }
 
@@ -443,7 +462,7 @@ __device__ __forceinline__ void read_dh(const ProductArgs& p, const Patch& w, co
             tmem_ld64(w.tmem + ch * 64, v);
             stage_reuse(w.lane);
             stage16<F16>(w, v, f, false);
-            store_rows(w.staging, w.lane, to ? to + ch * 64 : nullptr, w.cols - ch * 64);
+            store_rows(w.staging, w.lane, to ? to + ch * 64 : nullptr, w.cols - ch * 64, p.dh_unit);
         }
         return;
     }
@@ -915,6 +934,12 @@ static int launch(const VocabCall& c, int64_t v0, int64_t v1, bool first, bool i
     p.direct = c.dhp == nullptr;
     // (the copies' hardware cuts a row's end in steps of 16 bytes, so the rows' length counts too)
     p.wide = (((uintptr_t)c.dw | (uintptr_t)(2 * c.lddw) | (uintptr_t)(2 * c.D)) & 15) == 0;
+    auto unit = [](const void* base, int64_t ld) {
+        const uintptr_t x = (uintptr_t)base | (uintptr_t)(2 * ld);
+        return (x & 15) == 0 ? 8 : (x & 7) == 0 ? 4 : (x & 3) == 0 ? 2 : 1;
+    };
+    p.dh_unit = unit(c.dh, c.lddh);
+    p.dw_unit = unit(c.dw, c.lddw);
     return c.f16 ? launch_product<P, true>(p, sm_count, st) : launch_product<P, false>(p, sm_count, st);
 }
 
