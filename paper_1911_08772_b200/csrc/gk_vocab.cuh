@@ -110,9 +110,10 @@ int vocab_dh_splits(int64_t n, int64_t D, int64_t vb, bool dw, int sm_count);
 
 #ifdef __CUDACC__
 
-// Everything before it in the stream is done and seen; the next kernel may be set up.
+// The next kernel may be set up (it waits in the same way); then everything before in the stream is done
+// and seen.
 __device__ __forceinline__ void after_previous() {
-    asm volatile("griddepcontrol.wait;\ngriddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;\ngriddepcontrol.wait;" ::: "memory");
 }
 
 __device__ __forceinline__ bool teacher_ascending(const float4& t) { return ((int)t.w & 1) != 0; }

@@ -581,6 +581,13 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     const uint32_t stage_bytes = (p.narrow ? 2 : 3) * kOperandBytes;
     const int64_t cluster = blockIdx.x >> 1, clusters = gridDim.x >> 1;
 
+    if (tid == 32) {       // the descriptors are on their way while the rest is set up
+        for (const CUtensorMap* m : {&map_a, &map_b, &map_out})
+            asm volatile("prefetch.tensormap [%0];" ::"l"(m) : "memory");
+        if (P == kGrads)
+            for (const CUtensorMap* m : {&map_a2, &map_b2, &map_out2})
+                asm volatile("prefetch.tensormap [%0];" ::"l"(m) : "memory");
+    }
     if (tid == 0) {
         for (int s = 0; s < kMaxStages; ++s) {
             mbar_init(smem_u32(&bar_full[s]), 1);
