@@ -242,6 +242,7 @@ __device__ __forceinline__ uint4 load8(const uint16_t* p, int64_t left) {
 // RANK (few rows): each CTA takes a row of the caller's and finds its number itself, by looking at all rows
 // (2048 rows are 16 loads a thread, where a launch of its own costs 3 to 6 us); one of them writes the
 // control block.
+// CTAs from n_pad on make the copy of w with rows that start and end on 16-byte boundaries, where w's own do not.
 constexpr int64_t kRankRows = 2048;
 
 template <bool F16, bool RANK>
@@ -250,6 +251,15 @@ __global__ void __launch_bounds__(128) k_vocab_gather(VocabCall c) {
     __shared__ float tops[4];
     after_previous();
     const int tid = threadIdx.x, lane = tid & 31;
+    if (blockIdx.x >= c.n_pad) {
+        const int64_t words = c.Dp / 8, total = c.V * words, threads = (gridDim.x - c.n_pad) * 128;
+#pragma unroll 4
+        for (int64_t i = (blockIdx.x - c.n_pad) * 128 + tid; i < total; i += threads) {
+            const int64_t v = i / words, k = (i - v * words) * 8;
+            ((uint4*)c.wc)[i] = load8((const uint16_t*)c.w + v * c.ldw + k, c.D - k);
+        }
+        return;
+    }
     int at = blockIdx.x, n_valid;
     int64_t r;
     bool left_out;
@@ -317,16 +327,15 @@ __global__ void __launch_bounds__(128) k_vocab_gather(VocabCall c) {
         if (!teacher_ascending(te)) { first = 0; last = c.K; }
     }
     __syncthreads();
-    const uint16_t* w = c.wc ? c.wc : (const uint16_t*)c.w;
-    const int64_t ldw = c.wc ? c.Dp : c.ldw, words = c.wc ? c.Dp / 8 : c.D / 8;   // rows of w in words: see run_head
+    const int64_t words = (c.D + 7) / 8;
     for (int j = first + (tid >> 5); j < last; j += 4) {
         const int64_t v = c.target ? c.target[r] : (int64_t)c.t_idx[r * c.K + j];
         float s = 0.f;
         if (v >= 0 && v < c.V) {
-            const uint4* wr = (const uint4*)(w + v * ldw);
+            const uint16_t* wr = (const uint16_t*)c.w + v * c.ldw;
             for (int64_t b = lane; b < words; b += 32) {
                 const uint4 x = ((const uint4*)to)[b];
-                const uint4 y = __ldg(wr + b);
+                const uint4 y = load8(wr + b * 8, c.D - b * 8);
                 const unsigned xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
@@ -340,16 +349,6 @@ __global__ void __launch_bounds__(128) k_vocab_gather(VocabCall c) {
             c.zt[(int64_t)at * c.K + j] = s;
             if (c.target || j == teacher_largest(c.teacher[r])) c.row[at].ref = s * c.zscale;
         }
-    }
-}
-
-// A copy of w with rows that start and end on 16-byte boundaries, where w's own do not.
-__global__ void __launch_bounds__(256) k_vocab_copy_w(VocabCall c) {
-    after_previous();
-    const int64_t words = c.Dp / 8, total = c.V * words;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-        const int64_t v = i / words, k = (i - v * words) * 8;
-        ((uint4*)c.wc)[i] = load8((const uint16_t*)c.w + v * c.ldw + k, c.D - k);
     }
 }
 
@@ -678,12 +677,10 @@ static int enqueue(const VocabCall& c, bool distill, int sms, cudaStream_t st) {
         GK_CUDA_TRY(cudaGetLastError());
     }
     if (c.n > kRankRows) GK_CUDA_TRY(launch_next(k_vocab_rows, dim3(1), 1024, 0, st, c));
-    if (c.wc) {
-        const int64_t blocks = (c.V * (c.Dp / 8) + 255) / 256;
-        GK_CUDA_TRY(launch_next(k_vocab_copy_w, dim3((unsigned)(blocks < 16 * sms ? blocks : 16 * sms)), 256, 0, st, c));
-    }
-    GK_CUDA_TRY(launch_next(c.n > kRankRows ? k_vocab_gather<F16, false> : k_vocab_gather<F16, true>, dim3((unsigned)c.n_pad), 128, 0, st, c));
-    note_launch(1 + (distill ? 1 : 0) + (c.n > kRankRows ? 1 : 0) + (c.wc ? 1 : 0));
+    const int64_t copies = c.wc ? (c.V * (c.Dp / 8) + 127) / 128 : 0;
+    GK_CUDA_TRY(launch_next(c.n > kRankRows ? k_vocab_gather<F16, false> : k_vocab_gather<F16, true>,
+                            dim3((unsigned)(c.n_pad + (copies < 16 * sms ? copies : 16 * sms))), 128, 0, st, c));
+    note_launch(1 + (distill ? 1 : 0) + (c.n > kRankRows ? 1 : 0));
     const int64_t kept = grad ? (c.vb < c.V ? c.vb : c.V) : 0;
     int rc = GK_OK;
     if (kept > 0) rc = c.powers ? launch_vocab_powers(c, 0, kept, false, sms, st) : launch_vocab_logits(c, 0, kept, true, false, sms, st);

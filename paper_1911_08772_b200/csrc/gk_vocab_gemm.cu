@@ -789,14 +789,16 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                 w.col0 = (P == kGrads ? 0 : p.v0) + col;
                 constexpr bool kLogitUse = P == kLogits || P == kLogitsKeep || P == kPowers;
                 if constexpr (kLogitUse)
-                    if (c.t_idx && w.cols > 0) w.cursor = first_pair(c, w.row0 + lane, n_valid, w.col0);
+                    if (c.t_idx && w.cols > 0 && w.row0 < n_valid) w.cursor = first_pair(c, w.row0 + lane, n_valid, w.col0);
                 ok = warp_wait(smem_u32(&bar_sum[h]), phases >> h & 1);
                 if (!ok) break;
                 phases ^= 1u << h;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                if (w.cols > 0) {
+                // rows that are used: those that count, and for powers and gradients those that dw sums over
+                const bool used = P == kGrads || w.row0 < (P == kPowers || P == kAgain ? round_up(n_valid, 64) : n_valid);
+                if (w.cols > 0 && used) {
                     if constexpr (kLogitUse)
-                        if (c.t_idx) take_pairs(c, w, n_valid);
+                        if (c.t_idx && w.row0 < n_valid) take_pairs(c, w, n_valid);
                     if constexpr (P == kLogits || P == kLogitsKeep) {
                         if (w.cols >= 128) read_logits<P, F16, false>(p, w, &map_out, n_valid);
                         else read_logits<P, F16, true>(p, w, &map_out, n_valid);
