@@ -488,30 +488,36 @@ __device__ __forceinline__ void read_dh(const ProductArgs& p, const Patch& w, co
     }
 }
 
-// The tiles of a call in the order in which the clusters take them.
+// The tiles of a call in the order in which the clusters take them.  In 32 bits (the sums of 2^31 tiles'
+// rows would take more memory than there is): 64-bit divisions cost a microsecond a tile.
 struct Tiles {
-    int64_t tm, tn, total;
+    uint32_t tm, tn, total;
     int kb, splits;
-    __device__ __forceinline__ void at(int64_t t, int64_t& m, int64_t& n, int& split) const {
-        const int64_t per = tm * tn;
-        split = (int)(t / per);
-        t -= split * per;
-        const int64_t band = t / (kRasterRows * tn), m0 = band * kRasterRows;
-        const int64_t rows = tm - m0 < kRasterRows ? tm - m0 : kRasterRows;
-        t -= band * kRasterRows * tn;
-        m = m0 + t % rows;
-        n = t / rows;
+    __device__ __forceinline__ void at(uint32_t t, int& m, int& n, int& split) const {
+        const uint32_t per = tm * tn;
+        uint32_t s = 0;
+        if (splits > 1) {
+            s = t / per;
+            t -= s * per;
+        }
+        const uint32_t band = t / (kRasterRows * tn), m0 = band * kRasterRows;
+        const uint32_t rows = tm - m0 < kRasterRows ? tm - m0 : kRasterRows;
+        t -= m0 * tn;
+        const uint32_t col = t / rows;
+        m = (int)(m0 + t - col * rows);
+        n = (int)col;
+        split = (int)s;
     }
     __device__ __forceinline__ void blocks(int split, int& k0, int& k1) const {
-        k0 = (int)((int64_t)kb * split / splits);
-        k1 = (int)((int64_t)kb * (split + 1) / splits);
+        k0 = splits > 1 ? kb * split / splits : 0;
+        k1 = splits > 1 ? kb * (split + 1) / splits : kb;
     }
 };
 
 __device__ __forceinline__ Tiles make_tiles(int64_t rows, int64_t cols, int64_t K, int width, int splits) {
     Tiles t;
-    t.tm = (rows + kTileM - 1) / kTileM;
-    t.tn = (cols + width - 1) / width;
+    t.tm = (uint32_t)((rows + kTileM - 1) / kTileM);
+    t.tn = (uint32_t)((cols + width - 1) / width);
     t.kb = (int)((K + kBlockK - 1) / kBlockK);
     t.splits = splits;
     t.total = t.tm * t.tn * splits;
@@ -522,19 +528,19 @@ __device__ __forceinline__ Tiles make_tiles(int64_t rows, int64_t cols, int64_t 
 // out in turn, so that some clusters have one more than the others; the others then get as much of the
 // second kind (dw's) as makes up for it, and the rest is dealt in turn again, beginning with them.
 struct Deal {
-    int64_t n1, n2, clusters, heavy;      // heavy: clusters with one more of the first kind
-    int64_t extra;                        // tiles of the second kind that make up for it
-    int64_t index, at;                    // the cluster, its next tile of the present kind
+    int n1, n2, clusters, heavy;      // heavy: clusters with one more of the first kind
+    int extra;                        // tiles of the second kind that make up for it
+    int index, at;                    // the cluster, its next tile of the present kind
     bool light;
     int kind;                             // 0: first, 1: extra, 2: rest
-    __device__ __forceinline__ Deal(const Tiles& a, const Tiles& b, int64_t cluster, int64_t clusters_) {
-        n1 = a.total;
-        n2 = b.total;
+    __device__ __forceinline__ Deal(const Tiles& a, const Tiles& b, int cluster, int clusters_) {
+        n1 = (int)a.total;
+        n2 = (int)b.total;
         clusters = clusters_;
         heavy = n1 % clusters;
         light = cluster >= heavy;
         // a tile costs its blocks and about two more
-        const int64_t each = heavy ? (a.kb / a.splits + 2) / (b.kb + 2) : 0;
+        const int each = heavy ? (a.kb / a.splits + 2) / (b.kb + 2) : 0;
         extra = each * (clusters - heavy);
         if (extra > n2) extra = n2;
         at = cluster;
@@ -542,19 +548,19 @@ struct Deal {
         index = cluster;
     }
     // The next tile: `dw`: of the second kind; false: none left.
-    __device__ __forceinline__ bool next(int64_t& t, bool& dw) {
+    __device__ __forceinline__ bool next(uint32_t& t, bool& dw) {
         if (kind == 0) {
-            if (at < n1) { t = at; dw = false; at += clusters; return true; }
+            if (at < n1) { t = (uint32_t)at; dw = false; at += clusters; return true; }
             kind = 1;
             at = light ? index - heavy : n2;
         }
         if (kind == 1) {
-            if (at < extra) { t = at; dw = true; at += clusters - heavy; return true; }
+            if (at < extra) { t = (uint32_t)at; dw = true; at += clusters - heavy; return true; }
             kind = 2;
             at = extra + (light ? index - heavy : index + clusters - heavy);
         }
         if (at >= n2) return false;
-        t = at;
+        t = (uint32_t)at;
         dw = true;
         at += clusters;
         return true;
@@ -579,7 +585,7 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     const int width = p.narrow ? kHalfN : kTileN;
     const int stages = p.narrow ? 6 : 4;
     const uint32_t stage_bytes = (p.narrow ? 2 : 3) * kOperandBytes;
-    const int64_t cluster = blockIdx.x >> 1, clusters = gridDim.x >> 1;
+    const int cluster = (int)(blockIdx.x >> 1), clusters = (int)(gridDim.x >> 1);
 
     if (tid == 32) {       // the descriptors are on their way while the rest is set up
         for (const CUtensorMap* m : {&map_a, &map_b, &map_out})
@@ -624,11 +630,10 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         // producer: this CTA's 128 rows of A and of each half of B; the leader's barrier counts both CTAs' bytes
         int stage = 0;
         uint32_t phase = 0;
-        int64_t t;
+        uint32_t t;
         bool dw;
         for (Deal deal(tiles, tiles2, cluster, clusters); ok && deal.next(t, dw);) {
-            int64_t m, n;
-            int split, k0, k1;
+            int m, n, split, k0, k1;
             if (P != kGrads) dw = false;
             (dw ? tiles2 : tiles).at(t, m, n, split);
             (dw ? tiles2 : tiles).blocks(split, k0, k1);
@@ -690,11 +695,10 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
             int stage_a = 0, stage_b = 0;     // next block of the first half (of the only one), of the second half
             uint32_t phase = 0, free0 = 0, free1 = 0;
             int only = 0;                     // the half a narrow tile has
-            int64_t t;
+            uint32_t t;
             bool dw;
             for (Deal deal(tiles, tiles2, cluster, clusters); ok && deal.next(t, dw);) {
-                int64_t m, n;
-                int split, k0, k1;
+                int m, n, split, k0, k1;
                 if (P != kGrads) dw = false;
                 (dw ? tiles2 : tiles).at(t, m, n, split);
                 (dw ? tiles2 : tiles).blocks(split, k0, k1);
@@ -771,16 +775,15 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         Patch w;
         w.lane = lane;
         w.staging = staging0 + (warp - 4) * kStagingBytes;
-        int64_t t;
+        uint32_t t;
         bool dw;
         for (Deal deal(tiles, tiles2, cluster, clusters); ok && deal.next(t, dw);) {
-            int64_t m, n;
-            int split, k0, k1;
+            int m, n, split, k0, k1;
             if (P != kGrads) dw = false;
             (dw ? tiles2 : tiles).at(t, m, n, split);
             (dw ? tiles2 : tiles).blocks(split, k0, k1);
             const bool two = !p.narrow && n * kTileN + kHalfN < n_cols;
-            w.row0 = m * kTileM + rank * 128 + quarter * 32;
+            w.row0 = m * kTileM + (int)rank * 128 + quarter * 32;
 #pragma unroll 1
             for (int h = only; h < (two ? 2 : only + 1); ++h) {
                 const int64_t col = n * width + (two ? h * kHalfN : 0) + side * 128;
