@@ -139,33 +139,41 @@ __device__ __forceinline__ void commit_pair(uint32_t bar) {
         "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
         ::"r"(bar), "h"((uint16_t)3) : "memory");
 }
-// One column, or 64, of this thread's lane.  All lanes of the warp take part, whatever rows they have.
+// One column, or 128, of this thread's lane.  All lanes of the warp take part, whatever rows they have.
 __device__ __forceinline__ float tmem_ld1(uint32_t addr) {
     uint32_t r;
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];\ntcgen05.wait::ld.sync.aligned;" : "=r"(r) : "r"(addr) : "memory");
     return __uint_as_float(r);
 }
-__device__ __forceinline__ void tmem_ld64(uint32_t addr, float (&v)[64]) {
-    uint32_t r[64];
-    __syncwarp();
+__device__ __forceinline__ void tmem_ld128(uint32_t addr, float (&v)[128]) {
     asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x64.b32 {"
+        "tcgen05.ld.sync.aligned.32x32b.x128.b32 {"
         "%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
         "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, "
         "%32, %33, %34, %35, %36, %37, %38, %39, %40, %41, %42, %43, %44, %45, %46, %47, "
-        "%48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, %62, %63}, [%64];\n"
+        "%48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, %62, %63, "
+        "%64, %65, %66, %67, %68, %69, %70, %71, %72, %73, %74, %75, %76, %77, %78, %79, "
+        "%80, %81, %82, %83, %84, %85, %86, %87, %88, %89, %90, %91, %92, %93, %94, %95, "
+        "%96, %97, %98, %99, %100, %101, %102, %103, %104, %105, %106, %107, %108, %109, %110, %111, "
+        "%112, %113, %114, %115, %116, %117, %118, %119, %120, %121, %122, %123, %124, %125, %126, %127}, [%128];\n"
         "tcgen05.wait::ld.sync.aligned;"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
-          "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
-          "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]),
-          "=r"(r[32]), "=r"(r[33]), "=r"(r[34]), "=r"(r[35]), "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]),
-          "=r"(r[40]), "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47]),
-          "=r"(r[48]), "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]), "=r"(r[54]), "=r"(r[55]),
-          "=r"(r[56]), "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]), "=r"(r[62]), "=r"(r[63])
+        : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]),
+          "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]),
+          "=f"(v[16]), "=f"(v[17]), "=f"(v[18]), "=f"(v[19]), "=f"(v[20]), "=f"(v[21]), "=f"(v[22]), "=f"(v[23]),
+          "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]), "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31]),
+          "=f"(v[32]), "=f"(v[33]), "=f"(v[34]), "=f"(v[35]), "=f"(v[36]), "=f"(v[37]), "=f"(v[38]), "=f"(v[39]),
+          "=f"(v[40]), "=f"(v[41]), "=f"(v[42]), "=f"(v[43]), "=f"(v[44]), "=f"(v[45]), "=f"(v[46]), "=f"(v[47]),
+          "=f"(v[48]), "=f"(v[49]), "=f"(v[50]), "=f"(v[51]), "=f"(v[52]), "=f"(v[53]), "=f"(v[54]), "=f"(v[55]),
+          "=f"(v[56]), "=f"(v[57]), "=f"(v[58]), "=f"(v[59]), "=f"(v[60]), "=f"(v[61]), "=f"(v[62]), "=f"(v[63]),
+          "=f"(v[64]), "=f"(v[65]), "=f"(v[66]), "=f"(v[67]), "=f"(v[68]), "=f"(v[69]), "=f"(v[70]), "=f"(v[71]),
+          "=f"(v[72]), "=f"(v[73]), "=f"(v[74]), "=f"(v[75]), "=f"(v[76]), "=f"(v[77]), "=f"(v[78]), "=f"(v[79]),
+          "=f"(v[80]), "=f"(v[81]), "=f"(v[82]), "=f"(v[83]), "=f"(v[84]), "=f"(v[85]), "=f"(v[86]), "=f"(v[87]),
+          "=f"(v[88]), "=f"(v[89]), "=f"(v[90]), "=f"(v[91]), "=f"(v[92]), "=f"(v[93]), "=f"(v[94]), "=f"(v[95]),
+          "=f"(v[96]), "=f"(v[97]), "=f"(v[98]), "=f"(v[99]), "=f"(v[100]), "=f"(v[101]), "=f"(v[102]), "=f"(v[103]),
+          "=f"(v[104]), "=f"(v[105]), "=f"(v[106]), "=f"(v[107]), "=f"(v[108]), "=f"(v[109]), "=f"(v[110]), "=f"(v[111]),
+          "=f"(v[112]), "=f"(v[113]), "=f"(v[114]), "=f"(v[115]), "=f"(v[116]), "=f"(v[117]), "=f"(v[118]), "=f"(v[119]),
+          "=f"(v[120]), "=f"(v[121]), "=f"(v[122]), "=f"(v[123]), "=f"(v[124]), "=f"(v[125]), "=f"(v[126]), "=f"(v[127])
         : "r"(addr) : "memory");
-#pragma unroll
-    for (int i = 0; i < 64; ++i) v[i] = __uint_as_float(r[i]);
 }
 // A warp's 32 rows x 128 bytes in shared memory to global memory: 16-byte words are stored at
 // (word ^ row mod 8), the 128-byte swizzle of the tensor map.
@@ -270,35 +278,30 @@ __device__ __forceinline__ void take_pairs(const VocabCall& c, const Patch& w, i
     }
 }
 
-template <int P, bool F16, bool EDGE>
-__device__ __forceinline__ void read_logits(const ProductArgs& p, const Patch& w, const CUtensorMap* out, int n_valid) {
+// The readers work on 128 columns in registers: the tensor memory is free for the next tile's sums as soon as
+// it has been copied (a wide tile of 32 blocks took 24.2 us when it was read out column by column, 17.5 of them
+// sums).  Columns past the result's end hold -inf in the uses that make logits.
+template <int P, bool F16>
+__device__ __forceinline__ void read_logits(const ProductArgs& p, const Patch& w, const CUtensorMap* out, int n_valid, float (&v)[128]) {
     const VocabCall& c = p.c;
     const int64_t row = w.row0 + w.lane;
-    const int cols = (int)(w.cols < 128 ? w.cols : 128);
-    float v[64];
-    float m = -INFINITY;
-#pragma unroll 1
-    for (int ch = 0; ch < 2; ++ch) {
-        tmem_ld64(w.tmem + ch * 64, v);
+    float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-        for (int i = 0; i < 64; ++i)
-            if (!EDGE || ch * 64 + i < cols) m = fmaxf(m, v[i]);
-    }
+    for (int i = 0; i < 128; ++i) top[i & 3] = fmaxf(top[i & 3], v[i]);
+    const float m = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
     const float ref = m == -INFINITY ? 0.f : m;   // all -inf: every term is exp(-inf)
     const float step = -c.zscale * kept_steps<F16>();
     float s[4] = {};
-#pragma unroll 1
+#pragma unroll
     for (int ch = 0; ch < 2; ++ch) {
-        tmem_ld64(w.tmem + ch * 64, v);
         if constexpr (P == kLogitsKeep) stage_reuse(w.lane);
 #pragma unroll
         for (int g = 0; g < 8; ++g) {
             unsigned code[4];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float d = v[g * 8 + i] - ref;
-                const float e = exp2_fast(d * c.zscale);
-                if (!EDGE || ch * 64 + g * 8 + i < cols) s[i & 3] += e;
+                const float d = v[ch * 64 + g * 8 + i] - ref;
+                s[i & 3] += exp2_fast(d * c.zscale);
                 if constexpr (P == kLogitsKeep) {
                     // 2^23 + x has x in its low bits; 65535 steps stand for themselves and more
                     const unsigned x = __float_as_uint(fminf(fmaf(d, step, 8388608.f), 8388608.f + 65535.f));
@@ -309,38 +312,35 @@ __device__ __forceinline__ void read_logits(const ProductArgs& p, const Patch& w
             if constexpr (P == kLogitsKeep) stage_word(w.staging, w.lane, g, code[0], code[1], code[2], code[3]);
         }
         if constexpr (P == kLogitsKeep)
-            if (!EDGE || ch * 64 < cols) stage_store(w.staging, w.lane, out, (int)(w.col0 - p.v0) + ch * 64, (int)w.row0);
+            if (ch * 64 < w.cols) stage_store(w.staging, w.lane, out, (int)(w.col0 - p.v0) + ch * 64, (int)w.row0);
     }
     if (row < n_valid) c.part[w.col0 / kVocabTile * c.n_pad + row] = make_float2(m * c.zscale, (s[0] + s[1]) + (s[2] + s[3]));
 }
 
-// Powers of two of the scaled logits relative to the row's reference.  One pass; what they are worth
-// comes with the log-sum-exp: e^T (hs) and (e w) take it as a factor of their rows.
-template <bool F16, bool EDGE>
-__device__ __forceinline__ void read_powers(const ProductArgs& p, const Patch& w, const CUtensorMap* out, int n_valid) {
+// Powers of two of the scaled logits relative to the row's reference.  What they are worth comes with the
+// log-sum-exp: e^T (hs) and (e w) take it as a factor of their rows.
+template <bool F16>
+__device__ __forceinline__ void read_powers(const ProductArgs& p, const Patch& w, const CUtensorMap* out, int n_valid, float (&v)[128]) {
     const VocabCall& c = p.c;
     const int64_t row = w.row0 + w.lane;
-    const int cols = (int)(w.cols < 128 ? w.cols : 128);
     const bool on = row < n_valid;
     const float ref = on ? c.row[row].ref : 0.f;
     float s[4] = {};
-#pragma unroll 1
+#pragma unroll
     for (int ch = 0; ch < 2; ++ch) {
-        if (EDGE && ch * 64 >= cols) break;
-        float v[64];
-        tmem_ld64(w.tmem + ch * 64, v);
+        if (ch * 64 >= w.cols) break;
         stage_reuse(w.lane);
 #pragma unroll
         for (int g = 0; g < 8; ++g) {
-            float e[8];
+            unsigned o[4];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                e[i] = exp2_fast(fmaf(v[g * 8 + i], c.zscale, -ref));
-                if (!EDGE || ch * 64 + g * 8 + i < cols) s[i & 3] += e[i];
+            for (int i = 0; i < 4; ++i) {
+                const float a = exp2_fast(fmaf(v[ch * 64 + g * 8 + 2 * i], c.zscale, -ref));
+                const float b = exp2_fast(fmaf(v[ch * 64 + g * 8 + 2 * i + 1], c.zscale, -ref));
+                s[i] += a + b;
+                o[i] = on ? pack16<F16>(a, b) : 0u;     // rows up to the padding are summed over by dw
             }
-            // rows up to the padding are summed over by dw
-            stage_word(w.staging, w.lane, g, on ? pack16<F16>(e[0], e[1]) : 0u, on ? pack16<F16>(e[2], e[3]) : 0u,
-                       on ? pack16<F16>(e[4], e[5]) : 0u, on ? pack16<F16>(e[6], e[7]) : 0u);
+            stage_word(w.staging, w.lane, g, o[0], o[1], o[2], o[3]);
         }
         stage_store(w.staging, w.lane, out, (int)(w.col0 - p.v0) + ch * 64, (int)w.row0);
     }
@@ -348,24 +348,22 @@ __device__ __forceinline__ void read_powers(const ProductArgs& p, const Patch& w
 }
 
 template <bool F16>
-__device__ __forceinline__ void read_gradients(const ProductArgs& p, const Patch& w, const CUtensorMap* out, int n_valid) {
+__device__ __forceinline__ void read_gradients(const ProductArgs& p, const Patch& w, const CUtensorMap* out, int n_valid, float (&v)[128]) {
     const VocabCall& c = p.c;
     const int64_t row = w.row0 + w.lane;
     VocabRow vr = {};
     if (row < n_valid) vr = c.row[row];
-#pragma unroll 1
+#pragma unroll
     for (int ch = 0; ch < 2; ++ch) {
         if (ch * 64 >= w.cols) break;
-        float v[64];
-        tmem_ld64(w.tmem + ch * 64, v);
         stage_reuse(w.lane);
 #pragma unroll
         for (int g = 0; g < 8; ++g) {
             unsigned o[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float a = vr.coef * exp2_fast(fmaf(v[g * 8 + 2 * i], c.zscale, -vr.lse2));
-                const float b = vr.coef * exp2_fast(fmaf(v[g * 8 + 2 * i + 1], c.zscale, -vr.lse2));
+                const float a = vr.coef * exp2_fast(fmaf(v[ch * 64 + g * 8 + 2 * i], c.zscale, -vr.lse2));
+                const float b = vr.coef * exp2_fast(fmaf(v[ch * 64 + g * 8 + 2 * i + 1], c.zscale, -vr.lse2));
                 o[i] = row < n_valid ? pack16<F16>(a, b) : 0u;    // rows up to the padding are summed over by dw
             }
             stage_word(w.staging, w.lane, g, o[0], o[1], o[2], o[3]);
@@ -375,46 +373,54 @@ __device__ __forceinline__ void read_gradients(const ProductArgs& p, const Patch
 }
 
 // A warp's 32 rows x 64 16-bit columns from its staging memory to rows on boundaries of VEC values, VEC a lane:
-// one row at a time by two values, two by four, four by eight (dw of 10000 x 1500, whose rows start on 8
-// bytes: 62 us for both gradients by two, 45 by four).  `to`: where the thread's own row has column 0 of
-// the 64, nullptr: nowhere.
+// one row at a time by two values, two by four, four by eight; four steps' loads go before their stores.
+// `to`: column 0 of the 64 in the result's row 0; `row`: the thread's own row there, -1: nowhere.
 template <int VEC>
-__device__ __forceinline__ void store_rows(uint32_t staging, int lane, uint16_t* to, int64_t cols) {
-    constexpr int kLanes = 64 / VEC, kRows = 32 / kLanes;
+__device__ __forceinline__ void store_rows(uint32_t staging, int lane, uint16_t* to, int64_t ld, int row, int64_t cols) {
+    constexpr int kLanes = 64 / VEC, kRows = 32 / kLanes, kSteps = 32 / kRows, kBatch = kSteps < 4 ? kSteps : 4;
     __syncwarp();
     const int col = lane % kLanes * VEC;
-#pragma unroll 4
-    for (int r0 = 0; r0 < 32; r0 += kRows) {
-        const int r = r0 + lane / kLanes;
-        uint16_t* at = (uint16_t*)__shfl_sync(0xffffffffu, (unsigned long long)to, r);
-        if (!at || col >= cols) continue;
-        const uint32_t from = staging + r * 128 + (((col >> 3) ^ (r & 7)) << 4) + (col & 7) * 2;
-        uint32_t x[4];
-        if constexpr (VEC == 2) asm volatile("ld.shared.b32 %0, [%1];" : "=r"(x[0]) : "r"(from) : "memory");
-        else if constexpr (VEC == 4) asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(x[0]), "=r"(x[1]) : "r"(from) : "memory");
-        else asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(from) : "memory");
-        at += col;
-        if (col + VEC <= cols && ((uintptr_t)at & (2 * VEC - 1)) == 0) {
-            if constexpr (VEC == 2) *(uint32_t*)at = x[0];
-            else if constexpr (VEC == 4) *(uint2*)at = make_uint2(x[0], x[1]);
-            else *(uint4*)at = make_uint4(x[0], x[1], x[2], x[3]);
-        } else {
+    const bool whole = col + VEC <= cols;
+#pragma unroll 1
+    for (int s0 = 0; s0 < kSteps; s0 += kBatch) {
+        uint32_t x[kBatch][4];
+        int at[kBatch];
 #pragma unroll
-            for (int i = 0; i < VEC; ++i)
-                if (col + i < cols) at[i] = (uint16_t)(x[i / 2] >> (i % 2 * 16));
+        for (int i = 0; i < kBatch; ++i) {
+            const int r = (s0 + i) * kRows + lane / kLanes;
+            at[i] = __shfl_sync(0xffffffffu, row, r);
+            const uint32_t from = staging + r * 128 + (((col >> 3) ^ (r & 7)) << 4) + (col & 7) * 2;
+            if constexpr (VEC == 2) asm volatile("ld.shared.b32 %0, [%1];" : "=r"(x[i][0]) : "r"(from) : "memory");
+            else if constexpr (VEC == 4) asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(x[i][0]), "=r"(x[i][1]) : "r"(from) : "memory");
+            else asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x[i][0]), "=r"(x[i][1]), "=r"(x[i][2]), "=r"(x[i][3]) : "r"(from) : "memory");
+        }
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            uint16_t* p = to + at[i] * ld + col;
+            if (at[i] < 0) continue;
+            if (whole && (VEC > 2 || ((uintptr_t)p & 3) == 0)) {
+                if constexpr (VEC == 2) *(uint32_t*)p = x[i][0];
+                else if constexpr (VEC == 4) *(uint2*)p = make_uint2(x[i][0], x[i][1]);
+                else *(uint4*)p = make_uint4(x[i][0], x[i][1], x[i][2], x[i][3]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e)
+                    if (col + e < cols) p[e] = (uint16_t)(x[i][e / 2] >> (e % 2 * 16));
+            }
         }
     }
     __syncwarp();
 }
 // `unit`: the boundary in values that all rows start on.
-__device__ __forceinline__ void store_rows(uint32_t staging, int lane, uint16_t* to, int64_t cols, int unit) {
-    if (unit >= 8) store_rows<8>(staging, lane, to, cols);
-    else if (unit >= 4) store_rows<4>(staging, lane, to, cols);
-    else store_rows<2>(staging, lane, to, cols);
+__device__ __forceinline__ void store_rows(uint32_t staging, int lane, uint16_t* to, int64_t ld, int row, int64_t cols, int unit) {
+    if (unit >= 8) store_rows<8>(staging, lane, to, ld, row, cols);
+    else if (unit >= 4) store_rows<4>(staging, lane, to, ld, row, cols);
+    else store_rows<2>(staging, lane, to, ld, row, cols);
 }
 
 template <bool F16>
-__device__ __forceinline__ void stage16(const Patch& w, const float (&v)[64], float f, bool empty) {
+__device__ __forceinline__ void stage16(const Patch& w, const float* v, float f, bool empty) {
+    stage_reuse(w.lane);
 #pragma unroll
     for (int g = 0; g < 8; ++g) {
         uint32_t x[4];
@@ -425,66 +431,55 @@ __device__ __forceinline__ void stage16(const Patch& w, const float (&v)[64], fl
 }
 
 template <bool F16>
-__device__ __forceinline__ void read_dw(const ProductArgs& p, const Patch& w, const CUtensorMap* out, bool empty) {
+__device__ __forceinline__ void read_dw(const ProductArgs& p, const Patch& w, const CUtensorMap* out, bool empty, float (&v)[128]) {
     const VocabCall& c = p.c;
     const float inv = c.ctl->inv_scale;
     const int64_t rows = p.v1 - p.v0 - w.row0;   // rows of the result from the warp's first on
     if (rows <= 0) return;
-#pragma unroll 1
+#pragma unroll
     for (int ch = 0; ch < 2; ++ch) {
         if (ch * 64 >= w.cols) break;
-        float v[64];
-        tmem_ld64(w.tmem + ch * 64, v);
-        stage_reuse(w.lane);
-        stage16<F16>(w, v, inv, empty);
+        stage16<F16>(w, v + ch * 64, inv, empty);
         if (p.wide) stage_store(w.staging, w.lane, out, (int)w.col0 + ch * 64, (int)w.row0);
-        else store_rows(w.staging, w.lane, w.lane < rows ? (uint16_t*)c.dw + (p.v0 + w.row0 + w.lane) * c.lddw + w.col0 + ch * 64 : nullptr,
+        else store_rows(w.staging, w.lane, (uint16_t*)c.dw + (p.v0 + w.row0) * c.lddw + w.col0 + ch * 64, c.lddw, w.lane < rows ? w.lane : -1,
                         w.cols - ch * 64, p.dw_unit);
     }
 }
 
 template <bool F16>
-__device__ __forceinline__ void read_dh(const ProductArgs& p, const Patch& w, const CUtensorMap* out, int n_valid, int split) {
+__device__ __forceinline__ void read_dh(const ProductArgs& p, const Patch& w, const CUtensorMap* out, int n_valid, int split, float (&v)[128]) {
     const VocabCall& c = p.c;
     if (w.row0 >= n_valid) return;
     const int64_t row = w.row0 + w.lane;
     if (p.direct) {
         float f = 0.f;
-        uint16_t* to = nullptr;
+        int to = -1;
         if (row < n_valid) {
             f = c.ctl->inv_scale * (c.powers ? powers_worth(c.row[row]) : 1.f);
-            to = (uint16_t*)c.dh + (int64_t)c.row_of[row] * c.lddh + w.col0;
+            to = c.row_of[row];
         }
-#pragma unroll 1
+#pragma unroll
         for (int ch = 0; ch < 2; ++ch) {
             if (ch * 64 >= w.cols) break;
-            float v[64];
-            tmem_ld64(w.tmem + ch * 64, v);
-            stage_reuse(w.lane);
-            stage16<F16>(w, v, f, false);
-            store_rows(w.staging, w.lane, to ? to + ch * 64 : nullptr, w.cols - ch * 64, p.dh_unit);
+            stage16<F16>(w, v + ch * 64, f, false);
+            store_rows(w.staging, w.lane, (uint16_t*)c.dh + w.col0 + ch * 64, c.lddh, to, w.cols - ch * 64, p.dh_unit);
         }
         return;
     }
     const int y = (int)(split * c.n_pad + w.row0);
-#pragma unroll 1
-    for (int ch = 0; ch < 2; ++ch) {
-        if (ch * 64 >= w.cols) break;
-        float v[64];
-        tmem_ld64(w.tmem + ch * 64, v);
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            stage_reuse(w.lane);
+    for (int part = 0; part < 4; ++part) {
+        if (part / 2 * 64 >= w.cols) break;
+        stage_reuse(w.lane);
 #pragma unroll
-            for (int g = 0; g < 8; ++g) {
-                const float* x = v + half * 32 + g * 4;
-                stage_word(w.staging, w.lane, g, __float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
-            }
-            const int x0 = (int)w.col0 + ch * 64 + half * 32;
-            // one tile adds to an element and launches follow one another: the order is fixed
-            if (p.first) stage_store(w.staging, w.lane, out, x0, y);
-            else stage_add(w.staging, w.lane, out, x0, y);
+        for (int g = 0; g < 8; ++g) {
+            const float* x = v + part * 32 + g * 4;
+            stage_word(w.staging, w.lane, g, __float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
         }
+        const int x0 = (int)w.col0 + part * 32;
+        // one tile adds to an element and launches follow one another: the order is fixed
+        if (p.first) stage_store(w.staging, w.lane, out, x0, y);
+        else stage_add(w.staging, w.lane, out, x0, y);
     }
 }
 
@@ -799,25 +794,32 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 // rows that are used: those that count, and for powers and gradients those that dw sums over
                 const bool used = P == kGrads || w.row0 < (P == kPowers || P == kAgain ? round_up(n_valid, 64) : n_valid);
+                float v[128];
                 if (w.cols > 0 && used) {
+                    __syncwarp();
+                    tmem_ld128(w.tmem, v);
                     if constexpr (kLogitUse)
                         if (c.t_idx && w.row0 < n_valid) take_pairs(c, w, n_valid);
-                    if constexpr (P == kLogits || P == kLogitsKeep) {
-                        if (w.cols >= 128) read_logits<P, F16, false>(p, w, &map_out, n_valid);
-                        else read_logits<P, F16, true>(p, w, &map_out, n_valid);
-                    } else if constexpr (P == kPowers) {
-                        if (w.cols >= 128) read_powers<F16, false>(p, w, &map_out, n_valid);
-                        else read_powers<F16, true>(p, w, &map_out, n_valid);
-                    } else if constexpr (P == kAgain) {
-                        read_gradients<F16>(p, w, &map_out, n_valid);
-                    } else {
-                        if (dw) read_dw<F16>(p, w, &map_out2, k0 == k1);
-                        else read_dh<F16>(p, w, &map_out, n_valid, split);
-                    }
                 }
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) mbar_arrive_remote(in_cta(smem_u32(&bar_free[h]), 0));
+                if (w.cols > 0 && used) {
+                    if (kLogitUse && w.cols < 128) {
+#pragma unroll
+                        for (int i = 0; i < 128; ++i) v[i] = i < w.cols ? v[i] : -INFINITY;
+                    }
+                    if constexpr (P == kLogits || P == kLogitsKeep) {
+                        read_logits<P, F16>(p, w, &map_out, n_valid, v);
+                    } else if constexpr (P == kPowers) {
+                        read_powers<F16>(p, w, &map_out, n_valid, v);
+                    } else if constexpr (P == kAgain) {
+                        read_gradients<F16>(p, w, &map_out, n_valid, v);
+                    } else {
+                        if (dw) read_dw<F16>(p, w, &map_out2, k0 == k1, v);
+                        else read_dh<F16>(p, w, &map_out, n_valid, split, v);
+                    }
+                }
             }
             if (p.narrow) only ^= 1;
         }
@@ -871,16 +873,17 @@ static int make_map(CUtensorMap* map, Element type, const void* base, int64_t co
 }
 
 // An estimate of a launch's time in us, for choosing between tiles and parts: what the busiest pair of
-// SMs sums, at 0.55 us a block of 64 of a wide tile and 0.29 us of a narrow one (5 % more per column: 4096 x
-// 4096 x 32000, logits, 713 against 749 us), 1 us a tile and 4 us to fill and empty.  The first kind
+// SMs sums, at 0.60 us a block of 64 of a wide tile and 0.37 us of a narrow one (as measured with all SMs
+// reading: 700 x 1500 x 10000), at least 3 us a half for its readout, 0.5 us a tile and 4 us to fill and empty.  The first kind
 // of tile (dh's, in `splits` parts) is dealt out before the second, which evens the shares out.
 struct Share { int64_t rows, cols, kb; };
 static double launch_time(const Share& first, int splits, const Share& second, bool narrow, int sm_count) {
     const int64_t width = narrow ? kHalfN : kTileN, most = sm_count / 2 > 0 ? sm_count / 2 : 1;
     const int64_t n1 = (first.rows + kTileM - 1) / kTileM * ((first.cols + width - 1) / width) * splits;
     const int64_t n2 = (second.rows + kTileM - 1) / kTileM * ((second.cols + width - 1) / width);
-    const double block = narrow ? 0.29 : 0.55;
-    const double t1 = (double)((first.kb + splits - 1) / splits) * block + 1.0, t2 = (double)second.kb * block + 1.0;
+    const double block = narrow ? 0.37 : 0.60, read = narrow ? 3.0 : 6.0;
+    auto tile = [&](int64_t kb) { const double us = (double)kb * block; return (us > read ? us : read) + 0.5; };
+    const double t1 = tile((first.kb + splits - 1) / splits), t2 = tile(second.kb);
     const double rounds1 = (double)((n1 + most - 1) / most), all = ((double)n1 * t1 + (double)n2 * t2) / (double)most;
     const double longest = rounds1 * t1, even = n2 ? all + 0.5 * t2 : 0.0;
     return (longest > even ? longest : even) + 4.0;
