@@ -660,12 +660,12 @@ static int vocab_workspace(size_t bytes, cudaStream_t st, VocabWorkspace** out) 
     return GK_OK;
 }
 
-static void size_call(VocabCall& c, bool want_dh, bool want_dw, int sm_count) {
+static void size_call(VocabCall& c, bool want_dh, DwRows dw, int sm_count) {
     c.n_pad = round_up(c.n, kVocabRowPad);
     c.Dp = round_up(c.D, 64);
-    c.vb = want_dh || want_dw ? piece_columns(c.n_pad, c.V) : 0;
+    c.vb = want_dh || dw != DwRows::none ? piece_columns(c.n_pad, c.V) : 0;
     c.powers = !c.f16 && c.vb > 0 && c.n * c.V >= kPowersFrom;
-    c.splits = want_dh ? vocab_dh_splits(c.n, c.D, c.vb < c.V ? c.vb : c.V, want_dw, sm_count) : 0;
+    c.splits = want_dh ? vocab_dh_splits(c.n, c.D, c.vb < c.V ? c.vb : c.V, dw, sm_count) : 0;
 }
 
 template <bool F16>
@@ -755,7 +755,8 @@ static int run_head(VocabCall& c, bool distill, cudaStream_t st) {
     if (rc != GK_OK) return rc;
     // rows that start and end on 16-byte boundaries are copied to shared memory as they lie
     const bool w_vec = (((uintptr_t)c.w | (uintptr_t)(2 * c.ldw) | (uintptr_t)(2 * c.D)) & 15) == 0;
-    size_call(c, c.dh != nullptr, c.dw != nullptr, ws->sm_count);
+    const bool dw_vec = (((uintptr_t)c.dw | (uintptr_t)(2 * c.lddw) | (uintptr_t)(2 * c.D)) & 15) == 0;
+    size_call(c, c.dh != nullptr, !c.dw ? DwRows::none : dw_vec ? DwRows::aligned : DwRows::unaligned, ws->sm_count);
     rc = vocab_workspace(lay_out(c, distill, !w_vec, nullptr), st, &ws);
     if (rc != GK_OK) return rc;
     lay_out(c, distill, !w_vec, (char*)ws->base);
@@ -815,8 +816,13 @@ extern "C" int gk_vocab_set_budget(int64_t bytes) {
 // gradients (or no gradient), over rows of w on any boundary.
 static size_t largest(VocabCall& c, int64_t n, int64_t D, int64_t V, int32_t K, int grad, int sms) {
     c.n = n; c.D = D; c.V = V; c.K = K;
-    size_call(c, grad != 0, grad != 0, sms);
-    return lay_out(c, true, D % 8 != 0, nullptr);
+    size_t most = 0;
+    for (DwRows dw : {DwRows::none, DwRows::aligned, DwRows::unaligned}) {     // dh is split by what it shares the SMs with
+        size_call(c, grad != 0, grad ? dw : DwRows::none, sms);
+        const size_t bytes = lay_out(c, true, D % 8 != 0, nullptr);
+        most = bytes > most ? bytes : most;
+    }
+    return most;
 }
 
 static int head_sizes_ok(int64_t n, int64_t D, int64_t V, int32_t K) {

@@ -106,7 +106,8 @@ int launch_vocab_again(const VocabCall& c, int64_t v0, int64_t v1, int sm_count,
 // dw rows [v0, v1) = e^T hs / scale, and dh = e w[v0:v1] times each row's factor, or its sums in fp32 in
 // `splits` parts added to dhp (first: overwritten).
 int launch_vocab_grads(const VocabCall& c, int64_t v0, int64_t v1, bool first, int sm_count, cudaStream_t st);
-int vocab_dh_splits(int64_t n, int64_t D, int64_t vb, bool dw, int sm_count);
+enum class DwRows { none, aligned, unaligned };     // dw's rows start and end on 16-byte boundaries, or not
+int vocab_dh_splits(int64_t n, int64_t D, int64_t vb, DwRows dw, int sm_count);
 
 #ifdef __CUDACC__
 

@@ -872,18 +872,27 @@ static int make_map(CUtensorMap* map, Element type, const void* base, int64_t co
     return r == CUDA_SUCCESS ? GK_OK : cuda_fail(cudaErrorInvalidValue);
 }
 
-// An estimate of a launch's time in us, for choosing between tiles and parts: what the busiest pair of
-// SMs sums, at 0.60 us a block of 64 of a wide tile and 0.37 us of a narrow one (as measured with all SMs
-// reading: 700 x 1500 x 10000), at least 3 us a half for its readout, 0.5 us a tile and 4 us to fill and empty.  The first kind
-// of tile (dh's, in `splits` parts) is dealt out before the second, which evens the shares out.
-struct Share { int64_t rows, cols, kb; };
+// An estimate of a launch's time in us, for choosing between tiles and parts: what the busiest pair of SMs does,
+// and 4 us to fill and empty.  A tile takes its blocks of 64 or its readout, whichever is longer, and what of
+// them does not overlap.  As measured: a block 0.60 us in a wide tile, 0.31 (logits) and 0.34 (gradients) in a
+// narrow one; a readout 6 and 3.4 us, by rows that do not start on 16 bytes 10 and 5.  Wide over narrow tiles: logits
+// 8192 x 4096 x 128000 6110 : 6360 us, 1024 x 1024 x 32000 76 : 67; both gradients 20160 : 22950 and 216 : 215 in all; 300 x
+// 512 x 20000 75 : 63 in all.  The first kind of tile (dh's, in `splits` parts) is dealt out before the second (dw's),
+// which evens the shares out.
+struct Share {
+    int64_t rows, cols, kb;
+    bool unaligned;
+};
 static double launch_time(const Share& first, int splits, const Share& second, bool narrow, int sm_count) {
     const int64_t width = narrow ? kHalfN : kTileN, most = sm_count / 2 > 0 ? sm_count / 2 : 1;
     const int64_t n1 = (first.rows + kTileM - 1) / kTileM * ((first.cols + width - 1) / width) * splits;
     const int64_t n2 = (second.rows + kTileM - 1) / kTileM * ((second.cols + width - 1) / width);
-    const double block = narrow ? 0.37 : 0.60, read = narrow ? 3.0 : 6.0;
-    auto tile = [&](int64_t kb) { const double us = (double)kb * block; return (us > read ? us : read) + 0.5; };
-    const double t1 = tile((first.kb + splits - 1) / splits), t2 = tile(second.kb);
+    auto tile = [&](int64_t kb, bool unaligned) {
+        const double us = (double)kb * (narrow ? (second.rows ? 0.34 : 0.31) : 0.60);
+        const double read = unaligned ? (narrow ? 5.0 : 10.0) : narrow ? 3.4 : 6.0;
+        return (us > read ? us : read) + (narrow ? 0.5 : 1.5);
+    };
+    const double t1 = tile((first.kb + splits - 1) / splits, first.unaligned), t2 = tile(second.kb, second.unaligned);
     const double rounds1 = (double)((n1 + most - 1) / most), all = ((double)n1 * t1 + (double)n2 * t2) / (double)most;
     const double longest = rounds1 * t1, even = n2 ? all + 0.5 * t2 : 0.0;
     return (longest > even ? longest : even) + 4.0;
@@ -896,7 +905,7 @@ static int launch_product(ProductArgs p, int sm_count, cudaStream_t st) {
     const int64_t ldw = c.wc ? c.Dp : c.ldw, nv = p.v1 - p.v0;
     const Element type = F16 ? kF16 : kBf16;
     CUtensorMap a, b, out, a2, b2, out2;
-    Share first, second = {0, 1, 1};
+    Share first, second = {0, 1, 1, false};
     int rc;
     if (P == kGrads) {
         rc = make_map(&a, type, c.e, nv, c.n_pad, c.vb, 128);
@@ -907,15 +916,15 @@ static int launch_product(ProductArgs p, int sm_count, cudaStream_t st) {
         if (rc == GK_OK) rc = make_map(&b2, type, c.hs, c.Dp, c.n_pad, c.Dp, 64);
         out2 = a2;   // rows on other boundaries are stored without a map
         if (rc == GK_OK && c.dw && p.wide) rc = make_map(&out2, type, (const uint16_t*)c.dw + p.v0 * c.lddw, c.D, nv, c.lddw, 32);
-        first = {c.dh ? c.n : 0, c.D, (nv + kBlockK - 1) / kBlockK};
-        second = {c.dw ? nv : 0, c.D, (c.n + kBlockK - 1) / kBlockK};
+        first = {c.dh ? c.n : 0, c.D, (nv + kBlockK - 1) / kBlockK, false};
+        second = {c.dw ? nv : 0, c.D, (c.n + kBlockK - 1) / kBlockK, !p.wide};
     } else {
         rc = make_map(&a, type, c.hc, c.Dp, c.n_pad, c.Dp, 128);
         if (rc == GK_OK) rc = make_map(&b, type, w, c.D, c.V, ldw, 128);
         out = a;     // kLogits keeps nothing
         if (rc == GK_OK && P != kLogits) rc = make_map(&out, type, c.e, nv, c.n_pad, c.vb, 32);
         a2 = b2 = out2 = a;
-        first = {c.n, nv, (c.D + kBlockK - 1) / kBlockK};
+        first = {c.n, nv, (c.D + kBlockK - 1) / kBlockK, false};
     }
     if (rc != GK_OK) return rc;
     p.narrow = launch_time(first, p.splits, second, true, sm_count) < launch_time(first, p.splits, second, false, sm_count);
@@ -974,8 +983,9 @@ int launch_vocab_grads(const VocabCall& c, int64_t v0, int64_t v1, bool first, i
 // Into how many parts the summed axis of dh is split.  dh has few tiles (rows / 256 x D / 512) and a
 // long sum, so without parts most pairs of SMs would idle; parts cost a write and a read of fp32 sums,
 // taken at 5 TB/s, and a launch that adds them.
-int vocab_dh_splits(int64_t n, int64_t D, int64_t vb, bool dw, int sm_count) {
-    const Share first = {n, D, (vb + kBlockK - 1) / kBlockK}, second = {dw ? vb : 0, D, (n + kBlockK - 1) / kBlockK};
+int vocab_dh_splits(int64_t n, int64_t D, int64_t vb, DwRows dw, int sm_count) {
+    const Share first = {n, D, (vb + kBlockK - 1) / kBlockK, false};
+    const Share second = {dw == DwRows::none ? 0 : vb, D, (n + kBlockK - 1) / kBlockK, dw == DwRows::unaligned};
     int best = 1;
     double least = 0;
     for (int s = 1; s <= 32 && (s == 1 || s * 4 <= first.kb); ++s) {
