@@ -13,8 +13,8 @@
 // the second half catches up, and again at the start of the next tile, while the second half is
 // read out.  Eight warps read out: four for the lanes, two for the columns of a half.
 //
-// Where 256 x 256 tiles fill the SMs better (few tiles, or a bad last round) they are used instead, six
-// blocks of 32 KB in flight, one half of the tensor memory summing while the other is read out.
+// Logits, and gradients where they fill the SMs better, are 256 x 256 tiles: six blocks of 32 KB in flight, one half
+// of the tensor memory summing while the other is read out.
 //
 //   use          A (M x K)            B (N x K)            what the readout does
 //   kLogits      hc  rows x D         w   columns x D      maximum and sum of 128 columns per row
@@ -45,6 +45,9 @@ constexpr int kTileM = 256, kHalfN = 256, kTileN = 2 * kHalfN, kBlockK = 64;
 constexpr int kOperandBytes = 128 * kBlockK * 2;            // a CTA's share of A, or of a half of B, in a block
 constexpr int kBlockBytes = 12 * kOperandBytes;             // four blocks of a wide tile, six of a narrow one
 constexpr int kMaxStages = 6;
+// Logits are summed over 12 blocks (768 of D) at a time in tensor memory, whose sums are cut, not rounded, and
+// added up in fp32 registers: over 4096 at once they were low by 3.4e-6 of themselves, log-sum-exps with them.
+constexpr int kChunk = 12;
 constexpr int kReaders = 8;                                 // warps that read the sums out
 constexpr int kStagingBytes = 32 * 128;                     // of each of them
 constexpr int kProductSmem = kBlockBytes + kReaders * kStagingBytes + 1024;   // and the alignment of the first block
@@ -139,11 +142,14 @@ __device__ __forceinline__ void commit_pair(uint32_t bar) {
         "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
         ::"r"(bar), "h"((uint16_t)3) : "memory");
 }
-// One column, or 128, of this thread's lane.  All lanes of the warp take part, whatever rows they have.
-__device__ __forceinline__ float tmem_ld1(uint32_t addr) {
-    uint32_t r;
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];\ntcgen05.wait::ld.sync.aligned;" : "=r"(r) : "r"(addr) : "memory");
-    return __uint_as_float(r);
+// 16 or 128 columns of this thread's lane.  All lanes of the warp take part, whatever rows they have.
+__device__ __forceinline__ void tmem_ld16(uint32_t addr, float (&v)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]),
+          "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
+        : "r"(addr) : "memory");
 }
 __device__ __forceinline__ void tmem_ld128(uint32_t addr, float (&v)[128]) {
     asm volatile(
@@ -240,8 +246,8 @@ struct Patch {
 };
 
 // A row's teacher pairs in ascending order are met one patch of columns at a time: the logit at each is
-// taken from tensor memory as it is summed there, instead of by a dot product of its own.
-// first_pair runs while the patch is still being summed.
+// taken as it passes, instead of by a dot product of its own.  first_pair runs while the patch is still being
+// summed.
 __device__ __forceinline__ int pair_index(const VocabCall& c, const int32_t* pairs, int j) {
     const int32_t i = j < c.K ? __ldg(pairs + j) : -1;
     return i < 0 || i >= c.V ? 0x7fffffff : i;     // pairs left out are at the end of an ascending row
@@ -259,22 +265,35 @@ __device__ __forceinline__ int first_pair(const VocabCall& c, int64_t row, int n
     }
     return lo;
 }
-__device__ __forceinline__ void take_pairs(const VocabCall& c, const Patch& w, int n_valid) {
+// `v`: the patch's columns; a register cannot be chosen at run time, so stretches of 32 columns with a pair in
+// any of the warp's rows go through the staging memory.
+__device__ __forceinline__ void take_pairs(const VocabCall& c, const Patch& w, int n_valid, const float (&v)[128]) {
     const int64_t row = w.row0 + w.lane;
     const int32_t* pairs = row < n_valid ? c.t_idx + (int64_t)c.row_of[row] * c.K : nullptr;
-    const int end = (int)(w.col0 + (w.cols < 128 ? w.cols : 128));
     int j = w.cursor;
     int next = j < c.K ? pair_index(c, pairs, j) : 0x7fffffff;
-    unsigned lanes;
-    while ((lanes = __ballot_sync(0xffffffffu, next < end)) != 0) {
-        const int col = __shfl_sync(0xffffffffu, next, __ffs(lanes) - 1);
-        const float z = tmem_ld1(w.tmem + (uint32_t)(col - (int)w.col0));
-        if (next == col) {
-            c.zt[row * c.K + j] = z;
-            ++j;
-            next = j < c.K ? pair_index(c, pairs, j) : 0x7fffffff;
+#pragma unroll
+    for (int part = 0; part < 4; ++part) {
+        const int from = (int)w.col0 + part * 32;
+        const int end = from + (int)(w.cols - part * 32 < 32 ? w.cols - part * 32 : 32);
+        if (__any_sync(0xffffffffu, next < end)) {
+            stage_reuse(w.lane);
+#pragma unroll
+            for (int g = 0; g < 8; ++g) {
+                const float* x = v + part * 32 + g * 4;
+                stage_word(w.staging, w.lane, g, __float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+            }
+            while (next < end) {         // a row's own values: nothing to wait for
+                const int col = next - from;
+                float z;
+                asm volatile("ld.shared.f32 %0, [%1];"
+                             : "=f"(z) : "r"(w.staging + w.lane * 128 + (((col >> 2) ^ (w.lane & 7)) << 4) + (col & 3) * 4) : "memory");
+                c.zt[row * c.K + j] = z;
+                ++j;
+                next = j < c.K ? pair_index(c, pairs, j) : 0x7fffffff;
+            }
+            __syncwarp();
         }
-        __syncwarp();
     }
 }
 
@@ -577,9 +596,10 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     const uint32_t rank = cluster_rank();
     const uint32_t stage0 = (smem_u32(smem_raw) + 1023u) & ~1023u, staging0 = stage0 + kBlockBytes;
     const VocabCall& c = p.c;
-    const int width = p.narrow ? kHalfN : kTileN;
-    const int stages = p.narrow ? 6 : 4;
-    const uint32_t stage_bytes = (p.narrow ? 2 : 3) * kOperandBytes;
+    const bool narrow = P != kGrads || p.narrow;
+    const int width = narrow ? kHalfN : kTileN;
+    const int stages = narrow ? 6 : 4;
+    const uint32_t stage_bytes = (narrow ? 2 : 3) * kOperandBytes;
     const int cluster = (int)(blockIdx.x >> 1), clusters = (int)(gridDim.x >> 1);
 
     if (tid == 32) {       // the descriptors are on their way while the rest is set up
@@ -632,7 +652,7 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
             if (P != kGrads) dw = false;
             (dw ? tiles2 : tiles).at(t, m, n, split);
             (dw ? tiles2 : tiles).blocks(split, k0, k1);
-            const bool two = !p.narrow && n * kTileN + kHalfN < n_cols;
+            const bool two = !narrow && n * kTileN + kHalfN < n_cols;
             const int ma = (int)(m * kTileM + rank * 128), nb = (int)(n * width + rank * 128);
             const uint32_t bytes = 2 * (two ? 3 : 2) * kOperandBytes;
             for (int k = k0; k < k1; ++k) {
@@ -661,7 +681,6 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                     } else {
                         tma_load(a, &map_a, k * kBlockK, ma, bar);
                         tma_load(b, &map_b, k * kBlockK, (int)p.v0 + nb, bar);
-                        if (two) tma_load(b + kOperandBytes, &map_b, k * kBlockK, (int)p.v0 + nb + kHalfN, bar);
                     }
                 }
                 __syncwarp();
@@ -681,7 +700,7 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
             // one block of one half, by the elected lane
             auto issue = [&](int stage, int half, bool fresh) {
                 const uint32_t at = stage * (stage_bytes / 16);
-                const uint32_t a = a0 + at, b = b0 + at + (p.narrow ? 0 : half * (kOperandBytes / 16));
+                const uint32_t a = a0 + at, b = b0 + at + (narrow ? 0 : half * (kOperandBytes / 16));
                 const uint32_t d = tmem + half * kHalfN;
                 mma_pair(d, a, b, kOperandHi, idesc, !fresh);
 #pragma unroll
@@ -698,13 +717,14 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                 (dw ? tiles2 : tiles).at(t, m, n, split);
                 (dw ? tiles2 : tiles).blocks(split, k0, k1);
                 const int blocks = k1 - k0;
-                const bool two = !p.narrow && n * kTileN + kHalfN < n_cols;
+                const bool two = !narrow && n * kTileN + kHalfN < n_cols;
                 if (dw) {
                     idesc = kDesc | 1u << 15;
                     step_a = 2048 / 16;
                     a0 = operand_lo<true>(stage0);
                 }
                 int a = 0, b = 0;             // blocks issued for each half
+                int count = blocks;           // of a chunk
                 auto first_half = [&](int half, bool release) {
                     ok = warp_wait(smem_u32(&bar_full[stage_a]), phase);
                     if (!ok) return;
@@ -712,7 +732,7 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                     if (elected()) {
                         issue(stage_a, half, a == 0);
                         if (release) commit_pair(smem_u32(&bar_empty[stage_a]));
-                        if (a + 1 == blocks) commit_pair(smem_u32(&bar_sum[half]));
+                        if (a + 1 == count) commit_pair(smem_u32(&bar_sum[half]));
                     }
                     __syncwarp();
                     ++a;
@@ -729,26 +749,34 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                     if (++stage_b == stages) stage_b = 0;
                 };
                 // the first half's sums, or a narrow tile's, have been read out
-                if (!(ok = warp_wait(smem_u32(&bar_free[only]), (only ? free1 : free0) ^ 1))) break;
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                if (only) free1 ^= 1;
-                else free0 ^= 1;
-                if (blocks == 0 && elected()) commit_pair(smem_u32(&bar_sum[only]));
-                __syncwarp();
+                auto wait_free = [&](int half) {
+                    ok = warp_wait(smem_u32(&bar_free[half]), (half ? free1 : free0) ^ 1);
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    if (half) free1 ^= 1;
+                    else free0 ^= 1;
+                    if (ok && blocks == 0 && elected()) commit_pair(smem_u32(&bar_sum[half]));
+                    __syncwarp();
+                };
                 if (!two) {
-                    while (a < blocks && ok) first_half(only, true);
+                    int left = blocks;
+                    do {
+                        wait_free(only);
+                        count = P == kGrads || left < kChunk ? left : kChunk;
+                        a = 0;
+                        while (a < count && ok) first_half(only, true);
+                        left -= count;
+                        if (narrow) only ^= 1;
+                    } while (ok && left > 0);
                     stage_b = stage_a;
-                    if (p.narrow) only ^= 1;
                     continue;
                 }
+                wait_free(0);
+                if (!ok) break;
                 // ahead, as far as blocks are in flight, while the second half's sums are still being read out
                 while (ok && a < blocks && a < stages && !__all_sync(0xffffffffu, mbar_test(smem_u32(&bar_free[1]), free1 ^ 1)))
                     first_half(0, false);
-                if (!ok || !(ok = warp_wait(smem_u32(&bar_free[1]), free1 ^ 1))) break;
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                free1 ^= 1;
-                if (blocks == 0 && elected()) commit_pair(smem_u32(&bar_sum[1]));
-                __syncwarp();
+                if (ok) wait_free(1);
+                if (!ok) break;
                 while (b < a && a < blocks) second_half();
                 while (ok && a < blocks - stages) {
                     first_half(0, false);
@@ -777,51 +805,77 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
             if (P != kGrads) dw = false;
             (dw ? tiles2 : tiles).at(t, m, n, split);
             (dw ? tiles2 : tiles).blocks(split, k0, k1);
-            const bool two = !p.narrow && n * kTileN + kHalfN < n_cols;
+            const bool two = !narrow && n * kTileN + kHalfN < n_cols;
             w.row0 = m * kTileM + (int)rank * 128 + quarter * 32;
-#pragma unroll 1
-            for (int h = only; h < (two ? 2 : only + 1); ++h) {
-                const int64_t col = n * width + (two ? h * kHalfN : 0) + side * 128;
-                w.tmem = tmem + h * kHalfN + side * 128 + ((uint32_t)(quarter * 32) << 16);
-                w.cols = n_cols - col;
-                w.col0 = (P == kGrads ? 0 : p.v0) + col;
-                constexpr bool kLogitUse = P == kLogits || P == kLogitsKeep || P == kPowers;
-                if constexpr (kLogitUse)
-                    if (c.t_idx && w.cols > 0 && w.row0 < n_valid) w.cursor = first_pair(c, w.row0 + lane, n_valid, w.col0);
+            // rows that are used: those that count, and for powers and gradients those that dw sums over
+            const bool used_rows = P == kGrads || w.row0 < (P == kPowers || P == kAgain ? round_up(n_valid, 64) : n_valid);
+            const uint32_t lanes = tmem + side * 128 + ((uint32_t)(quarter * 32) << 16);
+            float v[128];
+            auto wait_sums = [&](int h) {
                 ok = warp_wait(smem_u32(&bar_sum[h]), phases >> h & 1);
-                if (!ok) break;
                 phases ^= 1u << h;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                // rows that are used: those that count, and for powers and gradients those that dw sums over
-                const bool used = P == kGrads || w.row0 < (P == kPowers || P == kAgain ? round_up(n_valid, 64) : n_valid);
-                float v[128];
-                if (w.cols > 0 && used) {
-                    __syncwarp();
-                    tmem_ld128(w.tmem, v);
-                    if constexpr (kLogitUse)
-                        if (c.t_idx && w.row0 < n_valid) take_pairs(c, w, n_valid);
-                }
+            };
+            auto give_back = [&](int h) {
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) mbar_arrive_remote(in_cta(smem_u32(&bar_free[h]), 0));
-                if (w.cols > 0 && used) {
-                    if (kLogitUse && w.cols < 128) {
+            };
+            if constexpr (P != kGrads) {
+                const int64_t col = (int64_t)n * width + side * 128;
+                w.cols = n_cols - col;
+                w.col0 = p.v0 + col;
+                const bool used = used_rows && w.cols > 0, pairs = P != kAgain && c.t_idx && used && w.row0 < n_valid;
+                if (pairs) w.cursor = first_pair(c, w.row0 + lane, n_valid, w.col0);
+                for (int done = 0; done < k1 - k0; done += kChunk) {
+                    wait_sums(only);
+                    if (!ok) break;
+                    w.tmem = lanes + only * kHalfN;
+                    if (used) {
+                        __syncwarp();
+                        if (done == 0) {
+                            tmem_ld128(w.tmem, v);
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) {
+                                float x[16];
+                                tmem_ld16(w.tmem + i * 16, x);
+#pragma unroll
+                                for (int j = 0; j < 16; ++j) v[i * 16 + j] += x[j];
+                            }
+                        }
+                    }
+                    give_back(only);
+                    only ^= 1;
+                }
+                if (!ok) break;
+                if (pairs) take_pairs(c, w, n_valid, v);
+                if (used) {
+                    if (P != kAgain && w.cols < 128) {
 #pragma unroll
                         for (int i = 0; i < 128; ++i) v[i] = i < w.cols ? v[i] : -INFINITY;
                     }
-                    if constexpr (P == kLogits || P == kLogitsKeep) {
-                        read_logits<P, F16>(p, w, &map_out, n_valid, v);
-                    } else if constexpr (P == kPowers) {
-                        read_powers<F16>(p, w, &map_out, n_valid, v);
-                    } else if constexpr (P == kAgain) {
-                        read_gradients<F16>(p, w, &map_out, n_valid, v);
-                    } else {
+                    if constexpr (P == kLogits || P == kLogitsKeep) read_logits<P, F16>(p, w, &map_out, n_valid, v);
+                    else if constexpr (P == kPowers) read_powers<F16>(p, w, &map_out, n_valid, v);
+                    else read_gradients<F16>(p, w, &map_out, n_valid, v);
+                }
+            } else {
+#pragma unroll 1
+                for (int h = only; h < (two ? 2 : only + 1); ++h) {
+                    w.col0 = (int64_t)n * width + (two ? h * kHalfN : 0) + side * 128;
+                    w.cols = n_cols - w.col0;
+                    wait_sums(h);
+                    if (!ok) break;
+                    __syncwarp();
+                    tmem_ld128(lanes + h * kHalfN, v);
+                    give_back(h);
+                    if (w.cols > 0) {
                         if (dw) read_dw<F16>(p, w, &map_out2, k0 == k1, v);
                         else read_dh<F16>(p, w, &map_out, n_valid, split, v);
                     }
                 }
+                if (narrow) only ^= 1;
             }
-            if (p.narrow) only ^= 1;
         }
         if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
@@ -874,10 +928,9 @@ static int make_map(CUtensorMap* map, Element type, const void* base, int64_t co
 
 // An estimate of a launch's time in us, for choosing between tiles and parts: what the busiest pair of SMs does,
 // and 4 us to fill and empty.  A tile takes its blocks of 64 or its readout, whichever is longer, and what of
-// them does not overlap.  As measured: a block 0.60 us in a wide tile, 0.31 (logits) and 0.34 (gradients) in a
-// narrow one; a readout 6 and 3.4 us, by rows that do not start on 16 bytes 10 and 5.  Wide over narrow tiles: logits
-// 8192 x 4096 x 128000 6110 : 6360 us, 1024 x 1024 x 32000 76 : 67; both gradients 20160 : 22950 and 216 : 215 in all; 300 x
-// 512 x 20000 75 : 63 in all.  The first kind of tile (dh's, in `splits` parts) is dealt out before the second (dw's),
+// them does not overlap.  As measured: a block 0.60 us in a wide tile, 0.34 in a
+// narrow one; a readout 6 and 3.4 us, by rows that do not start on 16 bytes 10 and 5.  Whole calls with wide and with
+// narrow tiles for the gradients: 8192 x 4096 x 128000 20160 : 22950 us, 1024 x 1024 x 32000 216 : 215, 300 x 512 x 20000 75 : 63.  The first kind of tile (dh's, in `splits` parts) is dealt out before the second (dw's),
 // which evens the shares out.
 struct Share {
     int64_t rows, cols, kb;
@@ -888,7 +941,7 @@ static double launch_time(const Share& first, int splits, const Share& second, b
     const int64_t n1 = (first.rows + kTileM - 1) / kTileM * ((first.cols + width - 1) / width) * splits;
     const int64_t n2 = (second.rows + kTileM - 1) / kTileM * ((second.cols + width - 1) / width);
     auto tile = [&](int64_t kb, bool unaligned) {
-        const double us = (double)kb * (narrow ? (second.rows ? 0.34 : 0.31) : 0.60);
+        const double us = (double)kb * (narrow ? 0.34 : 0.60);
         const double read = unaligned ? (narrow ? 5.0 : 10.0) : narrow ? 3.4 : 6.0;
         return (us > read ? us : read) + (narrow ? 0.5 : 1.5);
     };
@@ -927,7 +980,7 @@ static int launch_product(ProductArgs p, int sm_count, cudaStream_t st) {
         first = {c.n, nv, (c.D + kBlockK - 1) / kBlockK, false};
     }
     if (rc != GK_OK) return rc;
-    p.narrow = launch_time(first, p.splits, second, true, sm_count) < launch_time(first, p.splits, second, false, sm_count);
+    p.narrow = P != kGrads || launch_time(first, p.splits, second, true, sm_count) < launch_time(first, p.splits, second, false, sm_count);
     const int64_t width = p.narrow ? kHalfN : kTileN;
     const int64_t pairs = (first.rows + kTileM - 1) / kTileM * ((first.cols + width - 1) / width) * p.splits +
                           (second.rows + kTileM - 1) / kTileM * ((second.cols + width - 1) / width);
