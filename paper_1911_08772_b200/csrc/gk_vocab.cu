@@ -15,23 +15,19 @@
 //      piece of the vocabulary (all of it where the budget allows) something of each logit in 16 bits;
 //      (distill) the logits at the teacher's pairs as they pass;
 //   4. the row's log-sum-exp from the tiles, loss;
-//   5. per piece: the operand of the gradients in 16 bits (from what was kept, or from the product
-//      taken again), then dw and dh as products with it.
+//   5. per piece: the logit gradients in 16 bits (from what was kept, or from the product taken again),
+//      then dw and dh as products with them.
 // Kept between the steps is one piece, whose size the budget bounds whatever n and V are.
 //
-// What is kept of a logit.  Large bf16 calls keep powers: exp(z_nv / T - r_n), where r_n, the row's
-// reference, is its logit at the target.  As dz_nv = c_n (exp(z_nv / T - r_n) - ...) with
-// c_n = (g_n Q_n / T) exp(r_n - lse_n), they are the operand itself: c_n scales the rows of h before
-// dw and those of dh after it, and no pass over n x V values lies between the products (8192 x 128000: 0.8 of
-// 20 ms).  bf16 has fp32's exponents, so a reference may be 2^100 below the sum (a loss of 69) and nothing
-// overflows; where it is further below, the step is done again with the log-sum-exp itself as the
-// reference.
-// fp16 has no such exponents, and small calls would notice the kernels that look for overflow: they
-// keep a logit's distance from the largest of its 128 columns in fixed point, for bf16 in steps of 2^-9 in
-// the exponent of two: the exponential it stands for is then off by at most 2^-10 log 2 = 6.8e-4 of itself, where
-// a bf16 exponential is off by up to 2^-9 = 2.0e-3, and a logit of 16 by 3e-2; the 65536 steps reach 2^-128, as
-// bf16 itself does.  For fp16 the steps are 2^-11 (1.7e-4, against 4.9e-4) and reach 2^-32, where fp16
-// gradients have ended.  A pass over them makes the logit gradients.
+// What is kept of a logit is its distance from the largest of its 128 columns in fixed point.  For bf16 in steps
+// of 2^-9 in the exponent of two: the exponential it stands for is then off by at most 2^-10 log 2 = 6.8e-4 of
+// itself, where a bf16 exponential is off by up to 2^-9 = 2.0e-3, and a logit of 16 by 3e-2; the 65536 codes reach
+// 2^-128, as bf16 itself does.  For fp16 the steps are 2^-12 (8.5e-5, against 4.9e-4) down to 2^-8 of the largest,
+// and coarser to 2^-32, where fp16 gradients have ended.  A pass over them makes the logit gradients: the one
+// rounding to the operands' type that the products dw and dh need.  (Exponentials relative to a reference known
+// beforehand, the logit at the target, could be the operand themselves, with the rows of h scaled for dw instead:
+// that saved the pass, 5 to 7 % of a call, but rounds once more, and dw was off by 1.7 times what an exact dw
+// rounded to bf16 is off by, where it now is by 1.3 times.)
 #include <atomic>
 #include <map>
 #include <mutex>
@@ -69,22 +65,19 @@ __global__ void __launch_bounds__(256) k_vocab_teacher(VocabCall c) {
     // value do not overflow; with the teacher's own log-sum-exp there is nothing to take off
     float top = -INFINITY;
     bool any = false, ascending = true;
-    int largest = 0;
     for (int j = lane; j < c.K; j += 32) {
         const int32_t i = ti[j], before = j > 0 ? ti[j - 1] : -1;
         const float t = tv[j];
         const bool in = i >= 0 && i < c.V;
         if (in && t != -INFINITY) {
             any = true;
-            if (t > top) { top = t; largest = j; }
+            top = fmaxf(top, t);
         }
         if (in && j > 0 && (before >= i || before < 0)) ascending = false;
     }
     any = __any_sync(0xffffffffu, any);
     ascending = __all_sync(0xffffffffu, ascending);
     const float most = warp_max_f(top);
-    const unsigned holds = __ballot_sync(0xffffffffu, top == most);
-    largest = __shfl_sync(0xffffffffu, largest, holds ? __ffs(holds) - 1 : 0);
     float L;
     if (c.t_lse) {
         L = c.t_lse[r];
@@ -104,7 +97,7 @@ __global__ void __launch_bounds__(256) k_vocab_teacher(VocabCall c) {
         Q += q;
     }
     Q = warp_sum_f(Q);
-    if (lane == 0) c.teacher[r] = make_float4(Q, L, top, (float)((ascending ? 1 : 0) + (any ? 2 : 0) + 4 * largest));
+    if (lane == 0) c.teacher[r] = make_float4(Q, L, top, (float)((ascending ? 1 : 0) + (any ? 2 : 0)));
 }
 
 // ---------------------------------------------------------------------------
@@ -142,7 +135,6 @@ __device__ __forceinline__ void write_ctl(const VocabCall& c, int n_valid, float
     e = min(max((c.f16 ? 11 : 1) - e, -100), 100);
     c.ctl->n_valid = n_valid;
     c.ctl->status = 0;
-    c.ctl->missed = 0;
     c.ctl->scale = ldexpf(1.f, e);
     c.ctl->inv_scale = ldexpf(1.f, -e);
 }
@@ -319,16 +311,14 @@ __global__ void __launch_bounds__(128) k_vocab_gather(VocabCall c) {
     }
     const uint16_t* from = (const uint16_t*)c.h + r * c.ldh;
     for (int64_t i = tid; i < c.Dp / 8; i += 128) ((uint4*)to)[i] = load8(from + i * 8, c.D - i * 8);
-    int first = 0, last = 1;
+    int last = 1;
     if (!c.target) {
         const float4 te = c.teacher[r];
-        first = teacher_largest(te);
-        last = c.powers ? first + 1 : first;
-        if (!teacher_ascending(te)) { first = 0; last = c.K; }
+        last = teacher_ascending(te) ? 0 : c.K;
     }
     __syncthreads();
     const int64_t words = (c.D + 7) / 8;
-    for (int j = first + (tid >> 5); j < last; j += 4) {
+    for (int j = tid >> 5; j < last; j += 4) {
         const int64_t v = c.target ? c.target[r] : (int64_t)c.t_idx[r * c.K + j];
         float s = 0.f;
         if (v >= 0 && v < c.V) {
@@ -345,22 +335,16 @@ __global__ void __launch_bounds__(128) k_vocab_gather(VocabCall c) {
             }
         }
         s = warp_sum_f(s);
-        if (lane == 0) {
-            c.zt[(int64_t)at * c.K + j] = s;
-            if (c.target || j == teacher_largest(c.teacher[r])) c.row[at].ref = s * c.zscale;
-        }
+        if (lane == 0) c.zt[(int64_t)at * c.K + j] = s;
     }
 }
 
 // ---------------------------------------------------------------------------
 // 4. Log-sum-exp and loss.  A CTA takes 32 compact rows; its 32 warps share the tiles, a fixed order
 // joins them, and each warp finishes a row.
-// SECOND: after the references did not hold and the logits have been taken again; the log-sum-exp
-// becomes the reference.
 // ---------------------------------------------------------------------------
 
 // A row from its log-sum-exp, by one warp: its loss (write) and what the gradients need of it.
-template <bool SECOND>
 __device__ __forceinline__ VocabRow finish_row(const VocabCall& c, int64_t at, int n_valid, float lse2, int lane, bool write) {
     const int64_t r = c.row_of[at];
     float Q = 1.f, loss = 0.f;
@@ -387,20 +371,17 @@ __device__ __forceinline__ VocabRow finish_row(const VocabCall& c, int64_t at, i
     out.unit = c.ctl->scale * ((c.row_grad ? c.row_grad[r] : 1.f / (float)n_valid) * c.inv_T);
     out.lse2 = lse2;
     out.coef = out.unit * Q;
-    out.ref = SECOND ? lse2 : c.powers ? c.row[at].ref : 0.f;
-    // powers up to 2^100, and their products with w and h, are far from the types' ends
-    if (!SECOND && c.powers && lane == 0 && lse2 - out.ref >= 100.f) c.ctl->missed = 1;
+    out.pad = 0.f;
     return out;
 }
 
-template <bool SECOND>
 __global__ void __launch_bounds__(1024) k_vocab_rows_done(VocabCall c) {
     __shared__ float sm[32][33], ss[32][33];
     after_previous();
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
     const int64_t at0 = (int64_t)blockIdx.x * 32;
     const int n_valid = c.ctl->n_valid;
-    if (at0 >= n_valid || (SECOND && c.ctl->missed == 0)) return;
+    if (at0 >= n_valid) return;
     const int64_t tiles = (c.V + kVocabTile - 1) / kVocabTile;
     // With 32 rows a lane is a row; with fewer, lanes of a row share its tiles (one row: 1024 loads at once).
     const int rows = (int)(n_valid - at0 < 32 ? n_valid - at0 : 32);
@@ -438,12 +419,12 @@ __global__ void __launch_bounds__(1024) k_vocab_rows_done(VocabCall c) {
         m = ml;
         s = sl;
     }
-    const VocabRow out = finish_row<SECOND>(c, at, n_valid, m + log2f(s), lane, true);
+    const VocabRow out = finish_row(c, at, n_valid, m + log2f(s), lane, true);
     if (lane == 0) c.row[at] = out;
 }
 
 // ---------------------------------------------------------------------------
-// 5. The gradients' operand for one piece.  The targets' entries are formed in fp32 from their own logits
+// 5. The logit gradients of one piece.  The targets' entries are formed in fp32 from their own logits
 // and written over, so that 1 - p loses nothing where p is near 1.
 // ---------------------------------------------------------------------------
 template <bool F16>
@@ -451,7 +432,6 @@ __device__ __forceinline__ void write_targets(const VocabCall& c, int64_t at, co
                                               int tid, int threads) {
     const int64_t r = c.row_of[at];
     const float4 te = c.target ? make_float4(1.f, 0.f, 0.f, 1.f) : c.teacher[r];
-    if (c.powers && !(te.x > 0.f)) return;      // the row's powers are worth nothing
     for (int j = tid; j < c.K; j += threads) {
         const int64_t v = c.target ? c.target[r] : (int64_t)c.t_idx[r * c.K + j];
         if (v < lo || v >= hi) continue;
@@ -462,15 +442,14 @@ __device__ __forceinline__ void write_targets(const VocabCall& c, int64_t at, co
                 if (c.t_idx[r * c.K + i] == v) q += c.q[r * c.K + i];
         }
         const float p = exp2_fast(c.zt[at * c.K + j] * c.zscale - vr.lse2);
-        const float x = c.powers ? (p - q / te.x) * exp2f(vr.lse2 - vr.ref) : fmaf(vr.coef, p, -(vr.unit * q));
-        c.e[at * c.vb + (v - v0)] = to16<F16>(x);
+        c.e[at * c.vb + (v - v0)] = to16<F16>(fmaf(vr.coef, p, -(vr.unit * q)));
     }
 }
 
 constexpr int kGradCols = 4096;   // columns a CTA scales
 constexpr int64_t kOwnTiles = 128;   // tiles a CTA joins itself
 
-// From the distances kept of the piece [v0, v1): e <- coef 2^(m_tile - lse - x / steps), in place, and zero
+// From the distances kept of the piece [v0, v1): e <- coef 2^(m_tile - lse - distance), in place, and zero
 // for the rows up to the padding, which the product for dw sums over.  DONE (vocabularies of up to
 // 128 tiles): each CTA joins the row's tiles itself, and the first of a row writes its loss, instead
 // of a launch of its own before this one.
@@ -513,7 +492,7 @@ __global__ void __launch_bounds__(256) k_vocab_scale(VocabCall c, int64_t v0, in
         s = ss[0];
 #pragma unroll
         for (int k = 1; k < 4; ++k) join_max_sum(m, s, sm[k], ss[k]);
-        vr = finish_row<false>(c, at, n_valid, m + log2f(s), lane, blockIdx.y == 0 && wid == 0);
+        vr = finish_row(c, at, n_valid, m + log2f(s), lane, blockIdx.y == 0 && wid == 0);
         if (blockIdx.y == 0 && tid == 0) c.row[at] = vr;
     } else {
         vr = c.row[at];
@@ -524,42 +503,16 @@ __global__ void __launch_bounds__(256) k_vocab_scale(VocabCall c, int64_t v0, in
         const uint4 x = *p;
         unsigned xs[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            // the bits of 2^23 + x, less 2^23
-            const float lo_x = __uint_as_float(0x4b000000u | (xs[q] & 0xffffu)) - 8388608.f;
-            const float hi_x = __uint_as_float(0x4b000000u | (xs[q] >> 16)) - 8388608.f;
-            xs[q] = pack16<F16>(vr.coef * exp2_fast(fmaf(lo_x, -1.f / kept_steps<F16>(), base)),
-                                vr.coef * exp2_fast(fmaf(hi_x, -1.f / kept_steps<F16>(), base)));
-        }
+        for (int q = 0; q < 4; ++q)
+            xs[q] = pack16<F16>(vr.coef * exp2_fast(base - kept_distance<F16>(xs[q] & 0xffffu)),
+                                vr.coef * exp2_fast(base - kept_distance<F16>(xs[q] >> 16)));
         *p = make_uint4(xs[0], xs[1], xs[2], xs[3]);
     }
     __syncthreads();
     write_targets<F16>(c, at, vr, lo, hi, v0, threadIdx.x, 256);
 }
 
-// Powers: hs <- hc times what each row's powers are worth, with zero rows to a multiple of 64, and the
-// targets' entries of the first piece.
-template <bool F16>
-__global__ void __launch_bounds__(128) k_vocab_worth(VocabCall c, int64_t v1) {
-    after_previous();
-    const int64_t at = blockIdx.x;
-    const int n_valid = c.ctl->n_valid;
-    if (at >= round_up(n_valid, 64)) return;
-    const bool on = at < n_valid;
-    if (on) write_targets<F16>(c, at, c.row[at], 0, v1, 0, threadIdx.x, 128);
-    const float f = on ? powers_worth(c.row[at]) : 0.f;
-    const uint4* from = (const uint4*)(c.hc + at * c.Dp);
-    uint4* to = (uint4*)(c.hs + at * c.Dp);
-    for (int64_t i = threadIdx.x; i < c.Dp / 8; i += 128) {
-        const uint4 x = on ? from[i] : make_uint4(0, 0, 0, 0);
-        unsigned xs[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-        for (int q = 0; q < 4; ++q) xs[q] = on ? pack16<F16>(f * from16<F16>((uint16_t)xs[q]), f * from16<F16>((uint16_t)(xs[q] >> 16))) : 0u;
-        to[i] = make_uint4(xs[0], xs[1], xs[2], xs[3]);
-    }
-}
-
-// The product taken again has written a piece's operand; only the targets' entries are left.
+// The product taken again has written the gradients; only the targets' entries are left.
 template <bool F16>
 __global__ void __launch_bounds__(128) k_vocab_targets(VocabCall c, int64_t v0, int64_t v1) {
     after_previous();
@@ -574,7 +527,7 @@ __global__ void __launch_bounds__(256) k_vocab_finish_dh(VocabCall c) {
     after_previous();
     const int64_t at = blockIdx.x, i = ((int64_t)blockIdx.y * 256 + threadIdx.x) * 2;
     if (at >= c.ctl->n_valid || i >= c.D) return;
-    const float f = c.ctl->inv_scale * (c.powers ? powers_worth(c.row[at]) : 1.f);
+    const float f = c.ctl->inv_scale;
     const float* from = c.dhp + at * c.Dp + i;
     const int64_t part = c.n_pad * c.Dp;
     float2 s = *(const float2*)from;
@@ -601,10 +554,6 @@ static std::mutex g_vocab_mu;
 static std::map<std::pair<int, cudaStream_t>, VocabWorkspace> g_vocab_ws;
 static std::atomic<int64_t> g_vocab_budget{(int64_t)2 << 30};
 
-// Logits from which bf16 calls keep powers: below, the pass that powers save costs less than the three
-// launches that stand by for references that do not hold.
-constexpr int64_t kPowersFrom = 1 << 23;
-
 static int64_t piece_columns(int64_t n_pad, int64_t V) {
     const int64_t fit = g_vocab_budget.load() / (2 * n_pad) / 256 * 256;
     const int64_t all = round_up(V, 256);
@@ -627,7 +576,6 @@ static size_t lay_out(VocabCall& c, bool distill, bool copy_w, char* base) {
     c.q = (float*)(distill ? take(4 * n * K) : nullptr);
     c.teacher = (float4*)(distill ? take(16 * n) : nullptr);
     c.hc = (uint16_t*)take(2 * np * c.Dp);
-    c.hs = c.powers ? (uint16_t*)take(2 * np * c.Dp) : c.hc;
     c.wc = (uint16_t*)(copy_w ? take(2 * (size_t)c.V * c.Dp) : nullptr);
     c.zt = (float*)take(4 * np * K);
     c.part = (float2*)take(8 * tiles * np);
@@ -664,7 +612,6 @@ static void size_call(VocabCall& c, bool want_dh, DwRows dw, int sm_count) {
     c.n_pad = round_up(c.n, kVocabRowPad);
     c.Dp = round_up(c.D, 64);
     c.vb = want_dh || dw != DwRows::none ? piece_columns(c.n_pad, c.V) : 0;
-    c.powers = !c.f16 && c.vb > 0 && c.n * c.V >= kPowersFrom;
     c.splits = want_dh ? vocab_dh_splits(c.n, c.D, c.vb < c.V ? c.vb : c.V, dw, sm_count) : 0;
 }
 
@@ -683,32 +630,23 @@ static int enqueue(const VocabCall& c, bool distill, int sms, cudaStream_t st) {
     note_launch(1 + (distill ? 1 : 0) + (c.n > kRankRows ? 1 : 0));
     const int64_t kept = grad ? (c.vb < c.V ? c.vb : c.V) : 0;
     int rc = GK_OK;
-    if (kept > 0) rc = c.powers ? launch_vocab_powers(c, 0, kept, false, sms, st) : launch_vocab_logits(c, 0, kept, true, false, sms, st);
-    if (rc == GK_OK && kept < c.V) rc = launch_vocab_logits(c, kept, c.V, false, false, sms, st);
+    if (kept > 0) rc = launch_vocab_logits(c, 0, kept, true, sms, st);
+    if (rc == GK_OK && kept < c.V) rc = launch_vocab_logits(c, kept, c.V, false, sms, st);
     if (rc != GK_OK) return rc;
-    const bool own = grad && !c.powers && (c.V + kVocabTile - 1) / kVocabTile <= kOwnTiles;
+    const bool own = grad && (c.V + kVocabTile - 1) / kVocabTile <= kOwnTiles;
     if (!own) {
-        GK_CUDA_TRY(launch_next(k_vocab_rows_done<false>, dim3(groups), 1024, 0, st, c));
+        GK_CUDA_TRY(launch_next(k_vocab_rows_done, dim3(groups), 1024, 0, st, c));
         note_launch();
     }
     if (!grad) return GK_OK;
-    if (c.powers) {
-        rc = launch_vocab_logits(c, 0, kept, false, true, sms, st);
-        if (rc != GK_OK) return rc;
-        GK_CUDA_TRY(launch_next(k_vocab_rows_done<true>, dim3(groups), 1024, 0, st, c));
-        rc = launch_vocab_powers(c, 0, kept, true, sms, st);
-        if (rc != GK_OK) return rc;
-        GK_CUDA_TRY(launch_next(k_vocab_worth<F16>, dim3((unsigned)round_up(n, 64)), 128, 0, st, c, kept));
-        note_launch(2);
-    }
     for (int64_t v0 = 0; v0 < c.V; v0 += c.vb) {
         const int64_t v1 = v0 + c.vb < c.V ? v0 + c.vb : c.V;
         if (v0 > 0) {
-            rc = c.powers ? launch_vocab_powers(c, v0, v1, false, sms, st) : launch_vocab_again(c, v0, v1, sms, st);
+            rc = launch_vocab_again(c, v0, v1, sms, st);
             if (rc != GK_OK) return rc;
             GK_CUDA_TRY(launch_next(k_vocab_targets<F16>, dim3(n), 128, 0, st, c, v0, v1));
             note_launch();
-        } else if (!c.powers) {
+        } else {
             const dim3 grid((unsigned)round_up(n, 64), (unsigned)((v1 + kGradCols - 1) / kGradCols));
             GK_CUDA_TRY(launch_next(own ? k_vocab_scale<F16, true> : k_vocab_scale<F16, false>, grid, 256, 0, st, c, v0, v1));
             note_launch();

@@ -18,7 +18,6 @@ constexpr int kVocabMaxPairs = 1024;    // largest K of gk_vocab_distill and gk_
 struct VocabCtl {
     int n_valid;           // rows that count
     unsigned int status;   // GK_DEV_* flags
-    int missed;            // a row's reference was too far below its logits: powers overflowed
     float scale;           // power of two that brings the largest row coefficient to the 16-bit type's range
     float inv_scale;
 };
@@ -28,7 +27,7 @@ struct VocabRow {
     float lse2;     // log-sum-exp of the scaled logits, in units of log 2
     float coef;     // scale * g_n * Q_n / T: what multiplies p_nv
     float unit;     // scale * g_n / T: what multiplies q_nj
-    float ref;      // reference of the row's powers, in units of log 2
+    float pad;
 };
 
 // One call's sizes and device pointers, passed to the kernels by value.
@@ -60,16 +59,13 @@ struct VocabCall {
     int32_t* at_of;             // row -> compact row, -1 where left out
     float* q;                   // n x K teacher probabilities (distill), 0 for a pair left out
     float4* teacher;            // per row: Q, log-sum-exp L relative to a reference, the reference, and a whole
-                                // number: 1 (indices strictly ascending, pairs left out at the end) + 2 (a pair
-                                // counts) + 4 x place of the largest
-    bool powers;                // e holds powers relative to the rows' references, else logits below their tile's maximum
+                                // number: 1 (indices strictly ascending, pairs left out at the end) + 2 (a pair counts)
     uint16_t* hc;               // n_pad x Dp compact rows of h
-    uint16_t* hs;               // powers: hc with each row times what its powers are worth, else hc
     uint16_t* wc;               // V x Dp copy of w where w itself cannot be the source of bulk copies, else nullptr
     float* zt;                  // n_pad x K raw logits at the targets
     float2* part;               // per (vocabulary tile, compact row): maximum (units of log 2), sum
     VocabRow* row;              // n_pad
-    uint16_t* e;                // n_pad x vb: one piece's powers, or kept logits and then logit gradients
+    uint16_t* e;                // n_pad x vb: one piece's kept logits, then its logit gradients
     int64_t vb;                 // columns of a piece, a multiple of 256 (the pitch of e)
     float* dhp;                 // splits x n_pad x Dp partial sums of dh; nullptr: dh is stored by its product
     int splits;
@@ -94,16 +90,13 @@ inline cudaError_t launch_next(void (*kernel)(Params...), dim3 grid, unsigned th
 
 __host__ __device__ inline int64_t round_up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
 
-// The products (gk_vocab_gemm.cu).  v0, v1: the columns of the vocabulary [v0, v1); if_missed: nothing is
-// done unless ctl->missed.
+// The products (gk_vocab_gemm.cu).  v0, v1: the columns of the vocabulary [v0, v1).
 // Logits of all compact rows: per tile of the vocabulary the maximum and the sum; keep: the
-// logits go to e, as 16-bit whole numbers of steps (kept_steps) below the tile's maximum.
-int launch_vocab_logits(const VocabCall& c, int64_t v0, int64_t v1, bool keep, bool if_missed, int sm_count, cudaStream_t st);
-// The same relative to the rows' references: sums, and the powers go to e.
-int launch_vocab_powers(const VocabCall& c, int64_t v0, int64_t v1, bool if_missed, int sm_count, cudaStream_t st);
+// logits go to e, as 16-bit codes of their distance from the tile's maximum.
+int launch_vocab_logits(const VocabCall& c, int64_t v0, int64_t v1, bool keep, int sm_count, cudaStream_t st);
 // The same product again with the rows' log-sum-exp known: e receives the logit gradients.
 int launch_vocab_again(const VocabCall& c, int64_t v0, int64_t v1, int sm_count, cudaStream_t st);
-// dw rows [v0, v1) = e^T hs / scale, and dh = e w[v0:v1] times each row's factor, or its sums in fp32 in
+// dw rows [v0, v1) = e^T hc / scale, and dh = e w[v0:v1] / scale, or its sums in fp32 in
 // `splits` parts added to dhp (first: overwritten).
 int launch_vocab_grads(const VocabCall& c, int64_t v0, int64_t v1, bool first, int sm_count, cudaStream_t st);
 enum class DwRows { none, aligned, unaligned };     // dw's rows start and end on 16-byte boundaries, or not
@@ -119,7 +112,6 @@ __device__ __forceinline__ void after_previous() {
 
 __device__ __forceinline__ bool teacher_ascending(const float4& t) { return ((int)t.w & 1) != 0; }
 __device__ __forceinline__ bool teacher_counts(const float4& t) { return ((int)t.w & 2) != 0; }
-__device__ __forceinline__ int teacher_largest(const float4& t) { return (int)t.w >> 2; }
 
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;
@@ -127,10 +119,23 @@ __device__ __forceinline__ float exp2_fast(float x) {
     return y;
 }
 
-// Steps a unit of log 2 in which a logit's distance from its tile's maximum is kept: 2^-9 over a
-// range of 128 (the exponents bf16 gradients can have), 2^-11 over 32 (fp16's).
+// The 16-bit code of a logit's distance d <= 0 from its tile's maximum, in units of log 2.  bf16: steps of 2^-9 over
+// a range of 128, the exponents bf16 gradients can have.  fp16: steps of 2^-12 over the first 8 and of 1 / 1365.25
+// over the next 24, where fp16 gradients have ended.  The last code stands for itself and more.
 template <bool F16>
-__device__ __forceinline__ constexpr float kept_steps() { return F16 ? 2048.f : 512.f; }
+__device__ __forceinline__ unsigned kept_code(float d) {
+    // the bits of 2^23 + x hold x
+    const float end = 8388608.f + 65535.f;
+    float x = fminf(fmaf(d, F16 ? -4096.f : -512.f, 8388608.f), end);
+    if constexpr (F16) x = fminf(x, fmaf(d, -1365.25f, 8388608.f + 21846.f));
+    return __float_as_uint(x) & 0xffffu;
+}
+template <bool F16>
+__device__ __forceinline__ float kept_distance(unsigned code) {      // -d
+    const float x = __uint_as_float(0x4b000000u | code) - 8388608.f;
+    if constexpr (F16) return fmaxf(x * (1.f / 4096.f), (x - 21846.f) * (1.f / 1365.25f));
+    else return x * (1.f / 512.f);
+}
 
 // 16-bit storage <-> fp32, round to nearest even (F16: fp16, else bf16).
 template <bool F16>
@@ -158,9 +163,6 @@ __device__ __forceinline__ unsigned pack16(float lo, float hi) {
     else asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
-
-// What a row's powers are worth.
-__device__ __forceinline__ float powers_worth(const VocabRow& r) { return r.coef * exp2f(r.ref - r.lse2); }
 
 // Joins (m, s) pairs of a running maximum and sum, in units of log 2.  A part without a term
 // has m = -inf and s = 0.

@@ -20,14 +20,12 @@
 //   kLogits      hc  rows x D         w   columns x D      maximum and sum of 128 columns per row
 //   kLogitsKeep  the same                                  and the logits, as 16-bit steps below that
 //                                                          maximum
-//   kPowers      the same                                  sum of 128 columns' powers relative to the row's
-//                                                          reference, and the powers in 16 bits
 //   kAgain       the same                                  logit gradients, the log-sum-exp being known
 //   kGrads, dh   e   rows x columns   w^T  D x columns     16-bit rows of dh, or fp32 partial sums of them
-//   kGrads, dw   e^T columns x rows   hs^T D x rows        16-bit rows of dw
+//   kGrads, dw   e^T columns x rows   hc^T D x rows        16-bit rows of dw
 //
 // The two gradients are tiles of one launch, dh's long ones first, so that they fill the SMs together.
-// (hs: hc, or with powers hc with its rows scaled.)  e, hc and w are stored once, by rows; where the summed axis is not the contiguous one the
+// e, hc and w are stored once, by rows; where the summed axis is not the contiguous one the
 // operand is read as it lies (MN-major descriptors) instead of being transposed in memory.
 // Results leave through shared memory, 32 rows x 128 bytes a warp, as TMA stores: a thread has a row of
 // its own, and stores of 16 bytes to 32 rows at once would take the time of 32.
@@ -39,7 +37,7 @@
 
 namespace gk {
 
-enum Product { kLogits, kLogitsKeep, kPowers, kAgain, kGrads };
+enum Product { kLogits, kLogitsKeep, kAgain, kGrads };
 
 constexpr int kTileM = 256, kHalfN = 256, kTileN = 2 * kHalfN, kBlockK = 64;
 constexpr int kOperandBytes = 128 * kBlockK * 2;            // a CTA's share of A, or of a half of B, in a block
@@ -226,7 +224,6 @@ struct ProductArgs {
     VocabCall c;
     int64_t v0, v1;
     int narrow;      // tiles of 256 columns instead of 512
-    int if_missed;   // only if the rows' references did not hold
     int first;       // dh: overwrite the partial sums
     int splits;      // dh: parts of the summed axis
     int direct;      // dh: one part and one piece, 16-bit rows are stored at once
@@ -242,7 +239,7 @@ struct Patch {
     int64_t row0;        // of the warp; the thread's row is row0 + lane
     int64_t col0;        // of the 128
     int64_t cols;        // columns of the result from col0 on (may be more than 128, or none)
-    int cursor;          // kLogits, kLogitsKeep, kPowers with a teacher: the row's first pair at or after col0
+    int cursor;          // kLogits, kLogitsKeep with a teacher: the row's first pair at or after col0
 };
 
 // A row's teacher pairs in ascending order are met one patch of columns at a time: the logit at each is
@@ -309,7 +306,6 @@ __device__ __forceinline__ void read_logits(const ProductArgs& p, const Patch& w
     for (int i = 0; i < 128; ++i) top[i & 3] = fmaxf(top[i & 3], v[i]);
     const float m = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
     const float ref = m == -INFINITY ? 0.f : m;   // all -inf: every term is exp(-inf)
-    const float step = -c.zscale * kept_steps<F16>();
     float s[4] = {};
 #pragma unroll
     for (int ch = 0; ch < 2; ++ch) {
@@ -319,11 +315,10 @@ __device__ __forceinline__ void read_logits(const ProductArgs& p, const Patch& w
             unsigned code[4];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float d = v[ch * 64 + g * 8 + i] - ref;
-                s[i & 3] += exp2_fast(d * c.zscale);
+                const float d = (v[ch * 64 + g * 8 + i] - ref) * c.zscale;
+                s[i & 3] += exp2_fast(d);
                 if constexpr (P == kLogitsKeep) {
-                    // 2^23 + x has x in its low bits; 65535 steps stand for themselves and more
-                    const unsigned x = __float_as_uint(fminf(fmaf(d, step, 8388608.f), 8388608.f + 65535.f));
+                    const unsigned x = kept_code<F16>(d);
                     if (i & 1) code[i >> 1] = __byte_perm(code[i >> 1], x, 0x5410);
                     else code[i >> 1] = x;
                 }
@@ -334,36 +329,6 @@ __device__ __forceinline__ void read_logits(const ProductArgs& p, const Patch& w
             if (ch * 64 < w.cols) stage_store(w.staging, w.lane, out, (int)(w.col0 - p.v0) + ch * 64, (int)w.row0);
     }
     if (row < n_valid) c.part[w.col0 / kVocabTile * c.n_pad + row] = make_float2(m * c.zscale, (s[0] + s[1]) + (s[2] + s[3]));
-}
-
-// Powers of two of the scaled logits relative to the row's reference.  What they are worth comes with the
-// log-sum-exp: e^T (hs) and (e w) take it as a factor of their rows.
-template <bool F16>
-__device__ __forceinline__ void read_powers(const ProductArgs& p, const Patch& w, const CUtensorMap* out, int n_valid, float (&v)[128]) {
-    const VocabCall& c = p.c;
-    const int64_t row = w.row0 + w.lane;
-    const bool on = row < n_valid;
-    const float ref = on ? c.row[row].ref : 0.f;
-    float s[4] = {};
-#pragma unroll
-    for (int ch = 0; ch < 2; ++ch) {
-        if (ch * 64 >= w.cols) break;
-        stage_reuse(w.lane);
-#pragma unroll
-        for (int g = 0; g < 8; ++g) {
-            unsigned o[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float a = exp2_fast(fmaf(v[ch * 64 + g * 8 + 2 * i], c.zscale, -ref));
-                const float b = exp2_fast(fmaf(v[ch * 64 + g * 8 + 2 * i + 1], c.zscale, -ref));
-                s[i] += a + b;
-                o[i] = on ? pack16<F16>(a, b) : 0u;     // rows up to the padding are summed over by dw
-            }
-            stage_word(w.staging, w.lane, g, o[0], o[1], o[2], o[3]);
-        }
-        stage_store(w.staging, w.lane, out, (int)(w.col0 - p.v0) + ch * 64, (int)w.row0);
-    }
-    if (on) c.part[w.col0 / kVocabTile * c.n_pad + row] = make_float2(ref, (s[0] + s[1]) + (s[2] + s[3]));
 }
 
 template <bool F16>
@@ -474,7 +439,7 @@ __device__ __forceinline__ void read_dh(const ProductArgs& p, const Patch& w, co
         float f = 0.f;
         int to = -1;
         if (row < n_valid) {
-            f = c.ctl->inv_scale * (c.powers ? powers_worth(c.row[row]) : 1.f);
+            f = c.ctl->inv_scale;
             to = c.row_of[row];
         }
 #pragma unroll
@@ -637,11 +602,9 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     const int64_t nv = p.v1 - p.v0, n_cols = P == kGrads ? c.D : nv;      // columns of the result
     const Tiles tiles = P == kGrads ? make_tiles(c.dh ? n_valid : 0, c.D, nv, width, p.splits) : make_tiles(n_valid, nv, c.D, width, 1);
     const Tiles tiles2 = make_tiles(P == kGrads && c.dw ? nv : 0, c.D, n_valid, width, 1);
-    const bool idle = p.if_missed && c.ctl->missed == 0;
 
     bool ok = true;
-    if (idle) {
-    } else if (warp == 0) {
+    if (warp == 0) {
         // producer: this CTA's 128 rows of A and of each half of B; the leader's barrier counts both CTAs' bytes
         int stage = 0;
         uint32_t phase = 0;
@@ -807,8 +770,8 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
             (dw ? tiles2 : tiles).blocks(split, k0, k1);
             const bool two = !narrow && n * kTileN + kHalfN < n_cols;
             w.row0 = m * kTileM + (int)rank * 128 + quarter * 32;
-            // rows that are used: those that count, and for powers and gradients those that dw sums over
-            const bool used_rows = P == kGrads || w.row0 < (P == kPowers || P == kAgain ? round_up(n_valid, 64) : n_valid);
+            // rows that are used: those that count, and of logit gradients those that dw sums over
+            const bool used_rows = P == kGrads || w.row0 < (P == kAgain ? round_up(n_valid, 64) : n_valid);
             const uint32_t lanes = tmem + side * 128 + ((uint32_t)(quarter * 32) << 16);
             float v[128];
             auto wait_sums = [&](int h) {
@@ -856,7 +819,6 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                         for (int i = 0; i < 128; ++i) v[i] = i < w.cols ? v[i] : -INFINITY;
                     }
                     if constexpr (P == kLogits || P == kLogitsKeep) read_logits<P, F16>(p, w, &map_out, n_valid, v);
-                    else if constexpr (P == kPowers) read_powers<F16>(p, w, &map_out, n_valid, v);
                     else read_gradients<F16>(p, w, &map_out, n_valid, v);
                 }
             } else {
@@ -966,7 +928,7 @@ static int launch_product(ProductArgs p, int sm_count, cudaStream_t st) {
         out = a;     // not used by direct stores
         if (rc == GK_OK && c.dh && !p.direct) rc = make_map(&out, kF32, c.dhp, c.Dp, p.splits * c.n_pad, c.Dp, 32);
         if (rc == GK_OK) rc = make_map(&a2, type, c.e, nv, c.n_pad, c.vb, 64);
-        if (rc == GK_OK) rc = make_map(&b2, type, c.hs, c.Dp, c.n_pad, c.Dp, 64);
+        if (rc == GK_OK) rc = make_map(&b2, type, c.hc, c.Dp, c.n_pad, c.Dp, 64);
         out2 = a2;   // rows on other boundaries are stored without a map
         if (rc == GK_OK && c.dw && p.wide) rc = make_map(&out2, type, (const uint16_t*)c.dw + p.v0 * c.lddw, c.D, nv, c.lddw, 32);
         first = {c.dh ? c.n : 0, c.D, (nv + kBlockK - 1) / kBlockK, false};
@@ -999,13 +961,12 @@ static int launch_product(ProductArgs p, int sm_count, cudaStream_t st) {
 }
 
 template <int P>
-static int launch(const VocabCall& c, int64_t v0, int64_t v1, bool first, bool if_missed, int sm_count, cudaStream_t st) {
+static int launch(const VocabCall& c, int64_t v0, int64_t v1, bool first, int sm_count, cudaStream_t st) {
     ProductArgs p;
     p.c = c;
     p.v0 = v0;
     p.v1 = v1;
     p.narrow = 0;
-    p.if_missed = if_missed;
     p.first = first;
     p.splits = P == kGrads && c.splits > 0 ? c.splits : 1;
     p.direct = c.dhp == nullptr;
@@ -1020,17 +981,14 @@ static int launch(const VocabCall& c, int64_t v0, int64_t v1, bool first, bool i
     return c.f16 ? launch_product<P, true>(p, sm_count, st) : launch_product<P, false>(p, sm_count, st);
 }
 
-int launch_vocab_logits(const VocabCall& c, int64_t v0, int64_t v1, bool keep, bool if_missed, int sm_count, cudaStream_t st) {
-    return keep ? launch<kLogitsKeep>(c, v0, v1, true, if_missed, sm_count, st) : launch<kLogits>(c, v0, v1, true, if_missed, sm_count, st);
-}
-int launch_vocab_powers(const VocabCall& c, int64_t v0, int64_t v1, bool if_missed, int sm_count, cudaStream_t st) {
-    return launch<kPowers>(c, v0, v1, true, if_missed, sm_count, st);
+int launch_vocab_logits(const VocabCall& c, int64_t v0, int64_t v1, bool keep, int sm_count, cudaStream_t st) {
+    return keep ? launch<kLogitsKeep>(c, v0, v1, true, sm_count, st) : launch<kLogits>(c, v0, v1, true, sm_count, st);
 }
 int launch_vocab_again(const VocabCall& c, int64_t v0, int64_t v1, int sm_count, cudaStream_t st) {
-    return launch<kAgain>(c, v0, v1, true, false, sm_count, st);
+    return launch<kAgain>(c, v0, v1, true, sm_count, st);
 }
 int launch_vocab_grads(const VocabCall& c, int64_t v0, int64_t v1, bool first, int sm_count, cudaStream_t st) {
-    return launch<kGrads>(c, v0, v1, first, false, sm_count, st);
+    return launch<kGrads>(c, v0, v1, first, sm_count, st);
 }
 
 // Into how many parts the summed axis of dh is split.  dh has few tiles (rows / 256 x D / 512) and a
