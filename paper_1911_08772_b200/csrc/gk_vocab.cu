@@ -232,10 +232,11 @@ __device__ __forceinline__ uint4 load8(const uint16_t* p, int64_t left) {
 }
 
 // RANK (few rows): each CTA takes a row of the caller's and finds its number itself, by looking at all rows
-// (2048 rows are 16 loads a thread, where a launch of its own costs 3 to 6 us); one of them writes the
+// (1024 rows are 8 loads a thread, where a launch of its own costs 3 to 6 us; 2048 rows took 25 us so, and 17 by two
+// launches); one of them writes the
 // control block.
 // CTAs from n_pad on make the copy of w with rows that start and end on 16-byte boundaries, where w's own do not.
-constexpr int64_t kRankRows = 2048;
+constexpr int64_t kRankRows = 1024;
 
 template <bool F16, bool RANK>
 __global__ void __launch_bounds__(128) k_vocab_gather(VocabCall c) {
@@ -427,45 +428,74 @@ __global__ void __launch_bounds__(1024) k_vocab_rows_done(VocabCall c) {
 // 5. The logit gradients of one piece.  The targets' entries are formed in fp32 from their own logits
 // and written over, so that 1 - p loses nothing where p is near 1.
 // ---------------------------------------------------------------------------
-template <bool F16>
-__device__ __forceinline__ void write_targets(const VocabCall& c, int64_t at, const VocabRow& vr, int64_t lo, int64_t hi, int64_t v0,
-                                              int tid, int threads) {
-    const int64_t r = c.row_of[at];
-    const float4 te = c.target ? make_float4(1.f, 0.f, 0.f, 1.f) : c.teacher[r];
-    for (int j = tid; j < c.K; j += threads) {
-        const int64_t v = c.target ? c.target[r] : (int64_t)c.t_idx[r * c.K + j];
-        if (v < lo || v >= hi) continue;
-        float q = c.target ? 1.f : c.q[r * c.K + j];
-        if (!teacher_ascending(te)) {      // an index given more than once: each of its pairs writes the same sum
-            q = 0.f;
-            for (int i = 0; i < c.K; ++i)
-                if (c.t_idx[r * c.K + i] == v) q += c.q[r * c.K + i];
-        }
-        const float p = exp2_fast(c.zt[at * c.K + j] * c.zscale - vr.lse2);
-        c.e[at * c.vb + (v - v0)] = to16<F16>(fmaf(vr.coef, p, -(vr.unit * q)));
+// A thread's pair: fetched before it is needed, written where its column is in [lo, hi).
+struct Target {
+    int64_t v;
+    float z, q;
+};
+__device__ __forceinline__ Target fetch_target(const VocabCall& c, int64_t at, int64_t r, int j) {
+    Target t = {-1, 0.f, 0.f};
+    if (j < c.K) {
+        t.v = c.target ? c.target[r] : (int64_t)c.t_idx[r * c.K + j];
+        t.z = c.zt[at * c.K + j];
+        t.q = c.target ? 1.f : c.q[r * c.K + j];
     }
+    return t;
+}
+template <bool F16>
+__device__ __forceinline__ void write_target(const VocabCall& c, int64_t at, int64_t r, const VocabRow& vr, bool distinct, Target t,
+                                             int64_t lo, int64_t hi, int64_t v0) {
+    if (t.v < lo || t.v >= hi) return;
+    if (!distinct) {      // an index given more than once: each of its pairs writes the same sum
+        t.q = 0.f;
+        for (int i = 0; i < c.K; ++i)
+            if (c.t_idx[r * c.K + i] == t.v) t.q += c.q[r * c.K + i];
+    }
+    const float p = exp2_fast(t.z * c.zscale - vr.lse2);
+    c.e[at * c.vb + (t.v - v0)] = to16<F16>(fmaf(vr.coef, p, -(vr.unit * t.q)));
 }
 
-constexpr int kGradCols = 4096;   // columns a CTA scales
 constexpr int64_t kOwnTiles = 128;   // tiles a CTA joins itself
 
 // From the distances kept of the piece [v0, v1): e <- coef 2^(m_tile - lse - distance), in place, and zero
 // for the rows up to the padding, which the product for dw sums over.  DONE (vocabularies of up to
 // 128 tiles): each CTA joins the row's tiles itself, and the first of a row writes its loss, instead
-// of a launch of its own before this one.
+// of a launch of its own before this one.  All of a thread's words are on their way before anything that they
+// wait for is looked at: a CTA's time is a few memory latencies, whatever it moves (8192 x 128000: 1050 us with half
+// as many words and those after the row's values).
+template <bool DONE>
+constexpr int kScaleWords = DONE ? 2 : 4;                                  // 16-byte words a thread
+template <bool DONE>
+constexpr int kGradCols = 256 * 8 * kScaleWords<DONE>;                     // columns a CTA
+
 template <bool F16, bool DONE>
 __global__ void __launch_bounds__(256) k_vocab_scale(VocabCall c, int64_t v0, int64_t v1) {
     __shared__ float sm[4], ss[4];
     after_previous();
     const int64_t at = blockIdx.x;
+    const int64_t lo = v0 + (int64_t)blockIdx.y * kGradCols<DONE>;
+    const int64_t hi = lo + kGradCols<DONE> < v1 ? lo + kGradCols<DONE> : v1;
+    uint4* const mine = (uint4*)(c.e + at * c.vb + (lo - v0)) + threadIdx.x;
+    const int left = (int)((hi - lo + 7) / 8) - (int)threadIdx.x;          // words from this thread's first on
+    uint4 x[kScaleWords<DONE>];
+    float top[kScaleWords<DONE>];
+#pragma unroll
+    for (int j = 0; j < kScaleWords<DONE>; ++j)
+        if (j * 256 < left) {
+            x[j] = __ldcs(mine + j * 256);
+            top[j] = __ldg(&c.part[(lo + (j * 256 + threadIdx.x) * 8) / kVocabTile * c.n_pad + at].x);
+        }
     const int n_valid = c.ctl->n_valid;
+    const int64_t r = c.row_of[at < c.n ? at : 0];
     if (at >= round_up(n_valid, 64)) return;
-    const int64_t lo = v0 + (int64_t)blockIdx.y * kGradCols;
-    const int64_t hi = lo + kGradCols < v1 ? lo + kGradCols : v1;
     if (at >= n_valid) {
-        for (int64_t v = lo + threadIdx.x * 8; v < hi; v += 256 * 8) *(uint4*)(c.e + at * c.vb + (v - v0)) = make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int j = 0; j < kScaleWords<DONE>; ++j)
+            if (j * 256 < left) mine[j * 256] = make_uint4(0, 0, 0, 0);
         return;
     }
+    const bool distinct = c.target || teacher_ascending(c.teacher[r]);
+    const Target first = fetch_target(c, at, r, threadIdx.x);
     VocabRow vr;
     if constexpr (DONE) {
         const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
@@ -497,19 +527,20 @@ __global__ void __launch_bounds__(256) k_vocab_scale(VocabCall c, int64_t v0, in
     } else {
         vr = c.row[at];
     }
-    for (int64_t v = lo + threadIdx.x * 8; v < hi; v += 256 * 8) {
-        const float base = __ldg(&c.part[v / kVocabTile * c.n_pad + at].x) - vr.lse2;
-        uint4* p = (uint4*)(c.e + at * c.vb + (v - v0));
-        const uint4 x = *p;
-        unsigned xs[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-            xs[q] = pack16<F16>(vr.coef * exp2_fast(base - kept_distance<F16>(xs[q] & 0xffffu)),
-                                vr.coef * exp2_fast(base - kept_distance<F16>(xs[q] >> 16)));
-        *p = make_uint4(xs[0], xs[1], xs[2], xs[3]);
-    }
+    for (int j = 0; j < kScaleWords<DONE>; ++j)
+        if (j * 256 < left) {
+            const float base = top[j] - vr.lse2;
+            unsigned xs[4] = {x[j].x, x[j].y, x[j].z, x[j].w};
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                xs[q] = pack16<F16>(vr.coef * exp2_fast(base - kept_distance<F16>(xs[q] & 0xffffu)),
+                                    vr.coef * exp2_fast(base - kept_distance<F16>(xs[q] >> 16)));
+            mine[j * 256] = make_uint4(xs[0], xs[1], xs[2], xs[3]);
+        }
     __syncthreads();
-    write_targets<F16>(c, at, vr, lo, hi, v0, threadIdx.x, 256);
+    write_target<F16>(c, at, r, vr, distinct, first, lo, hi, v0);
+    for (int j = threadIdx.x + 256; j < c.K; j += 256) write_target<F16>(c, at, r, vr, distinct, fetch_target(c, at, r, j), lo, hi, v0);
 }
 
 // The product taken again has written the gradients; only the targets' entries are left.
@@ -518,7 +549,9 @@ __global__ void __launch_bounds__(128) k_vocab_targets(VocabCall c, int64_t v0, 
     after_previous();
     const int64_t at = blockIdx.x;
     if (at >= c.ctl->n_valid) return;
-    write_targets<F16>(c, at, c.row[at], v0, v1, v0, threadIdx.x, 128);
+    const int64_t r = c.row_of[at];
+    const bool distinct = c.target || teacher_ascending(c.teacher[r]);
+    for (int j = threadIdx.x; j < c.K; j += 128) write_target<F16>(c, at, r, c.row[at], distinct, fetch_target(c, at, r, j), v0, v1, v0);
 }
 
 // dh in the caller's rows from its parts' sums, added in their order.
@@ -647,7 +680,8 @@ static int enqueue(const VocabCall& c, bool distill, int sms, cudaStream_t st) {
             GK_CUDA_TRY(launch_next(k_vocab_targets<F16>, dim3(n), 128, 0, st, c, v0, v1));
             note_launch();
         } else {
-            const dim3 grid((unsigned)round_up(n, 64), (unsigned)((v1 + kGradCols - 1) / kGradCols));
+            const int cols = own ? kGradCols<true> : kGradCols<false>;
+            const dim3 grid((unsigned)round_up(n, 64), (unsigned)((v1 + cols - 1) / cols));
             GK_CUDA_TRY(launch_next(own ? k_vocab_scale<F16, true> : k_vocab_scale<F16, false>, grid, 256, 0, st, c, v0, v1));
             note_launch();
         }
