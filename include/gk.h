@@ -321,8 +321,9 @@ int gk_set_params(int unbiased_std, int max_rounds);
  * has such a head; the paper does not treat it).  With z = h w^T, without keeping z,
  *     lse_n = log sum_v exp z_nv;   loss_n = lse_n - z_n,t(n);
  *     dz_nv = g_n (exp(z_nv - lse_n) - [v = t(n)]);   dh = dz w;   dw = dz^T h.
- * Products of 16-bit operands are summed in fp32, lse and loss are fp32; dz is rounded to the
- * operands' type before the products dh and dw, which are rounded once more at the end.
+ * Products of 16-bit operands are summed in fp32 (logits in pieces of 768, the pieces in fp32 registers), lse
+ * and loss are fp32; dz is rounded to the operands' type before the products dh and dw, which are rounded
+ * once more at the end.
  *
  *   h          DEVICE in   n rows of D elements of `dtype`, row stride ldh >= D (in elements)
  *   w          DEVICE in   V rows of D elements, row stride ldw >= D.  Rows that start and end on
@@ -341,9 +342,11 @@ int gk_set_params(int unbiased_std, int max_rounds);
  * each other.  Results do not depend on timing: no atomics on floating-point data.
  *
  * The workspace is the call's own, per (device, stream), grown on first use (gk_vocab_reserve
- * does that ahead; a call that fits allocates nothing and can be captured in a graph).  The
- * largest part is one piece of the vocabulary as n rows of 16-bit values, bounded by
- * gk_vocab_set_budget; a vocabulary that does not fit one piece costs the product h w^T twice.
+ * does that ahead; a call that fits allocates nothing and can be captured in a graph, which stays good until a
+ * call that does not fit replaces the workspace).  The
+ * largest part, with gradients, is one piece of the vocabulary as n rows of 16-bit values, bounded by
+ * gk_vocab_set_budget; of a vocabulary that does not fit one piece the product h w^T is taken twice.
+ * Memory for 8 bytes a row and 128 columns is needed beside it.
  */
 int gk_vocab_loss(const void* h, int64_t ldh, const void* w, int64_t ldw, int32_t dtype, int64_t n, int64_t D,
                   int64_t V, const int64_t* target, int64_t ignore_index, const float* row_grad, float* loss_out,
@@ -475,7 +478,9 @@ int gk_last_cta_trace(gk_stream_t stream, uint64_t* host_out, int* n_ctas);
  *   key 1  polls of a predecessor's status word in the look-back compaction (default 2^22)
  *   key 2  arrivals the barriers of the fused gk_sparsify kernel wait for beyond the grid
  *          size (default 0).  With 1 no barrier can complete: every CTA's wait runs out,
- *          the call ends with GK_DEV_TIMEOUT in gk_stats.status and invalid outputs.
+ *          the call ends with GK_DEV_TIMEOUT in gk_stats.status and invalid outputs.  Also in the
+ *          products of gk_vocab_loss and gk_vocab_distill, whose readers then wait for sums that never
+ *          arrive (a sixteenth of a second instead of two): GK_DEV_TIMEOUT in gk_vocab_last_info.
  *   key 3  a tile of the look-back compaction that keeps its status word to itself, so
  *          that its successors' waits run out (default -1: none)
  *   key 4  counting against predicted thresholds in the fused gk_sparsify / gk_select

@@ -98,14 +98,15 @@ __device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
         : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok != 0;
 }
-// Bounded: gives up after 2^32 clocks (about two seconds), or 2^24 polls, whichever is first.
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) {
+// Bounded: gives up after `limit` clocks, or 2^24 polls, whichever is first.
+constexpr long long kWaitClocks = 1ll << 32;       // about two seconds
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, long long limit) {
     if (mbar_try(bar, parity)) return true;
     const long long t0 = clock64();
 #pragma unroll 1
     for (int i = 0; i < (1 << 24); ++i) {
         if (mbar_try(bar, parity)) return true;
-        if ((i & 63) == 63 && clock64() - t0 > (1ll << 32)) return false;
+        if ((i & 63) == 63 && clock64() - t0 > limit) return false;
     }
     return false;
 }
@@ -113,8 +114,8 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) {
 // be the same in all lanes, and one elected lane only for the instructions themselves, their
 // operands stay in uniform registers.  (A loop run by lane 0 alone moved six operands per product out
 // of ordinary registers and could not keep the tensor pipe fed: 61 % busy, 4096 x 4096 x 32000.)
-__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity) {
-    return __all_sync(0xffffffffu, mbar_wait(bar, parity));
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, long long limit) {
+    return __all_sync(0xffffffffu, mbar_wait(bar, parity, limit));
 }
 __device__ __forceinline__ bool elected() {
     uint32_t p;
@@ -225,6 +226,8 @@ struct ProductArgs {
     int64_t v0, v1;
     int narrow;      // tiles of 256 columns instead of 512
     int first;       // dh: overwrite the partial sums
+    long long wait_clocks;   // limit of every wait
+    int extra_arrivals;      // test hook: arrivals the readers wait for that never come
     int splits;      // dh: parts of the summed axis
     int direct;      // dh: one part and one piece, 16-bit rows are stored at once
     int wide;        // dw: rows start and end on 16-byte boundaries
@@ -580,7 +583,7 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
             mbar_init(smem_u32(&bar_empty[s]), 1);
         }
         for (int b = 0; b < 2; ++b) {
-            mbar_init(smem_u32(&bar_sum[b]), 1);
+            mbar_init(smem_u32(&bar_sum[b]), 1 + p.extra_arrivals);
             mbar_init(smem_u32(&bar_free[b]), 2 * kReaders);
         }
         mbar_init(smem_u32(&bar_drain), 1);
@@ -619,7 +622,7 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
             const int ma = (int)(m * kTileM + rank * 128), nb = (int)(n * width + rank * 128);
             const uint32_t bytes = 2 * (two ? 3 : 2) * kOperandBytes;
             for (int k = k0; k < k1; ++k) {
-                if (!(ok = warp_wait(smem_u32(&bar_empty[stage]), phase ^ 1))) break;
+                if (!(ok = warp_wait(smem_u32(&bar_empty[stage]), phase ^ 1, p.wait_clocks))) break;
                 if (elected()) {
                     const uint32_t full = smem_u32(&bar_full[stage]);
                     if (rank == 0) mbar_expect(full, bytes);
@@ -651,7 +654,7 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
             }
         }
         if (!ok && rank == 0)   // the copies in flight land before the memory is given back
-            for (int s = 0; s < stages; ++s) mbar_wait(smem_u32(&bar_full[s]), s < stage ? phase : phase ^ 1);
+            for (int s = 0; s < stages; ++s) mbar_wait(smem_u32(&bar_full[s]), s < stage ? phase : phase ^ 1, p.wait_clocks);
     } else if (warp == 1) {
         if (rank == 0) {
             constexpr bool kMnB = P == kGrads;
@@ -689,7 +692,7 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                 int a = 0, b = 0;             // blocks issued for each half
                 int count = blocks;           // of a chunk
                 auto first_half = [&](int half, bool release) {
-                    ok = warp_wait(smem_u32(&bar_full[stage_a]), phase);
+                    ok = warp_wait(smem_u32(&bar_full[stage_a]), phase, p.wait_clocks);
                     if (!ok) return;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     if (elected()) {
@@ -713,7 +716,7 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                 };
                 // the first half's sums, or a narrow tile's, have been read out
                 auto wait_free = [&](int half) {
-                    ok = warp_wait(smem_u32(&bar_free[half]), (half ? free1 : free0) ^ 1);
+                    ok = warp_wait(smem_u32(&bar_free[half]), (half ? free1 : free0) ^ 1, p.wait_clocks);
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     if (half) free1 ^= 1;
                     else free0 ^= 1;
@@ -751,7 +754,7 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
             if (!ok) {   // products in flight end before the tensor memory is freed
                 if (elected()) commit_pair(smem_u32(&bar_drain));
                 __syncwarp();
-                mbar_wait(smem_u32(&bar_drain), 0);
+                mbar_wait(smem_u32(&bar_drain), 0, p.wait_clocks);
             }
         }
     } else if (warp >= 4) {
@@ -775,7 +778,7 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
             const uint32_t lanes = tmem + side * 128 + ((uint32_t)(quarter * 32) << 16);
             float v[128];
             auto wait_sums = [&](int h) {
-                ok = warp_wait(smem_u32(&bar_sum[h]), phases >> h & 1);
+                ok = warp_wait(smem_u32(&bar_sum[h]), phases >> h & 1, p.wait_clocks);
                 phases ^= 1u << h;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             };
@@ -968,6 +971,8 @@ static int launch(const VocabCall& c, int64_t v0, int64_t v1, bool first, int sm
     p.v1 = v1;
     p.narrow = 0;
     p.first = first;
+    p.extra_arrivals = host_knob(kKnobExtraArrivals) > 0 ? 1 : 0;
+    p.wait_clocks = p.extra_arrivals ? 1ll << 27 : kWaitClocks;
     p.splits = P == kGrads && c.splits > 0 ? c.splits : 1;
     p.direct = c.dhp == nullptr;
     // (the copies' hardware cuts a row's end in steps of 16 bytes, so the rows' length counts too)

@@ -200,15 +200,16 @@ __device__ __forceinline__ unsigned warp_search(unsigned t, int bit, int want, i
     for (; bit >= 0 && reach > most; bit -= 2) {
         const int low = bit > 0 ? bit - 1 : 0;
         const unsigned c1 = t | 1u << low, c2 = t | 1u << bit, c3 = c2 | 1u << low;
-        const unsigned c = __reduce_add_sync(0xffffffffu, count(c1, c2, c3));
-        const int n1 = (int)(c & 1023), n2 = (int)(c >> 10 & 1023), n3 = (int)(c >> 20);
+        const unsigned c = count(c1, c2, c3);
+        const int n1 = (int)__reduce_add_sync(0xffffffffu, c & 1023), n2 = (int)__reduce_add_sync(0xffffffffu, c >> 10 & 1023),
+                  n3 = (int)__reduce_add_sync(0xffffffffu, c >> 20);
         if (n3 >= want) { t = c3; reach = n3; }
         else if (n2 >= want) { t = c2; reach = n2; }
         else if (n1 >= want) { t = c1; reach = n1; }
     }
     return t;
 }
-constexpr int kFew = 768;      // keys one warp counts: its counts fit ten bits
+constexpr int kFew = 768;      // keys that one warp counts faster than all of them with barriers
 
 // keep_largest for up to kFew entries, by one warp, in the list's order.
 template <int THREADS>
