@@ -291,22 +291,26 @@ k_vocab_topk(const void* logits, int64_t ld, int64_t V, int K, float zscale, flo
     if (tid == 0) { sh.count = 0; sh.words = 0; }
 
     // Four words a thread at a time, from four places of the warp's share; the last THREADS words or fewer singly.
+    // A CTA that has its SM for itself (1024 threads) sends for eight words before the threshold is known; with four
+    // CTAs an SM that made the loop slower (4096 x 128000: 238 us, 312 so).
     constexpr int kWarps = THREADS / 32;
+    constexpr bool kLone = THREADS == 1024;
     const int share = words / THREADS, quarter = (share + 3) / 4;   // in steps of 32 words
     const uint4* own = body + wid * share * 32 + lane;
-    uint4 x[4];
+    uint4 x[4], next[4];
     auto fetch = [&](uint4 (&to)[4], int q) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             if (q < quarter && q + i * quarter < share) to[i] = __ldcs(own + (q + i * quarter) * 32);
     };
     fetch(x, 0);
+    if constexpr (kLone) fetch(next, 1);
 
     float tau = -INFINITY, m = -INFINITY, s = 0.f;
     if (V > kCap) {
         // The threshold.  With e of the row's k largest expected among the sample, the (e + 4 sqrt(e) + 4)-th largest
-        // of it is taken: about as many as k can hardly be above it.  Where that is a small part of the
-        // threads their maxima stand for the elements; the sample's largest are nearly always different threads'.
+        // of it is taken: about as many as k can hardly be above it.  Where that is a small part of 256, the maxima of
+        // 256 threads or groups of four stand for the elements; the sample's largest are nearly always different ones'.
         // (Elsewhere all but 16-bit types' fourth words count: a warp's count has to fit ten bits.)
         constexpr int kSample = TYPE == GK_TYPE_F32 ? 4 : 3;
         float top = -INFINITY;
@@ -325,7 +329,11 @@ k_vocab_topk(const void* logits, int64_t ld, int64_t V, int K, float zscale, flo
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
         if (lane == 0) sh.sampled[wid] = most;
-        sh.key[tid] = order_key(top);
+        if constexpr (THREADS == 1024) {
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        }
+        if (tid % (THREADS / 256) == 0) sh.key[tid / (THREADS / 256)] = order_key(top);
         __syncthreads();
         m = lane < kWarps ? sh.sampled[lane] : -INFINITY;
 #pragma unroll
@@ -334,10 +342,10 @@ k_vocab_topk(const void* logits, int64_t ld, int64_t V, int K, float zscale, flo
         float e = (float)K * (float)(steps * THREADS * kVec) / (float)V;
         int r = (int)(e + 4.f * sqrtf(e) + 4.f);
         unsigned t = 0;
-        if (r <= THREADS / 4) {
+        if (r <= 64) {
             if (wid == 0) {
                 // between the smallest and the largest of the maxima, which are kept in registers
-                constexpr int kOwn = THREADS / 32;
+                constexpr int kOwn = 256 / 32;
                 unsigned key[kOwn], least = 0xffffffffu;
 #pragma unroll
                 for (int j = 0; j < kOwn; ++j) {
@@ -347,7 +355,7 @@ k_vocab_topk(const void* logits, int64_t ld, int64_t V, int K, float zscale, flo
                 least = __reduce_min_sync(0xffffffffu, least);
                 const unsigned differ = least ^ order_key(m);
                 const int bit = differ ? 31 - __clz(differ) : -1;
-                int reach = THREADS;
+                int reach = 256;
                 t = warp_search(bit < 0 ? least : bit == 31 ? 0u : least >> (bit + 1) << (bit + 1), bit, r, r + r / 4, reach,
                                 [&](unsigned c1, unsigned c2, unsigned c3) {
                     unsigned c = 0;
@@ -438,10 +446,9 @@ k_vocab_topk(const void* logits, int64_t ld, int64_t V, int K, float zscale, flo
     };
     if (tid < head) single(tid);
     if (tid < V - head - (int64_t)words * kVec) single(head + (int64_t)words * kVec + tid);
-    // the next four words are on their way while four are looked at
+    // the next words are on their way while four are looked at
     for (int q = 0; q < quarter; ++q) {
-        uint4 next[4];
-        fetch(next, q + 1);
+        if (!kLone || q > 0) fetch(next, q + 1);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             if (q + i * quarter < share) word(x[i], (wid * share + q + i * quarter) * 32 + lane);
