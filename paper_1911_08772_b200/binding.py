@@ -359,7 +359,8 @@ def _head(h, w, loss_out, lse_out, row_grad, dh, dw, device):
 
 def _stream_of(device: int) -> int:
     import torch
-    return torch._C._cuda_getCurrentRawStream(device)
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)     # without the stream object where torch has the call
+    return raw(device) if raw is not None else int(torch.cuda.current_stream(device).cuda_stream)
 
 
 def gk_vocab_loss(h, w, target, loss_out, lse_out, row_grad=None, dh=None, dw=None, ignore_index: int = -100) -> None:

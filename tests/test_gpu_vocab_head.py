@@ -375,6 +375,64 @@ def test_the_same_call_gives_the_same_bits_on_any_stream_and_in_a_graph():
     assert same(third)
 
 
+@pytest.mark.parametrize("n,D,V,K", [(30, 64, 500, 1), (700, 1500, 10000, 1), (2100, 512, 9000, 40), (300, 136, 70001, 7)])
+def test_a_reserved_workspace_is_enough(n, D, V, K):
+    gen, h, w, hd, wd = make(n, D, V, torch.bfloat16, 42)
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        gk.gk_vocab_reserve(n, D, V, K, grad=True)
+        assert gk.gk_vocab_workspace_bytes(n, D, V, K) > 0
+        t_idx = torch.randint(0, V, (n, K), generator=gen).to(torch.int32).to(DEV)
+        t_val = torch.randn(n, K, generator=gen).to(DEV)
+        outs = [Out(n, D, V, torch.bfloat16, dh, dw, shift=shift) for dh, dw in ((True, True), (True, False), (False, True), (False, False))
+                for shift in (0, 1)]
+        stream.synchronize()
+        free = torch.cuda.mem_get_info()[0]
+        for out in outs:
+            gk.gk_vocab_distill(hd, wd, t_idx, t_val, out.loss[:n], out.lse[:n], dh=out.dh, dw=out.dw)
+        stream.synchronize()
+        assert torch.cuda.mem_get_info()[0] == free
+        assert gk.gk_vocab_last_info() == (0, n)
+
+
+def test_offsets_past_32_bits():
+    """2.5e9 logits in one piece: its bytes and its elements pass 2^32 and 2^31.  Some rows of dh and of dw
+    against 64 bits, taking every row's log-sum-exp from a sample of rows that is checked itself."""
+    n, D, V = 20000, 64, 125000
+    gen = torch.Generator(device=DEV).manual_seed(43)
+    h = torch.randn(n, D, generator=gen, device=DEV).bfloat16()
+    w = (torch.randn(V, D, generator=gen, device=DEV) / 4).bfloat16()
+    target = torch.randint(0, V, (n,), generator=gen, device=DEV)
+    loss, lse = torch.empty(n, device=DEV), torch.empty(n, device=DEV)
+    dh, dw = torch.empty_like(h), torch.empty_like(w)
+    g = torch.ones(n, device=DEV)
+    gk.gk_vocab_set_budget(6 << 30)
+    try:
+        gk.gk_vocab_loss(h, w, target, loss, lse, row_grad=g, dh=dh, dw=dw)
+        assert gk.gk_vocab_last_info() == (0, n)
+    finally:
+        gk.gk_vocab_set_budget(2 << 30)
+    rows = torch.cat([torch.arange(40), torch.arange(9990, 10030), torch.arange(n - 40, n)]).to(DEV)
+    hr, wd = h[rows], w
+    ref = head_reference(hr, wd, target[rows][:, None], torch.ones(len(rows), 1, dtype=torch.float64, device=DEV),
+                         torch.zeros(len(rows), 1, dtype=torch.float64, device=DEV), 1.0, torch.ones(len(rows), dtype=torch.float64, device=DEV))
+    one = torch.ones(len(rows), 1, dtype=torch.float64, device=DEV)
+    tol = bounds(hr, wd, ref, one, torch.zeros_like(one), 1.0, torch.bfloat16)
+    assert (loss[rows].double() - ref["loss"]).abs().max().item() <= tol["loss"]
+    assert (lse[rows].double() - ref["lse"]).abs().max().item() <= tol["lse"]
+    assert bool(((dh[rows].double() - ref["dh"]).abs() <= tol["dh"]).all())
+    # dw's rows need every row's probability of their word: from the log-sum-exps, whose bound is in lse_tol
+    words = torch.cat([torch.arange(20), torch.arange(62000, 62020), torch.arange(V - 20, V)]).to(DEV)
+    p = torch.exp(h.double() @ w[words].double().t() - lse.double()[:, None])
+    hard = (target[:, None] == words[None, :]).double()
+    dz, size = p - hard, p + hard
+    u = 2.0 ** -8
+    dz_tol = (2 * u * (1 + u) + 8 * tol["lse"]) * size
+    want = dz.t() @ h.double()
+    bound = (dz_tol + n * 2.0 ** -23 * (size + dz_tol)).t() @ h.double().abs()
+    assert bool(((dw[words].double() - want).abs() <= bound + u * (want.abs() + bound)).all())
+
+
 def test_a_logit_of_infinity_reaches_its_own_row_only():
     n, D, V = 9, 64, 300
     _, h, w, hd, wd = make(n, D, V, torch.bfloat16, 41)

@@ -109,6 +109,23 @@ def test_row_strides_and_unaligned_rows(pad, shift, dtype):
     check(z, 40, view=view)
 
 
+def test_offsets_past_32_bits():
+    n, V, k = 17000, 130001, 9          # 2.2e9 logits
+    gen = torch.Generator(device=DEV).manual_seed(7)
+    z = torch.empty(n, V, dtype=torch.bfloat16, device=DEV)
+    for a in range(0, n, 1000):
+        z[a:a + 1000] = torch.randn(1000, V, generator=gen, device=DEV).bfloat16()
+    idx, val, lse = torch.empty(n, k, dtype=torch.int32, device=DEV), torch.empty(n, k, device=DEV), torch.empty(n, device=DEV)
+    gk.gk_vocab_topk(z, k, idx, val, lse_out=lse)
+    for a in (0, 8000, n - 50):
+        rows = z[a:a + 50]
+        want = topk_reference(rows.cpu(), k)
+        assert torch.equal(idx[a:a + 50].cpu().long(), want)
+        assert torch.equal(val[a:a + 50].cpu(), torch.gather(rows.cpu().float(), 1, want))
+        ref = torch.logsumexp(rows.double(), 1)
+        assert bool(((lse[a:a + 50].double() - ref).abs() <= 2.0 ** -19 + 2.0 ** -21 * ref.abs()).all())
+
+
 def test_without_log_sum_exp_and_without_rows():
     z = torch.randn(3, 500, device=DEV)
     idx, val = torch.empty(3, 4, dtype=torch.int32, device=DEV), torch.empty(3, 4, device=DEV)
