@@ -1,6 +1,9 @@
 // Top logits of rows: what a teacher sends for distillation (include/gk.h: gk_vocab_topk).
 //
-// One CTA a row, one pass over it.  The floor is the row's bytes: 4096 x 128000 bf16 are 1.05 GB, 160 us.
+// One CTA a row, one pass over it.  The floor is the row's bytes: 4096 x 128000 bf16 are 1.05 GB, 160 us at the
+// rate of a copy; the call takes 234.  Of those the stream with its exponentials takes 165, the noting of words 25,
+// and 43 are selections that the other CTAs' streams do not hide (each of the three left out of a trial in turn).
+// More CTAs an SM, with fewer registers for words in flight, took 270 to 410.
 // Each warp streams a contiguous share of the row, four 16-byte words a thread at a time from four
 // places of the share.  The first four are the sample: 32 or more places spread over the row, from which a
 // threshold is taken that a little more than k elements are expected to reach.  The pass takes the
@@ -91,9 +94,12 @@ __device__ __forceinline__ void unpack(const uint4& x, float (&f)[TYPE == GK_TYP
 template <int THREADS>
 struct TopkShared {
     static constexpr int kCap = THREADS == 1024 ? 4096 : 3072;     // list entries
+    static constexpr int kWords = 2048, kData = THREADS == 1024 ? 448 : 896;
+    // the first of the noted words themselves: fetched again by number they cost 2000 x 100003 fp32 174 us, so 161
+    uint4 data[kData];
     unsigned key[kCap];
     alignas(16) int idx[kCap];
-    int word[2048];   // noted words
+    int word[kWords];           // noted words
     float m[THREADS / 32], s[THREADS / 32], sampled[THREADS / 32];
     float tau;
     int count;        // entries appended (may exceed the list)
@@ -284,7 +290,7 @@ k_vocab_topk(const void* logits, int64_t ld, int64_t V, int K, float zscale, flo
     const int words = (int)((V - head) / kVec);
     const uint4* body = (const uint4*)(row + head * kSize);
 
-    constexpr int kWords = 2048;
+    constexpr int kWords = TopkShared<THREADS>::kWords, kData = TopkShared<THREADS>::kData;
     // the low bits of a 16-bit type's keys follow from its sign
     constexpr int kDrop = TYPE == GK_TYPE_BF16 ? 16 : TYPE == GK_TYPE_F16 ? 13 : 0;
     const int index_bits = 32 - __clz((int)(V - 1) | 1);
@@ -292,7 +298,7 @@ k_vocab_topk(const void* logits, int64_t ld, int64_t V, int K, float zscale, flo
 
     // Four words a thread at a time, from four places of the warp's share; the last THREADS words or fewer singly.
     // A CTA that has its SM for itself (1024 threads) sends for eight words before the threshold is known; with four
-    // CTAs an SM that made the loop slower (4096 x 128000: 238 us, 312 so).
+    // CTAs an SM that made the loop slower (4096 x 128000: 234 us, 312 so).
     constexpr int kWarps = THREADS / 32;
     constexpr bool kLone = THREADS == 1024;
     const int share = words / THREADS, quarter = (share + 3) / 4;   // in steps of 32 words
@@ -428,6 +434,7 @@ k_vocab_topk(const void* logits, int64_t ld, int64_t V, int K, float zscale, flo
         if (!(g < tau)) {
             const int to = atomicAdd(&sh.words, 1);
             if (to < kWords) sh.word[to] = at;
+            if (to < kData) sh.data[to] = x;
             if (g > m) raise(g);
         }
         const uint64_t less = pair(-ref, -ref);
@@ -501,7 +508,7 @@ k_vocab_topk(const void* logits, int64_t ld, int64_t V, int K, float zscale, flo
         for (int j = tid; j < noted; j += THREADS) {
             const int w = sh.word[j];
             float f[kVec];
-            unpack<TYPE>(__ldg(body + w), f);
+            unpack<TYPE>(j < kData ? sh.data[j] : __ldg(body + w), f);
 #pragma unroll
             for (int i = 0; i < kVec; ++i)
                 if (!(f[i] < tau)) append(f[i], head + (int64_t)w * kVec + i);
