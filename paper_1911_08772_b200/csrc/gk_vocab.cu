@@ -52,13 +52,11 @@ __device__ __forceinline__ float warp_max_f(float v) {
 }
 
 // ---------------------------------------------------------------------------
-// 1. Teacher probabilities, one warp a row.
+// 1. Teacher probabilities, one warp a row, and of rows in ascending order which pairs are in which tile of the
+// vocabulary.
 // ---------------------------------------------------------------------------
-__global__ void __launch_bounds__(256) k_vocab_teacher(VocabCall c) {
-    after_previous();
-    const int64_t r = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-    const int lane = threadIdx.x & 31;
-    if (r >= c.n) return;
+// `place`: the pairs' indices, those left out above all; `held`: how many, none where they do not ascend.
+__device__ __forceinline__ void teacher_row(const VocabCall& c, int64_t r, int lane, int* place, int& held) {
     const int32_t* ti = c.t_idx + r * c.K;
     const float* tv = c.t_val + r * c.K;
     // the largest logit is taken off before the division by T, so that masks of the type's lowest
@@ -74,6 +72,7 @@ __global__ void __launch_bounds__(256) k_vocab_teacher(VocabCall c) {
             top = fmaxf(top, t);
         }
         if (in && j > 0 && (before >= i || before < 0)) ascending = false;
+        place[j] = in ? i : 0x7fffffff;
     }
     any = __any_sync(0xffffffffu, any);
     ascending = __all_sync(0xffffffffu, ascending);
@@ -97,7 +96,35 @@ __global__ void __launch_bounds__(256) k_vocab_teacher(VocabCall c) {
         Q += q;
     }
     Q = warp_sum_f(Q);
-    if (lane == 0) c.teacher[r] = make_float4(Q, L, top, (float)((ascending ? 1 : 0) + (any ? 2 : 0)));
+    if (lane == 0) {
+        held = ascending ? c.K : 0;
+        c.teacher[r] = make_float4(Q, L, top, (float)((ascending ? 1 : 0) + (any ? 2 : 0)));
+    }
+}
+__global__ void __launch_bounds__(256) k_vocab_teacher(VocabCall c) {
+    __shared__ int place[8][kVocabMaxPairs + 1];      // (the odd pitch: eight rows at one place are in eight banks)
+    __shared__ int held[8];
+    after_previous();
+    const int wid = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int64_t r = (int64_t)blockIdx.x * 8 + wid;
+    if (r < c.n) teacher_row(c, r, lane, place[wid], held[wid]);
+    else if (lane == 0) held[wid] = 0;
+    __syncthreads();
+    // eight rows' entries of a tile are one 32-byte sector
+    const int row = threadIdx.x & 7, n = held[row];
+    const int64_t tiles = (c.V + kVocabTile - 1) / kVocabTile;
+    for (int64_t t = threadIdx.x >> 3; t < tiles; t += 32) {
+        const int from = (int)t * kVocabTile;
+        int lo = 0, hi = n;
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (place[row][mid] < from) lo = mid + 1;
+            else hi = mid;
+        }
+        int end = lo;
+        while (end < n && place[row][end] < from + kVocabTile) ++end;
+        c.pairs_in[t * c.n_pad + (int64_t)blockIdx.x * 8 + row] = (unsigned)lo | (unsigned)(end - lo) << 16;
+    }
 }
 
 // ---------------------------------------------------------------------------
@@ -608,6 +635,7 @@ static size_t lay_out(VocabCall& c, bool distill, bool copy_w, char* base) {
     c.at_of = (int32_t*)take(4 * n);
     c.q = (float*)(distill ? take(4 * n * K) : nullptr);
     c.teacher = (float4*)(distill ? take(16 * n) : nullptr);
+    c.pairs_in = (unsigned*)(distill ? take(4 * tiles * np) : nullptr);
     c.hc = (uint16_t*)take(2 * np * c.Dp);
     c.wc = (uint16_t*)(copy_w ? take(2 * (size_t)c.V * c.Dp) : nullptr);
     c.zt = (float*)take(4 * np * K);

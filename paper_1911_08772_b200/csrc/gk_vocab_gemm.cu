@@ -242,36 +242,31 @@ struct Patch {
     int64_t row0;        // of the warp; the thread's row is row0 + lane
     int64_t col0;        // of the 128
     int64_t cols;        // columns of the result from col0 on (may be more than 128, or none)
-    int cursor;          // kLogits, kLogitsKeep with a teacher: the row's first pair at or after col0
+    int pair, pairs_end;     // kLogits, kLogitsKeep with a teacher: the row's pairs in the 128 columns
+    int next;                // column of the first
 };
 
 // A row's teacher pairs in ascending order are met one patch of columns at a time: the logit at each is
-// taken as it passes, instead of by a dot product of its own.  first_pair runs while the patch is still being
-// summed.
-__device__ __forceinline__ int pair_index(const VocabCall& c, const int32_t* pairs, int j) {
-    const int32_t i = j < c.K ? __ldg(pairs + j) : -1;
-    return i < 0 || i >= c.V ? 0x7fffffff : i;     // pairs left out are at the end of an ascending row
-}
-__device__ __forceinline__ int first_pair(const VocabCall& c, int64_t row, int n_valid, int64_t col0) {
-    if (row >= n_valid) return c.K;
-    const int64_t r = c.row_of[row];
-    if (!teacher_ascending(c.teacher[r])) return c.K;     // this row's logits are dot products
-    const int32_t* pairs = c.t_idx + r * c.K;
-    int lo = 0, hi = c.K;
-    while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (pair_index(c, pairs, mid) < col0) lo = mid + 1;
-        else hi = mid;
-    }
-    return lo;
+// taken as it passes, instead of by a dot product of its own.  Where they are, find_pairs learns while the patch is
+// still being summed, from a table that k_vocab_teacher made (searching the row's pairs instead, six dependent
+// loads by 32 rows apart, took 2048 x 2048 x 32000 with 64 pairs 746 us a call, the table 722).
+__device__ __forceinline__ void find_pairs(const VocabCall& c, Patch& w, int n_valid) {
+    const int64_t row = w.row0 + w.lane;
+    w.pair = w.pairs_end = 0;
+    w.next = 0x7fffffff;
+    if (row >= n_valid) return;
+    const int32_t r = c.row_of[row];
+    const unsigned x = c.pairs_in[w.col0 / kVocabTile * c.n_pad + r];
+    w.pair = (int)(x & 0xffff);
+    w.pairs_end = w.pair + (int)(x >> 16);
+    if (x >> 16) w.next = __ldg(c.t_idx + (int64_t)r * c.K + w.pair);
 }
 // `v`: the patch's columns; a register cannot be chosen at run time, so stretches of 32 columns with a pair in
 // any of the warp's rows go through the staging memory.
 __device__ __forceinline__ void take_pairs(const VocabCall& c, const Patch& w, int n_valid, const float (&v)[128]) {
     const int64_t row = w.row0 + w.lane;
     const int32_t* pairs = row < n_valid ? c.t_idx + (int64_t)c.row_of[row] * c.K : nullptr;
-    int j = w.cursor;
-    int next = j < c.K ? pair_index(c, pairs, j) : 0x7fffffff;
+    int j = w.pair, next = w.next;
 #pragma unroll
     for (int part = 0; part < 4; ++part) {
         const int from = (int)w.col0 + part * 32;
@@ -290,7 +285,7 @@ __device__ __forceinline__ void take_pairs(const VocabCall& c, const Patch& w, i
                              : "=f"(z) : "r"(w.staging + w.lane * 128 + (((col >> 2) ^ (w.lane & 7)) << 4) + (col & 3) * 4) : "memory");
                 c.zt[row * c.K + j] = z;
                 ++j;
-                next = j < c.K ? pair_index(c, pairs, j) : 0x7fffffff;
+                next = j < w.pairs_end ? __ldg(pairs + j) : 0x7fffffff;
             }
             __syncwarp();
         }
@@ -792,7 +787,7 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                 w.cols = n_cols - col;
                 w.col0 = p.v0 + col;
                 const bool used = used_rows && w.cols > 0, pairs = P != kAgain && c.t_idx && used && w.row0 < n_valid;
-                if (pairs) w.cursor = first_pair(c, w.row0 + lane, n_valid, w.col0);
+                if (pairs) find_pairs(c, w, n_valid);
                 for (int done = 0; done < k1 - k0; done += kChunk) {
                     wait_sums(only);
                     if (!ok) break;
