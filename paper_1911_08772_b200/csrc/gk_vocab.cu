@@ -233,9 +233,8 @@ __global__ void __launch_bounds__(1024) k_vocab_rows(VocabCall c) {
 
 // ---------------------------------------------------------------------------
 // 2. Compact rows of h (padded with zeros to the pitch, and zero rows to a multiple of 256, which
-// the products read) and the logits at the targets that the products do not deliver: the class, or
-// of a teacher's pairs the largest, which is the row's reference, and all of a row in no order.  One
-// CTA a row, one warp a dot product.
+// the products read) and the logits at the targets that the products do not deliver: the class, or all pairs
+// of a teacher's row in no order.  One CTA a row.
 // ---------------------------------------------------------------------------
 
 // Eight values from 2-byte-aligned memory, zero from `left` on.
@@ -256,6 +255,18 @@ __device__ __forceinline__ uint4 load8(const uint16_t* p, int64_t left) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = i < left ? __ldg(p + i) : 0u;
     return make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
+}
+
+// s plus eight products.
+template <bool F16>
+__device__ __forceinline__ float dot8(const uint4& x, const uint4& y, float s) {
+    const unsigned xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        s = fmaf(from16<F16>((uint16_t)xs[q]), from16<F16>((uint16_t)ys[q]), s);
+        s = fmaf(from16<F16>((uint16_t)(xs[q] >> 16)), from16<F16>((uint16_t)(ys[q] >> 16)), s);
+    }
+    return s;
 }
 
 // RANK (few rows): each CTA takes a row of the caller's and finds its number itself, by looking at all rows
@@ -283,6 +294,7 @@ __global__ void __launch_bounds__(128) k_vocab_gather(VocabCall c) {
     int at = blockIdx.x, n_valid;
     int64_t r;
     bool left_out;
+    __shared__ float sums[4];
     if constexpr (RANK) {
         r = blockIdx.x;
         int before = 0, all = 0;
@@ -319,6 +331,7 @@ __global__ void __launch_bounds__(128) k_vocab_gather(VocabCall c) {
         if (r >= n_valid && r < round_up(n_valid, kVocabRowPad))
             for (int64_t i = tid; i < c.Dp / 8; i += 128) ((uint4*)(c.hc + r * c.Dp))[i] = make_uint4(0, 0, 0, 0);
     } else {
+        r = c.row_of[at < c.n ? at : 0];       // a row of the call where at < n_valid
         n_valid = c.ctl->n_valid;
         left_out = at < c.n && c.at_of[at] < 0;
     }
@@ -335,32 +348,34 @@ __global__ void __launch_bounds__(128) k_vocab_gather(VocabCall c) {
             for (int64_t i = tid; i < c.Dp / 8; i += 128) ((uint4*)to)[i] = make_uint4(0, 0, 0, 0);
             return;
         }
-        r = c.row_of[at];
     }
     const uint16_t* from = (const uint16_t*)c.h + r * c.ldh;
-    for (int64_t i = tid; i < c.Dp / 8; i += 128) ((uint4*)to)[i] = load8(from + i * 8, c.D - i * 8);
-    int last = 1;
-    if (!c.target) {
-        const float4 te = c.teacher[r];
-        last = teacher_ascending(te) ? 0 : c.K;
+    const int64_t words = c.Dp / 8;
+    if (c.target) {
+        // the row that is copied and its class's row of w, fetched together
+        const uint16_t* wr = (const uint16_t*)c.w + c.target[r] * c.ldw;
+        float s = 0.f;
+#pragma unroll 2
+        for (int64_t i = tid; i < words; i += 128) {
+            const uint4 x = load8(from + i * 8, c.D - i * 8), y = load8(wr + i * 8, c.D - i * 8);
+            ((uint4*)to)[i] = x;
+            s = dot8<F16>(x, y, s);
+        }
+        s = warp_sum_f(s);
+        if (lane == 0) sums[tid >> 5] = s;
+        __syncthreads();
+        if (tid == 0) c.zt[at] = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+        return;
     }
+    for (int64_t i = tid; i < words; i += 128) ((uint4*)to)[i] = load8(from + i * 8, c.D - i * 8);
+    if (teacher_ascending(c.teacher[r])) return;
     __syncthreads();
-    const int64_t words = (c.D + 7) / 8;
-    for (int j = tid >> 5; j < last; j += 4) {
-        const int64_t v = c.target ? c.target[r] : (int64_t)c.t_idx[r * c.K + j];
+    for (int j = tid >> 5; j < c.K; j += 4) {
+        const int64_t v = c.t_idx[r * c.K + j];
         float s = 0.f;
         if (v >= 0 && v < c.V) {
             const uint16_t* wr = (const uint16_t*)c.w + v * c.ldw;
-            for (int64_t b = lane; b < words; b += 32) {
-                const uint4 x = ((const uint4*)to)[b];
-                const uint4 y = load8(wr + b * 8, c.D - b * 8);
-                const unsigned xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    s = fmaf(from16<F16>((uint16_t)xs[q]), from16<F16>((uint16_t)ys[q]), s);
-                    s = fmaf(from16<F16>((uint16_t)(xs[q] >> 16)), from16<F16>((uint16_t)(ys[q] >> 16)), s);
-                }
-            }
+            for (int64_t b = lane; b < words; b += 32) s = dot8<F16>(((const uint4*)to)[b], load8(wr + b * 8, c.D - b * 8), s);
         }
         s = warp_sum_f(s);
         if (lane == 0) c.zt[(int64_t)at * c.K + j] = s;
@@ -372,33 +387,44 @@ __global__ void __launch_bounds__(128) k_vocab_gather(VocabCall c) {
 // joins them, and each warp finishes a row.
 // ---------------------------------------------------------------------------
 
+// What a row's end needs besides its log-sum-exp; fetched while that is still being summed.
+struct RowEnd {
+    int64_t r;
+    float g, z;      // its gradient's coefficient; with a class its raw logit
+    float4 te;
+};
+__device__ __forceinline__ RowEnd fetch_end(const VocabCall& c, int64_t at, int64_t r, int n_valid) {
+    RowEnd e;
+    e.r = r;
+    e.g = c.row_grad ? c.row_grad[r] : 1.f / (float)n_valid;
+    e.z = c.target ? c.zt[at] : 0.f;
+    e.te = c.target ? make_float4(1.f, 0.f, 0.f, 0.f) : c.teacher[r];
+    return e;
+}
 // A row from its log-sum-exp, by one warp: its loss (write) and what the gradients need of it.
-__device__ __forceinline__ VocabRow finish_row(const VocabCall& c, int64_t at, int n_valid, float lse2, int lane, bool write) {
-    const int64_t r = c.row_of[at];
-    float Q = 1.f, loss = 0.f;
-    if (c.target) {
-        if (write) loss = (lse2 - c.zt[at] * c.zscale) * kLn2;
-    } else {
-        const float4 te = c.teacher[r];
-        Q = te.x;
-        if (write) {
+__device__ __forceinline__ VocabRow finish_row(const VocabCall& c, int64_t at, const RowEnd& e, float lse2, int lane, bool write) {
+    if (write) {
+        float loss;
+        if (c.target) {
+            loss = (lse2 - e.z * c.zscale) * kLn2;
+        } else {
             float sum = 0.f;
             for (int j = lane; j < c.K; j += 32) {
-                const float q = c.q[r * c.K + j];
-                if (q > 0.f) sum += q * (((c.t_val[r * c.K + j] - te.z) * c.inv_T - te.y) + (lse2 - c.zt[at * c.K + j] * c.zscale) * kLn2);
+                const float q = c.q[e.r * c.K + j];
+                if (q > 0.f) sum += q * (((c.t_val[e.r * c.K + j] - e.te.z) * c.inv_T - e.te.y) + (lse2 - c.zt[at * c.K + j] * c.zscale) * kLn2);
                 else if (q != q) sum = q;
             }
             loss = warp_sum_f(sum);
         }
-    }
-    if (write && lane == 0) {
-        c.loss[r] = loss;
-        c.lse[r] = lse2 * kLn2;
+        if (lane == 0) {
+            c.loss[e.r] = loss;
+            c.lse[e.r] = lse2 * kLn2;
+        }
     }
     VocabRow out;
-    out.unit = c.ctl->scale * ((c.row_grad ? c.row_grad[r] : 1.f / (float)n_valid) * c.inv_T);
+    out.unit = c.ctl->scale * (e.g * c.inv_T);
     out.lse2 = lse2;
-    out.coef = out.unit * Q;
+    out.coef = out.unit * e.te.x;
     out.pad = 0.f;
     return out;
 }
@@ -415,6 +441,8 @@ __global__ void __launch_bounds__(1024) k_vocab_rows_done(VocabCall c) {
     const int rows = (int)(n_valid - at0 < 32 ? n_valid - at0 : 32);
     const int pitch = rows > 16 ? 32 : rows > 8 ? 16 : rows > 4 ? 8 : rows > 2 ? 4 : rows;
     const int mine = lane % pitch, share = lane / pitch, shares = 32 / pitch;
+    const int64_t at = at0 + wid;
+    const int32_t r = at < n_valid ? c.row_of[at] : 0;
     float m = -INFINITY, s = 0.f;
     if (mine < rows) {
         const float2* p = c.part + at0 + mine;
@@ -433,8 +461,9 @@ __global__ void __launch_bounds__(1024) k_vocab_rows_done(VocabCall c) {
     }
     sm[wid][lane] = m;
     ss[wid][lane] = s;
+    RowEnd end = {};
+    if (at < n_valid) end = fetch_end(c, at, r, n_valid);
     __syncthreads();
-    const int64_t at = at0 + wid;
     if (at >= n_valid) return;
     m = sm[lane][wid];
     s = ss[lane][wid];
@@ -447,7 +476,7 @@ __global__ void __launch_bounds__(1024) k_vocab_rows_done(VocabCall c) {
         m = ml;
         s = sl;
     }
-    const VocabRow out = finish_row(c, at, n_valid, m + log2f(s), lane, true);
+    const VocabRow out = finish_row(c, at, end, m + log2f(s), lane, true);
     if (lane == 0) c.row[at] = out;
 }
 
@@ -488,8 +517,8 @@ constexpr int64_t kOwnTiles = 128;   // tiles a CTA joins itself
 // for the rows up to the padding, which the product for dw sums over.  DONE (vocabularies of up to
 // 128 tiles): each CTA joins the row's tiles itself, and the first of a row writes its loss, instead
 // of a launch of its own before this one.  All of a thread's words are on their way before anything that they
-// wait for is looked at: a CTA's time is a few memory latencies, whatever it moves (8192 x 128000: 1050 us with half
-// as many words and those after the row's values).
+// wait for is looked at.  Bound by memory: 4096 x 64000, 524 MB read and as many written, takes 174 us by itself,
+// 6.0 TB/s.
 template <bool DONE>
 constexpr int kScaleWords = DONE ? 2 : 4;                                  // 16-byte words a thread
 template <bool DONE>
@@ -527,6 +556,7 @@ __global__ void __launch_bounds__(256) k_vocab_scale(VocabCall c, int64_t v0, in
     if constexpr (DONE) {
         const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
         const int64_t tiles = (c.V + kVocabTile - 1) / kVocabTile;
+        const RowEnd end = fetch_end(c, at, r, n_valid);
         float m = -INFINITY, s = 0.f;
         if (wid < 4) {
             if (tid < tiles) {
@@ -549,7 +579,7 @@ __global__ void __launch_bounds__(256) k_vocab_scale(VocabCall c, int64_t v0, in
         s = ss[0];
 #pragma unroll
         for (int k = 1; k < 4; ++k) join_max_sum(m, s, sm[k], ss[k]);
-        vr = finish_row(c, at, n_valid, m + log2f(s), lane, blockIdx.y == 0 && wid == 0);
+        vr = finish_row(c, at, end, m + log2f(s), lane, blockIdx.y == 0 && wid == 0);
         if (blockIdx.y == 0 && tid == 0) c.row[at] = vr;
     } else {
         vr = c.row[at];

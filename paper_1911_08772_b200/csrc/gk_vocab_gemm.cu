@@ -1,20 +1,22 @@
 // The products of the vocabulary head (gk_vocab.cu) on the fifth-generation tensor cores.
 //
-// One persistent kernel and its uses.  A pair of SMs (a cluster of two CTAs) computes a
-// 256 x 512 tile of the result with tcgen05.mma.cta_group::2, as two 256 x 256 halves: each CTA holds
-// 128 rows of A, 128 of the 256 columns of each half of B, and 128 x 512 fp32 sums, which is all of its
-// tensor memory.  Operands arrive by TMA in blocks of 64 along the summed axis, four blocks in
-// flight (48 KB each and CTA).  A tile half as wide with double-buffered sums needs 64 bytes a clock
-// and SM from L2 to keep the tensor pipe fed and kept it 81 % busy (ncu, 4096 x 4096 x 32000); this one
-// needs 48.
+// One persistent kernel and its uses.  A pair of SMs (a cluster of two CTAs) computes a tile of 256 rows of the
+// result with tcgen05.mma.cta_group::2; each CTA holds 128 rows of A, half of the tile's rows of B, and the fp32 sums
+// of its 128 rows in tensor memory.  Operands arrive by TMA in blocks of 64 along the summed axis, 192 KB of them in
+// flight a CTA.  One warp sends for blocks, one issues products, eight read the sums out.  Bound by the tensor
+// pipes, and those by the power limit: 4096 x 2048 x 50000 kept them 95 % busy, logits and gradients alike, at
+// 1.4 to 1.5 GHz.
 //
-// The sums are not double buffered.  Instead the two halves of a tile are summed out of step at its
-// ends: the first half is ahead by up to four blocks at the end of a tile, so that it is read out while
-// the second half catches up, and again at the start of the next tile, while the second half is
-// read out.  Eight warps read out: four for the lanes, two for the columns of a half.
+// Narrow tiles (256 columns, six blocks of 32 KB in flight): one half of the tensor memory is summed into while
+// the other is read out.  Logits always are; they are summed in chunks (kChunk), which take turns on the halves.
+// Wide tiles (512 columns, four blocks of 48 KB, three quarters of the bytes a product): gradients where
+// launch_time expects them to be faster; 8192 x 4096 x 128000 took 20.2 ms a call with them, 23.0 with narrow
+// ones.  Their sums take all of the tensor memory, so the two halves of a tile are summed out of step at its
+// ends: the first is ahead by up to four blocks at the end of a tile, so that it is read out while
+// the second catches up, and again at the start of the next tile, while the second is read out.  (The logits
+// of 4096 x 4096 x 32000 took 713 us in wide tiles and 749 in narrow ones, when they were not summed in chunks.)
 //
-// Logits, and gradients where they fill the SMs better, are 256 x 256 tiles: six blocks of 32 KB in flight, one half
-// of the tensor memory summing while the other is read out.
+// The readers copy 128 columns of 32 rows to registers and give the tensor memory back before they work on them.
 //
 //   use          A (M x K)            B (N x K)            what the readout does
 //   kLogits      hc  rows x D         w   columns x D      maximum and sum of 128 columns per row
@@ -28,7 +30,7 @@
 // e, hc and w are stored once, by rows; where the summed axis is not the contiguous one the
 // operand is read as it lies (MN-major descriptors) instead of being transposed in memory.
 // Results leave through shared memory, 32 rows x 128 bytes a warp, as TMA stores: a thread has a row of
-// its own, and stores of 16 bytes to 32 rows at once would take the time of 32.
+// its own, and a store by all of them would be to 32 rows at once.
 #include <cuda.h>
 
 #include <atomic>
@@ -43,8 +45,10 @@ constexpr int kTileM = 256, kHalfN = 256, kTileN = 2 * kHalfN, kBlockK = 64;
 constexpr int kOperandBytes = 128 * kBlockK * 2;            // a CTA's share of A, or of a half of B, in a block
 constexpr int kBlockBytes = 12 * kOperandBytes;             // four blocks of a wide tile, six of a narrow one
 constexpr int kMaxStages = 6;
-// Logits are summed over 12 blocks (768 of D) at a time in tensor memory, whose sums are cut, not rounded, and
-// added up in fp32 registers: over 4096 at once they were low by 3.4e-6 of themselves, log-sum-exps with them.
+// Logits are summed over 12 blocks (768 of D) at a time in tensor memory, and the chunks are added up in fp32
+// registers: the tensor memory's sums are not rounded to nearest but lean one way, by more the longer they are.
+// Losses and log-sum-exps of 8192 x 4096 x 128000 were off by up to 3.4e-6 of the largest in one piece, and are
+// by 3e-7 to 6e-7, as a sum in fp32 is.  (dh and dw are rounded to 16 bits, which hides it.)
 constexpr int kChunk = 12;
 constexpr int kReaders = 8;                                 // warps that read the sums out
 constexpr int kStagingBytes = 32 * 128;                     // of each of them
@@ -110,10 +114,9 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, long lo
     }
     return false;
 }
-// The whole warp waits and the outcome is a vote: with loops over values that the compiler knows to
-// be the same in all lanes, and one elected lane only for the instructions themselves, their
-// operands stay in uniform registers.  (A loop run by lane 0 alone moved six operands per product out
-// of ordinary registers and could not keep the tensor pipe fed: 61 % busy, 4096 x 4096 x 32000.)
+// The whole warp waits and the outcome is a vote: the loops run over values that the compiler knows to be the
+// same in all lanes, and one elected lane only issues.  (Loops run by lane 0 alone could not keep the tensor pipe
+// fed: 61 % busy, 4096 x 4096 x 32000.)
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, long long limit) {
     return __all_sync(0xffffffffu, mbar_wait(bar, parity, limit));
 }
@@ -293,7 +296,7 @@ __device__ __forceinline__ void take_pairs(const VocabCall& c, const Patch& w, i
 }
 
 // The readers work on 128 columns in registers: the tensor memory is free for the next tile's sums as soon as
-// it has been copied (a wide tile of 32 blocks took 24.2 us when it was read out column by column, 17.5 of them
+// it has been copied (read out 16 columns at a time, a wide tile of 32 blocks took 24.2 us, 17.5 of them
 // sums).  Columns past the result's end hold -inf in the uses that make logits.
 template <int P, bool F16>
 __device__ __forceinline__ void read_logits(const ProductArgs& p, const Patch& w, const CUtensorMap* out, int n_valid, float (&v)[128]) {
@@ -355,7 +358,9 @@ __device__ __forceinline__ void read_gradients(const ProductArgs& p, const Patch
 }
 
 // A warp's 32 rows x 64 16-bit columns from its staging memory to rows on boundaries of VEC values, VEC a lane:
-// one row at a time by two values, two by four, four by eight; four steps' loads go before their stores.
+// one row at a time by two values, two by four, four by eight; four steps' loads go before their stores.  The
+// widest that the rows allow: with the 3000-byte rows of 700 x 1500 x 10000, both gradients took 62 us by two
+// values and 50 by four.
 // `to`: column 0 of the 64 in the result's row 0; `row`: the thread's own row there, -1: nowhere.
 template <int VEC>
 __device__ __forceinline__ void store_rows(uint32_t staging, int lane, uint16_t* to, int64_t ld, int row, int64_t cols) {
@@ -890,8 +895,9 @@ static int make_map(CUtensorMap* map, Element type, const void* base, int64_t co
 // and 4 us to fill and empty.  A tile takes its blocks of 64 or its readout, whichever is longer, and what of
 // them does not overlap.  As measured: a block 0.60 us in a wide tile, 0.34 in a
 // narrow one; a readout 6 and 3.4 us, by rows that do not start on 16 bytes 10 and 5.  Whole calls with wide and with
-// narrow tiles for the gradients: 8192 x 4096 x 128000 20160 : 22950 us, 1024 x 1024 x 32000 216 : 215, 300 x 512 x 20000 75 : 63.  The first kind of tile (dh's, in `splits` parts) is dealt out before the second (dw's),
-// which evens the shares out.
+// narrow tiles for the gradients: 8192 x 4096 x 128000 20160 : 22950 us, 1024 x 1024 x 32000 216 : 215,
+// 300 x 512 x 20000 75 : 63.  The first kind of tile (dh's, in `splits` parts) is dealt out before the second
+// (dw's), which evens the shares out.
 struct Share {
     int64_t rows, cols, kb;
     bool unaligned;
