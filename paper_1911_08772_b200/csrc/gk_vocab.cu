@@ -128,9 +128,10 @@ __global__ void __launch_bounds__(256) k_vocab_teacher(VocabCall c) {
 }
 
 // ---------------------------------------------------------------------------
-// The rows that count, numbered in their order, and the power of two that brings the gradients' largest
-// row coefficient to [1, 2) (bf16) or [1024, 2048) (fp16, whose smallest step is 2^-24: an entry 2^-34 of the
-// largest is still held).
+// The rows that count, numbered in their order, and the scale that brings the gradients' largest row
+// coefficient to 2 (bf16) or 2048 (fp16, whose smallest step is 2^-24: an entry 2^-34 of the largest is still
+// held).  A row that has learned little has an entry of nearly its whole coefficient, and the rounding to 16 bits
+// is finest, relative to the value, just below a power of two.
 // ---------------------------------------------------------------------------
 
 // Whether row r counts, and the magnitude of its gradient's coefficient (times T).
@@ -158,12 +159,13 @@ __device__ __forceinline__ void write_ctl(const VocabCall& c, int n_valid, float
     if (!c.row_grad && n_valid > 0) top /= (float)n_valid;
     top *= c.inv_T;
     int e = 0;
-    if (top > 0.f && top < INFINITY) frexpf(top, &e);   // top in [2^(e-1), 2^e)
+    float part = 1.f;
+    if (top > 0.f && top < INFINITY) part = frexpf(top, &e);   // top = part 2^e
     e = min(max((c.f16 ? 11 : 1) - e, -100), 100);
     c.ctl->n_valid = n_valid;
     c.ctl->status = 0;
-    c.ctl->scale = ldexpf(1.f, e);
-    c.ctl->inv_scale = ldexpf(1.f, -e);
+    c.ctl->scale = ldexpf(1.f, e) / part;
+    c.ctl->inv_scale = ldexpf(part, -e);
 }
 
 // By one CTA, 8192 rows at a time: all loads first, then one scan over the 256 counts of (32 rows).

@@ -18,7 +18,7 @@ constexpr int kVocabMaxPairs = 1024;    // largest K of gk_vocab_distill and gk_
 struct VocabCtl {
     int n_valid;           // rows that count
     unsigned int status;   // GK_DEV_* flags
-    float scale;           // power of two that brings the largest row coefficient to the 16-bit type's range
+    float scale;           // brings the largest row coefficient to a power of two in the 16-bit type's range
     float inv_scale;
 };
 

@@ -270,7 +270,7 @@ def test_classes_far_below_the_rest(low, budget):
 
 @pytest.mark.parametrize("scale", [1e-6, 1e5])
 def test_gradients_of_rows_of_any_size(scale):
-    """Row gradients far from 1: the 16-bit logit gradients are scaled by a power of two."""
+    """Row gradients far from 1: the 16-bit logit gradients are scaled to their type's range."""
     distill(150, 96, 700, 12, torch.bfloat16, seed=24, scale=scale)
     if scale > 1:
         scale = 100.0       # fp16 results end at 65504
