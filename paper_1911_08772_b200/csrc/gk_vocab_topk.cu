@@ -93,7 +93,7 @@ __device__ __forceinline__ void unpack(const uint4& x, float (&f)[TYPE == GK_TYP
 // others' streams; by 1024 threads where there are fewer rows than SMs and the rows are long.
 template <int THREADS>
 struct TopkShared {
-    static constexpr int kCap = THREADS == 1024 ? 4096 : 3072;     // list entries
+    static constexpr int kCap = (THREADS == 1024 ? 4 : 12) * THREADS;     // list entries
     static constexpr int kWords = 2048, kData = THREADS == 1024 ? 448 : 896;
     // the first of the noted words themselves: fetched again by number they cost 2000 x 100003 fp32 174 us, so 161
     uint4 data[kData];
