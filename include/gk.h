@@ -346,7 +346,7 @@ int gk_set_params(int unbiased_std, int max_rounds);
  * call that does not fit replaces the workspace).  The
  * largest part, with gradients, is one piece of the vocabulary as n rows of 16-bit values, bounded by
  * gk_vocab_set_budget; of a vocabulary that does not fit one piece the product h w^T is taken twice.
- * Memory for 8 bytes a row and 128 columns is needed beside it.
+ * Memory for 8 bytes a row and 128 columns (12 for gk_vocab_distill) is needed beside it.
  */
 int gk_vocab_loss(const void* h, int64_t ldh, const void* w, int64_t ldw, int32_t dtype, int64_t n, int64_t D,
                   int64_t V, const int64_t* target, int64_t ignore_index, const float* row_grad, float* loss_out,

@@ -31,6 +31,7 @@
 #include <atomic>
 #include <map>
 #include <mutex>
+#include <new>
 #include <utility>
 
 #include "gk_vocab.cuh"
@@ -679,7 +680,8 @@ static size_t lay_out(VocabCall& c, bool distill, bool copy_w, char* base) {
     return at;
 }
 
-static int vocab_workspace(size_t bytes, cudaStream_t st, VocabWorkspace** out) {
+// (no exception passes a C entry: the map's memory is the only source of one)
+static int vocab_workspace(size_t bytes, cudaStream_t st, VocabWorkspace** out) try {
     int dev = 0;
     GK_CUDA_TRY(cudaGetDevice(&dev));
     std::lock_guard<std::mutex> lock(g_vocab_mu);
@@ -699,6 +701,8 @@ static int vocab_workspace(size_t bytes, cudaStream_t st, VocabWorkspace** out) 
     if (ws.sm_count == 0) GK_CUDA_TRY(cudaDeviceGetAttribute(&ws.sm_count, cudaDevAttrMultiProcessorCount, dev));
     *out = &ws;
     return GK_OK;
+} catch (const std::bad_alloc&) {
+    return GK_ERR_NOMEM;
 }
 
 static void size_call(VocabCall& c, bool want_dh, DwRows dw, int sm_count) {
