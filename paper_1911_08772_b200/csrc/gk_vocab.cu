@@ -10,10 +10,10 @@
 //
 // One call:
 //   1. (distill) the teacher's probabilities; the rows that count, numbered in their order;
-//   2. those rows of h copied together, and the logit at the target as a dot product;
+//   2. those rows of h copied together;
 //   3. logits tile by tile, of which each row keeps the sums of the exponentials, and for the first
 //      piece of the vocabulary (all of it where the budget allows) something of each logit in 16 bits;
-//      (distill) the logits at the teacher's pairs as they pass;
+//      the logits at the class or at the teacher's pairs as they pass;
 //   4. the row's log-sum-exp from the tiles, loss;
 //   5. per piece: the logit gradients in 16 bits (from what was kept, or from the product taken again),
 //      then dw and dh as products with them.
@@ -236,8 +236,8 @@ __global__ void __launch_bounds__(1024) k_vocab_rows(VocabCall c) {
 
 // ---------------------------------------------------------------------------
 // 2. Compact rows of h (padded with zeros to the pitch, and zero rows to a multiple of 256, which
-// the products read) and the logits at the targets that the products do not deliver: the class, or all pairs
-// of a teacher's row in no order.  One CTA a row.
+// the products read), and where a teacher's pairs are in no order the logits at them, which the products
+// do not deliver then.  One CTA a row.
 // ---------------------------------------------------------------------------
 
 // Eight values from 2-byte-aligned memory, zero from `left` on.
@@ -297,7 +297,6 @@ __global__ void __launch_bounds__(128) k_vocab_gather(VocabCall c) {
     int at = blockIdx.x, n_valid;
     int64_t r;
     bool left_out;
-    __shared__ float sums[4];
     if constexpr (RANK) {
         r = blockIdx.x;
         int before = 0, all = 0;
@@ -354,24 +353,8 @@ __global__ void __launch_bounds__(128) k_vocab_gather(VocabCall c) {
     }
     const uint16_t* from = (const uint16_t*)c.h + r * c.ldh;
     const int64_t words = c.Dp / 8;
-    if (c.target) {
-        // the row that is copied and its class's row of w, fetched together
-        const uint16_t* wr = (const uint16_t*)c.w + c.target[r] * c.ldw;
-        float s = 0.f;
-#pragma unroll 2
-        for (int64_t i = tid; i < words; i += 128) {
-            const uint4 x = load8(from + i * 8, c.D - i * 8), y = load8(wr + i * 8, c.D - i * 8);
-            ((uint4*)to)[i] = x;
-            s = dot8<F16>(x, y, s);
-        }
-        s = warp_sum_f(s);
-        if (lane == 0) sums[tid >> 5] = s;
-        __syncthreads();
-        if (tid == 0) c.zt[at] = (sums[0] + sums[1]) + (sums[2] + sums[3]);
-        return;
-    }
     for (int64_t i = tid; i < words; i += 128) ((uint4*)to)[i] = load8(from + i * 8, c.D - i * 8);
-    if (teacher_ascending(c.teacher[r])) return;
+    if (c.target || teacher_ascending(c.teacher[r])) return;
     __syncthreads();
     for (int j = tid >> 5; j < c.K; j += 4) {
         const int64_t v = c.t_idx[r * c.K + j];

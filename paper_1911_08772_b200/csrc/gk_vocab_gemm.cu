@@ -245,20 +245,28 @@ struct Patch {
     int64_t row0;        // of the warp; the thread's row is row0 + lane
     int64_t col0;        // of the 128
     int64_t cols;        // columns of the result from col0 on (may be more than 128, or none)
-    int pair, pairs_end;     // kLogits, kLogitsKeep with a teacher: the row's pairs in the 128 columns
+    int pair, pairs_end;     // kLogits, kLogitsKeep: the row's pairs (or class) in the 128 columns
     int next;                // column of the first
 };
 
-// A row's teacher pairs in ascending order are met one patch of columns at a time: the logit at each is
-// taken as it passes, instead of by a dot product of its own.  Where they are, find_pairs learns while the patch is
-// still being summed, from a table that k_vocab_teacher made (searching the row's pairs instead, six dependent
-// loads by 32 rows apart, took 2048 x 2048 x 32000 with 64 pairs 746 us a call, the table 722).
+// A row's class, or its teacher's pairs in ascending order, are met one patch of columns at a time: the logit at each is
+// taken as it passes.  Taken from the same sums as the log-sum-exp, its error is that of the term it is in there, and
+// goes out of the loss of a confident row (a dot product of its own left losses off by 1e-6 of the largest).
+// Where a teacher's pairs are, find_pairs learns while the patch is still being summed, from a table that
+// k_vocab_teacher made (searching the row's pairs instead, six dependent loads by 32 rows apart, took
+// 2048 x 2048 x 32000 with 64 pairs 746 us a call, the table 722).
 __device__ __forceinline__ void find_pairs(const VocabCall& c, Patch& w, int n_valid) {
     const int64_t row = w.row0 + w.lane;
     w.pair = w.pairs_end = 0;
     w.next = 0x7fffffff;
     if (row >= n_valid) return;
     const int32_t r = c.row_of[row];
+    if (c.target) {
+        const int64_t t = __ldg(c.target + r) - w.col0;
+        w.pairs_end = 1;
+        if (t >= 0 && t < kVocabTile) w.next = (int)(w.col0 + t);
+        return;
+    }
     const unsigned x = c.pairs_in[w.col0 / kVocabTile * c.n_pad + r];
     w.pair = (int)(x & 0xffff);
     w.pairs_end = w.pair + (int)(x >> 16);
@@ -268,7 +276,7 @@ __device__ __forceinline__ void find_pairs(const VocabCall& c, Patch& w, int n_v
 // any of the warp's rows go through the staging memory.
 __device__ __forceinline__ void take_pairs(const VocabCall& c, const Patch& w, int n_valid, const float (&v)[128]) {
     const int64_t row = w.row0 + w.lane;
-    const int32_t* pairs = row < n_valid ? c.t_idx + (int64_t)c.row_of[row] * c.K : nullptr;
+    const int32_t* pairs = row < n_valid && c.t_idx ? c.t_idx + (int64_t)c.row_of[row] * c.K : nullptr;
     int j = w.pair, next = w.next;
 #pragma unroll
     for (int part = 0; part < 4; ++part) {
@@ -791,7 +799,7 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                 const int64_t col = (int64_t)n * width + side * 128;
                 w.cols = n_cols - col;
                 w.col0 = p.v0 + col;
-                const bool used = used_rows && w.cols > 0, pairs = P != kAgain && c.t_idx && used && w.row0 < n_valid;
+                const bool used = used_rows && w.cols > 0, pairs = P != kAgain && used && w.row0 < n_valid;
                 if (pairs) find_pairs(c, w, n_valid);
                 for (int done = 0; done < k1 - k0; done += kChunk) {
                     wait_sums(only);
