@@ -354,7 +354,11 @@ __global__ void __launch_bounds__(128) k_vocab_gather(VocabCall c) {
     const uint16_t* from = (const uint16_t*)c.h + r * c.ldh;
     const int64_t words = c.Dp / 8;
     for (int64_t i = tid; i < words; i += 128) ((uint4*)to)[i] = load8(from + i * 8, c.D - i * 8);
-    if (c.target || teacher_ascending(c.teacher[r])) return;
+    if (c.target) {
+        if (tid == 0) c.cls[at] = (int32_t)c.target[r];
+        return;
+    }
+    if (teacher_ascending(c.teacher[r])) return;
     __syncthreads();
     for (int j = tid >> 5; j < c.K; j += 4) {
         const int64_t v = c.t_idx[r * c.K + j];
@@ -651,6 +655,7 @@ static size_t lay_out(VocabCall& c, bool distill, bool copy_w, char* base) {
     c.at_of = (int32_t*)take(4 * n);
     c.q = (float*)(distill ? take(4 * n * K) : nullptr);
     c.teacher = (float4*)(distill ? take(16 * n) : nullptr);
+    c.cls = (int32_t*)(distill ? nullptr : take(4 * np));
     c.pairs_in = (unsigned*)(distill ? take(4 * tiles * np) : nullptr);
     c.hc = (uint16_t*)take(2 * np * c.Dp);
     c.wc = (uint16_t*)(copy_w ? take(2 * (size_t)c.V * c.Dp) : nullptr);

@@ -60,6 +60,7 @@ struct VocabCall {
     float* q;                   // n x K teacher probabilities (distill), 0 for a pair left out
     float4* teacher;            // per row: Q, log-sum-exp L relative to a reference, the reference, and a whole
                                 // number: 1 (indices strictly ascending, pairs left out at the end) + 2 (a pair counts)
+    int32_t* cls;               // compact rows' classes (loss)
     unsigned* pairs_in;         // per (vocabulary tile, row): its pairs there, the first's number + 2^16 how many (distill)
     uint16_t* hc;               // n_pad x Dp compact rows of h
     uint16_t* wc;               // V x Dp copy of w where w itself cannot be the source of bulk copies, else nullptr

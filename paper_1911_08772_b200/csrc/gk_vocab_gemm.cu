@@ -4,8 +4,8 @@
 // result with tcgen05.mma.cta_group::2; each CTA holds 128 rows of A, half of the tile's rows of B, and the fp32 sums
 // of its 128 rows in tensor memory.  Operands arrive by TMA in blocks of 64 along the summed axis, 192 KB of them in
 // flight a CTA.  One warp sends for blocks, one issues products, eight read the sums out.  Bound by the tensor
-// pipes, and those by the power limit: 4096 x 2048 x 50000 kept them 95 % busy, logits and gradients alike, at
-// 1.4 to 1.5 GHz.
+// pipes, and those by the power limit: in 4096 x 2048 x 50000 the logits kept them 89 to 95 % busy and the gradients 95 %,
+// at 1.4 to 1.5 GHz.
 //
 // Narrow tiles (256 columns, six blocks of 32 KB in flight): one half of the tensor memory is summed into while
 // the other is read out.  Logits always are; they are summed in chunks (kChunk), which take turns on the halves.
@@ -245,39 +245,45 @@ struct Patch {
     int64_t row0;        // of the warp; the thread's row is row0 + lane
     int64_t col0;        // of the 128
     int64_t cols;        // columns of the result from col0 on (may be more than 128, or none)
-    int pair, pairs_end;     // kLogits, kLogitsKeep: the row's pairs (or class) in the 128 columns
+    int row;                 // kLogits, kLogitsKeep: the row's class, or the row's number with the caller
+    unsigned pairs;          // its pairs in the 128 columns: the first's number + 2^16 how many
     int next;                // column of the first
 };
 
 // A row's class, or its teacher's pairs in ascending order, are met one patch of columns at a time: the logit at each is
 // taken as it passes.  Taken from the same sums as the log-sum-exp, its error is that of the term it is in there, and
 // goes out of the loss of a confident row (a dot product of its own left losses off by 1e-6 of the largest).
-// Where a teacher's pairs are, find_pairs learns while the patch is still being summed, from a table that
-// k_vocab_teacher made (searching the row's pairs instead, six dependent loads by 32 rows apart, took
-// 2048 x 2048 x 32000 with 64 pairs 746 us a call, the table 722).
-__device__ __forceinline__ void find_pairs(const VocabCall& c, Patch& w, int n_valid) {
+// Where a teacher's pairs are is in a table that k_vocab_teacher made (searching the row's pairs instead, six
+// dependent loads by 32 rows apart, took 2048 x 2048 x 32000 with 64 pairs 746 us a call, the table 722).  What is
+// found of them depends on one load after another, which are sent a chunk of sums apart and not waited for
+// between: 728 us with all of them before the first sums, 716 so.
+__device__ __forceinline__ void find_row(const VocabCall& c, Patch& w, int n_valid) {
     const int64_t row = w.row0 + w.lane;
-    w.pair = w.pairs_end = 0;
+    w.row = 0;
+    w.pairs = 0;
     w.next = 0x7fffffff;
-    if (row >= n_valid) return;
-    const int32_t r = c.row_of[row];
+    if (row < n_valid) w.row = c.target ? c.cls[row] : c.row_of[row];
+}
+__device__ __forceinline__ void find_pairs(const VocabCall& c, Patch& w, int n_valid) {
+    if (w.row0 + w.lane < n_valid && !c.target) w.pairs = c.pairs_in[w.col0 / kVocabTile * c.n_pad + w.row];
+}
+__device__ __forceinline__ void find_first(const VocabCall& c, Patch& w, int n_valid) {
     if (c.target) {
-        const int64_t t = __ldg(c.target + r) - w.col0;
-        w.pairs_end = 1;
-        if (t >= 0 && t < kVocabTile) w.next = (int)(w.col0 + t);
-        return;
+        if (w.row0 + w.lane < n_valid && w.row >= w.col0 && w.row < w.col0 + kVocabTile) {
+            w.pairs = 1u << 16;
+            w.next = w.row;
+        }
+    } else if (w.pairs >> 16) {
+        w.next = __ldg(c.t_idx + (int64_t)w.row * c.K + (w.pairs & 0xffff));
     }
-    const unsigned x = c.pairs_in[w.col0 / kVocabTile * c.n_pad + r];
-    w.pair = (int)(x & 0xffff);
-    w.pairs_end = w.pair + (int)(x >> 16);
-    if (x >> 16) w.next = __ldg(c.t_idx + (int64_t)r * c.K + w.pair);
 }
 // `v`: the patch's columns; a register cannot be chosen at run time, so stretches of 32 columns with a pair in
 // any of the warp's rows go through the staging memory.
-__device__ __forceinline__ void take_pairs(const VocabCall& c, const Patch& w, int n_valid, const float (&v)[128]) {
+__device__ __forceinline__ void take_pairs(const VocabCall& c, const Patch& w, const float (&v)[128]) {
     const int64_t row = w.row0 + w.lane;
-    const int32_t* pairs = row < n_valid && c.t_idx ? c.t_idx + (int64_t)c.row_of[row] * c.K : nullptr;
-    int j = w.pair, next = w.next;
+    const int32_t* pairs = c.t_idx + (int64_t)w.row * c.K;       // used with more than one
+    int j = (int)(w.pairs & 0xffff), next = w.next;
+    const int pairs_end = j + (int)(w.pairs >> 16);
 #pragma unroll
     for (int part = 0; part < 4; ++part) {
         const int from = (int)w.col0 + part * 32;
@@ -296,7 +302,7 @@ __device__ __forceinline__ void take_pairs(const VocabCall& c, const Patch& w, i
                              : "=f"(z) : "r"(w.staging + w.lane * 128 + (((col >> 2) ^ (w.lane & 7)) << 4) + (col & 3) * 4) : "memory");
                 c.zt[row * c.K + j] = z;
                 ++j;
-                next = j < w.pairs_end ? __ldg(pairs + j) : 0x7fffffff;
+                next = j < pairs_end ? __ldg(pairs + j) : 0x7fffffff;
             }
             __syncwarp();
         }
@@ -800,7 +806,7 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                 w.cols = n_cols - col;
                 w.col0 = p.v0 + col;
                 const bool used = used_rows && w.cols > 0, pairs = P != kAgain && used && w.row0 < n_valid;
-                if (pairs) find_pairs(c, w, n_valid);
+                if (pairs) find_row(c, w, n_valid);
                 for (int done = 0; done < k1 - k0; done += kChunk) {
                     wait_sums(only);
                     if (!ok) break;
@@ -809,7 +815,9 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                         __syncwarp();
                         if (done == 0) {
                             tmem_ld128(w.tmem, v);
+                            if (pairs) find_pairs(c, w, n_valid);
                         } else {
+                            if (pairs && done == kChunk) find_first(c, w, n_valid);
 #pragma unroll
                             for (int i = 0; i < 8; ++i) {
                                 float x[16];
@@ -823,7 +831,8 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                     only ^= 1;
                 }
                 if (!ok) break;
-                if (pairs) take_pairs(c, w, n_valid, v);
+                if (pairs && k1 - k0 <= kChunk) find_first(c, w, n_valid);
+                if (pairs) take_pairs(c, w, v);
                 if (used) {
                     if (P != kAgain && w.cols < 128) {
 #pragma unroll
