@@ -991,7 +991,10 @@ static int launch(const VocabCall& c, int64_t v0, int64_t v1, bool first, int sm
     p.first = first;
     p.extra_arrivals = host_knob(kKnobExtraArrivals) > 0 ? 1 : 0;
     p.wait_clocks = p.extra_arrivals ? 1ll << 27 : kWaitClocks;
-    p.splits = P == kGrads && c.splits > 0 ? c.splits : 1;
+    // (a part without a block would have no sums: the last piece of the vocabulary can be shorter than the parts, which
+    // the first, a full one, has four blocks for each of; parts that it does not reach keep the sums they have)
+    const int64_t blocks = (v1 - v0 + kBlockK - 1) / kBlockK;
+    p.splits = P == kGrads && c.splits > 0 ? (int)(c.splits < blocks ? c.splits : blocks) : 1;
     p.direct = c.dhp == nullptr;
     // (the copies' hardware cuts a row's end in steps of 16 bytes, so the rows' length counts too)
     p.wide = (((uintptr_t)c.dw | (uintptr_t)(2 * c.lddw) | (uintptr_t)(2 * c.D)) & 15) == 0;

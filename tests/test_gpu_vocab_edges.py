@@ -1,0 +1,29 @@
+"""Where the vocabulary head's operators can go wrong beyond sizes."""
+
+import pytest
+import torch
+
+from paper_1911_08772_b200 import binding as gk
+from test_gpu_vocab_head import TYPES, _library, distill, hard_loss  # noqa: F401  (_library: a fixture)
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture
+def budget():
+    yield gk.gk_vocab_set_budget
+    gk.gk_vocab_set_budget(2 << 30)
+
+
+# --- one part of the vocabulary after another -------------------------------------------------------------
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("dw", [True, False])
+@pytest.mark.parametrize("V,columns", [(2100, 2048), (4100, 4096), (4200, 4096)])
+def test_a_last_piece_of_fewer_blocks_than_dh_has_parts(V, columns, dw, dtype, budget):
+    """dh's sum over the vocabulary is split into parts by the full piece (here at least four); the last piece has
+    one or two blocks of 64 columns."""
+    budget(2 * 256 * columns)
+    hard_loss(200, 136, V, dtype, seed=60, left_out=0.1, dw=dw)
+    distill(200, 136, V, 9, dtype, seed=61, dw=dw)
