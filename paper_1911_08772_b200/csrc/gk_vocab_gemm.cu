@@ -818,6 +818,7 @@ k_vocab_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                             if (pairs) find_pairs(c, w, n_valid);
                         } else {
                             if (pairs && done == kChunk) find_first(c, w, n_valid);
+                            __syncwarp();       // lanes part there, and the copies below take the whole warp
 #pragma unroll
                             for (int i = 0; i < 8; ++i) {
                                 float x[16];

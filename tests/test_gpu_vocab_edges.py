@@ -27,3 +27,17 @@ def test_a_last_piece_of_fewer_blocks_than_dh_has_parts(V, columns, dw, dtype, b
     budget(2 * 256 * columns)
     hard_loss(200, 136, V, dtype, seed=60, left_out=0.1, dw=dw)
     distill(200, 136, V, 9, dtype, seed=61, dw=dw)
+
+
+# --- lanes of a reading warp that find something and lanes that do not ------------------------------------
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("D", [769, 1600, 2400])
+def test_few_rows_of_a_warp_have_pairs_in_a_tile(D, dtype):
+    """Over 768 the logits are summed in chunks, and a row's first pair is looked up between two of them, by the
+    lanes whose rows have one there."""
+    hard_loss(70, D, 900, dtype, seed=67, left_out=0.2)
+    distill(70, D, 900, 3, dtype, seed=68)
+    distill(33, D, 300, 40, dtype, seed=69, holes=0.7)
+    distill(70, D, 900, 3, dtype, seed=70, dh=False, dw=False)
