@@ -341,6 +341,9 @@ int gk_set_params(int unbiased_std, int max_rounds);
  * With neither dh nor dw only the forward pass runs (scoring).  dh and dw must not overlap h, w or
  * each other.  Results do not depend on timing: no atomics on floating-point data.
  *
+ * Calls of several host threads are safe on any streams: those on one stream are enqueued whole, one after the
+ * other (in no promised order), and each thread's cudaStreamPerThread has a workspace of its own.
+ *
  * The workspace is the call's own, per (device, stream), grown on first use (gk_vocab_reserve
  * does that ahead; a call that fits allocates nothing and can be captured in a graph, which stays good until a
  * call that does not fit replaces the workspace).  The

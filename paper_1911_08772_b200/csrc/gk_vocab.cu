@@ -32,7 +32,7 @@
 #include <map>
 #include <mutex>
 #include <new>
-#include <utility>
+#include <tuple>
 
 #include "gk_vocab.cuh"
 
@@ -623,15 +623,20 @@ __global__ void __launch_bounds__(256) k_vocab_finish_dh(VocabCall c) {
 }
 
 // ---------------------------------------------------------------------------
-// Workspace: one block per (device, stream), grown as calls need it.
+// Workspace: one block per (device, stream), grown as calls need it.  A call holds its stream's block from the
+// lookup to its last launch: a call is several launches over that block, so calls of two host threads on one
+// stream must not mix theirs, and neither may replace the block under the other.
 // ---------------------------------------------------------------------------
 struct VocabWorkspace {
+    std::mutex held;
     void* base = nullptr;
     size_t bytes = 0;
     int sm_count = 0;
 };
+// device, stream, and what tells apart the streams that share the per-thread handle
+using VocabKey = std::tuple<int, cudaStream_t, unsigned long long>;
 static std::mutex g_vocab_mu;
-static std::map<std::pair<int, cudaStream_t>, VocabWorkspace> g_vocab_ws;
+static std::map<VocabKey, VocabWorkspace> g_vocab_ws;      // (entries stay where they are)
 static std::atomic<int64_t> g_vocab_budget{(int64_t)2 << 30};
 
 static int64_t piece_columns(int64_t n_pad, int64_t V) {
@@ -668,29 +673,45 @@ static size_t lay_out(VocabCall& c, bool distill, bool copy_w, char* base) {
     return at;
 }
 
-// (no exception passes a C entry: the map's memory is the only source of one)
-static int vocab_workspace(size_t bytes, cudaStream_t st, VocabWorkspace** out) try {
+static int vocab_key(cudaStream_t st, VocabKey& key) {
     int dev = 0;
     GK_CUDA_TRY(cudaGetDevice(&dev));
-    std::lock_guard<std::mutex> lock(g_vocab_mu);
-    VocabWorkspace& ws = g_vocab_ws[std::make_pair(dev, st)];
-    if (ws.bytes < bytes) {
-        if (ws.base) {
-            GK_CUDA_TRY(cudaStreamSynchronize(st));   // work already enqueued may still use the old block
-            GK_CUDA_TRY(cudaFree(ws.base));
-            ws.base = nullptr;
-            ws.bytes = 0;
-        }
-        void* p = nullptr;
-        if (cudaMalloc(&p, bytes) != cudaSuccess) { cudaGetLastError(); return GK_ERR_NOMEM; }
-        ws.base = p;
-        ws.bytes = bytes;
-    }
-    if (ws.sm_count == 0) GK_CUDA_TRY(cudaDeviceGetAttribute(&ws.sm_count, cudaDevAttrMultiProcessorCount, dev));
-    *out = &ws;
+    unsigned long long id = 0;
+    if (st == cudaStreamPerThread) GK_CUDA_TRY(cudaStreamGetId(st, &id));
+    key = VocabKey(dev, st, id);
     return GK_OK;
-} catch (const std::bad_alloc&) {
-    return GK_ERR_NOMEM;
+}
+
+// The stream's workspace, held by `lock` from here on.
+static int vocab_workspace(cudaStream_t st, VocabWorkspace** out, std::unique_lock<std::mutex>& lock) {
+    VocabKey key;
+    const int rc = vocab_key(st, key);
+    if (rc != GK_OK) return rc;
+    VocabWorkspace* ws;
+    {
+        std::lock_guard<std::mutex> all(g_vocab_mu);
+        ws = &g_vocab_ws[key];
+    }
+    lock = std::unique_lock<std::mutex>(ws->held);
+    if (ws->sm_count == 0) GK_CUDA_TRY(cudaDeviceGetAttribute(&ws->sm_count, cudaDevAttrMultiProcessorCount, std::get<0>(key)));
+    *out = ws;
+    return GK_OK;
+}
+
+// At least `bytes` for a workspace that the caller holds.
+static int grow(VocabWorkspace& ws, size_t bytes, cudaStream_t st) {
+    if (ws.bytes >= bytes) return GK_OK;
+    if (ws.base) {
+        GK_CUDA_TRY(cudaStreamSynchronize(st));   // work already enqueued may still use the old block
+        GK_CUDA_TRY(cudaFree(ws.base));
+        ws.base = nullptr;
+        ws.bytes = 0;
+    }
+    void* p = nullptr;
+    if (cudaMalloc(&p, bytes) != cudaSuccess) { cudaGetLastError(); return GK_ERR_NOMEM; }
+    ws.base = p;
+    ws.bytes = bytes;
+    return GK_OK;
 }
 
 static void size_call(VocabCall& c, bool want_dh, DwRows dw, int sm_count) {
@@ -769,22 +790,26 @@ static int check_head(const VocabCall& c, int32_t dtype) {
     return GK_OK;
 }
 
-static int run_head(VocabCall& c, bool distill, cudaStream_t st) {
+// (no exception passes a C entry: the map's memory is the only source of one)
+static int run_head(VocabCall& c, bool distill, cudaStream_t st) try {
     if (c.n == 0) {   // no rows: the weights' gradient is zero
         if (c.dw) GK_CUDA_TRY(cudaMemset2DAsync(c.dw, 2 * c.lddw, 0, 2 * c.D, (size_t)c.V, st));
         return GK_OK;
     }
     VocabWorkspace* ws = nullptr;
-    int rc = vocab_workspace(0, st, &ws);
+    std::unique_lock<std::mutex> held;
+    int rc = vocab_workspace(st, &ws, held);
     if (rc != GK_OK) return rc;
     // rows that start and end on 16-byte boundaries are copied to shared memory as they lie
     const bool w_vec = (((uintptr_t)c.w | (uintptr_t)(2 * c.ldw) | (uintptr_t)(2 * c.D)) & 15) == 0;
     const bool dw_vec = (((uintptr_t)c.dw | (uintptr_t)(2 * c.lddw) | (uintptr_t)(2 * c.D)) & 15) == 0;
     size_call(c, c.dh != nullptr, !c.dw ? DwRows::none : dw_vec ? DwRows::aligned : DwRows::unaligned, ws->sm_count);
-    rc = vocab_workspace(lay_out(c, distill, !w_vec, nullptr), st, &ws);
+    rc = grow(*ws, lay_out(c, distill, !w_vec, nullptr), st);
     if (rc != GK_OK) return rc;
     lay_out(c, distill, !w_vec, (char*)ws->base);
     return c.f16 ? enqueue<true>(c, distill, ws->sm_count, st) : enqueue<false>(c, distill, ws->sm_count, st);
+} catch (const std::bad_alloc&) {
+    return GK_ERR_NOMEM;
 }
 
 }  // namespace gk
@@ -861,30 +886,36 @@ extern "C" int64_t gk_vocab_workspace_bytes(int64_t n, int64_t D, int64_t V, int
     return (int64_t)largest(c, n, D, V, K, grad, 148);
 }
 
-extern "C" int gk_vocab_reserve(int64_t n, int64_t D, int64_t V, int32_t K, int grad, gk_stream_t stream) {
+extern "C" int gk_vocab_reserve(int64_t n, int64_t D, int64_t V, int32_t K, int grad, gk_stream_t stream) try {
     const int rc = head_sizes_ok(n, D, V, K);
     if (rc != GK_OK) return rc;
     VocabWorkspace* ws = nullptr;
-    const int wrc = vocab_workspace(0, (cudaStream_t)stream, &ws);
+    std::unique_lock<std::mutex> held;
+    const int wrc = vocab_workspace((cudaStream_t)stream, &ws, held);
     if (wrc != GK_OK) return wrc;
     VocabCall c = {};
-    return vocab_workspace(largest(c, n, D, V, K, grad, ws->sm_count), (cudaStream_t)stream, &ws);
+    return grow(*ws, largest(c, n, D, V, K, grad, ws->sm_count), (cudaStream_t)stream);
+} catch (const std::bad_alloc&) {
+    return GK_ERR_NOMEM;
 }
 
 extern "C" int gk_vocab_last_info(gk_stream_t stream, int64_t* host_out) {
     if (!host_out) return GK_ERR_NULL;
-    int dev = 0;
-    GK_CUDA_TRY(cudaGetDevice(&dev));
-    void* base = nullptr;
+    VocabKey key;
+    const int rc = vocab_key((cudaStream_t)stream, key);
+    if (rc != GK_OK) return rc;
+    VocabWorkspace* ws = nullptr;
     {
-        std::lock_guard<std::mutex> lock(g_vocab_mu);
-        auto it = g_vocab_ws.find(std::make_pair(dev, (cudaStream_t)stream));
-        if (it != g_vocab_ws.end()) base = it->second.base;
+        std::lock_guard<std::mutex> all(g_vocab_mu);
+        auto it = g_vocab_ws.find(key);
+        if (it != g_vocab_ws.end()) ws = &it->second;
     }
-    if (!base) return GK_ERR_NULL;
-    VocabCtl ctl;
+    if (!ws) return GK_ERR_NULL;
     GK_CUDA_TRY(cudaStreamSynchronize((cudaStream_t)stream));
-    GK_CUDA_TRY(cudaMemcpy(&ctl, base, sizeof(ctl), cudaMemcpyDeviceToHost));
+    std::lock_guard<std::mutex> held(ws->held);
+    if (!ws->base) return GK_ERR_NULL;
+    VocabCtl ctl;
+    GK_CUDA_TRY(cudaMemcpy(&ctl, ws->base, sizeof(ctl), cudaMemcpyDeviceToHost));
     host_out[0] = ctl.status;
     host_out[1] = ctl.n_valid;
     return GK_OK;
