@@ -167,10 +167,13 @@ __device__ __forceinline__ unsigned pack16(float lo, float hi) {
 }
 
 // Joins (m, s) pairs of a running maximum and sum, in units of log 2.  A part without a term
-// has m = -inf and s = 0.
+// has m = -inf and s = 0, a part of nothing but NaN m = -inf and s = NaN.
 __device__ __forceinline__ void join_max_sum(float& m, float& s, float m2, float s2) {
     const float top = fmaxf(m, m2);
-    if (top == -INFINITY) return;
+    if (top == -INFINITY) {
+        s += s2;
+        return;
+    }
     // a NaN sum stays NaN through the products; exp2(-inf) = 0 drops empty parts; a part at the
     // common maximum is taken as it is, also where that is +inf
     s = (m == top ? s : s * exp2_fast(m - top)) + (m2 == top ? s2 : s2 * exp2_fast(m2 - top));

@@ -1,10 +1,11 @@
 """Where the vocabulary head's operators can go wrong beyond sizes."""
+import math
 
 import pytest
 import torch
 
 from paper_1911_08772_b200 import binding as gk
-from test_gpu_vocab_head import TYPES, _library, distill, hard_loss  # noqa: F401  (_library: a fixture)
+from test_gpu_vocab_head import DEV, TYPES, Out, _library, distill, hard_loss, make  # noqa: F401  (_library: a fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -41,3 +42,26 @@ def test_few_rows_of_a_warp_have_pairs_in_a_tile(D, dtype):
     distill(70, D, 900, 3, dtype, seed=68)
     distill(33, D, 300, 40, dtype, seed=69, holes=0.7)
     distill(70, D, 900, 3, dtype, seed=70, dh=False, dw=False)
+
+
+# --- rows that are not finite -----------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("V", [300, 20000])
+@pytest.mark.parametrize("grad", [True, False])
+@pytest.mark.parametrize("n", [1, 9, 40])
+def test_a_row_of_nan_that_counts_has_a_log_sum_exp_of_nan(n, grad, V):
+    D = 64
+    gen, h, w, hd, wd = make(n, D, V, torch.bfloat16, 63)
+    target = torch.randint(0, V, (n,), generator=gen).to(DEV)
+    g = torch.ones(n, device=DEV)
+    bad = n // 2
+    base, out = (Out(n, D, V, torch.bfloat16, dh=grad, dw=False) for _ in range(2))
+    gk.gk_vocab_loss(hd, wd, target, base.loss[:n], base.lse[:n], dh=base.dh, row_grad=g)
+    hd[bad] = math.nan
+    gk.gk_vocab_loss(hd, wd, target, out.loss[:n], out.lse[:n], dh=out.dh, row_grad=g)
+    rest = torch.arange(n, device=DEV) != bad
+    assert bool(torch.isnan(out.loss[bad])) and bool(torch.isnan(out.lse[bad]))
+    assert torch.equal(out.loss[:n][rest], base.loss[:n][rest]) and torch.equal(out.lse[:n][rest], base.lse[:n][rest])
+    if grad:
+        assert torch.equal(out.dh[rest], base.dh[rest]) and bool(torch.isnan(out.dh[bad]).all())
