@@ -132,10 +132,11 @@ __global__ void __launch_bounds__(256) k_vocab_teacher(VocabCall c) {
 // The rows that count, numbered in their order, and the scale that brings the gradients' largest row
 // coefficient to 2 (bf16) or 2048 (fp16, whose smallest step is 2^-24: an entry 2^-34 of the largest is still
 // held).  A row that has learned little has an entry of nearly its whole coefficient, and the rounding to 16 bits
-// is finest, relative to the value, just below a power of two.
+// is finest, relative to the value, just below a power of two.  A coefficient that is not finite has no say in it:
+// its own row of dh, and dw, are lost, the other rows of dh are not.
 // ---------------------------------------------------------------------------
 
-// Whether row r counts, and the magnitude of its gradient's coefficient (times T).
+// Whether row r counts, and the magnitude of its gradient's coefficient (times T), 0 where that is not finite.
 __device__ __forceinline__ bool row_counts(const VocabCall& c, int64_t r, float& g) {
     g = 0.f;
     if (r >= c.n) return false;
@@ -152,7 +153,7 @@ __device__ __forceinline__ bool row_counts(const VocabCall& c, int64_t r, float&
     }
     if (on) {
         g = fabsf(Q * rg);
-        if (!(g < INFINITY)) g = INFINITY;      // a NaN too
+        if (!(g * c.inv_T < INFINITY)) g = 0.f;     // a NaN too
     }
     return on;
 }
@@ -161,7 +162,7 @@ __device__ __forceinline__ void write_ctl(const VocabCall& c, int n_valid, float
     top *= c.inv_T;
     int e = 0;
     float part = 1.f;
-    if (top > 0.f && top < INFINITY) part = frexpf(top, &e);   // top = part 2^e
+    if (top > 0.f) part = frexpf(top, &e);   // top = part 2^e
     e = min(max((c.f16 ? 11 : 1) - e, -100), 100);
     c.ctl->n_valid = n_valid;
     c.ctl->status = 0;

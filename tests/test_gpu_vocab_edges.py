@@ -65,3 +65,49 @@ def test_a_row_of_nan_that_counts_has_a_log_sum_exp_of_nan(n, grad, V):
     assert torch.equal(out.loss[:n][rest], base.loss[:n][rest]) and torch.equal(out.lse[:n][rest], base.lse[:n][rest])
     if grad:
         assert torch.equal(out.dh[rest], base.dh[rest]) and bool(torch.isnan(out.dh[bad]).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n", [300, 1100])
+@pytest.mark.parametrize("size", [1e-6, 128.0])
+@pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf])
+def test_a_row_gradient_that_is_not_finite_reaches_its_own_row_of_dh_only(value, size, n, dtype):
+    """The rows share one scale, which the others' gradients set: their rows are those of the call with a zero in
+    the bad row's place, bit by bit."""
+    D, V, K, bad = 72, 500, 5, 17
+    gen, h, w, hd, wd = make(n, D, V, dtype, 64)
+    target = torch.randint(0, V, (n,), generator=gen).to(DEV)
+    idx = torch.stack([torch.randperm(V, generator=gen)[:K].sort().values for _ in range(n)]).to(torch.int32).to(DEV)
+    val = torch.randn(n, K, generator=gen).to(DEV)
+    g = (torch.randn(n, generator=gen) * size).to(DEV)
+    rest = torch.arange(n, device=DEV) != bad
+    for soft in (False, True):
+        dhs = []
+        for x in (0.0, value) + ((3e38,) if soft else ()):       # at T = 0.5 the last is infinite too
+            g[bad] = x
+            out = Out(n, D, V, dtype)
+            if soft:
+                gk.gk_vocab_distill(hd, wd, idx, val, out.loss[:n], out.lse[:n], temperature=0.5, row_grad=g, dh=out.dh, dw=out.dw)
+            else:
+                gk.gk_vocab_loss(hd, wd, target, out.loss[:n], out.lse[:n], row_grad=g, dh=out.dh, dw=out.dw)
+            dhs.append(out.dh[rest])
+        assert bool(torch.isfinite(dhs[0]).all()) and bool((dhs[0] != 0).any())
+        assert all(torch.equal(dhs[0], x) for x in dhs[1:])
+
+
+def test_a_teacher_mass_that_is_not_finite_reaches_its_own_row_of_dh_only():
+    n, D, V, K, bad = 300, 72, 500, 5, 17
+    gen, h, w, hd, wd = make(n, D, V, torch.float16, 65)
+    idx = torch.stack([torch.randperm(V, generator=gen)[:K].sort().values for _ in range(n)]).to(torch.int32).to(DEV)
+    val = torch.randn(n, K, generator=gen).to(DEV)
+    g = torch.full((n,), 128.0, device=DEV)
+    lse = torch.logsumexp(val, 1)
+    rest = torch.arange(n, device=DEV) != bad
+    dhs = []
+    for x in (float(lse[bad]), -math.inf, math.nan):
+        lse[bad] = x
+        out = Out(n, D, V, torch.float16)
+        gk.gk_vocab_distill(hd, wd, idx, val, out.loss[:n], out.lse[:n], t_lse=lse, row_grad=g, dh=out.dh, dw=out.dw)
+        dhs.append(out.dh[rest])
+    assert bool(torch.isfinite(dhs[0]).all())
+    assert torch.equal(dhs[0], dhs[1]) and torch.equal(dhs[0], dhs[2])
