@@ -402,8 +402,9 @@ int gk_vocab_topk(const void* logits, int64_t ld, int32_t dtype, int64_t n, int6
 int gk_vocab_set_budget(int64_t bytes);
 
 /* Create (or grow) the workspace of (current device, stream) for gk_vocab_loss (K = 1) and
- * gk_vocab_distill calls of these sizes at the present budget, with or without gradients, with
- * rows of w on 16-byte boundaries where D is a multiple of 8.  Synchronous. */
+ * gk_vocab_distill calls of up to n rows and K pairs and of this D and V, at the present budget, with or
+ * without gradients, with rows of w on 16-byte boundaries where D is a multiple of 8.  Synchronous.
+ * gk_vocab_workspace_bytes: what that takes, on a B200. */
 int gk_vocab_reserve(int64_t n, int64_t D, int64_t V, int32_t K, int grad, gk_stream_t stream);
 int64_t gk_vocab_workspace_bytes(int64_t n, int64_t D, int64_t V, int32_t K, int grad);
 

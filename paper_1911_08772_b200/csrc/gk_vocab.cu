@@ -862,15 +862,23 @@ extern "C" int gk_vocab_set_budget(int64_t bytes) {
     return GK_OK;
 }
 
-// Sizes of the largest call a workspace is asked for: a distillation with K pairs and both
-// gradients (or no gradient), over rows of w on any boundary.
+// What the largest call of up to n rows may ask for: a distillation with K pairs and both gradients (or no gradient),
+// over rows of w on any boundary.  Fewer rows can need more: dh is split into more parts, and a piece of the
+// vocabulary comes nearer to the budget.  Within 64 rows, a block of dw's sum, launch_time's tiles and blocks are the
+// same and a part costs more with more rows, so the fewest rows have the most parts.
 static size_t largest(VocabCall& c, int64_t n, int64_t D, int64_t V, int32_t K, int grad, int sms) {
-    c.n = n; c.D = D; c.V = V; c.K = K;
+    c.D = D; c.V = V; c.K = K;
     size_t most = 0;
-    for (DwRows dw : {DwRows::none, DwRows::aligned, DwRows::unaligned}) {     // dh is split by what it shares the SMs with
-        size_call(c, grad != 0, grad ? dw : DwRows::none, sms);
-        const size_t bytes = lay_out(c, true, D % 8 != 0, nullptr);
-        most = bytes > most ? bytes : most;
+    for (int64_t last = n; last > 0; last = (last - 1) / 64 * 64) {
+        const int64_t few = (last - 1) / 64 * 64 + 1;
+        for (DwRows dw : {DwRows::none, DwRows::aligned, DwRows::unaligned}) {     // dh is split by what it shares the SMs with
+            c.n = few;
+            size_call(c, grad != 0, grad ? dw : DwRows::none, sms);
+            c.n = last;
+            const size_t bytes = lay_out(c, true, D % 8 != 0, nullptr);
+            most = bytes > most ? bytes : most;
+            if (!grad) return most;      // grows with the rows
+        }
     }
     return most;
 }

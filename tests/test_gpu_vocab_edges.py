@@ -111,3 +111,28 @@ def test_a_teacher_mass_that_is_not_finite_reaches_its_own_row_of_dh_only():
         dhs.append(out.dh[rest])
     assert bool(torch.isfinite(dhs[0]).all())
     assert torch.equal(dhs[0], dhs[1]) and torch.equal(dhs[0], dhs[2])
+
+
+# --- the workspace ----------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("n,fewer,D,V", [(700, [700, 449, 200, 65, 1], 512, 9000), (2048, [1537, 1025, 300], 2048, 8000)])
+def test_a_workspace_reserved_for_more_rows_can_be_captured_with_fewer(n, fewer, D, V):
+    """A call that had to replace the workspace could not be captured: neither the wait nor the allocation may be."""
+    gen, h, w, hd, wd = make(n, D, V, torch.bfloat16, 71)
+    target = torch.randint(0, V, (n,), generator=gen).to(DEV)
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        gk.gk_vocab_reserve(n, D, V)
+        for m in fewer:
+            for dw in (False, True):
+                eager, out = (Out(m, D, V, torch.bfloat16, dw=dw) for _ in range(2))
+                graph = torch.cuda.CUDAGraph()
+                stream.synchronize()
+                with torch.cuda.graph(graph, stream=stream):
+                    gk.gk_vocab_loss(hd[:m], wd, target[:m], out.loss[:m], out.lse[:m], dh=out.dh, dw=out.dw)
+                graph.replay()
+                gk.gk_vocab_loss(hd[:m], wd, target[:m], eager.loss[:m], eager.lse[:m], dh=eager.dh, dw=eager.dw)
+                stream.synchronize()
+                assert torch.equal(out.loss, eager.loss) and torch.equal(out.dh, eager.dh)
+                assert not dw or torch.equal(out.dw, eager.dw)
