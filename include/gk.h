@@ -409,7 +409,8 @@ int gk_vocab_reserve(int64_t n, int64_t D, int64_t V, int32_t K, int grad, gk_st
 int64_t gk_vocab_workspace_bytes(int64_t n, int64_t D, int64_t V, int32_t K, int grad);
 
 /* Synchronise `stream` and write to HOST host_out[0..1] of the last gk_vocab_loss or
- * gk_vocab_distill call on it: GK_DEV_* flags, rows that counted. */
+ * gk_vocab_distill call on it, one without rows included (0, 0): GK_DEV_* flags, rows that counted.
+ * GK_ERR_NULL where there was no call. */
 int gk_vocab_last_info(gk_stream_t stream, int64_t* host_out);
 
 /* Output capacity of idx_out / val_out for the sparsify calls, in pairs.

@@ -633,6 +633,7 @@ struct VocabWorkspace {
     void* base = nullptr;
     size_t bytes = 0;
     int sm_count = 0;
+    bool called = false;
 };
 // device, stream, and what tells apart the streams that share the per-thread handle
 using VocabKey = std::tuple<int, cudaStream_t, unsigned long long>;
@@ -702,8 +703,10 @@ static int vocab_workspace(cudaStream_t st, VocabWorkspace** out, std::unique_lo
 // At least `bytes` for a workspace that the caller holds.
 static int grow(VocabWorkspace& ws, size_t bytes, cudaStream_t st) {
     if (ws.bytes >= bytes) return GK_OK;
+    VocabCtl last = {};       // what the last call reported is kept
     if (ws.base) {
         GK_CUDA_TRY(cudaStreamSynchronize(st));   // work already enqueued may still use the old block
+        GK_CUDA_TRY(cudaMemcpy(&last, ws.base, sizeof(last), cudaMemcpyDeviceToHost));
         GK_CUDA_TRY(cudaFree(ws.base));
         ws.base = nullptr;
         ws.bytes = 0;
@@ -712,6 +715,7 @@ static int grow(VocabWorkspace& ws, size_t bytes, cudaStream_t st) {
     if (cudaMalloc(&p, bytes) != cudaSuccess) { cudaGetLastError(); return GK_ERR_NOMEM; }
     ws.base = p;
     ws.bytes = bytes;
+    GK_CUDA_TRY(cudaMemcpyAsync(p, &last, sizeof(last), cudaMemcpyHostToDevice, st));      // (staged before it returns)
     return GK_OK;
 }
 
@@ -793,14 +797,16 @@ static int check_head(const VocabCall& c, int32_t dtype) {
 
 // (no exception passes a C entry: the map's memory is the only source of one)
 static int run_head(VocabCall& c, bool distill, cudaStream_t st) try {
-    if (c.n == 0) {   // no rows: the weights' gradient is zero
-        if (c.dw) GK_CUDA_TRY(cudaMemset2DAsync(c.dw, 2 * c.lddw, 0, 2 * c.D, (size_t)c.V, st));
-        return GK_OK;
-    }
     VocabWorkspace* ws = nullptr;
     std::unique_lock<std::mutex> held;
     int rc = vocab_workspace(st, &ws, held);
     if (rc != GK_OK) return rc;
+    if (c.n == 0) {   // no rows: the weights' gradient is zero
+        if (c.dw) GK_CUDA_TRY(cudaMemset2DAsync(c.dw, 2 * c.lddw, 0, 2 * c.D, (size_t)c.V, st));
+        if (ws->base) GK_CUDA_TRY(cudaMemsetAsync(ws->base, 0, sizeof(VocabCtl), st));
+        ws->called = true;
+        return GK_OK;
+    }
     // rows that start and end on 16-byte boundaries are copied to shared memory as they lie
     const bool w_vec = (((uintptr_t)c.w | (uintptr_t)(2 * c.ldw) | (uintptr_t)(2 * c.D)) & 15) == 0;
     const bool dw_vec = (((uintptr_t)c.dw | (uintptr_t)(2 * c.lddw) | (uintptr_t)(2 * c.D)) & 15) == 0;
@@ -808,6 +814,7 @@ static int run_head(VocabCall& c, bool distill, cudaStream_t st) try {
     rc = grow(*ws, lay_out(c, distill, !w_vec, nullptr), st);
     if (rc != GK_OK) return rc;
     lay_out(c, distill, !w_vec, (char*)ws->base);
+    ws->called = true;
     return c.f16 ? enqueue<true>(c, distill, ws->sm_count, st) : enqueue<false>(c, distill, ws->sm_count, st);
 } catch (const std::bad_alloc&) {
     return GK_ERR_NOMEM;
@@ -922,9 +929,10 @@ extern "C" int gk_vocab_last_info(gk_stream_t stream, int64_t* host_out) {
     if (!ws) return GK_ERR_NULL;
     GK_CUDA_TRY(cudaStreamSynchronize((cudaStream_t)stream));
     std::lock_guard<std::mutex> held(ws->held);
-    if (!ws->base) return GK_ERR_NULL;
-    VocabCtl ctl;
-    GK_CUDA_TRY(cudaMemcpy(&ctl, ws->base, sizeof(ctl), cudaMemcpyDeviceToHost));
+    if (!ws->called) return GK_ERR_NULL;
+    VocabCtl ctl = {};
+    if (ws->base)       // else no call had rows
+        GK_CUDA_TRY(cudaMemcpy(&ctl, ws->base, sizeof(ctl), cudaMemcpyDeviceToHost));
     host_out[0] = ctl.status;
     host_out[1] = ctl.n_valid;
     return GK_OK;

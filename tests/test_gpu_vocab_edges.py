@@ -136,3 +136,40 @@ def test_a_workspace_reserved_for_more_rows_can_be_captured_with_fewer(n, fewer,
                 stream.synchronize()
                 assert torch.equal(out.loss, eager.loss) and torch.equal(out.dh, eager.dh)
                 assert not dw or torch.equal(out.dw, eager.dw)
+
+
+# --- calls without rows -----------------------------------------------------------------------------------
+
+
+def test_a_call_without_rows_is_the_last_call():
+    w = torch.ones(30, 16, dtype=torch.bfloat16, device=DEV)
+    none = (torch.empty(0, 16, dtype=torch.bfloat16, device=DEV), w, torch.empty(0, dtype=torch.int64, device=DEV))
+    e, f = torch.empty(0, device=DEV), torch.empty(3, device=DEV)
+    stream = torch.cuda.Stream(priority=-1)       # (no other test's: torch deals streams out in turn)
+    with torch.cuda.stream(stream):
+        with pytest.raises(gk.GkError):
+            gk.gk_vocab_last_info()                       # no call yet
+        gk.gk_vocab_loss(*none, e, e, dw=torch.ones_like(w))
+        assert gk.gk_vocab_last_info() == (0, 0)
+        gk.gk_vocab_reserve(3, 16, 30)
+        assert gk.gk_vocab_last_info() == (0, 0)
+        gk.gk_vocab_loss(w[:3], w, torch.zeros(3, dtype=torch.int64, device=DEV), f, f.clone())
+        assert gk.gk_vocab_last_info() == (0, 3)
+        gk.gk_vocab_loss(*none, e, e, dw=torch.ones_like(w))
+        assert gk.gk_vocab_last_info() == (0, 0)
+        gk.gk_vocab_loss(w[:3], w, torch.zeros(3, dtype=torch.int64, device=DEV), f, f.clone())
+        assert gk.gk_vocab_last_info() == (0, 3)
+        gk.gk_vocab_reserve(3000, 16, 30)                 # a larger block: the last call stays the last
+        assert gk.gk_vocab_last_info() == (0, 3)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            gk.gk_vocab_loss(w[:5], w, torch.zeros(5, dtype=torch.int64, device=DEV), torch.empty(5, device=DEV), torch.empty(5, device=DEV))
+        gk.gk_vocab_loss(*none, e, e, dw=torch.ones_like(w))
+        assert gk.gk_vocab_last_info() == (0, 0)
+        graph.replay()
+        assert gk.gk_vocab_last_info() == (0, 5)
+    other = torch.cuda.Stream(priority=-1)
+    with torch.cuda.stream(other):
+        gk.gk_vocab_reserve(3, 16, 30)
+        with pytest.raises(gk.GkError):
+            gk.gk_vocab_last_info()
