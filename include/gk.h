@@ -44,7 +44,7 @@ typedef enum gk_status {
     GK_ERR_LIMIT = -9,     /* size beyond a fixed built-in limit */
     GK_ERR_TYPE = -10,     /* gk_vocab_*: not one of the element types the call takes */
     GK_ERR_STRIDE = -11,   /* gk_vocab_*: a row stride shorter than the row */
-    GK_ERR_TEMPERATURE = -12 /* gk_vocab_*: temperature not positive and finite */
+    GK_ERR_TEMPERATURE = -12 /* gk_vocab_*: temperature or its reciprocal not positive and finite */
 } gk_status;
 
 /* Element types of the gk_vocab_* calls. */

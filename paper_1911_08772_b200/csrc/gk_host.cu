@@ -307,7 +307,7 @@ extern "C" const char* gk_strerror(int code) {
         case GK_ERR_LIMIT: return "size beyond a built-in limit";
         case GK_ERR_TYPE: return "element type not taken by this call";
         case GK_ERR_STRIDE: return "row stride shorter than the row";
-        case GK_ERR_TEMPERATURE: return "temperature must be positive and finite";
+        case GK_ERR_TEMPERATURE: return "temperature must be positive and finite, and so must its reciprocal";
         default: return "unknown gk_status";
     }
 }

@@ -855,7 +855,7 @@ extern "C" int gk_vocab_distill(const void* h, int64_t ldh, const void* w, int64
     if (rc != GK_OK) return rc;
     if (n > 0 && (!t_idx || !t_val)) return GK_ERR_NULL;
     if (K < 1 || K > kVocabMaxPairs) return GK_ERR_K;
-    if (!(temperature > 0.f) || !(temperature < INFINITY)) return GK_ERR_TEMPERATURE;
+    if (!temperature_ok(temperature)) return GK_ERR_TEMPERATURE;
     c.K = K;
     c.f16 = dtype == GK_TYPE_F16;
     c.inv_T = 1.f / temperature;

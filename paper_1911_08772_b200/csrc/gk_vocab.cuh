@@ -90,6 +90,9 @@ inline cudaError_t launch_next(void (*kernel)(Params...), dim3 grid, unsigned th
     return cudaLaunchKernelEx(&cfg, kernel, static_cast<Args&&>(args)...);
 }
 
+// T and what the kernels multiply by, 1 / T and log2(e) / T, are positive and finite.
+inline bool temperature_ok(float T) { return T > 0.f && T < INFINITY && (float)(1.4426950408889634 / (double)T) < INFINITY; }
+
 __host__ __device__ inline int64_t round_up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
 
 // The products (gk_vocab_gemm.cu).  v0, v1: the columns of the vocabulary [v0, v1).

@@ -635,7 +635,7 @@ extern "C" int gk_vocab_topk(const void* logits, int64_t ld, int32_t dtype, int6
     if (ld < V) return GK_ERR_STRIDE;
     if (((uintptr_t)logits & (dtype == GK_TYPE_F32 ? 3 : 1)) != 0) return GK_ERR_ALIGN;
     if (k < 1 || k > V || k > kVocabMaxPairs) return GK_ERR_K;
-    if (!(temperature > 0.f) || !(temperature < INFINITY)) return GK_ERR_TEMPERATURE;
+    if (!temperature_ok(temperature)) return GK_ERR_TEMPERATURE;
     if (n == 0) return GK_OK;
     cudaStream_t st = (cudaStream_t)stream;
     int dev = 0, sms = 0;
