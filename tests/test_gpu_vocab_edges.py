@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from paper_1911_08772_b200 import binding as gk
-from test_gpu_vocab_head import DEV, TYPES, Out, _library, distill, hard_loss, make  # noqa: F401  (_library: a fixture)
+from test_gpu_vocab_head import DEV, TYPES, Out, _library, check, distill, hard_loss, make  # noqa: F401  (_library: a fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -28,6 +28,32 @@ def test_a_last_piece_of_fewer_blocks_than_dh_has_parts(V, columns, dw, dtype, b
     budget(2 * 256 * columns)
     hard_loss(200, 136, V, dtype, seed=60, left_out=0.1, dw=dw)
     distill(200, 136, V, 9, dtype, seed=61, dw=dw)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_columns_past_the_end_of_logits_far_below_zero(dtype, budget):
+    """With all logits near -200 the columns past the vocabulary's end, whose sums are 0, are far above the rest:
+    nothing of them may reach a gradient, in one piece or in the last of several, nor of what a call before, of a
+    vocabulary that ends on 16 bytes, left there."""
+    n, D = 200, 72
+    for V, columns in ((1301, 4096), (1301, 512), (1283, 256)):
+        budget(2 * 256 * columns)
+        _, _, _, hd, wd = make(n, D, (V + 7) // 8 * 8, dtype, 62)
+        last = Out(n, D, (V + 7) // 8 * 8, dtype)
+        gk.gk_vocab_loss(hd, wd, torch.zeros(n, dtype=torch.int64, device=DEV), last.loss[:n], last.lse[:n],
+                         row_grad=torch.full((n,), math.nan, device=DEV), dh=last.dh, dw=last.dw)
+        assert bool(torch.isnan(last.dw).all())
+        gen, h, w, hd, wd = make(n, D, V, dtype, 62)
+        h[:, 0] = 1.0
+        w[:, 0] = -200.0
+        hd.copy_(h)
+        wd.copy_(w)
+        target = torch.randint(0, V, (n,), generator=gen)
+        g = torch.randn(n, generator=gen)
+        out = Out(n, D, V, dtype)
+        gk.gk_vocab_loss(hd, wd, target.to(DEV), out.loss[:n], out.lse[:n], row_grad=g.to(DEV), dh=out.dh, dw=out.dw)
+        one = torch.ones(n, 1, dtype=torch.float64)
+        check(out, h, w, target[:, None], one, torch.zeros_like(one), 1.0, g.double(), torch.ones(n, dtype=torch.bool), dtype)
 
 
 # --- lanes of a reading warp that find something and lanes that do not ------------------------------------
@@ -173,3 +199,48 @@ def test_a_call_without_rows_is_the_last_call():
         gk.gk_vocab_reserve(3, 16, 30)
         with pytest.raises(gk.GkError):
             gk.gk_vocab_last_info()
+
+
+# --- numbers ----------------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,D,V,K", [(1, 16, 5, 1), (3, 65, 300, 300), (130, 72, 515, 7), (1100, 64, 3000, 40), (64, 136, 20000, 100)])
+def test_distillation_without_gradients(n, D, V, K, dtype):
+    distill(n, D, V, K, dtype, seed=n + K, T=1.0 if n % 2 else 2.0, mass=n % 3 == 0, dh=False, dw=False)
+    distill(n, D, V, K, dtype, seed=n + K + 1, T=1.5, mass=n % 3 != 0, holes=0.4, dh=False, dw=False)
+
+
+def off_by(got, want, dtype):
+    """How far `got` is from `want` (64 bits) in units of what want rounded to the type is off by, as norms."""
+    want = want.cpu()
+    return float((got.cpu().double() - want).norm() / (want.to(dtype).double() - want).norm())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("soft", [False, True])
+@pytest.mark.parametrize("n,D,V,columns", [(1000, 200, 3000, 0), (600, 256, 20000, 0), (600, 256, 20000, 4096)])
+def test_gradients_are_rounded_twice_and_no_more(n, D, V, columns, soft, dtype, budget):
+    """As norms over many rows the errors of independent roundings add as squares: a logit gradient's (1), what is
+    kept of a logit (0.48 of one in bf16: 3.9e-4 against 8.1e-4 root mean square, 0.25 in fp16) and the result's
+    own (1): at most sqrt(2.23) = 1.49 times the last alone.  One rounding more would be 1.79 (1.75).  (The bounds
+    element by element in vocab_util.py leave room for it.)"""
+    if columns:
+        budget(2 * 768 * columns)
+    gen, h, w, hd, wd = make(n, D, V, dtype, 66)
+    K = 30 if soft else 1
+    idx = torch.stack([torch.randperm(V, generator=gen)[:K].sort().values for _ in range(n)])
+    t = torch.randn(n, K, generator=gen) * 2
+    q = torch.softmax(t.double(), 1)
+    out = Out(n, D, V, dtype)
+    g = torch.rand(n, generator=gen) + 0.5
+    if soft:
+        gk.gk_vocab_distill(hd, wd, idx.to(torch.int32).to(DEV), t.to(DEV), out.loss[:n], out.lse[:n], row_grad=g.to(DEV), dh=out.dh, dw=out.dw)
+    else:
+        gk.gk_vocab_loss(hd, wd, idx[:, 0].to(DEV), out.loss[:n], out.lse[:n], row_grad=g.to(DEV), dh=out.dh, dw=out.dw)
+    hx, wx, gx, qx = (x.double().to(DEV) for x in (h, w, g, q))
+    dz = torch.softmax(hx @ wx.t(), 1)
+    dz.scatter_add_(1, idx.to(DEV), -qx)
+    dz *= gx[:, None]
+    assert off_by(out.dh, dz @ wx, dtype) <= 1.6
+    assert off_by(out.dw, dz.t() @ hx, dtype) <= 1.6
