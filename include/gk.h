@@ -14,7 +14,10 @@
  *   - The library owns a small scratch workspace per (device, stream), created
  *     by the first call that needs it (cudaMalloc; use gk_reserve to do that
  *     ahead of time).  Two calls that overlap on the GPU must use different
- *     streams.
+ *     streams.  Calls of several host threads are safe on any streams: those
+ *     on one stream are enqueued whole, one after the other in no promised
+ *     order, and each thread's cudaStreamPerThread has a workspace of its own.
+ *     (gk_sparsify_static's scratch is one for all: see there.)
  *   - Return value: GK_OK or a negative gk_status for errors detected on the
  *     host before anything is enqueued.  Conditions found on the device
  *     (truncated output, a bounded wait that ran out, a malformed segment
@@ -340,9 +343,6 @@ int gk_set_params(int unbiased_std, int max_rounds);
  *   dw_out     DEVICE out  V rows of D, row stride lddw; NULL: not wanted
  * With neither dh nor dw only the forward pass runs (scoring).  dh and dw must not overlap h, w or
  * each other.  Results do not depend on timing: no atomics on floating-point data.
- *
- * Calls of several host threads are safe on any streams: those on one stream are enqueued whole, one after the
- * other (in no promised order), and each thread's cudaStreamPerThread has a workspace of its own.
  *
  * The workspace is the call's own, per (device, stream), grown on first use (gk_vocab_reserve
  * does that ahead; a call that fits allocates nothing and can be captured in a graph, which stays good until a

@@ -592,7 +592,8 @@ static DgPlan* dgck_plan(int dev, int sm_count) {
 static int enqueue_dgck(const float* src, float* eps, int64_t d, int64_t k, const int32_t* sample_idx, int64_t m,
                         int32_t* idx_out, float* val_out, int64_t* nnz_out, cudaStream_t st) {
     Workspace* ws = nullptr;
-    const int wrc = acquire_workspace(d, 1, st, &ws);
+    WorkspaceLock held;
+    const int wrc = acquire_workspace(d, 1, st, &ws, held);
     if (wrc != GK_OK) return wrc;
     int dev = 0;
     GK_CUDA_TRY(cudaGetDevice(&dev));

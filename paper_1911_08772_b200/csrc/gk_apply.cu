@@ -146,7 +146,8 @@ k_apply_sparse(float* __restrict__ x, int64_t d, const ApplyLists L, const int64
 static int enqueue_apply(float* x, int64_t d, const ApplyLists& L, const int64_t* nnz, int32_t P, int64_t cap,
                          float alpha, cudaStream_t st) {
     Workspace* ws = nullptr;
-    const int wrc = acquire_workspace(1, 1, st, &ws);
+    WorkspaceLock held;
+    const int wrc = acquire_workspace(1, 1, st, &ws, held);
     if (wrc != GK_OK) return wrc;
     GK_CUDA_TRY(cudaMemsetAsync(&ws->ctrl->stats.status, 0, sizeof(int), st));
     const int64_t bpl = (cap + kApplyThreads - 1) / kApplyThreads;   // blocks per list

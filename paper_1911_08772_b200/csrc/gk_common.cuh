@@ -5,6 +5,9 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <mutex>
+#include <tuple>
+
 #include "gk.h"
 
 namespace gk {
@@ -91,7 +94,15 @@ struct Ctrl {
     unsigned long long dgc[4];
 };
 
+// Held by a call from the lookup to its last launch: calls of two host threads on one stream neither mix
+// their launches over the workspace nor replace it under one another.
+using WorkspaceLock = std::unique_lock<std::mutex>;
+// Device, stream, and what tells apart the streams that share the per-thread handle.
+using WorkspaceKey = std::tuple<int, cudaStream_t, unsigned long long>;
+int workspace_key(cudaStream_t stream, WorkspaceKey& key);
+
 struct Workspace {
+    std::mutex mu;
     void* base = nullptr;          // device allocation
     size_t bytes = 0;
     int64_t d_cap = 0;             // sizes the allocation was made for
@@ -118,7 +129,7 @@ struct Workspace {
 };
 
 // host side (gk_host.cu)
-int acquire_workspace(int64_t d, int32_t S, cudaStream_t stream, Workspace** out);
+int acquire_workspace(int64_t d, int32_t S, cudaStream_t stream, Workspace** out, WorkspaceLock& held);
 int cuda_fail(cudaError_t e);   // records the error text, returns GK_ERR_CUDA
 void note_launch(int n = 1);
 // Stage timing: mark(ws, st, i) records event i (0 = before the first kernel) when tracing is on.

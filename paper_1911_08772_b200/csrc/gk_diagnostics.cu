@@ -141,7 +141,8 @@ extern "C" int gk_histogram(const float* u, int64_t d, float lo, float inv_w, in
     if ((uintptr_t)u & 15u) return GK_ERR_ALIGN;
     cudaStream_t st = (cudaStream_t)stream;
     Workspace* ws = nullptr;
-    const int wrc = acquire_workspace(1, 1, st, &ws);
+    WorkspaceLock held;
+    const int wrc = acquire_workspace(1, 1, st, &ws, held);
     if (wrc != GK_OK) return wrc;
     GK_CUDA_TRY(cudaMemsetAsync(counts_out, 0, sizeof(int64_t) * (size_t)(nbins + 2), st));
     const int64_t n4 = d >> 2;
@@ -167,7 +168,8 @@ extern "C" int gk_error_ratio(const float* eps, int64_t d, const float* val, con
     if ((uintptr_t)eps & 15u) return GK_ERR_ALIGN;
     cudaStream_t st = (cudaStream_t)stream;
     Workspace* ws = nullptr;
-    const int wrc = acquire_workspace(d, 1, st, &ws);
+    WorkspaceLock held;
+    const int wrc = acquire_workspace(d, 1, st, &ws, held);
     if (wrc != GK_OK) return wrc;
     const int64_t n4 = d >> 2;
     int64_t grid = (n4 + 4 * kDiagThreads - 1) / (4 * kDiagThreads);

@@ -7,8 +7,8 @@
 #include <atomic>
 #include <map>
 #include <mutex>
+#include <new>
 #include <string>
-#include <utility>
 
 #include "gk_alg1.cuh"
 #include "gk_common.cuh"
@@ -17,7 +17,7 @@
 namespace gk {
 
 static std::mutex g_mu;
-static std::map<std::pair<int, cudaStream_t>, Workspace> g_ws;
+static std::map<WorkspaceKey, Workspace> g_ws;      // (entries stay where they are)
 static std::atomic<int64_t> g_launches{0};
 static std::atomic<int64_t> g_capacity{0};
 static thread_local std::string g_cuda_err;
@@ -69,11 +69,24 @@ static Layout layout_for(int64_t d, int32_t S) {
     return L;
 }
 
-int acquire_workspace(int64_t d, int32_t S, cudaStream_t stream, Workspace** out) {
+int workspace_key(cudaStream_t stream, WorkspaceKey& key) {
     int dev = 0;
     GK_CUDA_TRY(cudaGetDevice(&dev));
-    std::lock_guard<std::mutex> lock(g_mu);
-    Workspace& ws = g_ws[std::make_pair(dev, stream)];
+    unsigned long long id = 0;
+    if (stream == cudaStreamPerThread) GK_CUDA_TRY(cudaStreamGetId(stream, &id));
+    key = WorkspaceKey(dev, stream, id);
+    return GK_OK;
+}
+
+// (no exception passes a C entry: the map's memory is the only source of one)
+int acquire_workspace(int64_t d, int32_t S, cudaStream_t stream, Workspace** out, WorkspaceLock& held) try {
+    WorkspaceKey key;
+    const int rc = workspace_key(stream, key);
+    if (rc != GK_OK) return rc;
+    std::unique_lock<std::mutex> all(g_mu);
+    Workspace& ws = g_ws[key];
+    all.unlock();
+    held = WorkspaceLock(ws.mu);
     if (ws.base == nullptr || d > ws.d_cap || S > ws.s_cap) {
         const int64_t nd = d > ws.d_cap ? d : ws.d_cap;
         const int32_t ns = S > ws.s_cap ? S : ws.s_cap;
@@ -107,18 +120,27 @@ int acquire_workspace(int64_t d, int32_t S, cudaStream_t stream, Workspace** out
         ws.rowcnt = reinterpret_cast<unsigned int*>(b + L.rowcnt);
         ws.tile_status = reinterpret_cast<unsigned long long*>(b + L.tile_status);
         ws.seg_block = b + L.seg;
-        GK_CUDA_TRY(cudaDeviceGetAttribute(&ws.sm_count, cudaDevAttrMultiProcessorCount, dev));
+        GK_CUDA_TRY(cudaDeviceGetAttribute(&ws.sm_count, cudaDevAttrMultiProcessorCount, std::get<0>(key)));
     }
     *out = &ws;
     return GK_OK;
+} catch (const std::bad_alloc&) {
+    return GK_ERR_NOMEM;
 }
 
-static Workspace* find_workspace(cudaStream_t stream) {
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess) return nullptr;
-    std::lock_guard<std::mutex> lock(g_mu);
-    auto it = g_ws.find(std::make_pair(dev, stream));
-    return it == g_ws.end() ? nullptr : &it->second;
+// nullptr where no call was made on this stream
+static Workspace* find_workspace(cudaStream_t stream, WorkspaceLock& held) {
+    WorkspaceKey key;
+    if (workspace_key(stream, key) != GK_OK) return nullptr;
+    Workspace* ws;
+    {
+        std::lock_guard<std::mutex> all(g_mu);
+        auto it = g_ws.find(key);
+        if (it == g_ws.end()) return nullptr;
+        ws = &it->second;
+    }
+    held = WorkspaceLock(ws->mu);
+    return ws->base ? ws : nullptr;
 }
 
 // staging buffers of gk_sparsify_host, one set per device
@@ -198,7 +220,8 @@ extern "C" int gk_debug_set(int key, int64_t value) {
 extern "C" int gk_reserve(int64_t d, int32_t S, gk_stream_t stream) {
     if (d < 1 || d > 2147483647ll || S < 1 || S > kMaxSegments) return GK_ERR_SIZE;
     Workspace* ws = nullptr;
-    return acquire_workspace(d, S, (cudaStream_t)stream, &ws);
+    WorkspaceLock held;
+    return acquire_workspace(d, S, (cudaStream_t)stream, &ws, held);
 }
 
 extern "C" int64_t gk_workspace_bytes(int64_t d, int32_t S) {
@@ -208,7 +231,8 @@ extern "C" int64_t gk_workspace_bytes(int64_t d, int32_t S) {
 
 extern "C" int gk_last_stats(gk_stream_t stream, gk_stats* host_out) {
     if (!host_out) return GK_ERR_NULL;
-    Workspace* ws = find_workspace((cudaStream_t)stream);
+    WorkspaceLock held;
+    Workspace* ws = find_workspace((cudaStream_t)stream, held);
     if (!ws) return GK_ERR_NULL;
     GK_CUDA_TRY(cudaStreamSynchronize((cudaStream_t)stream));
     GK_CUDA_TRY(cudaMemcpy(host_out, &ws->ctrl->stats, sizeof(gk_stats), cudaMemcpyDeviceToHost));
@@ -217,7 +241,8 @@ extern "C" int gk_last_stats(gk_stream_t stream, gk_stats* host_out) {
 
 extern "C" int dgck_last_info(gk_stream_t stream, int64_t* host_out) {
     if (!host_out) return GK_ERR_NULL;
-    Workspace* ws = find_workspace((cudaStream_t)stream);
+    WorkspaceLock held;
+    Workspace* ws = find_workspace((cudaStream_t)stream, held);
     if (!ws) return GK_ERR_NULL;
     GK_CUDA_TRY(cudaStreamSynchronize((cudaStream_t)stream));
     unsigned long long v[4];
@@ -228,7 +253,8 @@ extern "C" int dgck_last_info(gk_stream_t stream, int64_t* host_out) {
 
 extern "C" int gk_last_segment_stats(gk_stream_t stream, int32_t S, gk_stats* host_out) {
     if (!host_out) return GK_ERR_NULL;
-    Workspace* ws = find_workspace((cudaStream_t)stream);
+    WorkspaceLock held;
+    Workspace* ws = find_workspace((cudaStream_t)stream, held);
     if (!ws || S < 1 || S > ws->s_cap) return GK_ERR_SIZE;
     GK_CUDA_TRY(cudaStreamSynchronize((cudaStream_t)stream));
     GK_CUDA_TRY(cudaMemcpy(host_out, segmented_stats_ptr(ws), sizeof(gk_stats) * (size_t)S,
@@ -245,7 +271,8 @@ extern "C" int gk_last_segment_stats(gk_stream_t stream, int32_t S, gk_stats* ho
 
 extern "C" int gk_last_path_info(gk_stream_t stream, int64_t* host_out) {
     if (!host_out) return GK_ERR_NULL;
-    Workspace* ws = find_workspace((cudaStream_t)stream);
+    WorkspaceLock held;
+    Workspace* ws = find_workspace((cudaStream_t)stream, held);
     if (!ws) return GK_ERR_NULL;
     GK_CUDA_TRY(cudaStreamSynchronize((cudaStream_t)stream));
     unsigned int v[5];
@@ -263,7 +290,8 @@ extern "C" int gk_stage_timing(int enable) {
 
 extern "C" int gk_last_stage_ms(gk_stream_t stream, float* ms_out, int* n_stages) {
     if (!ms_out || !n_stages) return GK_ERR_NULL;
-    Workspace* ws = find_workspace((cudaStream_t)stream);
+    WorkspaceLock held;
+    Workspace* ws = find_workspace((cudaStream_t)stream, held);
     if (!ws) return GK_ERR_NULL;
     GK_CUDA_TRY(cudaStreamSynchronize((cudaStream_t)stream));
     *n_stages = ws->n_stages;
@@ -281,7 +309,8 @@ extern "C" int gk_last_stage_ms(gk_stream_t stream, float* ms_out, int* n_stages
 
 extern "C" int gk_last_cta_trace(gk_stream_t stream, uint64_t* host_out, int* n_ctas) {
     if (!host_out || !n_ctas) return GK_ERR_NULL;
-    Workspace* ws = find_workspace((cudaStream_t)stream);
+    WorkspaceLock held;
+    Workspace* ws = find_workspace((cudaStream_t)stream, held);
     if (!ws) return GK_ERR_NULL;
     GK_CUDA_TRY(cudaStreamSynchronize((cudaStream_t)stream));
     *n_ctas = ws->last_fused ? ws->last_grid : 0;
@@ -346,7 +375,8 @@ extern "C" int gk_sparsify_host(const float* g, float* eps, int64_t d, int64_t k
     }
     cudaStream_t st = hs->stream;
     Workspace* ws = nullptr;
-    const int wrc = acquire_workspace(d, 1, st, &ws);
+    WorkspaceLock held;
+    const int wrc = acquire_workspace(d, 1, st, &ws, held);
     if (wrc != GK_OK) return wrc;
     GK_CUDA_TRY(cudaMemcpyAsync(hs->g, g, sizeof(float) * d, cudaMemcpyHostToDevice, st));
     GK_CUDA_TRY(cudaMemcpyAsync(hs->eps, eps, sizeof(float) * d, cudaMemcpyHostToDevice, st));

@@ -351,7 +351,8 @@ extern "C" int gk_sparsify_segmented(const float* g, float* eps, int64_t d, cons
     if (a < b + n && b < a + n) return GK_ERR_ALIAS;
     cudaStream_t st = (cudaStream_t)stream;
     Workspace* ws = nullptr;
-    const int wrc = acquire_workspace(d, S, st, &ws);
+    WorkspaceLock held;
+    const int wrc = acquire_workspace(d, S, st, &ws, held);
     if (wrc != GK_OK) return wrc;
     if (selected_path() == 0) {
         const int frc = enqueue_gk_fused_seg(ws, g, eps, d, seg_offsets, seg_k, S, idx_out, val_out, seg_nnz_out,

@@ -273,7 +273,8 @@ extern "C" int gk_sparsify(const float* g, float* eps, int64_t d, int64_t k, int
     const int rc = gk::check_vectors(g, eps, d, k, idx_out, val_out, nnz_out);
     if (rc != GK_OK) return rc;
     gk::Workspace* ws = nullptr;
-    const int wrc = gk::acquire_workspace(d, 1, (cudaStream_t)stream, &ws);
+    gk::WorkspaceLock held;
+    const int wrc = gk::acquire_workspace(d, 1, (cudaStream_t)stream, &ws, held);
     if (wrc != GK_OK) return wrc;
     return gk::enqueue_gk_sparsify(ws, g, eps, d, k, idx_out, val_out, nnz_out, (cudaStream_t)stream);
 }
@@ -285,7 +286,8 @@ extern "C" int gk_select(const float* u, int64_t d, int64_t k, int32_t* idx_out,
     if (k < 1 || k > d) return GK_ERR_K;
     if ((uintptr_t)u & 15u) return GK_ERR_ALIGN;
     gk::Workspace* ws = nullptr;
-    const int wrc = gk::acquire_workspace(d, 1, (cudaStream_t)stream, &ws);
+    gk::WorkspaceLock held;
+    const int wrc = gk::acquire_workspace(d, 1, (cudaStream_t)stream, &ws, held);
     if (wrc != GK_OK) return wrc;
     return gk::enqueue_gk_sparsify(ws, u, nullptr, d, k, idx_out, val_out, nnz_out, (cudaStream_t)stream);
 }

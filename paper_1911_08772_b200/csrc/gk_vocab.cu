@@ -32,7 +32,6 @@
 #include <map>
 #include <mutex>
 #include <new>
-#include <tuple>
 
 #include "gk_vocab.cuh"
 
@@ -635,10 +634,8 @@ struct VocabWorkspace {
     int sm_count = 0;
     bool called = false;
 };
-// device, stream, and what tells apart the streams that share the per-thread handle
-using VocabKey = std::tuple<int, cudaStream_t, unsigned long long>;
 static std::mutex g_vocab_mu;
-static std::map<VocabKey, VocabWorkspace> g_vocab_ws;      // (entries stay where they are)
+static std::map<WorkspaceKey, VocabWorkspace> g_vocab_ws;      // (entries stay where they are)
 static std::atomic<int64_t> g_vocab_budget{(int64_t)2 << 30};
 
 static int64_t piece_columns(int64_t n_pad, int64_t V) {
@@ -675,26 +672,17 @@ static size_t lay_out(VocabCall& c, bool distill, bool copy_w, char* base) {
     return at;
 }
 
-static int vocab_key(cudaStream_t st, VocabKey& key) {
-    int dev = 0;
-    GK_CUDA_TRY(cudaGetDevice(&dev));
-    unsigned long long id = 0;
-    if (st == cudaStreamPerThread) GK_CUDA_TRY(cudaStreamGetId(st, &id));
-    key = VocabKey(dev, st, id);
-    return GK_OK;
-}
-
 // The stream's workspace, held by `lock` from here on.
-static int vocab_workspace(cudaStream_t st, VocabWorkspace** out, std::unique_lock<std::mutex>& lock) {
-    VocabKey key;
-    const int rc = vocab_key(st, key);
+static int vocab_workspace(cudaStream_t st, VocabWorkspace** out, WorkspaceLock& lock) {
+    WorkspaceKey key;
+    const int rc = workspace_key(st, key);
     if (rc != GK_OK) return rc;
     VocabWorkspace* ws;
     {
         std::lock_guard<std::mutex> all(g_vocab_mu);
         ws = &g_vocab_ws[key];
     }
-    lock = std::unique_lock<std::mutex>(ws->held);
+    lock = WorkspaceLock(ws->held);
     if (ws->sm_count == 0) GK_CUDA_TRY(cudaDeviceGetAttribute(&ws->sm_count, cudaDevAttrMultiProcessorCount, std::get<0>(key)));
     *out = ws;
     return GK_OK;
@@ -798,7 +786,7 @@ static int check_head(const VocabCall& c, int32_t dtype) {
 // (no exception passes a C entry: the map's memory is the only source of one)
 static int run_head(VocabCall& c, bool distill, cudaStream_t st) try {
     VocabWorkspace* ws = nullptr;
-    std::unique_lock<std::mutex> held;
+    WorkspaceLock held;
     int rc = vocab_workspace(st, &ws, held);
     if (rc != GK_OK) return rc;
     if (c.n == 0) {   // no rows: the weights' gradient is zero
@@ -906,7 +894,7 @@ extern "C" int gk_vocab_reserve(int64_t n, int64_t D, int64_t V, int32_t K, int 
     const int rc = head_sizes_ok(n, D, V, K);
     if (rc != GK_OK) return rc;
     VocabWorkspace* ws = nullptr;
-    std::unique_lock<std::mutex> held;
+    WorkspaceLock held;
     const int wrc = vocab_workspace((cudaStream_t)stream, &ws, held);
     if (wrc != GK_OK) return wrc;
     VocabCall c = {};
@@ -917,8 +905,8 @@ extern "C" int gk_vocab_reserve(int64_t n, int64_t D, int64_t V, int32_t K, int 
 
 extern "C" int gk_vocab_last_info(gk_stream_t stream, int64_t* host_out) {
     if (!host_out) return GK_ERR_NULL;
-    VocabKey key;
-    const int rc = vocab_key((cudaStream_t)stream, key);
+    WorkspaceKey key;
+    const int rc = workspace_key((cudaStream_t)stream, key);
     if (rc != GK_OK) return rc;
     VocabWorkspace* ws = nullptr;
     {

@@ -303,7 +303,8 @@ extern "C" int topk_exact(const float* u, int64_t d, int64_t k, int32_t* idx_out
     if (k < 1 || k > d) return GK_ERR_K;
     if ((uintptr_t)u & 15u) return GK_ERR_ALIGN;
     Workspace* ws = nullptr;
-    const int wrc = acquire_workspace(d, 1, (cudaStream_t)stream, &ws);
+    WorkspaceLock held;
+    const int wrc = acquire_workspace(d, 1, (cudaStream_t)stream, &ws, held);
     if (wrc != GK_OK) return wrc;
     if (selected_path() == 0) {
         const int frc = enqueue_topk_fused(ws, u, nullptr, d, k, idx_out, val_out, nullptr, (cudaStream_t)stream);
@@ -323,7 +324,8 @@ extern "C" int topk_sparsify(const float* g, float* eps, int64_t d, int64_t k, i
     if (a < b + n && b < a + n) return GK_ERR_ALIAS;
     cudaStream_t st = (cudaStream_t)stream;
     Workspace* ws = nullptr;
-    const int wrc = acquire_workspace(d, 1, st, &ws);
+    WorkspaceLock held;
+    const int wrc = acquire_workspace(d, 1, st, &ws, held);
     if (wrc != GK_OK) return wrc;
     if (selected_path() == 0) {
         const int frc = enqueue_topk_fused(ws, g, eps, d, k, idx_out, val_out, nnz_out, st);
