@@ -18,6 +18,11 @@
  *     on one stream are enqueued whole, one after the other in no promised
  *     order, and each thread's cudaStreamPerThread has a workspace of its own.
  *     (gk_sparsify_static's scratch is one for all: see there.)
+ *   - A call that does not synchronise and has no workspace to allocate can be
+ *     captured in a graph, which stays good until a call that needs more
+ *     replaces the workspace of the stream that it was captured on.  All
+ *     graphs captured on a stream share its workspace, on whatever streams
+ *     they are replayed: their replays must not overlap.
  *   - Return value: GK_OK or a negative gk_status for errors detected on the
  *     host before anything is enqueued.  Conditions found on the device
  *     (truncated output, a bounded wait that ran out, a malformed segment

@@ -1488,6 +1488,11 @@ int enqueue_gk_fused(Workspace* ws, const float* src, float* eps, int64_t d, int
     ws->last_grid = (int)geo.G;
     stage_mark(ws, st, 0);
     if (++ws->fused_calls == 0u) ws->fused_calls = 1u;   // 0 is what an unwritten record holds
+    // A graph repeats a launch with its number: its records of the replay before are cleared ahead of it.
+    cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+    if (cudaStreamIsCapturing(st, &capture) != cudaSuccess) cudaGetLastError();
+    if (capture == cudaStreamCaptureStatusActive)
+        GK_CUDA_TRY(cudaMemsetAsync(ws->part_recs, 0, (size_t)32 * (kFusedGridCap + 1), st));
     GK_CUDA_TRY(launch_fused(geo, st, src, eps, d, k, z, ws->ctrl, ws->part_recs, ws->bars, ws->rowcnt, idx_out, val_out, nnz_out, output_capacity(d), ws->cta_trace, ws->fused_calls));
     note_launch();
     stage_mark(ws, st, 1);
@@ -1578,7 +1583,8 @@ extern "C" int gk_sparsify_static(const float* g, float* eps, int64_t d, int64_t
     if (geo.G > kFusedGridCap || geo.n_rows > kStaticRowCap || !geo.fits) return GK_ERR_LIMIT;
     // The array keeps what the last call left.  The barrier counters and the global counts must
     // start at zero; the kernel resets them when it ends, but a call that was cut short would not have.
-    GK_CUDA_TRY(cudaMemsetAsync(bars, 0, kStaticBarBytes, st));
+    // The records before them (of the partial sums) carry the call's number, which a graph repeats.
+    GK_CUDA_TRY(cudaMemsetAsync(partials, 0, kStaticPartialBytes + kStaticBarBytes, st));
     const double pq = 1.0 - (double)k / (double)d;
     const double z = normal_quantile_upper(1.0 - pq);
     unsigned long long* trace = nullptr;  // no trace array in the fixed scratch
