@@ -244,19 +244,19 @@ __global__ void __launch_bounds__(1024) k_vocab_rows(VocabCall c) {
 __device__ __forceinline__ uint4 load8(const uint16_t* p, int64_t left) {
     const uintptr_t a = (uintptr_t)p;
     if (left >= 8) {
-        if ((a & 15) == 0) return __ldg((const uint4*)p);
+        if ((a & 15) == 0) return *(const uint4*)p;
         if ((a & 7) == 0) {
-            const uint2 x = __ldg((const uint2*)p), y = __ldg((const uint2*)p + 1);
+            const uint2 x = *(const uint2*)p, y = *((const uint2*)p + 1);
             return make_uint4(x.x, x.y, y.x, y.y);
         }
         if ((a & 3) == 0) {
             const unsigned* q = (const unsigned*)p;
-            return make_uint4(__ldg(q), __ldg(q + 1), __ldg(q + 2), __ldg(q + 3));
+            return make_uint4(q[0], q[1], q[2], q[3]);
         }
     }
     unsigned v[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < left ? __ldg(p + i) : 0u;
+    for (int i = 0; i < 8; ++i) v[i] = i < left ? p[i] : 0u;
     return make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
 }
 
@@ -287,10 +287,17 @@ __global__ void __launch_bounds__(128) k_vocab_gather(VocabCall c) {
     const int tid = threadIdx.x, lane = tid & 31;
     if (blockIdx.x >= c.n_pad) {
         const int64_t words = c.Dp / 8, total = c.V * words, threads = (gridDim.x - c.n_pad) * 128;
-#pragma unroll 4
-        for (int64_t i = (blockIdx.x - c.n_pad) * 128 + tid; i < total; i += threads) {
-            const int64_t v = i / words, k = (i - v * words) * 8;
-            ((uint4*)c.wc)[i] = load8((const uint16_t*)c.w + v * c.ldw + k, c.D - k);
+        // (the loads of four words before their stores)
+        for (int64_t i0 = (blockIdx.x - c.n_pad) * 128 + tid; i0 < total; i0 += 4 * threads) {
+            uint4 x[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int64_t i = i0 + j * threads, v = i / words, k = (i - v * words) * 8;
+                if (i < total) x[j] = load8((const uint16_t*)c.w + v * c.ldw + k, c.D - k);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (i0 + j * threads < total) ((uint4*)c.wc)[i0 + j * threads] = x[j];
         }
         return;
     }
@@ -353,7 +360,15 @@ __global__ void __launch_bounds__(128) k_vocab_gather(VocabCall c) {
     }
     const uint16_t* from = (const uint16_t*)c.h + r * c.ldh;
     const int64_t words = c.Dp / 8;
-    for (int64_t i = tid; i < words; i += 128) ((uint4*)to)[i] = load8(from + i * 8, c.D - i * 8);
+    for (int64_t i0 = tid; i0 < words; i0 += 4 * 128) {
+        uint4 x[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (i0 + j * 128 < words) x[j] = load8(from + (i0 + j * 128) * 8, c.D - (i0 + j * 128) * 8);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (i0 + j * 128 < words) ((uint4*)to)[i0 + j * 128] = x[j];
+    }
     if (c.target) {
         if (tid == 0) c.cls[at] = (int32_t)c.target[r];
         return;
@@ -438,7 +453,7 @@ __global__ void __launch_bounds__(1024) k_vocab_rows_done(VocabCall c) {
         const float2* p = c.part + at0 + mine;
 #pragma unroll 4
         for (int64_t t = wid * shares + share; t < tiles; t += 32 * shares) {
-            const float2 x = __ldcs(p + t * c.n_pad);
+            const float2 x = load_once(p + t * c.n_pad);
             join_max_sum(m, s, x.x, x.y);
         }
     }
@@ -528,8 +543,8 @@ __global__ void __launch_bounds__(256) k_vocab_scale(VocabCall c, int64_t v0, in
 #pragma unroll
     for (int j = 0; j < kScaleWords<DONE>; ++j)
         if (j * 256 < left) {
-            x[j] = __ldcs(mine + j * 256);
-            top[j] = __ldg(&c.part[(lo + (j * 256 + threadIdx.x) * 8) / kVocabTile * c.n_pad + at].x);
+            x[j] = load_once(mine + j * 256);
+            top[j] = c.part[(lo + (j * 256 + threadIdx.x) * 8) / kVocabTile * c.n_pad + at].x;
         }
     const int n_valid = c.ctl->n_valid;
     const int64_t r = c.row_of[at < c.n ? at : 0];
@@ -550,7 +565,7 @@ __global__ void __launch_bounds__(256) k_vocab_scale(VocabCall c, int64_t v0, in
         float m = -INFINITY, s = 0.f;
         if (wid < 4) {
             if (tid < tiles) {
-                const float2 x = __ldg(c.part + tid * c.n_pad + at);
+                const float2 x = c.part[tid * c.n_pad + at];
                 m = x.x;
                 s = x.y;
             }

@@ -115,6 +115,20 @@ __device__ __forceinline__ void after_previous() {
     asm volatile("griddepcontrol.launch_dependents;\ngriddepcontrol.wait;" ::: "memory");
 }
 
+// What earlier kernels wrote, the caller's inputs among it, is read by ordinary loads after that: __ldg and its kin
+// are for memory that nothing writes while the kernel is there, and may be moved ahead of the wait.  These two are
+// for what is read once.
+__device__ __forceinline__ uint4 load_once(const uint4* p) {
+    uint4 x;
+    asm volatile("ld.global.cs.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "l"(p));
+    return x;
+}
+__device__ __forceinline__ float2 load_once(const float2* p) {
+    float2 x;
+    asm volatile("ld.global.cs.v2.f32 {%0, %1}, [%2];" : "=f"(x.x), "=f"(x.y) : "l"(p));
+    return x;
+}
+
 __device__ __forceinline__ bool teacher_ascending(const float4& t) { return ((int)t.w & 1) != 0; }
 __device__ __forceinline__ bool teacher_counts(const float4& t) { return ((int)t.w & 2) != 0; }
 

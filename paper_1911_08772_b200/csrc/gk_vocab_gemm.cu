@@ -274,7 +274,7 @@ __device__ __forceinline__ void find_first(const VocabCall& c, Patch& w, int n_v
             w.next = w.row;
         }
     } else if (w.pairs >> 16) {
-        w.next = __ldg(c.t_idx + (int64_t)w.row * c.K + (w.pairs & 0xffff));
+        w.next = c.t_idx[(int64_t)w.row * c.K + (w.pairs & 0xffff)];
     }
 }
 // `v`: the patch's columns; a register cannot be chosen at run time, so stretches of 32 columns with a pair in
@@ -300,9 +300,9 @@ __device__ __forceinline__ void take_pairs(const VocabCall& c, const Patch& w, c
                 float z;
                 asm volatile("ld.shared.f32 %0, [%1];"
                              : "=f"(z) : "r"(w.staging + w.lane * 128 + (((col >> 2) ^ (w.lane & 7)) << 4) + (col & 3) * 4) : "memory");
-                c.zt[row * c.K + j] = z;
-                ++j;
-                next = j < pairs_end ? __ldg(pairs + j) : 0x7fffffff;
+                const int at = j++;
+                next = j < pairs_end ? pairs[j] : 0x7fffffff;
+                c.zt[row * c.K + at] = z;
             }
             __syncwarp();
         }

@@ -244,3 +244,38 @@ def test_gradients_are_rounded_twice_and_no_more(n, D, V, columns, soft, dtype, 
     dz *= gx[:, None]
     assert off_by(out.dh, dz @ wx, dtype) <= 1.6
     assert off_by(out.dw, dz.t() @ hx, dtype) <= 1.6
+
+
+# --- calls one after another ------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("n,D,V", [(300, 200, 1501), (1100, 72, 3000), (64, 136, 20000)])
+def test_calls_that_read_what_the_call_before_wrote(n, D, V):
+    """The kernels of a call are set up while the one before them runs: without a wait between calls, over buffers
+    that each call writes anew, the results are those of calls with a wait after each."""
+    gen = torch.Generator(device=DEV).manual_seed(72)
+    w = (torch.randn(V, D, generator=gen, device=DEV) / 4).bfloat16()
+    hs = [torch.randn(n, D, generator=gen, device=DEV).bfloat16() for _ in range(6)]
+    zs = [torch.randn(n, V, generator=gen, device=DEV) * 3 for _ in range(6)]
+    K = 20
+
+    def steps(wait):
+        t_idx, t_val, t_lse = torch.empty(n, K, dtype=torch.int32, device=DEV), torch.empty(n, K, device=DEV), torch.empty(n, device=DEV)
+        x = torch.empty(n, D, dtype=torch.bfloat16, device=DEV)
+        loss, lse, dh, dw = torch.zeros(n, device=DEV), torch.zeros(n, device=DEV), torch.zeros_like(x), torch.zeros_like(w)
+        got = []
+        for h, z in zip(hs, zs):
+            x.copy_(h)
+            for call in (lambda: gk.gk_vocab_topk(z, K, t_idx, t_val, lse_out=t_lse),
+                         lambda: gk.gk_vocab_distill(x, w, t_idx, t_val, loss, lse, t_lse=t_lse, dh=dh, dw=dw),
+                         lambda: gk.gk_vocab_loss(dh, dw, t_idx[:, 3].long(), loss, lse, dh=x),       # the gradients as inputs
+                         lambda: gk.gk_vocab_loss(x, w, t_idx[:, 0].long(), loss, lse, dh=dh, dw=dw)):
+                call()
+                if wait:
+                    torch.cuda.synchronize()
+                got += [loss.clone(), lse.clone(), dh.clone(), x.clone(), dw.clone()]
+        torch.cuda.synchronize()
+        return got
+
+    for a, b in zip(steps(True), steps(False)):
+        assert torch.equal(a, b)
