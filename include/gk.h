@@ -11,9 +11,10 @@
  *     synchronising, unless stated otherwise.
  *   - Vectors are fp32, indices int32, so 1 <= d <= 2^31 - 1.  Base pointers of
  *     g, eps and u must be 16-byte aligned.  Inputs must be finite.
- *   - The library owns a small scratch workspace per (device, stream), created
+ *   - The library owns a scratch workspace per (device, stream), created
  *     by the first call that needs it (cudaMalloc; use gk_reserve to do that
- *     ahead of time).  Two calls that overlap on the GPU must use different
+ *     ahead of time) and kept: small for the sparsifiers, up to gk_vocab_set_budget
+ *     and more, in a block of its own, for the vocabulary head.  Two calls that overlap on the GPU must use different
  *     streams.  Calls of several host threads are safe on any streams: those
  *     on one stream are enqueued whole, one after the other in no promised
  *     order, and each thread's cudaStreamPerThread has a workspace of its own.
@@ -330,8 +331,13 @@ int gk_set_params(int unbiased_std, int max_rounds);
  *     lse_n = log sum_v exp z_nv;   loss_n = lse_n - z_n,t(n);
  *     dz_nv = g_n (exp(z_nv - lse_n) - [v = t(n)]);   dh = dz w;   dw = dz^T h.
  * Products of 16-bit operands are summed in fp32 (logits in pieces of 768, the pieces in fp32 registers), lse
- * and loss are fp32; dz is rounded to the operands' type before the products dh and dw, which are rounded
- * once more at the end.
+ * and loss are fp32.  The gradients go through 16 bits three times.  A logit of the vocabulary's first piece (see
+ * below) is kept as a 16-bit distance from the largest of its 128 columns, which puts its probability off by at
+ * most 6.8e-4 of itself (bf16) or 8.5e-5 (fp16; 2.5e-4 below 2^-8, and 2^-32 is the least); of later pieces it is
+ * computed again in fp32.  dz is rounded to the operands' type, scaled so that the call's largest finite row
+ * coefficient is a power of two (fp16: a row 2^-34 of it is lost).  dh and dw are rounded at the end.  Together, as
+ * norms, at most 1.5 times the last rounding alone over many rows.  The same call gives the same bits; under
+ * another gk_vocab_set_budget, or with one gradient instead of both, they can be others.
  *
  *   h          DEVICE in   n rows of D elements of `dtype`, row stride ldh >= D (in elements)
  *   w          DEVICE in   V rows of D elements, row stride ldw >= D.  Rows that start and end on
@@ -349,11 +355,11 @@ int gk_set_params(int unbiased_std, int max_rounds);
  * With neither dh nor dw only the forward pass runs (scoring).  dh and dw must not overlap h, w or
  * each other.  Results do not depend on timing: no atomics on floating-point data.
  *
- * The workspace is the call's own, per (device, stream), grown on first use (gk_vocab_reserve
- * does that ahead; a call that fits allocates nothing and can be captured in a graph, which stays good until a
- * call that does not fit replaces the workspace).  The
+ * The workspace is the call's own, per (device, stream), grown on first use and kept until the process ends
+ * (gk_vocab_reserve makes it ahead; a call that fits it allocates nothing).  For a capture in a graph reserve it on
+ * the stream that is captured, which torch.cuda.graph makes anew unless it is given one.  The
  * largest part, with gradients, is one piece of the vocabulary as n rows of 16-bit values, bounded by
- * gk_vocab_set_budget; of a vocabulary that does not fit one piece the product h w^T is taken twice.
+ * gk_vocab_set_budget; of the pieces after the first the product h w^T is taken twice.
  * Memory for 8 bytes a row and 128 columns (12 for gk_vocab_distill) is needed beside it.
  */
 int gk_vocab_loss(const void* h, int64_t ldh, const void* w, int64_t ldw, int32_t dtype, int64_t n, int64_t D,
@@ -369,7 +375,10 @@ int gk_vocab_loss(const void* h, int64_t ldh, const void* w, int64_t ldw, int32_
  *     dz_nv = (g_n / T) (exp(z_nv / T - lse_n) sum_j q_nj - sum_{j: i(n,j) = v} q_nj).
  *
  *   t_idx      DEVICE in   n x K int32 (contiguous), in any order; an index given twice counts
- *                          twice.  Pairs with an index outside [0, V) or a logit of -inf are left
+ *                          twice.  Rows in strictly ascending order, pairs left out last, as
+ *                          gk_vocab_topk writes them, are faster: the logits at other rows' pairs
+ *                          are dot products of their own (2048 x 2048 x 32000 with 64 pairs: 600
+ *                          and 740 us).  Pairs with an index outside [0, V) or a logit of -inf are left
  *                          out (rows with fewer pairs are filled up with -1); a row without any
  *                          pair is left out as in gk_vocab_loss.
  *   t_val      DEVICE in   n x K floats, the teacher's logits (not divided by T)
@@ -377,7 +386,7 @@ int gk_vocab_loss(const void* h, int64_t ldh, const void* w, int64_t ldw, int32_
  *   t_lse      DEVICE in   n floats, the teacher's log-sum-exp at T over its whole vocabulary
  *                          (gk_vocab_topk's lse_out): q is then the teacher's probability and
  *                          sums to at most 1.  NULL: q is normalised over the K pairs.
- *   temperature  T > 0
+ *   temperature  T > 0, with a finite reciprocal
  * The other arguments as for gk_vocab_loss.
  */
 int gk_vocab_distill(const void* h, int64_t ldh, const void* w, int64_t ldw, int32_t dtype, int64_t n, int64_t D,
@@ -393,7 +402,7 @@ int gk_vocab_distill(const void* h, int64_t ldh, const void* w, int64_t ldw, int
  *
  *   logits     DEVICE in   n rows of V elements of `dtype` (GK_TYPE_F32, _BF16 or _F16), row stride ld >= V
  *   n, V, k    n >= 0, 1 <= V <= 2^31 - 1, 1 <= k <= min(V, 1024)
- *   temperature  T > 0, for lse_out only
+ *   temperature  T > 0 with a finite reciprocal, for lse_out only
  *   idx_out    DEVICE out  n x k int32;   val_out  DEVICE out  n x k floats
  *   lse_out    DEVICE out  n floats, log sum_v exp(logit / T); -inf for a row of nothing but
  *                          -inf.  NULL: not wanted

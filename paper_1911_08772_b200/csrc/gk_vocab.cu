@@ -23,7 +23,7 @@
 // of 2^-9 in the exponent of two: the exponential it stands for is then off by at most 2^-10 log 2 = 6.8e-4 of
 // itself, where a bf16 exponential is off by up to 2^-9 = 2.0e-3, and a logit of 16 by 3e-2; the 65536 codes reach
 // 2^-128, as bf16 itself does.  For fp16 the steps are 2^-12 (8.5e-5, against 4.9e-4) down to 2^-8 of the largest,
-// and coarser to 2^-32, where fp16 gradients have ended.  A pass over them makes the logit gradients: the one
+// and coarser (2.5e-4) to 2^-32, below which all count as that.  A pass over them makes the logit gradients: the one
 // rounding to the operands' type that the products dw and dh need.  (Exponentials relative to a reference known
 // beforehand, the logit at the target, could be the operand themselves, with the rows of h scaled for dw instead:
 // that saved the pass, 5 to 7 % of a call, but rounds once more, and dw was off by 1.7 times what an exact dw
@@ -272,10 +272,9 @@ __device__ __forceinline__ float dot8(const uint4& x, const uint4& y, float s) {
     return s;
 }
 
-// RANK (few rows): each CTA takes a row of the caller's and finds its number itself, by looking at all rows
-// (1024 rows are 8 loads a thread, where a launch of its own costs 3 to 6 us; 2048 rows took 25 us so, and 17 by two
-// launches); one of them writes the
-// control block.
+// RANK (few rows): each CTA takes a row of the caller's and finds its number itself, by looking at all rows; one of
+// them writes the control block.  1024 rows are 8 loads a thread, where a launch of its own costs 3 to 6 us; 2048 rows
+// took 25 us so, and 17 by two launches.
 // CTAs from n_pad on make the copy of w with rows that start and end on 16-byte boundaries, where w's own do not.
 constexpr int64_t kRankRows = 1024;
 

@@ -73,8 +73,8 @@ struct VocabCall {
     int splits;
 };
 
-// Launches after a call's first: the kernel may be set up while the one before it ends, and waits for
-// that with after_previous() before it reads or writes anything of the call.
+// A call's launches (k_vocab_teacher's apart, which is a plain one): the kernel may be set up while the one before it
+// in the stream ends, and waits for that with after_previous() before it reads or writes anything of the call.
 template <class... Params, class... Args>
 inline cudaError_t launch_next(void (*kernel)(Params...), dim3 grid, unsigned threads, size_t smem, cudaStream_t st, Args&&... args) {
     cudaLaunchAttribute attr[1];
@@ -140,7 +140,8 @@ __device__ __forceinline__ float exp2_fast(float x) {
 
 // The 16-bit code of a logit's distance d <= 0 from its tile's maximum, in units of log 2.  bf16: steps of 2^-9 over
 // a range of 128, the exponents bf16 gradients can have.  fp16: steps of 2^-12 over the first 8 and of 1 / 1365.25
-// over the next 24, where fp16 gradients have ended.  The last code stands for itself and more.
+// over the next 24.  The last code stands for itself and more: 2^-32 (2.3e-10) of the tile's largest exponential is the
+// least that an fp16 call's first piece tells from zero (fp16 gradients without a scale end at 6e-8).
 template <bool F16>
 __device__ __forceinline__ unsigned kept_code(float d) {
     // the bits of 2^23 + x hold x

@@ -11,7 +11,7 @@
 // the other is read out.  Logits always are; they are summed in chunks (kChunk), which take turns on the halves.
 // Wide tiles (512 columns, four blocks of 48 KB, three quarters of the bytes a product): gradients where
 // launch_time expects them to be faster; 8192 x 4096 x 128000 took 20.2 ms a call with them, 23.0 with narrow
-// ones.  Their sums take all of the tensor memory, so the two halves of a tile are summed out of step at its
+// ones on the same GPU (19.6 to 21.9 ms on others).  Their sums take all of the tensor memory, so the two halves of a tile are summed out of step at its
 // ends: the first is ahead by up to four blocks at the end of a tile, so that it is read out while
 // the second catches up, and again at the start of the next tile, while the second is read out.  (The logits
 // of 4096 x 4096 x 32000 took 713 us in wide tiles and 749 in narrow ones, when they were not summed in chunks.)
