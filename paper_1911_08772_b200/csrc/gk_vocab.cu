@@ -702,11 +702,12 @@ static int vocab_workspace(cudaStream_t st, VocabWorkspace** out, WorkspaceLock&
     return GK_OK;
 }
 
-// At least `bytes` for a workspace that the caller holds.
+// At least `bytes` for a workspace that the caller holds.  What the last call reported goes along.
 static int grow(VocabWorkspace& ws, size_t bytes, cudaStream_t st) {
     if (ws.bytes >= bytes) return GK_OK;
-    VocabCtl last = {};       // what the last call reported is kept
-    if (ws.base) {
+    const bool had = ws.base != nullptr;
+    VocabCtl last = {};
+    if (had) {
         GK_CUDA_TRY(cudaStreamSynchronize(st));   // work already enqueued may still use the old block
         GK_CUDA_TRY(cudaMemcpy(&last, ws.base, sizeof(last), cudaMemcpyDeviceToHost));
         GK_CUDA_TRY(cudaFree(ws.base));
@@ -717,7 +718,9 @@ static int grow(VocabWorkspace& ws, size_t bytes, cudaStream_t st) {
     if (cudaMalloc(&p, bytes) != cudaSuccess) { cudaGetLastError(); return GK_ERR_NOMEM; }
     ws.base = p;
     ws.bytes = bytes;
-    GK_CUDA_TRY(cudaMemcpyAsync(p, &last, sizeof(last), cudaMemcpyHostToDevice, st));      // (staged before it returns)
+    // (a stream that could be waited for is not being captured: the copy is staged before it returns)
+    if (had) GK_CUDA_TRY(cudaMemcpyAsync(p, &last, sizeof(last), cudaMemcpyHostToDevice, st));
+    else GK_CUDA_TRY(cudaMemsetAsync(p, 0, sizeof(last), st));
     return GK_OK;
 }
 

@@ -164,6 +164,26 @@ def test_a_workspace_reserved_for_more_rows_can_be_captured_with_fewer(n, fewer,
                 assert not dw or torch.equal(out.dw, eager.dw)
 
 
+def test_a_first_call_within_a_capture_that_may_allocate():
+    """In a capture in relaxed mode the stream's first call makes its workspace; replays are the eager call's."""
+    n, D, V = 50, 72, 500
+    gen, h, w, hd, wd = make(n, D, V, torch.bfloat16, 73)
+    target = torch.randint(0, V, (n,), generator=gen).to(DEV)
+    eager, out = Out(n, D, V, torch.bfloat16), Out(n, D, V, torch.bfloat16)
+    gk.gk_vocab_loss(hd, wd, target, eager.loss[:n], eager.lse[:n], dh=eager.dh, dw=eager.dw)
+    torch.cuda.synchronize()
+    stream = torch.cuda.Stream(priority=-1)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(stream), torch.cuda.graph(graph, stream=stream, capture_error_mode="relaxed"):
+        gk.gk_vocab_loss(hd, wd, target, out.loss[:n], out.lse[:n], dh=out.dh, dw=out.dw)
+    for _ in range(2):
+        out.dh.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out.loss, eager.loss) and torch.equal(out.dh, eager.dh) and torch.equal(out.dw, eager.dw)
+
+
 # --- calls without rows -----------------------------------------------------------------------------------
 
 
