@@ -53,10 +53,11 @@ typedef enum gk_status {
     GK_ERR_LIMIT = -9,     /* size beyond a fixed built-in limit */
     GK_ERR_TYPE = -10,     /* gk_vocab_*: not one of the element types the call takes */
     GK_ERR_STRIDE = -11,   /* gk_vocab_*: a row stride shorter than the row */
-    GK_ERR_TEMPERATURE = -12 /* gk_vocab_*: temperature or its reciprocal not positive and finite */
+    GK_ERR_TEMPERATURE = -12, /* gk_vocab_*: temperature or its reciprocal not positive and finite */
+    GK_ERR_NORM = -13      /* gk_grad_clip: max_norm not positive */
 } gk_status;
 
-/* Element types of the gk_vocab_* calls. */
+/* Element types of the gk_vocab_* and gk_grad_* calls. */
 typedef enum gk_type { GK_TYPE_F32 = 0, GK_TYPE_BF16 = 1, GK_TYPE_F16 = 2 } gk_type;
 
 /* Values of gk_stats.status (bit flags, written by the device). */
@@ -426,6 +427,51 @@ int64_t gk_vocab_workspace_bytes(int64_t n, int64_t D, int64_t V, int32_t K, int
  * gk_vocab_distill call on it, one without rows included (0, 0): GK_DEV_* flags, rows that counted.
  * GK_ERR_NULL where there was no call. */
 int gk_vocab_last_info(gk_stream_t stream, int64_t* host_out);
+
+/*
+ * gk_grad_norm -- the Euclidean norm over the gradients of many tensors together, and each tensor's own:
+ *     norm = sqrt(sum_i sum_x g_i(x)^2);   norms_i = sqrt(sum_x g_i(x)^2).
+ * What a training step looks at, and clips by, before its gradient is compressed (the paper does not treat it).
+ *
+ *   grads      HOST   in   T pointers to DEVICE tensors of sizes[i] contiguous elements, on an element's
+ *                          boundary; NULL allowed for an empty one
+ *   types      HOST   in   T gk_type: each tensor's own
+ *   sizes      HOST   in   T int64, 0 <= sizes[i] <= 2^44
+ *   T          0 <= T <= 65536; more than 1000 need gk_reserve(1, T) before a capture, fewer gk_reserve(1, 1)
+ *   norm_out   DEVICE out  one float
+ *   norms_out  DEVICE out  T floats; NULL: not wanted
+ * The lists are read before the call returns (they travel as the kernel's argument); a captured call keeps them.
+ * Any values: squares beyond fp32's range are taken in fp64, an infinity gives infinity, NaN gives NaN.  A tensor
+ * given twice counts twice.  Sums of 16 to 32 squares in fp32, the rest in fp64, in an order that the sizes, the
+ * 16-byte boundaries within the tensors and the device decide: the same call gives the same bits.
+ *
+ * gk_grad_clip -- the gradients scaled so that their norm is at most max_norm, in place or into other tensors:
+ *     out_i = c s g_i,   c = max_norm / norm where norm = |s| ||g|| is above max_norm and finite, else 1.
+ * With outputs of fp32 one after the other in one buffer this is the step from a backward pass to the vector g
+ * that gk_sparsify takes (local gradient clipping before compression).
+ *
+ *   grads, types, sizes, T   as above
+ *   outs       HOST   in   T pointers to DEVICE tensors of the same sizes.  An output is its own input (same
+ *                          pointer, same type: in place) or shares memory with no input and no other output
+ *   out_types  HOST   in   T gk_type.  A product is taken in fp32 and rounded once to the output's type
+ *   max_norm   > 0; infinity clips nothing
+ *   scale      DEVICE in   s, one float, as the reciprocal of a loss scale; NULL: 1
+ *   norm_in    DEVICE in   the norm, of the scaled gradients, where the caller knows it (over tensors that other
+ *                          ranks hold, say); NULL: taken over these tensors
+ *   norm_out   DEVICE out  one float, the norm before clipping; NULL: not wanted
+ * A norm that is not finite clips nothing (c = 1): the caller finds it in norm_out and drops the step.  Where
+ * nothing is clipped or scaled, tensors in place are not written.  One cooperative kernel (the device must support
+ * that); should its bounded barrier run out, norm_out is NaN and no output is complete.
+ */
+int gk_grad_norm(const void* const* grads, const int32_t* types, const int64_t* sizes, int32_t T, float* norm_out,
+                 float* norms_out, gk_stream_t stream);
+int gk_grad_clip(const void* const* grads, const int32_t* types, void* const* outs, const int32_t* out_types,
+                 const int64_t* sizes, int32_t T, float max_norm, const float* scale, const float* norm_in,
+                 float* norm_out, gk_stream_t stream);
+
+/* Synchronise `stream` and write to HOST host_out[0..1] of the last gk_grad_clip call on it: GK_DEV_* flags,
+ * whether it clipped.  GK_ERR_NULL where no call has made the stream's workspace. */
+int gk_grad_last_info(gk_stream_t stream, int64_t* host_out);
 
 /* Output capacity of idx_out / val_out for the sparsify calls, in pairs.
  * 0 (the default) means "d".  Process-wide; returns GK_ERR_CAPACITY if cap < 0. */

@@ -29,6 +29,7 @@ EXPORTS = [
     "gk_apply_sparse", "gk_apply_gathered", "gk_histogram", "gk_debug_set", "gk_last_path_info", "gk_select", "gk_set_params",
     "gk_vocab_loss", "gk_vocab_distill", "gk_vocab_topk", "gk_vocab_set_budget", "gk_vocab_reserve",
     "gk_vocab_workspace_bytes", "gk_vocab_last_info",
+    "gk_grad_norm", "gk_grad_clip", "gk_grad_last_info",
 ]
 
 
@@ -141,6 +142,13 @@ def load() -> C.CDLL:
     L.gk_vocab_workspace_bytes.restype = i64
     L.gk_vocab_last_info.argtypes = [vp, C.POINTER(i64)]
     L.gk_vocab_last_info.restype = C.c_int
+    grads = [C.POINTER(vp), C.POINTER(i32)]
+    L.gk_grad_norm.argtypes = grads + [C.POINTER(i64), i32, vp, vp, vp]
+    L.gk_grad_norm.restype = C.c_int
+    L.gk_grad_clip.argtypes = grads + grads + [C.POINTER(i64), i32, C.c_float, vp, vp, vp, vp]
+    L.gk_grad_clip.restype = C.c_int
+    L.gk_grad_last_info.argtypes = [vp, C.POINTER(i64)]
+    L.gk_grad_last_info.restype = C.c_int
     for name in ("gk_sparsify", "gk_sparsify_segmented", "topk_exact", "topk_sparsify", "gk_sparsify_host",
                  "gk_set_capacity", "gk_set_path", "gk_reserve", "gk_last_stats", "gk_last_segment_stats", "gk_version"):
         getattr(L, name).restype = C.c_int
@@ -423,6 +431,97 @@ def gk_vocab_last_info():
     out = (C.c_int64 * 2)()
     _check(load().gk_vocab_last_info(_stream(), out))
     return int(out[0]), int(out[1])
+
+
+class GradList:
+    """Many tensors' gradients, and where gk_grad_clip puts them, as the library takes them: pointers, sizes
+    and element types, looked up once.  Good while the tensors stay where they are; make another when
+    they do not.
+
+    grads: contiguous CUDA tensors of float32, bfloat16 or float16 on the current device.  out: None (in
+    place), as many tensors of the same sizes, or one 1-D tensor that takes them one after the other
+    (float32: the vector that gk_sparsify takes)."""
+
+    def __init__(self, grads, out=None):
+        import torch
+        grads = list(grads)
+        self.device = torch.cuda.current_device()
+        self.pointers, self.types, counts = self._look_up(grads, "gradient")
+        if out is None:
+            self.out_pointers, self.out_types = self.pointers, self.types
+        else:
+            if isinstance(out, torch.Tensor):
+                if out.dim() != 1 or out.numel() != sum(counts):
+                    raise GkError("out: expected a 1-D tensor of the gradients' size together")
+                outs = torch.split(out, counts) if grads else []
+            else:
+                outs = list(out)
+            self.out_pointers, self.out_types, out_counts = self._look_up(outs, "output")
+            if out_counts != counts:
+                raise GkError("out: expected tensors of the gradients' sizes")
+        self.sizes = (C.c_int64 * len(grads))(*counts)
+        self.tensors = (grads, out)      # the memory stays theirs
+
+    def _look_up(self, tensors, name):
+        import torch
+        pointers, types, counts = [], [], []
+        for i, t in enumerate(tensors):
+            if not isinstance(t, torch.Tensor) or not t.is_cuda or not t.is_contiguous():
+                raise GkError(f"{name} {i}: expected a contiguous CUDA tensor")
+            if t.get_device() != self.device:
+                raise GkError(f"{name} {i} is not on the current device")
+            pointers.append(t.data_ptr())
+            types.append(t.dtype)
+            counts.append(t.numel())
+        code = {d: _type(d) for d in set(types)}
+        return (C.c_void_p * len(pointers))(*pointers), (C.c_int32 * len(types))(*[code[d] for d in types]), counts
+
+    def __len__(self) -> int:
+        return len(self.sizes)
+
+
+def _grad_list(grads, out=None) -> GradList:
+    import torch
+    if not isinstance(grads, GradList):
+        return GradList(grads, out)
+    if out is not None:
+        raise GkError("a GradList has its outputs already")
+    if torch.cuda.current_device() != grads.device:
+        raise GkError("the gradients are not on the current device")
+    return grads
+
+
+def _one(t, device, name):
+    import torch
+    return None if t is None else _vec(t, torch.float32, device, (1,), name)
+
+
+def gk_grad_norm(grads, norm_out, norms_out=None) -> None:
+    """The norm over many gradients together, and each one's (see gk.h).  grads: a list of tensors, or a
+    GradList, which saves looking them up at every call; norm_out (1,) float32; norms_out (len(grads),) float32."""
+    import torch
+    g = _grad_list(grads)
+    _check(load().gk_grad_norm(g.pointers, g.types, g.sizes, len(g), _one(norm_out, g.device, "norm_out") or 0,
+                               None if norms_out is None else _vec(norms_out, torch.float32, g.device, (len(g),), "norms_out"),
+                               _stream_of(g.device)))
+
+
+def gk_grad_clip(grads, max_norm: float, out=None, norm_out=None, scale=None, norm_in=None) -> None:
+    """The gradients, times scale, scaled so that their norm is at most max_norm (see gk.h).  grads: a list of
+    tensors, with out as for GradList (None: in place), or a GradList, which has both; norm_out, scale,
+    norm_in: (1,) float32 or None."""
+    g = _grad_list(grads, out)
+    d = g.device
+    _check(load().gk_grad_clip(g.pointers, g.types, g.out_pointers, g.out_types, g.sizes, len(g), max_norm,
+                               _one(scale, d, "scale"), _one(norm_in, d, "norm_in"), _one(norm_out, d, "norm_out"),
+                               _stream_of(d)))
+
+
+def gk_grad_last_info():
+    """(GK_DEV_* flags, whether it clipped) of the last gk_grad_clip on the current stream.  Synchronises the stream."""
+    out = (C.c_int64 * 2)()
+    _check(load().gk_grad_last_info(_stream(), out))
+    return int(out[0]), bool(out[1])
 
 
 def gk_set_capacity(cap: int) -> None:

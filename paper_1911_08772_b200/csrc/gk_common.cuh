@@ -120,6 +120,8 @@ struct Workspace {
     int last_grid = 0;                      // CTAs of the last fused launch
     // segmented call
     void* seg_block = nullptr;
+    // norm and clipping of many tensors' gradients
+    void* grad_block = nullptr;
     int sm_count = 0;
     // per-stage timing (tracing aid)
     cudaEvent_t ev[6] = {nullptr, nullptr, nullptr, nullptr, nullptr, nullptr};

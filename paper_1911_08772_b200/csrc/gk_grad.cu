@@ -1,0 +1,519 @@
+// The gradients of many tensors: their norm, and clipping them by it (include/gk.h: gk_grad_norm,
+// gk_grad_clip).
+//
+// The work is cut into units of 16 KB of a tensor's gradients; a CTA has a contiguous stretch of all units, so
+// that of each tensor it meets it has one contiguous span.  Squares are added in fp32 over 16 (fp32) or 32
+// (16-bit) elements and those sums in fp64; where such a sum says that squares left fp32's range, or is zero,
+// the elements are squared again in fp64.  Sums are joined in a fixed order: threads, warps, CTAs.
+//
+// Clipping is one cooperative kernel: squares, a barrier of the grid, and the scaling from the last unit back
+// to the first, which meets in L2 what the squares read last.
+#include <algorithm>
+#include <new>
+#include <utility>
+#include <vector>
+
+#include "gk_coop.cuh"
+#include "gk_grad.cuh"
+#include "gk_segmented.cuh"
+
+namespace gk {
+
+constexpr int kGradThreads = 512, kGradWarps = kGradThreads / 32;
+constexpr int kGradUnit = 16384;          // bytes of source in a unit
+
+struct GradRec {
+    const void* src;
+    void* dst;
+    int64_t n;              // elements
+    unsigned first;         // units of the tensors before
+    unsigned types;         // of src, and of dst in bits 8 and up
+};
+// The table travels as a kernel argument where it fits (a captured call then needs nothing of the host),
+// else kernels with a part of it as their argument write it to the workspace first.
+constexpr int kGradFew = 64, kGradMany = 1000;
+template <int CAP>
+struct GradTable {
+    GradRec rec[CAP];
+};
+
+struct GradCall {
+    const GradRec* table;   // nullptr: the kernel's argument
+    int T;
+    unsigned units;
+    GradCtl* ctl;
+    double* cta_sums;       // one a CTA
+    double* span_sums;      // tensor + CTA: a CTA's span of a tensor
+    float* norm_out;
+    float* norms_out;
+    const float* scale;
+    const float* norm_in;
+    float max_norm;
+    unsigned extra;         // arrivals that the barrier expects beyond the grid's (test hook)
+};
+
+__device__ __forceinline__ double block_total(double v, double* smem) {
+    v = warp_sum(v);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) smem[threadIdx.x >> 5] = v;
+    __syncthreads();
+    double r = 0.0;
+#pragma unroll
+    for (int i = 0; i < kGradWarps; ++i) r += smem[i];
+    return r;
+}
+
+template <int TYPE>
+struct Elem {
+    static constexpr int size = TYPE == GK_TYPE_F32 ? 4 : 2, vec = 16 / size;
+};
+template <int TYPE>
+__device__ __forceinline__ float load_elem(const char* p, int64_t i) {
+    if constexpr (TYPE == GK_TYPE_F32) return ((const float*)p)[i];
+    else return from16<TYPE == GK_TYPE_F16>(((const uint16_t*)p)[i]);
+}
+template <int TYPE>
+__device__ __forceinline__ void store_elem(char* p, int64_t i, float v) {
+    if constexpr (TYPE == GK_TYPE_F32) ((float*)p)[i] = v;
+    else ((uint16_t*)p)[i] = to16<TYPE == GK_TYPE_F16>(v);
+}
+
+// Sum of the squares of n elements at p, this thread's part of it.
+template <int TYPE>
+__device__ __forceinline__ double squares(const char* p, int64_t n) {
+    constexpr int kVec = Elem<TYPE>::vec, kSize = Elem<TYPE>::size, kWords = 4;
+    const int tid = threadIdx.x;
+    int64_t head = (16 - ((uintptr_t)p & 15)) % 16 / kSize;
+    if (head > n) head = n;
+    const int64_t words = (n - head) / kVec;
+    const uint4* body = (const uint4*)(p + head * kSize);
+    double acc = 0.0;
+#pragma unroll 1
+    for (int64_t w0 = 0; w0 < words; w0 += kWords * kGradThreads) {
+        const int left = (int)(words - w0 < kWords * kGradThreads ? words - w0 : kWords * kGradThreads) - tid;
+        const uint4* own = body + w0 + tid;
+        uint4 x[kWords];
+#pragma unroll
+        for (int j = 0; j < kWords; ++j) x[j] = j * kGradThreads < left ? own[j * kGradThreads] : make_uint4(0, 0, 0, 0);
+        float s = 0.f, t = 0.f;
+#pragma unroll
+        for (int j = 0; j < kWords; ++j) {
+            float f[kVec];
+            unpack16B<TYPE>(x[j], f);
+#pragma unroll
+            for (int e = 0; e < kVec; e += 2) {
+                s = fmaf(f[e], f[e], s);
+                t = fmaf(f[e + 1], f[e + 1], t);
+            }
+        }
+        s += t;
+        if (s > 7.9e-31f && s < INFINITY) {      // 2^-100: what lies below fp32's range is nothing beside it
+            acc += (double)s;
+        } else {
+#pragma unroll
+            for (int j = 0; j < kWords; ++j) {
+                float f[kVec];
+                unpack16B<TYPE>(x[j], f);
+#pragma unroll
+                for (int e = 0; e < kVec; ++e) acc = fma((double)f[e], (double)f[e], acc);
+            }
+        }
+    }
+    // before the first 16-byte boundary and after the last
+    const int64_t tail = n - head - words * kVec;
+    if (tid < head) {
+        const double v = (double)load_elem<TYPE>(p, tid);
+        acc = fma(v, v, acc);
+    }
+    if (tid < tail) {
+        const double v = (double)load_elem<TYPE>(p, n - tail + tid);
+        acc = fma(v, v, acc);
+    }
+    return acc;
+}
+__device__ __forceinline__ double squares(int type, const char* p, int64_t n) {
+    switch (type) {
+        case GK_TYPE_F32: return squares<GK_TYPE_F32>(p, n);
+        case GK_TYPE_BF16: return squares<GK_TYPE_BF16>(p, n);
+        default: return squares<GK_TYPE_F16>(p, n);
+    }
+}
+
+// dst = c src, n elements, from the last to the first.
+template <int SRC, int DST>
+__device__ __noinline__ void scaled(const char* src, char* dst, int64_t n, float c) {
+    constexpr int kS = Elem<SRC>::size, kD = Elem<DST>::size;
+    const int tid = threadIdx.x;
+    // elements before the first one that starts 16 bytes on both sides, where there is one
+    int head = -1;
+#pragma unroll
+    for (int h = 7; h >= 0; --h)
+        if ((((uintptr_t)src + h * kS) & 15) == 0 && (((uintptr_t)dst + h * kD) & 15) == 0) head = h;
+    // (a step's places are offsets from its first, so that their addresses take no registers)
+    if (head < 0) {
+        constexpr int kEach = 8, kStep = kEach * kGradThreads;
+#pragma unroll 1
+        for (int64_t i0 = (n - 1) / kStep * kStep; i0 >= 0; i0 -= kStep) {
+            const int left = (int)(n - i0 < kStep ? n - i0 : kStep) - tid;
+            const char* s = src + (i0 + tid) * kS;
+            char* d = dst + (i0 + tid) * kD;
+            float f[kEach];
+#pragma unroll
+            for (int j = 0; j < kEach; ++j)
+                if (j * kGradThreads < left) f[j] = load_elem<SRC>(s, j * kGradThreads);
+#pragma unroll
+            for (int j = 0; j < kEach; ++j)
+                if (j * kGradThreads < left) store_elem<DST>(d, j * kGradThreads, c * f[j]);
+        }
+        return;
+    }
+    if (head > n) head = (int)n;
+    const int64_t words = (n - head) / 8;      // of eight elements
+    constexpr int kWords = 2, kStep = kWords * kGradThreads;
+#pragma unroll 1
+    for (int64_t w0 = (words - 1) / kStep * kStep; w0 >= 0; w0 -= kStep) {
+        const int left = (int)(words - w0 < kStep ? words - w0 : kStep) - tid;
+        const uint4* s = (const uint4*)(src + head * kS) + (w0 + tid) * (kS / 2);
+        uint4* d = (uint4*)(dst + head * kD) + (w0 + tid) * (kD / 2);
+        uint4 x[kWords][kS / 2];
+#pragma unroll
+        for (int j = 0; j < kWords; ++j)
+#pragma unroll
+            for (int e = 0; e < kS / 2; ++e)
+                if (j * kGradThreads < left) x[j][e] = s[j * kGradThreads * (kS / 2) + e];
+#pragma unroll
+        for (int j = 0; j < kWords; ++j) {
+            if (j * kGradThreads >= left) break;
+            float f[8];
+#pragma unroll
+            for (int e = 0; e < kS / 2; ++e) {
+                float g[Elem<SRC>::vec];
+                unpack16B<SRC>(x[j][e], g);
+#pragma unroll
+                for (int a = 0; a < Elem<SRC>::vec; ++a) f[e * Elem<SRC>::vec + a] = c * g[a];
+            }
+            uint4* to = d + j * kGradThreads * (kD / 2);
+            if constexpr (DST == GK_TYPE_F32) {
+                ((float4*)to)[0] = make_float4(f[0], f[1], f[2], f[3]);
+                ((float4*)to)[1] = make_float4(f[4], f[5], f[6], f[7]);
+            } else {
+                constexpr bool F16 = DST == GK_TYPE_F16;
+                to[0] = make_uint4(pack16<F16>(f[0], f[1]), pack16<F16>(f[2], f[3]), pack16<F16>(f[4], f[5]), pack16<F16>(f[6], f[7]));
+            }
+        }
+    }
+    const int64_t tail = n - head - words * 8;
+    if (tid < head) store_elem<DST>(dst, tid, c * load_elem<SRC>(src, tid));
+    if (tid < tail) store_elem<DST>(dst, n - tail + tid, c * load_elem<SRC>(src, n - tail + tid));
+}
+__device__ __forceinline__ void scaled(unsigned types, const char* src, char* dst, int64_t n, float c) {
+    switch (types) {
+#define GK_PAIR(S, D) case (S | D << 8): scaled<S, D>(src, dst, n, c); break;
+        GK_PAIR(0, 0) GK_PAIR(0, 1) GK_PAIR(0, 2) GK_PAIR(1, 0) GK_PAIR(1, 1) GK_PAIR(1, 2) GK_PAIR(2, 0) GK_PAIR(2, 1)
+        default: scaled<2, 2>(src, dst, n, c); break;
+#undef GK_PAIR
+    }
+}
+
+// A CTA's stretch of units, and the tensor that it begins in.
+__device__ __forceinline__ unsigned unit_of(unsigned units, unsigned b, unsigned G) { return (unsigned)((uint64_t)units * b / G); }
+__device__ __forceinline__ int tensor_of(const GradRec* rec, int T, unsigned unit) {
+    int lo = 0, hi = T - 1;      // the last tensor whose first unit is not behind `unit`: empty ones have none of their own
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (rec[mid].first <= unit) lo = mid; else hi = mid - 1;
+    }
+    return lo;
+}
+// Elements of tensor r in the units [u0, u1), which it has some of.
+__device__ __forceinline__ void span_of(const GradRec& r, unsigned u0, unsigned u1, int64_t& from, int64_t& to) {
+    const int each = (r.types & 255u) == GK_TYPE_F32 ? kGradUnit / 4 : kGradUnit / 2;
+    from = u0 > r.first ? (int64_t)(u0 - r.first) * each : 0;
+    to = (int64_t)(u1 - r.first) * each;
+    if (to > r.n) to = r.n;
+}
+
+// Every thread: the square root of the CTAs' sums, in the order of the CTAs.
+__device__ __forceinline__ double total_norm(const double* cta_sums, unsigned G, double* smem) {
+    double v = 0.0;
+    for (unsigned b = threadIdx.x; b < G; b += kGradThreads) v += __ldcg(&cta_sums[b]);
+    v = warp_sum(v);
+    return sqrt(block_total((threadIdx.x & 31) == 0 ? v : 0.0, smem));
+}
+
+template <bool CLIP, int CAP>
+__global__ void __launch_bounds__(kGradThreads, 2) k_grad(const GradCall c, const __grid_constant__ GradTable<CAP> table) {
+    __shared__ double smem[kGradWarps];
+    __shared__ int flag;
+    const GradRec* rec = c.table ? c.table : table.rec;
+    const unsigned G = gridDim.x, b = blockIdx.x;
+    const unsigned u0 = unit_of(c.units, b, G), u1 = unit_of(c.units, b + 1, G);
+    const int tid = threadIdx.x;
+    int last = -1;      // the tensor that the stretch ends in
+    if (!CLIP || !c.norm_in) {
+        double all = 0.0;
+        if (u0 < u1)
+            for (int i = tensor_of(rec, c.T, u0); i < c.T && rec[i].first < u1; ++i) {
+                const GradRec r = rec[i];
+                int64_t from, to;
+                span_of(r, u0, u1, from, to);
+                if (from >= to) continue;
+                last = i;
+                const double v = squares((int)(r.types & 255u), (const char*)r.src + from * ((r.types & 255u) == GK_TYPE_F32 ? 4 : 2), to - from);
+                if (!CLIP && c.norms_out) {
+                    const double sum = block_total(v, smem);
+                    if (tid == 0) c.span_sums[i + b] = sum;
+                }
+                all += v;
+            }
+        all = block_total(all, smem);
+        if (tid == 0) c.cta_sums[b] = all;
+    }
+    if constexpr (!CLIP) {
+        // the CTA that is done last joins the sums
+        if (tid == 0) {
+            __threadfence();
+            flag = atomicInc(&c.ctl->done, G - 1) == G - 1;
+            __threadfence();
+        }
+        __syncthreads();
+        if (!flag) return;
+        const double norm = total_norm(c.cta_sums, G, smem);
+        if (tid == 0) c.norm_out[0] = (float)norm;
+        if (c.norms_out)
+            for (int i0 = 0; i0 < c.T; i0 += kGradThreads / 8) {
+                // eight lanes a tensor: its spans are those of the CTAs from its first unit's to its last's
+                const int i = i0 + tid / 8;
+                double v = 0.0;
+                if (i < c.T && rec[i].n > 0) {
+                    const unsigned f = rec[i].first, l = i + 1 < c.T ? rec[i + 1].first - 1 : c.units - 1;
+                    const unsigned b0 = (unsigned)((((uint64_t)f + 1) * G - 1) / c.units), b1 = (unsigned)((((uint64_t)l + 1) * G - 1) / c.units);
+                    for (unsigned a = b0 + tid % 8; a <= b1; a += 8) v += __ldcg(&c.span_sums[i + a]);
+                }
+#pragma unroll
+                for (int o = 4; o > 0; o >>= 1) v += __shfl_down_sync(0xffffffffu, v, o, 8);
+                if (i < c.T && tid % 8 == 0) c.norms_out[i] = (float)sqrt(v);
+            }
+    } else {
+        const float scale = c.scale ? *c.scale : 1.f;
+        double norm;
+        if (c.norm_in) {
+            norm = (double)*c.norm_in;
+        } else {
+            if (b == 0 && tid == 0) c.ctl->status = GK_DEV_OK;
+            const bool ok = grid_barrier(&c.ctl->arrived, G + c.extra, &flag);
+            if (tid == 0) {
+                // whoever leaves last makes the counters ready for the next call
+                if (atomicInc(&c.ctl->left, G - 1) == G - 1) c.ctl->arrived = 0;
+            }
+            if (!ok) {
+                if (tid == 0) {
+                    atomicOr(&c.ctl->status, GK_DEV_TIMEOUT);
+                    if (b == 0 && c.norm_out) c.norm_out[0] = NAN;
+                }
+                return;
+            }
+            norm = total_norm(c.cta_sums, G, smem) * fabs((double)scale);
+        }
+        // norms that are not finite clip nothing: the caller sees them
+        const bool clips = norm > (double)c.max_norm && norm < (double)INFINITY;
+        const float by = clips ? (float)((double)scale * ((double)c.max_norm / norm)) : scale;
+        if (b == 0 && tid == 0) {
+            if (c.norm_out) c.norm_out[0] = (float)norm;
+            if (c.norm_in) c.ctl->status = GK_DEV_OK;
+            c.ctl->clipped = clips;
+        }
+        if (u0 >= u1) return;
+        if (last < 0) last = tensor_of(rec, c.T, u1 - 1);
+        for (int i = last; i >= 0; --i) {
+            const GradRec r = rec[i];
+            if (r.n > 0 && !(by == 1.f && r.src == r.dst)) {
+                int64_t from, to;
+                span_of(r, u0, u1, from, to);
+                const int64_t s = (r.types & 255u) == GK_TYPE_F32 ? 4 : 2, d = r.types >> 8 == GK_TYPE_F32 ? 4 : 2;
+                scaled(r.types, (const char*)r.src + from * s, (char*)r.dst + from * d, to - from, by);
+            }
+            if (r.first <= u0) break;
+        }
+    }
+}
+
+// A part of a long table into the workspace.
+__global__ void k_grad_table(GradRec* to, int n, const __grid_constant__ GradTable<kGradMany> part) {
+    const int i = blockIdx.x * blockDim.x + threadIdx.x;
+    if (i < n) to[i] = part.rec[i];
+}
+
+size_t grad_scratch_bytes(int32_t S) {
+    const size_t T = S > kGradMany ? S : kGradMany;
+    return 256 + sizeof(double) * (kGradMaxCtas + kGradMaxCtas + T) + (S > kGradMany ? sizeof(GradRec) * (size_t)S : 0);
+}
+
+// CTAs of a device, 0 where it has no cooperative launch.
+static int grad_grid(int dev, int sm_count, int* grid) {
+    static std::mutex mu;
+    static int known[64];
+    if (dev < 0 || dev >= 64) return GK_ERR_LIMIT;
+    std::lock_guard<std::mutex> lock(mu);
+    if (!known[dev]) {
+        int coop = 0, occ = 0;
+        GK_CUDA_TRY(cudaDeviceGetAttribute(&coop, cudaDevAttrCooperativeLaunch, dev));
+        if (!coop) return GK_ERR_LIMIT;
+        GK_CUDA_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&occ, k_grad<true, kGradMany>, kGradThreads, 0));
+        known[dev] = std::min(occ * sm_count, kGradMaxCtas);
+    }
+    *grid = known[dev];
+    return *grid > 0 ? GK_OK : GK_ERR_LIMIT;
+}
+
+static bool known_type(int32_t t) { return t == GK_TYPE_F32 || t == GK_TYPE_BF16 || t == GK_TYPE_F16; }
+static int type_size(int32_t t) { return t == GK_TYPE_F32 ? 4 : 2; }
+
+// What both calls refuse of their lists.
+static int check_list(const void* const* grads, const int32_t* types, const int64_t* sizes, int32_t T) {
+    if (T < 0) return GK_ERR_SIZE;
+    if (T > kMaxSegments) return GK_ERR_LIMIT;
+    if (T > 0 && (!grads || !types || !sizes)) return GK_ERR_NULL;
+    uint64_t units = 0;
+    for (int32_t i = 0; i < T; ++i) {
+        if (!known_type(types[i])) return GK_ERR_TYPE;
+        if (sizes[i] < 0) return GK_ERR_SIZE;
+        if (sizes[i] > (int64_t)1 << 44) return GK_ERR_LIMIT;
+        if (sizes[i] > 0 && !grads[i]) return GK_ERR_NULL;
+        if ((uintptr_t)grads[i] & (type_size(types[i]) - 1)) return GK_ERR_ALIGN;
+        units += ((uint64_t)sizes[i] * type_size(types[i]) + kGradUnit - 1) / kGradUnit;
+        if (units > 0xfffffffeull) return GK_ERR_LIMIT;
+    }
+    return GK_OK;
+}
+
+// Whether an output shares memory with another output or with an input that is not its own.
+static bool outputs_overlap(const void* const* grads, const int32_t* types, void* const* outs, const int32_t* out_types,
+                            const int64_t* sizes, int32_t T) {
+    using Range = std::pair<uintptr_t, uintptr_t>;
+    std::vector<Range> in, out;
+    in.reserve(T);
+    out.reserve(T);
+    for (int32_t i = 0; i < T; ++i) {
+        if (sizes[i] == 0) continue;
+        const uintptr_t a = (uintptr_t)grads[i], b = (uintptr_t)outs[i];
+        out.emplace_back(b, b + sizes[i] * type_size(out_types[i]));
+        if (a != b || types[i] != out_types[i]) in.emplace_back(a, a + sizes[i] * type_size(types[i]));
+    }
+    if (!std::is_sorted(out.begin(), out.end())) std::sort(out.begin(), out.end());
+    if (!std::is_sorted(in.begin(), in.end())) std::sort(in.begin(), in.end());
+    for (size_t i = 1; i < out.size(); ++i)
+        if (out[i].first < out[i - 1].second) return true;
+    // inputs may share memory with one another
+    size_t o = 0;
+    uintptr_t seen = 0;      // the furthest end of an input that starts before the output at hand
+    for (const Range& r : out) {
+        while (o < in.size() && in[o].first < r.second) seen = std::max(seen, in[o++].second);
+        if (seen > r.first) return true;
+    }
+    return false;
+}
+
+template <bool CLIP, int CAP>
+static cudaError_t launch_grad(const GradCall& c, const GradTable<CAP>& table, unsigned G, cudaStream_t st) {
+    if (!CLIP || c.norm_in) {
+        k_grad<CLIP, CAP><<<G, kGradThreads, 0, st>>>(c, table);
+        return cudaGetLastError();
+    }
+    void* args[] = {(void*)&c, (void*)&table};
+    return cudaLaunchCooperativeKernel((const void*)k_grad<CLIP, CAP>, dim3(G), dim3(kGradThreads), args, 0, st);
+}
+
+template <bool CLIP>
+static int enqueue_grad(GradCall& c, const void* const* grads, const int32_t* types, void* const* outs,
+                        const int32_t* out_types, const int64_t* sizes, cudaStream_t st) {
+    Workspace* ws = nullptr;
+    WorkspaceLock held;
+    const int wrc = acquire_workspace(1, c.T > kGradMany ? c.T : 1, st, &ws, held);
+    if (wrc != GK_OK) return wrc;
+    int dev = 0, most = 0;
+    GK_CUDA_TRY(cudaGetDevice(&dev));
+    const int grc = grad_grid(dev, ws->sm_count, &most);
+    if (grc != GK_OK) return grc;
+    char* at = static_cast<char*>(ws->grad_block);
+    c.ctl = reinterpret_cast<GradCtl*>(at);
+    c.cta_sums = reinterpret_cast<double*>(at + 256);
+    c.span_sums = c.cta_sums + kGradMaxCtas;
+    // (the records before the sums' end by the workspace's own size, which may be for more tensors)
+    GradRec* in_ws = reinterpret_cast<GradRec*>(c.span_sums + kGradMaxCtas + (ws->s_cap > kGradMany ? ws->s_cap : kGradMany));
+    c.extra = (unsigned)host_knob(kKnobExtraArrivals);
+    unsigned units = 0;
+    auto record = [&](GradRec& r, int32_t i) {
+        r.src = grads[i];
+        r.dst = CLIP ? outs[i] : nullptr;
+        r.n = sizes[i];
+        r.first = units;
+        r.types = (unsigned)types[i] | (CLIP ? (unsigned)out_types[i] << 8 : 0u);
+        units += (unsigned)(((uint64_t)sizes[i] * type_size(types[i]) + kGradUnit - 1) / kGradUnit);
+    };
+    auto grid = [&]() { return units < (unsigned)most ? std::max(units, 1u) : (unsigned)most; };
+    if (c.T <= kGradFew) {
+        GradTable<kGradFew> table;
+        for (int32_t i = 0; i < c.T; ++i) record(table.rec[i], i);
+        c.units = units;
+        GK_CUDA_TRY((launch_grad<CLIP, kGradFew>(c, table, grid(), st)));
+    } else {
+        GradTable<kGradMany> table;
+        if (c.T <= kGradMany) {
+            for (int32_t i = 0; i < c.T; ++i) record(table.rec[i], i);
+        } else {
+            for (int32_t i = 0; i < c.T; i += kGradMany) {
+                const int n = std::min(kGradMany, c.T - i);
+                for (int j = 0; j < n; ++j) record(table.rec[j], i + j);
+                k_grad_table<<<(n + 255) / 256, 256, 0, st>>>(in_ws + i, n, table);
+                GK_CUDA_TRY(cudaGetLastError());
+                note_launch();
+            }
+            c.table = in_ws;
+        }
+        c.units = units;
+        GK_CUDA_TRY((launch_grad<CLIP, kGradMany>(c, table, grid(), st)));
+    }
+    note_launch();
+    return GK_OK;
+}
+
+}  // namespace gk
+
+using namespace gk;
+
+extern "C" int gk_grad_norm(const void* const* grads, const int32_t* types, const int64_t* sizes, int32_t T,
+                            float* norm_out, float* norms_out, gk_stream_t stream) {
+    const int rc = check_list(grads, types, sizes, T);
+    if (rc != GK_OK) return rc;
+    if (!norm_out) return GK_ERR_NULL;
+    GradCall c = {};
+    c.T = T;
+    c.norm_out = norm_out;
+    c.norms_out = norms_out;
+    return enqueue_grad<false>(c, grads, types, nullptr, nullptr, sizes, (cudaStream_t)stream);
+}
+
+extern "C" int gk_grad_clip(const void* const* grads, const int32_t* types, void* const* outs, const int32_t* out_types,
+                            const int64_t* sizes, int32_t T, float max_norm, const float* scale, const float* norm_in,
+                            float* norm_out, gk_stream_t stream) try {
+    const int rc = check_list(grads, types, sizes, T);
+    if (rc != GK_OK) return rc;
+    if (T > 0 && (!outs || !out_types)) return GK_ERR_NULL;
+    if (!(max_norm > 0.f)) return GK_ERR_NORM;
+    for (int32_t i = 0; i < T; ++i) {
+        if (!known_type(out_types[i])) return GK_ERR_TYPE;
+        if (sizes[i] > 0 && !outs[i]) return GK_ERR_NULL;
+        if ((uintptr_t)outs[i] & (type_size(out_types[i]) - 1)) return GK_ERR_ALIGN;
+    }
+    if (outputs_overlap(grads, types, outs, out_types, sizes, T)) return GK_ERR_ALIAS;
+    GradCall c = {};
+    c.T = T;
+    c.max_norm = max_norm;
+    c.scale = scale;
+    c.norm_in = norm_in;
+    c.norm_out = norm_out;
+    return enqueue_grad<true>(c, grads, types, outs, out_types, sizes, (cudaStream_t)stream);
+} catch (const std::bad_alloc&) {
+    return GK_ERR_NOMEM;
+}

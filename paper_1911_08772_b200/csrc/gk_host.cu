@@ -12,6 +12,7 @@
 
 #include "gk_alg1.cuh"
 #include "gk_common.cuh"
+#include "gk_grad.cuh"
 #include "gk_segmented.cuh"
 
 namespace gk {
@@ -49,7 +50,7 @@ int64_t output_capacity(int64_t d) {
 static size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 struct Layout {
-    size_t ctrl, partials, part_recs, hist, cta_counts, bars, cta_trace, rowcnt, tile_status, seg, total;
+    size_t ctrl, partials, part_recs, hist, cta_counts, bars, cta_trace, rowcnt, tile_status, seg, grad, total;
 };
 
 static Layout layout_for(int64_t d, int32_t S) {
@@ -65,6 +66,7 @@ static Layout layout_for(int64_t d, int32_t S) {
     L.rowcnt = at;      at = align_up(at + sizeof(unsigned int) * 2 * ((size_t)(d >> 12) + 2), 256);
     L.tile_status = at; at = align_up(at + sizeof(unsigned long long) * (size_t)num_compact_tiles(d), 256);
     L.seg = at;         at = align_up(at + segmented_scratch_bytes(d, S), 256);
+    L.grad = at;        at = align_up(at + grad_scratch_bytes(S), 256);
     L.total = at;
     return L;
 }
@@ -120,6 +122,7 @@ int acquire_workspace(int64_t d, int32_t S, cudaStream_t stream, Workspace** out
         ws.rowcnt = reinterpret_cast<unsigned int*>(b + L.rowcnt);
         ws.tile_status = reinterpret_cast<unsigned long long*>(b + L.tile_status);
         ws.seg_block = b + L.seg;
+        ws.grad_block = b + L.grad;
         GK_CUDA_TRY(cudaDeviceGetAttribute(&ws.sm_count, cudaDevAttrMultiProcessorCount, std::get<0>(key)));
     }
     *out = &ws;
@@ -251,6 +254,19 @@ extern "C" int dgck_last_info(gk_stream_t stream, int64_t* host_out) {
     return GK_OK;
 }
 
+extern "C" int gk_grad_last_info(gk_stream_t stream, int64_t* host_out) {
+    if (!host_out) return GK_ERR_NULL;
+    WorkspaceLock held;
+    Workspace* ws = find_workspace((cudaStream_t)stream, held);
+    if (!ws) return GK_ERR_NULL;
+    GK_CUDA_TRY(cudaStreamSynchronize((cudaStream_t)stream));
+    GradCtl ctl;
+    GK_CUDA_TRY(cudaMemcpy(&ctl, ws->grad_block, sizeof(ctl), cudaMemcpyDeviceToHost));
+    host_out[0] = ctl.status;
+    host_out[1] = ctl.clipped;
+    return GK_OK;
+}
+
 extern "C" int gk_last_segment_stats(gk_stream_t stream, int32_t S, gk_stats* host_out) {
     if (!host_out) return GK_ERR_NULL;
     WorkspaceLock held;
@@ -337,6 +353,7 @@ extern "C" const char* gk_strerror(int code) {
         case GK_ERR_TYPE: return "element type not taken by this call";
         case GK_ERR_STRIDE: return "row stride shorter than the row";
         case GK_ERR_TEMPERATURE: return "temperature must be positive and finite, and so must its reciprocal";
+        case GK_ERR_NORM: return "the largest norm must be positive";
         default: return "unknown gk_status";
     }
 }
