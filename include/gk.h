@@ -411,6 +411,54 @@ int gk_vocab_distill(const void* h, int64_t ldh, const void* w, int64_t ldw, int
 int gk_vocab_topk(const void* logits, int64_t ld, int32_t dtype, int64_t n, int64_t V, int32_t k, float temperature,
                   int32_t* idx_out, float* val_out, float* lse_out, gk_stream_t stream);
 
+/*
+ * gk_vocab_logprob -- log probabilities of given tokens under rows of logits, with the rows' entropies and their most
+ * probable tokens: what a policy or preference loss takes of its rollouts, and a server answers with.  With y = z / T,
+ *     lse_n = log sum_v exp y_nv;   logp_nj = y_n,t(n,j) - lse_n;   p_nv = exp(y_nv - lse_n);
+ *     entropy_n = -sum_v p_nv log p_nv;
+ *     rank_n = #{v: z_nv > z_nt, or z_nv = z_nt and v < t},  t = t(n,0)   (0: the most probable).
+ *
+ *   logits     DEVICE in   n rows of V elements of `dtype` (any gk_type), row stride ld >= V
+ *   n, V       n >= 0, 1 <= V <= 2^31 - 1
+ *   token      DEVICE in   n x m int64 (contiguous), 0 <= m <= 128; NULL for m = 0.  A token outside [0, V) is left
+ *                          out: logp 0.  A row that was given tokens, all of them left out, is left out itself:
+ *                          zeros, rank -1, idx -1, whatever its logits hold, which are not read
+ *   temperature  T > 0 with a finite reciprocal
+ *   k          alternatives, 0 <= k <= min(V, 128)
+ *   logp_out   DEVICE out  n x m floats; NULL: not wanted (as the next three)
+ *   rank_out   DEVICE out  n int32: the rank of the row's first token, -1 where that is left out or m = 0
+ *   entropy_out, lse_out  DEVICE out  n floats each
+ *   idx_out    DEVICE out  n x k int32: the k largest logits' places, the largest first, equal ones in order of
+ *                          increasing index (+0 and -0 tie, NaN counts as above +inf)
+ *   val_out    DEVICE out  n x k floats, their log probabilities.  Both, or k = 0
+ * A row of nothing but -inf has lse -inf, entropy 0 and log probabilities -inf; +inf or NaN in a row that counts
+ * gives what the formulas give with it: lse +inf, entropy NaN, log probabilities -inf (NaN at +inf); NaN everywhere.
+ * One pass over the logits, sums in fp32 relative to the row's maximum; no workspace; the same call gives the same
+ * bits.
+ *
+ * gk_vocab_logprob_grad -- the gradient with respect to the logits of
+ *     sum_nj a_nj logp_nj + sum_n b_n entropy_n + sum_n c_n lse_n:
+ *     dz_nv = (1 / T) (sum_j a_nj ([v = t(n,j)] - p_nv) - b_n p_nv (log p_nv + entropy_n) + c_n p_nv).
+ *
+ *   logits, ld, dtype, n, V, token, m, temperature   as given to gk_vocab_logprob
+ *   lse, entropy   DEVICE in   n floats each, what that call wrote; entropy may be NULL where entropy_grad is
+ *   logp_grad  DEVICE in   a, n x m floats (those of tokens left out are not read); NULL: 0
+ *   entropy_grad   DEVICE in   b, n floats; NULL: 0
+ *   lse_grad   DEVICE in   c, n floats (a penalty on the log-sum-exp); NULL: 0
+ *   dlogits    DEVICE out  n rows of V elements of `dtype`, row stride lddz >= V.  The logits themselves (same
+ *                          pointer and stride: in place), or memory that shares nothing with them
+ * A token given twice counts twice.  Rows left out get zeros, and so do rows whose lse is below -1e30: their masks, of
+ * -inf or of a type's lowest value, leave nothing.  So do logits of -inf that are no token.  log p is taken from lse
+ * and has its rounding, 2^-24 of |lse|.  Rounded once to `dtype`.  No workspace.
+ */
+int gk_vocab_logprob(const void* logits, int64_t ld, int32_t dtype, int64_t n, int64_t V, const int64_t* token, int32_t m,
+                     float temperature, int32_t k, float* logp_out, int32_t* rank_out, float* entropy_out, float* lse_out,
+                     int32_t* idx_out, float* val_out, gk_stream_t stream);
+int gk_vocab_logprob_grad(const void* logits, int64_t ld, int32_t dtype, int64_t n, int64_t V, const int64_t* token,
+                          int32_t m, float temperature, const float* lse, const float* entropy, const float* logp_grad,
+                          const float* entropy_grad, const float* lse_grad, void* dlogits, int64_t lddz,
+                          gk_stream_t stream);
+
 /* Bytes that one piece of the vocabulary may take in the workspace of gk_vocab_loss and
  * gk_vocab_distill (default 2 GiB).  A piece has at least 256 columns.  Process-wide; returns
  * GK_ERR_CAPACITY if bytes < 0. */

@@ -29,7 +29,7 @@ EXPORTS = [
     "gk_apply_sparse", "gk_apply_gathered", "gk_histogram", "gk_debug_set", "gk_last_path_info", "gk_select", "gk_set_params",
     "gk_vocab_loss", "gk_vocab_distill", "gk_vocab_topk", "gk_vocab_set_budget", "gk_vocab_reserve",
     "gk_vocab_workspace_bytes", "gk_vocab_last_info",
-    "gk_grad_norm", "gk_grad_clip", "gk_grad_last_info",
+    "gk_vocab_logprob", "gk_vocab_logprob_grad", "gk_grad_norm", "gk_grad_clip", "gk_grad_last_info",
 ]
 
 
@@ -142,6 +142,11 @@ def load() -> C.CDLL:
     L.gk_vocab_workspace_bytes.restype = i64
     L.gk_vocab_last_info.argtypes = [vp, C.POINTER(i64)]
     L.gk_vocab_last_info.restype = C.c_int
+    rows = [vp, i64, i32, i64, i64, vp, i32, C.c_float]
+    L.gk_vocab_logprob.argtypes = rows + [i32, vp, vp, vp, vp, vp, vp, vp]
+    L.gk_vocab_logprob.restype = C.c_int
+    L.gk_vocab_logprob_grad.argtypes = rows + [vp, vp, vp, vp, vp, vp, i64, vp]
+    L.gk_vocab_logprob_grad.restype = C.c_int
     grads = [C.POINTER(vp), C.POINTER(i32)]
     L.gk_grad_norm.argtypes = grads + [C.POINTER(i64), i32, vp, vp, vp]
     L.gk_grad_norm.restype = C.c_int
@@ -410,6 +415,72 @@ def gk_vocab_topk(logits, k: int, idx_out, val_out, lse_out=None, temperature: f
                                 _vec(val_out, torch.float32, device, (n, k), "val_out"),
                                 None if lse_out is None else _vec(lse_out, torch.float32, device, (n,), "lse_out"),
                                 _stream_of(device)))
+
+
+def _given(token, n, device):
+    """(pointer, tokens a row) of the tokens given to each row."""
+    import torch
+    if token is None:
+        return None, 0
+    m = token.shape[1] if isinstance(token, torch.Tensor) and token.dim() == 2 else 1
+    shape = (n, m) if token.dim() == 2 else (n,)
+    return _vec(token, torch.int64, device, shape, "token"), m
+
+
+def _want(t, dtype, device, shape, name):
+    """The pointer of a tensor that may be left away; of its shape, or flat where a row has one value."""
+    import torch
+    if t is None:
+        return None
+    if len(shape) == 2 and shape[1] == 1 and isinstance(t, torch.Tensor) and t.dim() == 1:
+        shape = shape[:1]
+    return _vec(t, dtype, device, shape, name)
+
+
+def gk_vocab_logprob(logits, token, logp_out=None, rank_out=None, entropy_out=None, lse_out=None, idx_out=None, val_out=None,
+                     temperature: float = 1.0) -> None:
+    """Log probabilities of given tokens under rows of logits, the rank of each row's first one, the rows'
+    entropies and log-sum-exps, and their most probable tokens with log probabilities (see gk.h).
+    logits (n, V): float32, bfloat16 or float16, row stride allowed; token (n, m) or (n,) int64 or None;
+    logp_out like token, float32; rank_out (n,) int32; entropy_out, lse_out (n,) float32;
+    idx_out (n, k) int32 with val_out (n, k) float32.  Any output may be None."""
+    import torch
+    device = _matrices(logits)
+    n, V = logits.shape
+    p, ld = _rows(logits, logits.dtype, device, name="logits")
+    tp, m = _given(token, n, device)
+    if (idx_out is None) != (val_out is None):
+        raise GkError("idx_out and val_out go together")
+    k = 0 if idx_out is None else int(idx_out.shape[-1])
+    f32, row = torch.float32, (n,)
+    _check(load().gk_vocab_logprob(p, ld, _type(logits.dtype), n, V, tp, m, temperature, k,
+                                   _want(logp_out, f32, device, (n, m), "logp_out"),
+                                   _want(rank_out, torch.int32, device, row, "rank_out"),
+                                   _want(entropy_out, f32, device, row, "entropy_out"),
+                                   _want(lse_out, f32, device, row, "lse_out"),
+                                   None if k == 0 else _vec(idx_out, torch.int32, device, (n, k), "idx_out"),
+                                   None if k == 0 else _vec(val_out, f32, device, (n, k), "val_out"), _stream_of(device)))
+
+
+def gk_vocab_logprob_grad(logits, token, lse, dlogits, logp_grad=None, entropy=None, entropy_grad=None, lse_grad=None,
+                          temperature: float = 1.0) -> None:
+    """The gradient at the logits from those of what gk_vocab_logprob wrote (see gk.h): logp_grad like token,
+    entropy_grad (with entropy) and lse_grad (n,), float32 or None.  lse (n,): gk_vocab_logprob's; dlogits (n, V):
+    of the logits' type, row stride allowed, or the logits themselves."""
+    import torch
+    device = _matrices(logits, dlogits)
+    n, V = logits.shape
+    p, ld = _rows(logits, logits.dtype, device, name="logits")
+    dp, lddz = _rows(dlogits, logits.dtype, device, n, V, name="dlogits")
+    tp, m = _given(token, n, device)
+    f32, row = torch.float32, (n,)
+    if logp_grad is not None and m == 0:
+        raise GkError("logp_grad without tokens")
+    _check(load().gk_vocab_logprob_grad(p, ld, _type(logits.dtype), n, V, tp, m, temperature,
+                                        _vec(lse, f32, device, row, "lse"), _want(entropy, f32, device, row, "entropy"),
+                                        _want(logp_grad, f32, device, (n, m), "logp_grad"),
+                                        _want(entropy_grad, f32, device, row, "entropy_grad"),
+                                        _want(lse_grad, f32, device, row, "lse_grad"), dp, lddz, _stream_of(device)))
 
 
 def gk_vocab_set_budget(nbytes: int) -> None:

@@ -16,6 +16,7 @@
 #include "gk_coop.cuh"
 #include "gk_grad.cuh"
 #include "gk_segmented.cuh"
+#include "gk_words.cuh"
 
 namespace gk {
 
@@ -99,7 +100,7 @@ __device__ __forceinline__ double squares(const char* p, int64_t n) {
 #pragma unroll
         for (int j = 0; j < kWords; ++j) {
             float f[kVec];
-            unpack16B<TYPE>(x[j], f);
+            unpack<TYPE>(x[j], f);
 #pragma unroll
             for (int e = 0; e < kVec; e += 2) {
                 s = fmaf(f[e], f[e], s);
@@ -113,7 +114,7 @@ __device__ __forceinline__ double squares(const char* p, int64_t n) {
 #pragma unroll
             for (int j = 0; j < kWords; ++j) {
                 float f[kVec];
-                unpack16B<TYPE>(x[j], f);
+                unpack<TYPE>(x[j], f);
 #pragma unroll
                 for (int e = 0; e < kVec; ++e) acc = fma((double)f[e], (double)f[e], acc);
             }
@@ -188,7 +189,7 @@ __device__ __noinline__ void scaled(const char* src, char* dst, int64_t n, float
 #pragma unroll
             for (int e = 0; e < kS / 2; ++e) {
                 float g[Elem<SRC>::vec];
-                unpack16B<SRC>(x[j][e], g);
+                unpack<SRC>(x[j][e], g);
 #pragma unroll
                 for (int a = 0; a < Elem<SRC>::vec; ++a) f[e * Elem<SRC>::vec + a] = c * g[a];
             }
