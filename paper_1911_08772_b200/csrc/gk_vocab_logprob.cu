@@ -1,32 +1,37 @@
 // Log probabilities of given tokens with entropy, rank and the most probable tokens, and their gradient
 // (include/gk.h: gk_vocab_logprob, gk_vocab_logprob_grad).
 //
-// Forward: one CTA a row, one pass.  With m the row's maximum so far and d = (z - m) / T in units of log 2, the
-// pass sums S0 = 2^d and S1 = d 2^d; a larger maximum by b rescales S0 by 2^b and S1 to 2^b (S1 + b S0).  Then
+// Forward: one pass over a row, by a CTA or, where there are few rows, by the CTAs of a cluster.  With m about the row's
+// maximum and d = (z - m) / T in units of log 2, threads sum S0 = 2^d and S1 = d 2^d; a larger m by b rescales S0 by
+// 2^-b and S1 to 2^-b (S1 - b S0).  At the end, with the maximum itself,
 //     lse = m / T + log S0,   entropy = log S0 - log(2) S1 / S0,
-// two terms of one sign, as m is the maximum at the end, so that a small entropy keeps its digits.  The rank counts
-// the elements before the token that are not below it, and those behind it that are above.
+// two terms of one sign, so that a small entropy keeps its digits.  The rank counts the elements before the token that
+// are not below it, and those behind it that are above.
 //
-// Alternatives: a threshold from a sample of the row, which a little more than k elements are expected to be above;
-// those are listed, and the place of each among them is counted, which sorts them.  Where fewer than k are above, the
-// first elements equal to the threshold fill the list (rows whose mask leaves little); where that is not enough
-// either, or the list is too short, the row is walked again in chunks and the list cut whenever it is full.
+// Alternatives: a threshold from a sample of the row, which a little more than k elements are expected to be above.
+// Words that have some are noted; their elements are listed, and the place of each among them is counted, which sorts
+// them.  Where fewer than k are above, the first elements equal to the threshold fill the list (rows whose mask leaves
+// little); where that is not enough either, or the list is too short, the row is walked again in chunks, from a bound
+// that the list gives, and the list cut whenever it is full.
 #include "gk_words.cuh"
 
 namespace gk {
 
 constexpr int kLogprobMaxTokens = 128, kLogprobMaxAlternatives = 128;
-constexpr int kLpThreads = 256, kLpWarps = kLpThreads / 32;
-constexpr int kLpList = 2048;       // entries of the list of alternatives
-constexpr int kLpRanked = 512;      // as many as are sorted by counting; a longer list is cut first
 constexpr float kLpFloor = -200.f;  // powers of two below this are zero in fp32, and their products with it too
+constexpr int kLpQuad = 4;          // words a thread fetches together, from four places: the first are a sample of the row
+constexpr int kLpParts = 8;         // CTAs a row at most (a cluster)
+constexpr int kLpShort = 4096;      // words of a row that few threads take
+constexpr float kLpSlack = 4.f;     // how far a logit may be above what the sums are relative to, in powers of two
+// Exponents of maxima up to this are kept to a sixteenth and better by one rounding.
+constexpr float kLpLargest = 1048576.f;
 
 struct LogprobCall {
     const char* logits;
     int64_t ld, n, V;
     const int64_t* token;
-    int m, k;
-    float T, zscale;      // zscale: log2(e) / T
+    int m, k, parts;
+    float inv_T, inv_T_low, zscale;      // 1 / T in two parts, log2(e) / T
     float* logp;
     int32_t* rank;
     float* entropy;
@@ -40,6 +45,59 @@ __device__ __forceinline__ float max_nan(float a, float b) {
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
     return r;
 }
+// A value as a threshold for a word's elements, and the next smaller one: in both halves of a word for 16-bit types.
+template <int TYPE>
+__device__ __forceinline__ unsigned threshold_of(float v, bool below) {
+    unsigned b = TYPE == GK_TYPE_F32 ? __float_as_uint(v) : to16<TYPE == GK_TYPE_F16>(v);
+    const unsigned sign = TYPE == GK_TYPE_F32 ? 0x80000000u : 0x8000u;
+    if (below) b = (b & ~sign) == 0 ? sign + 1u : b & sign ? b + 1u : b - 1u;
+    return TYPE == GK_TYPE_F32 ? b : b << 16 | b;
+}
+// On the two halves of a word of 16-bit elements: all ones for above a threshold, maxima without regard to NaN, and
+// with.
+#define GK_HALVES(NAME, F16_OP, BF16_OP)                                                            \
+    template <int TYPE>                                                                             \
+    __device__ __forceinline__ unsigned NAME(unsigned a, unsigned b) {                              \
+        unsigned r;                                                                                 \
+        if constexpr (TYPE == GK_TYPE_F16) asm(F16_OP " %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));   \
+        else asm(BF16_OP " %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));                                \
+        return r;                                                                                   \
+    }
+GK_HALVES(above2, "set.gt.u32.f16x2", "set.gt.u32.bf16x2")
+GK_HALVES(max2, "max.f16x2", "max.bf16x2")
+GK_HALVES(max2_nan, "max.NaN.f16x2", "max.NaN.bf16x2")
+#undef GK_HALVES
+template <int TYPE>
+__device__ __forceinline__ unsigned above(unsigned a, unsigned threshold) {
+    if constexpr (TYPE == GK_TYPE_F32) {
+        unsigned r;
+        asm("set.gt.u32.f32 %0, %1, %2;" : "=r"(r) : "f"(__uint_as_float(a)), "f"(__uint_as_float(threshold)));
+        return r;
+    } else {
+        return above2<TYPE>(a, threshold);
+    }
+}
+template <int TYPE>
+__device__ __forceinline__ uint4 max2(const uint4& a, const uint4& b) {
+    return make_uint4(max2<TYPE>(a.x, b.x), max2<TYPE>(a.y, b.y), max2<TYPE>(a.z, b.z), max2<TYPE>(a.w, b.w));
+}
+template <int TYPE>
+__device__ __forceinline__ float max_of(const uint4& y) {      // a word's largest element, -inf for nothing but NaN
+    if constexpr (TYPE == GK_TYPE_F32) {
+        return fmaxf(max3(__uint_as_float(y.x), __uint_as_float(y.y), __uint_as_float(y.z)), fmaxf(__uint_as_float(y.w), -INFINITY));
+    } else {
+        const unsigned g = max2<TYPE>(max2<TYPE>(y.x, y.y), max2<TYPE>(y.z, y.w));
+        return max3(from16<TYPE == GK_TYPE_F16>((uint16_t)g), from16<TYPE == GK_TYPE_F16>((uint16_t)(g >> 16)), -INFINITY);
+    }
+}
+template <int TYPE>
+__device__ __forceinline__ float max_of(const uint4 (&x)[kLpQuad]) {
+    if constexpr (TYPE == GK_TYPE_F32) return fmaxf(max3(max_of<TYPE>(x[0]), max_of<TYPE>(x[1]), max_of<TYPE>(x[2])), max_of<TYPE>(x[3]));
+    else return max_of<TYPE>(max2<TYPE>(max2<TYPE>(x[0], x[1]), max2<TYPE>(x[2], x[3])));
+}
+// What the sums take for anything lower, -inf among it: far enough below any maximum, or the row is taken again.
+template <int TYPE>
+constexpr float kLpLowest = TYPE == GK_TYPE_F16 ? -65504.f : -1e30f;
 
 // Maximum (as it is in the logits) and the two sums relative to it.
 struct Sums {
@@ -58,323 +116,588 @@ __device__ __forceinline__ void lp_join(Sums& a, const Sums& b, float zscale) {
     a.m = top;
 }
 
+// Barrier of a cluster's CTAs, and a value in the shared memory of one of them.
+__device__ __forceinline__ void lp_cluster_barrier() {
+    asm volatile("barrier.cluster.arrive.release;\nbarrier.cluster.wait.acquire;" ::: "memory");
+}
+template <class T>
+__device__ __forceinline__ T remote(const T& here, int cta) {
+    uint64_t p;
+    asm volatile("mapa.u64 %0, %1, %2;" : "=l"(p) : "l"(&here), "r"(cta));
+    return *reinterpret_cast<const volatile T*>(p);
+}
+
+template <int NT>
 struct LpShared {
-    uint64_t list[kLpList];      // key of the value above, complement of the index below: all differ
-    uint64_t best[kLogprobMaxAlternatives];
-    float sample[kLpThreads];
-    float m[kLpWarps], s0[kLpWarps], s1[kLpWarps];
-    int above[kLpWarps];
-    int count, any;
-    float tau, first, top;
+    static constexpr int kList = NT == 256 ? 1280 : 512;        // entries of the list of alternatives
+    static constexpr int kNotes = NT == 256 ? 1024 : 384;       // words noted for it, the first with their contents
+    static constexpr int kNoted = NT == 256 ? 512 : 96;
+    static constexpr int kPlaced = NT == 256 ? 256 : 128;       // entries sorted by counting; a longer list is cut first
+    static constexpr int kCtas = NT == 256 ? 4 : 12;            // CTAs an SM
+    alignas(16) uint64_t list[kList];      // key of the value above, complement of the index below: all differ
+    uint4 data[kNoted];
+    int note[kNotes];
+    uint64_t best[kLogprobMaxAlternatives], all[kLpParts * kLogprobMaxAlternatives];      // SPLIT: this CTA's alternatives, all CTAs'
+    Sums sums[8];
+    int above[8];
+    int scratch[2][8];
+    int notes, listed;      // (may exceed their lists)
+    float tau;
+    // what the other CTAs of a row read
+    Sums part;
+    int part_above, part_count;
 };
 __device__ __forceinline__ uint64_t lp_entry(float v, int64_t i) { return (uint64_t)order_key(v) << 32 | (uint32_t)~(uint32_t)i; }
 
-// The list of `cnt` entries cut to the k largest and at most kLpRanked - k more; returns a bound that all kept reach
-// and that at least k do.  By all threads, which see `cnt` alike.
-__device__ __noinline__ uint64_t lp_cut(LpShared& sh, int& cnt, int k) {
-    const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
-    uint64_t own[kLpList / kLpThreads];
-#pragma unroll
-    for (int j = 0; j < kLpList / kLpThreads; ++j) own[j] = tid + j * kLpThreads < cnt ? sh.list[tid + j * kLpThreads] : 0;
-    uint64_t t = 0;
-    int reach = cnt;
-    for (int bit = 63; bit >= 0 && reach > kLpRanked; --bit) {
+// How many of all threads' n there are; `turn` alternates from call to call.
+template <int NT>
+__device__ __forceinline__ int lp_count(LpShared<NT>& sh, int n, int turn) {
+    n = (int)__reduce_add_sync(0xffffffffu, (unsigned)n);
+    const int lane = threadIdx.x & 31;
+    if (lane == 0) sh.scratch[turn & 1][threadIdx.x >> 5] = n;
+    __syncthreads();
+    return (int)__reduce_add_sync(0xffffffffu, lane < NT / 32 ? (unsigned)sh.scratch[turn & 1][lane] : 0u);
+}
+// The same, and how many of them are before this thread's (which is one or none).
+template <int NT>
+__device__ __forceinline__ int lp_count_before(LpShared<NT>& sh, bool on, int turn, int& before) {
+    const unsigned ballot = __ballot_sync(0xffffffffu, on);
+    const int all = lp_count(sh, on, turn);
+    before = __popc(ballot & ((1u << (threadIdx.x & 31)) - 1u));
+    for (int w = 0; w < (int)threadIdx.x / 32; ++w) before += sh.scratch[turn & 1][w];
+    return all;
+}
+
+// The bit that a search for a bound starts with, all keys lying between lo and hi, and the bits above it.
+__device__ __forceinline__ int lp_first_bit(unsigned lo, unsigned hi, uint64_t& t) {
+    const unsigned differ = lo ^ hi;
+    const int bit = differ ? 63 - __clz(differ) : 31;
+    t = bit == 63 ? 0 : ((uint64_t)lo << 32) >> (bit + 1) << (bit + 1);
+    return bit;
+}
+
+// The list of `cnt` entries, of keys between lo and hi, cut to between k and `most` >= k of the largest; returns a
+// bound that all kept reach and no other.  All threads see `cnt` alike.
+template <int NT>
+__device__ __noinline__ uint64_t lp_cut(LpShared<NT>& sh, int& cnt, int k, int most, unsigned lo, unsigned hi) {
+    const int tid = (int)threadIdx.x;
+    uint64_t t;
+    __syncthreads();
+    int reach = cnt, turn = 0;
+    for (int bit = lp_first_bit(lo, hi, t); bit >= 0 && reach > most; --bit) {
         const uint64_t c = t | 1ull << bit;
         int n = 0;
-#pragma unroll
-        for (int j = 0; j < kLpList / kLpThreads; ++j) n += own[j] >= c;
-        n = (int)__reduce_add_sync(0xffffffffu, (unsigned)n);
-        __syncthreads();
-        if (lane == 0) sh.above[wid] = n;
-        __syncthreads();
-        n = 0;
-#pragma unroll
-        for (int w = 0; w < kLpWarps; ++w) n += sh.above[w];
+#pragma unroll 4
+        for (int j = tid; j < cnt; j += NT) n += sh.list[j] >= c;
+        n = lp_count(sh, n, turn++);
         if (n >= k) { t = c; reach = n; }
     }
     __syncthreads();
-    if (tid == 0) sh.count = 0;
-    __syncthreads();
-#pragma unroll
-    for (int j = 0; j < kLpList / kLpThreads; ++j)
-        if (own[j] && own[j] >= t) sh.list[atomicAdd(&sh.count, 1)] = own[j];
-    __syncthreads();
-    cnt = sh.count;
+    // those that reach it to the front, behind what has been read
+    int at = 0;
+    for (int j0 = 0; j0 < cnt; j0 += NT) {
+        const int j = j0 + tid;
+        const uint64_t e = j < cnt ? sh.list[j] : 0;
+        const bool on = j < cnt && e >= t;
+        int before;
+        const int all = lp_count_before(sh, on, turn++, before);
+        if (on) sh.list[at + before] = e;
+        at += all;
+        __syncthreads();
+    }
+    cnt = at;
     return t;
 }
 
-// The k largest of a row into sh.list, by walking it; cnt: how many came into the list, k at least.
-template <int TYPE>
-__device__ __noinline__ void lp_walk(LpShared& sh, const char* row, int64_t V, int k, int& cnt) {
-    constexpr int kEach = 4, kChunk = kEach * kLpThreads;
-    static_assert(kLpRanked + kChunk <= kLpList, "a chunk has to fit beside a cut list");
-    const int tid = threadIdx.x;
-    uint64_t least = 0;
+// The k largest of the elements [v0, v1) of a row (all of them if they are fewer) into sh.list, by walking them; cnt:
+// how many came into the list, k at least.  At least k elements reach `least`.  Eight elements a thread at a time where
+// those that reach it fit the list; else one, and the list is cut when it is full.
+template <int TYPE, int NT>
+__device__ __noinline__ void lp_walk(LpShared<NT>& sh, const char* row, int64_t v0, int64_t v1, int k, uint64_t least, int& cnt) {
+    constexpr int kList = LpShared<NT>::kList, kKept = kList - NT, kEach = 8;
+    static_assert(kKept >= kLogprobMaxAlternatives, "a cut list holds all that are asked for");
+    const int tid = (int)threadIdx.x;
+    int turn = 0;
+    cnt = 0;
+    float next[kEach];
+    auto fetch = [&](int64_t i0) {
+#pragma unroll
+        for (int j = 0; j < kEach; ++j)
+            if (i0 + j * NT + tid < v1) next[j] = load_logit<TYPE>(row, i0 + j * NT + tid);
+    };
+    fetch(v0);
     __syncthreads();
-    if (tid == 0) sh.count = 0;
-    __syncthreads();
-    for (int64_t i0 = 0; i0 < V; i0 += kChunk) {
-        float v[kEach];
+    for (int64_t i0 = v0; i0 < v1; i0 += kEach * NT) {
+        uint64_t e[kEach];
+        int n = 0;
 #pragma unroll
         for (int j = 0; j < kEach; ++j) {
-            const int64_t i = i0 + j * kLpThreads + tid;
-            v[j] = i < V ? load_logit<TYPE>(row, i) : 0.f;
+            const int64_t i = i0 + j * NT + tid;
+            e[j] = i < v1 ? lp_entry(next[j], i) : 0;
+            n += i < v1 && e[j] >= least;
         }
-#pragma unroll
+        fetch(i0 + kEach * NT);
+        n = lp_count(sh, n, turn++);
+        if (n == 0) continue;
+        const bool fits = cnt + n <= kList;
+#pragma unroll 1
         for (int j = 0; j < kEach; ++j) {
-            const int64_t i = i0 + j * kLpThreads + tid;
-            const uint64_t e = lp_entry(v[j], i);
-            if (i < V && e >= least) sh.list[atomicAdd(&sh.count, 1)] = e;
+            uint64_t own = e[0];
+#pragma unroll
+            for (int i = 1; i < kEach; ++i) own = i == j ? e[i] : own;
+            int before;
+            const bool on = own != 0 && own >= least;
+            const int all = lp_count_before(sh, on, turn++, before);
+            if (on) sh.list[cnt + before] = own;
+            cnt += all;
+            if (!fits && cnt > kKept) least = lp_cut(sh, cnt, k, kKept, 0u, ~0u);
         }
-        __syncthreads();
-        cnt = sh.count;
-        __syncthreads();
-        if (cnt > kLpRanked) least = lp_cut(sh, cnt, k);
+        if (cnt > kKept) least = lp_cut(sh, cnt, k, kKept, 0u, ~0u);
+    }
+    __syncthreads();
+}
+
+// The first elements that equal v into the list behind its `cnt` entries, until it has k.
+template <int TYPE, int NT>
+__device__ __noinline__ void lp_fill(LpShared<NT>& sh, const char* row, int64_t v0, int64_t v1, float v, int k, int& cnt) {
+    const int tid = (int)threadIdx.x;
+    int turn = 0;
+    __syncthreads();
+    for (int64_t i0 = v0; i0 < v1 && cnt < k; i0 += NT) {
+        const int64_t i = i0 + tid;
+        const bool is = i < v1 && load_logit<TYPE>(row, i) == v;
+        int before;
+        const int all = lp_count_before(sh, is, turn++, before);
+        if (is && cnt + before < k) sh.list[cnt + before] = lp_entry(v, i);
+        cnt += all;
+    }
+    cnt = min(cnt, k);
+    __syncthreads();
+}
+
+// W warps' sums, those of a warp's threads relative to the same maximum, joined in one order.
+template <int W>
+__device__ __forceinline__ Sums lp_join_warps(const Sums (&part)[8], float zscale) {
+    Sums a = part[threadIdx.x & (W - 1)];
+#pragma unroll
+    for (int o = W / 2; o > 0; o >>= 1) {
+        Sums b;
+        b.m = __shfl_xor_sync(0xffffffffu, a.m, o);
+        b.s0 = __shfl_xor_sync(0xffffffffu, a.s0, o);
+        b.s1 = __shfl_xor_sync(0xffffffffu, a.s1, o);
+        lp_join(a, b, zscale);
+    }
+    return a;
+}
+__device__ __forceinline__ void lp_join_lanes(Sums& a) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        a.s0 += __shfl_xor_sync(0xffffffffu, a.s0, o);
+        a.s1 += __shfl_xor_sync(0xffffffffu, a.s1, o);
     }
 }
 
-template <int TYPE>
-__global__ void __launch_bounds__(kLpThreads, 4) k_vocab_logprob(const LogprobCall c) {
-    constexpr int kVec = TYPE == GK_TYPE_F32 ? 4 : 8, kSize = TYPE == GK_TYPE_F32 ? 4 : 2;
-    __shared__ LpShared sh;
+// The sums of the elements [v0, v1) once more, without the shortcuts of the pass: differences first, then the scale.
+template <int TYPE, int NT>
+__device__ __noinline__ Sums lp_again(LpShared<NT>& sh, const char* row, int64_t v0, int64_t v1, float m, float zscale) {
+    Sums a = {m, 0.f, 0.f};
+    const float ref = lp_ref(m);
+#pragma unroll 4
+    for (int64_t i = v0 + (int)threadIdx.x; i < v1; i += NT) {
+        const float d = max_nan((load_logit<TYPE>(row, i) - ref) * zscale, kLpFloor), e = exp2_fast(d);
+        a.s0 += e;
+        a.s1 = fmaf(e, d, a.s1);
+    }
+    lp_join_lanes(a);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) sh.sums[threadIdx.x >> 5] = a;
+    __syncthreads();
+    return lp_join_warps<NT / 32>(sh.sums, zscale);
+}
+
+// Elements [v0, v1) that come before element `first` in the order that puts NaN above +inf.
+template <int TYPE, int NT>
+__device__ __noinline__ int lp_rank_again(LpShared<NT>& sh, const char* row, int64_t v0, int64_t v1, float first_v, int first) {
+    const uint64_t mark = lp_entry(first_v, first);
+    int rank = 0;
+    for (int64_t i = v0 + (int)threadIdx.x; i < v1; i += NT) rank += lp_entry(load_logit<TYPE>(row, i), i) > mark;
+    __syncthreads();
+    return lp_count(sh, rank, 0);
+}
+
+// A row's results from its sums.
+struct LpResult {
+    float m, log_s0, inv_T, inv_T_low;
+    bool nan, inf, none;
+    __device__ __forceinline__ LpResult(const LogprobCall& c, const Sums& a)
+        : m(a.m), log_s0(logf(a.s0)), inv_T(c.inv_T), inv_T_low(c.inv_T_low), nan(a.s0 != a.s0), inf(a.m == INFINITY), none(a.m == -INFINITY && a.s0 == a.s0) {}
+    // (the second part of 1 / T times an infinity is one of either sign)
+    __device__ __forceinline__ float scaled(float d) const { return fabsf(d) < INFINITY ? fmaf(d, inv_T, d * inv_T_low) : d; }
+    __device__ __forceinline__ float logp(float v) const { return none ? -INFINITY : nan ? NAN : inf ? (v < INFINITY ? -INFINITY : NAN) : scaled(v - m) - log_s0; }
+    __device__ __forceinline__ float lse() const { return none ? -INFINITY : nan ? NAN : inf ? INFINITY : scaled(m) + log_s0; }
+    __device__ __forceinline__ float entropy(const Sums& a) const { return none ? 0.f : nan || inf ? NAN : log_s0 - 0.69314718f * __fdividef(a.s1, a.s0); }
+};
+
+// SPLIT: the CTAs of a cluster share a row.
+template <int TYPE, int NT, bool SPLIT>
+__global__ void __launch_bounds__(NT, SPLIT ? 2 : LpShared<NT>::kCtas) k_vocab_logprob(const LogprobCall c) {
+    using Shared = LpShared<NT>;
+    constexpr int kVec = TYPE == GK_TYPE_F32 ? 4 : 8, kSize = TYPE == GK_TYPE_F32 ? 4 : 2, kWarps = NT / 32;
+    __shared__ Shared sh;
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
-    const int64_t r = blockIdx.x, V = c.V;
+    const int parts = SPLIT ? c.parts : 1, part = SPLIT ? (int)(blockIdx.x % (unsigned)parts) : 0;
+    const int64_t r = SPLIT ? blockIdx.x / (unsigned)parts : blockIdx.x;
     const char* row = c.logits + r * c.ld * kSize;
-    // the given tokens
-    const int64_t t = tid < c.m ? c.token[r * c.m + tid] : -1;
-    const bool mine = t >= 0 && t < V;
-    if (c.m > 0 && !__syncthreads_or(mine)) {
-        if (tid < c.m && c.logp) c.logp[r * c.m + tid] = 0.f;
-        if (tid == 0) {
-            if (c.rank) c.rank[r] = -1;
-            if (c.entropy) c.entropy[r] = 0.f;
-            if (c.lse) c.lse[r] = 0.f;
+    // this CTA's share of the row: elements before its words and behind them, whole words
+    const int V = (int)c.V, edge = min((int)((16 - ((uintptr_t)row & 15)) % 16) / kSize, V), all_words = (V - edge) / kVec;
+    const int first_of = SPLIT ? (int)((int64_t)all_words * part / parts) : 0, words = (SPLIT ? (int)((int64_t)all_words * (part + 1) / parts) : all_words) - first_of;
+    const int before = part == 0 ? edge : 0, behind = part == parts - 1 ? V - edge - all_words * kVec : 0;
+    const int head = edge + first_of * kVec, v0 = head - before, v1 = head + words * kVec + behind;
+    const uint4* own = (const uint4*)(row + edge * kSize) + first_of + tid;
+    const int quarter = (words + NT * kLpQuad - 1) / (NT * kLpQuad), step = quarter * NT;
+    // words past the end are -inf, which adds to nothing
+    constexpr unsigned kNone = TYPE == GK_TYPE_F32 ? 0xff800000u : TYPE == GK_TYPE_F16 ? 0xfc00fc00u : 0xff80ff80u;
+    auto fetch = [&](uint4 (&to)[kLpQuad], int q) {
+        if (q >= quarter) return;
+        const int w = q * NT;
+        if (w + (kLpQuad - 1) * step + NT <= words) {
+#pragma unroll
+            for (int i = 0; i < kLpQuad; ++i) to[i] = __ldcs(own + w + i * step);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kLpQuad; ++i)
+                to[i] = w + i * step + tid < words ? __ldcs(own + w + i * step) : make_uint4(kNone, kNone, kNone, kNone);
         }
-        if (tid < c.k) { c.idx[r * c.k + tid] = -1; c.val[r * c.k + tid] = 0.f; }
+    };
+    uint4 x[kLpQuad], y[kLpQuad];
+    fetch(x, 0);
+    // the given tokens
+    const int64_t token = tid < c.m ? c.token[r * c.m + tid] : -1;
+    const bool mine = token >= 0 && token < V;
+    bool any = mine;
+    for (int j = tid + NT; j < c.m; j += NT) {
+        const int64_t t = c.token[r * c.m + j];
+        any |= t >= 0 && t < V;
+    }
+    const bool odd = lane < 16 ? lane < before : lane - 16 < behind;      // a warp's elements outside the words
+    const int odd_at = lane < 16 ? v0 + lane : v1 - behind + lane - 16;
+    const float odd_v = odd ? load_logit<TYPE>(row, odd_at) : -INFINITY;
+    if (tid == 0) sh.notes = sh.listed = 0;
+    if (!__syncthreads_or(any) && c.m > 0) {
+        if (part == 0) {
+            for (int j = tid; j < c.m && c.logp; j += NT) c.logp[r * c.m + j] = 0.f;
+            for (int j = tid; j < c.k; j += NT) { c.idx[r * c.k + j] = -1; c.val[r * c.k + j] = 0.f; }
+            if (tid == 0) {
+                if (c.rank) c.rank[r] = -1;
+                if (c.entropy) c.entropy[r] = 0.f;
+                if (c.lse) c.lse[r] = 0.f;
+            }
+        }
         return;
     }
-    const float own = mine ? load_logit<TYPE>(row, t) : 0.f;
-    if (tid == 0) {
-        sh.count = 0;
-        sh.first = own;
-        sh.any = mine ? (int)t : -1;
-    }
-    // elements before the first 16-byte boundary, whole words, the rest
-    int64_t head = (16 - ((uintptr_t)row & 15)) % 16 / kSize;
-    if (head > V) head = V;
-    const int words = (int)((V - head) / kVec);
-    const int64_t rest = V - head - (int64_t)words * kVec;
-    const uint4* body = (const uint4*)(row + head * kSize);
-    // four words a thread at a time, from four places of the row
-    const int steps = (words + kLpThreads - 1) / kLpThreads, quarter = (steps + 3) / 4;
-    uint4 x[4];
-    auto fetch = [&](int q) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int w = (q + i * quarter) * kLpThreads + tid;
-            if (q + i * quarter < steps && w < words) x[i] = __ldcs(body + w);
-        }
-    };
-    fetch(0);
-    auto each = [&](int q, auto&& use) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int w = (q + i * quarter) * kLpThreads + tid;
-            if (q + i * quarter < steps && w < words) use(x[i], w);
-        }
-    };
+    // the first one's logit, by all
+    const int64_t t0 = c.m > 0 ? c.token[r * c.m] : -1;
+    const int first = t0 >= 0 && t0 < V ? (int)t0 : -1;
+    const float first_v = first >= 0 ? load_logit<TYPE>(row, first) : 0.f;
+    fetch(y, 1);
+
     // the first words are the sample: their maximum is where the sums start
-    float top = -INFINITY;
-    each(0, [&](const uint4& y, int) {
-        float f[kVec];
-        unpack<TYPE>(y, f);
-#pragma unroll
-        for (int e = 0; e < kVec; ++e) top = fmaxf(top, f[e]);
-    });
-    sh.sample[tid] = top;
-    __syncthreads();
-    const int first = sh.any;
-    const float first_v = sh.first;
+    float top = quarter > 0 ? max_of<TYPE>(x) : -INFINITY;
     float tau = INFINITY;
     if (c.k > 0) {
-        // with e of the k largest expected in the sample, the (e + 4 sqrt(e) + 4)-th largest of the threads' maxima is
-        // hardly among the row's k largest; where the sample is the row, the k + 1-th
-        const float e = (float)c.k * fminf(1.f, 4.f * kLpThreads * kVec / (float)V);
-        const int want = min(c.k + 1, (int)(e + 4.f * sqrtf(e) + 4.f));
-        int above = 0, equal = 0;
-        for (int j = 0; j < kLpThreads; ++j) {
-            above += sh.sample[j] > top;
-            equal += sh.sample[j] == top;
+        // With e of the k largest expected in the sample, the (e + 4 sqrt(e) + 4)-th largest of 64 groups' or all
+        // threads' maxima is hardly among the row's k largest; where the sample is all there is, the k + 8-th leaves room
+        // for equal ones.
+        const float e = (float)c.k * fminf(1.f, (float)(kLpQuad * NT * kVec) / (float)(v1 - v0));
+        const int want = min(min(c.k + 8, NT), (int)(e + 4.f * sqrtf(e) + 4.f));
+        const int count = NT > 64 && want <= 32 ? 64 : NT;
+        float* sample = reinterpret_cast<float*>(sh.data);
+        float mine = top;
+        if (NT > 64 && count == 64) {
+#pragma unroll
+            for (int o = 1; o < NT / 64; o *= 2) mine = fmaxf(mine, __shfl_xor_sync(0xffffffffu, mine, o));
+            if (lane % (NT / 64) == 0) sample[tid / (NT / 64)] = mine;
+        } else {
+            sample[tid] = mine;
         }
-        static_assert(kLogprobMaxAlternatives < kLpThreads, "the threshold is one of the threads' maxima");
-        if (above < want && above + equal >= want) sh.tau = top;      // all who write write the same
+        __syncthreads();
+        if (tid < count) {
+            mine = sample[tid];
+            int n = 0, reach = 0;
+#pragma unroll 4
+            for (int j = 0; j < count; j += 4) {
+                const float4 s = *(const float4*)&sample[j];
+                n += (s.x > mine) + (s.y > mine) + (s.z > mine) + (s.w > mine);
+                reach += (s.x >= mine) + (s.y >= mine) + (s.z >= mine) + (s.w >= mine);
+            }
+            if (n < want && reach >= want) sh.tau = mine;      // all who write write the same
+        }
         __syncthreads();
         tau = sh.tau;
     }
-    Sums a = {top, 0.f, 0.f};
+    // The powers' exponents are z log2(e) / T - ref, one rounding, ref the rounded exponent of about the maximum:
+    // it is taken anew where a logit is kLpSlack powers of two above.  What it is off by is put right at the end.
+    const float zscale = c.zscale;
+    const uint64_t zscale2 = pair(zscale, zscale);
+    float m = top, least_up = top;      // the largest so far, and what raises ref
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) a.m = fmaxf(a.m, __shfl_xor_sync(0xffffffffu, a.m, o));
-    float ref = lp_ref(a.m);
-    uint64_t s0 = pair(0.f, 0.f), s1 = pair(0.f, 0.f);
-    const uint64_t zscale2 = pair(c.zscale, c.zscale);
-    int rank = 0;
+    for (int o = 16; o > 0; o >>= 1) least_up = fmaxf(least_up, __shfl_xor_sync(0xffffffffu, least_up, o));
+    auto ref_of = [&](float v) { return v == -INFINITY ? 0.f : fminf(fmaxf(v * zscale, -1e30f), 1e30f); };
+    float ref = ref_of(least_up);
+    bool empty = least_up == -INFINITY;
+    least_up += empty ? 0.f : kLpSlack / zscale;
+    float stir = fminf(least_up, tau);      // what a word's largest element has to be above to be looked at
+    uint64_t s0 = pair(0.f, 0.f), s1 = s0, less = pair(-ref, -ref);
     auto raise = [&](float to) {
-        const float d = lp_shift(a.m, to, c.zscale), by = exp2_fast(d);
+        const float r2 = ref_of(to), d = empty ? kLpFloor : fmaxf(ref - r2, kLpFloor), by = exp2_fast(d);
         const uint64_t by2 = pair(by, by);
         s1 = mul2(fma2(s0, pair(d, d), s1), by2);
         s0 = mul2(s0, by2);
-        a.m = to;
-        ref = lp_ref(to);
+        ref = r2;
+        empty = false;
+        least_up = to + kLpSlack / zscale;
+        stir = fminf(least_up, tau);
+        less = pair(-ref, -ref);
     };
-    auto append = [&](float v, int64_t i) {
-        const int at = atomicAdd(&sh.count, 1);
-        if (at < kLpList) sh.list[at] = lp_entry(v, i);
-    };
-    auto single = [&](int64_t i) {
-        const float v = load_logit<TYPE>(row, i);
-        if (v > a.m) raise(v);
-        if (v > tau) append(v, i);
-        if (first >= 0) rank += v > first_v || (v == first_v && i < first);
-        const float d = max_nan((v - ref) * c.zscale, kLpFloor), e = exp2_fast(d);
-        s0 = add2(s0, pair(e, 0.f));
-        s1 = add2(s1, pair(e * d, 0.f));
-    };
-    auto word = [&](const uint4& y, int w) {
-        float f[kVec];
-        unpack<TYPE>(y, f);
-        float g;
-        if constexpr (kVec == 8) {
-            g = max3(f[0], f[1], f[2]);
-            g = max3(g, f[3], f[4]);
-            g = fmaxf(max3(g, f[5], f[6]), f[7]);
+    // The rank: elements not below the token's before it, and above it behind it; by words, the token's own among those
+    // behind until the end.
+    const bool ranked = c.rank != nullptr && first >= 0;
+    const int first_at = first - head, first_word = first_at >= 0 ? first_at / kVec : -1;      // (may be past the words)
+    const unsigned th_behind = threshold_of<TYPE>(first_v, false), th_before = threshold_of<TYPE>(first_v, true);
+    unsigned masks = 0;      // less the all-ones of elements above
+    int rank = 0;
+    auto count_masks = [&]() {
+        if constexpr (TYPE == GK_TYPE_F32) {
+            rank += (int)masks;
         } else {
-            g = fmaxf(max3(f[0], f[1], f[2]), f[3]);
+            // 65536 (upper - lower) + lower
+            const unsigned lower = masks & 0xffffu;
+            rank += (int)(lower + (((masks >> 16) + lower) & 0xffffu));
         }
-        if (g > a.m) raise(g);
-        const int64_t i0 = head + (int64_t)w * kVec;
-        if (g > tau) {
-#pragma unroll
-            for (int e = 0; e < kVec; ++e)
-                if (f[e] > tau) append(f[e], i0 + e);
+        masks = 0;
+    };
+    auto word = [&](const uint4& x, int w) {
+        const float g = max_of<TYPE>(x);
+        m = fmaxf(m, g);
+        if (g > stir) {
+            if (g > least_up) raise(g);
+            if (g > tau) {
+                const int to = atomicAdd(&sh.notes, 1);
+                if (to < Shared::kNotes) sh.note[to] = w;
+                if (to < Shared::kNoted) sh.data[to] = x;
+            }
         }
-        if (first >= 0 && g >= first_v) {
-#pragma unroll
-            for (int e = 0; e < kVec; ++e) rank += f[e] > first_v || (f[e] == first_v && i0 + e < first);
+        if (ranked) {
+            const unsigned th = w < first_word ? th_before : th_behind;
+            masks -= above<TYPE>(x.x, th) + above<TYPE>(x.y, th);
+            masks -= above<TYPE>(x.z, th) + above<TYPE>(x.w, th);
         }
-        const uint64_t less = pair(-ref, -ref);
+        float f[kVec];
+        if constexpr (TYPE == GK_TYPE_F32) {
+            unpack<TYPE>(x, f);
+        } else {
+            const unsigned n = threshold_of<TYPE>(kLpLowest<TYPE>, false);
+            unpack<TYPE>(make_uint4(max2_nan<TYPE>(x.x, n), max2_nan<TYPE>(x.y, n), max2_nan<TYPE>(x.z, n), max2_nan<TYPE>(x.w, n)), f);
+        }
 #pragma unroll
         for (int e = 0; e < kVec; e += 2) {
+            if constexpr (TYPE == GK_TYPE_F32) {
+                f[e] = max_nan(f[e], kLpLowest<TYPE>);
+                f[e + 1] = max_nan(f[e + 1], kLpLowest<TYPE>);
+            }
+            const uint64_t d = fma2(pair(f[e], f[e + 1]), zscale2, less);
             float d0, d1;
-            unpair(mul2(add2(pair(f[e], f[e + 1]), less), zscale2), d0, d1);
-            d0 = max_nan(d0, kLpFloor);
-            d1 = max_nan(d1, kLpFloor);
+            unpair(d, d0, d1);
             const uint64_t p = pair(exp2_fast(d0), exp2_fast(d1));
             s0 = add2(s0, p);
-            s1 = fma2(p, pair(d0, d1), s1);
+            s1 = fma2(p, d, s1);
         }
     };
-    if (tid < head) single(tid);
-    if (tid < rest) single(V - rest + tid);
-    for (int q = 0; q < quarter; ++q) {
-        if (q > 0) fetch(q);
-        each(q, word);
+    auto quad = [&](const uint4 (&x)[kLpQuad], int q) {
+        if (q >= quarter) return;
+#pragma unroll
+        for (int i = 0; i < kLpQuad; ++i) word(x[i], q * NT + i * step + tid);
+        if ((q & 2047) == 2047) count_masks();      // 2^15 of a half
+    };
+    // the next words are on their way while four are looked at
+#pragma unroll 1
+    for (int q = 0; q < quarter; q += 2) {
+        quad(x, q);
+        fetch(x, q + 2);
+        quad(y, q + 1);
+        fetch(y, q + 3);
     }
+    count_masks();
+    if (wid == 0 && odd) {
+        m = fmaxf(m, odd_v);
+        if (odd_v > least_up) raise(odd_v);
+        if (odd_v > tau) sh.list[atomicAdd(&sh.listed, 1)] = lp_entry(odd_v, odd_at);      // 32 at most, the first
+        if (ranked) rank += odd_v > first_v || (odd_v == first_v && odd_at < first);
+        const float d = max_nan(fmaf(odd_v, zscale, -ref), kLpFloor), e = exp2_fast(d);
+        s0 = add2(s0, pair(e, 0.f));
+        s1 = add2(s1, pair(e * d, 0.f));
+    }
+    // equal elements in the token's own word before it
+    if (ranked && first_word >= 0 && first_word < words && tid < first_at % kVec)
+        rank += load_logit<TYPE>(row, first - first_at % kVec + tid) == first_v;
+    const float own_v = tid == 0 ? first_v : mine ? load_logit<TYPE>(row, token) : 0.f;
+    Sums a;
     {
         float lo, hi;
         unpair(s0, lo, hi);
         a.s0 = lo + hi;
         unpair(s1, lo, hi);
         a.s1 = lo + hi;
-    }
-    // the row's sums
+        // Relative to the warp's maximum itself, which is at or above what this thread's ref was taken from.  (Where
+        // that is too large for it, the sums are nothing beside the row's, or the row goes through lp_again.)
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        Sums b;
-        b.m = __shfl_xor_sync(0xffffffffu, a.m, o);
-        b.s0 = __shfl_xor_sync(0xffffffffu, a.s0, o);
-        b.s1 = __shfl_xor_sync(0xffffffffu, a.s1, o);
-        lp_join(a, b, c.zscale);
-    }
-    rank = (int)__reduce_add_sync(0xffffffffu, (unsigned)rank);
-    if (lane == 0) {
-        sh.m[wid] = a.m;
-        sh.s0[wid] = a.s0;
-        sh.s1[wid] = a.s1;
-        sh.above[wid] = rank;
-    }
-    __syncthreads();
-    a = {sh.m[0], sh.s0[0], sh.s1[0]};
-    rank = sh.above[0];
-#pragma unroll
-    for (int w = 1; w < kLpWarps; ++w) {
-        const Sums b = {sh.m[w], sh.s0[w], sh.s1[w]};
-        lp_join(a, b, c.zscale);
-        rank += sh.above[w];
-    }
-    const bool nan = a.s0 != a.s0, inf = a.m == INFINITY, none = a.m == -INFINITY && !nan;
-    const float log_s0 = logf(a.s0);
-    // the log probability of a logit
-    auto logp_of = [&](float v) { return none ? -INFINITY : nan ? NAN : inf ? (v < INFINITY ? -INFINITY : NAN) : (v - a.m) / c.T - log_s0; };
-    if (tid < c.m && c.logp) c.logp[r * c.m + tid] = mine ? logp_of(own) : 0.f;
-    if (nan && c.rank && first >= 0) {
-        // in the order that puts NaN above +inf
-        const uint64_t mark = lp_entry(first_v, first);
-        rank = 0;
-        for (int64_t i = tid; i < V; i += kLpThreads) rank += lp_entry(load_logit<TYPE>(row, i), i) > mark;
+        for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+        a.m = m;
+        const float off = fabsf(ref) < kLpLargest && m > -INFINITY ? fminf(fmaxf(fmaf(m, zscale, -ref), -1.f), -kLpFloor) : 0.f;
+        const float by = exp2_fast(-off);
+        a.s1 = fmaf(-off, a.s0, a.s1) * by;
+        a.s0 *= by;
+        lp_join_lanes(a);
         rank = (int)__reduce_add_sync(0xffffffffu, (unsigned)rank);
-        __syncthreads();
-        if (lane == 0) sh.above[wid] = rank;
-        __syncthreads();
-        rank = 0;
-#pragma unroll
-        for (int w = 0; w < kLpWarps; ++w) rank += sh.above[w];
-    }
-    if (tid == 0) {
-        if (c.rank) c.rank[r] = first >= 0 ? rank : -1;
-        if (c.entropy) c.entropy[r] = none ? 0.f : nan || inf ? NAN : log_s0 - 0.69314718f * (a.s1 / a.s0);
-        if (c.lse) c.lse[r] = none ? -INFINITY : nan ? NAN : inf ? INFINITY : a.m / c.T + log_s0;
-    }
-    if (c.k == 0) return;
-    // the alternatives
-    int cnt = sh.count;
-    __syncthreads();
-    if (!nan && cnt < c.k) {
-        // the first elements that equal the threshold
-        for (int64_t i0 = 0; i0 < V && cnt < c.k; i0 += kLpThreads) {
-            const int64_t i = i0 + tid;
-            const float v = i < V ? load_logit<TYPE>(row, i) : 0.f;
-            const bool is = i < V && v == tau;
-            const unsigned ballot = __ballot_sync(0xffffffffu, is);
-            __syncthreads();
-            if (lane == 0) sh.above[wid] = __popc(ballot);
-            __syncthreads();
-            int at = cnt + __popc(ballot & ((1u << lane) - 1u));
-#pragma unroll
-            for (int w = 0; w < kLpWarps; ++w) {
-                at += w < wid ? sh.above[w] : 0;
-                cnt += sh.above[w];
-            }
-            if (is && at < c.k) sh.list[at] = lp_entry(v, i);
+        if (lane == 0) {
+            sh.above[wid] = rank;
+            sh.sums[wid] = a;
         }
-        cnt = min(cnt, c.k);
-        __syncthreads();
-    }
-    if (nan || cnt < c.k || cnt > kLpList) lp_walk<TYPE>(sh, row, V, c.k, cnt);
-    if (cnt > kLpRanked) lp_cut(sh, cnt, c.k);
-    // the place of each is how many are above it
-    for (int j = tid; j < cnt; j += kLpThreads) {
-        const uint64_t e = sh.list[j];
-        int place = 0;
-        for (int i = 0; i < cnt; ++i) place += sh.list[i] > e;
-        if (place < c.k) sh.best[place] = e;
     }
     __syncthreads();
-    if (tid < c.k) {
-        const uint64_t e = sh.best[tid];
-        const int i = (int)~(uint32_t)e;
-        c.idx[r * c.k + tid] = i;
-        c.val[r * c.k + tid] = logp_of(load_logit<TYPE>(row, i));
+    a = lp_join_warps<kWarps>(sh.sums, zscale);
+    rank = (int)__reduce_add_sync(0xffffffffu, lane < kWarps ? (unsigned)sh.above[lane] : 0u);
+    // exponents that fp32 has no digits for, and infinities: differences first
+    if (a.m > -INFINITY && !(fabsf(a.m * zscale) < kLpLargest && (a.m - kLpLowest<TYPE>) * zscale > -kLpFloor))
+        a = lp_again<TYPE>(sh, row, v0, v1, a.m, zscale);
+    // (nothing is next below -inf)
+    if (ranked && (a.s0 != a.s0 || first_v == -INFINITY)) rank = lp_rank_again<TYPE>(sh, row, v0, v1, first_v, first);
+    const int k = SPLIT ? min(c.k, v1 - v0) : c.k;      // of this CTA's elements
+    int cnt = 0;
+    if (k > 0) {
+        // the list of what may be among the alternatives
+        const int notes = sh.notes;
+        const bool nan = a.s0 != a.s0;
+        for (int j = tid; !nan && j < min(notes, Shared::kNotes); j += NT) {
+            const int w = sh.note[j];
+            float f[kVec];
+            unpack<TYPE>(j < Shared::kNoted ? sh.data[j] : __ldg(own - tid + w), f);
+#pragma unroll
+            for (int e = 0; e < kVec; ++e)
+                if (f[e] > tau) {
+                    const int to = atomicAdd(&sh.listed, 1);
+                    if (to < Shared::kList) sh.list[to] = lp_entry(f[e], head + w * kVec + e);
+                }
+        }
+        __syncthreads();
+        cnt = sh.listed;
+        const bool listed = !nan && notes <= Shared::kNotes && cnt <= Shared::kList;
+        if (listed && cnt < k) lp_fill<TYPE>(sh, row, v0, v1, tau, k, cnt);
+        if (!listed || cnt < k) {
+            // what there is of a list that is too long gives a bound
+            uint64_t least = 0;
+            cnt = min(cnt, Shared::kList);
+            if (!nan && !listed && cnt >= k) least = lp_cut(sh, cnt, k, max(k, Shared::kPlaced / 2), order_key(tau), order_key(a.m));
+            lp_walk<TYPE>(sh, row, v0, v1, k, least, cnt);
+        }
+        if (cnt > Shared::kPlaced)
+            lp_cut(sh, cnt, k, max(k, Shared::kPlaced / 2), listed ? order_key(tau) : 0u, listed ? order_key(a.m) : ~0u);
     }
+    // the place of each is how many are above it
+    auto place_all = [&](auto&& put) {
+        for (int j = tid; j < cnt; j += NT) {
+            const uint64_t e = sh.list[j];
+            int place = 0, i = 0;
+#pragma unroll 2
+            for (; i + 4 <= cnt; i += 4) {
+                const ulonglong2 p = *(const ulonglong2*)&sh.list[i], q = *(const ulonglong2*)&sh.list[i + 2];
+                place += (p.x > e) + (p.y > e) + (q.x > e) + (q.y > e);
+            }
+            for (; i < cnt; ++i) place += sh.list[i] > e;
+            if (place < k) put(place, e);
+        }
+    };
+    if constexpr (SPLIT) {
+        place_all([&](int place, uint64_t e) { sh.best[place] = e; });
+        if (tid == 0) {
+            sh.part = a;
+            sh.part_above = rank;
+            sh.part_count = k;
+        }
+        lp_cluster_barrier();
+        // every CTA joins all parts' sums in one order
+        auto part_of = [&](int p) { return Sums{remote(sh.part.m, p), remote(sh.part.s0, p), remote(sh.part.s1, p)}; };
+        a = part_of(0);
+        rank = remote(sh.part_above, 0);
+        for (int p = 1; p < parts; ++p) {
+            lp_join(a, part_of(p), zscale);
+            rank += remote(sh.part_above, p);
+        }
+    }
+    const LpResult result(c, a);
+    if (part == 0) {
+        if (c.logp && tid < c.m) c.logp[r * c.m + tid] = mine ? result.logp(own_v) : 0.f;
+        for (int j = tid + NT; NT < kLogprobMaxTokens && c.logp && j < c.m; j += NT) {
+            const int64_t t = c.token[r * c.m + j];
+            c.logp[r * c.m + j] = t >= 0 && t < V ? result.logp(load_logit<TYPE>(row, t)) : 0.f;
+        }
+        if (tid == 0) {
+            if (c.rank) c.rank[r] = first >= 0 ? rank : -1;
+            if (c.entropy) c.entropy[r] = result.entropy(a);
+            if (c.lse) c.lse[r] = result.lse();
+        }
+    }
+    auto write = [&](int place, uint64_t e) {
+        c.idx[r * c.k + place] = (int)~(uint32_t)e;
+        c.val[r * c.k + place] = result.logp(key_value((unsigned)(e >> 32)));
+    };
+    if constexpr (!SPLIT) {
+        place_all(write);
+    } else {
+        // all parts' alternatives beside one another, and how many of each part are above each of this CTA's
+        for (int j = tid; j < parts * c.k; j += NT) {
+            const int p = j / c.k, i = j - p * c.k;
+            sh.all[j] = i < remote(sh.part_count, p) ? remote(sh.best[i], p) : 0;
+        }
+        __syncthreads();
+        if (tid < k) {
+            const uint64_t e = sh.all[part * c.k + tid];
+            int place = 0;
+            for (int p = 0; p < parts; ++p) {
+                int lo = 0, hi = c.k;      // entries that fill up a list are zero, below all
+                while (lo < hi) {
+                    const int mid = (lo + hi) >> 1;
+                    if (sh.all[p * c.k + mid] > e) lo = mid + 1; else hi = mid;
+                }
+                place += lo;
+            }
+            if (place < c.k) write(place, e);
+        }
+        lp_cluster_barrier();      // the others have read what is here
+    }
+}
+
+template <int TYPE>
+static cudaError_t launch_logprob(LogprobCall& c, int sms, cudaStream_t st) {
+    const int64_t words = c.V / (TYPE == GK_TYPE_F32 ? 4 : 8);
+    // CTAs a row: as many as there is room for, while each still has a word for every thread
+    while (c.parts < kLpParts && c.n * c.parts * 2 <= 4 * sms && words >= 2 * c.parts * 256) c.parts *= 2;
+    if (c.parts > 1) {
+        cudaLaunchConfig_t cfg = {};
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = (unsigned)c.parts;
+        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        cfg.stream = st;
+        cfg.blockDim = dim3(256);
+        cfg.gridDim = dim3((unsigned)(c.n * c.parts));
+        return cudaLaunchKernelEx(&cfg, k_vocab_logprob<TYPE, 256, true>, c);
+    }
+    if (words <= kLpShort) k_vocab_logprob<TYPE, 64, false><<<(unsigned)c.n, 64, 0, st>>>(c);
+    else k_vocab_logprob<TYPE, 256, false><<<(unsigned)c.n, 256, 0, st>>>(c);
+    return cudaGetLastError();
 }
 
 struct LogprobGradCall {
@@ -391,11 +714,13 @@ struct LogprobGradCall {
     const float* c;
 };
 
+constexpr int kLgThreads = 256;
+
 // A CTA a piece of a row of at most kWords words a thread, the logits read and their gradients written once.
 //     dz = p (k0 + k1 log p),  k0 = (c - sum a - b entropy) / T,  k1 = -b / T,
 // and a / T more at a token, which the CTA that has it writes again at the end.
 template <int TYPE>
-__global__ void __launch_bounds__(kLpThreads, 4) k_vocab_logprob_grad(const LogprobGradCall c) {
+__global__ void __launch_bounds__(kLgThreads, 4) k_vocab_logprob_grad(const LogprobGradCall c) {
     constexpr int kVec = TYPE == GK_TYPE_F32 ? 4 : 8, kSize = TYPE == GK_TYPE_F32 ? 4 : 2, kWords = 4;
     __shared__ int64_t tokens[kLogprobMaxTokens];
     const int tid = threadIdx.x, lane = tid & 31;
@@ -416,7 +741,7 @@ __global__ void __launch_bounds__(kLpThreads, 4) k_vocab_logprob_grad(const Logp
         if (!apart) {
 #pragma unroll
             for (int j = 0; j < kWords; ++j)
-                if (w0 + j * kLpThreads + tid < w1) x[j] = __ldcs((const uint4*)(row + head * kSize) + w0 + j * kLpThreads + tid);
+                if (w0 + j * kLgThreads + tid < w1) x[j] = __ldcs((const uint4*)(row + head * kSize) + w0 + j * kLgThreads + tid);
         }
         const float lse = c.lse[r], b = c.b ? c.b[r] : 0.f;
         float k0 = c.c ? c.c[r] : 0.f;
@@ -470,11 +795,11 @@ __global__ void __launch_bounds__(kLpThreads, 4) k_vocab_logprob_grad(const Logp
             __syncthreads();      // read before it is written over, where dlogits are the logits
         }
         if (apart) {
-            for (int64_t i = v0 + tid; i < v1; i += kLpThreads) store(i, grad(plain(row, i)));
+            for (int64_t i = v0 + tid; i < v1; i += kLgThreads) store(i, grad(plain(row, i)));
         } else {
 #pragma unroll
             for (int j = 0; j < kWords; ++j) {
-                if (w0 + j * kLpThreads + tid >= w1) break;
+                if (w0 + j * kLgThreads + tid >= w1) break;
                 float f[kVec];
                 unpack<TYPE>(x[j], f);
 #pragma unroll
@@ -486,7 +811,7 @@ __global__ void __launch_bounds__(kLpThreads, 4) k_vocab_logprob_grad(const Logp
                     constexpr bool F16 = TYPE == GK_TYPE_F16;
                     y = make_uint4(pack16<F16>(f[0], f[1]), pack16<F16>(f[2], f[3]), pack16<F16>(f[4], f[5]), pack16<F16>(f[6], f[7]));
                 }
-                __stcs((uint4*)(out + head * kSize) + w0 + j * kLpThreads + tid, y);
+                __stcs((uint4*)(out + head * kSize) + w0 + j * kLgThreads + tid, y);
             }
             if (piece == 0 && tid < head) store(tid, grad(plain(row, tid)));
             const int64_t rest = V - head - words * kVec;
@@ -522,15 +847,19 @@ extern "C" int gk_vocab_logprob(const void* logits, int64_t ld, int32_t dtype, i
     if (k < 0 || k > V || k > kLogprobMaxAlternatives) return GK_ERR_K;
     if (n > 0 && k > 0 && (!idx_out || !val_out)) return GK_ERR_NULL;
     if (n == 0) return GK_OK;
-    const LogprobCall c = {(const char*)logits, ld, n, V, token, m, k, temperature, (float)(1.4426950408889634 / (double)temperature),
-                           logp_out, rank_out, entropy_out, lse_out, idx_out, val_out};
-    cudaStream_t st = (cudaStream_t)stream;
+    const double inv_T = 1.0 / (double)temperature;
+    LogprobCall c = {(const char*)logits, ld, n, V, token, m, k, 1, (float)inv_T, (float)(inv_T - (double)(float)inv_T), (float)(1.4426950408889634 * inv_T),
+                     logp_out, rank_out, entropy_out, lse_out, idx_out, val_out};
+    int dev = 0, sms = 0;
+    GK_CUDA_TRY(cudaGetDevice(&dev));
+    GK_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+    cudaError_t e;
     switch (dtype) {
-        case GK_TYPE_F32: k_vocab_logprob<GK_TYPE_F32><<<(unsigned)n, kLpThreads, 0, st>>>(c); break;
-        case GK_TYPE_BF16: k_vocab_logprob<GK_TYPE_BF16><<<(unsigned)n, kLpThreads, 0, st>>>(c); break;
-        default: k_vocab_logprob<GK_TYPE_F16><<<(unsigned)n, kLpThreads, 0, st>>>(c); break;
+        case GK_TYPE_F32: e = launch_logprob<GK_TYPE_F32>(c, sms, (cudaStream_t)stream); break;
+        case GK_TYPE_BF16: e = launch_logprob<GK_TYPE_BF16>(c, sms, (cudaStream_t)stream); break;
+        default: e = launch_logprob<GK_TYPE_F16>(c, sms, (cudaStream_t)stream); break;
     }
-    GK_CUDA_TRY(cudaGetLastError());
+    if (e != cudaSuccess) return cuda_fail(e);
     note_launch();
     return GK_OK;
 }
@@ -550,16 +879,16 @@ extern "C" int gk_vocab_logprob_grad(const void* logits, int64_t ld, int32_t dty
     if (z0 < d1 && d0 < z1 && (z0 != d0 || (ld != lddz && n > 1))) return GK_ERR_ALIAS;
     const int64_t words = V / (16 / size);
     const double inv_T = 1.0 / (double)temperature;
-    const int64_t pieces = words <= 4 * kLpThreads ? 1 : (words + 4 * kLpThreads - 1) / (4 * kLpThreads);
+    const int64_t pieces = words <= 4 * kLgThreads ? 1 : (words + 4 * kLgThreads - 1) / (4 * kLgThreads);
     const LogprobGradCall c = {(const char*)logits, (char*)dlogits, ld, lddz, n, V, token, m, (int)pieces, (float)inv_T,
                                (float)(inv_T - (double)(float)inv_T), lse, entropy, logp_grad, entropy_grad, lse_grad};
     const int64_t jobs = n * pieces;
     const unsigned grid = (unsigned)(jobs < (1 << 30) ? jobs : 1 << 30);
     cudaStream_t st = (cudaStream_t)stream;
     switch (dtype) {
-        case GK_TYPE_F32: k_vocab_logprob_grad<GK_TYPE_F32><<<grid, kLpThreads, 0, st>>>(c); break;
-        case GK_TYPE_BF16: k_vocab_logprob_grad<GK_TYPE_BF16><<<grid, kLpThreads, 0, st>>>(c); break;
-        default: k_vocab_logprob_grad<GK_TYPE_F16><<<grid, kLpThreads, 0, st>>>(c); break;
+        case GK_TYPE_F32: k_vocab_logprob_grad<GK_TYPE_F32><<<grid, kLgThreads, 0, st>>>(c); break;
+        case GK_TYPE_BF16: k_vocab_logprob_grad<GK_TYPE_BF16><<<grid, kLgThreads, 0, st>>>(c); break;
+        default: k_vocab_logprob_grad<GK_TYPE_F16><<<grid, kLgThreads, 0, st>>>(c); break;
     }
     GK_CUDA_TRY(cudaGetLastError());
     note_launch();
