@@ -21,7 +21,7 @@ constexpr int kLogprobMaxTokens = 128, kLogprobMaxAlternatives = 128;
 constexpr float kLpFloor = -200.f;  // powers of two below this are zero in fp32, and their products with it too
 constexpr int kLpQuad = 4;          // words a thread fetches together, from four places: the first are a sample of the row
 constexpr int kLpParts = 8;         // CTAs a row at most (a cluster)
-constexpr int kLpShort = 4096;      // words of a row that few threads take
+constexpr int kLpShort = 1500, kLpMiddle = 6000;      // words of a row that 64 threads take, and 128
 constexpr float kLpSlack = 4.f;     // how far a logit may be above what the sums are relative to, in powers of two
 // Exponents of maxima up to this are kept to a sixteenth and better by one rounding.
 constexpr float kLpLargest = 1048576.f;
@@ -129,15 +129,15 @@ __device__ __forceinline__ T remote(const T& here, int cta) {
 
 template <int NT>
 struct LpShared {
-    static constexpr int kList = NT == 256 ? 1280 : 512;        // entries of the list of alternatives
-    static constexpr int kNotes = NT == 256 ? 1024 : 384;       // words noted for it, the first with their contents
-    static constexpr int kNoted = NT == 256 ? 512 : 96;
-    static constexpr int kPlaced = NT == 256 ? 256 : 128;       // entries sorted by counting; a longer list is cut first
-    static constexpr int kCtas = NT == 256 ? 4 : 12;            // CTAs an SM
+    static constexpr int kCtas = 1024 / NT;                     // CTAs an SM
+    static constexpr int kList = NT == 256 ? 1280 : NT == 128 ? 1024 : 512;      // entries of the list of alternatives
+    static constexpr int kNotes = kList, kNoted = kList / 5 * 2;                 // words noted for it, the first with their contents
+    static constexpr int kPlaced = NT == 64 ? 128 : 256;        // entries sorted by counting; a longer list is cut first
+    static_assert(NT != 256 || kNoted * sizeof(uint4) >= kLpParts * kLogprobMaxAlternatives * sizeof(uint64_t), "all CTAs' alternatives");
     alignas(16) uint64_t list[kList];      // key of the value above, complement of the index below: all differ
-    uint4 data[kNoted];
+    uint4 data[kNoted];                    // (before that the sample; SPLIT: at last all CTAs' alternatives)
     int note[kNotes];
-    uint64_t best[kLogprobMaxAlternatives], all[kLpParts * kLogprobMaxAlternatives];      // SPLIT: this CTA's alternatives, all CTAs'
+    uint64_t best[kLogprobMaxAlternatives];      // SPLIT: this CTA's
     Sums sums[8];
     int above[8];
     int scratch[2][8];
@@ -371,6 +371,7 @@ __global__ void __launch_bounds__(NT, SPLIT ? 2 : LpShared<NT>::kCtas) k_vocab_l
     };
     uint4 x[kLpQuad], y[kLpQuad];
     fetch(x, 0);
+    fetch(y, 1);
     // the given tokens
     const int64_t token = tid < c.m ? c.token[r * c.m + tid] : -1;
     const bool mine = token >= 0 && token < V;
@@ -399,7 +400,6 @@ __global__ void __launch_bounds__(NT, SPLIT ? 2 : LpShared<NT>::kCtas) k_vocab_l
     const int64_t t0 = c.m > 0 ? c.token[r * c.m] : -1;
     const int first = t0 >= 0 && t0 < V ? (int)t0 : -1;
     const float first_v = first >= 0 ? load_logit<TYPE>(row, first) : 0.f;
-    fetch(y, 1);
 
     // the first words are the sample: their maximum is where the sums start
     float top = quarter > 0 ? max_of<TYPE>(x) : -INFINITY;
@@ -655,19 +655,20 @@ __global__ void __launch_bounds__(NT, SPLIT ? 2 : LpShared<NT>::kCtas) k_vocab_l
         place_all(write);
     } else {
         // all parts' alternatives beside one another, and how many of each part are above each of this CTA's
+        uint64_t* all = reinterpret_cast<uint64_t*>(sh.data);
         for (int j = tid; j < parts * c.k; j += NT) {
             const int p = j / c.k, i = j - p * c.k;
-            sh.all[j] = i < remote(sh.part_count, p) ? remote(sh.best[i], p) : 0;
+            all[j] = i < remote(sh.part_count, p) ? remote(sh.best[i], p) : 0;
         }
         __syncthreads();
         if (tid < k) {
-            const uint64_t e = sh.all[part * c.k + tid];
+            const uint64_t e = all[part * c.k + tid];
             int place = 0;
             for (int p = 0; p < parts; ++p) {
                 int lo = 0, hi = c.k;      // entries that fill up a list are zero, below all
                 while (lo < hi) {
                     const int mid = (lo + hi) >> 1;
-                    if (sh.all[p * c.k + mid] > e) lo = mid + 1; else hi = mid;
+                    if (all[p * c.k + mid] > e) lo = mid + 1; else hi = mid;
                 }
                 place += lo;
             }
@@ -680,8 +681,9 @@ __global__ void __launch_bounds__(NT, SPLIT ? 2 : LpShared<NT>::kCtas) k_vocab_l
 template <int TYPE>
 static cudaError_t launch_logprob(LogprobCall& c, int sms, cudaStream_t st) {
     const int64_t words = c.V / (TYPE == GK_TYPE_F32 ? 4 : 8);
-    // CTAs a row: as many as there is room for, while each still has a word for every thread
-    while (c.parts < kLpParts && c.n * c.parts * 2 <= 4 * sms && words >= 2 * c.parts * 256) c.parts *= 2;
+    // CTAs a row: as many as there is room for, while each still has four words for every thread (64 rows of 32000 bf16,
+    // 2 CTAs a row 14.3 us, 4 16.4, 8 28; one row of 50001 fp32, 8 CTAs 16, one 27)
+    while (c.parts < kLpParts && c.n * c.parts * 2 <= 2 * sms && words >= 8 * c.parts * 256) c.parts *= 2;
     if (c.parts > 1) {
         cudaLaunchConfig_t cfg = {};
         cudaLaunchAttribute attr[1];
@@ -695,7 +697,13 @@ static cudaError_t launch_logprob(LogprobCall& c, int sms, cudaStream_t st) {
         cfg.gridDim = dim3((unsigned)(c.n * c.parts));
         return cudaLaunchKernelEx(&cfg, k_vocab_logprob<TYPE, 256, true>, c);
     }
-    if (words <= kLpShort) k_vocab_logprob<TYPE, 64, false><<<(unsigned)c.n, 64, 0, st>>>(c);
+    // 4096 rows of 10000 bf16 with 10 alternatives: 51 us by 64 threads a row, 59 by 128, 76 by 256; of 32000: 106, 102
+    // and 108; of 128000: 1000, 300 and 280 (few threads' samples are small, and their lists overflow).  Twice the
+    // threads while there is room for them.
+    int threads = words <= kLpShort ? 64 : words <= kLpMiddle ? 128 : 256;
+    while (threads < 256 && c.n * threads * 2 <= 1024ll * sms && words >= 4 * threads) threads *= 2;
+    if (threads == 64) k_vocab_logprob<TYPE, 64, false><<<(unsigned)c.n, 64, 0, st>>>(c);
+    else if (threads == 128) k_vocab_logprob<TYPE, 128, false><<<(unsigned)c.n, 128, 0, st>>>(c);
     else k_vocab_logprob<TYPE, 256, false><<<(unsigned)c.n, 256, 0, st>>>(c);
     return cudaGetLastError();
 }
