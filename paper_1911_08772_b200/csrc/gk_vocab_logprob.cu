@@ -287,6 +287,10 @@ __device__ __forceinline__ Sums lp_join_warps(const Sums (&part)[8], float zscal
         b.s1 = __shfl_xor_sync(0xffffffffu, a.s1, o);
         lp_join(a, b, zscale);
     }
+    // (a join's last bit depends on which comes first: all take the first lane's)
+    a.m = __shfl_sync(0xffffffffu, a.m, 0);
+    a.s0 = __shfl_sync(0xffffffffu, a.s0, 0);
+    a.s1 = __shfl_sync(0xffffffffu, a.s1, 0);
     return a;
 }
 __device__ __forceinline__ void lp_join_lanes(Sums& a) {
