@@ -717,7 +717,7 @@ struct LogprobGradCall {
     char* dz;
     int64_t ld, lddz, n, V;
     const int64_t* token;
-    int m, pieces;
+    int m;
     float inv_T, inv_T_low;      // 1 / T in two parts
     const float* lse;
     const float* entropy;
@@ -725,37 +725,38 @@ struct LogprobGradCall {
     const float* b;
     const float* c;
 };
-
 constexpr int kLgThreads = 256;
 
-// A CTA a piece of a row of at most kWords words a thread, the logits read and their gradients written once.
+// A CTA a piece of a row (grid: pieces by rows), logits read and gradients written once, four words a thread at a time
+// and four on their way.
 //     dz = p (k0 + k1 log p),  k0 = (c - sum a - b entropy) / T,  k1 = -b / T,
 // and a / T more at a token, which the CTA that has it writes again at the end.
 template <int TYPE>
 __global__ void __launch_bounds__(kLgThreads, 4) k_vocab_logprob_grad(const LogprobGradCall c) {
     constexpr int kVec = TYPE == GK_TYPE_F32 ? 4 : 8, kSize = TYPE == GK_TYPE_F32 ? 4 : 2, kWords = 4;
+    constexpr float kLowest = TYPE == GK_TYPE_F32 ? -3.402823466e38f : TYPE == GK_TYPE_BF16 ? -3.3895313892515355e38f : -65504.f;
     __shared__ int64_t tokens[kLogprobMaxTokens];
     const int tid = threadIdx.x, lane = tid & 31;
-    const int64_t V = c.V;
-    for (int64_t job = blockIdx.x; job < c.n * c.pieces; job += gridDim.x) {
-        const int64_t r = job / c.pieces;
-        const int piece = (int)(job - r * c.pieces);
+    const int V = (int)c.V;
+    for (int64_t r = blockIdx.y; r < c.n; r += gridDim.y) {
         const char* row = c.logits + r * c.ld * kSize;
         char* out = c.dz + r * c.lddz * kSize;
         // the piece's elements [v0, v1); words where both rows have the same 16-byte boundaries
         const bool apart = (((uintptr_t)row ^ (uintptr_t)out) & 15) != 0;
-        int64_t head = (16 - ((uintptr_t)row & 15)) % 16 / kSize;
-        if (head > V) head = V;
-        const int64_t words = (V - head) / kVec;
-        const int64_t w0 = words * piece / c.pieces, w1 = words * (piece + 1) / c.pieces;
-        const int64_t v0 = piece == 0 ? 0 : head + w0 * kVec, v1 = piece == c.pieces - 1 ? V : head + w1 * kVec;
-        uint4 x[kWords];
-        if (!apart) {
+        const int head = min((int)((16 - ((uintptr_t)row & 15)) % 16) / kSize, V), all = (V - head) / kVec;
+        const int w0 = (int)((int64_t)all * blockIdx.x / gridDim.x), words = (int)((int64_t)all * (blockIdx.x + 1) / gridDim.x) - w0;
+        const int v0 = blockIdx.x == 0 ? 0 : head + w0 * kVec, v1 = blockIdx.x == gridDim.x - 1 ? V : head + (w0 + words) * kVec;
+        const uint4* from = (const uint4*)(row + head * kSize) + w0 + tid;
+        uint4* to = (uint4*)(out + head * kSize) + w0 + tid;
+        uint4 x[kWords], y[kWords];
+        auto fetch = [&](uint4 (&x)[kWords], int w) {
+            if (apart) return;
 #pragma unroll
             for (int j = 0; j < kWords; ++j)
-                if (w0 + j * kLgThreads + tid < w1) x[j] = __ldcs((const uint4*)(row + head * kSize) + w0 + j * kLgThreads + tid);
-        }
-        const float lse = c.lse[r], b = c.b ? c.b[r] : 0.f;
+                if (w + j * kLgThreads + tid < words) x[j] = __ldcs(from + w + j * kLgThreads);
+        };
+        fetch(x, 0);
+        const float lse = c.lse[r], b = c.b ? c.b[r] : 0.f, entropy = c.b ? c.entropy[r] : 0.f;
         float k0 = c.c ? c.c[r] : 0.f;
         bool counts = c.m == 0, here = false;
         float sum = 0.f;
@@ -767,27 +768,38 @@ __global__ void __launch_bounds__(kLgThreads, 4) k_vocab_logprob_grad(const Logp
             if (valid && c.a) sum += c.a[r * c.m + j0 + lane];
             if (tid < 32 && j0 + lane < c.m) tokens[j0 + lane] = t;
         }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        counts = counts && !(lse < -1e30f);      // else nothing is left, or masks of a type's lowest value alone
-        k0 = (k0 - sum - (c.b ? b * c.entropy[r] : 0.f)) * c.inv_T;
-        const float k1 = -b * c.inv_T;
-        auto plain = [&](const char* p, int64_t i) {
-            if constexpr (TYPE == GK_TYPE_F32) return ((const float*)p)[i];
-            else return from16<TYPE == GK_TYPE_F16>(((const uint16_t*)p)[i]);
-        };
+        fetch(y, kWords * kLgThreads);
         auto store = [&](int64_t i, float v) {
             if constexpr (TYPE == GK_TYPE_F32) ((float*)out)[i] = v;
             else ((uint16_t*)out)[i] = to16<TYPE == GK_TYPE_F16>(v);
         };
+        counts = counts && !(lse < -1e30f);      // else nothing is left, or masks of a type's lowest value alone
+        if (!counts) {
+            if (apart) {
+                for (int i = v0 + tid; i < v1; i += kLgThreads) store(i, 0.f);
+                continue;
+            }
+            for (int w = tid; w < words; w += kLgThreads) __stcs(to + w - tid, make_uint4(0, 0, 0, 0));
+            if (tid < head - v0) store(v0 + tid, 0.f);
+            if (head + (w0 + words) * kVec + tid < v1) store(head + (w0 + words) * kVec + tid, 0.f);
+            continue;
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        k0 = (k0 - sum - b * entropy) * c.inv_T;
+        const float k1 = -b * c.inv_T;
+        auto plain = [&](int64_t i) {
+            if constexpr (TYPE == GK_TYPE_F32) return ((const float*)row)[i];
+            else return from16<TYPE == GK_TYPE_F16>(((const uint16_t*)row)[i]);
+        };
         // (a logit of -inf has a finite stand-in, and so has its log probability: both go into products with zero)
         auto grad = [&](float z) {
-            z = max_nan(z, -3.402823466e38f);
-            const float y = max_nan(fmaf(z, c.inv_T_low, fmaf(z, c.inv_T, -lse)), -1e30f);
-            return counts ? exp2_fast(y * 1.44269504f) * fmaf(k1, y, k0) : 0.f;
+            z = max_nan(z, kLowest);
+            const float d = max_nan(fmaf(z, c.inv_T_low, fmaf(z, c.inv_T, -lse)), -1e30f);
+            return exp2_fast(d * 1.44269504f) * fmaf(k1, d, k0);
         };
-        here = here && counts && c.a;
-        // a token's gradients are added up by the first of the threads that have it
+        // A token's gradients are added up by the first of the threads that have it.
+        here = here && c.a;
         float at_token = 0.f;
         int64_t t = -1;
         if (here) {
@@ -801,33 +813,72 @@ __global__ void __launch_bounds__(kLgThreads, 4) k_vocab_logprob_grad(const Logp
                     float more = 0.f;
                     for (int j = tid; j < c.m; ++j)
                         if (tokens[j] == t) more += c.a[r * c.m + j];
-                    at_token = fmaf(more, c.inv_T, grad(plain(row, t)));
+                    at_token = fmaf(more, c.inv_T, grad(plain(t)));
                 }
             }
             __syncthreads();      // read before it is written over, where dlogits are the logits
         }
         if (apart) {
-            for (int64_t i = v0 + tid; i < v1; i += kLgThreads) store(i, grad(plain(row, i)));
+            for (int i = v0 + tid; i < v1; i += kLgThreads) store(i, grad(plain(i)));
         } else {
-#pragma unroll
-            for (int j = 0; j < kWords; ++j) {
-                if (w0 + j * kLgThreads + tid >= w1) break;
+            // One bound takes the place of all logits below it, -inf among them, where their probabilities are zero in fp32
+            // and the bound's is too: 200 nats below the log-sum-exp, with room for its own rounding to 16 bits.  Where no
+            // such value exists (fp16 at temperatures of hundreds), element by element.
+            const float bound = fmaxf(fmaf(-fabsf(lse), 0.0078125f, lse - 200.f) / c.inv_T, kLowest);
+            const bool paired = fmaf(bound, c.inv_T, -lse) <= -110.f;
+            const unsigned bound2 = threshold_of<TYPE>(bound, false);
+            const uint64_t hi = pair(c.inv_T, c.inv_T), lo = pair(c.inv_T_low, c.inv_T_low), less = pair(-lse, -lse),
+                           log2e = pair(1.44269504f, 1.44269504f), a0 = pair(k0, k0), a1 = pair(k1, k1);
+            auto word = [&](const uint4& x) {
                 float f[kVec];
-                unpack<TYPE>(x[j], f);
+                if (paired) {
+                    if constexpr (TYPE == GK_TYPE_F32) {
+                        unpack<TYPE>(x, f);
 #pragma unroll
-                for (int e = 0; e < kVec; ++e) f[e] = grad(f[e]);
-                uint4 y;
+                        for (int e = 0; e < kVec; ++e) f[e] = max_nan(f[e], bound);
+                    } else {
+                        unpack<TYPE>(make_uint4(max2_nan<TYPE>(x.x, bound2), max2_nan<TYPE>(x.y, bound2), max2_nan<TYPE>(x.z, bound2), max2_nan<TYPE>(x.w, bound2)), f);
+                    }
+#pragma unroll
+                    for (int e = 0; e < kVec; e += 2) {
+                        const uint64_t z = pair(f[e], f[e + 1]), d = fma2(z, lo, fma2(z, hi, less));
+                        float d0, d1;
+                        unpair(mul2(d, log2e), d0, d1);
+                        unpair(mul2(pair(exp2_fast(d0), exp2_fast(d1)), fma2(a1, d, a0)), f[e], f[e + 1]);
+                    }
+                } else {
+                    unpack<TYPE>(x, f);
+#pragma unroll 1
+                    for (int e = 0; e < kVec; ++e) {
+                        const float g = grad(f[0]);      // (turned round, so that the code is there once)
+#pragma unroll
+                        for (int i = 0; i + 1 < kVec; ++i) f[i] = f[i + 1];
+                        f[kVec - 1] = g;
+                    }
+                }
                 if constexpr (TYPE == GK_TYPE_F32) {
-                    y = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+                    return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
                 } else {
                     constexpr bool F16 = TYPE == GK_TYPE_F16;
-                    y = make_uint4(pack16<F16>(f[0], f[1]), pack16<F16>(f[2], f[3]), pack16<F16>(f[4], f[5]), pack16<F16>(f[6], f[7]));
+                    return make_uint4(pack16<F16>(f[0], f[1]), pack16<F16>(f[2], f[3]), pack16<F16>(f[4], f[5]), pack16<F16>(f[6], f[7]));
                 }
-                __stcs((uint4*)(out + head * kSize) + w0 + j * kLgThreads + tid, y);
+            };
+            auto words_of = [&](const uint4 (&x)[kWords], int w) {
+#pragma unroll
+                for (int j = 0; j < kWords; ++j)
+                    if (w + j * kLgThreads + tid < words) __stcs(to + w + j * kLgThreads, word(x[j]));
+            };
+            constexpr int kStep = kWords * kLgThreads;
+#pragma unroll 1
+            for (int w = 0; w < words; w += 2 * kStep) {
+                words_of(x, w);
+                fetch(x, w + 2 * kStep);
+                words_of(y, w + kStep);
+                fetch(y, w + 3 * kStep);
             }
-            if (piece == 0 && tid < head) store(tid, grad(plain(row, tid)));
-            const int64_t rest = V - head - words * kVec;
-            if (piece == c.pieces - 1 && tid < rest) store(V - rest + tid, grad(plain(row, V - rest + tid)));
+            if (tid < head - v0) store(v0 + tid, grad(plain(v0 + tid)));
+            const int behind = head + (w0 + words) * kVec + tid;
+            if (behind < v1) store(behind, grad(plain(behind)));
         }
         if (here) {
             __syncthreads();
@@ -889,13 +940,18 @@ extern "C" int gk_vocab_logprob_grad(const void* logits, int64_t ld, int32_t dty
     if (n == 0) return GK_OK;
     const uintptr_t z0 = (uintptr_t)logits, z1 = z0 + ((n - 1) * ld + V) * size, d0 = (uintptr_t)dlogits, d1 = d0 + ((n - 1) * lddz + V) * size;
     if (z0 < d1 && d0 < z1 && (z0 != d0 || (ld != lddz && n > 1))) return GK_ERR_ALIAS;
+    int dev = 0, sms = 0;
+    GK_CUDA_TRY(cudaGetDevice(&dev));
+    GK_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+    // sixteen words a thread, fewer where there are not enough CTAs
     const int64_t words = V / (16 / size);
+    int64_t pieces = (words + 16 * kLgThreads - 1) / (16 * kLgThreads);
+    if (pieces < 1) pieces = 1;
+    while (n * pieces < 4 * sms && words > 2 * kLgThreads * pieces) pieces *= 2;
     const double inv_T = 1.0 / (double)temperature;
-    const int64_t pieces = words <= 4 * kLgThreads ? 1 : (words + 4 * kLgThreads - 1) / (4 * kLgThreads);
-    const LogprobGradCall c = {(const char*)logits, (char*)dlogits, ld, lddz, n, V, token, m, (int)pieces, (float)inv_T,
+    const LogprobGradCall c = {(const char*)logits, (char*)dlogits, ld, lddz, n, V, token, m, (float)inv_T,
                                (float)(inv_T - (double)(float)inv_T), lse, entropy, logp_grad, entropy_grad, lse_grad};
-    const int64_t jobs = n * pieces;
-    const unsigned grid = (unsigned)(jobs < (1 << 30) ? jobs : 1 << 30);
+    const dim3 grid((unsigned)pieces, (unsigned)(n < 65535 ? n : 65535));
     cudaStream_t st = (cudaStream_t)stream;
     switch (dtype) {
         case GK_TYPE_F32: k_vocab_logprob_grad<GK_TYPE_F32><<<grid, kLgThreads, 0, st>>>(c); break;
