@@ -22,6 +22,7 @@ namespace gk {
 
 constexpr int kGradThreads = 512, kGradWarps = kGradThreads / 32;
 constexpr int kGradUnit = 16384;          // bytes of source in a unit
+constexpr int kGradParts = 32;            // sums of spans kept before they are joined
 
 struct GradRec {
     const void* src;
@@ -32,7 +33,7 @@ struct GradRec {
 };
 // The table travels as a kernel argument where it fits (a captured call then needs nothing of the host),
 // else kernels with a part of it as their argument write it to the workspace first.
-constexpr int kGradFew = 64, kGradMany = 1000;
+constexpr int kGradFew = 128, kGradSome = 512, kGradMany = 1000;
 template <int CAP>
 struct GradTable {
     GradRec rec[CAP];
@@ -79,23 +80,37 @@ __device__ __forceinline__ void store_elem(char* p, int64_t i, float v) {
     else ((uint16_t*)p)[i] = to16<TYPE == GK_TYPE_F16>(v);
 }
 
-// Sum of the squares of n elements at p, this thread's part of it.
 template <int TYPE>
-__device__ __forceinline__ double squares(const char* p, int64_t n) {
-    constexpr int kVec = Elem<TYPE>::vec, kSize = Elem<TYPE>::size, kWords = 4;
-    const int tid = threadIdx.x;
+__device__ __noinline__ double squares64(uint4 a, uint4 b, uint4 c, uint4 d) {
+    double acc = 0.0;
+#pragma unroll 1
+    for (int j = 0; j < 4; ++j) {
+        float f[Elem<TYPE>::vec];
+        unpack<TYPE>(a, f);
+        a = b;
+        b = c;
+        c = d;
+#pragma unroll
+        for (int e = 0; e < Elem<TYPE>::vec; ++e) acc = fma((double)f[e], (double)f[e], acc);
+    }
+    return acc;
+}
+
+// Sum of the squares of n elements at p, the part of thread tid of G.
+template <int TYPE, int G>
+__device__ __forceinline__ double squares(const char* p, int64_t n, int tid) {
+    constexpr int kVec = Elem<TYPE>::vec, kSize = Elem<TYPE>::size, kWords = 8;
     int64_t head = (16 - ((uintptr_t)p & 15)) % 16 / kSize;
     if (head > n) head = n;
     const int64_t words = (n - head) / kVec;
-    const uint4* body = (const uint4*)(p + head * kSize);
+    const uint4* own = (const uint4*)(p + head * kSize) + tid;
     double acc = 0.0;
 #pragma unroll 1
-    for (int64_t w0 = 0; w0 < words; w0 += kWords * kGradThreads) {
-        const int left = (int)(words - w0 < kWords * kGradThreads ? words - w0 : kWords * kGradThreads) - tid;
-        const uint4* own = body + w0 + tid;
+    for (int64_t w0 = 0; w0 < words; w0 += kWords * G) {
+        const int left = (int)(words - w0 < kWords * G ? words - w0 : kWords * G) - tid;
         uint4 x[kWords];
 #pragma unroll
-        for (int j = 0; j < kWords; ++j) x[j] = j * kGradThreads < left ? own[j * kGradThreads] : make_uint4(0, 0, 0, 0);
+        for (int j = 0; j < kWords; ++j) x[j] = j * G < left ? own[w0 + j * G] : make_uint4(0, 0, 0, 0);
         float s = 0.f, t = 0.f;
 #pragma unroll
         for (int j = 0; j < kWords; ++j) {
@@ -112,12 +127,7 @@ __device__ __forceinline__ double squares(const char* p, int64_t n) {
             acc += (double)s;
         } else {
 #pragma unroll
-            for (int j = 0; j < kWords; ++j) {
-                float f[kVec];
-                unpack<TYPE>(x[j], f);
-#pragma unroll
-                for (int e = 0; e < kVec; ++e) acc = fma((double)f[e], (double)f[e], acc);
-            }
+            for (int j = 0; j < kWords; j += 4) acc += squares64<TYPE>(x[j], x[j + 1], x[j + 2], x[j + 3]);
         }
     }
     // before the first 16-byte boundary and after the last
@@ -132,86 +142,98 @@ __device__ __forceinline__ double squares(const char* p, int64_t n) {
     }
     return acc;
 }
-__device__ __forceinline__ double squares(int type, const char* p, int64_t n) {
+template <int G>
+__device__ __noinline__ double squares(int type, const char* p, int64_t n, int tid) {
     switch (type) {
-        case GK_TYPE_F32: return squares<GK_TYPE_F32>(p, n);
-        case GK_TYPE_BF16: return squares<GK_TYPE_BF16>(p, n);
-        default: return squares<GK_TYPE_F16>(p, n);
+        case GK_TYPE_F32: return squares<GK_TYPE_F32, G>(p, n, tid);
+        case GK_TYPE_BF16: return squares<GK_TYPE_BF16, G>(p, n, tid);
+        default: return squares<GK_TYPE_F16, G>(p, n, tid);
     }
 }
 
-// dst = c src, n elements, from the last to the first.
-template <int SRC, int DST>
-__device__ __noinline__ void scaled(const char* src, char* dst, int64_t n, float c) {
-    constexpr int kS = Elem<SRC>::size, kD = Elem<DST>::size;
-    const int tid = threadIdx.x;
-    // elements before the first one that starts 16 bytes on both sides, where there is one
-    int head = -1;
+// The eight elements that begin `off` of a 16-byte word's elements into w.
+template <int TYPE, int W>
+__device__ __forceinline__ void shifted(unsigned (&w)[W], int off, float (&f)[8]) {
+    if constexpr (TYPE == GK_TYPE_F32) {
 #pragma unroll
-    for (int h = 7; h >= 0; --h)
-        if ((((uintptr_t)src + h * kS) & 15) == 0 && (((uintptr_t)dst + h * kD) & 15) == 0) head = h;
-    // (a step's places are offsets from its first, so that their addresses take no registers)
-    if (head < 0) {
-        constexpr int kEach = 8, kStep = kEach * kGradThreads;
-#pragma unroll 1
-        for (int64_t i0 = (n - 1) / kStep * kStep; i0 >= 0; i0 -= kStep) {
-            const int left = (int)(n - i0 < kStep ? n - i0 : kStep) - tid;
-            const char* s = src + (i0 + tid) * kS;
-            char* d = dst + (i0 + tid) * kD;
-            float f[kEach];
+        for (int i = 0; i + 1 < W; ++i) w[i] = off & 1 ? w[i + 1] : w[i];
 #pragma unroll
-            for (int j = 0; j < kEach; ++j)
-                if (j * kGradThreads < left) f[j] = load_elem<SRC>(s, j * kGradThreads);
+        for (int i = 0; i + 2 < W; ++i) w[i] = off & 2 ? w[i + 2] : w[i];
 #pragma unroll
-            for (int j = 0; j < kEach; ++j)
-                if (j * kGradThreads < left) store_elem<DST>(d, j * kGradThreads, c * f[j]);
-        }
-        return;
+        for (int e = 0; e < 8; ++e) f[e] = __uint_as_float(w[e]);
+    } else {
+#pragma unroll
+        for (int i = 0; i + 2 < W; ++i) w[i] = off & 4 ? w[i + 2] : w[i];
+#pragma unroll
+        for (int i = 0; i + 1 < W; ++i) w[i] = off & 2 ? w[i + 1] : w[i];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = off & 1 ? __funnelshift_r(w[i], w[i + 1], 16) : w[i];
+        unpack<TYPE>(make_uint4(w[0], w[1], w[2], w[3]), f);
     }
-    if (head > n) head = (int)n;
-    const int64_t words = (n - head) / 8;      // of eight elements
-    constexpr int kWords = 2, kStep = kWords * kGradThreads;
+}
+
+// dst = c src, n elements, from the last to the first, by thread tid of G.  A thread has eight elements at a time that begin on a boundary
+// of 32 bytes (fp32) or 16 in dst; where they lie otherwise in src, they are cut out of the 16-byte words around them.
+template <int SRC, int DST, int G>
+__device__ __forceinline__ void scaled(const char* src, char* dst, int64_t n, float c, int tid) {
+    constexpr int kS = Elem<SRC>::size, kD = Elem<DST>::size, kEach = SRC == GK_TYPE_F32 ? 2 : 4;
+    constexpr int kLoads = SRC == GK_TYPE_F32 ? 3 : 2;      // words around eight elements
+    // elements before the first boundary; eight more where the first words would begin before src
+    int64_t head = (8 * kD - (int)((uintptr_t)dst & (8 * kD - 1))) % (8 * kD) / kD;
+    const int off = (int)(((uintptr_t)src + head * kS) & 15) / kS;
+    if (off > head) head += 8;
+    // and no words end behind src
+    const int64_t room = n - head + off - (off ? kLoads : kLoads - 1) * (16 / kS);
+    int64_t groups = room < 0 ? 0 : room / 8 + 1;
+    if (groups == 0) head = 0;
+    const uint4* s = (const uint4*)(src + (head - off) * kS) + tid * (kS / 2);
+    char* d = dst + (head + tid * 8) * kD;
+    constexpr int kStep = kEach * G;
 #pragma unroll 1
-    for (int64_t w0 = (words - 1) / kStep * kStep; w0 >= 0; w0 -= kStep) {
-        const int left = (int)(words - w0 < kStep ? words - w0 : kStep) - tid;
-        const uint4* s = (const uint4*)(src + head * kS) + (w0 + tid) * (kS / 2);
-        uint4* d = (uint4*)(dst + head * kD) + (w0 + tid) * (kD / 2);
-        uint4 x[kWords][kS / 2];
+    for (int64_t g0 = (groups - 1) / kStep * kStep; groups > 0 && g0 >= 0; g0 -= kStep) {
+        const int left = (int)(groups - g0 < kStep ? groups - g0 : kStep) - tid;
+        const uint4* from = s + g0 * (kS / 2);
+        char* to = d + g0 * 8 * kD;
+        uint4 x[kEach][kLoads];
 #pragma unroll
-        for (int j = 0; j < kWords; ++j)
+        for (int j = 0; j < kEach; ++j)
 #pragma unroll
-            for (int e = 0; e < kS / 2; ++e)
-                if (j * kGradThreads < left) x[j][e] = s[j * kGradThreads * (kS / 2) + e];
+            for (int i = 0; i < kLoads; ++i)
+                x[j][i] = j * G < left && (i + 1 < kLoads || off) ? from[j * G * (kS / 2) + i] : make_uint4(0, 0, 0, 0);
 #pragma unroll
-        for (int j = 0; j < kWords; ++j) {
-            if (j * kGradThreads >= left) break;
+        for (int j = 0; j < kEach; ++j) {
+            if (j * G >= left) break;
+            unsigned w[kLoads * 4];
             float f[8];
 #pragma unroll
-            for (int e = 0; e < kS / 2; ++e) {
-                float g[Elem<SRC>::vec];
-                unpack<SRC>(x[j][e], g);
-#pragma unroll
-                for (int a = 0; a < Elem<SRC>::vec; ++a) f[e * Elem<SRC>::vec + a] = c * g[a];
+            for (int i = 0; i < kLoads; ++i) {
+                w[4 * i] = x[j][i].x;
+                w[4 * i + 1] = x[j][i].y;
+                w[4 * i + 2] = x[j][i].z;
+                w[4 * i + 3] = x[j][i].w;
             }
-            uint4* to = d + j * kGradThreads * (kD / 2);
+            shifted<SRC>(w, off, f);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[e] *= c;
             if constexpr (DST == GK_TYPE_F32) {
-                ((float4*)to)[0] = make_float4(f[0], f[1], f[2], f[3]);
-                ((float4*)to)[1] = make_float4(f[4], f[5], f[6], f[7]);
+                float4* at = (float4*)(to + (int64_t)j * G * 32);
+                at[0] = make_float4(f[0], f[1], f[2], f[3]);
+                at[1] = make_float4(f[4], f[5], f[6], f[7]);
             } else {
                 constexpr bool F16 = DST == GK_TYPE_F16;
-                to[0] = make_uint4(pack16<F16>(f[0], f[1]), pack16<F16>(f[2], f[3]), pack16<F16>(f[4], f[5]), pack16<F16>(f[6], f[7]));
+                *(uint4*)(to + (int64_t)j * G * 16) = make_uint4(pack16<F16>(f[0], f[1]), pack16<F16>(f[2], f[3]), pack16<F16>(f[4], f[5]), pack16<F16>(f[6], f[7]));
             }
         }
     }
-    const int64_t tail = n - head - words * 8;
-    if (tid < head) store_elem<DST>(dst, tid, c * load_elem<SRC>(src, tid));
-    if (tid < tail) store_elem<DST>(dst, n - tail + tid, c * load_elem<SRC>(src, n - tail + tid));
+    for (int64_t i = tid; i < head; i += G) store_elem<DST>(dst, i, c * load_elem<SRC>(src, i));
+    for (int64_t i = head + groups * 8 + tid; i < n; i += G) store_elem<DST>(dst, i, c * load_elem<SRC>(src, i));
 }
-__device__ __forceinline__ void scaled(unsigned types, const char* src, char* dst, int64_t n, float c) {
+template <int G>
+__device__ __noinline__ void scaled(unsigned types, const char* src, char* dst, int64_t n, float c, int tid) {
     switch (types) {
-#define GK_PAIR(S, D) case (S | D << 8): scaled<S, D>(src, dst, n, c); break;
+#define GK_PAIR(S, D) case (S | D << 8): scaled<S, D, G>(src, dst, n, c, tid); break;
         GK_PAIR(0, 0) GK_PAIR(0, 1) GK_PAIR(0, 2) GK_PAIR(1, 0) GK_PAIR(1, 1) GK_PAIR(1, 2) GK_PAIR(2, 0) GK_PAIR(2, 1)
-        default: scaled<2, 2>(src, dst, n, c); break;
+        default: scaled<2, 2, G>(src, dst, n, c, tid); break;
 #undef GK_PAIR
     }
 }
@@ -243,16 +265,30 @@ __device__ __forceinline__ double total_norm(const double* cta_sums, unsigned G,
 }
 
 template <bool CLIP, int CAP>
-__global__ void __launch_bounds__(kGradThreads, 2) k_grad(const GradCall c, const __grid_constant__ GradTable<CAP> table) {
+__global__ void __launch_bounds__(kGradThreads, 1) k_grad(const GradCall c, const __grid_constant__ GradTable<CAP> table) {
     __shared__ double smem[kGradWarps];
+    __shared__ double part[kGradParts][kGradWarps];      // the warps' sums of spans that all take, and whose they are
+    __shared__ int part_of[kGradParts];
     __shared__ int flag;
     const GradRec* rec = c.table ? c.table : table.rec;
     const unsigned G = gridDim.x, b = blockIdx.x;
     const unsigned u0 = unit_of(c.units, b, G), u1 = unit_of(c.units, b + 1, G);
-    const int tid = threadIdx.x;
+    const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
     int last = -1;      // the tensor that the stretch ends in
     if (!CLIP || !c.norm_in) {
+        const bool each = !CLIP && c.norms_out;
         double all = 0.0;
+        int little = 0, parts = 0;
+        auto join_parts = [&]() {
+            __syncthreads();
+            if (tid < parts) {
+                double v = 0.0;
+#pragma unroll
+                for (int w = 0; w < kGradWarps; ++w) v += part[tid][w];
+                c.span_sums[part_of[tid] + b] = v;
+            }
+            parts = 0;
+        };
         if (u0 < u1)
             for (int i = tensor_of(rec, c.T, u0); i < c.T && rec[i].first < u1; ++i) {
                 const GradRec r = rec[i];
@@ -260,18 +296,38 @@ __global__ void __launch_bounds__(kGradThreads, 2) k_grad(const GradCall c, cons
                 span_of(r, u0, u1, from, to);
                 if (from >= to) continue;
                 last = i;
-                const double v = squares((int)(r.types & 255u), (const char*)r.src + from * ((r.types & 255u) == GK_TYPE_F32 ? 4 : 2), to - from);
-                if (!CLIP && c.norms_out) {
-                    const double sum = block_total(v, smem);
-                    if (tid == 0) c.span_sums[i + b] = sum;
+                const int type = (int)(r.types & 255u), size = type == GK_TYPE_F32 ? 4 : 2;
+                const char* p = (const char*)r.src + from * size;
+                // a span of a unit or less is one warp's, the next such the next one's
+                if ((to - from) * size <= kGradUnit) {
+                    if (little++ % kGradWarps != wid) continue;
+                    double v = squares<32>(type, p, to - from, lane);
+                    all += v;
+                    if (each) {
+                        v = warp_sum(v);
+                        if (lane == 0) c.span_sums[i + b] = v;
+                    }
+                } else {
+                    double v = squares<kGradThreads>(type, p, to - from, tid);
+                    all += v;
+                    if (each) {
+                        v = warp_sum(v);
+                        if (lane == 0) part[parts][wid] = v;
+                        if (tid == 0) part_of[parts] = i;
+                        if (++parts == kGradParts) {
+                            join_parts();
+                            __syncthreads();
+                        }
+                    }
                 }
-                all += v;
             }
+        if (each) join_parts();
         all = block_total(all, smem);
         if (tid == 0) c.cta_sums[b] = all;
     }
     if constexpr (!CLIP) {
         // the CTA that is done last joins the sums
+        __syncthreads();
         if (tid == 0) {
             __threadfence();
             flag = atomicInc(&c.ctl->done, G - 1) == G - 1;
@@ -281,20 +337,35 @@ __global__ void __launch_bounds__(kGradThreads, 2) k_grad(const GradCall c, cons
         if (!flag) return;
         const double norm = total_norm(c.cta_sums, G, smem);
         if (tid == 0) c.norm_out[0] = (float)norm;
-        if (c.norms_out)
-            for (int i0 = 0; i0 < c.T; i0 += kGradThreads / 8) {
-                // eight lanes a tensor: its spans are those of the CTAs from its first unit's to its last's
-                const int i = i0 + tid / 8;
-                double v = 0.0;
-                if (i < c.T && rec[i].n > 0) {
-                    const unsigned f = rec[i].first, l = i + 1 < c.T ? rec[i + 1].first - 1 : c.units - 1;
-                    const unsigned b0 = (unsigned)((((uint64_t)f + 1) * G - 1) / c.units), b1 = (unsigned)((((uint64_t)l + 1) * G - 1) / c.units);
-                    for (unsigned a = b0 + tid % 8; a <= b1; a += 8) v += __ldcg(&c.span_sums[i + a]);
-                }
+        if (!c.norms_out) return;
+        // a tensor's spans are those of the CTAs from its first unit's to its last's: up to eight by a thread, more by a warp
+        auto spans_of = [&](int i, unsigned& b0, unsigned& b1) {
+            const unsigned f = rec[i].first, l = i + 1 < c.T ? rec[i + 1].first - 1 : c.units - 1;
+            b0 = (unsigned)((((uint64_t)f + 1) * G - 1) / c.units);
+            b1 = (unsigned)((((uint64_t)l + 1) * G - 1) / c.units);
+        };
+        for (int i0 = 0; i0 < c.T; i0 += kGradThreads) {
+            const int i = i0 + tid;
+            unsigned b0 = 1, b1 = 0;
+            if (i < c.T && rec[i].n > 0) spans_of(i, b0, b1);
+            const bool lengthy = b1 >= b0 + 8 && b0 <= b1;
+            if (i < c.T && !lengthy) {
+                double v[8], sum = 0.0;
 #pragma unroll
-                for (int o = 4; o > 0; o >>= 1) v += __shfl_down_sync(0xffffffffu, v, o, 8);
-                if (i < c.T && tid % 8 == 0) c.norms_out[i] = (float)sqrt(v);
+                for (unsigned j = 0; j < 8; ++j) v[j] = b0 + j <= b1 ? __ldcg(&c.span_sums[i + b0 + j]) : 0.0;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) sum += v[j];
+                c.norms_out[i] = (float)sqrt(sum);
             }
+            for (unsigned more = __ballot_sync(0xffffffffu, lengthy); more; more &= more - 1) {
+                const int l = __ffs(more) - 1, t = i0 + wid * 32 + l;
+                const unsigned from = __shfl_sync(0xffffffffu, b0, l), to = __shfl_sync(0xffffffffu, b1, l);
+                double v = 0.0;
+                for (unsigned a = from + lane; a <= to; a += 32) v += __ldcg(&c.span_sums[t + a]);
+                v = warp_sum(v);
+                if (lane == 0) c.norms_out[t] = (float)sqrt(v);
+            }
+        }
     } else {
         const float scale = c.scale ? *c.scale : 1.f;
         double norm;
@@ -326,13 +397,17 @@ __global__ void __launch_bounds__(kGradThreads, 2) k_grad(const GradCall c, cons
         }
         if (u0 >= u1) return;
         if (last < 0) last = tensor_of(rec, c.T, u1 - 1);
+        int little = 0;
         for (int i = last; i >= 0; --i) {
             const GradRec r = rec[i];
             if (r.n > 0 && !(by == 1.f && r.src == r.dst)) {
                 int64_t from, to;
                 span_of(r, u0, u1, from, to);
                 const int64_t s = (r.types & 255u) == GK_TYPE_F32 ? 4 : 2, d = r.types >> 8 == GK_TYPE_F32 ? 4 : 2;
-                scaled(r.types, (const char*)r.src + from * s, (char*)r.dst + from * d, to - from, by);
+                const char* p = (const char*)r.src + from * s;
+                char* q = (char*)r.dst + from * d;
+                if ((to - from) * s > kGradUnit) scaled<kGradThreads>(r.types, p, q, to - from, by, tid);
+                else if (little++ % kGradWarps == wid) scaled<32>(r.types, p, q, to - from, by, lane);
             }
             if (r.first <= u0) break;
         }
@@ -452,28 +527,34 @@ static int enqueue_grad(GradCall& c, const void* const* grads, const int32_t* ty
         r.types = (unsigned)types[i] | (CLIP ? (unsigned)out_types[i] << 8 : 0u);
         units += (unsigned)(((uint64_t)sizes[i] * type_size(types[i]) + kGradUnit - 1) / kGradUnit);
     };
-    auto grid = [&]() { return units < (unsigned)most ? std::max(units, 1u) : (unsigned)most; };
+    auto grid = [&]() { return std::min(std::max(units, 1u), (unsigned)most); };
+    auto launch = [&](auto& table) -> cudaError_t {
+        if (!c.table)
+            for (int32_t i = 0; i < c.T; ++i) record(table.rec[i], i);
+        c.units = units;
+        return launch_grad<CLIP>(c, table, grid(), st);
+    };
     if (c.T <= kGradFew) {
         GradTable<kGradFew> table;
-        for (int32_t i = 0; i < c.T; ++i) record(table.rec[i], i);
-        c.units = units;
-        GK_CUDA_TRY((launch_grad<CLIP, kGradFew>(c, table, grid(), st)));
-    } else {
+        GK_CUDA_TRY(launch(table));
+    } else if (c.T <= kGradSome) {
+        GradTable<kGradSome> table;
+        GK_CUDA_TRY(launch(table));
+    } else if (c.T <= kGradMany) {
         GradTable<kGradMany> table;
-        if (c.T <= kGradMany) {
-            for (int32_t i = 0; i < c.T; ++i) record(table.rec[i], i);
-        } else {
-            for (int32_t i = 0; i < c.T; i += kGradMany) {
-                const int n = std::min(kGradMany, c.T - i);
-                for (int j = 0; j < n; ++j) record(table.rec[j], i + j);
-                k_grad_table<<<(n + 255) / 256, 256, 0, st>>>(in_ws + i, n, table);
-                GK_CUDA_TRY(cudaGetLastError());
-                note_launch();
-            }
-            c.table = in_ws;
+        GK_CUDA_TRY(launch(table));
+    } else {
+        GradTable<kGradMany> part;
+        for (int32_t i = 0; i < c.T; i += kGradMany) {
+            const int n = std::min(kGradMany, c.T - i);
+            for (int j = 0; j < n; ++j) record(part.rec[j], i + j);
+            k_grad_table<<<(n + 255) / 256, 256, 0, st>>>(in_ws + i, n, part);
+            GK_CUDA_TRY(cudaGetLastError());
+            note_launch();
         }
-        c.units = units;
-        GK_CUDA_TRY((launch_grad<CLIP, kGradMany>(c, table, grid(), st)));
+        c.table = in_ws;
+        GradTable<kGradFew> none;
+        GK_CUDA_TRY(launch(none));
     }
     note_launch();
     return GK_OK;
