@@ -312,10 +312,16 @@ def gk_sparsify_host(g, eps, k: int, idx_out, val_out):
 _TYPES = {"torch.float32": 0, "torch.bfloat16": 1, "torch.float16": 2}
 
 
+_codes: dict = {}
+
+
 def _type(dtype) -> int:
-    code = _TYPES.get(str(dtype))
+    code = _codes.get(dtype)
     if code is None:
-        raise GkError(f"element type {dtype} is not one of float32, bfloat16, float16")
+        code = _TYPES.get(str(dtype))
+        if code is None:
+            raise GkError(f"element type {dtype} is not one of float32, bfloat16, float16")
+        _codes[dtype] = code
     return code
 
 
@@ -417,24 +423,47 @@ def gk_vocab_topk(logits, k: int, idx_out, val_out, lse_out=None, temperature: f
                                 _stream_of(device)))
 
 
-def _given(token, n, device):
-    """(pointer, tokens a row) of the tokens given to each row."""
-    import torch
-    if token is None:
-        return None, 0
-    m = token.shape[1] if isinstance(token, torch.Tensor) and token.dim() == 2 else 1
-    shape = (n, m) if token.dim() == 2 else (n,)
-    return _vec(token, torch.int64, device, shape, "token"), m
+_F32 = _I32 = _I64 = None
 
 
-def _want(t, dtype, device, shape, name):
-    """The pointer of a tensor that may be left away; of its shape, or flat where a row has one value."""
-    import torch
+def _quick(t, dtype, device, shape, name):
+    """The pointer of a contiguous CUDA tensor; what is wrong with it is looked for only where something is."""
     if t is None:
         return None
-    if len(shape) == 2 and shape[1] == 1 and isinstance(t, torch.Tensor) and t.dim() == 1:
-        shape = shape[:1]
+    try:
+        if t.dtype is dtype and t.get_device() == device and t.shape == shape and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        pass
     return _vec(t, dtype, device, shape, name)
+
+
+def _token_rows(logits, token, name="logits"):
+    """What both calls on given tokens begin with: (device, n, shape of a value per token, their first arguments)."""
+    import torch
+    global _F32, _I32, _I64
+    if _F32 is None:
+        _F32, _I32, _I64 = torch.float32, torch.int32, torch.int64
+    device = _matrices(logits)
+    n, V = logits.shape
+    p, ld = _rows(logits, logits.dtype, device, name=name)
+    if token is None:
+        return device, n, (n, 0), (p, ld, _type(logits.dtype), n, V, None, 0)
+    if not isinstance(token, torch.Tensor) or token.dim() not in (1, 2):
+        raise GkError(f"token: expected a contiguous {_I64} CUDA tensor of shape ({n},) or ({n}, m)")
+    m = token.shape[1] if token.dim() == 2 else 1
+    shape = (n, m) if token.dim() == 2 else (n,)
+    return device, n, shape, (p, ld, _type(logits.dtype), n, V, _quick(token, _I64, device, shape, "token"), m)
+
+
+def _per_token(t, device, shape, name):
+    """A value for each given token: laid out as the tokens, or flat (or not) where a row has one."""
+    if t is not None and len(shape) != getattr(t, "ndim", 0):
+        if len(shape) == 1:
+            shape = (shape[0], 1)
+        elif shape[1] == 1:
+            shape = shape[:1]
+    return _quick(t, _F32, device, shape, name)
 
 
 def gk_vocab_logprob(logits, token, logp_out=None, rank_out=None, entropy_out=None, lse_out=None, idx_out=None, val_out=None,
@@ -444,22 +473,17 @@ def gk_vocab_logprob(logits, token, logp_out=None, rank_out=None, entropy_out=No
     logits (n, V): float32, bfloat16 or float16, row stride allowed; token (n, m) or (n,) int64 or None;
     logp_out like token, float32; rank_out (n,) int32; entropy_out, lse_out (n,) float32;
     idx_out (n, k) int32 with val_out (n, k) float32.  Any output may be None."""
-    import torch
-    device = _matrices(logits)
-    n, V = logits.shape
-    p, ld = _rows(logits, logits.dtype, device, name="logits")
-    tp, m = _given(token, n, device)
+    device, n, shape, head = _token_rows(logits, token)
     if (idx_out is None) != (val_out is None):
         raise GkError("idx_out and val_out go together")
     k = 0 if idx_out is None else int(idx_out.shape[-1])
-    f32, row = torch.float32, (n,)
-    _check(load().gk_vocab_logprob(p, ld, _type(logits.dtype), n, V, tp, m, temperature, k,
-                                   _want(logp_out, f32, device, (n, m), "logp_out"),
-                                   _want(rank_out, torch.int32, device, row, "rank_out"),
-                                   _want(entropy_out, f32, device, row, "entropy_out"),
-                                   _want(lse_out, f32, device, row, "lse_out"),
-                                   None if k == 0 else _vec(idx_out, torch.int32, device, (n, k), "idx_out"),
-                                   None if k == 0 else _vec(val_out, f32, device, (n, k), "val_out"), _stream_of(device)))
+    row = (n,)
+    _check(load().gk_vocab_logprob(*head, temperature, k, _per_token(logp_out, device, shape, "logp_out"),
+                                   _quick(rank_out, _I32, device, row, "rank_out"),
+                                   _quick(entropy_out, _F32, device, row, "entropy_out"),
+                                   _quick(lse_out, _F32, device, row, "lse_out"),
+                                   None if k == 0 else _quick(idx_out, _I32, device, (n, k), "idx_out"),
+                                   None if k == 0 else _quick(val_out, _F32, device, (n, k), "val_out"), _stream_of(device)))
 
 
 def gk_vocab_logprob_grad(logits, token, lse, dlogits, logp_grad=None, entropy=None, entropy_grad=None, lse_grad=None,
@@ -467,20 +491,17 @@ def gk_vocab_logprob_grad(logits, token, lse, dlogits, logp_grad=None, entropy=N
     """The gradient at the logits from those of what gk_vocab_logprob wrote (see gk.h): logp_grad like token,
     entropy_grad (with entropy) and lse_grad (n,), float32 or None.  lse (n,): gk_vocab_logprob's; dlogits (n, V):
     of the logits' type, row stride allowed, or the logits themselves."""
-    import torch
-    device = _matrices(logits, dlogits)
-    n, V = logits.shape
-    p, ld = _rows(logits, logits.dtype, device, name="logits")
-    dp, lddz = _rows(dlogits, logits.dtype, device, n, V, name="dlogits")
-    tp, m = _given(token, n, device)
-    f32, row = torch.float32, (n,)
-    if logp_grad is not None and m == 0:
+    device, n, shape, head = _token_rows(logits, token)
+    _matrices(dlogits)
+    dp, lddz = _rows(dlogits, logits.dtype, device, n, logits.shape[1], name="dlogits")
+    if logp_grad is not None and token is None:
         raise GkError("logp_grad without tokens")
-    _check(load().gk_vocab_logprob_grad(p, ld, _type(logits.dtype), n, V, tp, m, temperature,
-                                        _vec(lse, f32, device, row, "lse"), _want(entropy, f32, device, row, "entropy"),
-                                        _want(logp_grad, f32, device, (n, m), "logp_grad"),
-                                        _want(entropy_grad, f32, device, row, "entropy_grad"),
-                                        _want(lse_grad, f32, device, row, "lse_grad"), dp, lddz, _stream_of(device)))
+    row = (n,)
+    _check(load().gk_vocab_logprob_grad(*head, temperature, _quick(lse, _F32, device, row, "lse"),
+                                        _quick(entropy, _F32, device, row, "entropy"),
+                                        _per_token(logp_grad, device, shape, "logp_grad"),
+                                        _quick(entropy_grad, _F32, device, row, "entropy_grad"),
+                                        _quick(lse_grad, _F32, device, row, "lse_grad"), dp, lddz, _stream_of(device)))
 
 
 def gk_vocab_set_budget(nbytes: int) -> None:
@@ -564,7 +585,7 @@ def _grad_list(grads, out=None) -> GradList:
 
 def _one(t, device, name):
     import torch
-    return None if t is None else _vec(t, torch.float32, device, (1,), name)
+    return _quick(t, torch.float32, device, (1,), name)
 
 
 def gk_grad_norm(grads, norm_out, norms_out=None) -> None:
@@ -572,9 +593,8 @@ def gk_grad_norm(grads, norm_out, norms_out=None) -> None:
     GradList, which saves looking them up at every call; norm_out (1,) float32; norms_out (len(grads),) float32."""
     import torch
     g = _grad_list(grads)
-    _check(load().gk_grad_norm(g.pointers, g.types, g.sizes, len(g), _one(norm_out, g.device, "norm_out") or 0,
-                               None if norms_out is None else _vec(norms_out, torch.float32, g.device, (len(g),), "norms_out"),
-                               _stream_of(g.device)))
+    _check(load().gk_grad_norm(g.pointers, g.types, g.sizes, len(g), _one(norm_out, g.device, "norm_out"),
+                               _quick(norms_out, torch.float32, g.device, (len(g),), "norms_out"), _stream_of(g.device)))
 
 
 def gk_grad_clip(grads, max_norm: float, out=None, norm_out=None, scale=None, norm_in=None) -> None:

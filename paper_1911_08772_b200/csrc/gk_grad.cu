@@ -33,7 +33,7 @@ struct GradRec {
 };
 // The table travels as a kernel argument where it fits (a captured call then needs nothing of the host),
 // else kernels with a part of it as their argument write it to the workspace first.
-constexpr int kGradFew = 128, kGradSome = 512, kGradMany = 1000;
+constexpr int kGradFew = 64, kGradMany = 1000;      // (and sizes between: an argument of 16 KB takes the host 4 us more)
 template <int CAP>
 struct GradTable {
     GradRec rec[CAP];
@@ -537,8 +537,14 @@ static int enqueue_grad(GradCall& c, const void* const* grads, const int32_t* ty
     if (c.T <= kGradFew) {
         GradTable<kGradFew> table;
         GK_CUDA_TRY(launch(table));
-    } else if (c.T <= kGradSome) {
-        GradTable<kGradSome> table;
+    } else if (c.T <= 2 * kGradFew) {
+        GradTable<2 * kGradFew> table;
+        GK_CUDA_TRY(launch(table));
+    } else if (c.T <= 3 * kGradFew) {
+        GradTable<3 * kGradFew> table;
+        GK_CUDA_TRY(launch(table));
+    } else if (c.T <= 6 * kGradFew) {
+        GradTable<6 * kGradFew> table;
         GK_CUDA_TRY(launch(table));
     } else if (c.T <= kGradMany) {
         GradTable<kGradMany> table;
