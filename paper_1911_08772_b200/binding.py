@@ -423,7 +423,17 @@ def gk_vocab_topk(logits, k: int, idx_out, val_out, lse_out=None, temperature: f
                                 _stream_of(device)))
 
 
-_F32 = _I32 = _I64 = None
+_torch = _F32 = _I32 = _I64 = _device_now = _stream_now = None
+
+
+def _ready() -> None:
+    """Names that the calls below use at every turn, looked up once (importing this module does not import torch)."""
+    global _torch, _F32, _I32, _I64, _device_now, _stream_now
+    import torch
+    _F32, _I32, _I64 = torch.float32, torch.int32, torch.int64
+    _device_now = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    _stream_now = getattr(torch._C, "_cuda_getCurrentRawStream", None) or _stream_of
+    _torch = torch
 
 
 def _quick(t, dtype, device, shape, name):
@@ -438,22 +448,22 @@ def _quick(t, dtype, device, shape, name):
     return _vec(t, dtype, device, shape, name)
 
 
-def _token_rows(logits, token, name="logits"):
+def _token_rows(logits, token):
     """What both calls on given tokens begin with: (device, n, shape of a value per token, their first arguments)."""
-    import torch
-    global _F32, _I32, _I64
-    if _F32 is None:
-        _F32, _I32, _I64 = torch.float32, torch.int32, torch.int64
-    device = _matrices(logits)
+    if _torch is None:
+        _ready()
+    if not isinstance(logits, _torch.Tensor) or not logits.is_cuda or logits.ndim != 2:
+        raise GkError("logits: expected a 2-D CUDA tensor")
+    device = _device_now()
+    dtype = logits.dtype
     n, V = logits.shape
-    p, ld = _rows(logits, logits.dtype, device, name=name)
+    p, ld = _rows(logits, dtype, device, name="logits")
     if token is None:
-        return device, n, (n, 0), (p, ld, _type(logits.dtype), n, V, None, 0)
-    if not isinstance(token, torch.Tensor) or token.dim() not in (1, 2):
+        return device, n, (n, 0), (p, ld, _type(dtype), n, V, None, 0)
+    shape = getattr(token, "shape", ())
+    if len(shape) not in (1, 2) or shape[0] != n:
         raise GkError(f"token: expected a contiguous {_I64} CUDA tensor of shape ({n},) or ({n}, m)")
-    m = token.shape[1] if token.dim() == 2 else 1
-    shape = (n, m) if token.dim() == 2 else (n,)
-    return device, n, shape, (p, ld, _type(logits.dtype), n, V, _quick(token, _I64, device, shape, "token"), m)
+    return device, n, shape, (p, ld, _type(dtype), n, V, _quick(token, _I64, device, shape, "token"), shape[1] if len(shape) == 2 else 1)
 
 
 def _per_token(t, device, shape, name):
@@ -483,7 +493,7 @@ def gk_vocab_logprob(logits, token, logp_out=None, rank_out=None, entropy_out=No
                                    _quick(entropy_out, _F32, device, row, "entropy_out"),
                                    _quick(lse_out, _F32, device, row, "lse_out"),
                                    None if k == 0 else _quick(idx_out, _I32, device, (n, k), "idx_out"),
-                                   None if k == 0 else _quick(val_out, _F32, device, (n, k), "val_out"), _stream_of(device)))
+                                   None if k == 0 else _quick(val_out, _F32, device, (n, k), "val_out"), _stream_now(device)))
 
 
 def gk_vocab_logprob_grad(logits, token, lse, dlogits, logp_grad=None, entropy=None, entropy_grad=None, lse_grad=None,
@@ -492,7 +502,8 @@ def gk_vocab_logprob_grad(logits, token, lse, dlogits, logp_grad=None, entropy=N
     entropy_grad (with entropy) and lse_grad (n,), float32 or None.  lse (n,): gk_vocab_logprob's; dlogits (n, V):
     of the logits' type, row stride allowed, or the logits themselves."""
     device, n, shape, head = _token_rows(logits, token)
-    _matrices(dlogits)
+    if not isinstance(dlogits, _torch.Tensor):
+        raise GkError("dlogits: expected a 2-D CUDA tensor")
     dp, lddz = _rows(dlogits, logits.dtype, device, n, logits.shape[1], name="dlogits")
     if logp_grad is not None and token is None:
         raise GkError("logp_grad without tokens")
@@ -501,7 +512,7 @@ def gk_vocab_logprob_grad(logits, token, lse, dlogits, logp_grad=None, entropy=N
                                         _quick(entropy, _F32, device, row, "entropy"),
                                         _per_token(logp_grad, device, shape, "logp_grad"),
                                         _quick(entropy_grad, _F32, device, row, "entropy_grad"),
-                                        _quick(lse_grad, _F32, device, row, "lse_grad"), dp, lddz, _stream_of(device)))
+                                        _quick(lse_grad, _F32, device, row, "lse_grad"), dp, lddz, _stream_now(device)))
 
 
 def gk_vocab_set_budget(nbytes: int) -> None:
@@ -573,28 +584,24 @@ class GradList:
 
 
 def _grad_list(grads, out=None) -> GradList:
-    import torch
+    if _torch is None:
+        _ready()
     if not isinstance(grads, GradList):
         return GradList(grads, out)
     if out is not None:
         raise GkError("a GradList has its outputs already")
-    if torch.cuda.current_device() != grads.device:
+    if _device_now() != grads.device:
         raise GkError("the gradients are not on the current device")
     return grads
-
-
-def _one(t, device, name):
-    import torch
-    return _quick(t, torch.float32, device, (1,), name)
 
 
 def gk_grad_norm(grads, norm_out, norms_out=None) -> None:
     """The norm over many gradients together, and each one's (see gk.h).  grads: a list of tensors, or a
     GradList, which saves looking them up at every call; norm_out (1,) float32; norms_out (len(grads),) float32."""
-    import torch
     g = _grad_list(grads)
-    _check(load().gk_grad_norm(g.pointers, g.types, g.sizes, len(g), _one(norm_out, g.device, "norm_out"),
-                               _quick(norms_out, torch.float32, g.device, (len(g),), "norms_out"), _stream_of(g.device)))
+    d, n = g.device, len(g.sizes)
+    _check(load().gk_grad_norm(g.pointers, g.types, g.sizes, n, _quick(norm_out, _F32, d, (1,), "norm_out"),
+                               _quick(norms_out, _F32, d, (n,), "norms_out"), _stream_now(d)))
 
 
 def gk_grad_clip(grads, max_norm: float, out=None, norm_out=None, scale=None, norm_in=None) -> None:
@@ -603,9 +610,10 @@ def gk_grad_clip(grads, max_norm: float, out=None, norm_out=None, scale=None, no
     norm_in: (1,) float32 or None."""
     g = _grad_list(grads, out)
     d = g.device
-    _check(load().gk_grad_clip(g.pointers, g.types, g.out_pointers, g.out_types, g.sizes, len(g), max_norm,
-                               _one(scale, d, "scale"), _one(norm_in, d, "norm_in"), _one(norm_out, d, "norm_out"),
-                               _stream_of(d)))
+    one = (1,)
+    _check(load().gk_grad_clip(g.pointers, g.types, g.out_pointers, g.out_types, g.sizes, len(g.sizes), max_norm,
+                               _quick(scale, _F32, d, one, "scale"), _quick(norm_in, _F32, d, one, "norm_in"),
+                               _quick(norm_out, _F32, d, one, "norm_out"), _stream_now(d)))
 
 
 def gk_grad_last_info():

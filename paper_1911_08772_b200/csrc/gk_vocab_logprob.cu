@@ -13,6 +13,8 @@
 // them.  Where fewer than k are above, the first elements equal to the threshold fill the list (rows whose mask leaves
 // little); where that is not enough either, or the list is too short, the row is walked again in chunks, from a bound
 // that the list gives, and the list cut whenever it is full.
+#include <atomic>
+
 #include "gk_words.cuh"
 
 namespace gk {
@@ -892,6 +894,19 @@ __global__ void __launch_bounds__(kLgThreads, 4) k_vocab_logprob_grad(const Logp
 
 using namespace gk;
 
+// SMs of the current device, looked up once.
+static cudaError_t sm_count(int& sms) {
+    static std::atomic<int> known[64];
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    sms = dev < 64 ? known[dev].load(std::memory_order_relaxed) : 0;
+    if (sms > 0) return cudaSuccess;
+    e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    if (e == cudaSuccess && dev < 64) known[dev].store(sms, std::memory_order_relaxed);
+    return e;
+}
+
 static int check_rows(const void* logits, int64_t ld, int32_t dtype, int64_t n, int64_t V, const int64_t* token, int32_t m, float T) {
     if (n < 0 || V < 1 || V > 2147483647ll || m < 0) return GK_ERR_SIZE;
     if (n > 2147483647ll || m > kLogprobMaxTokens) return GK_ERR_LIMIT;
@@ -913,9 +928,8 @@ extern "C" int gk_vocab_logprob(const void* logits, int64_t ld, int32_t dtype, i
     const double inv_T = 1.0 / (double)temperature;
     LogprobCall c = {(const char*)logits, ld, n, V, token, m, k, 1, (float)inv_T, (float)(inv_T - (double)(float)inv_T), (float)(1.4426950408889634 * inv_T),
                      logp_out, rank_out, entropy_out, lse_out, idx_out, val_out};
-    int dev = 0, sms = 0;
-    GK_CUDA_TRY(cudaGetDevice(&dev));
-    GK_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+    int sms = 0;
+    GK_CUDA_TRY(sm_count(sms));
     cudaError_t e;
     switch (dtype) {
         case GK_TYPE_F32: e = launch_logprob<GK_TYPE_F32>(c, sms, (cudaStream_t)stream); break;
@@ -940,9 +954,8 @@ extern "C" int gk_vocab_logprob_grad(const void* logits, int64_t ld, int32_t dty
     if (n == 0) return GK_OK;
     const uintptr_t z0 = (uintptr_t)logits, z1 = z0 + ((n - 1) * ld + V) * size, d0 = (uintptr_t)dlogits, d1 = d0 + ((n - 1) * lddz + V) * size;
     if (z0 < d1 && d0 < z1 && (z0 != d0 || (ld != lddz && n > 1))) return GK_ERR_ALIAS;
-    int dev = 0, sms = 0;
-    GK_CUDA_TRY(cudaGetDevice(&dev));
-    GK_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+    int sms = 0;
+    GK_CUDA_TRY(sm_count(sms));
     // sixteen words a thread, fewer where there are not enough CTAs
     const int64_t words = V / (16 / size);
     int64_t pieces = (words + 16 * kLgThreads - 1) / (16 * kLgThreads);
