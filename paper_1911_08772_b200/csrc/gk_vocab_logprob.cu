@@ -344,8 +344,8 @@ struct LpResult {
     __device__ __forceinline__ float entropy(const Sums& a) const { return none ? 0.f : nan || inf ? NAN : log_s0 - 0.69314718f * __fdividef(a.s1, a.s0); }
 };
 
-// SPLIT: the CTAs of a cluster share a row.
-template <int TYPE, int NT, bool SPLIT>
+// SPLIT: the CTAs of a cluster share a row.  LISTS: with alternatives.
+template <int TYPE, int NT, bool SPLIT, bool LISTS>
 __global__ void __launch_bounds__(NT, SPLIT ? 2 : LpShared<NT>::kCtas) k_vocab_logprob(const LogprobCall c) {
     using Shared = LpShared<NT>;
     constexpr int kVec = TYPE == GK_TYPE_F32 ? 4 : 8, kSize = TYPE == GK_TYPE_F32 ? 4 : 2, kWarps = NT / 32;
@@ -410,7 +410,7 @@ __global__ void __launch_bounds__(NT, SPLIT ? 2 : LpShared<NT>::kCtas) k_vocab_l
     // the first words are the sample: their maximum is where the sums start
     float top = quarter > 0 ? max_of<TYPE>(x) : -INFINITY;
     float tau = INFINITY;
-    if (c.k > 0) {
+    if constexpr (LISTS) {
         // With e of the k largest expected in the sample, the (e + 4 sqrt(e) + 4)-th largest of 64 groups' or all
         // threads' maxima is hardly among the row's k largest; where the sample is all there is, the k + 8-th leaves room
         // for equal ones.
@@ -452,7 +452,7 @@ __global__ void __launch_bounds__(NT, SPLIT ? 2 : LpShared<NT>::kCtas) k_vocab_l
     float ref = ref_of(least_up);
     bool empty = least_up == -INFINITY;
     least_up += empty ? 0.f : kLpSlack / zscale;
-    float stir = fminf(least_up, tau);      // what a word's largest element has to be above to be looked at
+    float stir = fminf(least_up, tau);      // what four words' largest element has to be above for them to be looked at
     uint64_t s0 = pair(0.f, 0.f), s1 = s0, less = pair(-ref, -ref);
     auto raise = [&](float to) {
         const float r2 = ref_of(to), d = empty ? kLpFloor : fmaxf(ref - r2, kLpFloor), by = exp2_fast(d);
@@ -483,16 +483,6 @@ __global__ void __launch_bounds__(NT, SPLIT ? 2 : LpShared<NT>::kCtas) k_vocab_l
         masks = 0;
     };
     auto word = [&](const uint4& x, int w) {
-        const float g = max_of<TYPE>(x);
-        m = fmaxf(m, g);
-        if (g > stir) {
-            if (g > least_up) raise(g);
-            if (g > tau) {
-                const int to = atomicAdd(&sh.notes, 1);
-                if (to < Shared::kNotes) sh.note[to] = w;
-                if (to < Shared::kNoted) sh.data[to] = x;
-            }
-        }
         if (ranked) {
             const unsigned th = w < first_word ? th_before : th_behind;
             masks -= above<TYPE>(x.x, th) + above<TYPE>(x.y, th);
@@ -521,6 +511,20 @@ __global__ void __launch_bounds__(NT, SPLIT ? 2 : LpShared<NT>::kCtas) k_vocab_l
     };
     auto quad = [&](const uint4 (&x)[kLpQuad], int q) {
         if (q >= quarter) return;
+        const float g = max_of<TYPE>(x);
+        m = fmaxf(m, g);
+        if (g > stir) {
+            if (g > least_up) raise(g);
+            if (LISTS && g > tau) {
+#pragma unroll
+                for (int i = 0; i < kLpQuad; ++i)
+                    if (max_of<TYPE>(x[i]) > tau) {
+                        const int to = atomicAdd(&sh.notes, 1);
+                        if (to < Shared::kNotes) sh.note[to] = q * NT + i * step + tid;
+                        if (to < Shared::kNoted) sh.data[to] = x[i];
+                    }
+            }
+        }
 #pragma unroll
         for (int i = 0; i < kLpQuad; ++i) word(x[i], q * NT + i * step + tid);
         if ((q & 2047) == 2047) count_masks();      // 2^15 of a half
@@ -537,7 +541,7 @@ __global__ void __launch_bounds__(NT, SPLIT ? 2 : LpShared<NT>::kCtas) k_vocab_l
     if (wid == 0 && odd) {
         m = fmaxf(m, odd_v);
         if (odd_v > least_up) raise(odd_v);
-        if (odd_v > tau) sh.list[atomicAdd(&sh.listed, 1)] = lp_entry(odd_v, odd_at);      // 32 at most, the first
+        if (LISTS && odd_v > tau) sh.list[atomicAdd(&sh.listed, 1)] = lp_entry(odd_v, odd_at);      // 32 at most, the first
         if (ranked) rank += odd_v > first_v || (odd_v == first_v && odd_at < first);
         const float d = max_nan(fmaf(odd_v, zscale, -ref), kLpFloor), e = exp2_fast(d);
         s0 = add2(s0, pair(e, 0.f));
@@ -580,7 +584,7 @@ __global__ void __launch_bounds__(NT, SPLIT ? 2 : LpShared<NT>::kCtas) k_vocab_l
     if (ranked && (a.s0 != a.s0 || first_v == -INFINITY)) rank = lp_rank_again<TYPE>(sh, row, v0, v1, first_v, first);
     const int k = SPLIT ? min(c.k, v1 - v0) : c.k;      // of this CTA's elements
     int cnt = 0;
-    if (k > 0) {
+    if constexpr (LISTS) {
         // the list of what may be among the alternatives
         const int notes = sh.notes;
         const bool nan = a.s0 != a.s0;
@@ -624,7 +628,7 @@ __global__ void __launch_bounds__(NT, SPLIT ? 2 : LpShared<NT>::kCtas) k_vocab_l
         }
     };
     if constexpr (SPLIT) {
-        place_all([&](int place, uint64_t e) { sh.best[place] = e; });
+        if constexpr (LISTS) place_all([&](int place, uint64_t e) { sh.best[place] = e; });
         if (tid == 0) {
             sh.part = a;
             sh.part_above = rank;
@@ -658,7 +662,7 @@ __global__ void __launch_bounds__(NT, SPLIT ? 2 : LpShared<NT>::kCtas) k_vocab_l
         c.val[r * c.k + place] = result.logp(key_value((unsigned)(e >> 32)));
     };
     if constexpr (!SPLIT) {
-        place_all(write);
+        if constexpr (LISTS) place_all(write);
     } else {
         // all parts' alternatives beside one another, and how many of each part are above each of this CTA's
         uint64_t* all = reinterpret_cast<uint64_t*>(sh.data);
@@ -684,7 +688,7 @@ __global__ void __launch_bounds__(NT, SPLIT ? 2 : LpShared<NT>::kCtas) k_vocab_l
     }
 }
 
-template <int TYPE>
+template <int TYPE, bool LISTS>
 static cudaError_t launch_logprob(LogprobCall& c, int sms, cudaStream_t st) {
     const int64_t words = c.V / (TYPE == GK_TYPE_F32 ? 4 : 8);
     // CTAs a row: as many as there is room for, while each still has four words for every thread (64 rows of 32000 bf16,
@@ -701,16 +705,16 @@ static cudaError_t launch_logprob(LogprobCall& c, int sms, cudaStream_t st) {
         cfg.stream = st;
         cfg.blockDim = dim3(256);
         cfg.gridDim = dim3((unsigned)(c.n * c.parts));
-        return cudaLaunchKernelEx(&cfg, k_vocab_logprob<TYPE, 256, true>, c);
+        return cudaLaunchKernelEx(&cfg, k_vocab_logprob<TYPE, 256, true, LISTS>, c);
     }
     // 4096 rows of 10000 bf16 with 10 alternatives: 51 us by 64 threads a row, 59 by 128, 76 by 256; of 32000: 106, 102
     // and 108; of 128000: 1000, 300 and 280 (few threads' samples are small, and their lists overflow).  Twice the
     // threads while there is room for them.
     int threads = words <= kLpShort ? 64 : words <= kLpMiddle ? 128 : 256;
     while (threads < 256 && c.n * threads * 2 <= 1024ll * sms && words >= 4 * threads) threads *= 2;
-    if (threads == 64) k_vocab_logprob<TYPE, 64, false><<<(unsigned)c.n, 64, 0, st>>>(c);
-    else if (threads == 128) k_vocab_logprob<TYPE, 128, false><<<(unsigned)c.n, 128, 0, st>>>(c);
-    else k_vocab_logprob<TYPE, 256, false><<<(unsigned)c.n, 256, 0, st>>>(c);
+    if (threads == 64) k_vocab_logprob<TYPE, 64, false, LISTS><<<(unsigned)c.n, 64, 0, st>>>(c);
+    else if (threads == 128) k_vocab_logprob<TYPE, 128, false, LISTS><<<(unsigned)c.n, 128, 0, st>>>(c);
+    else k_vocab_logprob<TYPE, 256, false, LISTS><<<(unsigned)c.n, 256, 0, st>>>(c);
     return cudaGetLastError();
 }
 
@@ -932,9 +936,11 @@ extern "C" int gk_vocab_logprob(const void* logits, int64_t ld, int32_t dtype, i
     GK_CUDA_TRY(sm_count(sms));
     cudaError_t e;
     switch (dtype) {
-        case GK_TYPE_F32: e = launch_logprob<GK_TYPE_F32>(c, sms, (cudaStream_t)stream); break;
-        case GK_TYPE_BF16: e = launch_logprob<GK_TYPE_BF16>(c, sms, (cudaStream_t)stream); break;
-        default: e = launch_logprob<GK_TYPE_F16>(c, sms, (cudaStream_t)stream); break;
+#define GK_LAUNCH(TYPE) e = k > 0 ? launch_logprob<TYPE, true>(c, sms, (cudaStream_t)stream) : launch_logprob<TYPE, false>(c, sms, (cudaStream_t)stream)
+        case GK_TYPE_F32: GK_LAUNCH(GK_TYPE_F32); break;
+        case GK_TYPE_BF16: GK_LAUNCH(GK_TYPE_BF16); break;
+        default: GK_LAUNCH(GK_TYPE_F16); break;
+#undef GK_LAUNCH
     }
     if (e != cudaSuccess) return cuda_fail(e);
     note_launch();
