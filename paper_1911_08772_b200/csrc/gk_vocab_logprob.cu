@@ -379,15 +379,13 @@ __global__ void __launch_bounds__(NT, SPLIT ? 2 : LpShared<NT>::kCtas) k_vocab_l
     fetch(x, 0);
     fetch(y, 1);
     // the given tokens
-    const int64_t token = tid < c.m ? c.token[r * c.m + tid] : -1;
-    const bool mine = token >= 0 && token < V;
-    bool any = mine;
-    for (int j = tid + NT; j < c.m; j += NT) {
+    bool any = false;
+    for (int j = tid; j < c.m; j += NT) {
         const int64_t t = c.token[r * c.m + j];
         any |= t >= 0 && t < V;
     }
     const bool odd = lane < 16 ? lane < before : lane - 16 < behind;      // a warp's elements outside the words
-    const int odd_at = lane < 16 ? v0 + lane : v1 - behind + lane - 16;
+    const int odd_at = !odd ? 0 : lane < 16 ? v0 + lane : v1 - behind + (lane - 16);      // (no sum past 2^31 on the way)
     const float odd_v = odd ? load_logit<TYPE>(row, odd_at) : -INFINITY;
     if (tid == 0) sh.notes = sh.listed = 0;
     if (!__syncthreads_or(any) && c.m > 0) {
@@ -550,6 +548,8 @@ __global__ void __launch_bounds__(NT, SPLIT ? 2 : LpShared<NT>::kCtas) k_vocab_l
     // equal elements in the token's own word before it
     if (ranked && first_word >= 0 && first_word < words && tid < first_at % kVec)
         rank += load_logit<TYPE>(row, first - first_at % kVec + tid) == first_v;
+    const int64_t token = tid < c.m ? c.token[r * c.m + tid] : -1;
+    const bool mine = token >= 0 && token < V;
     const float own_v = tid == 0 ? first_v : mine ? load_logit<TYPE>(row, token) : 0.f;
     Sums a;
     {
@@ -710,7 +710,7 @@ static cudaError_t launch_logprob(LogprobCall& c, int sms, cudaStream_t st) {
     // 4096 rows of 10000 bf16 with 10 alternatives: 51 us by 64 threads a row, 59 by 128, 76 by 256; of 32000: 106, 102
     // and 108; of 128000: 1000, 300 and 280 (few threads' samples are small, and their lists overflow).  Twice the
     // threads while there is room for them.
-    int threads = words <= kLpShort ? 64 : words <= kLpMiddle ? 128 : 256;
+    int threads = words <= kLpShort && c.k <= 48 ? 64 : words <= kLpMiddle ? 128 : 256;
     while (threads < 256 && c.n * threads * 2 <= 1024ll * sms && words >= 4 * threads) threads *= 2;
     if (threads == 64) k_vocab_logprob<TYPE, 64, false, LISTS><<<(unsigned)c.n, 64, 0, st>>>(c);
     else if (threads == 128) k_vocab_logprob<TYPE, 128, false, LISTS><<<(unsigned)c.n, 128, 0, st>>>(c);
@@ -752,6 +752,7 @@ __global__ void __launch_bounds__(kLgThreads, 4) k_vocab_logprob_grad(const Logp
         const int head = min((int)((16 - ((uintptr_t)row & 15)) % 16) / kSize, V), all = (V - head) / kVec;
         const int w0 = (int)((int64_t)all * blockIdx.x / gridDim.x), words = (int)((int64_t)all * (blockIdx.x + 1) / gridDim.x) - w0;
         const int v0 = blockIdx.x == 0 ? 0 : head + w0 * kVec, v1 = blockIdx.x == gridDim.x - 1 ? V : head + (w0 + words) * kVec;
+        const int behind = v1 - (head + (w0 + words) * kVec);      // elements behind the words (sums past 2^31 are not formed)
         const uint4* from = (const uint4*)(row + head * kSize) + w0 + tid;
         uint4* to = (uint4*)(out + head * kSize) + w0 + tid;
         uint4 x[kWords], y[kWords];
@@ -782,12 +783,12 @@ __global__ void __launch_bounds__(kLgThreads, 4) k_vocab_logprob_grad(const Logp
         counts = counts && !(lse < -1e30f);      // else nothing is left, or masks of a type's lowest value alone
         if (!counts) {
             if (apart) {
-                for (int i = v0 + tid; i < v1; i += kLgThreads) store(i, 0.f);
+                for (int64_t i = (int64_t)v0 + tid; i < v1; i += kLgThreads) store(i, 0.f);
                 continue;
             }
             for (int w = tid; w < words; w += kLgThreads) __stcs(to + w - tid, make_uint4(0, 0, 0, 0));
             if (tid < head - v0) store(v0 + tid, 0.f);
-            if (head + (w0 + words) * kVec + tid < v1) store(head + (w0 + words) * kVec + tid, 0.f);
+            if (tid < behind) store(v1 - behind + tid, 0.f);
             continue;
         }
 #pragma unroll
@@ -825,7 +826,7 @@ __global__ void __launch_bounds__(kLgThreads, 4) k_vocab_logprob_grad(const Logp
             __syncthreads();      // read before it is written over, where dlogits are the logits
         }
         if (apart) {
-            for (int i = v0 + tid; i < v1; i += kLgThreads) store(i, grad(plain(i)));
+            for (int64_t i = (int64_t)v0 + tid; i < v1; i += kLgThreads) store(i, grad(plain(i)));
         } else {
             // One bound takes the place of all logits below it, -inf among them, where their probabilities are zero in fp32
             // and the bound's is too: 200 nats below the log-sum-exp, with room for its own rounding to 16 bits.  Where no
@@ -883,8 +884,7 @@ __global__ void __launch_bounds__(kLgThreads, 4) k_vocab_logprob_grad(const Logp
                 fetch(y, w + 3 * kStep);
             }
             if (tid < head - v0) store(v0 + tid, grad(plain(v0 + tid)));
-            const int behind = head + (w0 + words) * kVec + tid;
-            if (behind < v1) store(behind, grad(plain(behind)));
+            if (tid < behind) store(v1 - behind + tid, grad(plain(v1 - behind + tid)));
         }
         if (here) {
             __syncthreads();
