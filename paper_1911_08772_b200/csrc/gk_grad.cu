@@ -275,6 +275,13 @@ __device__ __forceinline__ double total_norm(const double* cta_sums, unsigned G,
     return sqrt(block_total((threadIdx.x & 31) == 0 ? v : 0.0, smem));
 }
 
+// atomicInc that all before it is seen by whoever counts later.
+__device__ __forceinline__ unsigned count_in(unsigned* counter, unsigned last) {
+    unsigned before;
+    asm volatile("atom.acq_rel.gpu.global.inc.u32 %0, [%1], %2;" : "=r"(before) : "l"(counter), "r"(last) : "memory");
+    return before;
+}
+
 template <bool CLIP, int CAP>
 __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const GradCall c, const __grid_constant__ GradTable<CAP> table) {
     __shared__ double smem[kGradWarps];
@@ -339,11 +346,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const GradCall c, cons
     if constexpr (!CLIP) {
         // the CTA that is done last joins the sums
         __syncthreads();
-        if (tid == 0) {
-            __threadfence();
-            flag = atomicInc(&c.ctl->done, G - 1) == G - 1;
-            __threadfence();
-        }
+        if (tid == 0) flag = count_in(&c.ctl->done, G - 1) == G - 1;
         __syncthreads();
         if (!flag) return;
         const double norm = total_norm(c.cta_sums, G, smem);
