@@ -22,6 +22,7 @@ namespace gk {
 
 constexpr int kGradThreads = 512, kGradWarps = kGradThreads / 32;
 constexpr int kGradUnit = 16384;          // bytes of source in a unit
+constexpr int kGradSmall = 65536, kGradPiece = 4096;      // bytes of a span that is cut into a warp's pieces
 constexpr int kGradParts = 32;            // sums of spans kept before they are joined
 
 struct GradRec {
@@ -316,15 +317,19 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const GradCall c, cons
                 last = i;
                 const int type = (int)(r.types & 255u), size = type == GK_TYPE_F32 ? 4 : 2;
                 const char* p = (const char*)r.src + from * size;
-                // a span of a unit or less is one warp's, the next such the next one's
-                if ((to - from) * size <= kGradUnit) {
-                    if (little++ % kGradWarps != wid) continue;
+                // a small span is cut into pieces, a warp each; where its own sum is wanted, one of a unit or less is one warp's
+                if (!each && (to - from) * size <= kGradSmall) {
+                    const int64_t step = kGradPiece / size;
+                    const int pieces = (int)((to - from + step - 1) / step);
+                    for (int j = (wid - little) & (kGradWarps - 1); j < pieces; j += kGradWarps)
+                        all += squares<32>(type, p + (int64_t)j * kGradPiece, min(step, to - from - j * step), lane);
+                    little += pieces;
+                } else if (each && (to - from) * size <= kGradUnit) {
+                    if (((little++ - wid) & (kGradWarps - 1)) != 0) continue;
                     double v = squares<32>(type, p, to - from, lane);
                     all += v;
-                    if (each) {
-                        v = warp_sum(v);
-                        if (lane == 0) c.span_sums[i + b] = v;
-                    }
+                    v = warp_sum(v);
+                    if (lane == 0) c.span_sums[i + b] = v;
                 } else {
                     double v = squares<kGradThreads>(type, p, to - from, tid);
                     all += v;
@@ -420,8 +425,15 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const GradCall c, cons
                 const int64_t s = (r.types & 255u) == GK_TYPE_F32 ? 4 : 2, d = r.types >> 8 == GK_TYPE_F32 ? 4 : 2;
                 const char* p = (const char*)r.src + from * s;
                 char* q = (char*)r.dst + from * d;
-                if ((to - from) * s > kGradUnit) scaled<kGradThreads>(r.types, p, q, to - from, by, tid);
-                else if (little++ % kGradWarps == wid) scaled<32>(r.types, p, q, to - from, by, lane);
+                if ((to - from) * s > kGradSmall) {
+                    scaled<kGradThreads>(r.types, p, q, to - from, by, tid);
+                } else {
+                    const int64_t step = kGradPiece / s;
+                    const int pieces = (int)((to - from + step - 1) / step);
+                    for (int j = (wid - little) & (kGradWarps - 1); j < pieces; j += kGradWarps)
+                        scaled<32>(r.types, p + (int64_t)j * kGradPiece, q + j * step * d, min(step, to - from - j * step), by, lane);
+                    little += pieces;
+                }
             }
             if (r.first <= u0) break;
         }
