@@ -35,7 +35,6 @@
 
 #include <atomic>
 
-#include "gk_mbarrier.cuh"
 #include "gk_vocab.cuh"
 
 namespace gk {
@@ -61,6 +60,7 @@ static_assert(kVocabTile == 128, "a reading warp's columns have one maximum and 
 // ---------------------------------------------------------------------------
 // PTX
 // ---------------------------------------------------------------------------
+__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ uint32_t cluster_rank() {
     uint32_t r;
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
@@ -74,8 +74,56 @@ __device__ __forceinline__ uint32_t in_cta(uint32_t addr, uint32_t rank) {
 __device__ __forceinline__ void cluster_barrier() {
     asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
+__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
 __device__ __forceinline__ void mbar_arrive_remote(uint32_t cluster_addr) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+__device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n.reg .pred p;\n"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n"
+        "selp.u32 %0, 1, 0, p;\n}"
+        : "=r"(ok) : "r"(bar), "r"(parity), "r"(1000000) : "memory");
+    return ok != 0;
+}
+// The same without waiting.
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n.reg .pred p;\n"
+        "mbarrier.test_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"
+        "selp.u32 %0, 1, 0, p;\n}"
+        : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
+}
+// Bounded: gives up after `limit` clocks, or 2^24 polls, whichever is first.
+constexpr long long kWaitClocks = 1ll << 32;       // about two seconds
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, long long limit) {
+    if (mbar_try(bar, parity)) return true;
+    const long long t0 = clock64();
+#pragma unroll 1
+    for (int i = 0; i < (1 << 24); ++i) {
+        if (mbar_try(bar, parity)) return true;
+        if ((i & 63) == 63 && clock64() - t0 > limit) return false;
+    }
+    return false;
+}
+// The whole warp waits and the outcome is a vote: the loops run over values that the compiler knows to be the
+// same in all lanes, and one elected lane only issues.  (Loops run by lane 0 alone could not keep the tensor pipe
+// fed: 61 % busy, 4096 x 4096 x 32000.)
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, long long limit) {
+    return __all_sync(0xffffffffu, mbar_wait(bar, parity, limit));
+}
+__device__ __forceinline__ bool elected() {
+    uint32_t p;
+    asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(p));
+    return p != 0;
 }
 __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar_cluster) {
     asm volatile(
