@@ -176,3 +176,28 @@ def test_as_many_tensors_as_are_allowed():
     check_clipped([flat], [out], 1.0)
     with pytest.raises(gk.GkError):
         gk.gk_grad_norm(grads + [flat[:1]], norm)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_gradients_between_the_rows_of_their_logits(dtype):
+    """Two halves of one buffer's rows; rows that meet are refused."""
+    n, V, gap = 9, 1003, 5
+    gen = torch.Generator().manual_seed(4)
+    both = torch.full((n, 2 * V + gap), 7.0, dtype=dtype, device=DEV)
+    z, dz = both[:, :V], both[:, V + 2:2 * V + 2]
+    z.copy_((torch.randn(n, V, generator=gen) * 2).to(dtype))
+    token, a = torch.randint(0, V, (n, 1), generator=gen), torch.randn(n, 1, generator=gen)
+    lse, entropy = torch.empty(n, device=DEV), torch.empty(n, device=DEV)
+    gk.gk_vocab_logprob(z, token.to(DEV), lse_out=lse, entropy_out=entropy)
+    kept = z.cpu()
+    gk.gk_vocab_logprob_grad(z, token.to(DEV), lse, dz, logp_grad=a.to(DEV))
+    want, tol = grad_reference(kept, token, 1.0, lse.cpu(), entropy.cpu(), a, None, None)
+    u = torch.finfo(dtype).eps / 2
+    assert close(dz, want, tol + u * (want.abs() + tol) + (2.0 ** -25 if dtype == F16 else 2.0 ** -126))
+    assert torch.equal(z.cpu(), kept)
+    assert bool((both[:, V:V + 2] == 7).all()) and bool((both[:, 2 * V + 2:] == 7).all())
+    for bad in (both[:, V - 1:2 * V - 1], both.as_strided((n - 1, V), (2 * V + gap + 1, 1), V + 2)):
+        with pytest.raises(gk.GkError):
+            gk.gk_vocab_logprob_grad(z[:len(bad)], token[:len(bad)].to(DEV), lse[:len(bad)], bad, logp_grad=a[:len(bad)].to(DEV))
+    # the logits behind their gradients
+    gk.gk_vocab_logprob_grad(dz, token.to(DEV), lse, z, logp_grad=a.to(DEV))

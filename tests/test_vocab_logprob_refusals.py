@@ -44,3 +44,12 @@ def test_gradients(lib, change, want):
 def test_no_rows(lib):
     assert forward(lib, n=0, logits=None, token=None, idx=None, val=None) == 0
     assert backward(lib, n=0, logits=None, token=None, lse=None, dz=None, entropy=None) == 0
+
+
+def test_rows_between_rows(lib):
+    """Rows of 50 floats, 103 apart: gradients 50 to 53 elements on lie between the logits, any others that begin among
+    them do not."""
+    for by in (1, 49, 54, 102, 103, 103 + 49, 103 + 54):
+        assert backward(lib, n=4, ld=103, lddz=103, dz=A + 4 * by) == -5
+        assert backward(lib, n=4, ld=103, lddz=103, logits=A + 4 * by, dz=A) == -5
+    assert backward(lib, n=4, ld=103, lddz=104, dz=A + 4 * 51) == -5
