@@ -13,7 +13,7 @@
  *     g, eps and u must be 16-byte aligned.  Inputs must be finite.
  *   - The library owns a scratch workspace per (device, stream), created
  *     by the first call that needs it (cudaMalloc; use gk_reserve to do that
- *     ahead of time) and kept: small for the sparsifiers, up to gk_vocab_set_budget
+ *     ahead of time) and kept: small for the sparsifiers and gk_grad_*, up to gk_vocab_set_budget
  *     and more, in a block of its own, for the vocabulary head.  Two calls that overlap on the GPU must use different
  *     streams.  Calls of several host threads are safe on any streams: those
  *     on one stream are enqueued whole, one after the other in no promised
@@ -44,9 +44,9 @@ typedef enum gk_status {
     GK_OK = 0,
     GK_ERR_NULL = -1,      /* a required pointer is NULL */
     GK_ERR_SIZE = -2,      /* d < 1 or d > 2^31 - 1, or S < 1 */
-    GK_ERR_K = -3,         /* k < 1 or k > d */
-    GK_ERR_ALIGN = -4,     /* g / eps / u not 16-byte aligned */
-    GK_ERR_ALIAS = -5,     /* g overlaps eps */
+    GK_ERR_K = -3,         /* k < 1 or k > d; gk_vocab_logprob: k < 0, k > V or k > 128 */
+    GK_ERR_ALIGN = -4,     /* g / eps / u not 16-byte aligned; gk_vocab_*, gk_grad_*: a pointer off its type's boundary */
+    GK_ERR_ALIAS = -5,     /* g overlaps eps; gk_vocab_logprob_grad, gk_grad_clip: an output overlaps what it must not */
     GK_ERR_CUDA = -6,      /* a CUDA runtime call failed (see gk_last_cuda_error) */
     GK_ERR_NOMEM = -7,     /* workspace allocation failed */
     GK_ERR_CAPACITY = -8,  /* gk_set_capacity: cap < 0 */
@@ -446,9 +446,10 @@ int gk_vocab_topk(const void* logits, int64_t ld, int32_t dtype, int64_t n, int6
  *   entropy_grad   DEVICE in   b, n floats; NULL: 0
  *   lse_grad   DEVICE in   c, n floats (a penalty on the log-sum-exp); NULL: 0
  *   dlogits    DEVICE out  n rows of V elements of `dtype`, row stride lddz >= V.  The logits themselves (same
- *                          pointer and stride: in place), or memory that shares nothing with them
+ *                          pointer and stride: in place), or memory that shares nothing with them: before or behind
+ *                          all of them, or, of the same stride, between their rows
  * A token given twice counts twice.  Rows left out get zeros, and so do rows whose lse is below -1e30: their masks, of
- * -inf or of a type's lowest value, leave nothing.  So do logits of -inf that are no token.  log p is taken from lse
+ * -inf or of fp32's or bf16's lowest value, leave nothing.  So do logits of -inf that are no token.  log p is taken from lse
  * and has its rounding, 2^-24 of |lse|.  Rounded once to `dtype`.  No workspace.
  */
 int gk_vocab_logprob(const void* logits, int64_t ld, int32_t dtype, int64_t n, int64_t V, const int64_t* token, int32_t m,
@@ -490,7 +491,7 @@ int gk_vocab_last_info(gk_stream_t stream, int64_t* host_out);
  *   norms_out  DEVICE out  T floats; NULL: not wanted
  * The lists are read before the call returns (they travel as the kernel's argument); a captured call keeps them.
  * Any values: squares beyond fp32's range are taken in fp64, an infinity gives infinity, NaN gives NaN.  A tensor
- * given twice counts twice.  Sums of 16 to 32 squares in fp32, the rest in fp64, in an order that the sizes, the
+ * given twice counts twice.  Sums of 32 squares (fp32) or 64 (16 bits) in fp32, the rest in fp64, in an order that the sizes, the
  * 16-byte boundaries within the tensors and the device decide: the same call gives the same bits.
  *
  * gk_grad_clip -- the gradients scaled so that their norm is at most max_norm, in place or into other tensors:

@@ -2,12 +2,16 @@
 // gk_grad_clip).
 //
 // The work is cut into units of 16 KB of a tensor's gradients; a CTA has a contiguous stretch of all units, so
-// that of each tensor it meets it has one contiguous span.  Squares are added in fp32 over 16 (fp32) or 32
-// (16-bit) elements and those sums in fp64; where such a sum says that squares left fp32's range, or is zero,
-// the elements are squared again in fp64.  Sums are joined in a fixed order: threads, warps, CTAs.
+// that of each tensor it meets it has one contiguous span.  A long span is the whole CTA's; a short one is cut
+// into pieces of 4 KB, or where each tensor's norm is wanted left whole, for a warp each.  Squares are added in fp32
+// over 32 (fp32) or 64 (16-bit) elements and those sums in fp64; where such a sum says that squares left fp32's
+// range, or is zero, the elements are squared again in fp64.  Sums are joined in a fixed order: threads, warps, CTAs.
+// Bounded by memory, with eight words a thread (64 KB an SM) on their way: the norm of 1e9 bf16 in 400 tensors, 2 GB,
+// takes 297 us (a copy's rate; two CTAs an SM with four words, double-buffered, 350), of 25.6 M fp32 in 161 tensors 28.
 //
 // Clipping is one cooperative kernel: squares, a barrier of the grid, and the scaling from the last unit back
-// to the first, which meets in L2 what the squares read last.
+// to the first, which meets in L2 what the squares read last.  4e8 elements of bf16 and fp32 into one fp32 vector: 3.0 GB
+// in 551 us; 25.6 M fp32 in 161 tensors, from L2 the second time, 57; 269722 in 65, 8.6, most of it the barrier.
 #include <algorithm>
 #include <new>
 #include <utility>
@@ -173,8 +177,9 @@ __device__ __forceinline__ void shifted(unsigned (&w)[W], int off, float (&f)[8]
     }
 }
 
-// dst = c src, n elements, from the last to the first, by thread tid of G.  A thread has eight elements at a time that begin on a boundary
-// of 32 bytes (fp32) or 16 in dst; where they lie otherwise in src, they are cut out of the 16-byte words around them.
+// dst = c src, n elements, from the last to the first, by thread tid of G.  A thread has eight elements at a time that
+// begin on a boundary of 32 bytes (fp32) or 16 in dst; where they lie otherwise in src, they are cut out of the 16-byte
+// words around them.
 template <int SRC, int DST, int G>
 __device__ __forceinline__ void scaled(const char* src, char* dst, int64_t n, float c, int tid) {
     constexpr int kS = Elem<SRC>::size, kD = Elem<DST>::size, kEach = SRC == GK_TYPE_F32 ? 2 : DST == GK_TYPE_F32 ? 4 : 8;

@@ -343,9 +343,9 @@ extern "C" const char* gk_strerror(int code) {
         case GK_OK: return "ok";
         case GK_ERR_NULL: return "a required pointer is NULL (or no call was made on this stream)";
         case GK_ERR_SIZE: return "size out of range (need 1 <= d <= 2^31-1, 1 <= S <= 65536)";
-        case GK_ERR_K: return "k out of range (need 1 <= k <= d)";
-        case GK_ERR_ALIGN: return "vector base pointer is not 16-byte aligned";
-        case GK_ERR_ALIAS: return "g overlaps eps";
+        case GK_ERR_K: return "k out of range (need 1 <= k <= d, or what this call takes)";
+        case GK_ERR_ALIGN: return "pointer is not on the boundary that this call needs (vectors: 16 bytes)";
+        case GK_ERR_ALIAS: return "g overlaps eps, or an output what it must not";
         case GK_ERR_CUDA: return "CUDA runtime error (see gk_last_cuda_error)";
         case GK_ERR_NOMEM: return "could not allocate the scratch workspace";
         case GK_ERR_CAPACITY: return "capacity must be >= 0";

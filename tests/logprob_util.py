@@ -5,8 +5,9 @@ Bounds, from the arithmetic (u = 2^-24; y = z / T; m the row's maximum):
   * a power 2^d of the pass, d = (z - m) log2(e) / T: the difference, the product and log2(e) / T are each rounded,
     3 u |d| log 2 in the exponent, and the power itself is off by 4 u at most: with |d| <= 30 for every power that shows
     (2^-30 and less together are below 2^-13 of the sum for any V here, and off by less than 200 u of themselves),
-    a sum is off by at most (3 x 21 + 4) u of itself plus that of adding: 64 terms a thread or fewer at a time, warps
-    and CTAs after: 30 u.  S_TOL = 128 u covers a sum of terms of one sign;
+    a sum is off by at most (3 x 21 + 4) u of itself plus that of adding: a thread adds N <= 100 terms in each half of
+    a pair, each addition off by u of the sum so far, which is half of the last one on average: 50 u; the halves, lanes,
+    warps and CTAs after: 10 u.  S_TOL = 128 u covers a sum of terms of one sign;
   * lse: log S0 by S_TOL absolute, its own rounding and that of m / T and the sum: 3 u of the larger;
   * logp = (z - m) / T - log S0: the difference rounded once, so 3 u of |(z - m) / T| instead;
   * entropy = log S0 - log 2 S1 / S0: S_TOL + 2 S_TOL |S1 / S0| log 2 <= S_TOL (1 + 2 H), and 4 u (1 + H);
