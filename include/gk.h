@@ -508,7 +508,8 @@ int gk_vocab_last_info(gk_stream_t stream, int64_t* host_out);
  *   norm_in    DEVICE in   the norm, of the scaled gradients, where the caller knows it (over tensors that other
  *                          ranks hold, say); NULL: taken over these tensors
  *   norm_out   DEVICE out  one float, the norm before clipping; NULL: not wanted
- * A norm that is not finite clips nothing (c = 1): the caller finds it in norm_out and drops the step.  Where
+ * A norm that is not finite as a float clips nothing (c = 1): the caller finds it in norm_out and drops the step.
+ * A factor c s below 2^-126 has the absolute steps of fp32 there.  Where
  * nothing is clipped or scaled, tensors in place are not written.  One cooperative kernel (the device must support
  * that); should its bounded barrier run out, norm_out is NaN and no output is complete.
  */

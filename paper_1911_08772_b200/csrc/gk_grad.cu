@@ -411,8 +411,8 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const GradCall c, cons
             }
             norm = total_norm(c.cta_sums, G, smem) * fabs((double)scale);
         }
-        // norms that are not finite clip nothing: the caller sees them
-        const bool clips = norm > (double)c.max_norm && norm < (double)INFINITY;
+        // norms that are not finite in norm_out clip nothing: the caller sees them
+        const bool clips = norm > (double)c.max_norm && (float)norm < INFINITY;
         const float by = clips ? (float)((double)scale * ((double)c.max_norm / norm)) : scale;
         if (b == 0 && tid == 0) {
             if (c.norm_out) c.norm_out[0] = (float)norm;

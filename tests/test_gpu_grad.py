@@ -156,6 +156,20 @@ def test_a_norm_and_a_scale_that_the_caller_has():
     check_clipped(before, grads, math.inf, scale=-0.5)
 
 
+def test_a_norm_beyond_fp32_clips_nothing():
+    for g in (torch.full((2000,), 3e38, device=DEV), torch.full((70000,), 3e38, dtype=BF16, device=DEV)):
+        before, norm, out = g.clone(), torch.empty(1, device=DEV), torch.zeros(g.numel(), device=DEV)
+        gk.gk_grad_clip([g], 1.0, out=out, norm_out=norm)
+        assert math.isinf(float(norm)) and gk.gk_grad_last_info() == (0, False) and torch.equal(out, before.float())
+        gk.gk_grad_clip([g], 1.0, norm_in=norm)
+        assert torch.equal(g, before)
+        # within fp32 once scaled
+        scale = torch.full((1,), 2.0 ** -40, device=DEV)
+        gk.gk_grad_clip([g], 2.0 ** 20, scale=scale, norm_out=norm)
+        check_norms([before.double() * 2.0 ** -40], norm)
+        check_clipped([before], [g], 2.0 ** 20, scale=2.0 ** -40)
+
+
 def test_offsets_past_32_bits():
     n = (1 << 32) + 4099
     g = torch.zeros(n, dtype=BF16, device=DEV)
