@@ -3,11 +3,11 @@
 //
 // The work is cut into units of 16 KB of a tensor's gradients; a CTA has a contiguous stretch of all units, so
 // that of each tensor it meets it has one contiguous span.  A long span is the whole CTA's; a short one is cut
-// into pieces of 4 KB, or where each tensor's norm is wanted left whole, for a warp each.  Squares are added in fp32
+// into pieces of 4 KB, a warp each.  Squares are added in fp32
 // over 32 (fp32) or 64 (16-bit) elements and those sums in fp64; where such a sum says that squares left fp32's
 // range, or is zero, the elements are squared again in fp64.  Sums are joined in a fixed order: threads, warps, CTAs.
 // Bounded by memory, with eight words a thread (64 KB an SM) on their way: the norm of 1e9 bf16 in 400 tensors, 2 GB,
-// takes 297 us (a copy's rate; two CTAs an SM with four words, double-buffered, 350), of 25.6 M fp32 in 161 tensors 28.
+// takes 297 us (a copy's rate; two CTAs an SM with four words, double-buffered, 350), of 25.6 M fp32 in 161 tensors 26.
 //
 // Clipping is one cooperative kernel: squares, a barrier of the grid, and the scaling from the last unit back
 // to the first, which meets in L2 what the squares read last.  4e8 elements of bf16 and fp32 into one fp32 vector: 3.0 GB
@@ -26,7 +26,10 @@ namespace gk {
 
 constexpr int kGradThreads = 512, kGradWarps = kGradThreads / 32;
 constexpr int kGradUnit = 16384;          // bytes of source in a unit
-constexpr int kGradSmall = 65536, kGradPiece = 4096;      // bytes of a span that is cut into a warp's pieces
+// Bytes of a span that is cut into pieces, a warp each, and of a piece.  The CTA's warps together take 64 KB in turns, the
+// last of them only in part: the norms of 25.6 M fp32 in 161 tensors 20.1 us (spans beyond 64 KB so), 19.3 (128 KB),
+// 19.2 (256 KB); of 1e9 bf16, where all spans are long, 312 against 322 in pieces.
+constexpr int kGradSmall = 131072, kGradPiece = 4096;
 constexpr int kGradParts = 32;            // sums of spans kept before they are joined
 
 struct GradRec {
@@ -322,31 +325,28 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const GradCall c, cons
                 last = i;
                 const int type = (int)(r.types & 255u), size = type == GK_TYPE_F32 ? 4 : 2;
                 const char* p = (const char*)r.src + from * size;
-                // a small span is cut into pieces, a warp each; where its own sum is wanted, one of a unit or less is one warp's
-                if (!each && (to - from) * size <= kGradSmall) {
-                    const int64_t step = kGradPiece / size;
-                    const int pieces = (int)((to - from + step - 1) / step);
-                    for (int j = (wid - little) & (kGradWarps - 1); j < pieces; j += kGradWarps)
-                        all += squares<32>(type, p + (int64_t)j * kGradPiece, min(step, to - from - j * step), lane);
-                    little += pieces;
-                } else if (each && (to - from) * size <= kGradUnit) {
-                    if (((little++ - wid) & (kGradWarps - 1)) != 0) continue;
-                    double v = squares<32>(type, p, to - from, lane);
-                    all += v;
-                    v = warp_sum(v);
+                // a small span is cut into pieces, a warp each
+                const int64_t bytes = (to - from) * size, step = kGradPiece / size;
+                const int pieces = bytes <= kGradSmall ? (int)((bytes + kGradPiece - 1) / kGradPiece) : 0;
+                const int at = (wid - little) & (kGradWarps - 1);      // this warp's first
+                little += pieces;
+                if (pieces == 1 && at > 0) continue;
+                double v = 0.0;
+                for (int j = at; j < pieces; j += kGradWarps)
+                    v += squares<32>(type, p + (int64_t)j * kGradPiece, min(step, to - from - j * step), lane);
+                if (pieces == 0) v = squares<kGradThreads>(type, p, to - from, tid);
+                all += v;
+                if (!each) continue;
+                v = warp_sum(v);
+                if (pieces == 1) {
                     if (lane == 0) c.span_sums[i + b] = v;
-                } else {
-                    double v = squares<kGradThreads>(type, p, to - from, tid);
-                    all += v;
-                    if (each) {
-                        v = warp_sum(v);
-                        if (lane == 0) part[parts][wid] = v;
-                        if (tid == 0) part_of[parts] = i;
-                        if (++parts == kGradParts) {
-                            join_parts();
-                            __syncthreads();
-                        }
-                    }
+                    continue;
+                }
+                if (lane == 0) part[parts][wid] = v;
+                if (tid == 0) part_of[parts] = i;
+                if (++parts == kGradParts) {
+                    join_parts();
+                    __syncthreads();
                 }
             }
         if (each) join_parts();
