@@ -147,7 +147,7 @@ struct LpShared {
     float tau;
     // what the other CTAs of a row read
     Sums part;
-    int part_above, part_count;
+    int part_above;
 };
 __device__ __forceinline__ uint64_t lp_entry(float v, int64_t i) { return (uint64_t)order_key(v) << 32 | (uint32_t)~(uint32_t)i; }
 
@@ -277,22 +277,27 @@ __device__ __noinline__ void lp_fill(LpShared<NT>& sh, const char* row, int64_t 
     __syncthreads();
 }
 
+// Sums joined with those of the lane that is o across.
+__device__ __forceinline__ void lp_join_across(Sums& a, int o, float zscale) {
+    Sums b;
+    b.m = __shfl_xor_sync(0xffffffffu, a.m, o);
+    b.s0 = __shfl_xor_sync(0xffffffffu, a.s0, o);
+    b.s1 = __shfl_xor_sync(0xffffffffu, a.s1, o);
+    lp_join(a, b, zscale);
+}
+// (a join's last bit depends on which comes first: all take the first lane's)
+__device__ __forceinline__ void lp_first_lanes(Sums& a) {
+    a.m = __shfl_sync(0xffffffffu, a.m, 0);
+    a.s0 = __shfl_sync(0xffffffffu, a.s0, 0);
+    a.s1 = __shfl_sync(0xffffffffu, a.s1, 0);
+}
 // W warps' sums, those of a warp's threads relative to the same maximum, joined in one order.
 template <int W>
 __device__ __forceinline__ Sums lp_join_warps(const Sums (&part)[8], float zscale) {
     Sums a = part[threadIdx.x & (W - 1)];
 #pragma unroll
-    for (int o = W / 2; o > 0; o >>= 1) {
-        Sums b;
-        b.m = __shfl_xor_sync(0xffffffffu, a.m, o);
-        b.s0 = __shfl_xor_sync(0xffffffffu, a.s0, o);
-        b.s1 = __shfl_xor_sync(0xffffffffu, a.s1, o);
-        lp_join(a, b, zscale);
-    }
-    // (a join's last bit depends on which comes first: all take the first lane's)
-    a.m = __shfl_sync(0xffffffffu, a.m, 0);
-    a.s0 = __shfl_sync(0xffffffffu, a.s0, 0);
-    a.s1 = __shfl_sync(0xffffffffu, a.s1, 0);
+    for (int o = W / 2; o > 0; o >>= 1) lp_join_across(a, o, zscale);
+    lp_first_lanes(a);
     return a;
 }
 __device__ __forceinline__ void lp_join_lanes(Sums& a) {
@@ -349,7 +354,8 @@ struct LpResult {
 // alone, without exponentials and rank, 190), bounded by issue: nine instructions a logit.  Two words a take 264, three
 // fetches of four 244; rows through rings in shared memory 231 to 300.  With alternatives a row's own work shows, some
 // 1000 instructions a warp: k = 20 256 us, k = 100 335; 2000 x 50001 fp16 with k = 20 69.  Few rows are a chain of
-// latencies: 1 x 50001 fp32 11 us.
+// latencies: 1 x 50001 fp32, k = 20, 9 us (11 where each CTA joined the others' sums and alternatives one part after the
+// other), k = 0 5.4.
 template <int TYPE, int NT, bool SPLIT, bool LISTS>
 __global__ void __launch_bounds__(NT, SPLIT ? 2 : LpShared<NT>::kCtas) k_vocab_logprob(const LogprobCall c) {
     using Shared = LpShared<NT>;
@@ -633,21 +639,22 @@ __global__ void __launch_bounds__(NT, SPLIT ? 2 : LpShared<NT>::kCtas) k_vocab_l
         }
     };
     if constexpr (SPLIT) {
-        if constexpr (LISTS) place_all([&](int place, uint64_t e) { sh.best[place] = e; });
+        if constexpr (LISTS) {
+            if (tid >= k && tid < c.k) sh.best[tid] = 0;      // below all
+            place_all([&](int place, uint64_t e) { sh.best[place] = e; });
+        }
         if (tid == 0) {
             sh.part = a;
             sh.part_above = rank;
-            sh.part_count = k;
         }
         lp_cluster_barrier();
-        // every CTA joins all parts' sums in one order
-        auto part_of = [&](int p) { return Sums{remote(sh.part.m, p), remote(sh.part.s0, p), remote(sh.part.s1, p)}; };
-        a = part_of(0);
-        rank = remote(sh.part_above, 0);
-        for (int p = 1; p < parts; ++p) {
-            lp_join(a, part_of(p), zscale);
-            rank += remote(sh.part_above, p);
-        }
+        // every warp joins all parts' sums, a lane each, in one order
+        const int p = lane & (parts - 1);
+        a = Sums{remote(sh.part.m, p), remote(sh.part.s0, p), remote(sh.part.s1, p)};
+        rank = remote(sh.part_above, p);
+        rank = (int)__reduce_add_sync(0xffffffffu, lane < parts ? (unsigned)rank : 0u);
+        for (int o = parts / 2; o > 0; o >>= 1) lp_join_across(a, o, zscale);
+        lp_first_lanes(a);
     }
     const LpResult result(c, a);
     if (part == 0) {
@@ -669,25 +676,20 @@ __global__ void __launch_bounds__(NT, SPLIT ? 2 : LpShared<NT>::kCtas) k_vocab_l
     if constexpr (!SPLIT) {
         if constexpr (LISTS) place_all(write);
     } else {
-        // all parts' alternatives beside one another, and how many of each part are above each of this CTA's
+        // all parts' alternatives beside one another, and how many of each part are above each of this CTA's: a thread a part
         uint64_t* all = reinterpret_cast<uint64_t*>(sh.data);
-        for (int j = tid; j < parts * c.k; j += NT) {
-            const int p = j / c.k, i = j - p * c.k;
-            all[j] = i < remote(sh.part_count, p) ? remote(sh.best[i], p) : 0;
-        }
+        for (int j = tid; j < parts * c.k; j += NT) all[j] = remote(sh.best[j / parts], j & (parts - 1));
         __syncthreads();
-        if (tid < k) {
-            const uint64_t e = all[part * c.k + tid];
-            int place = 0;
-            for (int p = 0; p < parts; ++p) {
-                int lo = 0, hi = c.k;      // entries that fill up a list are zero, below all
-                while (lo < hi) {
-                    const int mid = (lo + hi) >> 1;
-                    if (all[p * c.k + mid] > e) lo = mid + 1; else hi = mid;
-                }
-                place += lo;
+        for (int j0 = 0; LISTS && j0 < parts * k; j0 += NT) {
+            const int i = min((j0 + tid) / parts, k - 1), p = tid & (parts - 1);
+            const uint64_t e = all[i * parts + part];
+            int lo = 0, hi = c.k;
+            while (lo < hi) {
+                const int mid = (lo + hi) >> 1;
+                if (all[mid * parts + p] > e) lo = mid + 1; else hi = mid;
             }
-            if (place < c.k) write(place, e);
+            for (int o = parts / 2; o > 0; o >>= 1) lo += __shfl_xor_sync(0xffffffffu, lo, o);
+            if (p == 0 && j0 + tid < parts * k && lo < c.k) write(lo, e);
         }
         lp_cluster_barrier();      // the others have read what is here
     }
@@ -696,8 +698,8 @@ __global__ void __launch_bounds__(NT, SPLIT ? 2 : LpShared<NT>::kCtas) k_vocab_l
 template <int TYPE, bool LISTS>
 static cudaError_t launch_logprob(LogprobCall& c, int sms, cudaStream_t st) {
     const int64_t words = c.V / (TYPE == GK_TYPE_F32 ? 4 : 8);
-    // CTAs a row: as many as there is room for, while each still has four words for every thread (64 rows of 32000 bf16,
-    // 2 CTAs a row 14.3 us, 4 16.4, 8 28; one row of 50001 fp32, 8 CTAs 16, one 27)
+    // CTAs a row: as many as there is room for (two an SM: 64 rows of 128000 bf16, 4 a row 13 us, 8 22), while each still
+    // has four words for every thread (64 rows of 32000 bf16, 2 a row 9.1, 4 9.8; one row of 50001 fp32, 8 a row 8.6, 4 9.7)
     while (c.parts < kLpParts && c.n * c.parts * 2 <= 2 * sms && words >= 8 * c.parts * 256) c.parts *= 2;
     if (c.parts > 1) {
         cudaLaunchConfig_t cfg = {};
