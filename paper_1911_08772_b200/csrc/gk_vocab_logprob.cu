@@ -25,7 +25,8 @@ constexpr int kLpQuad = 4;          // words a thread fetches together, from fou
 constexpr int kLpParts = 8;         // CTAs a row at most (a cluster)
 constexpr int kLpShort = 1500, kLpMiddle = 6000;      // words of a row that 64 threads take, and 128
 constexpr float kLpSlack = 4.f;     // how far a logit may be above what the sums are relative to, in powers of two
-// Exponents of maxima up to this are kept to a sixteenth and better by one rounding.
+// Exponents of rows' maxima up to this are kept to a sixteenth and better by one rounding; so are those down to twice
+// its negative, the lowest that sums start from.
 constexpr float kLpLargest = 1048576.f;
 
 struct LogprobCall {
@@ -97,9 +98,10 @@ __device__ __forceinline__ float max_of(const uint4 (&x)[kLpQuad]) {
     if constexpr (TYPE == GK_TYPE_F32) return fmaxf(max3(max_of<TYPE>(x[0]), max_of<TYPE>(x[1]), max_of<TYPE>(x[2])), max_of<TYPE>(x[3]));
     else return max_of<TYPE>(max2<TYPE>(max2<TYPE>(x[0], x[1]), max2<TYPE>(x[2], x[3])));
 }
-// What the sums take for anything lower, -inf among it: far enough below any maximum, or the row is taken again.
+// What the sums take for anything lower, -inf among it: far enough below any maximum, or the row is taken again.  (A
+// value of the type: -2^100 for fp32 and bf16.)
 template <int TYPE>
-constexpr float kLpLowest = TYPE == GK_TYPE_F16 ? -65504.f : -1e30f;
+constexpr float kLpLowest = TYPE == GK_TYPE_F16 ? -65504.f : -1267650600228229401496703205376.f;
 
 // Maximum (as it is in the logits) and the two sums relative to it.
 struct Sums {
@@ -452,12 +454,14 @@ __global__ void __launch_bounds__(NT, SPLIT ? 2 : LpShared<NT>::kCtas) k_vocab_l
     }
     // The powers' exponents are z log2(e) / T - ref, one rounding, ref the rounded exponent of about the maximum:
     // it is taken anew where a logit is kLpSlack powers of two above.  What it is off by is put right at the end.
+    // It is never below -2 kLpLargest: of logits further down, as masks are, the rounding of their exponents, or the
+    // bound kLpLowest, would leave any power of two.  So their powers are at most one, and nothing beside the row's.
     const float zscale = c.zscale;
     const uint64_t zscale2 = pair(zscale, zscale);
     float m = top, least_up = top;      // the largest so far, and what raises ref
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) least_up = fmaxf(least_up, __shfl_xor_sync(0xffffffffu, least_up, o));
-    auto ref_of = [&](float v) { return v == -INFINITY ? 0.f : fminf(fmaxf(v * zscale, -1e30f), 1e30f); };
+    auto ref_of = [&](float v) { return v == -INFINITY ? 0.f : fminf(fmaxf(fmaxf(v, kLpLowest<TYPE>) * zscale, -2.f * kLpLargest), 1e30f); };
     float ref = ref_of(least_up);
     bool empty = least_up == -INFINITY;
     least_up += empty ? 0.f : kLpSlack / zscale;
@@ -569,12 +573,14 @@ __global__ void __launch_bounds__(NT, SPLIT ? 2 : LpShared<NT>::kCtas) k_vocab_l
         a.s0 = lo + hi;
         unpair(s1, lo, hi);
         a.s1 = lo + hi;
-        // Relative to the warp's maximum itself, which is at or above what this thread's ref was taken from.  (Where
-        // that is too large for it, the sums are nothing beside the row's, or the row goes through lp_again.)
+        // Relative to the warp's maximum itself, which is at or above what this thread's ref was taken from, and far
+        // above where the thread met masked logits alone: their sums become nothing.  (A maximum that is too large for
+        // this, or lower than ref can be, is that of a row that goes through lp_again, or of a warp that is nothing
+        // beside the row's.)
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
         a.m = m;
-        const float off = fabsf(ref) < kLpLargest && m > -INFINITY ? fminf(fmaxf(fmaf(m, zscale, -ref), -1.f), -kLpFloor) : 0.f;
+        const float off = ref < kLpLargest && m > -INFINITY ? fminf(fmaxf(fmaf(m, zscale, -ref), -1.f), -kLpFloor) : 0.f;
         const float by = exp2_fast(-off);
         a.s1 = fmaf(-off, a.s0, a.s1) * by;
         a.s0 *= by;
