@@ -594,8 +594,9 @@ __global__ void __launch_bounds__(NT, SPLIT ? 2 : LpShared<NT>::kCtas) k_vocab_l
     __syncthreads();
     a = lp_join_warps<kWarps>(sh.sums, zscale);
     rank = (int)__reduce_add_sync(0xffffffffu, lane < kWarps ? (unsigned)sh.above[lane] : 0u);
-    // exponents that fp32 has no digits for, and infinities: differences first
-    if (a.m > -INFINITY && !(fabsf(a.m * zscale) < kLpLargest && (a.m - kLpLowest<TYPE>) * zscale > -kLpFloor))
+    // Exponents that fp32 has no digits for, and infinities: differences first.  So too where s1 alone is NaN: at small
+    // T the exponent of kLpLowest is -inf, its power 0.
+    if ((a.m > -INFINITY && !(fabsf(a.m * zscale) < kLpLargest && (a.m - kLpLowest<TYPE>) * zscale > -kLpFloor)) || (a.s1 != a.s1 && a.s0 == a.s0))
         a = lp_again<TYPE>(sh, row, v0, v1, a.m, zscale);
     // (nothing is next below -inf)
     if (ranked && (a.s0 != a.s0 || first_v == -INFINITY)) rank = lp_rank_again<TYPE>(sh, row, v0, v1, first_v, first);

@@ -1,0 +1,71 @@
+"""gk_vocab_logprob and gk_vocab_logprob_grad at the ends of what they take."""
+import math
+
+import pytest
+import torch
+
+from logprob_util import bounds, close, reference
+from paper_1911_08772_b200 import binding as gk
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _library():
+    from paper_1911_08772_b200 import build
+    build.build()
+    gk.load()
+    yield
+
+
+def run(z, token, T, k=0):
+    n, m = token.shape
+    out = {"logp": torch.empty(n, m, device=DEV), "rank": torch.empty(n, dtype=torch.int32, device=DEV), "entropy": torch.empty(n, device=DEV),
+           "lse": torch.empty(n, device=DEV)}
+    if k:
+        out["idx"], out["val"] = torch.empty(n, k, dtype=torch.int32, device=DEV), torch.empty(n, k, device=DEV)
+    gk.gk_vocab_logprob(z.to(DEV), token.to(DEV), temperature=T, **{name + "_out": x for name, x in out.items()})
+    return out
+
+
+def near_zero(V, T, dtype, gen):
+    """Rows whose largest logit is 0, the others a few T below it or far."""
+    z = -torch.randn(6, V, generator=gen).abs().double() * 4 * T
+    z[:, V // 2] = 0
+    z[0] = 0
+    z[2, torch.rand(V, generator=gen) < 0.5] = -math.inf
+    z[3, 5:V // 2] = torch.finfo(dtype).min
+    z[4, ::3] = -1.0
+    z[5, :V // 2] = -math.inf
+    return z.to(dtype)
+
+
+@pytest.mark.parametrize("T", [1e-7, 1e-9, 1e-20, 1e-30, 1e-37])
+@pytest.mark.parametrize("V", [60, 1003, 8192, 50001])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_entropies_at_the_smallest_temperatures(T, V, dtype):
+    T = float(torch.tensor(T, dtype=F32))
+    gen = torch.Generator().manual_seed(V)
+    z = near_zero(V, T, dtype, gen)
+    token = torch.stack([torch.randint(0, V, (6,), generator=gen), torch.full((6,), V // 2)], 1)
+    out, ref = run(z, token, T, 4), reference(z, token, T, 4)
+    tol = bounds(torch.zeros_like(z), ref, T)
+    assert close(out["lse"], ref["lse"], tol["lse"])
+    assert close(out["entropy"], ref["entropy"], tol["entropy"])
+    assert torch.equal(out["rank"].cpu().long(), ref["rank"]) and torch.equal(out["idx"].cpu().long(), ref["idx"])
+
+
+@pytest.mark.parametrize("T", [1e-7, 1e-20, 1e-36])
+def test_fp16_at_the_smallest_temperatures(T):
+    """Logits that differ are infinitely far apart here, beside 2^-24."""
+    z = torch.full((3, 1003), -2.0, dtype=F16)
+    z[:, 700:704] = 0
+    z[1, :700] = -math.inf
+    z[2, :500] = torch.finfo(F16).min
+    T = float(torch.tensor(T, dtype=F32))
+    token = torch.tensor([[701], [702], [1]])
+    out, ref = run(z, token, T), reference(z, token, T, 0)
+    tol = bounds(torch.zeros_like(z), ref, T)
+    assert close(out["lse"], ref["lse"], tol["lse"]) and close(out["entropy"], ref["entropy"], tol["entropy"])
