@@ -344,8 +344,11 @@ struct LpResult {
     bool nan, inf, none;
     __device__ __forceinline__ LpResult(const LogprobCall& c, const Sums& a)
         : m(a.m), log_s0(logf(a.s0)), inv_T(c.inv_T), inv_T_low(c.inv_T_low), nan(a.s0 != a.s0), inf(a.m == INFINITY), none(a.m == -INFINITY && a.s0 == a.s0) {}
-    // (the second part of 1 / T times an infinity is one of either sign)
-    __device__ __forceinline__ float scaled(float d) const { return fabsf(d) < INFINITY ? fmaf(d, inv_T, d * inv_T_low) : d; }
+    // (where the product leaves fp32's range, one with the second part of 1 / T may too, with either sign)
+    __device__ __forceinline__ float scaled(float d) const {
+        const float product = d * inv_T;
+        return fabsf(product) < INFINITY ? fmaf(d, inv_T, d * inv_T_low) : product;
+    }
     __device__ __forceinline__ float logp(float v) const { return none ? -INFINITY : nan ? NAN : inf ? (v < INFINITY ? -INFINITY : NAN) : scaled(v - m) - log_s0; }
     __device__ __forceinline__ float lse() const { return none ? -INFINITY : nan ? NAN : inf ? INFINITY : scaled(m) + log_s0; }
     __device__ __forceinline__ float entropy(const Sums& a) const { return none ? 0.f : nan || inf ? NAN : log_s0 - 0.69314718f * __fdividef(a.s1, a.s0); }

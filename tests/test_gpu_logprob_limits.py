@@ -4,7 +4,7 @@ import math
 import pytest
 import torch
 
-from logprob_util import bounds, close, reference
+from logprob_util import bounds, close, logp_tol, reference
 from paper_1911_08772_b200 import binding as gk
 
 pytestmark = pytest.mark.gpu
@@ -69,3 +69,24 @@ def test_fp16_at_the_smallest_temperatures(T):
     out, ref = run(z, token, T), reference(z, token, T, 0)
     tol = bounds(torch.zeros_like(z), ref, T)
     assert close(out["lse"], ref["lse"], tol["lse"]) and close(out["entropy"], ref["entropy"], tol["entropy"])
+
+
+@pytest.mark.parametrize("T", [3.3e-8, 1e-9, 1.1e-9, 1.3e-9, 7.7e-10, 3.3e-12])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_log_probabilities_below_the_range_of_fp32(T, dtype):
+    """z / T beyond fp32 is an infinity of the logit's own sign, whatever that of the second part of 1 / T (which is
+    negative but for 1e-9)."""
+    V = 1003
+    t = float(torch.tensor(T, dtype=F32))
+    z = torch.zeros(4, V)
+    z[0, 7:] = torch.finfo(dtype).min
+    z[1, :900] = -1e38
+    z[2] = torch.finfo(dtype).min
+    z[3] = 3e38
+    z = z.to(dtype)
+    token = torch.tensor([[500, 3], [1, 999], [8, 9], [8, 9]])
+    out, ref = run(z, token, t, 9), reference(z, token, t, 9)
+    for name in ("logp", "val", "lse"):
+        want = ref[name].float().double()
+        assert close(out[name], want, logp_tol(want)), (name, t)
+    assert close(out["entropy"], ref["entropy"], bounds(torch.zeros_like(z), ref, t)["entropy"])
