@@ -426,7 +426,8 @@ int gk_vocab_topk(const void* logits, int64_t ld, int32_t dtype, int64_t n, int6
  *   temperature  T > 0 with a finite reciprocal
  *   k          alternatives, 0 <= k <= min(V, 128)
  *   logp_out   DEVICE out  n x m floats; NULL: not wanted (as the next three)
- *   rank_out   DEVICE out  n int32: the rank of the row's first token, -1 where that is left out or m = 0
+ *   rank_out   DEVICE out  n int32: the rank of the row's first token, in the order of idx_out; -1 where that is left
+ *                          out or m = 0
  *   entropy_out, lse_out  DEVICE out  n floats each
  *   idx_out    DEVICE out  n x k int32: the k largest logits' places, the largest first, equal ones in order of
  *                          increasing index (+0 and -0 tie, NaN counts as above +inf)

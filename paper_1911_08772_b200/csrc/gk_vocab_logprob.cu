@@ -601,8 +601,8 @@ __global__ void __launch_bounds__(NT, SPLIT ? 2 : LpShared<NT>::kCtas) k_vocab_l
     // T the exponent of kLpLowest is -inf, its power 0.
     if ((a.m > -INFINITY && !(fabsf(a.m * zscale) < kLpLargest && (a.m - kLpLowest<TYPE>) * zscale > -kLpFloor)) || (a.s1 != a.s1 && a.s0 == a.s0))
         a = lp_again<TYPE>(sh, row, v0, v1, a.m, zscale);
-    // (nothing is next below -inf)
-    if (ranked && (a.s0 != a.s0 || first_v == -INFINITY)) rank = lp_rank_again<TYPE>(sh, row, v0, v1, first_v, first);
+    // (-inf and NaN have no next smaller value; where the token's logit is NaN, only one of a row's CTAs has it in its sums)
+    if (ranked && (a.s0 != a.s0 || first_v == -INFINITY || first_v != first_v)) rank = lp_rank_again<TYPE>(sh, row, v0, v1, first_v, first);
     const int k = SPLIT ? min(c.k, v1 - v0) : c.k;      // of this CTA's elements
     int cnt = 0;
     if constexpr (LISTS) {

@@ -90,3 +90,18 @@ def test_log_probabilities_below_the_range_of_fp32(T, dtype):
         want = ref[name].float().double()
         assert close(out[name], want, logp_tol(want)), (name, t)
     assert close(out["entropy"], ref["entropy"], bounds(torch.zeros_like(z), ref, t)["entropy"])
+
+
+@pytest.mark.parametrize("bits", [-1, 0x7fffffff, 0x7fc00000, -0x400000, 0x7f800001, -0x7fffff])
+@pytest.mark.parametrize("n,V", [(1, 50001), (3, 128000), (2, 700), (300, 8001)])
+def test_the_rank_of_a_token_whose_logit_is_nan(n, V, bits):
+    """NaN counts as above +inf, whatever its bits; equal ones in order of increasing index."""
+    z = torch.randn(n, V, generator=torch.Generator().manual_seed(V)).abs()
+    z[:, 11] = math.inf
+    z.view(torch.int32)[:, V - 9] = bits
+    token = torch.full((n, 1), V - 9)
+    out = run(z, token, 1.0, 2)
+    assert bool((out["rank"] == 0).all()) and bool((out["idx"] == torch.tensor([V - 9, 11], device=DEV)).all())
+    z.view(torch.int32)[:, V // 2] = 0x7fc00000
+    out = run(z, token, 1.0, 2)
+    assert bool((out["rank"] == 1).all()) and bool((out["idx"] == torch.tensor([V // 2, V - 9], device=DEV)).all())
