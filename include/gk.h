@@ -450,8 +450,9 @@ int gk_vocab_topk(const void* logits, int64_t ld, int32_t dtype, int64_t n, int6
  *                          pointer and stride: in place), or memory that shares nothing with them: before or behind
  *                          all of them, or, of the same stride, between their rows
  * A token given twice counts twice.  Rows left out get zeros, and so do rows whose lse is below -1e30: their masks, of
- * -inf or of fp32's or bf16's lowest value, leave nothing.  So do logits of -inf that are no token.  log p is taken from lse
- * and has its rounding, 2^-24 of |lse|.  Rounded once to `dtype`.  No workspace.
+ * -inf or of fp32's or bf16's lowest value, leave nothing.  So do logits of -inf that are no token.  A row that counts
+ * and whose lse is +inf or NaN gets NaN throughout.  log p is taken from lse and has its rounding, 2^-24 of |lse|.
+ * Rounded once to `dtype`.  No workspace.
  */
 int gk_vocab_logprob(const void* logits, int64_t ld, int32_t dtype, int64_t n, int64_t V, const int64_t* token, int32_t m,
                      float temperature, int32_t k, float* logp_out, int32_t* rank_out, float* entropy_out, float* lse_out,

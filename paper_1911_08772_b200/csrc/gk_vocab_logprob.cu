@@ -811,7 +811,7 @@ __global__ void __launch_bounds__(kLgThreads, 4) k_vocab_logprob_grad(const Logp
         }
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        k0 = (k0 - sum - b * entropy) * c.inv_T;
+        k0 = lse < INFINITY ? (k0 - sum - b * entropy) * c.inv_T : NAN;      // a row without a log-sum-exp: NaN throughout
         const float k1 = -b * c.inv_T;
         auto plain = [&](int64_t i) {
             if constexpr (TYPE == GK_TYPE_F32) return ((const float*)row)[i];

@@ -105,3 +105,42 @@ def test_the_rank_of_a_token_whose_logit_is_nan(n, V, bits):
     z.view(torch.int32)[:, V // 2] = 0x7fc00000
     out = run(z, token, 1.0, 2)
     assert bool((out["rank"] == 1).all()) and bool((out["idx"] == torch.tensor([V // 2, V - 9], device=DEV)).all())
+
+
+def layouts(n, V, dtype):
+    """(logits' rows, gradients' rows) as views: alike, at odd places, at other 16-byte boundaries, in place."""
+    def view(pad, shift):
+        return torch.full((n * (V + pad) + shift,), 7.0, dtype=dtype, device=DEV)[shift:].view(n, V + pad)[:, :V]
+    yield view(0, 0), view(0, 0)
+    yield view(5, 3), view(5, 3)
+    yield view(0, 0), view(3, 1)
+    z = view(1, 1)
+    yield z, z
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("given", ["logp", "entropy", "lse", "all"])
+def test_gradients_of_rows_without_a_log_sum_exp_are_nan_throughout(given, dtype):
+    n, V = 4, 1003
+    z = torch.randn(n, V, generator=torch.Generator().manual_seed(2)).to(dtype)
+    z[1, 500], z[2, 3] = math.inf, math.nan
+    z[:, 40:60] = -math.inf
+    z[1:3, V - 1] = -math.inf
+    token = torch.tensor([[1], [2], [3], [4]], device=DEV)
+    ones = torch.ones(n, device=DEV)
+    for view, out in layouts(n, V, dtype):
+        view.copy_(z)
+        lse, entropy = torch.empty(n, device=DEV), torch.empty(n, device=DEV)
+        gk.gk_vocab_logprob(view, token, lse_out=lse, entropy_out=entropy)
+        assert float(lse[1]) == math.inf and math.isnan(float(lse[2]))
+        gk.gk_vocab_logprob_grad(view, token, lse, out, logp_grad=ones[:, None] if given in ("logp", "all") else None,
+                                 entropy=entropy, entropy_grad=ones if given in ("entropy", "all") else None,
+                                 lse_grad=ones if given in ("lse", "all") else None)
+        assert torch.isnan(out).all(1).tolist() == [False, True, True, False]
+        assert torch.isnan(out).any(1).tolist() == [False, True, True, False]
+    # left out, they are zero
+    token[1:3] = -100
+    for view, out in layouts(n, V, dtype):
+        view.copy_(z)
+        gk.gk_vocab_logprob_grad(view, token, lse, out, logp_grad=ones[:, None])
+        assert bool((out[1:3] == 0).all())
