@@ -817,10 +817,9 @@ __global__ void __launch_bounds__(kLgThreads, 4) k_vocab_logprob_grad(const Logp
             if constexpr (TYPE == GK_TYPE_F32) return ((const float*)row)[i];
             else return from16<TYPE == GK_TYPE_F16>(((const uint16_t*)row)[i]);
         };
-        // (a logit of -inf has a finite stand-in, and so has its log probability: both go into products with zero)
+        // (the log probability of -inf has a finite stand-in: it goes into a product with zero)
         auto grad = [&](float z) {
-            z = max_nan(z, kLowest);
-            const float d = max_nan(fmaf(z, c.inv_T_low, fmaf(z, c.inv_T, -lse)), -1e30f);
+            const float d = z == -INFINITY ? -1e30f : max_nan(fmaf(z, c.inv_T_low, fmaf(z, c.inv_T, -lse)), -1e30f);
             return exp2_fast(d * 1.44269504f) * fmaf(k1, d, k0);
         };
         // A token's gradients are added up by the first of the threads that have it.

@@ -4,12 +4,13 @@ import math
 import pytest
 import torch
 
-from logprob_util import bounds, close, logp_tol, reference
+from logprob_util import bounds, close, grad_reference, logp_tol, reference
 from paper_1911_08772_b200 import binding as gk
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
 F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+SMALLEST = {F32: 2.0 ** -126, BF16: 2.0 ** -126, F16: 2.0 ** -25}
 
 
 @pytest.fixture(scope="module", autouse=True)
@@ -144,3 +145,45 @@ def test_gradients_of_rows_without_a_log_sum_exp_are_nan_throughout(given, dtype
         view.copy_(z)
         gk.gk_vocab_logprob_grad(view, token, lse, out, logp_grad=ones[:, None])
         assert bool((out[1:3] == 0).all())
+
+
+EXTREMES = [(1e5, 300.0), (3e37, 1e36)]
+
+
+@pytest.mark.parametrize("T,size", EXTREMES)
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_masked_logits_have_no_gradient(dtype, T, size):
+    """Logits of -inf have no gradient, whatever T and the gradients given: at large T the type's lowest value has a
+    probability."""
+    n, V = 5, 1003
+    gen = torch.Generator().manual_seed(3)
+    z = torch.randn(n, V, generator=gen)
+    if T < 1:
+        # one logit at 8, in the others' words or at the row's end, the rest at 7 and below
+        z = z.clamp(-7, 7)
+        z[torch.arange(n), torch.tensor([0, 5, 500, V - 1, 77])] = 8.0
+    z[:, 100:300] = -math.inf
+    z[:, V - 3:V - 1] = -math.inf
+    z[1:, 1] = -math.inf
+    z = z.to(dtype)
+    token = torch.tensor([[0], [5], [500], [V - 1], [200]])
+    a, b = torch.randn(n, 1, generator=gen) * size, torch.randn(n, generator=gen) * size
+    if dtype == F16 and T < 1:
+        a, b = a * T, b * T      # in fp16's range
+    T = float(torch.tensor(T, dtype=F32))
+    ref = reference(z, token, T, 0)
+    lse, entropy = ref["lse"].float(), ref["entropy"].float()
+    if T < 1:
+        assert torch.equal(lse.double(), ref["lse"])
+    want, tol = grad_reference(z, token, T, lse, entropy, a, b, None)
+    u = torch.finfo(dtype).eps / 2
+    flushed = 2.0 ** -126 * (1 + (a.abs().sum(1) + b.abs() * (entropy + 104)).double() / T)[:, None]
+    gone = (z == -math.inf).to(DEV)
+    gone[torch.arange(n), token[:, 0]] = False
+    for view, out in layouts(n, V, dtype):
+        view.copy_(z)
+        gk.gk_vocab_logprob_grad(view, token.to(DEV), lse.to(DEV), out, logp_grad=a.to(DEV), entropy=entropy.to(DEV), entropy_grad=b.to(DEV),
+                                 temperature=T)
+        assert bool((out[gone] == 0).all()), T
+        fine = (want.abs() < torch.finfo(dtype).max)
+        assert close(torch.where(fine.to(DEV), out, 0.0), torch.where(fine, want, 0.0), tol + u * (want.abs() + tol) + flushed + SMALLEST[dtype]), T
