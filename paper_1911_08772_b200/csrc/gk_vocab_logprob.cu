@@ -817,10 +817,10 @@ __global__ void __launch_bounds__(kLgThreads, 4) k_vocab_logprob_grad(const Logp
             if constexpr (TYPE == GK_TYPE_F32) return ((const float*)row)[i];
             else return from16<TYPE == GK_TYPE_F16>(((const uint16_t*)row)[i]);
         };
-        // (the log probability of -inf has a finite stand-in: it goes into a product with zero)
+        // (zero where the probability is, whatever factor it has: log p is -inf there, or times 1 / T past fp32)
         auto grad = [&](float z) {
-            const float d = z == -INFINITY ? -1e30f : max_nan(fmaf(z, c.inv_T_low, fmaf(z, c.inv_T, -lse)), -1e30f);
-            return exp2_fast(d * 1.44269504f) * fmaf(k1, d, k0);
+            const float d = z == -INFINITY ? z : fmaf(z, c.inv_T_low, fmaf(z, c.inv_T, -lse)), p = exp2_fast(d * 1.44269504f);
+            return p == 0.f && k0 == k0 ? 0.f : p * fmaf(k1, d, k0);
         };
         // A token's gradients are added up by the first of the threads that have it.
         here = here && c.a;
@@ -847,9 +847,10 @@ __global__ void __launch_bounds__(kLgThreads, 4) k_vocab_logprob_grad(const Logp
         } else {
             // One bound takes the place of all logits below it, -inf among them, where their probabilities are zero in fp32
             // and the bound's is too: 200 nats below the log-sum-exp, with room for its own rounding to 16 bits.  Where no
-            // such value exists (fp16 at temperatures of hundreds), element by element.
-            const float bound = fmaxf(fmaf(-fabsf(lse), 0.0078125f, lse - 200.f) / c.inv_T, kLowest);
-            const bool paired = fmaf(bound, c.inv_T, -lse) <= -110.f;
+            // such value exists (fp16 at temperatures of hundreds), or the factor of its probability is past fp32 (twice it:
+            // the rounding), element by element.
+            const float bound = fmaxf(fmaf(-fabsf(lse), 0.0078125f, lse - 200.f) / c.inv_T, kLowest), below = fmaf(bound, c.inv_T, -lse);
+            const bool paired = below <= -110.f && fmaf(fabsf(k1 * below), 2.f, fabsf(k0)) < INFINITY;
             const unsigned bound2 = threshold_of<TYPE>(bound, false);
             const uint64_t hi = pair(c.inv_T, c.inv_T), lo = pair(c.inv_T_low, c.inv_T_low), less = pair(-lse, -lse),
                            log2e = pair(1.44269504f, 1.44269504f), a0 = pair(k0, k0), a1 = pair(k1, k1);

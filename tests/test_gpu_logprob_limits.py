@@ -147,14 +147,14 @@ def test_gradients_of_rows_without_a_log_sum_exp_are_nan_throughout(given, dtype
         assert bool((out[1:3] == 0).all())
 
 
-EXTREMES = [(1e5, 300.0), (3e37, 1e36)]
+EXTREMES = [(1e5, 300.0), (3e37, 1e36), (2.0 ** -30, 1.0), (2.0 ** -66, 2.0 ** -66), (2.0 ** -66, 1.0), (2.0 ** -100, 1.0)]
 
 
 @pytest.mark.parametrize("T,size", EXTREMES)
 @pytest.mark.parametrize("dtype", [F32, BF16, F16])
 def test_masked_logits_have_no_gradient(dtype, T, size):
     """Logits of -inf have no gradient, whatever T and the gradients given: at large T the type's lowest value has a
-    probability."""
+    probability, at small T factors of 1 / T go past fp32 beside a probability of zero."""
     n, V = 5, 1003
     gen = torch.Generator().manual_seed(3)
     z = torch.randn(n, V, generator=gen)
