@@ -513,7 +513,7 @@ int gk_vocab_last_info(gk_stream_t stream, int64_t* host_out);
  * A norm that is not finite as a float clips nothing (c = 1): the caller finds it in norm_out and drops the step.
  * A factor c s below 2^-126 has the absolute steps of fp32 there.  Where
  * nothing is clipped or scaled, tensors in place are not written.  One cooperative kernel (the device must support
- * that); should its bounded barrier run out, norm_out is NaN and no output is complete.
+ * that); should its bounded barrier run out, norm_out is NaN and no output is written.
  */
 int gk_grad_norm(const void* const* grads, const int32_t* types, const int64_t* sizes, int32_t T, float* norm_out,
                  float* norms_out, gk_stream_t stream);

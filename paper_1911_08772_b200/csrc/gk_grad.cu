@@ -291,6 +291,30 @@ __device__ __forceinline__ unsigned count_in(unsigned* counter, unsigned last) {
     return before;
 }
 
+// Arrive at the barrier and wait for all G arrivals; false where a CTA's bounded wait ran out before they were complete.
+// All CTAs get the same answer: one gives up by a mark in the counter, made by compare-and-swap while arrivals are
+// missing, and whoever looks later finds it.
+constexpr unsigned kGradGivenUp = 0x80000000u;
+__device__ __forceinline__ bool all_arrive(unsigned* arrived, unsigned G, int* flag) {
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        __threadfence();
+        atomicAdd(arrived, 1u);
+        const int limit = g_barrier_poll_limit;
+        int polls = 0;
+        unsigned v;
+        while (true) {
+            asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(arrived) : "memory");
+            if (v >= G) break;      // complete, or marked
+            if (++polls <= limit) __nanosleep(40);
+            else if (atomicCAS(arrived, v, v | kGradGivenUp) == v) { v |= kGradGivenUp; break; }      // else one arrived: look again
+        }
+        *flag = v < kGradGivenUp;
+    }
+    __syncthreads();
+    return *flag != 0;
+}
+
 template <bool CLIP, int CAP>
 __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const GradCall c, const __grid_constant__ GradTable<CAP> table) {
     __shared__ double smem[kGradWarps];
@@ -396,16 +420,16 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const GradCall c, cons
         if (c.norm_in) {
             norm = (double)*c.norm_in;
         } else {
-            if (b == 0 && tid == 0) c.ctl->status = GK_DEV_OK;
-            const bool ok = grid_barrier(&c.ctl->arrived, G + c.extra, &flag);
+            const bool ok = all_arrive(&c.ctl->arrived, G + c.extra, &flag);
             if (tid == 0) {
                 // whoever leaves last makes the counters ready for the next call
                 if (atomicInc(&c.ctl->left, G - 1) == G - 1) c.ctl->arrived = 0;
             }
             if (!ok) {
-                if (tid == 0) {
-                    atomicOr(&c.ctl->status, GK_DEV_TIMEOUT);
-                    if (b == 0 && c.norm_out) c.norm_out[0] = NAN;
+                if (b == 0 && tid == 0) {
+                    c.ctl->status = GK_DEV_TIMEOUT;
+                    c.ctl->clipped = 0;
+                    if (c.norm_out) c.norm_out[0] = NAN;
                 }
                 return;
             }
@@ -416,7 +440,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const GradCall c, cons
         const float by = clips ? (float)((double)scale * ((double)c.max_norm / norm)) : scale;
         if (b == 0 && tid == 0) {
             if (c.norm_out) c.norm_out[0] = (float)norm;
-            if (c.norm_in) c.ctl->status = GK_DEV_OK;
+            c.ctl->status = GK_DEV_OK;
             c.ctl->clipped = clips;
         }
         if (u0 >= u1) return;
@@ -548,7 +572,7 @@ static int enqueue_grad(GradCall& c, const void* const* grads, const int32_t* ty
     c.span_sums = c.cta_sums + kGradMaxCtas;
     // (the records before the sums' end by the workspace's own size, which may be for more tensors)
     GradRec* in_ws = reinterpret_cast<GradRec*>(c.span_sums + kGradMaxCtas + (ws->s_cap > kGradMany ? ws->s_cap : kGradMany));
-    c.extra = (unsigned)host_knob(kKnobExtraArrivals);
+    c.extra = host_knob(kKnobExtraArrivals) > 0 ? 1u : 0u;
     unsigned units = 0;
     auto record = [&](GradRec& r, int32_t i) {
         r.src = grads[i];
