@@ -509,7 +509,9 @@ int gk_vocab_last_info(gk_stream_t stream, int64_t* host_out);
  *   scale      DEVICE in   s, one float, as the reciprocal of a loss scale; NULL: 1
  *   norm_in    DEVICE in   the norm, of the scaled gradients, where the caller knows it (over tensors that other
  *                          ranks hold, say); NULL: taken over these tensors
- *   norm_out   DEVICE out  one float, the norm before clipping; NULL: not wanted
+ *   norm_out   DEVICE out  one float, the norm before clipping; NULL: not wanted.  It shares memory with none of the
+ *                          others, but may be norm_in, or scale where norm_in is NULL.  Scale and norm_in share
+ *                          none with an output
  * A norm that is not finite as a float clips nothing (c = 1): the caller finds it in norm_out and drops the step.
  * A factor c s below 2^-126 has the absolute steps of fp32 there.  Where
  * nothing is clipped or scaled, tensors in place are not written.  One cooperative kernel (the device must support

@@ -415,7 +415,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_grad(const GradCall c, cons
             }
         }
     } else {
-        const float scale = c.scale ? *c.scale : 1.f;
+        const float scale = c.scale ? *c.scale : 1.f;      // (read before the barrier: norm_out may be its place)
         double norm;
         if (c.norm_in) {
             norm = (double)*c.norm_in;
@@ -518,19 +518,25 @@ static int check_list(const void* const* grads, const int32_t* types, const int6
     return GK_OK;
 }
 
-// Whether an output shares memory with another output or with an input that is not its own.
+// Whether an output shares memory with another output or with an input that is not its own, the scalars among them.  (A
+// norm may go where it was given, being the same number, or where the scale was, which all CTAs have read when they
+// meet.)
 static bool outputs_overlap(const void* const* grads, const int32_t* types, void* const* outs, const int32_t* out_types,
-                            const int64_t* sizes, int32_t T) {
+                            const int64_t* sizes, int32_t T, const float* scale, const float* norm_in, const float* norm_out) {
     using Range = std::pair<uintptr_t, uintptr_t>;
     std::vector<Range> in, out;
-    in.reserve(T);
-    out.reserve(T);
+    in.reserve(T + 2);
+    out.reserve(T + 1);
     for (int32_t i = 0; i < T; ++i) {
         if (sizes[i] == 0) continue;
         const uintptr_t a = (uintptr_t)grads[i], b = (uintptr_t)outs[i];
         out.emplace_back(b, b + sizes[i] * type_size(out_types[i]));
         if (a != b || types[i] != out_types[i]) in.emplace_back(a, a + sizes[i] * type_size(types[i]));
     }
+    auto one = [](const float* p) { return Range((uintptr_t)p, (uintptr_t)p + sizeof(float)); };
+    if (norm_out) out.push_back(one(norm_out));
+    if (scale && !(scale == norm_out && !norm_in)) in.push_back(one(scale));
+    if (norm_in && norm_in != norm_out) in.push_back(one(norm_in));
     if (!std::is_sorted(out.begin(), out.end())) std::sort(out.begin(), out.end());
     if (!std::is_sorted(in.begin(), in.end())) std::sort(in.begin(), in.end());
     for (size_t i = 1; i < out.size(); ++i)
@@ -649,7 +655,7 @@ extern "C" int gk_grad_clip(const void* const* grads, const int32_t* types, void
         if (sizes[i] > 0 && !outs[i]) return GK_ERR_NULL;
         if ((uintptr_t)outs[i] & (type_size(out_types[i]) - 1)) return GK_ERR_ALIGN;
     }
-    if (outputs_overlap(grads, types, outs, out_types, sizes, T)) return GK_ERR_ALIAS;
+    if (outputs_overlap(grads, types, outs, out_types, sizes, T, scale, norm_in, norm_out)) return GK_ERR_ALIAS;
     GradCall c = {};
     c.T = T;
     c.max_norm = max_norm;

@@ -1,10 +1,10 @@
-"""gk_grad_clip where its bounded wait runs out for some of its CTAs."""
+"""gk_grad_clip where its bounded wait runs out for some of its CTAs, and its scalars' places."""
 import math
 
 import pytest
 import torch
 
-from grad_util import check_clipped, tensors
+from grad_util import NORM_TOL, check_clipped, tensors
 from paper_1911_08772_b200 import binding as gk
 
 pytestmark = pytest.mark.gpu
@@ -48,3 +48,23 @@ def test_all_of_a_grid_or_none_of_it_gives_up():
     gk.gk_grad_clip(grads, 1e-3, norm_out=norm)
     assert gk.gk_grad_last_info() == (0, True)
     check_clipped(before, grads, 1e-3)
+
+
+def test_a_norm_where_a_scalar_was():
+    grads = tensors([300_000, 5000], [F32])
+    before = [g.clone() for g in grads]
+    total = math.sqrt(sum(float(g.double().square().sum()) for g in grads))
+    one = torch.full((1,), 2.0, device=DEV)
+    gk.gk_grad_clip(grads, 1.0, norm_in=one, norm_out=one)
+    assert float(one) == 2.0
+    check_clipped(before, grads, 1.0, norm=2.0)
+    for g, b in zip(grads, before):
+        g.copy_(b)
+    gk.gk_grad_clip(grads, 0.5 * total, scale=one, norm_out=one)
+    assert abs(float(one) - 2 * total) <= 2 * NORM_TOL * total
+    check_clipped(before, grads, 0.5 * total, scale=2.0)
+    with pytest.raises(gk.GkError):
+        gk.gk_grad_clip(grads, 1.0, scale=one, norm_in=torch.ones_like(one), norm_out=one)
+    for kw in ({"scale": grads[1][:1]}, {"norm_in": grads[0][:1]}, {"norm_out": grads[0][7:8]}):
+        with pytest.raises(gk.GkError):
+            gk.gk_grad_clip(grads, 1.0, **kw)
