@@ -51,9 +51,9 @@ typedef enum gk_status {
     GK_ERR_NOMEM = -7,     /* workspace allocation failed */
     GK_ERR_CAPACITY = -8,  /* gk_set_capacity: cap < 0 */
     GK_ERR_LIMIT = -9,     /* size beyond a fixed built-in limit */
-    GK_ERR_TYPE = -10,     /* gk_vocab_*: not one of the element types the call takes */
+    GK_ERR_TYPE = -10,     /* gk_vocab_*, gk_grad_*: not one of the element types the call takes */
     GK_ERR_STRIDE = -11,   /* gk_vocab_*: a row stride shorter than the row */
-    GK_ERR_TEMPERATURE = -12, /* gk_vocab_*: temperature or its reciprocal not positive and finite */
+    GK_ERR_TEMPERATURE = -12, /* gk_vocab_*: temperature or log2(e) over it not positive and finite */
     GK_ERR_NORM = -13      /* gk_grad_clip: max_norm not positive */
 } gk_status;
 

@@ -94,6 +94,12 @@ struct Ctrl {
     unsigned long long dgc[4];
 };
 
+// Whether one of the pointers is off a boundary of `size` bytes, a power of two.  (NULL is not.)
+template <class... P>
+inline bool off_boundary(unsigned size, const P*... p) {
+    return (((uintptr_t)p | ...) & (size - 1)) != 0;
+}
+
 // Held by a call from the lookup to its last launch: calls of two host threads on one stream neither mix
 // their launches over the workspace nor replace it under one another.
 using WorkspaceLock = std::unique_lock<std::mutex>;

@@ -636,6 +636,7 @@ extern "C" int gk_grad_norm(const void* const* grads, const int32_t* types, cons
     const int rc = check_list(grads, types, sizes, T);
     if (rc != GK_OK) return rc;
     if (!norm_out) return GK_ERR_NULL;
+    if (off_boundary(4, norm_out, norms_out)) return GK_ERR_ALIGN;
     GradCall c = {};
     c.T = T;
     c.norm_out = norm_out;
@@ -655,6 +656,7 @@ extern "C" int gk_grad_clip(const void* const* grads, const int32_t* types, void
         if (sizes[i] > 0 && !outs[i]) return GK_ERR_NULL;
         if ((uintptr_t)outs[i] & (type_size(out_types[i]) - 1)) return GK_ERR_ALIGN;
     }
+    if (off_boundary(4, scale, norm_in, norm_out)) return GK_ERR_ALIGN;
     if (outputs_overlap(grads, types, outs, out_types, sizes, T, scale, norm_in, norm_out)) return GK_ERR_ALIAS;
     GradCall c = {};
     c.T = T;

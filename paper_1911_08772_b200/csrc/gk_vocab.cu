@@ -792,6 +792,7 @@ static int check_head(const VocabCall& c, int32_t dtype) {
     if (!c.w || (c.n > 0 && (!c.h || !c.loss || !c.lse))) return GK_ERR_NULL;
     if (c.ldh < c.D || c.ldw < c.D || (c.dh && c.lddh < c.D) || (c.dw && c.lddw < c.D)) return GK_ERR_STRIDE;
     if ((((uintptr_t)c.h | (uintptr_t)c.w | (uintptr_t)c.dh | (uintptr_t)c.dw) & 1) != 0) return GK_ERR_ALIGN;
+    if (off_boundary(8, c.target) || off_boundary(4, c.t_idx, c.t_val, c.t_lse, c.row_grad, c.loss, c.lse)) return GK_ERR_ALIGN;
     const size_t hb = extent(c.n, c.D, c.ldh), wb = extent(c.V, c.D, c.ldw);
     const size_t dhb = c.dh ? extent(c.n, c.D, c.lddh) : 0, dwb = c.dw ? extent(c.V, c.D, c.lddw) : 0;
     if (dhb && (overlap(c.dh, dhb, c.h, hb) || overlap(c.dh, dhb, c.w, wb))) return GK_ERR_ALIAS;

@@ -935,7 +935,7 @@ static int check_rows(const void* logits, int64_t ld, int32_t dtype, int64_t n, 
     if (dtype != GK_TYPE_F32 && dtype != GK_TYPE_BF16 && dtype != GK_TYPE_F16) return GK_ERR_TYPE;
     if (n > 0 && (!logits || (m > 0 && !token))) return GK_ERR_NULL;
     if (ld < V) return GK_ERR_STRIDE;
-    if (((uintptr_t)logits & (dtype == GK_TYPE_F32 ? 3 : 1)) != 0) return GK_ERR_ALIGN;
+    if (off_boundary(dtype == GK_TYPE_F32 ? 4 : 2, logits) || off_boundary(8, token)) return GK_ERR_ALIGN;
     return temperature_ok(T) ? GK_OK : GK_ERR_TEMPERATURE;
 }
 
@@ -946,6 +946,7 @@ extern "C" int gk_vocab_logprob(const void* logits, int64_t ld, int32_t dtype, i
     if (rc != GK_OK) return rc;
     if (k < 0 || k > V || k > kLogprobMaxAlternatives) return GK_ERR_K;
     if (n > 0 && k > 0 && (!idx_out || !val_out)) return GK_ERR_NULL;
+    if (off_boundary(4, logp_out, rank_out, entropy_out, lse_out, idx_out, val_out)) return GK_ERR_ALIGN;
     if (n == 0) return GK_OK;
     const double inv_T = 1.0 / (double)temperature;
     LogprobCall c = {(const char*)logits, ld, n, V, token, m, k, 1, (float)inv_T, (float)(inv_T - (double)(float)inv_T), (float)(1.4426950408889634 * inv_T),
@@ -974,7 +975,7 @@ extern "C" int gk_vocab_logprob_grad(const void* logits, int64_t ld, int32_t dty
     if (n > 0 && (!lse || !dlogits || (entropy_grad && !entropy))) return GK_ERR_NULL;
     if (lddz < V) return GK_ERR_STRIDE;
     const int64_t size = dtype == GK_TYPE_F32 ? 4 : 2;
-    if (((uintptr_t)dlogits & (size - 1)) != 0) return GK_ERR_ALIGN;
+    if (off_boundary((unsigned)size, dlogits) || off_boundary(4, lse, entropy, logp_grad, entropy_grad, lse_grad)) return GK_ERR_ALIGN;
     if (n == 0) return GK_OK;
     const uintptr_t z0 = (uintptr_t)logits, z1 = z0 + ((n - 1) * ld + V) * size, d0 = (uintptr_t)dlogits, d1 = d0 + ((n - 1) * lddz + V) * size;
     if (z0 < d1 && d0 < z1 && (z0 != d0 || (ld != lddz && n > 1))) {

@@ -575,7 +575,7 @@ extern "C" int gk_vocab_topk(const void* logits, int64_t ld, int32_t dtype, int6
     if (dtype != GK_TYPE_F32 && dtype != GK_TYPE_BF16 && dtype != GK_TYPE_F16) return GK_ERR_TYPE;
     if (n > 0 && (!logits || !idx_out || !val_out)) return GK_ERR_NULL;
     if (ld < V) return GK_ERR_STRIDE;
-    if (((uintptr_t)logits & (dtype == GK_TYPE_F32 ? 3 : 1)) != 0) return GK_ERR_ALIGN;
+    if (off_boundary(dtype == GK_TYPE_F32 ? 4 : 2, logits) || off_boundary(4, idx_out, val_out, lse_out)) return GK_ERR_ALIGN;
     if (k < 1 || k > V || k > kVocabMaxPairs) return GK_ERR_K;
     if (!temperature_ok(temperature)) return GK_ERR_TEMPERATURE;
     if (n == 0) return GK_OK;
