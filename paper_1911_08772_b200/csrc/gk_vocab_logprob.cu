@@ -624,15 +624,16 @@ __global__ void __launch_bounds__(NT, SPLIT ? 2 : LpShared<NT>::kCtas) k_vocab_l
         cnt = sh.listed;
         const bool listed = !nan && notes <= Shared::kNotes && cnt <= Shared::kList;
         if (listed && cnt < k) lp_fill<TYPE>(sh, row, v0, v1, tau, k, cnt);
-        if (!listed || cnt < k) {
+        const bool walked = !listed || cnt < k;
+        if (walked) {
             // what there is of a list that is too long gives a bound
             uint64_t least = 0;
             cnt = min(cnt, Shared::kList);
             if (!nan && !listed && cnt >= k) least = lp_cut(sh, cnt, k, max(k, Shared::kPlaced / 2), order_key(tau), order_key(a.m));
             lp_walk<TYPE>(sh, row, v0, v1, k, least, cnt);
         }
-        if (cnt > Shared::kPlaced)
-            lp_cut(sh, cnt, k, max(k, Shared::kPlaced / 2), listed ? order_key(tau) : 0u, listed ? order_key(a.m) : ~0u);
+        if (cnt > Shared::kPlaced)      // (a walk's list has NaN, or elements below tau where there were too few above)
+            lp_cut(sh, cnt, k, max(k, Shared::kPlaced / 2), walked ? 0u : order_key(tau), walked ? ~0u : order_key(a.m));
     }
     // the place of each is how many are above it
     auto place_all = [&](auto&& put) {
