@@ -4,7 +4,7 @@ import math
 import pytest
 import torch
 
-from logprob_util import bounds, close, grad_reference, logp_tol, reference
+from logprob_util import U, bounds, close, grad_reference, logp_tol, reference
 from paper_1911_08772_b200 import binding as gk
 
 pytestmark = pytest.mark.gpu
@@ -187,3 +187,27 @@ def test_masked_logits_have_no_gradient(dtype, T, size):
         assert bool((out[gone] == 0).all()), T
         fine = (want.abs() < torch.finfo(dtype).max)
         assert close(torch.where(fine.to(DEV), out, 0.0), torch.where(fine, want, 0.0), tol + u * (want.abs() + tol) + flushed + SMALLEST[dtype]), T
+
+
+@pytest.mark.parametrize("T,size", [(1e31, 3e31), (1e34, 1e34), (1e36, 3e36), (1e38, 1e38), (3e38, 1e38)])
+@pytest.mark.parametrize("n,V", [(160, 700), (5, 8001), (2, 128000), (160, 33000)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_logits_that_are_further_apart_than_fp32_reaches(dtype, n, V, T, size):
+    """A mask of the lowest value under large logits, at temperatures that leave it a finite log probability."""
+    T = float(torch.tensor(T, dtype=F32))
+    gen = torch.Generator().manual_seed(V)
+    z = torch.randn(12, V, generator=gen).clamp(-3, 3) * size
+    z[:4, torch.rand(V, generator=gen) < 0.5] = torch.finfo(dtype).min
+    z[4:8, V // 9:] = torch.finfo(dtype).min
+    z[3] = torch.finfo(dtype).min
+    z[2, V // 2], z[7, 3] = 3.3e38, 3.3e38
+    z = z.to(dtype).repeat(-(-n // 12), 1)[:n] if n > 12 else z[[0, 2, 3, 5, 7]][:n].to(dtype)
+    token = torch.randint(0, V, (n, 2), generator=gen)
+    out, ref = run(z, token, T, 5), reference(z[:12], token[:12], T, 5)
+    # (a difference whose ends are scaled first is rounded two times more, both of numbers below it)
+    first = {name: x[:12] for name, x in out.items()}
+    assert close(first["lse"], ref["lse"], bounds(z[:12], ref, T)["lse"])
+    assert close(first["entropy"], ref["entropy"], bounds(z[:12], ref, T)["entropy"])
+    for name in ("logp", "val"):
+        assert close(first[name], ref[name], logp_tol(ref[name]) + 6 * U * ref[name].abs())
+    assert torch.equal(first["rank"].cpu().long(), ref["rank"]) and torch.equal(first["idx"].cpu().long(), ref["idx"])
