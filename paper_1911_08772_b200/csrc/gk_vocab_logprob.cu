@@ -108,16 +108,13 @@ struct Sums {
     float m, s0, s1;
 };
 __device__ __forceinline__ float lp_ref(float m) { return m == -INFINITY ? 0.f : fminf(m, 3.402823466e38f); }
-// (v - ref) scale.  Where that difference of finite numbers is beyond fp32 (a mask of the lowest value under logits of
-// 1e31 and more), scaled first.
-__device__ __forceinline__ float lp_apart(float v, float ref, float scale) {
-    const float d = v - ref;
-    return fabsf(d) == INFINITY && fabsf(v) < INFINITY ? fmaf(v, scale, -ref * scale) : d * scale;
-}
-// What sums relative to m are multiplied by to be relative to `to` >= m, as a power of two.
-__device__ __forceinline__ float lp_shift(float m, float to, float zscale) {
-    return m == to ? 0.f : m == -INFINITY ? kLpFloor : fmaxf(lp_apart(m, lp_ref(to), zscale), kLpFloor);
-}
+// Half of v - ref: within fp32 where the difference is not (a mask of the lowest value under logits of 1e31 and more).
+__device__ __forceinline__ float lp_half(float v, float ref) { return fmaf(v, 0.5f, -0.5f * ref); }
+// (v - ref) zscale, and kLpFloor at least.
+__device__ __forceinline__ float lp_apart(float v, float ref, float zscale) { return 2.f * max_nan(lp_half(v, ref) * zscale, 0.5f * kLpFloor); }
+// What sums relative to m are multiplied by to be relative to `to` >= m, as a power of two: nothing for +inf beside
+// itself, the floor for -inf, whose sums are nothing.
+__device__ __forceinline__ float lp_shift(float m, float to, float zscale) { return fminf(lp_apart(m, lp_ref(to), zscale), 0.f); }
 __device__ __forceinline__ void lp_join(Sums& a, const Sums& b, float zscale) {
     const float top = fmaxf(a.m, b.m), da = lp_shift(a.m, top, zscale), db = lp_shift(b.m, top, zscale);
     const float ea = exp2_fast(da), eb = exp2_fast(db);      // one where the shift is nothing
@@ -323,7 +320,7 @@ __device__ __noinline__ Sums lp_again(LpShared<NT>& sh, const char* row, int64_t
     const float ref = lp_ref(m);
 #pragma unroll 4
     for (int64_t i = v0 + (int)threadIdx.x; i < v1; i += NT) {
-        const float d = max_nan(lp_apart(load_logit<TYPE>(row, i), ref, zscale), kLpFloor), e = exp2_fast(d);
+        const float d = lp_apart(load_logit<TYPE>(row, i), ref, zscale), e = exp2_fast(d);
         a.s0 += e;
         a.s1 = fmaf(e, d, a.s1);
     }
@@ -355,11 +352,7 @@ struct LpResult {
         const float product = d * inv_T;
         return fabsf(product) < INFINITY ? fmaf(d, inv_T, d * inv_T_low) : product;
     }
-    __device__ __forceinline__ float scaled(float v, float ref) const {
-        const float d = v - ref;
-        return fabsf(d) == INFINITY && fabsf(v) < INFINITY ? lp_apart(v, ref, inv_T) : scaled(d);
-    }
-    __device__ __forceinline__ float logp(float v) const { return none ? -INFINITY : nan ? NAN : inf ? (v < INFINITY ? -INFINITY : NAN) : scaled(v, m) - log_s0; }
+    __device__ __forceinline__ float logp(float v) const { return none ? -INFINITY : nan ? NAN : inf ? (v < INFINITY ? -INFINITY : NAN) : 2.f * scaled(lp_half(v, m)) - log_s0; }
     __device__ __forceinline__ float lse() const { return none ? -INFINITY : nan ? NAN : inf ? INFINITY : scaled(m) + log_s0; }
     __device__ __forceinline__ float entropy(const Sums& a) const { return none ? 0.f : nan || inf ? NAN : log_s0 - 0.69314718f * __fdividef(a.s1, a.s0); }
 };
