@@ -422,7 +422,7 @@ int gk_vocab_topk(const void* logits, int64_t ld, int32_t dtype, int64_t n, int6
  *   n, V       n >= 0, 1 <= V <= 2^31 - 1
  *   token      DEVICE in   n x m int64 (contiguous), 0 <= m <= 128; NULL for m = 0.  A token outside [0, V) is left
  *                          out: logp 0.  A row that was given tokens, all of them left out, is left out itself:
- *                          zeros, rank -1, idx -1, whatever its logits hold, which are not read
+ *                          zeros, rank -1, idx -1, whatever its logits hold
  *   temperature  T > 0 with a finite reciprocal
  *   k          alternatives, 0 <= k <= min(V, 128)
  *   logp_out   DEVICE out  n x m floats; NULL: not wanted (as the next three)
@@ -434,7 +434,8 @@ int gk_vocab_topk(const void* logits, int64_t ld, int32_t dtype, int64_t n, int6
  *   val_out    DEVICE out  n x k floats, their log probabilities.  Both, or k = 0
  * A row of nothing but -inf has lse -inf, entropy 0 and log probabilities -inf; +inf or NaN in a row that counts
  * gives what the formulas give with it: lse +inf, entropy NaN, log probabilities -inf (NaN at +inf); NaN everywhere.
- * One pass over the logits, sums in fp32 relative to the row's maximum; no workspace; the same call gives the same
+ * One pass over the logits (two over rows whose exponents need it, at extreme temperatures or maxima); sums in fp32
+ * relative to the row's maximum, of which powers below 2^-126 are nothing; no workspace; the same call gives the same
  * bits.
  *
  * gk_vocab_logprob_grad -- the gradient with respect to the logits of

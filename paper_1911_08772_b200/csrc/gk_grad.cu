@@ -5,13 +5,14 @@
 // that of each tensor it meets it has one contiguous span.  A long span is the whole CTA's; a short one is cut
 // into pieces of 4 KB, a warp each.  Squares are added in fp32
 // over 32 (fp32) or 64 (16-bit) elements and those sums in fp64; where such a sum says that squares left fp32's
-// range, or is zero, the elements are squared again in fp64.  Sums are joined in a fixed order: threads, warps, CTAs.
+// range, or is zero, the elements are squared again in fp64 (4e8 zeros in bf16: 178 us, random ones 122).  Sums are joined in a fixed order: threads, warps, CTAs.
 // Bounded by memory, with eight words a thread (64 KB an SM) on their way: the norm of 1e9 bf16 in 400 tensors, 2 GB,
 // takes 297 us (a copy's rate; two CTAs an SM with four words, double-buffered, 350), of 25.6 M fp32 in 161 tensors 26.
 //
 // Clipping is one cooperative kernel: squares, a barrier of the grid, and the scaling from the last unit back
 // to the first, which meets in L2 what the squares read last.  4e8 elements of bf16 and fp32 into one fp32 vector: 3.0 GB
-// in 551 us; 25.6 M fp32 in 161 tensors, from L2 the second time, 57; 269722 in 65, 8.6, most of it the barrier.
+// in 551 us; 25.6 M fp32 in 161 tensors, from L2 the second time, 57; 269722 in 65, 8.6, most of it the barrier.  With the
+// norm given, gradients are read once and no CTA waits: 423 us and, with nothing in L2 before, 46 (66 without it).
 #include <algorithm>
 #include <new>
 #include <utility>

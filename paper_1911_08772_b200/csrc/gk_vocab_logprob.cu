@@ -359,9 +359,10 @@ struct LpResult {
 
 // SPLIT: the CTAs of a cluster share a row.  LISTS: with alternatives.
 // A thread keeps two times four words on their way, 64 KB an SM: 4096 x 128000 bf16 in 207 to 222 us (5 TB/s; the stream
-// alone, without exponentials and rank, 190), bounded by issue: nine instructions a logit.  Two words a take 264, three
+// alone, without exponentials and rank, 190).  No unit is full (57 % of the issue slots, at nine instructions a logit, 55 %
+// of the exponentials' unit and of DRAM): waiting bounds it, with 29 warps an SM there.  Two words a take 264, three
 // fetches of four 244; rows through rings in shared memory 231 to 300.  With alternatives a row's own work shows, some
-// 1000 instructions a warp: k = 20 256 us, k = 100 335; 2000 x 50001 fp16 with k = 20 69.  Few rows are a chain of
+// 1000 instructions a warp: k = 20 256 us, k = 100 335; 2000 x 50001 fp16 with k = 20 70.  Few rows are a chain of
 // latencies: 1 x 50001 fp32, k = 20, 9 us (11 where each CTA joined the others' sums and alternatives one part after the
 // other), k = 0 5.4.
 template <int TYPE, int NT, bool SPLIT, bool LISTS>
@@ -756,7 +757,8 @@ constexpr int kLgThreads = 256;
 
 // A CTA a piece of a row (grid: pieces by rows), logits read and gradients written once, four words a thread at a time
 // and four on their way.  Bounded by memory: 4096 x 128000 bf16, 2.1 GB, in 325 us, a copy's rate; with 30 % of the rows
-// left out, which are written only, 299.  700 x 10000 fp32, 56 MB, in 12 us on the GPU; 33 x 1003 fp16 in 3.5.
+// left out, which are written only, 299.  700 x 10000 fp32, 56 MB, in 12 us on the GPU; 33 x 1003 fp16 in 3.5.  Rows of
+// other 16-byte boundaries than their logits' go element by element: 4096 x 128000 bf16 in 1.7 to 1.9 ms.
 //     dz = p (k0 + k1 log p),  k0 = (c - sum a - b entropy) / T,  k1 = -b / T,
 // and a / T more at a token, which the CTA that has it writes again at the end.
 template <int TYPE>
