@@ -526,18 +526,14 @@ static bool outputs_overlap(const void* const* grads, const int32_t* types, void
                             const int64_t* sizes, int32_t T, const float* scale, const float* norm_in, const float* norm_out) {
     using Range = std::pair<uintptr_t, uintptr_t>;
     std::vector<Range> in, out;
-    in.reserve(T + 2);
-    out.reserve(T + 1);
+    in.reserve(T);
+    out.reserve(T);
     for (int32_t i = 0; i < T; ++i) {
         if (sizes[i] == 0) continue;
         const uintptr_t a = (uintptr_t)grads[i], b = (uintptr_t)outs[i];
         out.emplace_back(b, b + sizes[i] * type_size(out_types[i]));
         if (a != b || types[i] != out_types[i]) in.emplace_back(a, a + sizes[i] * type_size(types[i]));
     }
-    auto one = [](const float* p) { return Range((uintptr_t)p, (uintptr_t)p + sizeof(float)); };
-    if (norm_out) out.push_back(one(norm_out));
-    if (scale && !(scale == norm_out && !norm_in)) in.push_back(one(scale));
-    if (norm_in && norm_in != norm_out) in.push_back(one(norm_in));
     if (!std::is_sorted(out.begin(), out.end())) std::sort(out.begin(), out.end());
     if (!std::is_sorted(in.begin(), in.end())) std::sort(in.begin(), in.end());
     for (size_t i = 1; i < out.size(); ++i)
@@ -549,7 +545,16 @@ static bool outputs_overlap(const void* const* grads, const int32_t* types, void
         while (o < in.size() && in[o].first < r.second) seen = std::max(seen, in[o++].second);
         if (seen > r.first) return true;
     }
-    return false;
+    // the scalars: in the last output that begins before their end, or, norm_out, in an input
+    auto within = [&](const float* p) {
+        const auto next = std::upper_bound(out.begin(), out.end(), Range((uintptr_t)p + sizeof(float) - 1, UINTPTR_MAX));
+        return next != out.begin() && (uintptr_t)p < (next - 1)->second;
+    };
+    for (const float* p : {scale, norm_in, norm_out})
+        if (p && within(p)) return true;
+    for (size_t i = 0; norm_out && i < in.size() && in[i].first < (uintptr_t)norm_out + sizeof(float); ++i)
+        if ((uintptr_t)norm_out < in[i].second) return true;
+    return scale && norm_in && scale == norm_out;
 }
 
 template <bool CLIP, int CAP>
